@@ -211,6 +211,91 @@ int dpllm_decode_step(dpllm_model* m, const void* const* xs, void* const* ys, in
 int dpllm_decode_step_parts(dpllm_model* m, const void* const* xs, void* const* ys, int32_t* k_dev,
                             float* e_dev, int parts, void* stream);
 
+/*
+ * Around the linears: what a program does with their outputs when it verifies drafted tokens (a few nodes per sequence,
+ * which the small batches of dpllm_gemv serve; a draft of one token is ordinary decoding).
+ *
+ *   dpllm_rope            rotary positions of queries and keys, and the gradient of that
+ *   dpllm_tree_attention  attention of the drafted tokens over a paged cache and over one another
+ *   dpllm_verify          which drafted tokens stand against the target's probabilities, and the token after them
+ *   dpllm_cache_append    the keys and values of those that stand go into the cache
+ *
+ * These calls need no model.  They enqueue kernels on `stream` and nothing else: nothing is synchronised, allocated or copied, and
+ * all can be captured into a graph.  Lengths, page tables, masks, paths and counts are read on the device when the
+ * kernels run, so replays follow them.  dpllm_call_error() gives the text of the last of them that was refused in the calling thread.
+ *
+ * The drafted tokens of a sequence are its nodes: node 0 is the last token that already stands (it has been fed to the
+ * model together with the drafted ones), every other node has a parent with a lower number.  Node tensors are
+ * [batch][nodes][heads][head_dim]; the last dimension is contiguous and the other strides are free.
+ */
+#define DPLLM_F16 0
+#define DPLLM_BF16 1
+#define DPLLM_F32 2
+#define DPLLM_MAX_NODES 256    /* nodes of a tree                                        */
+#define DPLLM_MAX_HEAD_DIM 1024
+#define DPLLM_MAX_TENSORS 4    /* tensors of one dpllm_rope                              */
+
+/* A device tensor [batch][tokens][heads][head_dim]; strides in elements, of head_dim 1. */
+typedef struct dpllm_heads {
+  void* data;
+  int64_t batch_stride, token_stride, head_stride;
+} dpllm_heads;
+
+/* A paged cache of keys and values: a pool of `pages` pages of `page` tokens each, in every layer.  Token t of sequence b lies in
+ * page table[b * table_stride + t / page] at place t % page; table NULL: sequence b has page b (pages_per_seq is 1).
+ * A page id outside [0, pages), and a token past the sequence's pages_per_seq pages, hold nothing: they are not read, not seen, not written.
+ * k and v have the same strides (elements; head_dim has 1). */
+typedef struct dpllm_cache {
+  void *k, *v;
+  int64_t layer_stride, page_stride, token_stride, head_stride;
+  const int32_t* table;
+  int64_t table_stride;
+  int32_t dtype, layers, pages, page, pages_per_seq, heads, head_dim;
+} dpllm_cache;
+
+/* Text of the last refusal of dpllm_rope_frequencies, dpllm_rope, dpllm_tree_attention, dpllm_verify or dpllm_cache_append in the
+ * calling thread (valid until the next one). */
+const char* dpllm_call_error(void);
+
+/* The angles per position that dpllm_rope takes: freqs[i], i < rotary_dim / 2 (host, radians), and *scale, what the rotated part is
+ * multiplied by.  PLAIN: base^(-2i / rotary_dim).  For contexts `factor` (>= 1) times as long as the `trained` ones: LINEAR divides all by factor; NTK
+ * takes base * factor^(rotary_dim / (rotary_dim - 2)); YARN goes from the plain angle to the linear one over the pairs (by number) that turn `high`
+ * to `low` times over `trained` positions, and *scale = 0.1 ln(factor) + 1; BANDS goes the same way by the turns themselves
+ * (at least `high`: plain, at most `low`: linear) with *scale = 1.  PLAIN, LINEAR and NTK do not use trained, low, high.
+ * Errors: EINVAL, ESHAPE (rotary_dim odd or outside [2, DPLLM_MAX_HEAD_DIM]). */
+#define DPLLM_ROPE_PLAIN 0
+#define DPLLM_ROPE_LINEAR 1
+#define DPLLM_ROPE_NTK 2
+#define DPLLM_ROPE_YARN 3
+#define DPLLM_ROPE_BANDS 4
+int dpllm_rope_frequencies(int rotary_dim, double base, int scaling, double factor, double trained, double low, double high,
+                           double* freqs, float* scale);
+
+/* Rotary positions of up to DPLLM_MAX_TENSORS tensors (the queries and the keys, say) of the same tokens in one launch.  Pair i of a
+ * head, i < rotary_dim / 2, is (i, i + rotary_dim / 2) with DPLLM_ROPE_HALF and (2i, 2i + 1) with DPLLM_ROPE_INTERLEAVED; with
+ * t = position * freqs[i] it becomes scale * (a cos t - b sin t, a sin t + b cos t).  inverse != 0: -t instead, which is the
+ * transpose: from the gradient of the outputs it makes the gradient of the inputs.  Elements from rotary_dim on are copied.  Angles are formed
+ * in 64 bits, products in 32, results rounded once.
+ * x, out: host arrays of `tensors` views with heads[i] heads each; out[i] may be x[i] itself and must not overlap it otherwise.
+ * positions_dev: int32, positions_dev[b * positions_stride + t]; positions_stride 0: the same for every sequence.  freqs_dev: fp64.
+ * dtype: DPLLM_F16, DPLLM_BF16 or DPLLM_F32.  batch or tokens 0: nothing to do.
+ * Errors: EINVAL, ESHAPE, EHIP. */
+#define DPLLM_ROPE_HALF 0
+#define DPLLM_ROPE_INTERLEAVED 1
+int dpllm_rope(const dpllm_heads* x, const dpllm_heads* out, const int* heads, int tensors, int batch, int tokens, int head_dim,
+               int dtype, int rotary_dim, int layout, const double* freqs_dev, float scale, const int32_t* positions_dev,
+               int64_t positions_stride, int inverse, void* stream);
+
+/* Puts keys and values of some nodes behind what the cache holds, for n_layers layers from first_layer on: node path[b][i] of sequence b goes to token
+ * lens[b] + i, i < count[b] (rows of path are path_stride entries apart and hold `nodes`).  path_dev NULL: nodes in their order; count_dev NULL: all nodes.  Entries of path outside [0, nodes), tokens without a
+ * page and sequences with a negative length are left out; counts above nodes are taken as nodes.  lens is not changed (add the counts
+ * behind the call).  k_new, v_new: views of one layer's [batch][nodes][heads][head_dim] with the cache's type, layers k_layer_stride and v_layer_stride
+ * elements apart; they must not overlap the cache.  Slots that two sequences share take either's values.
+ * Errors: EINVAL, ESHAPE, EHIP. */
+int dpllm_cache_append(const dpllm_cache* cache, int first_layer, int n_layers, int batch, int nodes, const int32_t* lens_dev,
+                       const dpllm_heads* k_new, int64_t k_layer_stride, const dpllm_heads* v_new, int64_t v_layer_stride,
+                       const int32_t* path_dev, int64_t path_stride, const int32_t* count_dev, void* stream);
+
 /* Parity aid: writes the canonical k-bit codes of linear `id`, uint8 [out][in], read back
  * from the private device layout, to idx_dev (device).  Errors: EINVAL, ERANGE, ESTATE, EHIP. */
 int dpllm_debug_unpack(dpllm_model* m, int id, int k, uint8_t* idx_dev, void* stream);

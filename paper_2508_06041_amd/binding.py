@@ -17,13 +17,18 @@ DPLLM_MAX_BATCH = 8
 DPLLM_MAX_PAIRS = 8
 DPLLM_MAX_TARGETS = 8
 DPLLM_STEP_SELECT, DPLLM_STEP_GEMV = 1, 2
+DPLLM_F16, DPLLM_BF16, DPLLM_F32 = 0, 1, 2
+DPLLM_MAX_NODES = 256
+DPLLM_ROPE_PLAIN, DPLLM_ROPE_LINEAR, DPLLM_ROPE_NTK, DPLLM_ROPE_YARN, DPLLM_ROPE_BANDS = 0, 1, 2, 3, 4
+DPLLM_ROPE_HALF, DPLLM_ROPE_INTERLEAVED = 0, 1
 
 SYMBOLS = ["dpllm_model_create", "dpllm_model_destroy", "dpllm_last_error", "dpllm_linear_device_bytes",
            "dpllm_workspace_bytes", "dpllm_set_workspace",
            "dpllm_load_linear", "dpllm_set_selector", "dpllm_set_threshold", "dpllm_set_active_pair",
            "dpllm_set_target_entry", "dpllm_set_target", "dpllm_set_selector_input",
            "dpllm_estimate", "dpllm_estimate_noalloc", "dpllm_gemv", "dpllm_decode_step", "dpllm_decode_step_parts", "dpllm_debug_unpack", "dpllm_debug_locate",
-           "dpllm_debug_set_polls", "dpllm_debug_set_one_launch", "dpllm_debug_step_launches", "dpllm_debug_copy", "dpllm_debug_read"]
+           "dpllm_debug_set_polls", "dpllm_debug_set_one_launch", "dpllm_debug_step_launches", "dpllm_debug_copy", "dpllm_debug_read",
+           "dpllm_call_error", "dpllm_rope_frequencies", "dpllm_rope", "dpllm_cache_append"]
 
 
 class DpllmError(RuntimeError):
@@ -32,12 +37,24 @@ class DpllmError(RuntimeError):
         self.code = code
 
 
+class _Heads(C.Structure):
+    """dpllm_heads: a tensor [batch][tokens][heads][head_dim]."""
+    _fields_ = [("data", C.c_void_p), ("batch_stride", C.c_int64), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class _Cache(C.Structure):
+    """dpllm_cache."""
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("layer_stride", C.c_int64), ("page_stride", C.c_int64), ("token_stride", C.c_int64),
+                ("head_stride", C.c_int64), ("table", C.c_void_p), ("table_stride", C.c_int64), ("dtype", C.c_int32), ("layers", C.c_int32),
+                ("pages", C.c_int32), ("page", C.c_int32), ("pages_per_seq", C.c_int32), ("heads", C.c_int32), ("head_dim", C.c_int32)]
+
+
 def _load():
     if not os.path.exists(_LIB_PATH):
         raise ImportError("libdpllm.so is not built: run `python -c 'import __graft_entry__ as g; g.build()'` "
                           "(there is no fallback path)")
     L = C.CDLL(_LIB_PATH)
-    vp, i32, f32, sz = C.c_void_p, C.c_int, C.c_float, C.c_size_t
+    vp, i32, f32, sz, i64, f64, heads, cache = C.c_void_p, C.c_int, C.c_float, C.c_size_t, C.c_int64, C.c_double, C.POINTER(_Heads), C.POINTER(_Cache)
     L.dpllm_model_create.argtypes = [C.POINTER(vp), i32]
     L.dpllm_model_destroy.argtypes = [vp]
     L.dpllm_model_destroy.restype = None
@@ -65,6 +82,11 @@ def _load():
     L.dpllm_debug_step_launches.argtypes = [vp, C.POINTER(i32)]
     L.dpllm_debug_copy.argtypes = [vp, vp, sz, vp]
     L.dpllm_debug_read.argtypes = [vp, sz, vp, vp]
+    L.dpllm_call_error.argtypes = []
+    L.dpllm_call_error.restype = C.c_char_p
+    L.dpllm_rope_frequencies.argtypes = [i32, f64, i32, f64, f64, f64, f64, C.POINTER(f64), C.POINTER(f32)]
+    L.dpllm_rope.argtypes = [heads, heads, C.POINTER(i32), i32, i32, i32, i32, i32, i32, i32, vp, f32, vp, i64, i32, vp]
+    L.dpllm_cache_append.argtypes = [cache, i32, i32, i32, i32, vp, heads, i64, heads, i64, vp, i64, vp, vp]
     return L
 
 
@@ -117,6 +139,112 @@ def dpllm_debug_read(src, sink):
     rc = lib.dpllm_debug_read(_ptr(src), nbytes, _ptr(sink), _stream())
     if rc != 0:
         raise DpllmError(rc, "dpllm_debug_read")
+
+
+def _call(rc):
+    """Raises what a call without a model was refused for."""
+    if rc != 0:
+        raise DpllmError(rc, lib.dpllm_call_error().decode())
+
+
+_DTYPES = {torch.float16: DPLLM_F16, torch.bfloat16: DPLLM_BF16, torch.float32: DPLLM_F32}
+
+
+def _need(ok, what):
+    """Refuses what the library cannot see: types, shapes and devices of tensors."""
+    if not ok:
+        raise DpllmError(DPLLM_EINVAL, what)
+
+
+def _dtype(t, what):
+    _need(t.dtype in _DTYPES and t.is_cuda, what + " has to be a device tensor of float16, bfloat16 or float32")
+    return _DTYPES[t.dtype]
+
+
+def _index(t, shape, what):
+    """The pointer of a contiguous int32 device tensor of this shape (None: not given)."""
+    if t is None:
+        return None
+    _need(t.dtype == torch.int32 and t.is_cuda and tuple(t.shape) == tuple(shape) and t.is_contiguous(),
+          "%s has to be a contiguous int32 device tensor %s" % (what, list(shape)))
+    return t.data_ptr()
+
+
+def _view(t, what):
+    """dpllm_heads of a tensor [batch][tokens][heads][head_dim] (or of one layer of such)."""
+    _need(t.dim() == 4 and t.is_cuda, what + " has to be a device tensor [batch][tokens][heads][head_dim]")
+    b, n, h, d = t.stride()
+    _need(d == 1 or t.shape[3] == 1 or t.numel() == 0, "the last dimension of %s has to be contiguous" % what)
+    return _Heads(t.data_ptr(), b, n, h)
+
+
+def dpllm_rope_frequencies(rotary_dim, base=10000.0, scaling=DPLLM_ROPE_PLAIN, factor=1.0, trained=0, low=1.0, high=32.0):
+    """(angles per position: device, float64 [rotary_dim / 2]; what the rotated part is multiplied by): made once, for dpllm_rope."""
+    f, scale = (C.c_double * max(1, rotary_dim // 2))(), C.c_float(0.0)
+    _call(lib.dpllm_rope_frequencies(rotary_dim, base, scaling, factor, trained, low, high, f, C.byref(scale)))
+    return torch.tensor(list(f), dtype=torch.float64, device="cuda"), scale.value
+
+
+def dpllm_rope(x, positions, freqs, out=None, scale=1.0, layout=DPLLM_ROPE_HALF, inverse=False):
+    """x: a tensor [batch][tokens][heads][head_dim], or a tuple of such that share everything but their heads (queries, keys).  positions: int32
+    [batch][tokens], or [tokens] for all sequences.  out: where the results go (x itself: in place); new tensors unless given."""
+    xs = (x,) if isinstance(x, torch.Tensor) else tuple(x)
+    _need(0 < len(xs) <= 4, "dpllm_rope takes 1 to 4 tensors")
+    first = xs[0]
+    dtype = _dtype(first, "x")
+    outs = tuple(torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in xs) if out is None else (out,) if isinstance(out, torch.Tensor) else tuple(out)
+    _need(len(outs) == len(xs), "out has to hold a tensor for each of x")
+    views = [_view(t, "x") for t in xs]
+    into = [_view(t, "out") for t in outs]
+    b, n, _, d = first.shape
+    for t, o in zip(xs, outs):
+        _need(t.dtype == o.dtype == first.dtype and t.shape == o.shape and t.shape[:2] == (b, n) and t.shape[3] == d,
+              "the tensors of dpllm_rope share type, sequences, tokens and head_dim, and out the shapes of x")
+    _need(freqs.dtype == torch.float64 and freqs.is_cuda and freqs.is_contiguous() and freqs.dim() == 1, "freqs has to be a contiguous float64 device vector")
+    pos = _index(positions, (n,) if positions.dim() == 1 else (b, n), "positions")
+    m = len(xs)
+    _call(lib.dpllm_rope((_Heads * m)(*views), (_Heads * m)(*into), (C.c_int * m)(*[t.shape[2] for t in xs]), m, b, n, d, dtype, 2 * freqs.shape[0],
+                         layout, freqs.data_ptr(), scale, pos, 0 if positions.dim() == 1 else n, 1 if inverse else 0, _stream()))
+    return outs[0] if isinstance(x, torch.Tensor) else outs
+
+
+class Cache:
+    """A paged cache of keys and values: views of the caller's tensors k and v, [layers][pages][page][heads][head_dim] with the same strides (a pool
+    whose pages hold head after head is passed transposed), and the page table, int32 [batch][pages per sequence] on the device.  Without a
+    table sequence b has page b.  The table may change on the device at any time; the object holds the tensors alive."""
+
+    def __init__(self, k, v, table=None):
+        _need(k.dim() == 5 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype and k.is_cuda and v.is_cuda,
+              "k and v have to be device tensors [layers][pages][page][heads][head_dim] of one type, shape and strides")
+        dtype = _dtype(k, "k")
+        _need(k.stride(4) == 1 or k.shape[4] == 1, "the last dimension of k and v has to be contiguous")
+        if table is not None:
+            _need(table.dtype == torch.int32 and table.is_cuda and table.dim() == 2 and (table.stride(1) == 1 or table.shape[1] == 1),
+                  "table has to be an int32 device tensor [batch][pages per sequence]")
+        self.k, self.v, self.table = k, v, table
+        self.layers, self.pages, self.page, self.heads, self.head_dim = k.shape
+        self.pages_per_seq = 1 if table is None else table.shape[1]
+        self.batch = self.pages if table is None else table.shape[0]
+        self.capacity = self.pages_per_seq * self.page
+        self.c = _Cache(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), k.stride(3), _ptr(table), 0 if table is None else table.stride(0),
+                        dtype, self.layers, self.pages, self.page, self.pages_per_seq, self.heads, self.head_dim)
+
+
+def dpllm_cache_append(cache, lens, k_new, v_new, path=None, count=None, layer=0):
+    """k_new, v_new: [batch][nodes][heads][head_dim] for one layer, or [layers][batch]... for as many from `layer` on.  path: int32 [batch][nodes],
+    count: int32 [batch]."""
+    if k_new.dim() == 4:
+        k_new, v_new = k_new.unsqueeze(0), v_new.unsqueeze(0)
+    _need(k_new.dim() == 5 and k_new.shape == v_new.shape and k_new.dtype == v_new.dtype == cache.k.dtype,
+          "k_new and v_new have to be [layers][batch][nodes][heads][head_dim] of the cache's type")
+    layers, b, n, h, d = k_new.shape
+    _need((h, d) == (cache.heads, cache.head_dim) and b <= cache.batch, "k_new and v_new have to fit the cache's heads, head_dim and sequences")
+    _need(layers == 0 or (k_new[0].is_cuda and v_new[0].is_cuda), "k_new and v_new have to be device tensors")
+    if layers == 0:
+        return
+    _call(lib.dpllm_cache_append(C.byref(cache.c), layer, layers, b, n, _index(lens, (b,), "lens"), C.byref(_view(k_new[0], "k_new")), k_new.stride(0),
+                                 C.byref(_view(v_new[0], "v_new")), v_new.stride(0), _index(path, (b, n), "path"), n,
+                                 _index(count, (b,), "count"), _stream()))
 
 
 class Model:

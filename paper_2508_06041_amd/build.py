@@ -8,9 +8,9 @@ import sysconfig
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdpllm.so")
-SOURCES = ["dpllm_api.hip"]
+SOURCES = ["dpllm_api.hip", "token_api.hip", "token_host.hip"]
 CALLS = os.path.join(HERE, "_calls.so")
-FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-Wall", "-Wno-unused-result",
+FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-result",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          # the first kernel arguments arrive in scalar registers with the launch instead of being loaded from memory
          "-mllvm", "-amdgpu-kernarg-preload-count=14"]
@@ -28,17 +28,29 @@ def spilled(report: str) -> list:
 
 
 def build(verbose: bool = False, extra=()) -> str:
-    cmd = ["/opt/rocm/bin/hipcc", *FLAGS, *extra, "-o", LIB] + [os.path.join(CSRC, s) for s in SOURCES]
-    calls = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-Wextra", "-I" + sysconfig.get_paths()["include"], "-o", CALLS,
-             os.path.join(CSRC, "py_calls.cpp")]
-    for c in (calls, cmd + ["-Rpass-analysis=kernel-resource-usage", "-fno-caret-diagnostics"]):
-        if verbose:
-            print(" ".join(c))
-        done = subprocess.run(c, stderr=subprocess.PIPE, text=True)
-        sys.stderr.write("".join(line for line in done.stderr.splitlines(True) if "[-Rpass-analysis" not in line and not line.startswith("In file included")))
-        done.check_returncode()
-    if spilled(done.stderr):
-        raise RuntimeError("vector registers spilled: " + ", ".join(spilled(done.stderr)))
+    """Every source becomes an object of its own, all at once, so that the code of one does not move when another changes."""
+    objects = os.path.join(HERE, "_build")
+    os.makedirs(objects, exist_ok=True)
+    hipcc = "/opt/rocm/bin/hipcc"
+    made = [os.path.join(objects, s.replace(".hip", ".o")) for s in SOURCES]
+    cmds = [["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-Wextra", "-I" + sysconfig.get_paths()["include"], "-o", CALLS,
+             os.path.join(CSRC, "py_calls.cpp")]]
+    cmds += [[hipcc, *FLAGS, *extra, "-Rpass-analysis=kernel-resource-usage", "-fno-caret-diagnostics", "-c", os.path.join(CSRC, s), "-o", o]
+             for s, o in zip(SOURCES, made)]
+    link = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *made]
+    if verbose:
+        print("\n".join(" ".join(c) for c in [*cmds, link]))
+    running = [subprocess.Popen(c, stderr=subprocess.PIPE, text=True) for c in cmds]
+    reports = [p.communicate()[1] for p in running]
+    for report in reports:
+        sys.stderr.write("".join(line for line in report.splitlines(True) if "[-Rpass-analysis" not in line and not line.startswith("In file included")))
+    for p, c in zip(running, cmds):
+        if p.returncode:
+            raise subprocess.CalledProcessError(p.returncode, c)
+    bad = [k for report in reports for k in spilled(report)]
+    if bad:
+        raise RuntimeError("vector registers spilled: " + ", ".join(bad))
+    subprocess.run(link, check=True)
     return LIB
 
 

@@ -1,0 +1,164 @@
+// Host side of the calls around the linears that include/dpllm.h declares: argument checks and launches.  No kernel arithmetic lives here.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "append_kernel.hpp"
+#include "rope_kernel.hpp"
+#include "token_host.hpp"
+
+using namespace dpllm;
+
+namespace {
+
+template <typename T, int E>
+void launch_rope(const RopeArgs& a, bool half, int blocks, size_t lds, hipStream_t stream) {
+  if (half)
+    hipLaunchKernelGGL((rope_kernel<T, E, true>), dim3(blocks), dim3(kRopeThreads), lds, stream, a);
+  else
+    hipLaunchKernelGGL((rope_kernel<T, E, false>), dim3(blocks), dim3(kRopeThreads), lds, stream, a);
+}
+
+}  // namespace
+
+extern "C" {
+
+const char* dpllm_call_error(void) { return call_error(); }
+
+int dpllm_rope_frequencies(int rotary_dim, double base, int scaling, double factor, double trained, double low, double high, double* freqs,
+                           float* scale) {
+  if (!freqs || !scale) return refuse(DPLLM_EINVAL, "dpllm_rope_frequencies: freqs or scale is NULL");
+  if (rotary_dim < 2 || rotary_dim % 2 || rotary_dim > DPLLM_MAX_HEAD_DIM)
+    return refuse(DPLLM_ESHAPE, "dpllm_rope_frequencies: rotary_dim %d is odd or outside [2, %d]", rotary_dim, DPLLM_MAX_HEAD_DIM);
+  if (!(base > 1.0) || std::isinf(base)) return refuse(DPLLM_EINVAL, "dpllm_rope_frequencies: base has to be above 1 and finite");
+  if (scaling < DPLLM_ROPE_PLAIN || scaling > DPLLM_ROPE_BANDS) return refuse(DPLLM_EINVAL, "dpllm_rope_frequencies: unknown scaling %d", scaling);
+  if (scaling != DPLLM_ROPE_PLAIN && (!(factor >= 1.0) || std::isinf(factor)))
+    return refuse(DPLLM_EINVAL, "dpllm_rope_frequencies: factor has to be at least 1 and finite");
+  if (scaling == DPLLM_ROPE_NTK && rotary_dim == 2) return refuse(DPLLM_ESHAPE, "dpllm_rope_frequencies: NTK needs a rotary_dim above 2");
+  if (scaling >= DPLLM_ROPE_YARN && (!(trained > 0.0) || std::isinf(trained) || !(low > 0.0) || !(high > low) || std::isinf(high)))
+    return refuse(DPLLM_EINVAL, "dpllm_rope_frequencies: needs trained > 0 and high > low > 0");
+  const double tau = 6.283185307179586476925;
+  if (scaling == DPLLM_ROPE_NTK) base *= std::pow(factor, rotary_dim / (rotary_dim - 2.0));
+  // the pairs that turn `high` and `low` times over the trained positions, by number; a ramp of no width is given a little
+  const double lo = std::fmax(std::floor(rotary_dim * std::log(trained / (high * tau)) / (2 * std::log(base))), 0.0);
+  double hi = std::fmin(std::ceil(rotary_dim * std::log(trained / (low * tau)) / (2 * std::log(base))), rotary_dim - 1.0);
+  if (!(hi > lo)) hi = lo + 0.001;
+  *scale = scaling == DPLLM_ROPE_YARN ? (float)(0.1 * std::log(factor) + 1.0) : 1.0f;
+  for (int i = 0; i < rotary_dim / 2; ++i) {
+    const double f = std::pow(base, -2.0 * i / rotary_dim);
+    double plain = 1.0;   // how much of the plain angle is left
+    if (scaling == DPLLM_ROPE_LINEAR) plain = 0.0;
+    if (scaling == DPLLM_ROPE_YARN) plain = 1.0 - std::fmin(std::fmax((i - lo) / (hi - lo), 0.0), 1.0);
+    if (scaling == DPLLM_ROPE_BANDS) plain = std::fmin(std::fmax((trained * f / tau - low) / (high - low), 0.0), 1.0);
+    freqs[i] = plain * f + (1.0 - plain) * f / (scaling == DPLLM_ROPE_PLAIN || scaling == DPLLM_ROPE_NTK ? 1.0 : factor);
+  }
+  return DPLLM_OK;
+}
+
+int dpllm_rope(const dpllm_heads* x, const dpllm_heads* out, const int* heads, int tensors, int batch, int tokens, int head_dim, int dtype,
+               int rotary_dim, int layout, const double* freqs_dev, float scale, const int32_t* positions_dev, int64_t positions_stride, int inverse,
+               void* stream) {
+  if (!x || !out || !heads || !freqs_dev || (!positions_dev && batch > 0 && tokens > 0)) return refuse(DPLLM_EINVAL, "dpllm_rope: a pointer is NULL");
+  if (tensors < 1 || tensors > DPLLM_MAX_TENSORS) return refuse(DPLLM_ESHAPE, "dpllm_rope: %d tensors, takes 1 to %d", tensors, DPLLM_MAX_TENSORS);
+  if (dtype < DPLLM_F16 || dtype > DPLLM_F32) return refuse(DPLLM_EINVAL, "dpllm_rope: unknown dtype %d", dtype);
+  if (layout != DPLLM_ROPE_HALF && layout != DPLLM_ROPE_INTERLEAVED) return refuse(DPLLM_EINVAL, "dpllm_rope: unknown layout %d", layout);
+  if (batch < 0 || tokens < 0 || (int64_t)batch * tokens > INT32_MAX) return refuse(DPLLM_ESHAPE, "dpllm_rope: %d sequences of %d tokens", batch, tokens);
+  if (head_dim < 2 || head_dim > DPLLM_MAX_HEAD_DIM || rotary_dim < 2 || rotary_dim % 2 || rotary_dim > head_dim)
+    return refuse(DPLLM_ESHAPE, "dpllm_rope: rotary_dim %d of head_dim %d (even, at least 2, head_dim at most %d)", rotary_dim, head_dim, DPLLM_MAX_HEAD_DIM);
+  const int es = dtype == DPLLM_F32 ? 4 : 2, wide = 16 / es;
+  const bool half = layout == DPLLM_ROPE_HALF;
+  bool vector = rotary_dim % (half ? 2 * wide : wide) == 0 && (head_dim - rotary_dim) % wide == 0, same = true;
+  RopeArgs a{};
+  int64_t all_heads = 0;
+  for (int i = 0; i < tensors; ++i) {
+    if (heads[i] < 1) return refuse(DPLLM_ESHAPE, "dpllm_rope: tensor %d has %d heads", i, heads[i]);
+    if (batch > 0 && tokens > 0 && (!x[i].data || !out[i].data)) return refuse(DPLLM_EINVAL, "dpllm_rope: tensor %d is NULL", i);
+    if (((uintptr_t)x[i].data | (uintptr_t)out[i].data) % es) return refuse(DPLLM_EINVAL, "dpllm_rope: tensor %d is not aligned to its elements", i);
+    all_heads += heads[i];
+    if (all_heads * head_dim > (1 << 24)) return refuse(DPLLM_ESHAPE, "dpllm_rope: %lld heads of %d", (long long)all_heads, head_dim);
+    a.end[i] = (int)all_heads;
+    a.x[i] = view(x[i]);
+    a.out[i] = view(out[i]);
+    vector = vector && pieces(x[i], es) && pieces(out[i], es);
+    same = same && x[i].data == out[i].data;
+  }
+  if (batch == 0 || tokens == 0) return DPLLM_OK;
+  const int e = vector ? wide : 1;
+  a.freqs = freqs_dev;
+  a.positions = positions_dev;
+  a.positions_stride = positions_stride;
+  a.all = (int64_t)batch * tokens;
+  a.tokens = tokens;
+  a.heads = (int)all_heads;
+  a.pairs = rotary_dim / 2;
+  a.rotary = rotary_dim;
+  a.turned = half ? a.pairs / e : a.pairs / (e > 1 ? e / 2 : 1);
+  a.units = a.turned + (same ? 0 : (head_dim - rotary_dim) / e);
+  a.scale = scale;
+  a.inverse = inverse;
+  const int64_t row = (int64_t)a.heads * a.units;
+  a.at_a_time = 1;
+  a.by_tokens = Divide::by(tokens);
+  a.by_units = Divide::by(a.units);
+  a.by_row = Divide::by((uint32_t)row);
+  a.by_pairs = Divide::by(a.pairs);
+  const int64_t blocks = std::min<int64_t>((a.all + a.at_a_time - 1) / a.at_a_time, 1 << 20);
+  const size_t lds = sizeof(float2) * a.at_a_time * a.pairs;
+  const hipStream_t s = (hipStream_t)stream;
+  if (dtype == DPLLM_F16)
+    e > 1 ? launch_rope<half_t, 8>(a, half, (int)blocks, lds, s) : launch_rope<half_t, 1>(a, half, (int)blocks, lds, s);
+  else if (dtype == DPLLM_BF16)
+    e > 1 ? launch_rope<bfloat_t, 8>(a, half, (int)blocks, lds, s) : launch_rope<bfloat_t, 1>(a, half, (int)blocks, lds, s);
+  else
+    e > 1 ? launch_rope<float, 4>(a, half, (int)blocks, lds, s) : launch_rope<float, 1>(a, half, (int)blocks, lds, s);
+  return launched("dpllm_rope");
+}
+
+int dpllm_cache_append(const dpllm_cache* cache, int first_layer, int n_layers, int batch, int nodes, const int32_t* lens_dev, const dpllm_heads* k_new,
+                       int64_t k_layer_stride, const dpllm_heads* v_new, int64_t v_layer_stride, const int32_t* path_dev, int64_t path_stride,
+                       const int32_t* count_dev, void* stream) {
+  const char* who = "dpllm_cache_append";
+  if (int rc = check_cache(who, cache, batch)) return rc;
+  if ((!lens_dev && batch > 0) || !k_new || !v_new) return refuse(DPLLM_EINVAL, "%s: a pointer is NULL", who);
+  if (first_layer < 0 || n_layers < 0 || n_layers > cache->layers - first_layer || n_layers > 65535)
+    return refuse(DPLLM_ERANGE, "%s: layers %d to %lld of %d", who, first_layer, (long long)first_layer + n_layers, cache->layers);
+  if (batch < 0 || nodes < 0 || nodes > (1 << 24)) return refuse(DPLLM_ESHAPE, "%s: %d sequences of %d nodes", who, batch, nodes);
+  const int es = cache->dtype == DPLLM_F32 ? 4 : 2, wide = 16 / es;
+  if (((uintptr_t)k_new->data | (uintptr_t)v_new->data) % es) return refuse(DPLLM_EINVAL, "%s: k_new or v_new is not aligned to its elements", who);
+  if (n_layers == 0 || batch == 0 || nodes == 0) return DPLLM_OK;
+  if (!k_new->data || !v_new->data) return refuse(DPLLM_EINVAL, "%s: k_new or v_new is NULL", who);
+  const bool vector = cache->head_dim % wide == 0 && pieces(*k_new, es) && pieces(*v_new, es) && (k_layer_stride | v_layer_stride) % wide == 0 &&
+                      ((uintptr_t)cache->k | (uintptr_t)cache->v) % 16 == 0 &&
+                      (cache->layer_stride | cache->page_stride | cache->token_stride | cache->head_stride) % wide == 0;
+  const int e = vector ? wide : 1;
+  AppendArgs a{};
+  a.cache = view(*cache, first_layer);
+  a.k = view(*k_new);
+  a.v = view(*v_new);
+  a.k_layer = k_layer_stride;
+  a.v_layer = v_layer_stride;
+  a.lens = lens_dev;
+  a.path = path_dev;
+  a.count = count_dev;
+  a.path_stride = path_stride;
+  a.batch = batch;
+  a.tokens = nodes;
+  a.head_units = cache->head_dim / e;
+  a.units = a.head_units * cache->heads;
+  a.by_units = Divide::by(a.units);
+  a.by_head = Divide::by(a.head_units);
+  a.at_a_time = 16;
+  const dim3 grid(batch, n_layers, (nodes + a.at_a_time - 1) / a.at_a_time);
+  if (grid.z > 65535) return refuse(DPLLM_ESHAPE, "%s: %d nodes", who, nodes);
+  const hipStream_t s = (hipStream_t)stream;
+  if (e > 1)
+    hipLaunchKernelGGL(append_kernel<u32x4>, grid, dim3(kAppendThreads), 0, s, a, e);
+  else if (es == 2)
+    hipLaunchKernelGGL(append_kernel<uint16_t>, grid, dim3(kAppendThreads), 0, s, a, 1);
+  else
+    hipLaunchKernelGGL(append_kernel<uint32_t>, grid, dim3(kAppendThreads), 0, s, a, 1);
+  return launched(who);
+}
+
+}  // extern "C"
