@@ -286,6 +286,24 @@ int dpllm_rope(const dpllm_heads* x, const dpllm_heads* out, const int* heads, i
                int dtype, int rotary_dim, int layout, const double* freqs_dev, float scale, const int32_t* positions_dev,
                int64_t positions_stride, int inverse, void* stream);
 
+/* Attention of the nodes over what the cache holds and over one another: for every node i and query head h of sequence b,
+ * out = softmax_t(scale q . k_t) v over the tokens t < lens[b] of the cache (kv head h / (heads / cache->heads)) and those nodes j whose bit is set in
+ * row i of the mask: bit j % 64 of word mask[b * mask_stride + i * ceil(nodes / 64) + j / 64]; mask_stride 0: one mask for all sequences.  A node sees itself only if
+ * its own bit says so.  mask_dev NULL: the nodes are a chain, i sees j <= i.  k_new and v_new NULL: the cache only.  Nothing that is not seen is
+ * read as a number: infinities and NaN there change nothing.  A row that sees nothing is zero, its lse minus infinity.  lens: negative is 0, and no
+ * more than the sequence's pages hold.  max_len: how long the longest is expected to be; it sets how the work is split, not the result.
+ * q, out: [batch][nodes][heads][head_dim]; k_new, v_new: [batch][nodes][cache->heads][head_dim]; all of the cache's type, DPLLM_F16 or DPLLM_BF16,
+ * 16-byte aligned, strides multiples of 8 elements.  head_dim 64, 96, 128 or 256; heads a multiple of cache->heads; nodes up to DPLLM_MAX_NODES.
+ * lse_dev: float [batch][nodes][heads], the logarithm of the sum of exp(scale q . k_t), or NULL.  Scores, maxima and sums are kept in 32 bits, the weights
+ * are rounded to the type of v for the product with it.  ws_dev: 16-byte aligned, of at least dpllm_tree_attention_workspace_bytes for the same sizes (0:
+ * NULL is accepted), used until the call's kernels have run.  out must not overlap the inputs.  The same call gives the same bits.
+ * Errors: EINVAL, ESHAPE, ERANGE (layer), ESTATE (workspace), EHIP. */
+int dpllm_tree_attention_workspace_bytes(int batch, int nodes, int heads, int kv_heads, int head_dim, int max_len, size_t* bytes);
+int dpllm_tree_attention(const dpllm_cache* cache, int layer, int batch, int nodes, int heads, const int32_t* lens_dev, int max_len,
+                         const dpllm_heads* q, const dpllm_heads* k_new, const dpllm_heads* v_new, const uint64_t* mask_dev,
+                         int64_t mask_stride, float scale, const dpllm_heads* out, float* lse_dev, void* ws_dev, size_t ws_bytes,
+                         void* stream);
+
 /* Puts keys and values of some nodes behind what the cache holds, for n_layers layers from first_layer on: node path[b][i] of sequence b goes to token
  * lens[b] + i, i < count[b] (rows of path are path_stride entries apart and hold `nodes`).  path_dev NULL: nodes in their order; count_dev NULL: all nodes.  Entries of path outside [0, nodes), tokens without a
  * page and sequences with a negative length are left out; counts above nodes are taken as nodes.  lens is not changed (add the counts

@@ -28,7 +28,8 @@ SYMBOLS = ["dpllm_model_create", "dpllm_model_destroy", "dpllm_last_error", "dpl
            "dpllm_set_target_entry", "dpllm_set_target", "dpllm_set_selector_input",
            "dpllm_estimate", "dpllm_estimate_noalloc", "dpllm_gemv", "dpllm_decode_step", "dpllm_decode_step_parts", "dpllm_debug_unpack", "dpllm_debug_locate",
            "dpllm_debug_set_polls", "dpllm_debug_set_one_launch", "dpllm_debug_step_launches", "dpllm_debug_copy", "dpllm_debug_read",
-           "dpllm_call_error", "dpllm_rope_frequencies", "dpllm_rope", "dpllm_cache_append"]
+           "dpllm_call_error", "dpllm_rope_frequencies", "dpllm_rope",
+           "dpllm_tree_attention_workspace_bytes", "dpllm_tree_attention", "dpllm_cache_append"]
 
 
 class DpllmError(RuntimeError):
@@ -86,6 +87,8 @@ def _load():
     L.dpllm_call_error.restype = C.c_char_p
     L.dpllm_rope_frequencies.argtypes = [i32, f64, i32, f64, f64, f64, f64, C.POINTER(f64), C.POINTER(f32)]
     L.dpllm_rope.argtypes = [heads, heads, C.POINTER(i32), i32, i32, i32, i32, i32, i32, i32, vp, f32, vp, i64, i32, vp]
+    L.dpllm_tree_attention_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32, C.POINTER(sz)]
+    L.dpllm_tree_attention.argtypes = [cache, i32, i32, i32, i32, vp, i32, heads, heads, heads, vp, i64, f32, heads, vp, vp, sz, vp]
     L.dpllm_cache_append.argtypes = [cache, i32, i32, i32, i32, vp, heads, i64, heads, i64, vp, i64, vp, vp]
     return L
 
@@ -228,6 +231,44 @@ class Cache:
         self.capacity = self.pages_per_seq * self.page
         self.c = _Cache(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), k.stride(3), _ptr(table), 0 if table is None else table.stride(0),
                         dtype, self.layers, self.pages, self.page, self.pages_per_seq, self.heads, self.head_dim)
+
+
+def dpllm_tree_attention_workspace_bytes(batch, nodes, heads, kv_heads, head_dim, max_len):
+    n = C.c_size_t(0)
+    _call(lib.dpllm_tree_attention_workspace_bytes(batch, nodes, heads, kv_heads, head_dim, max_len, C.byref(n)))
+    return n.value
+
+
+def dpllm_tree_attention(cache, layer, lens, q, k_new=None, v_new=None, mask=None, scale=None, out=None, lse=None, max_len=None, workspace=None):
+    """q: [batch][nodes][heads][head_dim]; k_new, v_new: [batch][nodes][cache.heads][head_dim].  mask: int64 [batch or 1][nodes][ceil(nodes / 64)], bit j of
+    row i: node i sees node j; None: a chain.  scale: 1 / sqrt(head_dim) unless given.  lse: float32 [batch][nodes][heads] to be filled.  max_len: how long
+    the longest context is expected to be (the cache's capacity unless given).  workspace: uint8, allocated for the call unless given."""
+    _need(q.dim() == 4 and q.dtype == cache.k.dtype and q.shape[3] == cache.head_dim, "q has to be [batch][nodes][heads][head_dim] of the cache's type and head_dim")
+    b, n, h, d = q.shape
+    _need(b <= cache.batch, "q has more sequences than the cache")
+    new = (b, n, cache.heads, d)
+    _need((k_new is None) == (v_new is None), "k_new and v_new are given together or not at all")
+    if k_new is not None:
+        _need(k_new.shape == new and v_new.shape == new and k_new.dtype == v_new.dtype == q.dtype,
+              "k_new and v_new have to be [batch][nodes][kv heads][head_dim] of the cache's type")
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _need(out.shape == q.shape and out.dtype == q.dtype, "out has to have the shape and type of q")
+    if mask is not None:
+        _need(mask.dtype == torch.int64 and mask.is_cuda and mask.is_contiguous() and mask.dim() == 3 and mask.shape[0] in (1, b) and
+              mask.shape[1:] == (n, (n + 63) // 64), "mask has to be a contiguous int64 device tensor [batch or 1][nodes][ceil(nodes / 64)]")
+    _need(lse is None or (lse.dtype == torch.float32 and lse.is_cuda and lse.shape == (b, n, h) and lse.is_contiguous()),
+          "lse has to be a contiguous float32 device tensor [batch][nodes][heads]")
+    max_len = cache.capacity if max_len is None else min(max_len, cache.capacity)
+    if workspace is None:
+        need = dpllm_tree_attention_workspace_bytes(b, n, h, cache.heads, d, max_len)
+        workspace = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
+    _call(lib.dpllm_tree_attention(C.byref(cache.c), layer, b, n, h, _index(lens, (b,), "lens"), max_len, C.byref(_view(q, "q")),
+                                   None if k_new is None else C.byref(_view(k_new, "k_new")), None if v_new is None else C.byref(_view(v_new, "v_new")),
+                                   _ptr(mask), 0 if mask is None or mask.shape[0] == 1 else mask.stride(0), d ** -0.5 if scale is None else scale,
+                                   C.byref(_view(out, "out")), _ptr(lse), _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                   _stream()))
+    return out
 
 
 def dpllm_cache_append(cache, lens, k_new, v_new, path=None, count=None, layer=0):

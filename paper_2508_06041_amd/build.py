@@ -8,7 +8,7 @@ import sysconfig
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdpllm.so")
-SOURCES = ["dpllm_api.hip", "token_api.hip", "token_host.hip"]
+SOURCES = ["dpllm_api.hip", "token_api.hip", "attention_api.hip", "token_host.hip"]
 CALLS = os.path.join(HERE, "_calls.so")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-result",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -1,0 +1,128 @@
+// Host side of dpllm_tree_attention: argument checks, how the work is split, launches.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "token_host.hpp"
+#include "tree_attention.hpp"
+
+using namespace dpllm;
+
+namespace {
+
+struct Plan {
+  int rows, mt, row_tiles, splits;
+  int64_t groups;        // workgroups
+  size_t part, bytes;    // bytes of the partial results, and with their maxima and sums
+};
+
+Plan plan_of(int batch, int nodes, int heads, int kv_heads, int head_dim, int64_t max_len, int seen) {
+  Plan p;
+  p.rows = nodes * (heads / kv_heads);
+  p.mt = p.rows > 16 && head_dim < 256 ? 2 : 1;
+  p.row_tiles = (p.rows + 16 * p.mt - 1) / (16 * p.mt);
+  const int64_t lone = (int64_t)batch * kv_heads * p.row_tiles, steps = (max_len + kAttTile - 1) / kAttTile + (seen + kAttTile - 1) / kAttTile;
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(1024 + lone - 1) / std::max<int64_t>(lone, 1), (steps + kAttWaves - 1) / kAttWaves, kAttMaxSplits}));
+  p.groups = lone * p.splits;
+  p.part = p.splits > 1 ? (size_t)p.groups * 16 * p.mt * head_dim * sizeof(float) : 0;
+  p.bytes = p.splits > 1 ? p.part + (size_t)p.groups * 16 * p.mt * sizeof(float2) : 0;
+  return p;
+}
+
+template <typename T, int D>
+void launch(const AttentionArgs& a, const Plan& p, int64_t all_rows, hipStream_t s) {
+  if (p.mt == 1 || D == 256)
+    hipLaunchKernelGGL((tree_attention_kernel<T, D, 1>), dim3((unsigned)p.groups), dim3(kAttWaves * 64), 0, s, a);
+  else if constexpr (D < 256)
+    hipLaunchKernelGGL((tree_attention_kernel<T, D, 2>), dim3((unsigned)p.groups), dim3(kAttWaves * 64), 0, s, a);
+  if (p.splits > 1)
+    hipLaunchKernelGGL((tree_attention_join_kernel<T, D>), dim3((unsigned)((all_rows + 3) / 4)), dim3(256), 0, s, a, 16 * p.mt, all_rows);
+}
+
+template <typename T>
+void launch(int head_dim, const AttentionArgs& a, const Plan& p, int64_t all_rows, hipStream_t s) {
+  if (head_dim == 64) launch<T, 64>(a, p, all_rows, s);
+  if (head_dim == 96) launch<T, 96>(a, p, all_rows, s);
+  if (head_dim == 128) launch<T, 128>(a, p, all_rows, s);
+  if (head_dim == 256) launch<T, 256>(a, p, all_rows, s);
+}
+
+int check_sizes(const char* who, int batch, int nodes, int heads, int kv_heads, int head_dim) {
+  if (batch < 0 || batch > 65536 || nodes < 0 || nodes > DPLLM_MAX_NODES)
+    return refuse(DPLLM_ESHAPE, "%s: %d sequences of %d nodes (at most 65536 of %d)", who, batch, nodes, DPLLM_MAX_NODES);
+  if (heads < 1 || heads > 1024 || kv_heads < 1 || heads % kv_heads) return refuse(DPLLM_ESHAPE, "%s: %d heads over %d", who, heads, kv_heads);
+  if (head_dim != 64 && head_dim != 96 && head_dim != 128 && head_dim != 256) return refuse(DPLLM_ESHAPE, "%s: head_dim %d (64, 96, 128 or 256)", who, head_dim);
+  return DPLLM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int dpllm_tree_attention_workspace_bytes(int batch, int nodes, int heads, int kv_heads, int head_dim, int max_len, size_t* bytes) {
+  const char* who = "dpllm_tree_attention_workspace_bytes";
+  if (!bytes) return refuse(DPLLM_EINVAL, "%s: bytes is NULL", who);
+  if (int rc = check_sizes(who, batch, nodes, heads, kv_heads, head_dim)) return rc;
+  if (max_len < 0) return refuse(DPLLM_ESHAPE, "%s: max_len %d", who, max_len);
+  *bytes = batch == 0 || nodes == 0 ? 0 : plan_of(batch, nodes, heads, kv_heads, head_dim, max_len, nodes).bytes;
+  return DPLLM_OK;
+}
+
+int dpllm_tree_attention(const dpllm_cache* cache, int layer, int batch, int nodes, int heads, const int32_t* lens_dev, int max_len,
+                         const dpllm_heads* q, const dpllm_heads* k_new, const dpllm_heads* v_new, const uint64_t* mask_dev, int64_t mask_stride,
+                         float scale, const dpllm_heads* out, float* lse_dev, void* ws_dev, size_t ws_bytes, void* stream) {
+  const char* who = "dpllm_tree_attention";
+  if (int rc = check_cache(who, cache, batch)) return rc;
+  if (cache->dtype == DPLLM_F32) return refuse(DPLLM_EINVAL, "%s: takes float16 and bfloat16", who);
+  if (int rc = check_sizes(who, batch, nodes, heads, cache->heads, cache->head_dim)) return rc;
+  if (layer < 0 || layer >= cache->layers) return refuse(DPLLM_ERANGE, "%s: layer %d of %d", who, layer, cache->layers);
+  if (max_len < 0) return refuse(DPLLM_ESHAPE, "%s: max_len %d", who, max_len);
+  if ((int64_t)cache->pages_per_seq * cache->page > INT32_MAX - 256) return refuse(DPLLM_ESHAPE, "%s: more than 2^31 - 256 tokens to a sequence", who);
+  if (!std::isfinite(scale)) return refuse(DPLLM_EINVAL, "%s: scale is not finite", who);
+  if (batch == 0 || nodes == 0) return DPLLM_OK;
+  if (!lens_dev || !q || !out || !q->data || !out->data || !k_new != !v_new || (k_new && (!k_new->data || !v_new->data)))
+    return refuse(DPLLM_EINVAL, "%s: a pointer is NULL (k_new and v_new may be, together)", who);
+  if (!pieces(*q, 2) || !pieces(*out, 2) || (k_new && (!pieces(*k_new, 2) || !pieces(*v_new, 2))) || ((uintptr_t)cache->k | (uintptr_t)cache->v) % 16 ||
+      (cache->layer_stride | cache->page_stride | cache->token_stride | cache->head_stride) % 8)
+    return refuse(DPLLM_EINVAL, "%s: tensors have to be aligned to 16 bytes, with strides of whole 8 elements", who);
+  const Plan p = plan_of(batch, nodes, heads, cache->heads, cache->head_dim, std::min<int64_t>(max_len, (int64_t)cache->pages_per_seq * cache->page), nodes);
+  if (p.groups > 0x7fffff) return refuse(DPLLM_ESHAPE, "%s: %lld workgroups", who, (long long)p.groups);
+  if (p.bytes > 0 && (!ws_dev || ws_bytes < p.bytes || (uintptr_t)ws_dev % 16))
+    return refuse(DPLLM_ESTATE, "%s: needs a workspace of %zu bytes, aligned to 16", who, p.bytes);
+  AttentionArgs a{};
+  a.cache = view(*cache, layer);
+  a.q = view(*q);
+  a.out = view(*out);
+  if (k_new) {
+    a.k_new = view(*k_new);
+    a.v_new = view(*v_new);
+  }
+  a.lens = lens_dev;
+  a.mask = mask_dev;
+  a.mask_stride = mask_stride;
+  a.lse = lse_dev;
+  a.part = (float*)ws_dev;
+  a.stats = (float2*)((char*)ws_dev + p.part);
+  a.scale = std::fabs(scale);
+  a.scale_log2 = (float)(std::fabs((double)scale) * 1.44269504088896340736);
+  a.sign = scale < 0 ? 0x80008000u : 0u;
+  a.eights = cache->page % 8 == 0 || cache->pages_per_seq == 1;
+  a.group = heads / cache->heads;
+  a.by_group = Divide::by(a.group);
+  a.nodes = nodes;
+  a.seen_nodes = k_new ? nodes : 0;
+  a.words = (nodes + 63) / 64;
+  a.kv_heads = cache->heads;
+  a.rows = p.rows;
+  a.row_tiles = p.row_tiles;
+  a.splits = p.splits;
+  const int64_t all_rows = (int64_t)batch * cache->heads * p.rows;
+  if (cache->dtype == DPLLM_F16)
+    launch<half_t>(cache->head_dim, a, p, all_rows, (hipStream_t)stream);
+  else
+    launch<bfloat_t>(cache->head_dim, a, p, all_rows, (hipStream_t)stream);
+  return launched(who);
+}
+
+}  // extern "C"

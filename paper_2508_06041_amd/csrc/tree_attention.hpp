@@ -1,0 +1,448 @@
+// Attention of a few drafted tokens (the nodes of a tree) over a paged cache and over one another.
+//
+// For the row (node i, query head h) of a sequence: x_t = scale q . k_t over the tokens t of the cache and those nodes that the
+// mask of i names, out = sum_t exp(x_t - m) v_t / sum_t exp(x_t - m), m the largest x_t; a row that sees nothing is zero.
+#pragma once
+#include "token_common.hpp"
+
+namespace dpllm {
+
+constexpr int kAttWaves = 4;        // wavefronts of a workgroup
+constexpr int kAttTile = 32;        // tokens of a step
+constexpr int kAttMaxSplits = 64;
+
+struct AttentionArgs {
+  CacheView cache;                  // of the layer
+  Heads q, k_new, v_new, out;
+  const int32_t* lens;
+  const uint64_t* mask;             // [nodes][words]; nullptr: a chain
+  int64_t mask_stride;
+  float* lse;
+  float* part;                      // splits > 1: [workgroups][rows of a tile][head_dim], behind them the maxima and sums
+  float2* stats;
+  float scale, scale_log2;          // |scale|, and that / ln 2
+  uint32_t sign;                    // 0x80008000 for a negative scale: the queries change sign
+  Divide by_group;
+  int nodes, seen_nodes, words, kv_heads, group, rows, row_tiles, splits, eights;
+};
+
+template <typename T>
+struct Matrix;
+template <>
+struct Matrix<half_t> {
+  static constexpr uint32_t kNoNumber = 0x7c00u;   // the exponent of infinities and NaN
+  // weights reach the matrix pipe as 2^12 times what they are: with the slack of a row's top at most 2^15, and rounded to multiples of
+  // 2^-24, as a half below 2^-14 is, only where they are below 2^-26 of the top's
+  static constexpr float kLift = 12.f, kSlack = 3.f;
+  typedef half_t v8 __attribute__((ext_vector_type(8)));
+  static __device__ __forceinline__ f32x4 mad(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
+  }
+};
+template <>
+struct Matrix<bfloat_t> {
+  static constexpr uint32_t kNoNumber = 0x7f80u;
+  static constexpr float kLift = 0.f, kSlack = 8.f;      // the range of a float
+  typedef bfloat_t v8 __attribute__((ext_vector_type(8)));
+  static __device__ __forceinline__ f32x4 mad(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  typedef T two __attribute__((ext_vector_type(2)));
+  two v;
+  v[0] = (T)a;
+  v[1] = (T)b;
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+// Both halves of a word, those that are no finite numbers as 0.
+template <typename T>
+__device__ __forceinline__ uint32_t numbers(uint32_t w) {
+  constexpr uint32_t e = Matrix<T>::kNoNumber;
+  return ((w & e) == e ? 0u : w & 0xffffu) | ((w & (e << 16)) == (e << 16) ? 0u : w & 0xffff0000u);
+}
+
+// D elements of a token are 16 lanes of D / 16 elements: N words of each
+template <int N>
+struct Words {
+  uint32_t w[N];
+};
+template <int N>
+using WordsAtOnce = uint32_t __attribute__((ext_vector_type(N % 4 == 0 ? 4 : N % 2 == 0 ? 2 : 1)));
+template <int N>
+__device__ __forceinline__ Words<N> load_words(const char* p) {
+  typedef WordsAtOnce<N> some;
+  constexpr int A = sizeof(some) / 4;
+  Words<N> r;
+#pragma unroll
+  for (int i = 0; i < N / A; ++i) {
+    const some s = reinterpret_cast<const some*>(p)[i];
+#pragma unroll
+    for (int j = 0; j < A; ++j) r.w[i * A + j] = s[j];
+  }
+  return r;
+}
+template <int N>
+__device__ __forceinline__ void store_words(char* p, const uint32_t (&w)[N]) {
+  typedef WordsAtOnce<N> some;
+  constexpr int A = sizeof(some) / 4;
+#pragma unroll
+  for (int i = 0; i < N / A; ++i) {
+    some s;
+#pragma unroll
+    for (int j = 0; j < A; ++j) s[j] = w[i * A + j];
+    reinterpret_cast<some*>(p)[i] = s;
+  }
+}
+
+// The logarithm of the sum of exp(scale x) over a row whose weights relative to the score m add up to s.
+template <typename T>
+__device__ __forceinline__ float log_sum(float m, float s, float scale) {
+  return m == -INFINITY ? m : m * scale + (__builtin_amdgcn_logf(s) - Matrix<T>::kLift) * 0.69314718055994530942f;
+}
+
+// The largest value of the four lanes of a row (16 lanes apart).
+__device__ __forceinline__ float row_max(float x) {
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  const uint32_t w = __float_as_uint(x);
+  const u32x2 p = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(w, w, false, false));
+  const uint32_t v = __float_as_uint(fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1])));
+  const u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(v, v, false, false));
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// What a wavefront has of its rows: the weighted values, the weights' sum, and the score `top` they are relative to: a weight is
+// 2^((x - top) scale + lift).
+template <int MT, int DV>
+struct Rows {
+  f32x4 o[MT][DV];
+  float sum[MT], top[MT];      // sum: of the lane's own tokens
+};
+
+// One step of 32 tokens for 16 * MT rows.  Everything stays in registers: the lanes of the score product K Q^T (16 x 16 x 32
+// matrix instructions; lane l holds row l % 16 of Q and, of a result, the tokens 4 (l / 16) ... + 3) are those that the value product
+// V^T P^T wants its weights in, if the first 16 tokens of a step are numbered 8 (m / 4) + m % 4 and the second 16 four more: lane
+// group l / 16 then holds the weights of the tokens 8 (l / 16) ... + 7.  V is loaded as it lies, D / 16 elements of 8 tokens to a lane, and turned
+// inside the lane, 16 bits at a time.
+// `top` follows the largest score only when that has left it behind by 2^kSlack: in most steps no row's has, and the exchange between
+// lanes and the scaling of o are skipped.
+template <typename T, int D, int MT>
+__device__ __forceinline__ void attend_step(Rows<MT, D / 16>& r, const u32x4 (&q)[MT][D / 32], const u32x4 (&k)[2][D / 32], float scale_log2, bool all,
+                                            const uint32_t (&seen)[MT], u32x4 (&w)[MT]) {
+  constexpr int KK = D / 32, DV = D / 16;
+  constexpr float kLift = Matrix<T>::kLift, kSlack = Matrix<T>::kSlack;
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    f32x4 s0 = {0, 0, 0, 0}, s1 = {0, 0, 0, 0};
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      s0 = Matrix<T>::mad(k[0][kk], q[mt][kk], s0);
+      s1 = Matrix<T>::mad(k[1][kk], q[mt][kk], s1);
+    }
+    if (!all) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s0[i] = (seen[mt] >> i) & 1 ? s0[i] : -INFINITY;
+        s1[i] = (seen[mt] >> (4 + i)) & 1 ? s1[i] : -INFINITY;
+      }
+    }
+    float most = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
+    if (__any((most - r.top[mt]) * scale_log2 > kSlack)) {      // (top is -infinity at first, and no score at all is no reason: NaN > is false)
+      const float next = fmaxf(r.top[mt], row_max(most));
+      const float less = r.top[mt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((r.top[mt] - next) * scale_log2);
+      r.top[mt] = next;
+      r.sum[mt] *= less;
+#pragma unroll
+      for (int j = 0; j < DV; ++j) r.o[mt][j] *= less;
+    }
+    const float top = r.top[mt] == -INFINITY ? 0.f : r.top[mt], from = kLift - top * scale_log2;
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf(i < 4 ? s0[i & 3] : s1[i & 3], scale_log2, from);
+    if (__any(__builtin_fabsf(top) > 1e38f)) {      // top * scale / ln 2 may be past the floats though the scores are not
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = ((i < 4 ? s0[i & 3] : s1[i & 3]) - top) * scale_log2 + kLift;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_exp2f(x[i]);
+    r.sum[mt] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[mt][i] = pack2<T>(x[2 * i], x[2 * i + 1]);
+  }
+}
+
+template <typename T, int D, int MT>
+__device__ __forceinline__ void add_values(Rows<MT, D / 16>& r, const Words<D / 32> (&v)[8], const u32x4 (&w)[MT]) {
+#pragma unroll
+  for (int j = 0; j < D / 16; ++j) {
+    u32x4 t;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t[i] = __builtin_amdgcn_perm(v[2 * i + 1].w[j / 2], v[2 * i].w[j / 2], j & 1 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) r.o[mt][j] = Matrix<T>::mad(t, w[mt], r.o[mt][j]);
+  }
+}
+
+// One workgroup: up to 16 * MT rows (node, query head of one kv head) of one sequence over one of `splits` parts of its tokens; its wavefronts take
+// steps of 32 tokens in turns and meet at the end.  The weights are rounded to the type of V for the value product (their sum is not): half a step
+// of each, so the error is a mean of independent roundings, below the one rounding of the result.
+template <typename T, int D, int MT>
+__global__ void __launch_bounds__(kAttWaves * 64, D <= 128 ? 2 : 1) tree_attention_kernel(const AttentionArgs a) {
+  constexpr int KK = D / 32, DV = D / 16, N = DV / 2, R = 16 * MT;
+  __shared__ float sums[kAttWaves][4 * DV * MT][64];
+  __shared__ float2 tops[kAttWaves][MT][16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
+  uint32_t id = blockIdx.x;
+  const int split = id % a.splits;
+  id /= a.splits;
+  const int row_tile = id % a.row_tiles;
+  id /= a.row_tiles;
+  const int h = id % a.kv_heads, b = id / a.kv_heads;
+  const int len = min(max(a.lens[b], 0), a.cache.pages_per_seq * a.cache.page);
+  const int old_steps = (len + kAttTile - 1) / kAttTile, steps = old_steps + (a.seen_nodes + kAttTile - 1) / kAttTile;
+  const int each = (steps + a.splits - 1) / a.splits;
+  const int first = split * each, last = min(first + each, steps);
+
+  u32x4 q[MT][KK];
+  int node[MT];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const int r = row_tile * R + mt * 16 + n;
+    node[mt] = -1;
+    if (r < a.rows) {
+      node[mt] = a.by_group.of(r);
+      const char* p = a.q.data + 2 * (b * a.q.batch_stride + node[mt] * a.q.token_stride + (h * a.group + r - node[mt] * a.group) * a.q.head_stride + 8 * g);
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) q[mt][kk] = *reinterpret_cast<const u32x4*>(p + 64 * kk) ^ a.sign;
+    } else {
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) q[mt][kk] = u32x4{0, 0, 0, 0};
+    }
+  }
+  Rows<MT, DV> rows;
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    rows.top[mt] = -INFINITY;
+    rows.sum[mt] = 0.f;
+#pragma unroll
+    for (int j = 0; j < DV; ++j) rows.o[mt][j] = f32x4{0, 0, 0, 0};
+  }
+  const int k_token = 8 * (n >> 2) + (n & 3);      // of the first 16; the second are 4 further
+  const char *cache_k = a.cache.k + 2 * h * a.cache.head_stride, *cache_v = a.cache.v + 2 * h * a.cache.head_stride;
+
+  // The page ids of a step's tokens, asked for a step ahead: of the 8 tokens that this lane's row of K belongs to, and of the 8 whose V it loads.
+  const int full_steps = a.eights ? min(last, len / kAttTile) : 0;      // steps all of whose tokens are there, pages of whole eights
+  int id_k = 0, id_v = 0;
+  auto ask = [&](int step) {
+    const uint32_t t = min(step, full_steps - 1) * kAttTile;
+    const uint32_t jk = a.cache.by_page.of(t + 8 * (n >> 2)), jv = a.cache.by_page.of(t + 8 * g);
+    id_k = a.cache.table == nullptr ? b : a.cache.table[b * a.cache.table_stride + jk];
+    id_v = a.cache.table == nullptr ? b : a.cache.table[b * a.cache.table_stride + jv];
+  };
+  int step = first + wave;
+  if (step < full_steps) ask(step);
+  for (; step < last; step += kAttWaves) {
+    u32x4 k[2][KK];
+    Words<N> v[8];
+    u32x4 w[MT];
+    uint32_t seen[MT];                        // of the tokens 8 g ... + 7, a bit each, by row
+    const bool old = step < old_steps;
+    const int t0 = (old ? step : step - old_steps) * kAttTile;
+    const char *base_k = old ? cache_k : a.k_new.data + 2 * (b * a.k_new.batch_stride + h * a.k_new.head_stride),
+               *base_v = old ? cache_v : a.v_new.data + 2 * (b * a.v_new.batch_stride + h * a.v_new.head_stride);
+    const bool all = step < full_steps && __all((uint32_t)id_k < (uint32_t)a.cache.pages && (uint32_t)id_v < (uint32_t)a.cache.pages);
+    if (all) {
+      const uint32_t tk = step * kAttTile + k_token, tv = step * kAttTile + 8 * g;
+      const char* pk = cache_k + 2 * (id_k * a.cache.page_stride + (int64_t)(tk - a.cache.by_page.of(tk) * a.cache.page) * a.cache.token_stride + 8 * g);
+      const char* pv = cache_v + 2 * (id_v * a.cache.page_stride + (int64_t)(tv - a.cache.by_page.of(tv) * a.cache.page) * a.cache.token_stride + DV * n);
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) k[half][kk] = *reinterpret_cast<const u32x4*>(pk + half * 8 * a.cache.token_stride + 64 * kk);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = load_words<N>(pv + i * 2 * a.cache.token_stride);
+      ask(step + kAttWaves);
+    } else {
+      // Tokens that are not there are read from a place that is (node 0, token 0 of page 0) and count as zeros that nobody sees.
+      auto find = [&](int t, int64_t stride, int64_t* at) {
+        bool ok;
+        if (old) {
+          const int c = min(t, len - 1);      // a step before old_steps has a token, so len is at least 1
+          const uint32_t j = a.cache.by_page.of(c);
+          int page = b;
+          if (a.cache.table != nullptr) page = a.cache.table[b * a.cache.table_stride + j];
+          ok = t < len && (uint32_t)page < (uint32_t)a.cache.pages;
+          *at = ok ? page * a.cache.page_stride + (int64_t)(c - j * (uint32_t)a.cache.page) * a.cache.token_stride : 0;
+        } else {
+          ok = t < a.seen_nodes;
+          *at = ok ? t * stride : 0;
+        }
+        return ok;
+      };
+      uint32_t valid = 0;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        int64_t at;
+        find(t0 + k_token + 4 * half, a.k_new.token_stride, &at);
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) k[half][kk] = *reinterpret_cast<const u32x4*>(base_k + 2 * (at + 32 * kk + 8 * g));
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        int64_t at;
+        const bool ok = find(t0 + 8 * g + i, a.v_new.token_stride, &at);
+        valid |= (uint32_t)ok << i;
+        v[i] = load_words<N>(base_v + 2 * (at + DV * n));
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[i].w[j] = ok ? v[i].w[j] : 0u;
+      }
+      if (step + kAttWaves < full_steps) ask(step + kAttWaves);
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        seen[mt] = valid;
+        if (!old) {
+          const int t = t0 + 8 * g;
+          if (a.mask == nullptr)
+            seen[mt] &= node[mt] < t ? 0u : node[mt] - t >= 7 ? 0xffu : (2u << (node[mt] - t)) - 1u;
+          else
+            seen[mt] &= node[mt] < 0 || t >= a.seen_nodes ? 0u : (uint32_t)(a.mask[b * a.mask_stride + node[mt] * a.words + (t >> 6)] >> (t & 63));
+        }
+      }
+    }
+    attend_step<T, D, MT>(rows, q, k, a.scale_log2, all, seen, w);
+    if (!old) {
+      // a node may be seen by some rows only, and for the others its values may be anything: what is no finite number leaves the
+      // product, in which it would meet weights of zero, and is added to the rows that see it by itself
+      bool odd = false;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < N; ++j) odd = odd || numbers<T>(v[i].w[j]) != v[i].w[j];
+      if (__any(odd)) {
+#pragma unroll 1
+        for (int t = 0; t < min(kAttTile, a.seen_nodes - t0); ++t) {
+          const T* from = reinterpret_cast<const T*>(base_v) + (t0 + t) * a.v_new.token_stride + 4 * DV * g;
+          const int lane_of = (t >> 3) * 16 + n, i = t & 7;
+          float by[MT];
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) {
+            const uint32_t two = __shfl(i < 4 ? (i < 2 ? w[mt][0] : w[mt][1]) : (i < 6 ? w[mt][2] : w[mt][3]), lane_of);
+            typedef T half_pair __attribute__((ext_vector_type(2)));
+            const half_pair both = __builtin_bit_cast(half_pair, two);
+            by[mt] = (__shfl(seen[mt], lane_of) >> i) & 1 ? (float)(i & 1 ? both[1] : both[0]) : 0.f;
+          }
+#pragma unroll
+          for (int j = 0; j < 4 * DV; ++j) {
+            const float value = (float)from[j];
+            if (!__builtin_isfinite(value))
+#pragma unroll
+              for (int mt = 0; mt < MT; ++mt)
+                if (by[mt] != 0.f) rows.o[mt][j % DV][j / DV] += by[mt] * value;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int j = 0; j < N; ++j) v[i].w[j] = numbers<T>(v[i].w[j]);
+      }
+    }
+    add_values<T, D, MT>(rows, v, w);
+  }
+
+  // the wavefronts' rows meet: each wavefront adds up the quarter 4 g + wave of the elements
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    float s = rows.sum[mt];
+    s += __shfl_xor(s, 16);
+    s += __shfl_xor(s, 32);
+    if (g == 0) tops[wave][mt][n] = make_float2(rows.top[mt], s);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < DV; ++j) sums[wave][(mt * 4 + i) * DV + j][lane] = rows.o[mt][j][i];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const int r = row_tile * R + mt * 16 + n;
+    float m = -INFINITY, s = 0.f, f[kAttWaves];
+#pragma unroll
+    for (int w = 0; w < kAttWaves; ++w) m = fmaxf(m, tops[w][mt][n].x);
+#pragma unroll
+    for (int w = 0; w < kAttWaves; ++w) {
+      f[w] = tops[w][mt][n].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((tops[w][mt][n].x - m) * a.scale_log2);
+      s += tops[w][mt][n].y * f[w];
+    }
+    float e[DV];
+#pragma unroll
+    for (int j = 0; j < DV; ++j) {
+      e[j] = 0.f;
+#pragma unroll
+      for (int w = 0; w < kAttWaves; ++w) e[j] += sums[w][(mt * 4 + wave) * DV + j][lane] * f[w];
+    }
+    if (r >= a.rows) continue;
+    const int d = DV * (4 * g + wave);
+    if (a.splits == 1) {
+      const float by = m == -INFINITY ? 0.f : 1.f / s;
+      uint32_t words[N];
+#pragma unroll
+      for (int j = 0; j < N; ++j) words[j] = pack2<T>(e[2 * j] * by, e[2 * j + 1] * by);
+      const int head = h * a.group + r - node[mt] * a.group;
+      store_words(a.out.data + 2 * (b * a.out.batch_stride + node[mt] * a.out.token_stride + head * a.out.head_stride + d), words);
+      if (a.lse != nullptr && g == 0 && wave == 0) a.lse[((int64_t)b * a.nodes + node[mt]) * (a.kv_heads * a.group) + head] = log_sum<T>(m, s, a.scale);
+    } else {
+      const int64_t row = (int64_t)blockIdx.x * R + mt * 16 + n;
+      uint32_t words[DV];
+#pragma unroll
+      for (int j = 0; j < DV; ++j) words[j] = __builtin_bit_cast(uint32_t, e[j]);
+      if (m != -INFINITY) store_words(reinterpret_cast<char*>(a.part + row * D + d), words);
+      if (g == 0 && wave == 0) a.stats[row] = make_float2(m, s);
+    }
+  }
+}
+
+// The parts of a row meet: one wavefront to a row.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) tree_attention_join_kernel(const AttentionArgs a, int rows_of_tile, int64_t all_rows) {
+  const int lane = threadIdx.x & 63;
+  const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);      // [batch][kv head][row]
+  if (id >= all_rows) return;
+  const int bh = (int)(id / a.rows), r = (int)(id - (int64_t)bh * a.rows);
+  const int row_tile = r / rows_of_tile;
+  const int64_t first = ((int64_t)bh * a.row_tiles + row_tile) * a.splits * rows_of_tile + (r - row_tile * rows_of_tile);
+  const float2 mine = lane < a.splits ? a.stats[first + (int64_t)lane * rows_of_tile] : make_float2(-INFINITY, 0.f);
+  float m = mine.x;
+#pragma unroll
+  for (int i = 1; i < 64; i *= 2) m = fmaxf(m, __shfl_xor(m, i));
+  const float f = mine.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mine.x - m) * a.scale_log2);
+  float s = f * mine.y;
+#pragma unroll
+  for (int i = 1; i < 64; i *= 2) s += __shfl_xor(s, i);
+  constexpr int P = D >= 128 ? D / 128 : 1;      // a lane has two neighbouring elements of every 128 (D below 128: the first D / 2 lanes)
+  float e[P * 2] = {};
+  const bool active = D >= 128 || lane < D / 2;
+  for (int i = 0; i < a.splits; ++i) {
+    const float by = __shfl(f, i);
+    if (by == 0.f || !active) continue;
+    const float* p = a.part + (first + (int64_t)i * rows_of_tile) * D + lane * 2;
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+      const float2 v = *reinterpret_cast<const float2*>(p + j * 128);
+      e[2 * j] += by * v.x;
+      e[2 * j + 1] += by * v.y;
+    }
+  }
+  const float by = m == -INFINITY ? 0.f : 1.f / s;
+  const int node = a.by_group.of(r), h = bh % a.kv_heads, b = bh / a.kv_heads, head = h * a.group + r - node * a.group;
+  char* out = a.out.data + 2 * (b * a.out.batch_stride + node * a.out.token_stride + head * a.out.head_stride + lane * 2);
+  if (active)
+#pragma unroll
+    for (int j = 0; j < P; ++j) *reinterpret_cast<uint32_t*>(out + 256 * j) = pack2<T>(e[2 * j] * by, e[2 * j + 1] * by);
+  if (a.lse != nullptr && lane == 0)
+    a.lse[((int64_t)b * a.nodes + node) * (a.kv_heads * a.group) + head] = log_sum<T>(m, s, a.scale);
+}
+
+}  // namespace dpllm

@@ -111,3 +111,38 @@ def test_append(change, code, word):
 def test_append_of_nothing():
     for change in ({"batch": 0}, {"nodes": 0}, {"layers": 0, "first": 2}):
         assert lib.dpllm_cache_append(*dict(APPEND, **change).values()) == 0
+
+
+ATTEND = dict(cache=cache(), layer=0, batch=2, nodes=3, heads=8, lens=SOME, max_len=64, q=views(1), k=views(1), v=views(1), mask=SOME, mask_stride=3, scale=0.1,
+              out=views(1), lse=SOME, ws=SOME, ws_bytes=1 << 30, stream=None)
+
+
+@pytest.mark.parametrize("change,code,word", BAD_CACHES)
+def test_attention_over_a_bad_cache(change, code, word):
+    refused(lib.dpllm_tree_attention(*dict(ATTEND, cache=cache(**change)).values()), code, word)
+
+
+@pytest.mark.parametrize("change,code,word", [
+    ({"cache": None}, -1, "NULL"), ({"cache": cache(dtype=2)}, -1, "float16"), ({"cache": cache(head_dim=80)}, -2, "head_dim"), ({"layer": -1}, -3, "layer"),
+    ({"layer": 2}, -3, "layer"), ({"batch": -1}, -2, "sequences"), ({"batch": 65537}, -2, "sequences"), ({"nodes": -1}, -2, "nodes"), ({"nodes": 257}, -2, "nodes"),
+    ({"heads": 6}, -2, "heads"), ({"heads": 0}, -2, "heads"), ({"heads": 2048}, -2, "heads"), ({"max_len": -1}, -2, "max_len"), ({"scale": math.inf}, -1, "scale"),
+    ({"scale": math.nan}, -1, "scale"), ({"lens": None}, -1, "NULL"), ({"q": None}, -1, "NULL"), ({"q": views(1, data=None)}, -1, "NULL"), ({"out": None}, -1, "NULL"),
+    ({"k": None}, -1, "NULL"), ({"v": None}, -1, "NULL"), ({"k": views(1, data=None)}, -1, "NULL"), ({"q": views(1, data=SOME + 2)}, -1, "aligned"),
+    ({"out": views(1, strides=(1024, 512, 129))}, -1, "aligned"), ({"k": views(1, strides=(1024, 510, 128))}, -1, "aligned"),
+    ({"cache": cache(k=SOME + 8)}, -1, "aligned"), ({"cache": cache(page_stride=16 * 512 + 4)}, -1, "aligned"),
+    ({"cache": cache(page=1 << 30, pages_per_seq=8)}, -2, "tokens"), ({"ws": None}, -4, "workspace"), ({"ws_bytes": 100}, -4, "workspace"), ({"ws": SOME + 8}, -4, "workspace"),
+])
+def test_attention(change, code, word):
+    refused(lib.dpllm_tree_attention(*dict(ATTEND, cache=change.get("cache", cache(page=64)), max_len=change.get("max_len", 10000),
+                                           **{k: v for k, v in change.items() if k not in ("cache", "max_len")}).values()), code, word)
+
+
+def test_workspace_of_the_attention():
+    n = C.c_size_t(1)
+    f = lib.dpllm_tree_attention_workspace_bytes
+    assert f(0, 4, 8, 2, 128, 1000, C.byref(n)) == 0 and n.value == 0
+    assert f(1, 4, 8, 2, 128, 100000, C.byref(n)) == 0 and n.value > 0
+    refused(f(1, 4, 8, 2, 128, 1000, None), -1, "NULL")
+    refused(f(1, 4, 8, 3, 128, 1000, C.byref(n)), -2, "heads")
+    refused(f(1, 4, 8, 2, 100, 1000, C.byref(n)), -2, "head_dim")
+    refused(f(1, 4, 8, 2, 128, -1, C.byref(n)), -2, "max_len")
