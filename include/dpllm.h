@@ -304,6 +304,28 @@ int dpllm_tree_attention(const dpllm_cache* cache, int layer, int batch, int nod
                          int64_t mask_stride, float scale, const dpllm_heads* out, float* lse_dev, void* ws_dev, size_t ws_bytes,
                          void* stream);
 
+/* Which drafted tokens stand, and the token behind them.  Row i of `logits` is the target's answer behind node i, p_i = softmax(logits_i / temperature[b]);
+ * row i of `draft` the draft's, q_i, from which the tokens of i's children were drawn, each by itself.  From the root (node 0) on, the children of a node are
+ * asked in the order of their numbers: child c stands if uniforms[c] q(c) < r(c), where r is p at first and norm(max(r - q, 0)) behind every child that
+ * did not stand (r stays where nothing is left).  With draft_dev NULL the children were named, not drawn: c stands if uniforms[c] < r(c), and a
+ * child that does not leaves r.  The first child that stands is the next node; where none does, the token behind is drawn from r: the first word whose running sum of r exceeds uniforms[0] times
+ * the whole.  Tokens so chosen are distributed as if drawn from the target.  temperature[b] 0 (or less, or NaN): a child stands if it is the word with
+ * the largest logit, the lowest such word where several are, and that word is the token behind; the draft rows are not read.
+ * logits, draft: dtype [batch][nodes][vocabulary], the words contiguous, strides in elements.  tokens: int32 [batch][nodes] (that of node 0 is not read); a token outside the
+ * vocabulary never stands.  parents: int32 [batch][nodes]; a node whose parent is not a lower node is nobody's child; NULL: a chain.  uniforms: float
+ * [batch][nodes] in [0, 1).  temperature: float [batch].  Logits of minus infinity and NaN have probability 0; where one is plus infinity, only such have any.
+ * siblings (with draft rows only): the most children that a node has; a call makes that many passes over the rows whose children are refused.  Where a node has
+ * more, those beyond that did not stand leave r as it was and the children behind them are not asked.
+ * count [batch]: how many nodes stand, the root among them, which is also how many tokens there are in words.  path [batch][nodes]: those nodes.  words [batch][nodes]:
+ * the tokens of the drafted ones among them, then the token behind (-1 where the last row has no finite logit).  The rest of both is -1.  path and count are
+ * what dpllm_cache_append takes.  Logits are widened and everything is computed in 64 bits, so the answers do not depend on the order of additions but for ties to 1e-13.
+ * ws_dev: 16-byte aligned, of dpllm_verify_workspace_bytes, used until the call's kernels have run.  Errors: EINVAL, ESHAPE, ESTATE (workspace), EHIP. */
+int dpllm_verify_workspace_bytes(int batch, int nodes, int vocabulary, int dtype, int draft, int siblings, size_t* bytes);
+int dpllm_verify(int batch, int nodes, int vocabulary, int dtype, const void* logits_dev, int64_t logits_batch_stride,
+                 int64_t logits_node_stride, const void* draft_dev, int64_t draft_batch_stride, int64_t draft_node_stride,
+                 const int32_t* tokens_dev, const int32_t* parents_dev, const float* uniforms_dev, const float* temperature_dev,
+                 int siblings, int32_t* count_dev, int32_t* path_dev, int32_t* words_dev, void* ws_dev, size_t ws_bytes, void* stream);
+
 /* Puts keys and values of some nodes behind what the cache holds, for n_layers layers from first_layer on: node path[b][i] of sequence b goes to token
  * lens[b] + i, i < count[b] (rows of path are path_stride entries apart and hold `nodes`).  path_dev NULL: nodes in their order; count_dev NULL: all nodes.  Entries of path outside [0, nodes), tokens without a
  * page and sequences with a negative length are left out; counts above nodes are taken as nodes.  lens is not changed (add the counts

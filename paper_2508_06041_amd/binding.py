@@ -29,7 +29,8 @@ SYMBOLS = ["dpllm_model_create", "dpllm_model_destroy", "dpllm_last_error", "dpl
            "dpllm_estimate", "dpllm_estimate_noalloc", "dpllm_gemv", "dpllm_decode_step", "dpllm_decode_step_parts", "dpllm_debug_unpack", "dpllm_debug_locate",
            "dpllm_debug_set_polls", "dpllm_debug_set_one_launch", "dpllm_debug_step_launches", "dpllm_debug_copy", "dpllm_debug_read",
            "dpllm_call_error", "dpllm_rope_frequencies", "dpllm_rope",
-           "dpllm_tree_attention_workspace_bytes", "dpllm_tree_attention", "dpllm_cache_append"]
+           "dpllm_tree_attention_workspace_bytes", "dpllm_tree_attention", "dpllm_verify_workspace_bytes",
+           "dpllm_verify", "dpllm_cache_append"]
 
 
 class DpllmError(RuntimeError):
@@ -89,6 +90,8 @@ def _load():
     L.dpllm_rope.argtypes = [heads, heads, C.POINTER(i32), i32, i32, i32, i32, i32, i32, i32, vp, f32, vp, i64, i32, vp]
     L.dpllm_tree_attention_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32, C.POINTER(sz)]
     L.dpllm_tree_attention.argtypes = [cache, i32, i32, i32, i32, vp, i32, heads, heads, heads, vp, i64, f32, heads, vp, vp, sz, vp]
+    L.dpllm_verify_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32, C.POINTER(sz)]
+    L.dpllm_verify.argtypes = [i32, i32, i32, i32, vp, i64, i64, vp, i64, i64, vp, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
     L.dpllm_cache_append.argtypes = [cache, i32, i32, i32, i32, vp, heads, i64, heads, i64, vp, i64, vp, vp]
     return L
 
@@ -269,6 +272,38 @@ def dpllm_tree_attention(cache, layer, lens, q, k_new=None, v_new=None, mask=Non
                                    C.byref(_view(out, "out")), _ptr(lse), _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
                                    _stream()))
     return out
+
+
+def dpllm_verify_workspace_bytes(batch, nodes, vocabulary, dtype, draft, siblings):
+    n = C.c_size_t(0)
+    _call(lib.dpllm_verify_workspace_bytes(batch, nodes, vocabulary, dtype, 1 if draft else 0, siblings, C.byref(n)))
+    return n.value
+
+
+def dpllm_verify(logits, tokens, uniforms, temperature, parents=None, draft=None, siblings=None, count=None, path=None, words=None, workspace=None):
+    """logits, draft: [batch][nodes][vocabulary] of one type; tokens, parents: int32 [batch][nodes]; uniforms: float32 [batch][nodes]; temperature: float32
+    [batch].  siblings: the most children that a node has (1 for a chain; every node but the root unless given).  Returns (count [batch], path, words
+    [batch][nodes]), int32, new tensors unless given.  workspace: uint8, allocated for the call unless given."""
+    dtype = _dtype(logits, "logits")
+    _need(logits.dim() == 3 and (logits.stride(2) == 1 or logits.shape[2] == 1 or logits.numel() == 0), "logits has to be [batch][nodes][vocabulary], the words contiguous")
+    b, n, v = logits.shape
+    if draft is not None:
+        _need(draft.shape == logits.shape and draft.dtype == logits.dtype and draft.is_cuda and (draft.stride(2) == 1 or v == 1 or draft.numel() == 0),
+              "draft has to have the shape and type of logits, the words contiguous")
+    for t, shape, what in ((uniforms, (b, n), "uniforms"), (temperature, (b,), "temperature")):
+        _need(t.dtype == torch.float32 and t.is_cuda and tuple(t.shape) == shape and t.is_contiguous(), "%s has to be a contiguous float32 device tensor %s" % (what, list(shape)))
+    if siblings is None:
+        siblings = 1 if parents is None else max(1, n - 1)
+    count = torch.empty(b, dtype=torch.int32, device="cuda") if count is None else count
+    path = torch.empty((b, n), dtype=torch.int32, device="cuda") if path is None else path
+    words = torch.empty((b, n), dtype=torch.int32, device="cuda") if words is None else words
+    if workspace is None:
+        workspace = torch.empty(dpllm_verify_workspace_bytes(b, n, v, dtype, draft is not None, siblings), dtype=torch.uint8, device="cuda")
+    _call(lib.dpllm_verify(b, n, v, dtype, _ptr(logits), logits.stride(0), logits.stride(1), _ptr(draft), 0 if draft is None else draft.stride(0),
+                           0 if draft is None else draft.stride(1), _index(tokens, (b, n), "tokens"), _index(parents, (b, n), "parents"), _ptr(uniforms), _ptr(temperature),
+                           siblings, _index(count, (b,), "count"), _index(path, (b, n), "path"), _index(words, (b, n), "words"), _ptr(workspace),
+                           workspace.numel() * workspace.element_size(), _stream()))
+    return count, path, words
 
 
 def dpllm_cache_append(cache, lens, k_new, v_new, path=None, count=None, layer=0):

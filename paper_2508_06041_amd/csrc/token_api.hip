@@ -7,6 +7,7 @@
 #include "append_kernel.hpp"
 #include "rope_kernel.hpp"
 #include "token_host.hpp"
+#include "verify_kernels.hpp"
 
 using namespace dpllm;
 
@@ -18,6 +19,41 @@ void launch_rope(const RopeArgs& a, bool half, int blocks, size_t lds, hipStream
     hipLaunchKernelGGL((rope_kernel<T, E, true>), dim3(blocks), dim3(kRopeThreads), lds, stream, a);
   else
     hipLaunchKernelGGL((rope_kernel<T, E, false>), dim3(blocks), dim3(kRopeThreads), lds, stream, a);
+}
+
+// The workspace of a verification: the parts of the rows, then the sums of what is left.
+struct VerifySpace {
+  int chunks;
+  size_t parts, bytes;
+};
+
+VerifySpace verify_space(int batch, int nodes, int vocabulary, int dtype, bool draft, int siblings) {
+  const int e = dtype == DPLLM_F32 ? 4 : 8, chunk = kVerThreads * kVerPieces * e;
+  VerifySpace s;
+  s.chunks = (int)(((int64_t)vocabulary + e - 1 + chunk - 1) / chunk);      // a row may start up to e - 1 elements behind a 16-byte boundary
+  const size_t all = (size_t)batch * nodes * s.chunks;
+  s.parts = all * sizeof(VerifyPart) * (draft ? 2 : 1);
+  s.bytes = s.parts + (draft ? all * siblings * sizeof(double) : 0);
+  return s;
+}
+
+int check_verify(const char* who, int batch, int nodes, int vocabulary, int dtype, bool draft, int siblings) {
+  if (dtype < DPLLM_F16 || dtype > DPLLM_F32) return refuse(DPLLM_EINVAL, "%s: unknown dtype %d", who, dtype);
+  if (batch < 0 || batch > 65536 || nodes < 1 || nodes > DPLLM_MAX_NODES)
+    return refuse(DPLLM_ESHAPE, "%s: %d sequences of %d nodes (at most 65536 of 1 to %d)", who, batch, nodes, DPLLM_MAX_NODES);
+  if (vocabulary < 1 || vocabulary > (1 << 24)) return refuse(DPLLM_ESHAPE, "%s: a vocabulary of %d words (1 to 2^24)", who, vocabulary);
+  if (draft && (siblings < 1 || siblings > DPLLM_MAX_NODES)) return refuse(DPLLM_ESHAPE, "%s: %d siblings (1 to %d)", who, siblings, DPLLM_MAX_NODES);
+  if ((int64_t)batch * nodes * verify_space(1, 1, vocabulary, dtype, false, 1).chunks > 0xffffff)
+    return refuse(DPLLM_ESHAPE, "%s: %d sequences of %d nodes with %d words are too many at once", who, batch, nodes, vocabulary);
+  return DPLLM_OK;
+}
+
+template <typename T>
+void launch_verify(const VerifyArgs& a, hipStream_t s) {
+  const unsigned pieces = (unsigned)a.batch * a.nodes * a.chunks;
+  hipLaunchKernelGGL(verify_parts_kernel<T>, dim3(pieces, a.draft ? 2 : 1), dim3(kVerThreads), 0, s, a);
+  for (int round = 0; a.draft && round < a.siblings; ++round) hipLaunchKernelGGL(verify_rest_kernel<T>, dim3(pieces), dim3(kVerThreads), 0, s, a, round);
+  hipLaunchKernelGGL(verify_choose_kernel<T>, dim3(a.batch), dim3(kVerThreads), 0, s, a);
 }
 
 }  // namespace
@@ -158,6 +194,58 @@ int dpllm_cache_append(const dpllm_cache* cache, int first_layer, int n_layers, 
     hipLaunchKernelGGL(append_kernel<uint16_t>, grid, dim3(kAppendThreads), 0, s, a, 1);
   else
     hipLaunchKernelGGL(append_kernel<uint32_t>, grid, dim3(kAppendThreads), 0, s, a, 1);
+  return launched(who);
+}
+
+int dpllm_verify_workspace_bytes(int batch, int nodes, int vocabulary, int dtype, int draft, int siblings, size_t* bytes) {
+  const char* who = "dpllm_verify_workspace_bytes";
+  if (!bytes) return refuse(DPLLM_EINVAL, "%s: bytes is NULL", who);
+  if (int rc = check_verify(who, batch, nodes, vocabulary, dtype, draft != 0, siblings)) return rc;
+  *bytes = verify_space(batch, nodes, vocabulary, dtype, draft != 0, siblings).bytes;
+  return DPLLM_OK;
+}
+
+int dpllm_verify(int batch, int nodes, int vocabulary, int dtype, const void* logits_dev, int64_t logits_batch_stride, int64_t logits_node_stride,
+                 const void* draft_dev, int64_t draft_batch_stride, int64_t draft_node_stride, const int32_t* tokens_dev, const int32_t* parents_dev,
+                 const float* uniforms_dev, const float* temperature_dev, int siblings, int32_t* count_dev, int32_t* path_dev, int32_t* words_dev, void* ws_dev,
+                 size_t ws_bytes, void* stream) {
+  const char* who = "dpllm_verify";
+  if (int rc = check_verify(who, batch, nodes, vocabulary, dtype, draft_dev != nullptr, siblings)) return rc;
+  if (batch == 0) return DPLLM_OK;
+  if (!logits_dev || !tokens_dev || !uniforms_dev || !temperature_dev || !count_dev || !path_dev || !words_dev)
+    return refuse(DPLLM_EINVAL, "%s: a pointer is NULL (draft_dev and parents_dev may be)", who);
+  if (((uintptr_t)logits_dev | (uintptr_t)draft_dev) % (dtype == DPLLM_F32 ? 4 : 2)) return refuse(DPLLM_EINVAL, "%s: the rows are not aligned to their elements", who);
+  const VerifySpace space = verify_space(batch, nodes, vocabulary, dtype, draft_dev != nullptr, siblings);
+  if (!ws_dev || ws_bytes < space.bytes || (uintptr_t)ws_dev % 16)
+    return refuse(DPLLM_ESTATE, "%s: needs a workspace of %zu bytes, aligned to 16", who, space.bytes);
+  VerifyArgs a{};
+  a.logits = (const char*)logits_dev;
+  a.draft = (const char*)draft_dev;
+  a.logits_batch = logits_batch_stride;
+  a.logits_node = logits_node_stride;
+  a.draft_batch = draft_batch_stride;
+  a.draft_node = draft_node_stride;
+  a.tokens = tokens_dev;
+  a.parents = parents_dev;
+  a.uniforms = uniforms_dev;
+  a.temperature = temperature_dev;
+  a.count = count_dev;
+  a.path = path_dev;
+  a.words = words_dev;
+  a.parts = (VerifyPart*)ws_dev;
+  a.rest = (double*)((char*)ws_dev + space.parts);
+  a.batch = batch;
+  a.nodes = nodes;
+  a.vocabulary = vocabulary;
+  a.chunks = space.chunks;
+  a.by_chunks = Divide::by(space.chunks);
+  a.siblings = siblings;
+  if (dtype == DPLLM_F16)
+    launch_verify<half_t>(a, (hipStream_t)stream);
+  else if (dtype == DPLLM_BF16)
+    launch_verify<bfloat_t>(a, (hipStream_t)stream);
+  else
+    launch_verify<float>(a, (hipStream_t)stream);
   return launched(who);
 }
 

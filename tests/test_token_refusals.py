@@ -146,3 +146,29 @@ def test_workspace_of_the_attention():
     refused(f(1, 4, 8, 3, 128, 1000, C.byref(n)), -2, "heads")
     refused(f(1, 4, 8, 2, 100, 1000, C.byref(n)), -2, "head_dim")
     refused(f(1, 4, 8, 2, 128, -1, C.byref(n)), -2, "max_len")
+
+
+VERIFY = dict(batch=2, nodes=4, vocabulary=1000, dtype=1, logits=SOME, logits_batch=4000, logits_node=1000, draft=SOME, draft_batch=4000, draft_node=1000,
+              tokens=SOME, parents=SOME, uniforms=SOME, temperature=SOME, siblings=2, count=SOME, path=SOME, words=SOME, ws=SOME, ws_bytes=1 << 20, stream=None)
+
+
+@pytest.mark.parametrize("change,code,word", [
+    ({"batch": -1}, -2, "sequences"), ({"batch": 70000}, -2, "sequences"), ({"nodes": 0}, -2, "nodes"), ({"nodes": 257}, -2, "nodes"), ({"vocabulary": 0}, -2, "vocabulary"),
+    ({"vocabulary": 1 << 25}, -2, "vocabulary"), ({"dtype": 3}, -1, "dtype"), ({"siblings": 0}, -2, "siblings"), ({"siblings": 257}, -2, "siblings"),
+    ({"batch": 65536, "nodes": 256}, -2, "too many"), ({"logits": None}, -1, "NULL"), ({"tokens": None}, -1, "NULL"), ({"uniforms": None}, -1, "NULL"),
+    ({"temperature": None}, -1, "NULL"), ({"count": None}, -1, "NULL"), ({"path": None}, -1, "NULL"), ({"words": None}, -1, "NULL"),
+    ({"logits": SOME + 1}, -1, "aligned"), ({"draft": SOME + 2, "dtype": 2}, -1, "aligned"), ({"ws": None}, -4, "workspace"), ({"ws": SOME + 8}, -4, "workspace"),
+    ({"ws_bytes": 16}, -4, "workspace"),
+])
+def test_verify(change, code, word):
+    refused(lib.dpllm_verify(*dict(VERIFY, **change).values()), code, word)
+
+
+def test_verify_of_nothing_and_its_workspace():
+    assert lib.dpllm_verify(*dict(VERIFY, batch=0).values()) == 0
+    n, f = C.c_size_t(0), lib.dpllm_verify_workspace_bytes
+    assert f(2, 4, 1000, 0, 1, 2, C.byref(n)) == 0 and n.value >= 2 * 4 * (2 * 16 + 2 * 8)
+    small = n.value
+    assert f(2, 4, 1000, 0, 0, 0, C.byref(n)) == 0 and 2 * 4 * 16 <= n.value < small
+    refused(f(2, 4, 1000, 0, 1, 2, None), -1, "NULL")
+    refused(f(2, 4, 0, 0, 1, 2, C.byref(n)), -2, "vocabulary")
