@@ -106,6 +106,11 @@ except ImportError as e:
 _calls.bind(C.cast(lib.dpllm_gemv, C.c_void_p).value, C.cast(lib.dpllm_estimate, C.c_void_p).value,
             torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
 
+_calls.bind_tokens(tuple(C.cast(f, C.c_void_p).value for f in (lib.dpllm_rope, lib.dpllm_tree_attention_workspace_bytes, lib.dpllm_tree_attention,
+                                                               lib.dpllm_verify_workspace_bytes, lib.dpllm_verify, lib.dpllm_cache_append)),
+                   (torch.float16, torch.bfloat16, torch.float32, torch.int32, torch.int64, torch.float64), torch.empty_like,
+                   lambda n: torch.empty(n, dtype=torch.uint8, device="cuda"))
+
 
 def _stream():
     """The current stream's handle.  torch.cuda.current_stream() builds a Stream object for it (2.9 us of a call of
@@ -194,6 +199,12 @@ def dpllm_rope_frequencies(rotary_dim, base=10000.0, scaling=DPLLM_ROPE_PLAIN, f
 def dpllm_rope(x, positions, freqs, out=None, scale=1.0, layout=DPLLM_ROPE_HALF, inverse=False):
     """x: a tensor [batch][tokens][heads][head_dim], or a tuple of such that share everything but their heads (queries, keys).  positions: int32
     [batch][tokens], or [tokens] for all sequences.  out: where the results go (x itself: in place); new tensors unless given."""
+    made = _calls.rope(x, positions, freqs, out, scale, layout, inverse)
+    if type(made) is not int:
+        return made
+    if made != _calls.ELSEWHERE:
+        _call(made)
+    # out of the ordinary: the long way, with the errors that has
     xs = (x,) if isinstance(x, torch.Tensor) else tuple(x)
     _need(0 < len(xs) <= 4, "dpllm_rope takes 1 to 4 tensors")
     first = xs[0]
@@ -234,6 +245,7 @@ class Cache:
         self.capacity = self.pages_per_seq * self.page
         self.c = _Cache(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), k.stride(3), _ptr(table), 0 if table is None else table.stride(0),
                         dtype, self.layers, self.pages, self.page, self.pages_per_seq, self.heads, self.head_dim)
+        self.address = C.addressof(self.c)
 
 
 def dpllm_tree_attention_workspace_bytes(batch, nodes, heads, kv_heads, head_dim, max_len):
@@ -246,6 +258,11 @@ def dpllm_tree_attention(cache, layer, lens, q, k_new=None, v_new=None, mask=Non
     """q: [batch][nodes][heads][head_dim]; k_new, v_new: [batch][nodes][cache.heads][head_dim].  mask: int64 [batch or 1][nodes][ceil(nodes / 64)], bit j of
     row i: node i sees node j; None: a chain.  scale: 1 / sqrt(head_dim) unless given.  lse: float32 [batch][nodes][heads] to be filled.  max_len: how long
     the longest context is expected to be (the cache's capacity unless given).  workspace: uint8, allocated for the call unless given."""
+    made = _calls.attention(cache, layer, lens, q, k_new, v_new, mask, scale, out, lse, max_len, workspace)
+    if type(made) is not int:
+        return made
+    if made != _calls.ELSEWHERE:
+        _call(made)
     _need(q.dim() == 4 and q.dtype == cache.k.dtype and q.shape[3] == cache.head_dim, "q has to be [batch][nodes][heads][head_dim] of the cache's type and head_dim")
     b, n, h, d = q.shape
     _need(b <= cache.batch, "q has more sequences than the cache")
@@ -284,6 +301,13 @@ def dpllm_verify(logits, tokens, uniforms, temperature, parents=None, draft=None
     """logits, draft: [batch][nodes][vocabulary] of one type; tokens, parents: int32 [batch][nodes]; uniforms: float32 [batch][nodes]; temperature: float32
     [batch].  siblings: the most children that a node has (1 for a chain; every node but the root unless given).  Returns (count [batch], path, words
     [batch][nodes]), int32, new tensors unless given.  workspace: uint8, allocated for the call unless given."""
+    if count is None and path is None and words is None and workspace is None:
+        made = _calls.verify(logits, tokens, uniforms, temperature, parents, draft,
+                             siblings if siblings is not None else 1 if parents is None else max(1, tokens.shape[-1] - 1))
+        if type(made) is not int:
+            return made
+        if made != _calls.ELSEWHERE:
+            _call(made)
     dtype = _dtype(logits, "logits")
     _need(logits.dim() == 3 and (logits.stride(2) == 1 or logits.shape[2] == 1 or logits.numel() == 0), "logits has to be [batch][nodes][vocabulary], the words contiguous")
     b, n, v = logits.shape
@@ -309,6 +333,9 @@ def dpllm_verify(logits, tokens, uniforms, temperature, parents=None, draft=None
 def dpllm_cache_append(cache, lens, k_new, v_new, path=None, count=None, layer=0):
     """k_new, v_new: [batch][nodes][heads][head_dim] for one layer, or [layers][batch]... for as many from `layer` on.  path: int32 [batch][nodes],
     count: int32 [batch]."""
+    made = _calls.append(cache, lens, k_new, v_new, path, count, layer)
+    if made != _calls.ELSEWHERE:
+        return _call(made)
     if k_new.dim() == 4:
         k_new, v_new = k_new.unsqueeze(0), v_new.unsqueeze(0)
     _need(k_new.dim() == 5 and k_new.shape == v_new.shape and k_new.dtype == v_new.dtype == cache.k.dtype,
