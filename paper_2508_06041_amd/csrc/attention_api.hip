@@ -11,41 +11,56 @@ using namespace dpllm;
 
 namespace {
 
+// Which kernel, and how the work is split.
 struct Plan {
-  int rows, mt, row_tiles, splits;
+  int rows, mt, waves;   // rows of a kv head; tiles of 16 rows to a wavefront; waves > 0: the kernel for many rows with so many wavefronts
+  int tile, row_tiles, slots;
   int64_t groups;        // workgroups
-  size_t part, bytes;    // bytes of the partial results, and with their maxima and sums
+  size_t part, stats, bytes;
 };
 
-Plan plan_of(int batch, int nodes, int heads, int kv_heads, int head_dim, int64_t max_len, int seen) {
+Plan plan_of(int batch, int nodes, int heads, int kv_heads, int head_dim, int64_t max_len) {
   Plan p;
   p.rows = nodes * (heads / kv_heads);
-  p.mt = p.rows > 16 && head_dim < 256 ? 2 : 1;
-  p.row_tiles = (p.rows + 16 * p.mt - 1) / (16 * p.mt);
-  const int64_t lone = (int64_t)batch * kv_heads * p.row_tiles, steps = (max_len + kAttTile - 1) / kAttTile + (seen + kAttTile - 1) / kAttTile;
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(1024 + lone - 1) / std::max<int64_t>(lone, 1), (steps + kAttWaves - 1) / kAttWaves, kAttMaxSplits}));
-  p.groups = lone * p.splits;
-  p.part = p.splits > 1 ? (size_t)p.groups * 16 * p.mt * head_dim * sizeof(float) : 0;
-  p.bytes = p.splits > 1 ? p.part + (size_t)p.groups * 16 * p.mt * sizeof(float2) : 0;
+  p.waves = p.rows <= 32 ? 0 : p.rows <= 128 || head_dim == 256 ? 4 : 8;
+  p.mt = head_dim == 256 || p.rows <= 16 || (p.rows > 32 && p.rows <= 64) ? 1 : 2;
+  p.tile = 16 * p.mt * std::max(p.waves, 1);
+  p.row_tiles = (p.rows + p.tile - 1) / p.tile;
+  const int64_t steps = (max_len + kAttTile - 1) / kAttTile + (nodes + kAttTile - 1) / kAttTile, tiles = (int64_t)kv_heads * p.row_tiles;
+  const int unit = p.waves ? 1 : kAttWaves;
+  const int64_t most = batch * ((steps + unit - 1) / unit), fill = ((p.waves == 8 ? 256 : 512) + tiles - 1) / tiles;
+  p.slots = (int)std::max<int64_t>(batch, std::min(most, batch == 1 ? fill : std::max(fill, 3 * (int64_t)batch)));
+  p.groups = p.slots * tiles;
+  const bool whole = p.slots == batch;
+  p.part = whole ? 0 : (size_t)p.groups * p.tile * head_dim * sizeof(float);
+  p.stats = whole ? 0 : (size_t)p.groups * p.tile * sizeof(float2);
+  p.bytes = whole ? 0 : p.part + p.stats + (size_t)batch * sizeof(int2);
   return p;
 }
 
 template <typename T, int D>
-void launch(const AttentionArgs& a, const Plan& p, int64_t all_rows, hipStream_t s) {
-  if (p.mt == 1 || D == 256)
-    hipLaunchKernelGGL((tree_attention_kernel<T, D, 1>), dim3((unsigned)p.groups), dim3(kAttWaves * 64), 0, s, a);
-  else if constexpr (D < 256)
-    hipLaunchKernelGGL((tree_attention_kernel<T, D, 2>), dim3((unsigned)p.groups), dim3(kAttWaves * 64), 0, s, a);
-  if (p.splits > 1)
-    hipLaunchKernelGGL((tree_attention_join_kernel<T, D>), dim3((unsigned)((all_rows + 3) / 4)), dim3(256), 0, s, a, 16 * p.mt, all_rows);
+void launch(const AttentionArgs& a, const Plan& p, hipStream_t s) {
+  const dim3 groups((unsigned)p.groups);
+  if (p.waves == 0 && p.mt == 1) hipLaunchKernelGGL((tree_attention_kernel<T, D, 1>), groups, dim3(kAttWaves * 64), 0, s, a);
+  if (p.waves == 4 && p.mt == 1) hipLaunchKernelGGL((tree_attention_wide_kernel<T, D, 1, 4>), groups, dim3(4 * 64), 0, s, a);
+  if constexpr (D < 256) {
+    if (p.waves == 0 && p.mt == 2) hipLaunchKernelGGL((tree_attention_kernel<T, D, 2>), groups, dim3(kAttWaves * 64), 0, s, a);
+    if (p.waves == 4 && p.mt == 2) hipLaunchKernelGGL((tree_attention_wide_kernel<T, D, 2, 4>), groups, dim3(4 * 64), 0, s, a);
+    if (p.waves == 8 && p.mt == 2) hipLaunchKernelGGL((tree_attention_wide_kernel<T, D, 2, 8>), groups, dim3(8 * 64), 0, s, a);
+  }
+  if (p.bytes > 0) {
+    const uint32_t all_rows = (uint32_t)a.batch * a.kv_heads * a.rows;
+    hipLaunchKernelGGL((tree_attention_join_kernel<T, D>), dim3((all_rows + 3) / 4), dim3(256), 0, s, a, p.tile, Divide::by(a.rows), Divide::by(a.kv_heads),
+                       Divide::by(p.tile), all_rows);
+  }
 }
 
 template <typename T>
-void launch(int head_dim, const AttentionArgs& a, const Plan& p, int64_t all_rows, hipStream_t s) {
-  if (head_dim == 64) launch<T, 64>(a, p, all_rows, s);
-  if (head_dim == 96) launch<T, 96>(a, p, all_rows, s);
-  if (head_dim == 128) launch<T, 128>(a, p, all_rows, s);
-  if (head_dim == 256) launch<T, 256>(a, p, all_rows, s);
+void launch(int head_dim, const AttentionArgs& a, const Plan& p, hipStream_t s) {
+  if (head_dim == 64) launch<T, 64>(a, p, s);
+  if (head_dim == 96) launch<T, 96>(a, p, s);
+  if (head_dim == 128) launch<T, 128>(a, p, s);
+  if (head_dim == 256) launch<T, 256>(a, p, s);
 }
 
 int check_sizes(const char* who, int batch, int nodes, int heads, int kv_heads, int head_dim) {
@@ -65,7 +80,7 @@ int dpllm_tree_attention_workspace_bytes(int batch, int nodes, int heads, int kv
   if (!bytes) return refuse(DPLLM_EINVAL, "%s: bytes is NULL", who);
   if (int rc = check_sizes(who, batch, nodes, heads, kv_heads, head_dim)) return rc;
   if (max_len < 0) return refuse(DPLLM_ESHAPE, "%s: max_len %d", who, max_len);
-  *bytes = batch == 0 || nodes == 0 ? 0 : plan_of(batch, nodes, heads, kv_heads, head_dim, max_len, nodes).bytes;
+  *bytes = batch == 0 || nodes == 0 ? 0 : plan_of(batch, nodes, heads, kv_heads, head_dim, max_len).bytes;
   return DPLLM_OK;
 }
 
@@ -86,8 +101,8 @@ int dpllm_tree_attention(const dpllm_cache* cache, int layer, int batch, int nod
   if (!pieces(*q, 2) || !pieces(*out, 2) || (k_new && (!pieces(*k_new, 2) || !pieces(*v_new, 2))) || ((uintptr_t)cache->k | (uintptr_t)cache->v) % 16 ||
       (cache->layer_stride | cache->page_stride | cache->token_stride | cache->head_stride) % 8)
     return refuse(DPLLM_EINVAL, "%s: tensors have to be aligned to 16 bytes, with strides of whole 8 elements", who);
-  const Plan p = plan_of(batch, nodes, heads, cache->heads, cache->head_dim, std::min<int64_t>(max_len, (int64_t)cache->pages_per_seq * cache->page), nodes);
-  if (p.groups > 0x7fffff) return refuse(DPLLM_ESHAPE, "%s: %lld workgroups", who, (long long)p.groups);
+  const Plan p = plan_of(batch, nodes, heads, cache->heads, cache->head_dim, std::min<int64_t>(max_len, (int64_t)cache->pages_per_seq * cache->page));
+  if (p.groups > 0x7fffff || (int64_t)batch * heads * nodes > 0x7fffff) return refuse(DPLLM_ESHAPE, "%s: %lld workgroups", who, (long long)p.groups);
   if (p.bytes > 0 && (!ws_dev || ws_bytes < p.bytes || (uintptr_t)ws_dev % 16))
     return refuse(DPLLM_ESTATE, "%s: needs a workspace of %zu bytes, aligned to 16", who, p.bytes);
   AttentionArgs a{};
@@ -102,8 +117,11 @@ int dpllm_tree_attention(const dpllm_cache* cache, int layer, int batch, int nod
   a.mask = mask_dev;
   a.mask_stride = mask_stride;
   a.lse = lse_dev;
-  a.part = (float*)ws_dev;
-  a.stats = (float2*)((char*)ws_dev + p.part);
+  if (p.bytes > 0) {
+    a.part = (float*)ws_dev;
+    a.stats = (float2*)((char*)ws_dev + p.part);
+    a.places = (int2*)((char*)ws_dev + p.part + p.stats);
+  }
   a.scale = std::fabs(scale);
   a.scale_log2 = (float)(std::fabs((double)scale) * 1.44269504088896340736);
   a.sign = scale < 0 ? 0x80008000u : 0u;
@@ -116,12 +134,13 @@ int dpllm_tree_attention(const dpllm_cache* cache, int layer, int batch, int nod
   a.kv_heads = cache->heads;
   a.rows = p.rows;
   a.row_tiles = p.row_tiles;
-  a.splits = p.splits;
-  const int64_t all_rows = (int64_t)batch * cache->heads * p.rows;
+  a.batch = batch;
+  a.slots = p.slots;
+  a.unit = p.waves ? 1 : kAttWaves;
   if (cache->dtype == DPLLM_F16)
-    launch<half_t>(cache->head_dim, a, p, all_rows, (hipStream_t)stream);
+    launch<half_t>(cache->head_dim, a, p, (hipStream_t)stream);
   else
-    launch<bfloat_t>(cache->head_dim, a, p, all_rows, (hipStream_t)stream);
+    launch<bfloat_t>(cache->head_dim, a, p, (hipStream_t)stream);
   return launched(who);
 }
 

@@ -7,9 +7,8 @@
 
 namespace dpllm {
 
-constexpr int kAttWaves = 4;        // wavefronts of a workgroup
+constexpr int kAttWaves = 4;        // wavefronts of a workgroup of the kernel for few rows
 constexpr int kAttTile = 32;        // tokens of a step
-constexpr int kAttMaxSplits = 64;
 
 struct AttentionArgs {
   CacheView cache;                  // of the layer
@@ -18,12 +17,13 @@ struct AttentionArgs {
   const uint64_t* mask;             // [nodes][words]; nullptr: a chain
   int64_t mask_stride;
   float* lse;
-  float* part;                      // splits > 1: [workgroups][rows of a tile][head_dim], behind them the maxima and sums
-  float2* stats;
+  float* part;                      // [workgroups][rows of a tile][head_dim] where a sequence has several parts, then the tops and sums of the rows,
+  float2* stats;                    // and where the parts of every sequence are
+  int2* places;
   float scale, scale_log2;          // |scale|, and that / ln 2
   uint32_t sign;                    // 0x80008000 for a negative scale: the queries change sign
   Divide by_group;
-  int nodes, seen_nodes, words, kv_heads, group, rows, row_tiles, splits, eights;
+  int batch, nodes, seen_nodes, words, kv_heads, group, rows, row_tiles, slots, unit, eights;
 };
 
 template <typename T>
@@ -186,6 +186,111 @@ __device__ __forceinline__ void add_values(Rows<MT, D / 16>& r, const Words<D / 
   }
 }
 
+// How the tokens are dealt out.  For every kv head and tile of rows a launch has `slots` workgroups; all take parts of the same number of steps, the smallest
+// multiple of `unit` with which every sequence gets the parts it needs (at least one, which writes the zeros of a row that sees nothing).  With parts of
+// c steps the sequences need less than total / c + batch of them, so c = total / (slots - batch + 1) will do.  The lengths are on the device, so every
+// workgroup works this out for itself, 64 sequences at a time.
+struct Share {
+  int b, len, first, last;      // sequence (-1: nothing is left for this slot), its tokens in the cache, steps
+  int part, parts;              // of the sequence
+};
+
+__device__ __forceinline__ int tokens_of(const AttentionArgs& a, int b) { return min(max(a.lens[b], 0), a.cache.pages_per_seq * a.cache.page); }
+__device__ __forceinline__ int steps_of(int tokens) { return (int)(((uint32_t)tokens + kAttTile - 1) / kAttTile); }
+
+__device__ __forceinline__ Share share_of(const AttentionArgs& a, int slot) {
+  const int lane = threadIdx.x & 63, extra = steps_of(a.seen_nodes);
+  int64_t total = 0;
+  int len = 0;
+  for (int first = 0; first < a.batch; first += 64) {
+    const int b = first + lane;
+    len = b < a.batch ? tokens_of(a, b) : 0;
+    total += b < a.batch ? steps_of(len) + extra : 0;
+  }
+#pragma unroll
+  for (int i = 1; i < 64; i *= 2) total += __shfl_xor(total, i);
+  uint32_t each;      // steps of a part
+  const int64_t over = a.slots - a.batch + 1;
+  if (total >> 32 == 0)
+    each = ((uint32_t)total + (uint32_t)over - 1) / (uint32_t)over;      // (total is below 2^32 less slots but for more than 30 10^9 tokens)
+  else
+    each = (uint32_t)((total + over - 1) / over);
+  each = max(each + a.unit - 1, (uint32_t)a.unit) / a.unit * a.unit;
+  int before = 0;
+  for (int first = 0; first < a.batch; first += 64) {
+    const int b = first + lane;
+    if (a.batch > 64) len = b < a.batch ? tokens_of(a, b) : 0;
+    const int steps = steps_of(len) + extra, n = b < a.batch ? max(1, (int)((steps + each - 1) / each)) : 0;
+    int upto = n;
+#pragma unroll
+    for (int i = 1; i < 64; i *= 2) {
+      const int v = __shfl_up(upto, i);
+      if (lane >= i) upto += v;
+    }
+    upto += before;
+    const uint64_t mine = __ballot(slot < upto && slot >= upto - n);
+    if (mine != 0) {
+      const int l = __ffsll((unsigned long long)mine) - 1, part = slot - __shfl(upto - n, l), s = __shfl(steps, l);
+      return {first + l, __shfl(len, l), (int)(part * each), min((int)((part + 1) * each), s), part, __shfl(n, l)};
+    }
+    before = __shfl(upto, 63);
+  }
+  return {-1, 0, 0, 0, 0, 0};
+}
+
+// Where the rows of a workgroup's part lie among the parts.
+__device__ __forceinline__ int64_t part_row(const AttentionArgs& a, int slot, int h, int row_tile, int rows_of_tile) {
+  return (((int64_t)slot * a.kv_heads + h) * a.row_tiles + row_tile) * rows_of_tile;
+}
+
+// The nodes among t ... t + 7 that a node sees, a bit each.
+__device__ __forceinline__ uint32_t seen_of(const AttentionArgs& a, int b, int node, int t) {
+  if (node < 0 || t >= a.seen_nodes) return 0u;
+  if (a.mask == nullptr) return node < t ? 0u : node - t >= 7 ? 0xffu : (2u << (node - t)) - 1u;
+  return (uint32_t)(a.mask[b * a.mask_stride + node * a.words + (t >> 6)] >> (t & 63)) & 0xffu;
+}
+
+// Token t of a sequence (old: of its context, which is not empty; else one of its nodes, `stride` elements apart): where it starts, in elements, or false and 0, which is
+// a place that can be read.
+__device__ __forceinline__ bool find_token(const AttentionArgs& a, int b, int len, bool old, int t, int64_t stride, int64_t* at) {
+  bool ok;
+  if (old) {
+    const int c = min(t, len - 1);
+    const uint32_t j = a.cache.by_page.of(c);
+    const int page = a.cache.table == nullptr ? b : a.cache.table[b * a.cache.table_stride + j];
+    ok = t < len && (uint32_t)page < (uint32_t)a.cache.pages;
+    *at = ok ? page * a.cache.page_stride + (int64_t)(c - j * (uint32_t)a.cache.page) * a.cache.token_stride : 0;
+  } else {
+    ok = t < a.seen_nodes;
+    *at = ok ? t * stride : 0;
+  }
+  return ok;
+}
+
+// The rows that see node t add their weights times those of its values that are no finite numbers; `from`: the 4 DV values that a lane has, value 4 DV g + j
+// in o[j % DV][j / DV] (PLAIN) or 16 (j / 4) + 4 g + j % 4 in o[j / 4][j % 4].
+template <typename T, int D, int MT, bool PLAIN>
+__device__ __forceinline__ void add_odd_values(Rows<MT, D / 16>& r, const T* values, int t, const u32x4 (&w)[MT], const uint32_t (&seen)[MT]) {
+  constexpr int DV = D / 16;
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, lane_of = (t >> 3) * 16 + n, i = t & 7;
+  typedef T two __attribute__((ext_vector_type(2)));
+  float by[MT];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const uint32_t word = __shfl(i < 4 ? (i < 2 ? w[mt][0] : w[mt][1]) : (i < 6 ? w[mt][2] : w[mt][3]), lane_of);
+    const two both = __builtin_bit_cast(two, word);
+    by[mt] = (__shfl(seen[mt], lane_of) >> i) & 1 ? (float)(i & 1 ? both[1] : both[0]) : 0.f;
+  }
+#pragma unroll
+  for (int j = 0; j < 4 * DV; ++j) {
+    const float value = (float)values[PLAIN ? 4 * DV * g + j : 16 * (j / 4) + 4 * g + j % 4];
+    if (!__builtin_isfinite(value))
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+        if (by[mt] != 0.f) r.o[mt][PLAIN ? j % DV : j / 4][PLAIN ? j / DV : j % 4] += by[mt] * value;
+  }
+}
+
 // One workgroup: up to 16 * MT rows (node, query head of one kv head) of one sequence over one of `splits` parts of its tokens; its wavefronts take
 // steps of 32 tokens in turns and meet at the end.  The weights are rounded to the type of V for the value product (their sum is not): half a step
 // of each, so the error is a mean of independent roundings, below the one rounding of the result.
@@ -196,15 +301,13 @@ __global__ void __launch_bounds__(kAttWaves * 64, D <= 128 ? 2 : 1) tree_attenti
   __shared__ float2 tops[kAttWaves][MT][16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
   uint32_t id = blockIdx.x;
-  const int split = id % a.splits;
-  id /= a.splits;
-  const int row_tile = id % a.row_tiles;
-  id /= a.row_tiles;
-  const int h = id % a.kv_heads, b = id / a.kv_heads;
-  const int len = min(max(a.lens[b], 0), a.cache.pages_per_seq * a.cache.page);
-  const int old_steps = (len + kAttTile - 1) / kAttTile, steps = old_steps + (a.seen_nodes + kAttTile - 1) / kAttTile;
-  const int each = (steps + a.splits - 1) / a.splits;
-  const int first = split * each, last = min(first + each, steps);
+  const int h = id % a.kv_heads;
+  id /= a.kv_heads;
+  const int row_tile = id % a.row_tiles, slot = id / a.row_tiles;
+  const Share share = share_of(a, slot);
+  if (share.b < 0) return;
+  const int b = share.b, len = share.len, old_steps = steps_of(len), first = share.first, last = share.last;
+  if (share.part == 0 && h == 0 && row_tile == 0 && threadIdx.x == 0 && a.places != nullptr) a.places[b] = make_int2(slot, share.parts);
 
   u32x4 q[MT][KK];
   int node[MT];
@@ -267,33 +370,18 @@ __global__ void __launch_bounds__(kAttWaves * 64, D <= 128 ? 2 : 1) tree_attenti
       ask(step + kAttWaves);
     } else {
       // Tokens that are not there are read from a place that is (node 0, token 0 of page 0) and count as zeros that nobody sees.
-      auto find = [&](int t, int64_t stride, int64_t* at) {
-        bool ok;
-        if (old) {
-          const int c = min(t, len - 1);      // a step before old_steps has a token, so len is at least 1
-          const uint32_t j = a.cache.by_page.of(c);
-          int page = b;
-          if (a.cache.table != nullptr) page = a.cache.table[b * a.cache.table_stride + j];
-          ok = t < len && (uint32_t)page < (uint32_t)a.cache.pages;
-          *at = ok ? page * a.cache.page_stride + (int64_t)(c - j * (uint32_t)a.cache.page) * a.cache.token_stride : 0;
-        } else {
-          ok = t < a.seen_nodes;
-          *at = ok ? t * stride : 0;
-        }
-        return ok;
-      };
       uint32_t valid = 0;
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         int64_t at;
-        find(t0 + k_token + 4 * half, a.k_new.token_stride, &at);
+        find_token(a, b, len, old, t0 + k_token + 4 * half, a.k_new.token_stride, &at);
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) k[half][kk] = *reinterpret_cast<const u32x4*>(base_k + 2 * (at + 32 * kk + 8 * g));
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         int64_t at;
-        const bool ok = find(t0 + 8 * g + i, a.v_new.token_stride, &at);
+        const bool ok = find_token(a, b, len, old, t0 + 8 * g + i, a.v_new.token_stride, &at);
         valid |= (uint32_t)ok << i;
         v[i] = load_words<N>(base_v + 2 * (at + DV * n));
 #pragma unroll
@@ -301,16 +389,7 @@ __global__ void __launch_bounds__(kAttWaves * 64, D <= 128 ? 2 : 1) tree_attenti
       }
       if (step + kAttWaves < full_steps) ask(step + kAttWaves);
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        seen[mt] = valid;
-        if (!old) {
-          const int t = t0 + 8 * g;
-          if (a.mask == nullptr)
-            seen[mt] &= node[mt] < t ? 0u : node[mt] - t >= 7 ? 0xffu : (2u << (node[mt] - t)) - 1u;
-          else
-            seen[mt] &= node[mt] < 0 || t >= a.seen_nodes ? 0u : (uint32_t)(a.mask[b * a.mask_stride + node[mt] * a.words + (t >> 6)] >> (t & 63));
-        }
-      }
+      for (int mt = 0; mt < MT; ++mt) seen[mt] = old ? valid : valid & seen_of(a, b, node[mt], t0 + 8 * g);
     }
     attend_step<T, D, MT>(rows, q, k, a.scale_log2, all, seen, w);
     if (!old) {
@@ -323,26 +402,8 @@ __global__ void __launch_bounds__(kAttWaves * 64, D <= 128 ? 2 : 1) tree_attenti
         for (int j = 0; j < N; ++j) odd = odd || numbers<T>(v[i].w[j]) != v[i].w[j];
       if (__any(odd)) {
 #pragma unroll 1
-        for (int t = 0; t < min(kAttTile, a.seen_nodes - t0); ++t) {
-          const T* from = reinterpret_cast<const T*>(base_v) + (t0 + t) * a.v_new.token_stride + 4 * DV * g;
-          const int lane_of = (t >> 3) * 16 + n, i = t & 7;
-          float by[MT];
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt) {
-            const uint32_t two = __shfl(i < 4 ? (i < 2 ? w[mt][0] : w[mt][1]) : (i < 6 ? w[mt][2] : w[mt][3]), lane_of);
-            typedef T half_pair __attribute__((ext_vector_type(2)));
-            const half_pair both = __builtin_bit_cast(half_pair, two);
-            by[mt] = (__shfl(seen[mt], lane_of) >> i) & 1 ? (float)(i & 1 ? both[1] : both[0]) : 0.f;
-          }
-#pragma unroll
-          for (int j = 0; j < 4 * DV; ++j) {
-            const float value = (float)from[j];
-            if (!__builtin_isfinite(value))
-#pragma unroll
-              for (int mt = 0; mt < MT; ++mt)
-                if (by[mt] != 0.f) rows.o[mt][j % DV][j / DV] += by[mt] * value;
-          }
-        }
+        for (int t = 0; t < min(kAttTile, a.seen_nodes - t0); ++t)
+          add_odd_values<T, D, MT, true>(rows, reinterpret_cast<const T*>(base_v) + (t0 + t) * a.v_new.token_stride, t, w, seen);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
@@ -385,7 +446,7 @@ __global__ void __launch_bounds__(kAttWaves * 64, D <= 128 ? 2 : 1) tree_attenti
     }
     if (r >= a.rows) continue;
     const int d = DV * (4 * g + wave);
-    if (a.splits == 1) {
+    if (share.parts == 1) {
       const float by = m == -INFINITY ? 0.f : 1.f / s;
       uint32_t words[N];
 #pragma unroll
@@ -394,7 +455,7 @@ __global__ void __launch_bounds__(kAttWaves * 64, D <= 128 ? 2 : 1) tree_attenti
       store_words(a.out.data + 2 * (b * a.out.batch_stride + node[mt] * a.out.token_stride + head * a.out.head_stride + d), words);
       if (a.lse != nullptr && g == 0 && wave == 0) a.lse[((int64_t)b * a.nodes + node[mt]) * (a.kv_heads * a.group) + head] = log_sum<T>(m, s, a.scale);
     } else {
-      const int64_t row = (int64_t)blockIdx.x * R + mt * 16 + n;
+      const int64_t row = part_row(a, slot, h, row_tile, R) + mt * 16 + n;
       uint32_t words[DV];
 #pragma unroll
       for (int j = 0; j < DV; ++j) words[j] = __builtin_bit_cast(uint32_t, e[j]);
@@ -404,45 +465,264 @@ __global__ void __launch_bounds__(kAttWaves * 64, D <= 128 ? 2 : 1) tree_attenti
   }
 }
 
-// The parts of a row meet: one wavefront to a row.
+// The parts of a row meet: one wavefront to a row.  Tops first, then sums of eight parts at a time, so that their loads are on the way together.
 template <typename T, int D>
-__global__ void __launch_bounds__(256) tree_attention_join_kernel(const AttentionArgs a, int rows_of_tile, int64_t all_rows) {
+__global__ void __launch_bounds__(256) tree_attention_join_kernel(const AttentionArgs a, int rows_of_tile, Divide by_rows, Divide by_heads, Divide by_tile, uint32_t all_rows) {
   const int lane = threadIdx.x & 63;
-  const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);      // [batch][kv head][row]
+  const uint32_t id = blockIdx.x * 4 + (threadIdx.x >> 6);      // [batch][kv head][row]
   if (id >= all_rows) return;
-  const int bh = (int)(id / a.rows), r = (int)(id - (int64_t)bh * a.rows);
-  const int row_tile = r / rows_of_tile;
-  const int64_t first = ((int64_t)bh * a.row_tiles + row_tile) * a.splits * rows_of_tile + (r - row_tile * rows_of_tile);
-  const float2 mine = lane < a.splits ? a.stats[first + (int64_t)lane * rows_of_tile] : make_float2(-INFINITY, 0.f);
-  float m = mine.x;
-#pragma unroll
-  for (int i = 1; i < 64; i *= 2) m = fmaxf(m, __shfl_xor(m, i));
-  const float f = mine.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mine.x - m) * a.scale_log2);
-  float s = f * mine.y;
-#pragma unroll
-  for (int i = 1; i < 64; i *= 2) s += __shfl_xor(s, i);
+  const uint32_t bh = by_rows.of(id), r = id - bh * a.rows, b = by_heads.of(bh), h = bh - b * a.kv_heads, row_tile = by_tile.of(r);
+  const int2 place = a.places[b];
+  const int parts = place.y;
+  if (parts == 1) return;      // its workgroup has written the result
+  const int64_t first = part_row(a, place.x, h, row_tile, rows_of_tile) + (r - row_tile * rows_of_tile), step = (int64_t)a.kv_heads * a.row_tiles * rows_of_tile;
   constexpr int P = D >= 128 ? D / 128 : 1;      // a lane has two neighbouring elements of every 128 (D below 128: the first D / 2 lanes)
-  float e[P * 2] = {};
-  const bool active = D >= 128 || lane < D / 2;
-  for (int i = 0; i < a.splits; ++i) {
-    const float by = __shfl(f, i);
-    if (by == 0.f || !active) continue;
-    const float* p = a.part + (first + (int64_t)i * rows_of_tile) * D + lane * 2;
+  const int at = D >= 128 || lane < D / 2 ? lane * 2 : 0;
+  float m = -INFINITY, s = 0.f, e[P * 2] = {};
+  for (int p0 = 0; p0 < parts; p0 += 64) {
+    const float2 mine = p0 + lane < parts ? a.stats[first + (p0 + lane) * step] : make_float2(-INFINITY, 0.f);
+    float top = mine.x;
 #pragma unroll
-    for (int j = 0; j < P; ++j) {
-      const float2 v = *reinterpret_cast<const float2*>(p + j * 128);
-      e[2 * j] += by * v.x;
-      e[2 * j + 1] += by * v.y;
+    for (int i = 1; i < 64; i *= 2) top = fmaxf(top, __shfl_xor(top, i));
+    const float next = fmaxf(m, top), less = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - next) * a.scale_log2);
+    const float f = mine.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mine.x - next) * a.scale_log2);
+    float add = f * mine.y;
+#pragma unroll
+    for (int i = 1; i < 64; i *= 2) add += __shfl_xor(add, i);
+    m = next;
+    s = s * less + add;
+#pragma unroll
+    for (int j = 0; j < 2 * P; ++j) e[j] *= less;
+    const int here = min(64, parts - p0);
+    for (int i0 = 0; i0 < here; i0 += 8) {
+      float2 v[8][P];
+      float by[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int part = min(i0 + i, here - 1);
+        by[i] = i0 + i < here ? __shfl(f, part) : 0.f;
+        const float* p = a.part + (first + (p0 + part) * step) * D + at;
+#pragma unroll
+        for (int j = 0; j < P; ++j) v[i][j] = *reinterpret_cast<const float2*>(p + j * 128);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < P; ++j) {      // (a part that its rows saw nothing of has not been written)
+          e[2 * j] += by[i] == 0.f ? 0.f : by[i] * v[i][j].x;
+          e[2 * j + 1] += by[i] == 0.f ? 0.f : by[i] * v[i][j].y;
+        }
     }
   }
   const float by = m == -INFINITY ? 0.f : 1.f / s;
-  const int node = a.by_group.of(r), h = bh % a.kv_heads, b = bh / a.kv_heads, head = h * a.group + r - node * a.group;
-  char* out = a.out.data + 2 * (b * a.out.batch_stride + node * a.out.token_stride + head * a.out.head_stride + lane * 2);
-  if (active)
+  const int node = a.by_group.of(r), head = h * a.group + r - node * a.group;
+  char* out = a.out.data + 2 * (b * a.out.batch_stride + node * a.out.token_stride + head * a.out.head_stride + at);
+  if (D >= 128 || lane < D / 2)
 #pragma unroll
     for (int j = 0; j < P; ++j) *reinterpret_cast<uint32_t*>(out + 256 * j) = pack2<T>(e[2 * j] * by, e[2 * j + 1] * by);
-  if (a.lse != nullptr && lane == 0)
-    a.lse[((int64_t)b * a.nodes + node) * (a.kv_heads * a.group) + head] = log_sum<T>(m, s, a.scale);
+  if (a.lse != nullptr && lane == 0) a.lse[((int64_t)b * a.nodes + node) * (a.kv_heads * a.group) + head] = log_sum<T>(m, s, a.scale);
+}
+
+// The kernel for many rows: WAVES wavefronts with 16 * MT rows each take every step together.  K and V of a step are loaded once for all of them and kept
+// in LDS, two steps in turns: the next step's are asked for before this one's products and written behind them.
+//   K: pieces of 8 elements [D / 8][32 tokens], 16 bytes further from one piece to the next than the tokens take, so that neither the
+//      writing (a row of the cache at a time) nor the reading (16 tokens of a piece) meets itself in a bank;
+//   V: turned while it is written: [4 groups of 8 tokens][D] of 16 bytes, as the value product reads it.
+// A lane's results are the values 16 j + 4 g ... + 3 of its row, j < D / 16.
+template <typename T, int D, int MT, int WAVES>
+__global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) tree_attention_wide_kernel(const AttentionArgs a) {
+  constexpr int KK = D / 32, DV = D / 16, R = 16 * MT * WAVES, THREADS = WAVES * 64;
+  constexpr int U = (4 * D + THREADS - 1) / THREADS;      // units of 16 bytes of K, and of V, to a thread
+  constexpr int PIECE = kAttTile * 16 + 16;
+  __shared__ __align__(16) char lds_k[2][D / 8 * PIECE], lds_v[2][4 * D * 16];
+  __shared__ uint32_t lds_valid[2], lds_odd[2];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
+  uint32_t id = blockIdx.x;
+  const int h = id % a.kv_heads;
+  id /= a.kv_heads;
+  const int row_tile = id % a.row_tiles, slot = id / a.row_tiles;
+  const Share share = share_of(a, slot);
+  if (share.b < 0) return;
+  const int b = share.b, len = share.len, old_steps = steps_of(len), first = share.first, last = share.last;
+  if (share.part == 0 && h == 0 && row_tile == 0 && threadIdx.x == 0 && a.places != nullptr) a.places[b] = make_int2(slot, share.parts);
+
+  u32x4 q[MT][KK];
+  int node[MT];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const int r = row_tile * R + wave * 16 * MT + mt * 16 + n;
+    node[mt] = -1;
+    if (r < a.rows) {
+      node[mt] = a.by_group.of(r);
+      const char* p = a.q.data + 2 * (b * a.q.batch_stride + node[mt] * a.q.token_stride + (h * a.group + r - node[mt] * a.group) * a.q.head_stride + 8 * g);
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) q[mt][kk] = *reinterpret_cast<const u32x4*>(p + 64 * kk) ^ a.sign;
+    } else {
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) q[mt][kk] = u32x4{0, 0, 0, 0};
+    }
+  }
+  const bool works = row_tile * R + wave * 16 * MT < a.rows;      // a wavefront without rows only loads
+  Rows<MT, DV> rows;
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    rows.top[mt] = -INFINITY;
+    rows.sum[mt] = 0.f;
+#pragma unroll
+    for (int j = 0; j < DV; ++j) rows.o[mt][j] = f32x4{0, 0, 0, 0};
+  }
+
+  // What this thread loads of a step: unit u of K is piece u % (D / 8) of token u / (D / 8); of V it is the elements 2 (u % (D / 2)) and the next of four tokens.
+  const char *cache_k = a.cache.k + 2 * h * a.cache.head_stride, *cache_v = a.cache.v + 2 * h * a.cache.head_stride;
+  const int full_steps = a.eights ? min(last, len / kAttTile) : 0;
+  int id_k[U], id_v[U], id_t = 0;      // page ids, asked for a step ahead: of the tokens of the units, and of token lane % 32
+  auto ask = [&](int step) {
+    if (step >= full_steps) return;
+    const uint32_t t0 = step * kAttTile;
+    auto page_of = [&](uint32_t t) { return a.cache.table == nullptr ? b : a.cache.table[b * a.cache.table_stride + a.cache.by_page.of(t)]; };
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int u = min((int)threadIdx.x + i * THREADS, 4 * D - 1);
+      id_k[i] = page_of(t0 + u / (D / 8));
+      id_v[i] = page_of(t0 + 4 * (u / (D / 2)));
+    }
+    id_t = page_of(t0 + (lane & 31));
+  };
+  u32x4 load_k[U];
+  uint32_t load_v[U][4], valid = 0;
+  auto load = [&](int step) {
+    const bool old = step < old_steps;
+    const int t0 = (old ? step : step - old_steps) * kAttTile;
+    if (step < full_steps) {
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int u = min((int)threadIdx.x + i * THREADS, 4 * D - 1);
+        const bool ok_k = (uint32_t)id_k[i] < (uint32_t)a.cache.pages, ok_v = (uint32_t)id_v[i] < (uint32_t)a.cache.pages;
+        const uint32_t tk = t0 + u / (D / 8), tv = t0 + 4 * (u / (D / 2));
+        const int64_t at_k = ok_k ? id_k[i] * a.cache.page_stride + (int64_t)(tk - a.cache.by_page.of(tk) * a.cache.page) * a.cache.token_stride : 0;
+        const int64_t at_v = ok_v ? id_v[i] * a.cache.page_stride + (int64_t)(tv - a.cache.by_page.of(tv) * a.cache.page) * a.cache.token_stride : 0;
+        load_k[i] = *reinterpret_cast<const u32x4*>(cache_k + 2 * at_k + 16 * (u % (D / 8)));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t w = *reinterpret_cast<const uint32_t*>(cache_v + 2 * (at_v + (ok_v ? j : 0) * a.cache.token_stride) + 4 * (u % (D / 2)));
+          load_v[i][j] = ok_v ? w : 0u;
+        }
+      }
+      valid = (uint32_t)__ballot((uint32_t)id_t < (uint32_t)a.cache.pages);
+    } else {
+      const char *base_k = old ? cache_k : a.k_new.data + 2 * (b * a.k_new.batch_stride + h * a.k_new.head_stride),
+                 *base_v = old ? cache_v : a.v_new.data + 2 * (b * a.v_new.batch_stride + h * a.v_new.head_stride);
+      int64_t at;
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int u = min((int)threadIdx.x + i * THREADS, 4 * D - 1);
+        find_token(a, b, len, old, t0 + u / (D / 8), a.k_new.token_stride, &at);
+        load_k[i] = *reinterpret_cast<const u32x4*>(base_k + 2 * at + 16 * (u % (D / 8)));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const bool ok = find_token(a, b, len, old, t0 + 4 * (u / (D / 2)) + j, a.v_new.token_stride, &at);
+          const uint32_t w = *reinterpret_cast<const uint32_t*>(base_v + 2 * at + 4 * (u % (D / 2)));
+          load_v[i][j] = ok ? w : 0u;
+        }
+      }
+      valid = (uint32_t)__ballot(find_token(a, b, len, old, t0 + (lane & 31), a.k_new.token_stride, &at));
+    }
+    ask(step + 1);
+  };
+  // what is no finite number among a node's values leaves the product (see add_odd_values)
+  auto keep = [&](int step, int buffer) {
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int u = threadIdx.x + i * THREADS;
+      if (4 * D % THREADS != 0 && u >= 4 * D) continue;
+      if (step >= old_steps)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t w = numbers<T>(load_v[i][j]);
+          odd = odd || w != load_v[i][j];
+          load_v[i][j] = w;
+        }
+      const int token = u / (D / 8), place = ((token >> 2) & 1) * 16 + 4 * (token >> 3) + (token & 3);      // as attend_step numbers the tokens
+      *reinterpret_cast<u32x4*>(lds_k[buffer] + u % (D / 8) * PIECE + place * 16) = load_k[i];
+      const int four = u / (D / 2), d = 2 * (u % (D / 2));
+      char* to = lds_v[buffer] + ((four >> 1) * D + d) * 16 + (four & 1) * 8;
+      const uint32_t *v = load_v[i];
+      *reinterpret_cast<uint2*>(to) = make_uint2(__builtin_amdgcn_perm(v[1], v[0], 0x05040100u), __builtin_amdgcn_perm(v[3], v[2], 0x05040100u));
+      *reinterpret_cast<uint2*>(to + 16) = make_uint2(__builtin_amdgcn_perm(v[1], v[0], 0x07060302u), __builtin_amdgcn_perm(v[3], v[2], 0x07060302u));
+    }
+    if (threadIdx.x == 0) lds_valid[buffer] = valid;
+    if (odd) lds_odd[buffer] = step + 1;      // of this step; whatever else stands there is another's
+  };
+
+  if (threadIdx.x < 2) lds_odd[threadIdx.x] = 0;
+  __syncthreads();
+  if (first < last) {
+    ask(first);
+    load(first);
+    keep(first, 0);
+  }
+  __syncthreads();
+  for (int step = first; step < last; ++step) {
+    const int buffer = (step - first) & 1;
+    if (step + 1 < last) load(step + 1);
+    if (works) {
+      const uint32_t now = lds_valid[buffer];
+      const bool old = step < old_steps, all = old && now == 0xffffffffu;
+      const int t0 = (step - old_steps) * kAttTile;
+      u32x4 k[2][KK], w[MT];
+      uint32_t seen[MT];
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        seen[mt] = (now >> (8 * g)) & 0xffu;
+        if (!old) seen[mt] &= seen_of(a, b, node[mt], t0 + 8 * g);
+      }
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) k[half][kk] = *reinterpret_cast<const u32x4*>(lds_k[buffer] + (4 * kk + g) * PIECE + (half * 16 + n) * 16);
+      attend_step<T, D, MT>(rows, q, k, a.scale_log2, all, seen, w);
+      if (!old && lds_odd[buffer] == (uint32_t)step + 1) {
+#pragma unroll 1
+        for (int t = 0; t < min(kAttTile, a.seen_nodes - t0); ++t)
+          add_odd_values<T, D, MT, false>(rows, reinterpret_cast<const T*>(a.v_new.data) + b * a.v_new.batch_stride + h * a.v_new.head_stride + (t0 + t) * a.v_new.token_stride,
+                                          t, w, seen);
+      }
+#pragma unroll
+      for (int j = 0; j < DV; ++j) {
+        const u32x4 v = *reinterpret_cast<const u32x4*>(lds_v[buffer] + (g * D + 16 * j + n) * 16);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) rows.o[mt][j] = Matrix<T>::mad(v, w[mt], rows.o[mt][j]);
+      }
+    }
+    if (step + 1 < last) keep(step + 1, buffer ^ 1);
+    __syncthreads();
+  }
+  if (!works) return;
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const int in_tile = wave * 16 * MT + mt * 16 + n, r = row_tile * R + in_tile;
+    float s = rows.sum[mt];
+    s += __shfl_xor(s, 16);
+    s += __shfl_xor(s, 32);
+    if (r >= a.rows) continue;
+    const float m = rows.top[mt];
+    if (share.parts == 1) {
+      const float by = m == -INFINITY ? 0.f : 1.f / s;
+      const int head = h * a.group + r - node[mt] * a.group;
+      char* out = a.out.data + 2 * (b * a.out.batch_stride + node[mt] * a.out.token_stride + head * a.out.head_stride + 4 * g);
+#pragma unroll
+      for (int j = 0; j < DV; ++j)
+        *reinterpret_cast<uint2*>(out + 32 * j) = make_uint2(pack2<T>(rows.o[mt][j][0] * by, rows.o[mt][j][1] * by), pack2<T>(rows.o[mt][j][2] * by, rows.o[mt][j][3] * by));
+      if (a.lse != nullptr && g == 0) a.lse[((int64_t)b * a.nodes + node[mt]) * (a.kv_heads * a.group) + head] = log_sum<T>(m, s, a.scale);
+    } else {
+      const int64_t row = part_row(a, slot, h, row_tile, R) + in_tile;
+      if (m != -INFINITY)
+#pragma unroll
+        for (int j = 0; j < DV; ++j) *reinterpret_cast<f32x4*>(a.part + row * D + 16 * j + 4 * g) = rows.o[mt][j];
+      if (g == 0) a.stats[row] = make_float2(m, s);
+    }
+  }
 }
 
 }  // namespace dpllm
