@@ -125,7 +125,8 @@ int dpllm_tree_attention(const dpllm_cache* cache, int layer, int batch, int nod
   a.scale = std::fabs(scale);
   a.scale_log2 = (float)(std::fabs((double)scale) * 1.44269504088896340736);
   a.sign = scale < 0 ? 0x80008000u : 0u;
-  a.eights = cache->page % 8 == 0 || cache->pages_per_seq == 1;
+  a.keep = scale == 0 ? 0u : ~0u;
+  if (scale == 0) a.scale_log2 = 1.f;      // scores of 0, and a scale that the tops can be measured with
   a.group = heads / cache->heads;
   a.by_group = Divide::by(a.group);
   a.nodes = nodes;

@@ -21,9 +21,9 @@ struct AttentionArgs {
   float2* stats;                    // and where the parts of every sequence are
   int2* places;
   float scale, scale_log2;          // |scale|, and that / ln 2
-  uint32_t sign;                    // 0x80008000 for a negative scale: the queries change sign
+  uint32_t sign, keep;              // sign: 0x80008000 for a negative scale, with which the queries change theirs; keep: 0 for a scale of 0, of which they are zeros
   Divide by_group;
-  int batch, nodes, seen_nodes, words, kv_heads, group, rows, row_tiles, slots, unit, eights;
+  int batch, nodes, seen_nodes, words, kv_heads, group, rows, row_tiles, slots, unit;
 };
 
 template <typename T>
@@ -115,74 +115,93 @@ __device__ __forceinline__ float row_max(float x) {
 }
 
 // What a wavefront has of its rows: the weighted values, the weights' sum, and the score `top` they are relative to: a weight is
-// 2^((x - top) scale + lift).
+// 2^((x - top) scale + lift), formed as 2^(x scale + from).
 template <int MT, int DV>
 struct Rows {
   f32x4 o[MT][DV];
-  float sum[MT], top[MT];      // sum: of the lane's own tokens
+  float sum[MT], top[MT], from[MT];      // sum: of the lane's own tokens
+  bool huge;                             // some top times scale / ln 2 may be past the floats though the scores are not
+  __device__ __forceinline__ void clear(float lift) {
+    huge = false;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      top[mt] = -INFINITY;
+      from[mt] = lift;
+      sum[mt] = 0.f;
+#pragma unroll
+      for (int j = 0; j < DV; ++j) o[mt][j] = f32x4{0, 0, 0, 0};
+    }
+  }
 };
 
-// One step of 32 tokens for 16 * MT rows.  Everything stays in registers: the lanes of the score product K Q^T (16 x 16 x 32
-// matrix instructions; lane l holds row l % 16 of Q and, of a result, the tokens 4 (l / 16) ... + 3) are those that the value product
-// V^T P^T wants its weights in, if the first 16 tokens of a step are numbered 8 (m / 4) + m % 4 and the second 16 four more: lane
-// group l / 16 then holds the weights of the tokens 8 (l / 16) ... + 7.  V is loaded as it lies, D / 16 elements of 8 tokens to a lane, and turned
-// inside the lane, 16 bits at a time.
+// The weights of one step of 32 tokens for 16 * MT rows, in the lanes that the value product wants them in: with 16 x 16 x 32 matrix instructions lane l
+// holds row l % 16 of Q and, of a result of K Q^T, the tokens 4 (l / 16) ... + 3; if the first 16 tokens of a step are numbered 8 (m / 4) + m % 4 and the second 16
+// four more, lane group l / 16 holds the weights of the tokens 8 (l / 16) ... + 7, which is the operand of V^T P^T.
 // `top` follows the largest score only when that has left it behind by 2^kSlack: in most steps no row's has, and the exchange between
-// lanes and the scaling of o are skipped.
-template <typename T, int D, int MT>
-__device__ __forceinline__ void attend_step(Rows<MT, D / 16>& r, const u32x4 (&q)[MT][D / 32], const u32x4 (&k)[2][D / 32], float scale_log2, bool all,
-                                            const uint32_t (&seen)[MT], u32x4 (&w)[MT]) {
+// lanes and the scaling of o are skipped.  ALL: every row sees every token.
+template <typename T, int D, int MT, bool ALL>
+__device__ __forceinline__ void weigh(Rows<MT, D / 16>& r, const u32x4 (&q)[MT][D / 32], const u32x4 (&k)[2][D / 32], float scale_log2,
+                                      const uint32_t (&seen)[MT], u32x4 (&w)[MT]) {
   constexpr int KK = D / 32, DV = D / 16;
   constexpr float kLift = Matrix<T>::kLift, kSlack = Matrix<T>::kSlack;
+  f32x4 s[MT][2];
+  float most[MT];
+  bool behind = false;
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
-    f32x4 s0 = {0, 0, 0, 0}, s1 = {0, 0, 0, 0};
+    s[mt][0] = s[mt][1] = f32x4{0, 0, 0, 0};
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) {
-      s0 = Matrix<T>::mad(k[0][kk], q[mt][kk], s0);
-      s1 = Matrix<T>::mad(k[1][kk], q[mt][kk], s1);
+      s[mt][0] = Matrix<T>::mad(k[0][kk], q[mt][kk], s[mt][0]);
+      s[mt][1] = Matrix<T>::mad(k[1][kk], q[mt][kk], s[mt][1]);
     }
-    if (!all) {
+  }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        s0[i] = (seen[mt] >> i) & 1 ? s0[i] : -INFINITY;
-        s1[i] = (seen[mt] >> (4 + i)) & 1 ? s1[i] : -INFINITY;
-      }
+  for (int mt = 0; mt < MT; ++mt) {
+    if constexpr (!ALL) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s[mt][i / 4][i % 4] = (seen[mt] >> i) & 1 ? s[mt][i / 4][i % 4] : -INFINITY;
     }
-    float most = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
-    if (__any((most - r.top[mt]) * scale_log2 > kSlack)) {      // (top is -infinity at first, and no score at all is no reason: NaN > is false)
-      const float next = fmaxf(r.top[mt], row_max(most));
+    most[mt] = s[mt][0][0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) most[mt] = fmaxf(most[mt], s[mt][i / 4][i % 4]);
+    behind = behind || (most[mt] - r.top[mt]) * scale_log2 > kSlack;      // (a row without a score yet has NaN here if it gets none)
+  }
+  if (__any(behind)) {
+    bool huge = false;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      const float next = fmaxf(r.top[mt], row_max(most[mt]));
       const float less = r.top[mt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((r.top[mt] - next) * scale_log2);
       r.top[mt] = next;
+      r.from[mt] = next == -INFINITY ? kLift : __builtin_fmaf(-next, scale_log2, kLift);
+      huge = huge || (next != -INFINITY && __builtin_fabsf(next) > 1e38f);
       r.sum[mt] *= less;
 #pragma unroll
       for (int j = 0; j < DV; ++j) r.o[mt][j] *= less;
     }
-    const float top = r.top[mt] == -INFINITY ? 0.f : r.top[mt], from = kLift - top * scale_log2;
+    r.huge = __any(huge);
+  }
+  if (r.huge) {
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        s[mt][i / 4][i % 4] = r.top[mt] == -INFINITY ? -INFINITY : (s[mt][i / 4][i % 4] - r.top[mt]) * scale_log2 + kLift;
+  } else {
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s[mt][i / 4][i % 4] = __builtin_fmaf(s[mt][i / 4][i % 4], scale_log2, r.from[mt]);
+  }
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
     float x[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf(i < 4 ? s0[i & 3] : s1[i & 3], scale_log2, from);
-    if (__any(__builtin_fabsf(top) > 1e38f)) {      // top * scale / ln 2 may be past the floats though the scores are not
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = ((i < 4 ? s0[i & 3] : s1[i & 3]) - top) * scale_log2 + kLift;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_exp2f(x[i]);
+    for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_exp2f(s[mt][i / 4][i % 4]);
     r.sum[mt] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[mt][i] = pack2<T>(x[2 * i], x[2 * i + 1]);
-  }
-}
-
-template <typename T, int D, int MT>
-__device__ __forceinline__ void add_values(Rows<MT, D / 16>& r, const Words<D / 32> (&v)[8], const u32x4 (&w)[MT]) {
-#pragma unroll
-  for (int j = 0; j < D / 16; ++j) {
-    u32x4 t;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) t[i] = __builtin_amdgcn_perm(v[2 * i + 1].w[j / 2], v[2 * i].w[j / 2], j & 1 ? 0x07060302u : 0x05040100u);
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) r.o[mt][j] = Matrix<T>::mad(t, w[mt], r.o[mt][j]);
   }
 }
 
@@ -250,21 +269,44 @@ __device__ __forceinline__ uint32_t seen_of(const AttentionArgs& a, int b, int n
   return (uint32_t)(a.mask[b * a.mask_stride + node * a.words + (t >> 6)] >> (t & 63)) & 0xffu;
 }
 
-// Token t of a sequence (old: of its context, which is not empty; else one of its nodes, `stride` elements apart): where it starts, in elements, or false and 0, which is
-// a place that can be read.
-__device__ __forceinline__ bool find_token(const AttentionArgs& a, int b, int len, bool old, int t, int64_t stride, int64_t* at) {
-  bool ok;
-  if (old) {
-    const int c = min(t, len - 1);
-    const uint32_t j = a.cache.by_page.of(c);
-    const int page = a.cache.table == nullptr ? b : a.cache.table[b * a.cache.table_stride + j];
-    ok = t < len && (uint32_t)page < (uint32_t)a.cache.pages;
-    *at = ok ? page * a.cache.page_stride + (int64_t)(c - j * (uint32_t)a.cache.page) * a.cache.token_stride : 0;
-  } else {
-    ok = t < a.seen_nodes;
-    *at = ok ? t * stride : 0;
+// The queries of a wavefront's 16 * MT rows from row `first` on, and their nodes (-1: no row).
+template <int D, int MT>
+__device__ __forceinline__ void load_queries(const AttentionArgs& a, int b, int h, int first, u32x4 (&q)[MT][D / 32], int (&node)[MT]) {
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const int r = first + mt * 16 + n;
+    node[mt] = -1;
+#pragma unroll
+    for (int kk = 0; kk < D / 32; ++kk) q[mt][kk] = u32x4{0, 0, 0, 0};
+    if (r < a.rows) {
+      node[mt] = a.by_group.of(r);
+      const char* p = a.q.data + 2 * (b * a.q.batch_stride + node[mt] * a.q.token_stride + (h * a.group + r - node[mt] * a.group) * a.q.head_stride + 8 * g);
+#pragma unroll
+      for (int kk = 0; kk < D / 32; ++kk) q[mt][kk] = (*reinterpret_cast<const u32x4*>(p + 64 * kk) & a.keep) ^ a.sign;
+    }
   }
-  return ok;
+}
+
+// Where token lane % 32 of a step lies.  The page id is asked for a step or more before the place is needed; a place is an offset in elements from the head's
+// start in page 0 of the cache (a step of the context) or the number of a node, and -1 for a token that is not there.
+struct Lookup {
+  int page;
+  uint32_t token;
+};
+__device__ __forceinline__ Lookup ask(const AttentionArgs& a, const Share& s, int old_steps, int step) {
+  Lookup l{s.b, (uint32_t)step * kAttTile + (threadIdx.x & (kAttTile - 1))};
+  if (step >= old_steps) {
+    l.token -= (uint32_t)old_steps * kAttTile;
+  } else if (a.cache.table != nullptr) {
+    l.page = a.cache.table[s.b * a.cache.table_stride + a.cache.by_page.of(min(l.token, (uint32_t)s.len - 1))];      // (a step of the context has a token)
+  }
+  return l;
+}
+__device__ __forceinline__ int64_t place_of(const AttentionArgs& a, const Share& s, int old_steps, int step, const Lookup& l) {
+  if (step >= old_steps) return l.token < (uint32_t)a.seen_nodes ? (int64_t)l.token : -1;
+  if (l.token >= (uint32_t)s.len || (uint32_t)l.page >= (uint32_t)a.cache.pages) return -1;
+  return l.page * a.cache.page_stride + (int64_t)(l.token - a.cache.by_page.of(l.token) * (uint32_t)a.cache.page) * a.cache.token_stride;
 }
 
 // The rows that see node t add their weights times those of its values that are no finite numbers; `from`: the 4 DV values that a lane has, value 4 DV g + j
@@ -291,14 +333,17 @@ __device__ __forceinline__ void add_odd_values(Rows<MT, D / 16>& r, const T* val
   }
 }
 
-// One workgroup: up to 16 * MT rows (node, query head of one kv head) of one sequence over one of `splits` parts of its tokens; its wavefronts take
-// steps of 32 tokens in turns and meet at the end.  The weights are rounded to the type of V for the value product (their sum is not): half a step
-// of each, so the error is a mean of independent roundings, below the one rounding of the result.
+// The kernel for few rows.  One workgroup: up to 16 * MT rows (node, query head of one kv head) of one sequence over one part of its tokens; its wavefronts
+// take steps of 32 tokens in turns and meet at the end.  K and V go from memory to the registers they are used from: K as it lies is an operand,
+// V is loaded as it lies, D / 16 elements of 8 tokens to a lane, and turned inside the lane, 16 bits at a time.
+// The weights are rounded to the type of V for the value product (their sum is not): half a step of each, so the error is a mean of independent
+// roundings, below the one rounding of the result.
 template <typename T, int D, int MT>
 __global__ void __launch_bounds__(kAttWaves * 64, D <= 128 ? 2 : 1) tree_attention_kernel(const AttentionArgs a) {
   constexpr int KK = D / 32, DV = D / 16, N = DV / 2, R = 16 * MT;
   __shared__ float sums[kAttWaves][4 * DV * MT][64];
   __shared__ float2 tops[kAttWaves][MT][16];
+  __shared__ __align__(16) int64_t places[kAttWaves][2][kAttTile];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
   uint32_t id = blockIdx.x;
   const int h = id % a.kv_heads;
@@ -306,111 +351,85 @@ __global__ void __launch_bounds__(kAttWaves * 64, D <= 128 ? 2 : 1) tree_attenti
   const int row_tile = id % a.row_tiles, slot = id / a.row_tiles;
   const Share share = share_of(a, slot);
   if (share.b < 0) return;
-  const int b = share.b, len = share.len, old_steps = steps_of(len), first = share.first, last = share.last;
+  const int b = share.b, old_steps = steps_of(share.len), last = share.last;
   if (share.part == 0 && h == 0 && row_tile == 0 && threadIdx.x == 0 && a.places != nullptr) a.places[b] = make_int2(slot, share.parts);
 
   u32x4 q[MT][KK];
   int node[MT];
-#pragma unroll
-  for (int mt = 0; mt < MT; ++mt) {
-    const int r = row_tile * R + mt * 16 + n;
-    node[mt] = -1;
-    if (r < a.rows) {
-      node[mt] = a.by_group.of(r);
-      const char* p = a.q.data + 2 * (b * a.q.batch_stride + node[mt] * a.q.token_stride + (h * a.group + r - node[mt] * a.group) * a.q.head_stride + 8 * g);
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) q[mt][kk] = *reinterpret_cast<const u32x4*>(p + 64 * kk) ^ a.sign;
-    } else {
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) q[mt][kk] = u32x4{0, 0, 0, 0};
-    }
-  }
+  int step = share.first + wave, turn = 0;
+  Lookup next{};
+  if (step < last) next = ask(a, share, old_steps, step);
+  load_queries<D, MT>(a, b, h, row_tile * R, q, node);
   Rows<MT, DV> rows;
-#pragma unroll
-  for (int mt = 0; mt < MT; ++mt) {
-    rows.top[mt] = -INFINITY;
-    rows.sum[mt] = 0.f;
-#pragma unroll
-    for (int j = 0; j < DV; ++j) rows.o[mt][j] = f32x4{0, 0, 0, 0};
-  }
+  rows.clear(Matrix<T>::kLift);
   const int k_token = 8 * (n >> 2) + (n & 3);      // of the first 16; the second are 4 further
   const char *cache_k = a.cache.k + 2 * h * a.cache.head_stride, *cache_v = a.cache.v + 2 * h * a.cache.head_stride;
+  const char *new_k = a.k_new.data + 2 * (b * a.k_new.batch_stride + h * a.k_new.head_stride),
+             *new_v = a.v_new.data + 2 * (b * a.v_new.batch_stride + h * a.v_new.head_stride);
 
-  // The page ids of a step's tokens, asked for a step ahead: of the 8 tokens that this lane's row of K belongs to, and of the 8 whose V it loads.
-  const int full_steps = a.eights ? min(last, len / kAttTile) : 0;      // steps all of whose tokens are there, pages of whole eights
-  int id_k = 0, id_v = 0;
-  auto ask = [&](int step) {
-    const uint32_t t = min(step, full_steps - 1) * kAttTile;
-    const uint32_t jk = a.cache.by_page.of(t + 8 * (n >> 2)), jv = a.cache.by_page.of(t + 8 * g);
-    id_k = a.cache.table == nullptr ? b : a.cache.table[b * a.cache.table_stride + jk];
-    id_v = a.cache.table == nullptr ? b : a.cache.table[b * a.cache.table_stride + jv];
-  };
-  int step = first + wave;
-  if (step < full_steps) ask(step);
-  for (; step < last; step += kAttWaves) {
-    u32x4 k[2][KK];
-    Words<N> v[8];
-    u32x4 w[MT];
-    uint32_t seen[MT];                        // of the tokens 8 g ... + 7, a bit each, by row
+  for (; step < last; step += kAttWaves, turn ^= 1) {
+    // The places pass through LDS, from the lane that looked one up to those that load from it.  A wavefront's own accesses there are in order.
     const bool old = step < old_steps;
-    const int t0 = (old ? step : step - old_steps) * kAttTile;
-    const char *base_k = old ? cache_k : a.k_new.data + 2 * (b * a.k_new.batch_stride + h * a.k_new.head_stride),
-               *base_v = old ? cache_v : a.v_new.data + 2 * (b * a.v_new.batch_stride + h * a.v_new.head_stride);
-    const bool all = step < full_steps && __all((uint32_t)id_k < (uint32_t)a.cache.pages && (uint32_t)id_v < (uint32_t)a.cache.pages);
-    if (all) {
-      const uint32_t tk = step * kAttTile + k_token, tv = step * kAttTile + 8 * g;
-      const char* pk = cache_k + 2 * (id_k * a.cache.page_stride + (int64_t)(tk - a.cache.by_page.of(tk) * a.cache.page) * a.cache.token_stride + 8 * g);
-      const char* pv = cache_v + 2 * (id_v * a.cache.page_stride + (int64_t)(tv - a.cache.by_page.of(tv) * a.cache.page) * a.cache.token_stride + DV * n);
+    const int64_t mine = place_of(a, share, old_steps, step, next);
+    int64_t* table = places[wave][turn];
+    if (lane < kAttTile) table[lane] = mine;
+    const uint32_t there = (uint32_t)__ballot(mine >= 0);
+    const bool all = old && there == 0xffffffffu;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    u32x4 k[2][KK], w[MT];
+    Words<N> v[8];
+    const char *base_k = old ? cache_k : new_k, *base_v = old ? cache_v : new_v;
+    const int64_t per_k = old ? 1 : a.k_new.token_stride, per_v = old ? 1 : a.v_new.token_stride;
 #pragma unroll
-      for (int half = 0; half < 2; ++half)
+    for (int half = 0; half < 2; ++half) {
+      const int64_t at = table[k_token + 4 * half];
+      const char* p = base_k + 2 * ((at < 0 ? 0 : old ? at : at * per_k) + 8 * g);
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) k[half][kk] = *reinterpret_cast<const u32x4*>(pk + half * 8 * a.cache.token_stride + 64 * kk);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = load_words<N>(pv + i * 2 * a.cache.token_stride);
-      ask(step + kAttWaves);
-    } else {
-      // Tokens that are not there are read from a place that is (node 0, token 0 of page 0) and count as zeros that nobody sees.
-      uint32_t valid = 0;
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        int64_t at;
-        find_token(a, b, len, old, t0 + k_token + 4 * half, a.k_new.token_stride, &at);
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk) k[half][kk] = *reinterpret_cast<const u32x4*>(base_k + 2 * (at + 32 * kk + 8 * g));
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        int64_t at;
-        const bool ok = find_token(a, b, len, old, t0 + 8 * g + i, a.v_new.token_stride, &at);
-        valid |= (uint32_t)ok << i;
-        v[i] = load_words<N>(base_v + 2 * (at + DV * n));
-#pragma unroll
-        for (int j = 0; j < N; ++j) v[i].w[j] = ok ? v[i].w[j] : 0u;
-      }
-      if (step + kAttWaves < full_steps) ask(step + kAttWaves);
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) seen[mt] = old ? valid : valid & seen_of(a, b, node[mt], t0 + 8 * g);
+      for (int kk = 0; kk < KK; ++kk) k[half][kk] = *reinterpret_cast<const u32x4*>(p + 64 * kk);
     }
-    attend_step<T, D, MT>(rows, q, k, a.scale_log2, all, seen, w);
-    if (!old) {
-      // a node may be seen by some rows only, and for the others its values may be anything: what is no finite number leaves the
-      // product, in which it would meet weights of zero, and is added to the rows that see it by itself
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t at = table[8 * g + i];
+      v[i] = load_words<N>(base_v + 2 * ((at < 0 ? 0 : old ? at : at * per_v) + DV * n));
+    }
+    if (step + kAttWaves < last) next = ask(a, share, old_steps, step + kAttWaves);
+    uint32_t seen[MT] = {};
+    if (all) {
+      weigh<T, D, MT, true>(rows, q, k, a.scale_log2, seen, w);
+    } else {
+      const int t0 = (step - old_steps) * kAttTile;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        seen[mt] = (there >> (8 * g)) & 0xffu;
+        if (!old) seen[mt] &= seen_of(a, b, node[mt], t0 + 8 * g);
+      }
+      weigh<T, D, MT, false>(rows, q, k, a.scale_log2, seen, w);
+      // A token that is not there was read from a place that is, and counts as zeros.  A node may be seen by some rows only, and for the others its values may be
+      // anything: what is no finite number leaves the product, in which it would meet weights of zero, and is added to the rows that see it by itself.
       bool odd = false;
 #pragma unroll
       for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int j = 0; j < N; ++j) odd = odd || numbers<T>(v[i].w[j]) != v[i].w[j];
+        for (int j = 0; j < N; ++j) {
+          const uint32_t is = (there >> (8 * g + i)) & 1 ? v[i].w[j] : 0u, number = old ? is : numbers<T>(is);
+          odd = odd || number != is;
+          v[i].w[j] = number;
+        }
       if (__any(odd)) {
 #pragma unroll 1
         for (int t = 0; t < min(kAttTile, a.seen_nodes - t0); ++t)
-          add_odd_values<T, D, MT, true>(rows, reinterpret_cast<const T*>(base_v) + (t0 + t) * a.v_new.token_stride, t, w, seen);
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-          for (int j = 0; j < N; ++j) v[i].w[j] = numbers<T>(v[i].w[j]);
+          add_odd_values<T, D, MT, true>(rows, reinterpret_cast<const T*>(new_v) + (t0 + t) * a.v_new.token_stride, t, w, seen);
       }
     }
-    add_values<T, D, MT>(rows, v, w);
+#pragma unroll
+    for (int j = 0; j < DV; ++j) {
+      u32x4 t;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) t[i] = __builtin_amdgcn_perm(v[2 * i + 1].w[j / 2], v[2 * i].w[j / 2], j & 1 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) rows.o[mt][j] = Matrix<T>::mad(t, w[mt], rows.o[mt][j]);
+    }
   }
 
   // the wavefronts' rows meet: each wavefront adds up the quarter 4 g + wave of the elements
@@ -524,7 +543,8 @@ __global__ void __launch_bounds__(256) tree_attention_join_kernel(const Attentio
 }
 
 // The kernel for many rows: WAVES wavefronts with 16 * MT rows each take every step together.  K and V of a step are loaded once for all of them and kept
-// in LDS, two steps in turns: the next step's are asked for before this one's products and written behind them.
+// in LDS, two steps in turns: the next step's are asked for before this one's products and written behind them, and the places of the tokens
+// of the step after that are looked up meanwhile.
 //   K: pieces of 8 elements [D / 8][32 tokens], 16 bytes further from one piece to the next than the tokens take, so that neither the
 //      writing (a row of the cache at a time) nor the reading (16 tokens of a piece) meets itself in a bank;
 //   V: turned while it is written: [4 groups of 8 tokens][D] of 16 bytes, as the value product reads it.
@@ -535,7 +555,8 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) tree_attention_w
   constexpr int U = (4 * D + THREADS - 1) / THREADS;      // units of 16 bytes of K, and of V, to a thread
   constexpr int PIECE = kAttTile * 16 + 16;
   __shared__ __align__(16) char lds_k[2][D / 8 * PIECE], lds_v[2][4 * D * 16];
-  __shared__ uint32_t lds_valid[2], lds_odd[2];
+  __shared__ int64_t places[2][kAttTile];
+  __shared__ uint32_t lds_there[4], lds_odd[2];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
   uint32_t id = blockIdx.x;
   const int h = id % a.kv_heads;
@@ -543,150 +564,112 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) tree_attention_w
   const int row_tile = id % a.row_tiles, slot = id / a.row_tiles;
   const Share share = share_of(a, slot);
   if (share.b < 0) return;
-  const int b = share.b, len = share.len, old_steps = steps_of(len), first = share.first, last = share.last;
+  const int b = share.b, old_steps = steps_of(share.len), first = share.first, last = share.last;
   if (share.part == 0 && h == 0 && row_tile == 0 && threadIdx.x == 0 && a.places != nullptr) a.places[b] = make_int2(slot, share.parts);
 
+  // The first wavefront looks places up; those of step s are in places[s % 2] from the barrier two steps before its products on.
+  auto keep_places = [&](int step, const Lookup& l) {
+    const int64_t mine = place_of(a, share, old_steps, step, l);
+    if (lane < kAttTile) places[step & 1][lane] = mine;
+    const uint32_t there = (uint32_t)__ballot(mine >= 0);
+    if (lane == 0) lds_there[step & 3] = there;
+  };
+  if (wave == 0) {
+    if (first < last) keep_places(first, ask(a, share, old_steps, first));
+    if (first + 1 < last) keep_places(first + 1, ask(a, share, old_steps, first + 1));
+  }
+  if (threadIdx.x < 2) lds_odd[threadIdx.x] = 0;
   u32x4 q[MT][KK];
   int node[MT];
-#pragma unroll
-  for (int mt = 0; mt < MT; ++mt) {
-    const int r = row_tile * R + wave * 16 * MT + mt * 16 + n;
-    node[mt] = -1;
-    if (r < a.rows) {
-      node[mt] = a.by_group.of(r);
-      const char* p = a.q.data + 2 * (b * a.q.batch_stride + node[mt] * a.q.token_stride + (h * a.group + r - node[mt] * a.group) * a.q.head_stride + 8 * g);
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) q[mt][kk] = *reinterpret_cast<const u32x4*>(p + 64 * kk) ^ a.sign;
-    } else {
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) q[mt][kk] = u32x4{0, 0, 0, 0};
-    }
-  }
+  load_queries<D, MT>(a, b, h, row_tile * R + wave * 16 * MT, q, node);
   const bool works = row_tile * R + wave * 16 * MT < a.rows;      // a wavefront without rows only loads
   Rows<MT, DV> rows;
-#pragma unroll
-  for (int mt = 0; mt < MT; ++mt) {
-    rows.top[mt] = -INFINITY;
-    rows.sum[mt] = 0.f;
-#pragma unroll
-    for (int j = 0; j < DV; ++j) rows.o[mt][j] = f32x4{0, 0, 0, 0};
-  }
+  rows.clear(Matrix<T>::kLift);
 
   // What this thread loads of a step: unit u of K is piece u % (D / 8) of token u / (D / 8); of V it is the elements 2 (u % (D / 2)) and the next of four tokens.
   const char *cache_k = a.cache.k + 2 * h * a.cache.head_stride, *cache_v = a.cache.v + 2 * h * a.cache.head_stride;
-  const int full_steps = a.eights ? min(last, len / kAttTile) : 0;
-  int id_k[U], id_v[U], id_t = 0;      // page ids, asked for a step ahead: of the tokens of the units, and of token lane % 32
-  auto ask = [&](int step) {
-    if (step >= full_steps) return;
-    const uint32_t t0 = step * kAttTile;
-    auto page_of = [&](uint32_t t) { return a.cache.table == nullptr ? b : a.cache.table[b * a.cache.table_stride + a.cache.by_page.of(t)]; };
+  const char *new_k = a.k_new.data + 2 * (b * a.k_new.batch_stride + h * a.k_new.head_stride),
+             *new_v = a.v_new.data + 2 * (b * a.v_new.batch_stride + h * a.v_new.head_stride);
+  u32x4 load_k[U];
+  uint32_t load_v[U][4];
+  auto load = [&](int step) {
+    const bool old = step < old_steps;
+    const char *base_k = old ? cache_k : new_k, *base_v = old ? cache_v : new_v;
+    const int64_t* table = places[step & 1];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       const int u = min((int)threadIdx.x + i * THREADS, 4 * D - 1);
-      id_k[i] = page_of(t0 + u / (D / 8));
-      id_v[i] = page_of(t0 + 4 * (u / (D / 2)));
-    }
-    id_t = page_of(t0 + (lane & 31));
-  };
-  u32x4 load_k[U];
-  uint32_t load_v[U][4], valid = 0;
-  auto load = [&](int step) {
-    const bool old = step < old_steps;
-    const int t0 = (old ? step : step - old_steps) * kAttTile;
-    if (step < full_steps) {
+      const int64_t at_k = table[u / (D / 8)];
+      load_k[i] = *reinterpret_cast<const u32x4*>(base_k + 2 * (at_k < 0 ? 0 : old ? at_k : at_k * a.k_new.token_stride) + 16 * (u % (D / 8)));
 #pragma unroll
-      for (int i = 0; i < U; ++i) {
-        const int u = min((int)threadIdx.x + i * THREADS, 4 * D - 1);
-        const bool ok_k = (uint32_t)id_k[i] < (uint32_t)a.cache.pages, ok_v = (uint32_t)id_v[i] < (uint32_t)a.cache.pages;
-        const uint32_t tk = t0 + u / (D / 8), tv = t0 + 4 * (u / (D / 2));
-        const int64_t at_k = ok_k ? id_k[i] * a.cache.page_stride + (int64_t)(tk - a.cache.by_page.of(tk) * a.cache.page) * a.cache.token_stride : 0;
-        const int64_t at_v = ok_v ? id_v[i] * a.cache.page_stride + (int64_t)(tv - a.cache.by_page.of(tv) * a.cache.page) * a.cache.token_stride : 0;
-        load_k[i] = *reinterpret_cast<const u32x4*>(cache_k + 2 * at_k + 16 * (u % (D / 8)));
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t w = *reinterpret_cast<const uint32_t*>(cache_v + 2 * (at_v + (ok_v ? j : 0) * a.cache.token_stride) + 4 * (u % (D / 2)));
-          load_v[i][j] = ok_v ? w : 0u;
-        }
+      for (int j = 0; j < 4; ++j) {
+        const int64_t at_v = table[4 * (u / (D / 2)) + j];
+        load_v[i][j] = *reinterpret_cast<const uint32_t*>(base_v + 2 * (at_v < 0 ? 0 : old ? at_v : at_v * a.v_new.token_stride) + 4 * (u % (D / 2)));
       }
-      valid = (uint32_t)__ballot((uint32_t)id_t < (uint32_t)a.cache.pages);
-    } else {
-      const char *base_k = old ? cache_k : a.k_new.data + 2 * (b * a.k_new.batch_stride + h * a.k_new.head_stride),
-                 *base_v = old ? cache_v : a.v_new.data + 2 * (b * a.v_new.batch_stride + h * a.v_new.head_stride);
-      int64_t at;
-#pragma unroll
-      for (int i = 0; i < U; ++i) {
-        const int u = min((int)threadIdx.x + i * THREADS, 4 * D - 1);
-        find_token(a, b, len, old, t0 + u / (D / 8), a.k_new.token_stride, &at);
-        load_k[i] = *reinterpret_cast<const u32x4*>(base_k + 2 * at + 16 * (u % (D / 8)));
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const bool ok = find_token(a, b, len, old, t0 + 4 * (u / (D / 2)) + j, a.v_new.token_stride, &at);
-          const uint32_t w = *reinterpret_cast<const uint32_t*>(base_v + 2 * at + 4 * (u % (D / 2)));
-          load_v[i][j] = ok ? w : 0u;
-        }
-      }
-      valid = (uint32_t)__ballot(find_token(a, b, len, old, t0 + (lane & 31), a.k_new.token_stride, &at));
     }
-    ask(step + 1);
   };
-  // what is no finite number among a node's values leaves the product (see add_odd_values)
   auto keep = [&](int step, int buffer) {
+    const uint32_t there = lds_there[step & 3];
+    const bool old = step < old_steps;
     bool odd = false;
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       const int u = threadIdx.x + i * THREADS;
       if (4 * D % THREADS != 0 && u >= 4 * D) continue;
-      if (step >= old_steps)
+      const int four = u / (D / 2), d = 2 * (u % (D / 2));
+      if (!old || there != 0xffffffffu) {      // (as in the kernel for few rows)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const uint32_t w = numbers<T>(load_v[i][j]);
-          odd = odd || w != load_v[i][j];
-          load_v[i][j] = w;
+          const uint32_t is = (there >> (4 * four + j)) & 1 ? load_v[i][j] : 0u, number = old ? is : numbers<T>(is);
+          odd = odd || number != is;
+          load_v[i][j] = number;
         }
-      const int token = u / (D / 8), place = ((token >> 2) & 1) * 16 + 4 * (token >> 3) + (token & 3);      // as attend_step numbers the tokens
+      }
+      const int token = u / (D / 8), place = ((token >> 2) & 1) * 16 + 4 * (token >> 3) + (token & 3);      // as weigh() numbers the tokens
       *reinterpret_cast<u32x4*>(lds_k[buffer] + u % (D / 8) * PIECE + place * 16) = load_k[i];
-      const int four = u / (D / 2), d = 2 * (u % (D / 2));
       char* to = lds_v[buffer] + ((four >> 1) * D + d) * 16 + (four & 1) * 8;
-      const uint32_t *v = load_v[i];
+      const uint32_t* v = load_v[i];
       *reinterpret_cast<uint2*>(to) = make_uint2(__builtin_amdgcn_perm(v[1], v[0], 0x05040100u), __builtin_amdgcn_perm(v[3], v[2], 0x05040100u));
       *reinterpret_cast<uint2*>(to + 16) = make_uint2(__builtin_amdgcn_perm(v[1], v[0], 0x07060302u), __builtin_amdgcn_perm(v[3], v[2], 0x07060302u));
     }
-    if (threadIdx.x == 0) lds_valid[buffer] = valid;
     if (odd) lds_odd[buffer] = step + 1;      // of this step; whatever else stands there is another's
   };
 
-  if (threadIdx.x < 2) lds_odd[threadIdx.x] = 0;
   __syncthreads();
   if (first < last) {
-    ask(first);
     load(first);
     keep(first, 0);
   }
   __syncthreads();
   for (int step = first; step < last; ++step) {
     const int buffer = (step - first) & 1;
+    Lookup after{};
+    if (wave == 0 && step + 2 < last) after = ask(a, share, old_steps, step + 2);
     if (step + 1 < last) load(step + 1);
     if (works) {
-      const uint32_t now = lds_valid[buffer];
-      const bool old = step < old_steps, all = old && now == 0xffffffffu;
-      const int t0 = (step - old_steps) * kAttTile;
+      const uint32_t there = lds_there[step & 3];
+      const bool old = step < old_steps;
       u32x4 k[2][KK], w[MT];
-      uint32_t seen[MT];
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        seen[mt] = (now >> (8 * g)) & 0xffu;
-        if (!old) seen[mt] &= seen_of(a, b, node[mt], t0 + 8 * g);
-      }
+      uint32_t seen[MT] = {};
 #pragma unroll
       for (int half = 0; half < 2; ++half)
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) k[half][kk] = *reinterpret_cast<const u32x4*>(lds_k[buffer] + (4 * kk + g) * PIECE + (half * 16 + n) * 16);
-      attend_step<T, D, MT>(rows, q, k, a.scale_log2, all, seen, w);
-      if (!old && lds_odd[buffer] == (uint32_t)step + 1) {
+      if (old && there == 0xffffffffu) {
+        weigh<T, D, MT, true>(rows, q, k, a.scale_log2, seen, w);
+      } else {
+        const int t0 = (step - old_steps) * kAttTile;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          seen[mt] = (there >> (8 * g)) & 0xffu;
+          if (!old) seen[mt] &= seen_of(a, b, node[mt], t0 + 8 * g);
+        }
+        weigh<T, D, MT, false>(rows, q, k, a.scale_log2, seen, w);
+        if (!old && lds_odd[buffer] == (uint32_t)step + 1) {
 #pragma unroll 1
-        for (int t = 0; t < min(kAttTile, a.seen_nodes - t0); ++t)
-          add_odd_values<T, D, MT, false>(rows, reinterpret_cast<const T*>(a.v_new.data) + b * a.v_new.batch_stride + h * a.v_new.head_stride + (t0 + t) * a.v_new.token_stride,
-                                          t, w, seen);
+          for (int t = 0; t < min(kAttTile, a.seen_nodes - t0); ++t)
+            add_odd_values<T, D, MT, false>(rows, reinterpret_cast<const T*>(new_v) + (t0 + t) * a.v_new.token_stride, t, w, seen);
+        }
       }
 #pragma unroll
       for (int j = 0; j < DV; ++j) {
@@ -696,6 +679,7 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) tree_attention_w
       }
     }
     if (step + 1 < last) keep(step + 1, buffer ^ 1);
+    if (wave == 0 && step + 2 < last) keep_places(step + 2, after);      // over those of this step, which were read before the last barrier
     __syncthreads();
   }
   if (!works) return;

@@ -226,6 +226,14 @@ def test_the_lowest_value_is_a_number():
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("scale", [0.0, -0.2, 1e-30, 3.0])
+@pytest.mark.parametrize("nodes", [3, 40])
+def test_scales(dtype, scale, nodes):
+    """Negative ones turn the order round, 0 makes all weights equal."""
+    Case(dtype, 2, nodes, 4, 2, 128, 16, [333, 0], mask="tree", scale=scale).check()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_views(dtype):
     """Queries, keys and values as slices of one projection, heads before tokens in the results, pages that hold head after head."""
     c = Case(dtype, 2, 5, 6, 2, 128, 16, [37, 90], mask="tree")
