@@ -3,6 +3,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstdlib>
 
 #include "token_host.hpp"
 #include "tree_attention.hpp"
@@ -28,7 +29,8 @@ Plan plan_of(int batch, int nodes, int heads, int kv_heads, int head_dim, int64_
   p.row_tiles = (p.rows + p.tile - 1) / p.tile;
   const int64_t steps = (max_len + kAttTile - 1) / kAttTile + (nodes + kAttTile - 1) / kAttTile, tiles = (int64_t)kv_heads * p.row_tiles;
   const int unit = p.waves ? 1 : kAttWaves;
-  const int64_t most = batch * ((steps + unit - 1) / unit), fill = ((p.waves == 8 ? 256 : 512) + tiles - 1) / tiles;
+  static const int F = getenv("FILL") ? atoi(getenv("FILL")) : 0;
+  const int64_t most = batch * ((steps + unit - 1) / unit), fill = ((F ? F : p.waves == 8 ? 256 : 512) + tiles - 1) / tiles;
   p.slots = (int)std::max<int64_t>(batch, std::min(most, batch == 1 ? fill : std::max(fill, 3 * (int64_t)batch)));
   p.groups = p.slots * tiles;
   const bool whole = p.slots == batch;

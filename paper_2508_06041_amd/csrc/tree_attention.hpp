@@ -120,12 +120,13 @@ template <int MT, int DV>
 struct Rows {
   f32x4 o[MT][DV];
   float sum[MT], top[MT], from[MT];      // sum: of the lane's own tokens
+  float limit[MT];                       // the score from which on top has to follow
   bool huge;                             // some top times scale / ln 2 may be past the floats though the scores are not
   __device__ __forceinline__ void clear(float lift) {
     huge = false;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-      top[mt] = -INFINITY;
+      top[mt] = limit[mt] = -INFINITY;
       from[mt] = lift;
       sum[mt] = 0.f;
 #pragma unroll
@@ -165,7 +166,7 @@ __device__ __forceinline__ void weigh(Rows<MT, D / 16>& r, const u32x4 (&q)[MT][
     most[mt] = s[mt][0][0];
 #pragma unroll
     for (int i = 1; i < 8; ++i) most[mt] = fmaxf(most[mt], s[mt][i / 4][i % 4]);
-    behind = behind || (most[mt] - r.top[mt]) * scale_log2 > kSlack;      // (a row without a score yet has NaN here if it gets none)
+    behind = behind || most[mt] > r.limit[mt];
   }
   if (__any(behind)) {
     bool huge = false;
@@ -174,6 +175,7 @@ __device__ __forceinline__ void weigh(Rows<MT, D / 16>& r, const u32x4 (&q)[MT][
       const float next = fmaxf(r.top[mt], row_max(most[mt]));
       const float less = r.top[mt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((r.top[mt] - next) * scale_log2);
       r.top[mt] = next;
+      r.limit[mt] = next + kSlack / scale_log2;
       r.from[mt] = next == -INFINITY ? kLift : __builtin_fmaf(-next, scale_log2, kLift);
       huge = huge || (next != -INFINITY && __builtin_fabsf(next) > 1e38f);
       r.sum[mt] *= less;
@@ -288,11 +290,15 @@ __device__ __forceinline__ void load_queries(const AttentionArgs& a, int b, int 
   }
 }
 
-// Where token lane % 32 of a step lies.  The page id is asked for a step or more before the place is needed; a place is an offset in elements from the head's
-// start in page 0 of the cache (a step of the context) or the number of a node, and -1 for a token that is not there.
+// Where token lane % 32 of a step lies.  The page id is asked for a step or more before the place is needed.  Places are offsets in bytes from the start of the
+// head, in page 0 of the cache (a step of the context) or in node 0, separately for keys and values; a token that is not there has the place of one that is.
 struct Lookup {
   int page;
   uint32_t token;
+};
+struct Place {
+  int64_t k, v;
+  bool there;
 };
 __device__ __forceinline__ Lookup ask(const AttentionArgs& a, const Share& s, int old_steps, int step) {
   Lookup l{s.b, (uint32_t)step * kAttTile + (threadIdx.x & (kAttTile - 1))};
@@ -303,10 +309,19 @@ __device__ __forceinline__ Lookup ask(const AttentionArgs& a, const Share& s, in
   }
   return l;
 }
-__device__ __forceinline__ int64_t place_of(const AttentionArgs& a, const Share& s, int old_steps, int step, const Lookup& l) {
-  if (step >= old_steps) return l.token < (uint32_t)a.seen_nodes ? (int64_t)l.token : -1;
-  if (l.token >= (uint32_t)s.len || (uint32_t)l.page >= (uint32_t)a.cache.pages) return -1;
-  return l.page * a.cache.page_stride + (int64_t)(l.token - a.cache.by_page.of(l.token) * (uint32_t)a.cache.page) * a.cache.token_stride;
+__device__ __forceinline__ Place place_of(const AttentionArgs& a, const Share& s, int old_steps, int step, const Lookup& l) {
+  Place p;
+  if (step >= old_steps) {
+    p.there = l.token < (uint32_t)a.seen_nodes;
+    const int64_t t = p.there ? l.token : 0;
+    p.k = 2 * t * a.k_new.token_stride;
+    p.v = 2 * t * a.v_new.token_stride;
+  } else {
+    p.there = l.token < (uint32_t)s.len && (uint32_t)l.page < (uint32_t)a.cache.pages;
+    const int64_t at = l.page * a.cache.page_stride + (int64_t)(l.token - a.cache.by_page.of(l.token) * (uint32_t)a.cache.page) * a.cache.token_stride;
+    p.k = p.v = p.there ? 2 * at : 0;
+  }
+  return p;
 }
 
 // The rows that see node t add their weights times those of its values that are no finite numbers; `from`: the 4 DV values that a lane has, value 4 DV g + j
@@ -343,7 +358,7 @@ __global__ void __launch_bounds__(kAttWaves * 64, D <= 128 ? 2 : 1) tree_attenti
   constexpr int KK = D / 32, DV = D / 16, N = DV / 2, R = 16 * MT;
   __shared__ float sums[kAttWaves][4 * DV * MT][64];
   __shared__ float2 tops[kAttWaves][MT][16];
-  __shared__ __align__(16) int64_t places[kAttWaves][2][kAttTile];
+  __shared__ __align__(16) int64_t places[kAttWaves][2][2][kAttTile];      // [..][turn][keys, values][token]
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
   uint32_t id = blockIdx.x;
   const int h = id % a.kv_heads;
@@ -370,29 +385,27 @@ __global__ void __launch_bounds__(kAttWaves * 64, D <= 128 ? 2 : 1) tree_attenti
   for (; step < last; step += kAttWaves, turn ^= 1) {
     // The places pass through LDS, from the lane that looked one up to those that load from it.  A wavefront's own accesses there are in order.
     const bool old = step < old_steps;
-    const int64_t mine = place_of(a, share, old_steps, step, next);
-    int64_t* table = places[wave][turn];
-    if (lane < kAttTile) table[lane] = mine;
-    const uint32_t there = (uint32_t)__ballot(mine >= 0);
+    const Place mine = place_of(a, share, old_steps, step, next);
+    int64_t(*table)[kAttTile] = places[wave][turn];
+    if (lane < kAttTile) {
+      table[0][lane] = mine.k;
+      table[1][lane] = mine.v;
+    }
+    const uint32_t there = (uint32_t)__ballot(mine.there);
     const bool all = old && there == 0xffffffffu;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
     u32x4 k[2][KK], w[MT];
     Words<N> v[8];
-    const char *base_k = old ? cache_k : new_k, *base_v = old ? cache_v : new_v;
-    const int64_t per_k = old ? 1 : a.k_new.token_stride, per_v = old ? 1 : a.v_new.token_stride;
+    const char *base_k = (old ? cache_k : new_k) + 16 * g, *base_v = (old ? cache_v : new_v) + 2 * DV * n;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-      const int64_t at = table[k_token + 4 * half];
-      const char* p = base_k + 2 * ((at < 0 ? 0 : old ? at : at * per_k) + 8 * g);
+      const char* p = base_k + table[0][k_token + 4 * half];
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) k[half][kk] = *reinterpret_cast<const u32x4*>(p + 64 * kk);
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int64_t at = table[8 * g + i];
-      v[i] = load_words<N>(base_v + 2 * ((at < 0 ? 0 : old ? at : at * per_v) + DV * n));
-    }
+    for (int i = 0; i < 8; ++i) v[i] = load_words<N>(base_v + table[1][8 * g + i]);
     if (step + kAttWaves < last) next = ask(a, share, old_steps, step + kAttWaves);
     uint32_t seen[MT] = {};
     if (all) {
@@ -545,17 +558,16 @@ __global__ void __launch_bounds__(256) tree_attention_join_kernel(const Attentio
 // The kernel for many rows: WAVES wavefronts with 16 * MT rows each take every step together.  K and V of a step are loaded once for all of them and kept
 // in LDS, two steps in turns: the next step's are asked for before this one's products and written behind them, and the places of the tokens
 // of the step after that are looked up meanwhile.
-//   K: pieces of 8 elements [D / 8][32 tokens], 16 bytes further from one piece to the next than the tokens take, so that neither the
-//      writing (a row of the cache at a time) nor the reading (16 tokens of a piece) meets itself in a bank;
+//   K: pieces of 8 elements [D / 8][32 tokens], the tokens' places exclusive-or the piece's number, so that neither the writing (a row of the
+//      cache at a time) nor the reading (16 tokens of four pieces) meets itself in a bank;
 //   V: turned while it is written: [4 groups of 8 tokens][D] of 16 bytes, as the value product reads it.
 // A lane's results are the values 16 j + 4 g ... + 3 of its row, j < D / 16.
 template <typename T, int D, int MT, int WAVES>
 __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) tree_attention_wide_kernel(const AttentionArgs a) {
   constexpr int KK = D / 32, DV = D / 16, R = 16 * MT * WAVES, THREADS = WAVES * 64;
   constexpr int U = (4 * D + THREADS - 1) / THREADS;      // units of 16 bytes of K, and of V, to a thread
-  constexpr int PIECE = kAttTile * 16 + 16;
-  __shared__ __align__(16) char lds_k[2][D / 8 * PIECE], lds_v[2][4 * D * 16];
-  __shared__ int64_t places[2][kAttTile];
+  __shared__ __align__(16) char lds_k[2][4 * D * 16], lds_v[2][4 * D * 16];
+  __shared__ __align__(16) int64_t places[2][2][kAttTile];      // [step % 2][keys, values][token]
   __shared__ uint32_t lds_there[4], lds_odd[2];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
   uint32_t id = blockIdx.x;
@@ -569,9 +581,12 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) tree_attention_w
 
   // The first wavefront looks places up; those of step s are in places[s % 2] from the barrier two steps before its products on.
   auto keep_places = [&](int step, const Lookup& l) {
-    const int64_t mine = place_of(a, share, old_steps, step, l);
-    if (lane < kAttTile) places[step & 1][lane] = mine;
-    const uint32_t there = (uint32_t)__ballot(mine >= 0);
+    const Place mine = place_of(a, share, old_steps, step, l);
+    if (lane < kAttTile) {
+      places[step & 1][0][lane] = mine.k;
+      places[step & 1][1][lane] = mine.v;
+    }
+    const uint32_t there = (uint32_t)__ballot(mine.there);
     if (lane == 0) lds_there[step & 3] = there;
   };
   if (wave == 0) {
@@ -595,17 +610,13 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) tree_attention_w
   auto load = [&](int step) {
     const bool old = step < old_steps;
     const char *base_k = old ? cache_k : new_k, *base_v = old ? cache_v : new_v;
-    const int64_t* table = places[step & 1];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       const int u = min((int)threadIdx.x + i * THREADS, 4 * D - 1);
-      const int64_t at_k = table[u / (D / 8)];
-      load_k[i] = *reinterpret_cast<const u32x4*>(base_k + 2 * (at_k < 0 ? 0 : old ? at_k : at_k * a.k_new.token_stride) + 16 * (u % (D / 8)));
+      load_k[i] = *reinterpret_cast<const u32x4*>(base_k + places[step & 1][0][u / (D / 8)] + 16 * (u % (D / 8)));
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int64_t at_v = table[4 * (u / (D / 2)) + j];
-        load_v[i][j] = *reinterpret_cast<const uint32_t*>(base_v + 2 * (at_v < 0 ? 0 : old ? at_v : at_v * a.v_new.token_stride) + 4 * (u % (D / 2)));
-      }
+      for (int j = 0; j < 4; ++j)
+        load_v[i][j] = *reinterpret_cast<const uint32_t*>(base_v + places[step & 1][1][4 * (u / (D / 2)) + j] + 4 * (u % (D / 2)));
     }
   };
   auto keep = [&](int step, int buffer) {
@@ -626,7 +637,8 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) tree_attention_w
         }
       }
       const int token = u / (D / 8), place = ((token >> 2) & 1) * 16 + 4 * (token >> 3) + (token & 3);      // as weigh() numbers the tokens
-      *reinterpret_cast<u32x4*>(lds_k[buffer] + u % (D / 8) * PIECE + place * 16) = load_k[i];
+      const int piece = u % (D / 8);
+      *reinterpret_cast<u32x4*>(lds_k[buffer] + (piece * kAttTile + (place ^ (piece & 15))) * 16) = load_k[i];
       char* to = lds_v[buffer] + ((four >> 1) * D + d) * 16 + (four & 1) * 8;
       const uint32_t* v = load_v[i];
       *reinterpret_cast<uint2*>(to) = make_uint2(__builtin_amdgcn_perm(v[1], v[0], 0x05040100u), __builtin_amdgcn_perm(v[3], v[2], 0x05040100u));
@@ -654,7 +666,7 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) tree_attention_w
 #pragma unroll
       for (int half = 0; half < 2; ++half)
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) k[half][kk] = *reinterpret_cast<const u32x4*>(lds_k[buffer] + (4 * kk + g) * PIECE + (half * 16 + n) * 16);
+        for (int kk = 0; kk < KK; ++kk) k[half][kk] = *reinterpret_cast<const u32x4*>(lds_k[buffer] + ((4 * kk + g) * kAttTile + half * 16 + (n ^ ((4 * kk + g) & 15))) * 16);
       if (old && there == 0xffffffffu) {
         weigh<T, D, MT, true>(rows, q, k, a.scale_log2, seen, w);
       } else {
