@@ -23,15 +23,14 @@ struct Plan {
 Plan plan_of(int batch, int nodes, int heads, int kv_heads, int head_dim, int64_t max_len) {
   Plan p;
   p.rows = nodes * (heads / kv_heads);
-  p.waves = p.rows <= 32 ? 0 : p.rows <= 128 || head_dim == 256 ? 4 : 8;
+  p.waves = p.rows <= 32 ? 0 : p.rows <= 128 || head_dim == 256 || (getenv("W4") && atoi(getenv("W4"))) ? 4 : 8;
   p.mt = head_dim == 256 || p.rows <= 16 || (p.rows > 32 && p.rows <= 64) ? 1 : 2;
   p.tile = 16 * p.mt * std::max(p.waves, 1);
   p.row_tiles = (p.rows + p.tile - 1) / p.tile;
   const int64_t steps = (max_len + kAttTile - 1) / kAttTile + (nodes + kAttTile - 1) / kAttTile, tiles = (int64_t)kv_heads * p.row_tiles;
-  const int unit = p.waves ? 1 : kAttWaves;
   static const int F = getenv("FILL") ? atoi(getenv("FILL")) : 0;
-  const int64_t most = batch * ((steps + unit - 1) / unit), fill = ((F ? F : p.waves == 8 ? 256 : 512) + tiles - 1) / tiles;
-  p.slots = (int)std::max<int64_t>(batch, std::min(most, batch == 1 ? fill : std::max(fill, 3 * (int64_t)batch)));
+  const int64_t most = batch * ((steps + kAttWaves - 1) / kAttWaves), fill = ((F ? F : p.waves == 8 ? 256 : 512) + tiles - 1) / tiles;
+  p.slots = (int)std::max<int64_t>(batch, std::min(most, fill >= 2 * batch ? fill : 3 * (int64_t)batch));
   p.groups = p.slots * tiles;
   const bool whole = p.slots == batch;
   p.part = whole ? 0 : (size_t)p.groups * p.tile * head_dim * sizeof(float);
@@ -139,7 +138,7 @@ int dpllm_tree_attention(const dpllm_cache* cache, int layer, int batch, int nod
   a.row_tiles = p.row_tiles;
   a.batch = batch;
   a.slots = p.slots;
-  a.unit = p.waves ? 1 : kAttWaves;
+  a.least = kAttWaves;
   if (cache->dtype == DPLLM_F16)
     launch<half_t>(cache->head_dim, a, p, (hipStream_t)stream);
   else

@@ -23,7 +23,7 @@ struct AttentionArgs {
   float scale, scale_log2;          // |scale|, and that / ln 2
   uint32_t sign, keep;              // sign: 0x80008000 for a negative scale, with which the queries change theirs; keep: 0 for a scale of 0, of which they are zeros
   Divide by_group;
-  int batch, nodes, seen_nodes, words, kv_heads, group, rows, row_tiles, slots, unit;
+  int batch, nodes, seen_nodes, words, kv_heads, group, rows, row_tiles, slots, least;      // least: steps of the smallest part worth a workgroup
 };
 
 template <typename T>
@@ -208,9 +208,9 @@ __device__ __forceinline__ void weigh(Rows<MT, D / 16>& r, const u32x4 (&q)[MT][
 }
 
 // How the tokens are dealt out.  For every kv head and tile of rows a launch has `slots` workgroups; all take parts of the same number of steps, the smallest
-// multiple of `unit` with which every sequence gets the parts it needs (at least one, which writes the zeros of a row that sees nothing).  With parts of
-// c steps the sequences need less than total / c + batch of them, so c = total / (slots - batch + 1) will do.  The lengths are on the device, so every
-// workgroup works this out for itself, 64 sequences at a time.
+// with which the parts of all sequences fit (a sequence has at least one, which writes the zeros of a row that sees nothing).  With parts of c steps the
+// sequences need at least total / c and less than total / c + batch, so c is between total / slots and total / (slots - batch + 1); a batch of up
+// to 64 looks for it there, 64 values at a time, a larger one takes the latter.  The lengths are on the device, so every workgroup works this out for itself.
 struct Share {
   int b, len, first, last;      // sequence (-1: nothing is left for this slot), its tokens in the cache, steps
   int part, parts;              // of the sequence
@@ -221,6 +221,11 @@ __device__ __forceinline__ int steps_of(int tokens) { return (int)(((uint32_t)to
 
 __device__ __forceinline__ Share share_of(const AttentionArgs& a, int slot) {
   const int lane = threadIdx.x & 63, extra = steps_of(a.seen_nodes);
+  if (a.batch == 1) {
+    const int len = tokens_of(a, 0), steps = steps_of(len) + extra;
+    const int each = max((steps + a.slots - 1) / a.slots, a.least), parts = max(1, (steps + each - 1) / each);
+    return {slot < parts ? 0 : -1, len, slot * each, min((slot + 1) * each, steps), slot, parts};
+  }
   int64_t total = 0;
   int len = 0;
   for (int first = 0; first < a.batch; first += 64) {
@@ -230,18 +235,25 @@ __device__ __forceinline__ Share share_of(const AttentionArgs& a, int slot) {
   }
 #pragma unroll
   for (int i = 1; i < 64; i *= 2) total += __shfl_xor(total, i);
-  uint32_t each;      // steps of a part
   const int64_t over = a.slots - a.batch + 1;
-  if (total >> 32 == 0)
-    each = ((uint32_t)total + (uint32_t)over - 1) / (uint32_t)over;      // (total is below 2^32 less slots but for more than 30 10^9 tokens)
-  else
-    each = (uint32_t)((total + over - 1) / over);
-  each = max(each + a.unit - 1, (uint32_t)a.unit) / a.unit * a.unit;
+  int each = max((int)((total + over - 1) / over), a.least);      // steps of a part; it fits
+  if (a.batch <= 64 && a.slots > a.batch) {
+    const int steps = lane < a.batch ? steps_of(len) + extra : 0, from = max((int)((total + a.slots - 1) / a.slots), a.least);
+    const int mine = from + (int)((int64_t)(each - from) * lane / 64);
+    const float by = 1.0f / (float)mine;      // steps are below 2^26 and the quotient is raised by a step: at most one part too many is counted
+    int parts = 0;
+    for (int b = 0; b < a.batch; ++b) {
+      const int s = __builtin_amdgcn_readlane(steps, b);
+      parts += max(1, (int)((float)(s - 1) * by + 1.0f + 1.0f / 256));
+    }
+    const uint64_t fits = __ballot(parts <= a.slots);
+    if (fits != 0) each = __builtin_amdgcn_readlane(mine, __ffsll((unsigned long long)fits) - 1);
+  }
   int before = 0;
   for (int first = 0; first < a.batch; first += 64) {
     const int b = first + lane;
     if (a.batch > 64) len = b < a.batch ? tokens_of(a, b) : 0;
-    const int steps = steps_of(len) + extra, n = b < a.batch ? max(1, (int)((steps + each - 1) / each)) : 0;
+    const int steps = steps_of(len) + extra, n = b < a.batch ? max(1, (steps + each - 1) / each) : 0;
     int upto = n;
 #pragma unroll
     for (int i = 1; i < 64; i *= 2) {
@@ -252,7 +264,7 @@ __device__ __forceinline__ Share share_of(const AttentionArgs& a, int slot) {
     const uint64_t mine = __ballot(slot < upto && slot >= upto - n);
     if (mine != 0) {
       const int l = __ffsll((unsigned long long)mine) - 1, part = slot - __shfl(upto - n, l), s = __shfl(steps, l);
-      return {first + l, __shfl(len, l), (int)(part * each), min((int)((part + 1) * each), s), part, __shfl(n, l)};
+      return {first + l, __shfl(len, l), part * each, min((part + 1) * each, s), part, __shfl(n, l)};
     }
     before = __shfl(upto, 63);
   }
