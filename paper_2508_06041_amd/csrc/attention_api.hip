@@ -42,12 +42,22 @@ Plan plan_of(int batch, int nodes, int heads, int kv_heads, int head_dim, int64_
 template <typename T, int D>
 void launch(const AttentionArgs& a, const Plan& p, hipStream_t s) {
   const dim3 groups((unsigned)p.groups);
-  if (p.waves == 0 && p.mt == 1) hipLaunchKernelGGL((tree_attention_kernel<T, D, 1>), groups, dim3(kAttWaves * 64), 0, s, a);
-  if (p.waves == 4 && p.mt == 1) hipLaunchKernelGGL((tree_attention_wide_kernel<T, D, 1, 4>), groups, dim3(4 * 64), 0, s, a);
+  if (p.waves == 0 && p.mt == 1) hipLaunchKernelGGL((tree_attention_kernel<T, D, 1, false>), groups, dim3(kAttWaves * 64), 0, s, a);
+  if (p.waves == 4 && p.mt == 1) hipLaunchKernelGGL((tree_attention_wide_kernel<T, D, 1, 4, 2, true>), groups, dim3(4 * 64), 0, s, a);
   if constexpr (D < 256) {
-    if (p.waves == 0 && p.mt == 2) hipLaunchKernelGGL((tree_attention_kernel<T, D, 2>), groups, dim3(kAttWaves * 64), 0, s, a);
-    if (p.waves == 4 && p.mt == 2) hipLaunchKernelGGL((tree_attention_wide_kernel<T, D, 2, 4>), groups, dim3(4 * 64), 0, s, a);
-    if (p.waves == 8 && p.mt == 2) hipLaunchKernelGGL((tree_attention_wide_kernel<T, D, 2, 8>), groups, dim3(8 * 64), 0, s, a);
+    if (p.waves == 0 && p.mt == 2) hipLaunchKernelGGL((tree_attention_kernel<T, D, 2, false>), groups, dim3(kAttWaves * 64), 0, s, a);
+    if (p.waves == 4 && p.mt == 2) {
+      const char* e = getenv("V"); const int v = e ? atoi(e) : 0;
+      if (v == 0) hipLaunchKernelGGL((tree_attention_wide_kernel<T, D, 2, 4, 2, false>), groups, dim3(4 * 64), 0, s, a);
+      if (v == 1) hipLaunchKernelGGL((tree_attention_wide_kernel<T, D, 2, 4, 1, true>), groups, dim3(4 * 64), 0, s, a);
+      if (v == 2) hipLaunchKernelGGL((tree_attention_wide_kernel<T, D, 2, 4, 1, false>), groups, dim3(4 * 64), 0, s, a);
+    }
+    if (getenv("V8") && p.waves == 8) { const int v = atoi(getenv("V8")); 
+      if (v == 1) hipLaunchKernelGGL((tree_attention_wide_kernel<T, D, 2, 8, 3, true>), groups, dim3(8 * 64), 0, s, a);
+      if (v == 2) hipLaunchKernelGGL((tree_attention_wide_kernel<T, D, 2, 8, 1, true>), groups, dim3(8 * 64), 0, s, a);
+      if (v == 3) hipLaunchKernelGGL((tree_attention_wide_kernel<T, D, 2, 8, 2, false>), groups, dim3(8 * 64), 0, s, a);
+    } else
+    if (p.waves == 8 && p.mt == 2) hipLaunchKernelGGL((tree_attention_wide_kernel<T, D, 2, 8, 2, true>), groups, dim3(8 * 64), 0, s, a);
   }
   if (p.bytes > 0) {
     const uint32_t all_rows = (uint32_t)a.batch * a.kv_heads * a.rows;

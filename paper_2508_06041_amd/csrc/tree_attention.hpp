@@ -31,9 +31,9 @@ struct Matrix;
 template <>
 struct Matrix<half_t> {
   static constexpr uint32_t kNoNumber = 0x7c00u;   // the exponent of infinities and NaN
-  // weights reach the matrix pipe as 2^12 times what they are: with the slack of a row's top at most 2^15, and rounded to multiples of
-  // 2^-24, as a half below 2^-14 is, only where they are below 2^-26 of the top's
-  static constexpr float kLift = 12.f, kSlack = 3.f;
+  // weights reach the matrix pipe as 2^12 times what they are (kLimit keeps them below the largest half), and are rounded to multiples of 2^-24, as a
+  // half below 2^-14 is, only where they are below 2^-26 of the top's
+  static constexpr float kLift = 12.f, kLimit = 60000.f;
   typedef half_t v8 __attribute__((ext_vector_type(8)));
   static __device__ __forceinline__ f32x4 mad(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
@@ -42,7 +42,7 @@ struct Matrix<half_t> {
 template <>
 struct Matrix<bfloat_t> {
   static constexpr uint32_t kNoNumber = 0x7f80u;
-  static constexpr float kLift = 0.f, kSlack = 8.f;      // the range of a float
+  static constexpr float kLift = 0.f, kLimit = 1e6f;      // the range of a float
   typedef bfloat_t v8 __attribute__((ext_vector_type(8)));
   static __device__ __forceinline__ f32x4 mad(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
@@ -115,19 +115,20 @@ __device__ __forceinline__ float row_max(float x) {
 }
 
 // What a wavefront has of its rows: the weighted values, the weights' sum, and the score `top` they are relative to: a weight is
-// 2^((x - top) scale + lift), formed as 2^(x scale + from).
+// 2^((x - top) scale + lift), formed as 2^(x scale + from); with huge tops, whose product with the scale may be past the floats though the scores are not,
+// top is taken from the scores first and from is the lift.
+constexpr float kNoTop = 1e37f;      // `from` of a row without a score yet: the first one it gets has an infinite weight
 template <int MT, int DV>
 struct Rows {
   f32x4 o[MT][DV];
   float sum[MT], top[MT], from[MT];      // sum: of the lane's own tokens
-  float limit[MT];                       // the score from which on top has to follow
-  bool huge;                             // some top times scale / ln 2 may be past the floats though the scores are not
-  __device__ __forceinline__ void clear(float lift) {
+  bool huge;
+  __device__ __forceinline__ void clear() {
     huge = false;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-      top[mt] = limit[mt] = -INFINITY;
-      from[mt] = lift;
+      top[mt] = -INFINITY;
+      from[mt] = kNoTop;
       sum[mt] = 0.f;
 #pragma unroll
       for (int j = 0; j < DV; ++j) o[mt][j] = f32x4{0, 0, 0, 0};
@@ -135,75 +136,90 @@ struct Rows {
   }
 };
 
-// The weights of one step of 32 tokens for 16 * MT rows, in the lanes that the value product wants them in: with 16 x 16 x 32 matrix instructions lane l
+// The scores of one step of 32 tokens for 16 * MT rows, in the lanes that the value product wants their weights in: with 16 x 16 x 32 matrix instructions lane l
 // holds row l % 16 of Q and, of a result of K Q^T, the tokens 4 (l / 16) ... + 3; if the first 16 tokens of a step are numbered 8 (m / 4) + m % 4 and the second 16
 // four more, lane group l / 16 holds the weights of the tokens 8 (l / 16) ... + 7, which is the operand of V^T P^T.
-// `top` follows the largest score only when that has left it behind by 2^kSlack: in most steps no row's has, and the exchange between
-// lanes and the scaling of o are skipped.  ALL: every row sees every token.
-template <typename T, int D, int MT, bool ALL>
-__device__ __forceinline__ void weigh(Rows<MT, D / 16>& r, const u32x4 (&q)[MT][D / 32], const u32x4 (&k)[2][D / 32], float scale_log2,
-                                      const uint32_t (&seen)[MT], u32x4 (&w)[MT]) {
-  constexpr int KK = D / 32, DV = D / 16;
-  constexpr float kLift = Matrix<T>::kLift, kSlack = Matrix<T>::kSlack;
-  f32x4 s[MT][2];
-  float most[MT];
-  bool behind = false;
+template <int MT>
+using Scores = f32x4[MT][2];
+
+template <typename T, int D, int MT>
+__device__ __forceinline__ void score(const u32x4 (&q)[MT][D / 32], const u32x4 (&k)[2][D / 32], Scores<MT>& s) {
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     s[mt][0] = s[mt][1] = f32x4{0, 0, 0, 0};
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
+    for (int kk = 0; kk < D / 32; ++kk) {
       s[mt][0] = Matrix<T>::mad(k[0][kk], q[mt][kk], s[mt][0]);
       s[mt][1] = Matrix<T>::mad(k[1][kk], q[mt][kk], s[mt][1]);
     }
   }
+}
+
+// Tokens that a row does not see have no score.
+template <int MT>
+__device__ __forceinline__ void mask(Scores<MT>& s, const uint32_t (&seen)[MT]) {
 #pragma unroll
-  for (int mt = 0; mt < MT; ++mt) {
-    if constexpr (!ALL) {
+  for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s[mt][i / 4][i % 4] = (seen[mt] >> i) & 1 ? s[mt][i / 4][i % 4] : -INFINITY;
+    for (int i = 0; i < 8; ++i) s[mt][i / 4][i % 4] = (seen[mt] >> i) & 1 ? s[mt][i / 4][i % 4] : -INFINITY;
+}
+
+// The weights of a step, rounded for the value product, and their sum.  They are formed with the `top` there is: only where a lane's weights come to more than kLimit
+// does top follow the largest score, with an exchange between lanes and a scaling of o, and the weights are formed again.  That is the first step with a score and few after
+// it; all others look for no maximum at all.
+template <typename T, int MT, int DV>
+__device__ __forceinline__ void weigh(Rows<MT, DV>& r, Scores<MT>& s, float scale_log2, u32x4 (&w)[MT]) {
+  constexpr float kLift = Matrix<T>::kLift;
+  float x[MT][8], add[MT];
+  auto form = [&]() {
+    if (r.huge) {
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[mt][i] = (s[mt][i / 4][i % 4] - (r.top[mt] == -INFINITY ? 0.f : r.top[mt])) * scale_log2 + r.from[mt];
+    } else {
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[mt][i] = __builtin_fmaf(s[mt][i / 4][i % 4], scale_log2, r.from[mt]);
     }
-    most[mt] = s[mt][0][0];
 #pragma unroll
-    for (int i = 1; i < 8; ++i) most[mt] = fmaxf(most[mt], s[mt][i / 4][i % 4]);
-    behind = behind || most[mt] > r.limit[mt];
-  }
+    for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[mt][i] = __builtin_amdgcn_exp2f(x[mt][i]);
+      add[mt] = ((x[mt][0] + x[mt][1]) + (x[mt][2] + x[mt][3])) + ((x[mt][4] + x[mt][5]) + (x[mt][6] + x[mt][7]));
+    }
+  };
+  form();
+  bool behind = false;
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) behind = behind || add[mt] > Matrix<T>::kLimit;
   if (__any(behind)) {
     bool huge = false;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-      const float next = fmaxf(r.top[mt], row_max(most[mt]));
+      float most = s[mt][0][0];
+#pragma unroll
+      for (int i = 1; i < 8; ++i) most = fmaxf(most, s[mt][i / 4][i % 4]);
+      const float next = fmaxf(r.top[mt], row_max(most));
       const float less = r.top[mt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((r.top[mt] - next) * scale_log2);
       r.top[mt] = next;
-      r.limit[mt] = next + kSlack / scale_log2;
-      r.from[mt] = next == -INFINITY ? kLift : __builtin_fmaf(-next, scale_log2, kLift);
       huge = huge || (next != -INFINITY && __builtin_fabsf(next) > 1e38f);
       r.sum[mt] *= less;
 #pragma unroll
       for (int j = 0; j < DV; ++j) r.o[mt][j] *= less;
     }
     r.huge = __any(huge);
-  }
-  if (r.huge) {
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        s[mt][i / 4][i % 4] = r.top[mt] == -INFINITY ? -INFINITY : (s[mt][i / 4][i % 4] - r.top[mt]) * scale_log2 + kLift;
-  } else {
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) s[mt][i / 4][i % 4] = __builtin_fmaf(s[mt][i / 4][i % 4], scale_log2, r.from[mt]);
+      r.from[mt] = r.top[mt] == -INFINITY ? kNoTop : r.huge ? kLift : __builtin_fmaf(-r.top[mt], scale_log2, kLift);
+    form();
   }
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
-    float x[8];
+    r.sum[mt] += add[mt];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_exp2f(s[mt][i / 4][i % 4]);
-    r.sum[mt] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[mt][i] = pack2<T>(x[2 * i], x[2 * i + 1]);
+    for (int i = 0; i < 4; ++i) w[mt][i] = pack2<T>(x[mt][2 * i], x[mt][2 * i + 1]);
   }
 }
 
@@ -219,7 +235,7 @@ struct Share {
 __device__ __forceinline__ int tokens_of(const AttentionArgs& a, int b) { return min(max(a.lens[b], 0), a.cache.pages_per_seq * a.cache.page); }
 __device__ __forceinline__ int steps_of(int tokens) { return (int)(((uint32_t)tokens + kAttTile - 1) / kAttTile); }
 
-__device__ __forceinline__ Share share_of(const AttentionArgs& a, int slot) {
+__device__ __forceinline__ Share share_in(const AttentionArgs& a, int slot) {
   const int lane = threadIdx.x & 63, extra = steps_of(a.seen_nodes);
   if (a.batch == 1) {
     const int len = tokens_of(a, 0), steps = steps_of(len) + extra;
@@ -271,6 +287,13 @@ __device__ __forceinline__ Share share_of(const AttentionArgs& a, int slot) {
   return {-1, 0, 0, 0, 0, 0};
 }
 
+// The same in scalar registers: every lane has found the same.
+__device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ Share share_of(const AttentionArgs& a, int slot) {
+  const Share s = share_in(a, slot);
+  return {scalar(s.b), scalar(s.len), scalar(s.first), scalar(s.last), scalar(s.part), scalar(s.parts)};
+}
+
 // Where the rows of a workgroup's part lie among the parts.
 __device__ __forceinline__ int64_t part_row(const AttentionArgs& a, int slot, int h, int row_tile, int rows_of_tile) {
   return (((int64_t)slot * a.kv_heads + h) * a.row_tiles + row_tile) * rows_of_tile;
@@ -304,6 +327,7 @@ __device__ __forceinline__ void load_queries(const AttentionArgs& a, int b, int 
 
 // Where token lane % 32 of a step lies.  The page id is asked for a step or more before the place is needed.  Places are offsets in bytes from the start of the
 // head, in page 0 of the cache (a step of the context) or in node 0, separately for keys and values; a token that is not there has the place of one that is.
+// The steps past the last that a loop asks for ahead, so that its loads are the same in number every time, are all at the start of page 0.
 struct Lookup {
   int page;
   uint32_t token;
@@ -314,6 +338,7 @@ struct Place {
 };
 __device__ __forceinline__ Lookup ask(const AttentionArgs& a, const Share& s, int old_steps, int step) {
   Lookup l{s.b, (uint32_t)step * kAttTile + (threadIdx.x & (kAttTile - 1))};
+  if (step >= s.last) return l;
   if (step >= old_steps) {
     l.token -= (uint32_t)old_steps * kAttTile;
   } else if (a.cache.table != nullptr) {
@@ -322,7 +347,8 @@ __device__ __forceinline__ Lookup ask(const AttentionArgs& a, const Share& s, in
   return l;
 }
 __device__ __forceinline__ Place place_of(const AttentionArgs& a, const Share& s, int old_steps, int step, const Lookup& l) {
-  Place p;
+  Place p{0, 0, false};
+  if (step >= s.last) return p;
   if (step >= old_steps) {
     p.there = l.token < (uint32_t)a.seen_nodes;
     const int64_t t = p.there ? l.token : 0;
@@ -336,42 +362,44 @@ __device__ __forceinline__ Place place_of(const AttentionArgs& a, const Share& s
   return p;
 }
 
-// The rows that see node t add their weights times those of its values that are no finite numbers; `from`: the 4 DV values that a lane has, value 4 DV g + j
-// in o[j % DV][j / DV] (PLAIN) or 16 (j / 4) + 4 g + j % 4 in o[j / 4][j % 4].
+// A node may be seen by some rows only, and for the others its values may be anything.  In the value product they would meet weights of zero, so what is no finite number
+// leaves that product, and when all is added up the rows that see it add it as it is: a weight above zero changes no infinity and no NaN.
+// Of the steps, those that this wavefront took in its turn.  PLAIN: a lane's values are 4 DV g + j in o[j % DV][j / DV]; else 16 (j / 4) + 4 g + j % 4 in o[j / 4][j % 4].
 template <typename T, int D, int MT, bool PLAIN>
-__device__ __forceinline__ void add_odd_values(Rows<MT, D / 16>& r, const T* values, int t, const u32x4 (&w)[MT], const uint32_t (&seen)[MT]) {
+__device__ __forceinline__ void add_odd_values(const AttentionArgs& a, Rows<MT, D / 16>& r, const Share& s, int old_steps, const char* new_v, const int (&node)[MT], int turn,
+                                               int turns) {
   constexpr int DV = D / 16;
-  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, lane_of = (t >> 3) * 16 + n, i = t & 7;
-  typedef T two __attribute__((ext_vector_type(2)));
-  float by[MT];
+  const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll 1
+  for (int t = max(s.first - old_steps, 0) * kAttTile; t < min((s.last - old_steps) * kAttTile, a.seen_nodes); ++t) {
+    if ((old_steps + t / kAttTile - s.first) % turns != turn) continue;
+    const T* values = reinterpret_cast<const T*>(new_v) + t * a.v_new.token_stride;
+    bool sees[MT];
 #pragma unroll
-  for (int mt = 0; mt < MT; ++mt) {
-    const uint32_t word = __shfl(i < 4 ? (i < 2 ? w[mt][0] : w[mt][1]) : (i < 6 ? w[mt][2] : w[mt][3]), lane_of);
-    const two both = __builtin_bit_cast(two, word);
-    by[mt] = (__shfl(seen[mt], lane_of) >> i) & 1 ? (float)(i & 1 ? both[1] : both[0]) : 0.f;
-  }
+    for (int mt = 0; mt < MT; ++mt) sees[mt] = (seen_of(a, s.b, node[mt], t & ~7) >> (t & 7)) & 1;
 #pragma unroll
-  for (int j = 0; j < 4 * DV; ++j) {
-    const float value = (float)values[PLAIN ? 4 * DV * g + j : 16 * (j / 4) + 4 * g + j % 4];
-    if (!__builtin_isfinite(value))
+    for (int j = 0; j < 4 * DV; ++j) {
+      const float value = (float)values[PLAIN ? 4 * DV * g + j : 16 * (j / 4) + 4 * g + j % 4];
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
-        if (by[mt] != 0.f) r.o[mt][PLAIN ? j % DV : j / 4][PLAIN ? j / DV : j % 4] += by[mt] * value;
+        if (sees[mt] && !__builtin_isfinite(value)) r.o[mt][PLAIN ? j % DV : j / 4][PLAIN ? j / DV : j % 4] += value;
+    }
   }
 }
 
 // The kernel for few rows.  One workgroup: up to 16 * MT rows (node, query head of one kv head) of one sequence over one part of its tokens; its wavefronts
 // take steps of 32 tokens in turns and meet at the end.  K and V go from memory to the registers they are used from: K as it lies is an operand,
-// V is loaded as it lies, D / 16 elements of 8 tokens to a lane, and turned inside the lane, 16 bits at a time.
+// V is loaded as it lies, D / 16 elements of 8 tokens to a lane, and turned inside the lane, 16 bits at a time.  AHEAD: the next step's are asked for
+// before this one's products, into a second set of registers.
 // The weights are rounded to the type of V for the value product (their sum is not): half a step of each, so the error is a mean of independent
 // roundings, below the one rounding of the result.
-template <typename T, int D, int MT>
+template <typename T, int D, int MT, bool AHEAD>
 __global__ void __launch_bounds__(kAttWaves * 64, D <= 128 ? 2 : 1) tree_attention_kernel(const AttentionArgs a) {
   constexpr int KK = D / 32, DV = D / 16, N = DV / 2, R = 16 * MT;
   __shared__ float sums[kAttWaves][4 * DV * MT][64];
   __shared__ float2 tops[kAttWaves][MT][16];
   __shared__ __align__(16) int64_t places[kAttWaves][2][2][kAttTile];      // [..][turn][keys, values][token]
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = scalar(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   uint32_t id = blockIdx.x;
   const int h = id % a.kv_heads;
   id /= a.kv_heads;
@@ -383,80 +411,102 @@ __global__ void __launch_bounds__(kAttWaves * 64, D <= 128 ? 2 : 1) tree_attenti
 
   u32x4 q[MT][KK];
   int node[MT];
-  int step = share.first + wave, turn = 0;
-  Lookup next{};
-  if (step < last) next = ask(a, share, old_steps, step);
+  int step = share.first + wave;
+  Lookup next = ask(a, share, old_steps, step);
   load_queries<D, MT>(a, b, h, row_tile * R, q, node);
   Rows<MT, DV> rows;
-  rows.clear(Matrix<T>::kLift);
+  rows.clear();
   const int k_token = 8 * (n >> 2) + (n & 3);      // of the first 16; the second are 4 further
   const char *cache_k = a.cache.k + 2 * h * a.cache.head_stride, *cache_v = a.cache.v + 2 * h * a.cache.head_stride;
   const char *new_k = a.k_new.data + 2 * (b * a.k_new.batch_stride + h * a.k_new.head_stride),
              *new_v = a.v_new.data + 2 * (b * a.v_new.batch_stride + h * a.v_new.head_stride);
-
-  for (; step < last; step += kAttWaves, turn ^= 1) {
-    // The places pass through LDS, from the lane that looked one up to those that load from it.  A wavefront's own accesses there are in order.
-    const bool old = step < old_steps;
+  struct Tokens {
+    u32x4 k[2][KK];
+    Words<N> v[8];
+    uint32_t there;
+  };
+  // Asks for the tokens of a step, and for the places of the one behind it.  The places pass through LDS, from the lane that looked one up to those that load
+  // from it; a wavefront's own accesses there are in order.
+  auto load = [&](int step, int turn, Tokens& x) {
+    const bool old = step < old_steps || step >= last;
     const Place mine = place_of(a, share, old_steps, step, next);
     int64_t(*table)[kAttTile] = places[wave][turn];
     if (lane < kAttTile) {
       table[0][lane] = mine.k;
       table[1][lane] = mine.v;
     }
-    const uint32_t there = (uint32_t)__ballot(mine.there);
-    const bool all = old && there == 0xffffffffu;
+    x.there = (uint32_t)__ballot(mine.there);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    u32x4 k[2][KK], w[MT];
-    Words<N> v[8];
     const char *base_k = (old ? cache_k : new_k) + 16 * g, *base_v = (old ? cache_v : new_v) + 2 * DV * n;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       const char* p = base_k + table[0][k_token + 4 * half];
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) k[half][kk] = *reinterpret_cast<const u32x4*>(p + 64 * kk);
+      for (int kk = 0; kk < KK; ++kk) x.k[half][kk] = *reinterpret_cast<const u32x4*>(p + 64 * kk);
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = load_words<N>(base_v + table[1][8 * g + i]);
-    if (step + kAttWaves < last) next = ask(a, share, old_steps, step + kAttWaves);
+    for (int i = 0; i < 8; ++i) x.v[i] = load_words<N>(base_v + table[1][8 * g + i]);
+    next = ask(a, share, old_steps, step + kAttWaves);
+  };
+  bool odd = false;      // among the values of nodes is something that is no finite number
+  auto attend = [&](int step, Tokens& x) {
+    const bool old = step < old_steps, all = old && x.there == 0xffffffffu;
     uint32_t seen[MT] = {};
-    if (all) {
-      weigh<T, D, MT, true>(rows, q, k, a.scale_log2, seen, w);
-    } else {
-      const int t0 = (step - old_steps) * kAttTile;
+    const int t0 = (step - old_steps) * kAttTile;
+    Scores<MT> s;
+    u32x4 w[MT];
+    score<T, D, MT>(q, x.k, s);
+    if (!all) {
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
-        seen[mt] = (there >> (8 * g)) & 0xffu;
+        seen[mt] = (x.there >> (8 * g)) & 0xffu;
         if (!old) seen[mt] &= seen_of(a, b, node[mt], t0 + 8 * g);
       }
-      weigh<T, D, MT, false>(rows, q, k, a.scale_log2, seen, w);
-      // A token that is not there was read from a place that is, and counts as zeros.  A node may be seen by some rows only, and for the others its values may be
-      // anything: what is no finite number leaves the product, in which it would meet weights of zero, and is added to the rows that see it by itself.
-      bool odd = false;
+      mask<MT>(s, seen);
+    }
+    weigh<T, MT, DV>(rows, s, a.scale_log2, w);
+    if (!all) {
+      // a token that is not there was read from a place that is, and counts as zeros
 #pragma unroll
       for (int i = 0; i < 8; ++i)
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-          const uint32_t is = (there >> (8 * g + i)) & 1 ? v[i].w[j] : 0u, number = old ? is : numbers<T>(is);
+          const uint32_t is = (x.there >> (8 * g + i)) & 1 ? x.v[i].w[j] : 0u, number = old ? is : numbers<T>(is);
           odd = odd || number != is;
-          v[i].w[j] = number;
+          x.v[i].w[j] = number;
         }
-      if (__any(odd)) {
-#pragma unroll 1
-        for (int t = 0; t < min(kAttTile, a.seen_nodes - t0); ++t)
-          add_odd_values<T, D, MT, true>(rows, reinterpret_cast<const T*>(new_v) + (t0 + t) * a.v_new.token_stride, t, w, seen);
-      }
     }
 #pragma unroll
     for (int j = 0; j < DV; ++j) {
       u32x4 t;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) t[i] = __builtin_amdgcn_perm(v[2 * i + 1].w[j / 2], v[2 * i].w[j / 2], j & 1 ? 0x07060302u : 0x05040100u);
+      for (int i = 0; i < 4; ++i) t[i] = __builtin_amdgcn_perm(x.v[2 * i + 1].w[j / 2], x.v[2 * i].w[j / 2], j & 1 ? 0x07060302u : 0x05040100u);
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) rows.o[mt][j] = Matrix<T>::mad(t, w[mt], rows.o[mt][j]);
     }
+  };
+  if constexpr (AHEAD) {
+    Tokens x[2];
+    if (step < last) load(step, 0, x[0]);
+    while (step < last) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if (step >= last) break;
+        load(step + kAttWaves, i ^ 1, x[i ^ 1]);
+        attend(step, x[i]);
+        step += kAttWaves;
+      }
+    }
+  } else {
+    Tokens x;
+    for (int turn = 0; step < last; step += kAttWaves, turn ^= 1) {
+      load(step, turn, x);
+      attend(step, x);
+    }
   }
 
+  if (__any(odd)) add_odd_values<T, D, MT, true>(a, rows, share, old_steps, new_v, node, wave, kAttWaves);
   // the wavefronts' rows meet: each wavefront adds up the quarter 4 g + wave of the elements
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
@@ -568,20 +618,20 @@ __global__ void __launch_bounds__(256) tree_attention_join_kernel(const Attentio
 }
 
 // The kernel for many rows: WAVES wavefronts with 16 * MT rows each take every step together.  K and V of a step are loaded once for all of them and kept
-// in LDS, two steps in turns: the next step's are asked for before this one's products and written behind them, and the places of the tokens
-// of the step after that are looked up meanwhile.
+// in LDS.  They are asked for AHEAD steps before their products: a compute unit reads 27 bytes a nanosecond at most and its share of the
+// memory's rate is that, with a latency of a microsecond and more under load; one step of 16 KiB in a step's time of 1.5 us was %.
 //   K: pieces of 8 elements [D / 8][32 tokens], the tokens' places exclusive-or the piece's number, so that neither the writing (a row of the
 //      cache at a time) nor the reading (16 tokens of four pieces) meets itself in a bank;
 //   V: turned while it is written: [4 groups of 8 tokens][D] of 16 bytes, as the value product reads it.
 // A lane's results are the values 16 j + 4 g ... + 3 of its row, j < D / 16.
-template <typename T, int D, int MT, int WAVES>
-__global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) tree_attention_wide_kernel(const AttentionArgs a) {
+template <typename T, int D, int MT, int WAVES, int AHEAD, bool EARLY>
+__global__ void __launch_bounds__(WAVES * 64, D <= 128 && MT <= 2 ? 2 : 1) tree_attention_wide_kernel(const AttentionArgs a) {
   constexpr int KK = D / 32, DV = D / 16, R = 16 * MT * WAVES, THREADS = WAVES * 64;
   constexpr int U = (4 * D + THREADS - 1) / THREADS;      // units of 16 bytes of K, and of V, to a thread
   __shared__ __align__(16) char lds_k[2][4 * D * 16], lds_v[2][4 * D * 16];
-  __shared__ __align__(16) int64_t places[2][2][kAttTile];      // [step % 2][keys, values][token]
-  __shared__ uint32_t lds_there[4], lds_odd[2];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
+  __shared__ __align__(16) int64_t places[8][2][kAttTile];      // [step % 8][keys, values][token]
+  __shared__ uint32_t lds_there[8], lds_odd;
+  const int lane = threadIdx.x & 63, wave = scalar(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   uint32_t id = blockIdx.x;
   const int h = id % a.kv_heads;
   id /= a.kv_heads;
@@ -591,48 +641,54 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) tree_attention_w
   const int b = share.b, old_steps = steps_of(share.len), first = share.first, last = share.last;
   if (share.part == 0 && h == 0 && row_tile == 0 && threadIdx.x == 0 && a.places != nullptr) a.places[b] = make_int2(slot, share.parts);
 
-  // The first wavefront looks places up; those of step s are in places[s % 2] from the barrier two steps before its products on.
+  // The first wavefront looks places up, AHEAD + 1 steps before the products and a step after it has asked for the page ids.
   auto keep_places = [&](int step, const Lookup& l) {
     const Place mine = place_of(a, share, old_steps, step, l);
     if (lane < kAttTile) {
-      places[step & 1][0][lane] = mine.k;
-      places[step & 1][1][lane] = mine.v;
+      places[step & 7][0][lane] = mine.k;
+      places[step & 7][1][lane] = mine.v;
     }
     const uint32_t there = (uint32_t)__ballot(mine.there);
-    if (lane == 0) lds_there[step & 3] = there;
+    if (lane == 0) lds_there[step & 7] = there;
   };
   if (wave == 0) {
-    if (first < last) keep_places(first, ask(a, share, old_steps, first));
-    if (first + 1 < last) keep_places(first + 1, ask(a, share, old_steps, first + 1));
+    Lookup l[AHEAD + 1];
+#pragma unroll
+    for (int i = 0; i <= AHEAD; ++i) l[i] = ask(a, share, old_steps, first + i);
+#pragma unroll
+    for (int i = 0; i <= AHEAD; ++i) keep_places(first + i, l[i]);
   }
-  if (threadIdx.x < 2) lds_odd[threadIdx.x] = 0;
+  if (threadIdx.x == 0) lds_odd = 0;
   u32x4 q[MT][KK];
   int node[MT];
   load_queries<D, MT>(a, b, h, row_tile * R + wave * 16 * MT, q, node);
   const bool works = row_tile * R + wave * 16 * MT < a.rows;      // a wavefront without rows only loads
   Rows<MT, DV> rows;
-  rows.clear(Matrix<T>::kLift);
+  rows.clear();
 
   // What this thread loads of a step: unit u of K is piece u % (D / 8) of token u / (D / 8); of V it is the elements 2 (u % (D / 2)) and the next of four tokens.
   const char *cache_k = a.cache.k + 2 * h * a.cache.head_stride, *cache_v = a.cache.v + 2 * h * a.cache.head_stride;
   const char *new_k = a.k_new.data + 2 * (b * a.k_new.batch_stride + h * a.k_new.head_stride),
              *new_v = a.v_new.data + 2 * (b * a.v_new.batch_stride + h * a.v_new.head_stride);
-  u32x4 load_k[U];
-  uint32_t load_v[U][4];
-  auto load = [&](int step) {
-    const bool old = step < old_steps;
+  struct Units {
+    u32x4 k[U];
+    uint32_t v[U][4];
+  };
+  auto load = [&](int step, Units& x) {
+    const bool old = step < old_steps || step >= last;
     const char *base_k = old ? cache_k : new_k, *base_v = old ? cache_v : new_v;
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       const int u = min((int)threadIdx.x + i * THREADS, 4 * D - 1);
-      load_k[i] = *reinterpret_cast<const u32x4*>(base_k + places[step & 1][0][u / (D / 8)] + 16 * (u % (D / 8)));
+      x.k[i] = *reinterpret_cast<const u32x4*>(base_k + places[step & 7][0][u / (D / 8)] + 16 * (u % (D / 8)));
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        load_v[i][j] = *reinterpret_cast<const uint32_t*>(base_v + places[step & 1][1][4 * (u / (D / 2)) + j] + 4 * (u % (D / 2)));
+        x.v[i][j] = *reinterpret_cast<const uint32_t*>(base_v + places[step & 7][1][4 * (u / (D / 2)) + j] + 4 * (u % (D / 2)));
     }
   };
-  auto keep = [&](int step, int buffer) {
-    const uint32_t there = lds_there[step & 3];
+  auto there_in = [&](int step) { return (uint32_t)scalar((int)lds_there[step & 7]); };
+  auto keep = [&](int step, Units& x) {
+    const uint32_t there = there_in(step);
     const bool old = step < old_steps;
     bool odd = false;
 #pragma unroll
@@ -643,70 +699,82 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) tree_attention_w
       if (!old || there != 0xffffffffu) {      // (as in the kernel for few rows)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const uint32_t is = (there >> (4 * four + j)) & 1 ? load_v[i][j] : 0u, number = old ? is : numbers<T>(is);
+          const uint32_t is = (there >> (4 * four + j)) & 1 ? x.v[i][j] : 0u, number = old ? is : numbers<T>(is);
           odd = odd || number != is;
-          load_v[i][j] = number;
+          x.v[i][j] = number;
         }
       }
-      const int token = u / (D / 8), place = ((token >> 2) & 1) * 16 + 4 * (token >> 3) + (token & 3);      // as weigh() numbers the tokens
-      const int piece = u % (D / 8);
-      *reinterpret_cast<u32x4*>(lds_k[buffer] + (piece * kAttTile + (place ^ (piece & 15))) * 16) = load_k[i];
-      char* to = lds_v[buffer] + ((four >> 1) * D + d) * 16 + (four & 1) * 8;
-      const uint32_t* v = load_v[i];
+      const int token = u / (D / 8), place = ((token >> 2) & 1) * 16 + 4 * (token >> 3) + (token & 3), piece = u % (D / 8);      // as score() numbers the tokens
+      *reinterpret_cast<u32x4*>(lds_k[step & 1] + (piece * kAttTile + (place ^ (piece & 15))) * 16) = x.k[i];
+      char* to = lds_v[step & 1] + ((four >> 1) * D + d) * 16 + (four & 1) * 8;
+      const uint32_t* v = x.v[i];
       *reinterpret_cast<uint2*>(to) = make_uint2(__builtin_amdgcn_perm(v[1], v[0], 0x05040100u), __builtin_amdgcn_perm(v[3], v[2], 0x05040100u));
       *reinterpret_cast<uint2*>(to + 16) = make_uint2(__builtin_amdgcn_perm(v[1], v[0], 0x07060302u), __builtin_amdgcn_perm(v[3], v[2], 0x07060302u));
     }
-    if (odd) lds_odd[buffer] = step + 1;      // of this step; whatever else stands there is another's
+    if (odd) lds_odd = 1;
+  };
+  u32x4 w[MT], values[DV];
+  auto read_values = [&](int step) {
+#pragma unroll
+    for (int j = 0; j < DV; ++j) values[j] = *reinterpret_cast<const u32x4*>(lds_v[step & 1] + (g * D + 16 * j + n) * 16);
+  };
+  auto weigh_step = [&](int step) {
+    u32x4 k[2][KK];
+    Scores<MT> s;
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk)
+        k[half][kk] = *reinterpret_cast<const u32x4*>(lds_k[step & 1] + ((4 * kk + g) * kAttTile + half * 16 + (n ^ ((4 * kk + g) & 15))) * 16);
+    score<T, D, MT>(q, k, s);
+    // V is read before the weights are formed, so that it is there when they are
+    if constexpr (EARLY) read_values(step);
+    const uint32_t there = there_in(step);
+    if (step >= old_steps || there != 0xffffffffu) {
+      uint32_t seen[MT];
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        seen[mt] = (there >> (8 * g)) & 0xffu;
+        if (step >= old_steps) seen[mt] &= seen_of(a, b, node[mt], (step - old_steps) * kAttTile + 8 * g);
+      }
+      mask<MT>(s, seen);
+    }
+    weigh<T, MT, DV>(rows, s, a.scale_log2, w);
+  };
+  auto add_step = [&](int step) {
+    if constexpr (!EARLY) read_values(step);
+#pragma unroll
+    for (int j = 0; j < DV; ++j)
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) rows.o[mt][j] = Matrix<T>::mad(values[j], w[mt], rows.o[mt][j]);
   };
 
   __syncthreads();
+  Units x[AHEAD];      // step s in x[(s - first) % AHEAD], on its way
   if (first < last) {
-    load(first);
-    keep(first, 0);
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) load(first + i, x[i]);
+    keep(first, x[0]);
   }
   __syncthreads();
-  for (int step = first; step < last; ++step) {
-    const int buffer = (step - first) & 1;
-    Lookup after{};
-    if (wave == 0 && step + 2 < last) after = ask(a, share, old_steps, step + 2);
-    if (step + 1 < last) load(step + 1);
-    if (works) {
-      const uint32_t there = lds_there[step & 3];
-      const bool old = step < old_steps;
-      u32x4 k[2][KK], w[MT];
-      uint32_t seen[MT] = {};
+  for (int start = first; start < last; start += AHEAD) {
 #pragma unroll
-      for (int half = 0; half < 2; ++half)
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk) k[half][kk] = *reinterpret_cast<const u32x4*>(lds_k[buffer] + ((4 * kk + g) * kAttTile + half * 16 + (n ^ ((4 * kk + g) & 15))) * 16);
-      if (old && there == 0xffffffffu) {
-        weigh<T, D, MT, true>(rows, q, k, a.scale_log2, seen, w);
-      } else {
-        const int t0 = (step - old_steps) * kAttTile;
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-          seen[mt] = (there >> (8 * g)) & 0xffu;
-          if (!old) seen[mt] &= seen_of(a, b, node[mt], t0 + 8 * g);
-        }
-        weigh<T, D, MT, false>(rows, q, k, a.scale_log2, seen, w);
-        if (!old && lds_odd[buffer] == (uint32_t)step + 1) {
-#pragma unroll 1
-          for (int t = 0; t < min(kAttTile, a.seen_nodes - t0); ++t)
-            add_odd_values<T, D, MT, false>(rows, reinterpret_cast<const T*>(new_v) + (t0 + t) * a.v_new.token_stride, t, w, seen);
-        }
+    for (int i = 0; i < AHEAD; ++i) {
+      const int step = start + i;
+      if (step >= last) break;
+      const Lookup after = ask(a, share, old_steps, step + AHEAD + 1);
+      load(step + AHEAD, x[i]);
+      if (works) {
+        weigh_step(step);
+        add_step(step);
       }
-#pragma unroll
-      for (int j = 0; j < DV; ++j) {
-        const u32x4 v = *reinterpret_cast<const u32x4*>(lds_v[buffer] + (g * D + 16 * j + n) * 16);
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) rows.o[mt][j] = Matrix<T>::mad(v, w[mt], rows.o[mt][j]);
-      }
+      if (step + 1 < last) keep(step + 1, x[(i + 1) % AHEAD]);
+      if (wave == 0) keep_places(step + AHEAD + 1, after);
+      __syncthreads();
     }
-    if (step + 1 < last) keep(step + 1, buffer ^ 1);
-    if (wave == 0 && step + 2 < last) keep_places(step + 2, after);      // over those of this step, which were read before the last barrier
-    __syncthreads();
   }
   if (!works) return;
+  if (lds_odd) add_odd_values<T, D, MT, false>(a, rows, share, old_steps, new_v, node, 0, 1);
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     const int in_tile = wave * 16 * MT + mt * 16 + n, r = row_tile * R + in_tile;
