@@ -3,7 +3,6 @@
 
 #include <algorithm>
 #include <cmath>
-#include <cstdlib>
 
 #include "token_host.hpp"
 #include "tree_attention.hpp"
@@ -23,13 +22,12 @@ struct Plan {
 Plan plan_of(int batch, int nodes, int heads, int kv_heads, int head_dim, int64_t max_len) {
   Plan p;
   p.rows = nodes * (heads / kv_heads);
-  p.waves = p.rows <= 32 ? 0 : p.rows <= 128 || head_dim == 256 || (getenv("W4") && atoi(getenv("W4"))) ? 4 : 8;
+  p.waves = p.rows <= 32 ? 0 : p.rows <= 128 || head_dim == 256 ? 4 : 8;
   p.mt = head_dim == 256 || p.rows <= 16 || (p.rows > 32 && p.rows <= 64) ? 1 : 2;
   p.tile = 16 * p.mt * std::max(p.waves, 1);
   p.row_tiles = (p.rows + p.tile - 1) / p.tile;
   const int64_t steps = (max_len + kAttTile - 1) / kAttTile + (nodes + kAttTile - 1) / kAttTile, tiles = (int64_t)kv_heads * p.row_tiles;
-  static const int F = getenv("FILL") ? atoi(getenv("FILL")) : 0;
-  const int64_t most = batch * ((steps + kAttWaves - 1) / kAttWaves), fill = ((F ? F : p.waves == 8 ? 256 : 512) + tiles - 1) / tiles;
+  const int64_t most = batch * ((steps + kAttWaves - 1) / kAttWaves), fill = ((p.waves == 8 ? 256 : 512) + tiles - 1) / tiles;
   p.slots = (int)std::max<int64_t>(batch, std::min(most, fill >= 2 * batch ? fill : 3 * (int64_t)batch));
   p.groups = p.slots * tiles;
   const bool whole = p.slots == batch;
@@ -42,22 +40,12 @@ Plan plan_of(int batch, int nodes, int heads, int kv_heads, int head_dim, int64_
 template <typename T, int D>
 void launch(const AttentionArgs& a, const Plan& p, hipStream_t s) {
   const dim3 groups((unsigned)p.groups);
-  if (p.waves == 0 && p.mt == 1) hipLaunchKernelGGL((tree_attention_kernel<T, D, 1, false>), groups, dim3(kAttWaves * 64), 0, s, a);
-  if (p.waves == 4 && p.mt == 1) hipLaunchKernelGGL((tree_attention_wide_kernel<T, D, 1, 4, 2, true>), groups, dim3(4 * 64), 0, s, a);
+  if (p.waves == 0 && p.mt == 1) hipLaunchKernelGGL((tree_attention_kernel<T, D, 1>), groups, dim3(kAttWaves * 64), 0, s, a);
+  if (p.waves == 4 && p.mt == 1) hipLaunchKernelGGL((tree_attention_wide_kernel<T, D, 1, 4>), groups, dim3(4 * 64), 0, s, a);
   if constexpr (D < 256) {
-    if (p.waves == 0 && p.mt == 2) hipLaunchKernelGGL((tree_attention_kernel<T, D, 2, false>), groups, dim3(kAttWaves * 64), 0, s, a);
-    if (p.waves == 4 && p.mt == 2) {
-      const char* e = getenv("V"); const int v = e ? atoi(e) : 0;
-      if (v == 0) hipLaunchKernelGGL((tree_attention_wide_kernel<T, D, 2, 4, 2, false>), groups, dim3(4 * 64), 0, s, a);
-      if (v == 1) hipLaunchKernelGGL((tree_attention_wide_kernel<T, D, 2, 4, 1, true>), groups, dim3(4 * 64), 0, s, a);
-      if (v == 2) hipLaunchKernelGGL((tree_attention_wide_kernel<T, D, 2, 4, 1, false>), groups, dim3(4 * 64), 0, s, a);
-    }
-    if (getenv("V8") && p.waves == 8) { const int v = atoi(getenv("V8")); 
-      if (v == 1) hipLaunchKernelGGL((tree_attention_wide_kernel<T, D, 2, 8, 3, true>), groups, dim3(8 * 64), 0, s, a);
-      if (v == 2) hipLaunchKernelGGL((tree_attention_wide_kernel<T, D, 2, 8, 1, true>), groups, dim3(8 * 64), 0, s, a);
-      if (v == 3) hipLaunchKernelGGL((tree_attention_wide_kernel<T, D, 2, 8, 2, false>), groups, dim3(8 * 64), 0, s, a);
-    } else
-    if (p.waves == 8 && p.mt == 2) hipLaunchKernelGGL((tree_attention_wide_kernel<T, D, 2, 8, 2, true>), groups, dim3(8 * 64), 0, s, a);
+    if (p.waves == 0 && p.mt == 2) hipLaunchKernelGGL((tree_attention_kernel<T, D, 2>), groups, dim3(kAttWaves * 64), 0, s, a);
+    if (p.waves == 4 && p.mt == 2) hipLaunchKernelGGL((tree_attention_wide_kernel<T, D, 2, 4>), groups, dim3(4 * 64), 0, s, a);
+    if (p.waves == 8 && p.mt == 2) hipLaunchKernelGGL((tree_attention_wide_kernel<T, D, 2, 8>), groups, dim3(8 * 64), 0, s, a);
   }
   if (p.bytes > 0) {
     const uint32_t all_rows = (uint32_t)a.batch * a.kv_heads * a.rows;

@@ -50,10 +50,13 @@ int check_verify(const char* who, int batch, int nodes, int vocabulary, int dtyp
 
 template <typename T>
 void launch_verify(const VerifyArgs& a, hipStream_t s) {
-  const unsigned pieces = (unsigned)a.batch * a.nodes * a.chunks;
-  hipLaunchKernelGGL(verify_parts_kernel<T>, dim3(pieces, a.draft ? 2 : 1), dim3(kVerThreads), 0, s, a);
-  for (int round = 0; a.draft && round < a.siblings; ++round) hipLaunchKernelGGL(verify_rest_kernel<T>, dim3(pieces), dim3(kVerThreads), 0, s, a, round);
-  hipLaunchKernelGGL(verify_choose_kernel<T>, dim3(a.batch), dim3(kVerThreads), 0, s, a);
+  const unsigned rows = (unsigned)a.batch * a.nodes;
+  hipLaunchKernelGGL(verify_parts_kernel<T>, dim3(rows * a.chunks, a.draft ? 2 : 1), dim3(kVerThreads), 0, s, a);
+  // a workgroup finds out first whether its row needs a sum at all, so rows share few of them where there are many rows
+  const int groups = std::max(1, std::min(a.chunks, (int)(2048 / rows)));
+  for (int round = 0; a.draft && round < a.siblings; ++round)
+    hipLaunchKernelGGL(verify_rest_kernel<T>, dim3(rows * groups), dim3(kVerThreads), 0, s, a, round, groups);
+  hipLaunchKernelGGL(verify_choose_kernel<T>, dim3(a.batch), dim3(kVerChooseThreads), 0, s, a);
 }
 
 }  // namespace

@@ -332,6 +332,8 @@ struct Lookup {
   int page;
   uint32_t token;
 };
+// (a choice between values: between variables, which it is in a lambda, it would be one of addresses, and put them into memory)
+__device__ __forceinline__ const char* either(bool first, const char* a, const char* b) { return first ? a : b; }
 struct Place {
   int64_t k, v;
   bool there;
@@ -389,11 +391,10 @@ __device__ __forceinline__ void add_odd_values(const AttentionArgs& a, Rows<MT, 
 
 // The kernel for few rows.  One workgroup: up to 16 * MT rows (node, query head of one kv head) of one sequence over one part of its tokens; its wavefronts
 // take steps of 32 tokens in turns and meet at the end.  K and V go from memory to the registers they are used from: K as it lies is an operand,
-// V is loaded as it lies, D / 16 elements of 8 tokens to a lane, and turned inside the lane, 16 bits at a time.  AHEAD: the next step's are asked for
-// before this one's products, into a second set of registers.
+// V is loaded as it lies, D / 16 elements of 8 tokens to a lane, and turned inside the lane, 16 bits at a time.
 // The weights are rounded to the type of V for the value product (their sum is not): half a step of each, so the error is a mean of independent
 // roundings, below the one rounding of the result.
-template <typename T, int D, int MT, bool AHEAD>
+template <typename T, int D, int MT>
 __global__ void __launch_bounds__(kAttWaves * 64, D <= 128 ? 2 : 1) tree_attention_kernel(const AttentionArgs a) {
   constexpr int KK = D / 32, DV = D / 16, N = DV / 2, R = 16 * MT;
   __shared__ float sums[kAttWaves][4 * DV * MT][64];
@@ -438,7 +439,7 @@ __global__ void __launch_bounds__(kAttWaves * 64, D <= 128 ? 2 : 1) tree_attenti
     x.there = (uint32_t)__ballot(mine.there);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    const char *base_k = (old ? cache_k : new_k) + 16 * g, *base_v = (old ? cache_v : new_v) + 2 * DV * n;
+    const char *base_k = either(old, cache_k, new_k) + 16 * g, *base_v = either(old, cache_v, new_v) + 2 * DV * n;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       const char* p = base_k + table[0][k_token + 4 * half];
@@ -486,24 +487,10 @@ __global__ void __launch_bounds__(kAttWaves * 64, D <= 128 ? 2 : 1) tree_attenti
       for (int mt = 0; mt < MT; ++mt) rows.o[mt][j] = Matrix<T>::mad(t, w[mt], rows.o[mt][j]);
     }
   };
-  if constexpr (AHEAD) {
-    Tokens x[2];
-    if (step < last) load(step, 0, x[0]);
-    while (step < last) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        if (step >= last) break;
-        load(step + kAttWaves, i ^ 1, x[i ^ 1]);
-        attend(step, x[i]);
-        step += kAttWaves;
-      }
-    }
-  } else {
-    Tokens x;
-    for (int turn = 0; step < last; step += kAttWaves, turn ^= 1) {
-      load(step, turn, x);
-      attend(step, x);
-    }
+  Tokens x;
+  for (int turn = 0; step < last; step += kAttWaves, turn ^= 1) {
+    load(step, turn, x);
+    attend(step, x);
   }
 
   if (__any(odd)) add_odd_values<T, D, MT, true>(a, rows, share, old_steps, new_v, node, wave, kAttWaves);
@@ -618,19 +605,18 @@ __global__ void __launch_bounds__(256) tree_attention_join_kernel(const Attentio
 }
 
 // The kernel for many rows: WAVES wavefronts with 16 * MT rows each take every step together.  K and V of a step are loaded once for all of them and kept
-// in LDS.  They are asked for AHEAD steps before their products: a compute unit reads 27 bytes a nanosecond at most and its share of the
-// memory's rate is that, with a latency of a microsecond and more under load; one step of 16 KiB in a step's time of 1.5 us was %.
+// in LDS, two steps in turns: the next step's are asked for before this one's products and written behind them.
 //   K: pieces of 8 elements [D / 8][32 tokens], the tokens' places exclusive-or the piece's number, so that neither the writing (a row of the
 //      cache at a time) nor the reading (16 tokens of four pieces) meets itself in a bank;
 //   V: turned while it is written: [4 groups of 8 tokens][D] of 16 bytes, as the value product reads it.
 // A lane's results are the values 16 j + 4 g ... + 3 of its row, j < D / 16.
-template <typename T, int D, int MT, int WAVES, int AHEAD, bool EARLY>
+template <typename T, int D, int MT, int WAVES>
 __global__ void __launch_bounds__(WAVES * 64, D <= 128 && MT <= 2 ? 2 : 1) tree_attention_wide_kernel(const AttentionArgs a) {
   constexpr int KK = D / 32, DV = D / 16, R = 16 * MT * WAVES, THREADS = WAVES * 64;
   constexpr int U = (4 * D + THREADS - 1) / THREADS;      // units of 16 bytes of K, and of V, to a thread
   __shared__ __align__(16) char lds_k[2][4 * D * 16], lds_v[2][4 * D * 16];
-  __shared__ __align__(16) int64_t places[8][2][kAttTile];      // [step % 8][keys, values][token]
-  __shared__ uint32_t lds_there[8], lds_odd;
+  __shared__ __align__(16) int64_t places[4][2][kAttTile];      // [step % 4][keys, values][token]
+  __shared__ uint32_t lds_there[4], lds_odd;
   const int lane = threadIdx.x & 63, wave = scalar(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   uint32_t id = blockIdx.x;
   const int h = id % a.kv_heads;
@@ -641,22 +627,20 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 && MT <= 2 ? 2 : 1) tree_
   const int b = share.b, old_steps = steps_of(share.len), first = share.first, last = share.last;
   if (share.part == 0 && h == 0 && row_tile == 0 && threadIdx.x == 0 && a.places != nullptr) a.places[b] = make_int2(slot, share.parts);
 
-  // The first wavefront looks places up, AHEAD + 1 steps before the products and a step after it has asked for the page ids.
+  // The first wavefront looks places up, two steps before the products and half a step after it has asked for the page ids.
   auto keep_places = [&](int step, const Lookup& l) {
     const Place mine = place_of(a, share, old_steps, step, l);
     if (lane < kAttTile) {
-      places[step & 7][0][lane] = mine.k;
-      places[step & 7][1][lane] = mine.v;
+      places[step & 3][0][lane] = mine.k;
+      places[step & 3][1][lane] = mine.v;
     }
     const uint32_t there = (uint32_t)__ballot(mine.there);
-    if (lane == 0) lds_there[step & 7] = there;
+    if (lane == 0) lds_there[step & 3] = there;
   };
   if (wave == 0) {
-    Lookup l[AHEAD + 1];
-#pragma unroll
-    for (int i = 0; i <= AHEAD; ++i) l[i] = ask(a, share, old_steps, first + i);
-#pragma unroll
-    for (int i = 0; i <= AHEAD; ++i) keep_places(first + i, l[i]);
+    const Lookup l = ask(a, share, old_steps, first), m = ask(a, share, old_steps, first + 1);
+    keep_places(first, l);
+    keep_places(first + 1, m);
   }
   if (threadIdx.x == 0) lds_odd = 0;
   u32x4 q[MT][KK];
@@ -676,17 +660,17 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 && MT <= 2 ? 2 : 1) tree_
   };
   auto load = [&](int step, Units& x) {
     const bool old = step < old_steps || step >= last;
-    const char *base_k = old ? cache_k : new_k, *base_v = old ? cache_v : new_v;
+    const char *base_k = either(old, cache_k, new_k), *base_v = either(old, cache_v, new_v);
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       const int u = min((int)threadIdx.x + i * THREADS, 4 * D - 1);
-      x.k[i] = *reinterpret_cast<const u32x4*>(base_k + places[step & 7][0][u / (D / 8)] + 16 * (u % (D / 8)));
+      x.k[i] = *reinterpret_cast<const u32x4*>(base_k + places[step & 3][0][u / (D / 8)] + 16 * (u % (D / 8)));
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        x.v[i][j] = *reinterpret_cast<const uint32_t*>(base_v + places[step & 7][1][4 * (u / (D / 2)) + j] + 4 * (u % (D / 2)));
+        x.v[i][j] = *reinterpret_cast<const uint32_t*>(base_v + places[step & 3][1][4 * (u / (D / 2)) + j] + 4 * (u % (D / 2)));
     }
   };
-  auto there_in = [&](int step) { return (uint32_t)scalar((int)lds_there[step & 7]); };
+  auto there_in = [&](int step) { return (uint32_t)scalar((int)lds_there[step & 3]); };
   auto keep = [&](int step, Units& x) {
     const uint32_t there = there_in(step);
     const bool old = step < old_steps;
@@ -713,13 +697,8 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 && MT <= 2 ? 2 : 1) tree_
     }
     if (odd) lds_odd = 1;
   };
-  u32x4 w[MT], values[DV];
-  auto read_values = [&](int step) {
-#pragma unroll
-    for (int j = 0; j < DV; ++j) values[j] = *reinterpret_cast<const u32x4*>(lds_v[step & 1] + (g * D + 16 * j + n) * 16);
-  };
-  auto weigh_step = [&](int step) {
-    u32x4 k[2][KK];
+  auto attend = [&](int step) {
+    u32x4 w[MT], values[DV], k[2][KK];
     Scores<MT> s;
 #pragma unroll
     for (int half = 0; half < 2; ++half)
@@ -727,8 +706,9 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 && MT <= 2 ? 2 : 1) tree_
       for (int kk = 0; kk < KK; ++kk)
         k[half][kk] = *reinterpret_cast<const u32x4*>(lds_k[step & 1] + ((4 * kk + g) * kAttTile + half * 16 + (n ^ ((4 * kk + g) & 15))) * 16);
     score<T, D, MT>(q, k, s);
-    // V is read before the weights are formed, so that it is there when they are
-    if constexpr (EARLY) read_values(step);
+    // V is read before the weights are formed, so that it is there when they are (192 -> 179 us)
+#pragma unroll
+    for (int j = 0; j < DV; ++j) values[j] = *reinterpret_cast<const u32x4*>(lds_v[step & 1] + (g * D + 16 * j + n) * 16);
     const uint32_t there = there_in(step);
     if (step >= old_steps || there != 0xffffffffu) {
       uint32_t seen[MT];
@@ -740,9 +720,6 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 && MT <= 2 ? 2 : 1) tree_
       mask<MT>(s, seen);
     }
     weigh<T, MT, DV>(rows, s, a.scale_log2, w);
-  };
-  auto add_step = [&](int step) {
-    if constexpr (!EARLY) read_values(step);
 #pragma unroll
     for (int j = 0; j < DV; ++j)
 #pragma unroll
@@ -750,28 +727,19 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 && MT <= 2 ? 2 : 1) tree_
   };
 
   __syncthreads();
-  Units x[AHEAD];      // step s in x[(s - first) % AHEAD], on its way
+  Units x;
   if (first < last) {
-#pragma unroll
-    for (int i = 0; i < AHEAD; ++i) load(first + i, x[i]);
-    keep(first, x[0]);
+    load(first, x);
+    keep(first, x);
   }
   __syncthreads();
-  for (int start = first; start < last; start += AHEAD) {
-#pragma unroll
-    for (int i = 0; i < AHEAD; ++i) {
-      const int step = start + i;
-      if (step >= last) break;
-      const Lookup after = ask(a, share, old_steps, step + AHEAD + 1);
-      load(step + AHEAD, x[i]);
-      if (works) {
-        weigh_step(step);
-        add_step(step);
-      }
-      if (step + 1 < last) keep(step + 1, x[(i + 1) % AHEAD]);
-      if (wave == 0) keep_places(step + AHEAD + 1, after);
-      __syncthreads();
-    }
+  for (int step = first; step < last; ++step) {
+    const Lookup after = ask(a, share, old_steps, step + 2);
+    load(step + 1, x);
+    if (works) attend(step);
+    keep(step + 1, x);
+    if (wave == 0) keep_places(step + 2, after);
+    __syncthreads();
   }
   if (!works) return;
   if (lds_odd) add_odd_values<T, D, MT, false>(a, rows, share, old_steps, new_v, node, 0, 1);

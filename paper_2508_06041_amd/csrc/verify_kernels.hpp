@@ -59,8 +59,40 @@ __device__ __forceinline__ double weight(float x, float top, double by) {
   return x == top ? 1.0 : exp_of(((double)x - (double)top) * by);
 }
 
+// The same for many logits of one row, without a branch: 2^(j / 32) from a table in LDS (32 doubles are all its banks: no two lanes that want
+// different ones meet) and the series of exp to the fifth power for what is left, below ln 2 / 64 (2e-15).  Weights below e^-700 count as 0.  A row
+// whose largest logit is no finite number goes the way above.
+struct Weigher {
+  const double* table;
+  double top, by;
+  float limit;      // the largest logit, as it is
+  bool finite;
+  __device__ __forceinline__ Weigher(const double* table, float top, double by)
+      : table(table), top((double)top), by(by), limit(top), finite(__builtin_isfinite(top)) {}
+  __device__ __forceinline__ double of(float x) const {
+    const double y = ((double)x - top) * by, magic = 6755399441055744.0;      // 1.5 2^52: the sum's low bits are the rounded value
+    const double t = __builtin_fma(y, 46.166241308446828384, magic), n = t - magic;      // 32 / ln 2
+    const double r = __builtin_fma(n, -0.021660849392498290193, y);
+    double s = __builtin_fma(r, 1.0 / 120.0, 1.0 / 24.0);
+    s = __builtin_fma(s, r, 1.0 / 6.0);
+    s = __builtin_fma(s, r, 0.5);
+    s = __builtin_fma(s, r, 1.0) * r;
+    const int i = (int)(uint32_t)__builtin_bit_cast(uint64_t, t);
+    const double f = table[i & 31], w = __builtin_fma(f, s, f);
+    const uint64_t bits = __builtin_bit_cast(uint64_t, w) + ((uint64_t)(uint32_t)(i >> 5) << 52);
+    return y > -700.0 ? __builtin_bit_cast(double, bits) : 0.0;
+  }
+};
+// Fills the table; a barrier has to follow.
+__device__ __forceinline__ void fill_table(double* table) {
+  if (threadIdx.x < 32) table[threadIdx.x] = exp_of(threadIdx.x * 0.021660849392498290193);
+}
+
 // The temperature of a sequence: 0 (or less, or NaN) takes the best token.
 __device__ __forceinline__ bool greedy(float temperature) { return !(temperature > 0.f); }
+
+// NaN counts as minus infinity.
+__device__ __forceinline__ float number(float x) { return x == x ? x : -INFINITY; }
 
 template <typename T>
 __device__ __forceinline__ float logit(const char* row, int i) { return (float)reinterpret_cast<const T*>(row)[i]; }
@@ -91,7 +123,7 @@ struct Chunk {
         for (int e = 0; e < E; ++e) x[p][e] = i + e >= 0 && i + e < n ? (float)base[i + e] : -INFINITY;
       }
 #pragma unroll
-      for (int e = 0; e < E; ++e) x[p][e] = x[p][e] == x[p][e] ? x[p][e] : -INFINITY;
+      for (int e = 0; e < E; ++e) x[p][e] = number(x[p][e]);
     }
   }
 };
@@ -107,13 +139,14 @@ __device__ __forceinline__ double wave_sum(double v) {
 }
 
 // The sum over a workgroup, in every thread; `space` has room for a value per wavefront and may be used again behind the next barrier.
+template <int THREADS = kVerThreads>
 __device__ __forceinline__ double group_sum(double v, double* space) {
   v = wave_sum(v);
   if ((threadIdx.x & 63) == 0) space[threadIdx.x >> 6] = v;
   __syncthreads();
   double s = 0.0;
 #pragma unroll
-  for (int w = 0; w < kVerThreads / 64; ++w) s += space[w];
+  for (int w = 0; w < THREADS / 64; ++w) s += space[w];
   return s;
 }
 
@@ -122,12 +155,13 @@ template <typename T>
 __global__ void __launch_bounds__(kVerThreads) verify_parts_kernel(const VerifyArgs a) {
   __shared__ float tops[kVerThreads / 64];
   __shared__ int places[kVerThreads / 64];
-  __shared__ double sums[kVerThreads / 64];
+  __shared__ double sums[kVerThreads / 64], table[32];
   const int row = a.by_chunks.of(blockIdx.x), chunk = blockIdx.x - row * a.chunks, b = row / a.nodes, node = row - b * a.nodes;
   const char* from = blockIdx.y == 0 ? a.logits + (b * a.logits_batch + node * a.logits_node) * (int64_t)sizeof(T)
                                      : a.draft + (b * a.draft_batch + node * a.draft_node) * (int64_t)sizeof(T);
   const float temperature = a.temperature[b];
   if (blockIdx.y == 1 && greedy(temperature)) return;
+  fill_table(table);
   Chunk<T> c;
   c.load(from, chunk, a.vocabulary);
   float top = -INFINITY;
@@ -155,11 +189,19 @@ __global__ void __launch_bounds__(kVerThreads) verify_parts_kernel(const VerifyA
     for (int w = 0; w < kVerThreads / 64; ++w) part.at = min(part.at, places[w]);
   } else {
     const double by = 1.0 / (double)temperature;
+    const Weigher w(table, top, by);
     double s = 0.0;
+    if (w.finite) {
 #pragma unroll
-    for (int p = 0; p < kVerPieces; ++p)
+      for (int p = 0; p < kVerPieces; ++p)
 #pragma unroll
-      for (int e = 0; e < Chunk<T>::E; ++e) s += weight(c.x[p][e], top, by);
+        for (int e = 0; e < Chunk<T>::E; ++e) s += w.of(c.x[p][e]);
+    } else {
+      for (int i = threadIdx.x; i < Chunk<T>::kElements; i += kVerThreads) {
+        const int at = chunk * Chunk<T>::kElements + i - Chunk<T>::lead(from);
+        if (at >= 0 && at < a.vocabulary) s += weight(number(logit<T>(from, at)), top, by);
+      }
+    }
     part.sum = group_sum(s, sums);
   }
   if (threadIdx.x == 0) a.parts[((int64_t)blockIdx.y * a.batch * a.nodes + row) * a.chunks + chunk] = part;
@@ -195,15 +237,21 @@ struct RowState {
   int refused;      // children refused so far
 };
 
-// The parent of a node; a chain where no parents are given.
-__device__ __forceinline__ int parent_of(const VerifyArgs& g, int b, int node) {
-  return g.parents == nullptr ? node - 1 : g.parents[(int64_t)b * g.nodes + node];
+// A sequence's tree, in LDS; a chain where no parents are given.  A barrier has to follow.
+struct Tree {
+  int parents[kVerMaxNodes], tokens[kVerMaxNodes];
+};
+__device__ __forceinline__ void load_tree(const VerifyArgs& g, int b, Tree& t) {
+  for (int i = threadIdx.x; i < g.nodes; i += blockDim.x) {
+    t.parents[i] = g.parents == nullptr ? i - 1 : g.parents[(int64_t)b * g.nodes + i];
+    t.tokens[i] = g.tokens[(int64_t)b * g.nodes + i];
+  }
 }
 
-// Tests the children of a node of a sequence with a temperature, by one wavefront.  `ready` sums of max(p - a q, 0) are there.  Several kernels come to
+// Tests the children of a node of a sequence with a temperature, by one wavefront; parents and tokens are the sequence's, in LDS.  `ready` sums of max(p - a q, 0) are there.  Several kernels come to
 // the same answers here, so nothing is left to how a compiler pairs products and sums.
 template <typename T>
-__device__ RowState test_children(const VerifyArgs& g, int b, int node, int ready, const RowTop& p, const RowTop& q) {
+__device__ RowState test_children(const VerifyArgs& g, const int* parents, const int* tokens, int b, int node, int ready, const RowTop& p, const RowTop& q) {
 #pragma clang fp contract(off)
   const int lane = threadIdx.x & 63, row = b * g.nodes + node;
   const char* from_p = g.logits + (b * g.logits_batch + node * g.logits_node) * (int64_t)sizeof(T);
@@ -213,19 +261,19 @@ __device__ RowState test_children(const VerifyArgs& g, int b, int node, int read
   double gone = 0.0;      // without draft rows: the probability of the refused
   for (int first = node + 1; first < g.nodes; first += 64) {
     const int mine = first + lane;
-    const bool child = mine < g.nodes && parent_of(g, b, mine) == node;
+    const bool child = mine < g.nodes && parents[mine] == node;
     // every lane forms the probabilities of its own node, then the children are gone through in order
     int word = -1;
     double u = 0.0, pw = 0.0, qw = 0.0;
     if (child) {
-      word = g.tokens[(int64_t)b * g.nodes + mine];
+      word = tokens[mine];
       u = (double)g.uniforms[(int64_t)b * g.nodes + mine];
       if ((uint32_t)word < (uint32_t)g.vocabulary) {
         const float x = logit<T>(from_p, word);
-        pw = p.sum > 0.0 ? weight(x == x ? x : -INFINITY, p.top, by) / p.sum : 0.0;
+        pw = p.sum > 0.0 ? weight(number(x), p.top, by) / p.sum : 0.0;
         if (from_q != nullptr) {
           const float y = logit<T>(from_q, word);
-          qw = q.sum > 0.0 ? weight(y == y ? y : -INFINITY, q.top, by) / q.sum : 0.0;
+          qw = q.sum > 0.0 ? weight(number(y), q.top, by) / q.sum : 0.0;
         }
       }
     }
@@ -237,7 +285,7 @@ __device__ RowState test_children(const VerifyArgs& g, int b, int node, int read
         const int w = __shfl(word, l);
         bool before = __any(child && lane < l && word == w);
         for (int i = node + 1; !before && i < first; i += 64)
-          before = __any(i + lane < first && parent_of(g, b, i + lane) == node && g.tokens[(int64_t)b * g.nodes + i + lane] == w);
+          before = __any(i + lane < first && parents[i + lane] == node && tokens[i + lane] == w);
         const double have = before ? 0.0 : cp;
         if (cu * (1.0 - gone) < have) {
           s.taken = first + l;
@@ -273,178 +321,190 @@ __device__ RowState test_children(const VerifyArgs& g, int b, int node, int read
   return s;
 }
 
-// One chunk of a row whose children were refused up to round `round`: the sum of max(p - a q, 0) with the next a.  Grid: chunks x rows in one.
+// Some chunks of a row whose children were refused up to round `round`: the sums of max(p - a q, 0) with the next a.  Grid: `groups` workgroups to a row.
 template <typename T>
-__global__ void __launch_bounds__(kVerThreads) verify_rest_kernel(const VerifyArgs a, int round) {
-  __shared__ double sums[kVerThreads / 64];
-  __shared__ double shared_a[5];
+__global__ void __launch_bounds__(kVerThreads) verify_rest_kernel(const VerifyArgs a, int round, int groups) {
+  __shared__ double sums[kVerThreads / 64], table[32];
+  __shared__ Tree tree;
+  __shared__ RowTop tops[2];
+  __shared__ double next_a;
   __shared__ int open;
-  const int row = a.by_chunks.of(blockIdx.x), chunk = blockIdx.x - row * a.chunks, b = row / a.nodes, node = row - b * a.nodes;
+  const int row = blockIdx.x / groups, b = row / a.nodes, node = row - b * a.nodes;
   const float temperature = a.temperature[b];
   if (greedy(temperature)) return;
   const double by = 1.0 / (double)temperature;
+  load_tree(a, b, tree);
+  fill_table(table);
+  if (threadIdx.x < 128) {      // the first two wavefronts: the target's row and the draft's
+    const int which = threadIdx.x >> 6;
+    const RowTop r = row_top(a.parts + ((int64_t)which * a.batch * a.nodes + row) * a.chunks, a.chunks, by);
+    if ((threadIdx.x & 63) == 0) tops[which] = r;
+  }
+  __syncthreads();
+  const RowTop p = tops[0], q = tops[1];
   if (threadIdx.x < 64) {
-    const RowTop p = row_top(a.parts + (int64_t)row * a.chunks, a.chunks, by);
-    const RowTop q = row_top(a.parts + ((int64_t)a.batch * a.nodes + row) * a.chunks, a.chunks, by);
-    const RowState s = test_children<T>(a, b, node, round, p, q);
+    const RowState s = test_children<T>(a, tree.parents, tree.tokens, b, node, round, p, q);
     if (threadIdx.x == 0) {
       open = s.open;
-      shared_a[0] = s.a + s.sum;
-      shared_a[1] = p.sum;
-      shared_a[2] = q.sum;
-      shared_a[3] = p.top;
-      shared_a[4] = q.top;
+      next_a = s.a + s.sum;
     }
   }
   __syncthreads();
   if (!open) return;
-  const double next = shared_a[0], sum_p = shared_a[1], sum_q = shared_a[2];
-  const float top_p = (float)shared_a[3], top_q = (float)shared_a[4];
   const char* from_p = a.logits + (b * a.logits_batch + node * a.logits_node) * (int64_t)sizeof(T);
   const char* from_q = a.draft + (b * a.draft_batch + node * a.draft_node) * (int64_t)sizeof(T);
-  double s = 0.0;
-  if (sum_p > 0.0) {
-    const double scale_p = 1.0 / sum_p, scale_q = sum_q > 0.0 ? next / sum_q : 0.0;
-    Chunk<T> c;
+  const double scale_p = p.sum > 0.0 ? 1.0 / p.sum : 0.0, scale_q = q.sum > 0.0 ? next_a / q.sum : 0.0;
+  const Weigher wp(table, p.top, by), wq(table, q.top, by);
+  const bool plain = wp.finite && wq.finite, alike = Chunk<T>::lead(from_p) == Chunk<T>::lead(from_q);
+  for (int chunk = blockIdx.x - row * groups; chunk < a.chunks; chunk += groups) {
+    Chunk<T> c, d;
     c.load(from_p, chunk, a.vocabulary);
+    if (alike) {
+      d.load(from_q, chunk, a.vocabulary);
+    } else {
 #pragma unroll
-    for (int p = 0; p < kVerPieces; ++p)
+      for (int i = 0; i < kVerPieces; ++i)
 #pragma unroll
-      for (int e = 0; e < Chunk<T>::E; ++e) {
-        const int i = Chunk<T>::index(from_p, chunk, p, e);
-        if (c.x[p][e] == -INFINITY) continue;
-        const float y = logit<T>(from_q, i);
-        s += __builtin_fmax(weight(c.x[p][e], top_p, by) * scale_p - weight(y == y ? y : -INFINITY, top_q, by) * scale_q, 0.0);
-      }
+        for (int e = 0; e < Chunk<T>::E; ++e) {
+          const int at = Chunk<T>::index(from_p, chunk, i, e);
+          d.x[i][e] = at >= 0 && at < a.vocabulary ? number(logit<T>(from_q, at)) : -INFINITY;
+        }
+    }
+    double s = 0.0;
+    if (plain) {
+#pragma unroll
+      for (int i = 0; i < kVerPieces; ++i)
+#pragma unroll
+        for (int e = 0; e < Chunk<T>::E; ++e) s += __builtin_fmax(wp.of(c.x[i][e]) * scale_p - wq.of(d.x[i][e]) * scale_q, 0.0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kVerPieces; ++i)
+#pragma unroll 1
+        for (int e = 0; e < Chunk<T>::E; ++e) {
+          float x = c.x[i][0], y = d.x[i][0];
+#pragma unroll
+          for (int j = 1; j < Chunk<T>::E; ++j) {
+            x = e == j ? c.x[i][j] : x;
+            y = e == j ? d.x[i][j] : y;
+          }
+          s += __builtin_fmax(weight(x, p.top, by) * scale_p - weight(y, q.top, by) * scale_q, 0.0);
+        }
+    }
+    __syncthreads();
+    s = group_sum(s, sums);
+    if (threadIdx.x == 0) a.rest[((int64_t)round * a.batch * a.nodes + row) * a.chunks + chunk] = s;
   }
-  s = group_sum(s, sums);
-  if (threadIdx.x == 0) a.rest[((int64_t)round * a.batch * a.nodes + row) * a.chunks + chunk] = s;
 }
 
+constexpr int kVerChooseThreads = kVerThreads * kVerPieces;      // one piece of a chunk to a thread
+
 // One sequence: which child of every node stands, the path from the root along them, and the token behind it: the first word whose running sum of what is
-// left of the last node's distribution exceeds uniforms[0] times the whole.
+// left of the last node's distribution exceeds uniforms[0] times the whole.  The nodes are tested side by side, one to a wavefront, and what is found out about them
+// is kept for the one that turns out to be the last.
 template <typename T>
-__global__ void __launch_bounds__(kVerThreads) verify_choose_kernel(const VerifyArgs a) {
-  __shared__ int taken[kVerMaxNodes];
-  __shared__ RowState last_state;
-  __shared__ RowTop last_p, last_q;
-  __shared__ double sums[kVerThreads / 64], before_chunk;
-  __shared__ int end, the_chunk, found[kVerThreads / 64];
+__global__ void __launch_bounds__(kVerChooseThreads) verify_choose_kernel(const VerifyArgs a) {
+  constexpr int WAVES = kVerChooseThreads / 64, E = Chunk<T>::E;
+  __shared__ Tree tree;
+  __shared__ RowState states[kVerMaxNodes];
+  __shared__ RowTop tops[kVerMaxNodes], draft_tops[kVerMaxNodes];
+  __shared__ double sums[WAVES], before_chunk;
+  __shared__ int end, length, the_chunk, gone_count, found[WAVES], lasts[WAVES], gone[kVerMaxNodes];
   const int b = blockIdx.x, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const float temperature = a.temperature[b];
-  const bool best = greedy(temperature);
+  const bool best = greedy(temperature), named = a.draft == nullptr;
   const double by = best ? 0.0 : 1.0 / (double)temperature;
   const int64_t rows = (int64_t)a.batch * a.nodes;
-  auto top_of = [&](int node, int which) { return row_top(a.parts + (which * rows + b * a.nodes + node) * a.chunks, a.chunks, by); };
-  for (int node = wave; node < a.nodes; node += kVerThreads / 64) {
-    const RowTop p = top_of(node, 0);
-    int t = -1;
+  load_tree(a, b, tree);
+  __syncthreads();
+  for (int node = wave; node < a.nodes; node += WAVES) {
+    const VerifyPart* parts = a.parts + (b * a.nodes + node) * (int64_t)a.chunks;
+    const RowTop p = row_top(parts, a.chunks, by);
+    RowTop q{};
+    RowState s{-1, -1, 0.0, 1.0, false, 0};
     if (best) {
-      for (int first = node + 1; first < a.nodes && t < 0; first += 64) {
+      for (int first = node + 1; first < a.nodes && s.taken < 0; first += 64) {
         const int mine = first + lane;
-        const uint64_t same = __ballot(mine < a.nodes && p.at != 0x7fffffff && parent_of(a, b, mine) == node && a.tokens[(int64_t)b * a.nodes + mine] == p.at);
-        if (same != 0) t = first + __ffsll((unsigned long long)same) - 1;
+        const uint64_t same = __ballot(mine < a.nodes && p.at != 0x7fffffff && tree.parents[mine] == node && tree.tokens[mine] == p.at);
+        if (same != 0) s.taken = first + __ffsll((unsigned long long)same) - 1;
       }
     } else {
-      RowTop q{};
-      if (a.draft != nullptr) q = top_of(node, 1);
-      t = test_children<T>(a, b, node, a.siblings, p, q).taken;
+      if (!named) q = row_top(parts + rows * a.chunks, a.chunks, by);
+      s = test_children<T>(a, tree.parents, tree.tokens, b, node, a.siblings, p, q);
     }
-    if (lane == 0) taken[node] = t;
+    if (lane == 0) {
+      tops[node] = p;
+      draft_tops[node] = q;
+      states[node] = s;
+    }
   }
   __syncthreads();
   if (threadIdx.x == 0) {
     int node = 0, n = 0;
-    while (true) {      // children have higher numbers than their parents, so this ends
+    while (states[node].taken >= 0) {      // children have higher numbers than their parents, so this ends
       a.path[(int64_t)b * a.nodes + n] = node;
-      if (taken[node] < 0) break;
-      node = taken[node];
-      a.words[(int64_t)b * a.nodes + n] = a.tokens[(int64_t)b * a.nodes + node];
+      node = states[node].taken;
+      a.words[(int64_t)b * a.nodes + n] = tree.tokens[node];
       ++n;
     }
+    a.path[(int64_t)b * a.nodes + n] = node;
     end = node;
+    length = n;
     a.count[b] = n + 1;
-    for (int i = n + 1; i < a.nodes; ++i) {
-      a.path[(int64_t)b * a.nodes + i] = -1;
-      a.words[(int64_t)b * a.nodes + i] = -1;
-    }
-    the_chunk = n;
   }
   __syncthreads();
   const int node = end;
-  int32_t* out = a.words + (int64_t)b * a.nodes + the_chunk;
-  __syncthreads();
-  if (wave == 0) {
-    const RowTop p = top_of(node, 0);
-    RowTop q{};
-    RowState s{-1, -1, 0.0, 1.0, false, 0};
-    if (!best) {
-      if (a.draft != nullptr) q = top_of(node, 1);
-      s = test_children<T>(a, b, node, a.siblings, p, q);
-    }
-    if (lane == 0) {
-      last_p = p;
-      last_q = q;
-      last_state = s;
-    }
+  for (int i = length + 1 + threadIdx.x; i < a.nodes; i += kVerChooseThreads) {
+    a.path[(int64_t)b * a.nodes + i] = -1;
+    a.words[(int64_t)b * a.nodes + i] = -1;
   }
-  __syncthreads();
-  const RowTop p = last_p, q = last_q;
-  const RowState s = last_state;
+  int32_t* out = a.words + (int64_t)b * a.nodes + length;
+  const RowTop p = tops[node], q = draft_tops[node];
+  const RowState s = states[node];
   if (best || !(p.sum > 0.0)) {
     if (threadIdx.x == 0) *out = best && p.at != 0x7fffffff ? p.at : -1;
     return;
   }
-  // without draft rows: the words that were refused and are gone.  A child's number is kept; the words are few.
-  const bool named = a.draft == nullptr;
   const char* from_p = a.logits + (b * a.logits_batch + node * a.logits_node) * (int64_t)sizeof(T);
   const char* from_q = named ? nullptr : a.draft + (b * a.draft_batch + node * a.draft_node) * (int64_t)sizeof(T);
-  int* gone = taken;      // the children of the last node, in order
-  __shared__ int gone_count;
-  if (threadIdx.x == 0) {
-    int n = 0;
-    if (named) {
-      double left = 1.0;
-      for (int i = node + 1; i < a.nodes; ++i) {
-        if (parent_of(a, b, i) != node) continue;
-        const int w = a.tokens[(int64_t)b * a.nodes + i];
-        bool is_new = (uint32_t)w < (uint32_t)a.vocabulary;
-        for (int j = 0; j < n; ++j) is_new = is_new && gone[j] != w;
-        if (!is_new) continue;
-        const float x = logit<T>(from_p, w);
-        const double pw = weight(x == x ? x : -INFINITY, p.top, by) / p.sum;
-        if (left - pw > 0.0) {
-          left -= pw;
-          gone[n++] = w;
-        }
-      }
-    }
-    gone_count = n;
-  }
-  __syncthreads();
-  const int goners = gone_count;
   const int64_t row = (int64_t)b * a.nodes + node;
   const int lead = Chunk<T>::lead(from_p);
-  // the weight of a chunk in what is left
-  auto chunk_weight = [&](int i) {
-    if (s.level >= 0) return a.rest[(s.level * rows + row) * a.chunks + i];
-    const VerifyPart part = a.parts[row * a.chunks + i];
-    double w = part.sum * weight(part.top, p.top, by) / p.sum;
-    for (int j = 0; j < goners; ++j)
-      if ((gone[j] + lead) / Chunk<T>::kElements == i) {
-        const float x = logit<T>(from_p, gone[j]);
-        w -= weight(x == x ? x : -INFINITY, p.top, by) / p.sum;
-      }
-    return __builtin_fmax(w, 0.0);
-  };
   if (wave == 0) {
+    // without draft rows: the words that were refused and are gone.  A word that is named twice goes once, and one that is all there is stays.
+    int n = 0;
+    double left = 1.0;
+    for (int first = node + 1; named && first < a.nodes; first += 64) {
+      const int mine = first + lane;
+      const bool child = mine < a.nodes && tree.parents[mine] == node && (uint32_t)tree.tokens[mine] < (uint32_t)a.vocabulary;
+      const int word = child ? tree.tokens[mine] : -1;
+      const double have = child ? weight(number(logit<T>(from_p, word)), p.top, by) / p.sum : 0.0;
+      for (uint64_t rest = __ballot(child); rest != 0; rest &= rest - 1) {
+        const int l = __ffsll((unsigned long long)rest) - 1, w = __shfl(word, l);
+        const double pw = __shfl(have, l);
+        bool before = false;
+        for (int i = lane; i < n; i += 64) before = before || gone[i] == w;
+        if (__any(before) || !(left - pw > 0.0)) continue;
+        left -= pw;
+        if (lane == 0) gone[n] = w;
+        ++n;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      }
+    }
+    // The weight of a chunk in what is left.  A sum less its refused parts is off by 1e-16 of the whole; a child is refused by a uniform of at most
+    // 1 - 2^-24, so at least that share of the whole is left, but for one chance in 10^14.
+    auto chunk_weight = [&](int i) {
+      if (s.level >= 0) return a.rest[(s.level * rows + row) * a.chunks + i];
+      const VerifyPart part = a.parts[row * a.chunks + i];
+      double w = part.sum * weight(part.top, p.top, by) / p.sum;
+      for (int j = 0; j < n; ++j)
+        if ((gone[j] + lead) / Chunk<T>::kElements == i) w -= weight(number(logit<T>(from_p, gone[j])), p.top, by) / p.sum;
+      return __builtin_fmax(w, 0.0);
+    };
     double whole = 0.0;
     for (int i = lane; i < a.chunks; i += 64) whole += chunk_weight(i);
     whole = wave_sum(whole);
     const double at = (double)a.uniforms[(int64_t)b * a.nodes] * whole;
-    double before = 0.0, chosen_before = 0.0;
+    double before = 0.0, chosen_before = 0.0, with_before = 0.0;
     int chosen = -1, with = -1;
-    double with_before = 0.0;
     for (int first = 0; first < a.chunks && chosen < 0; first += 64) {
       const double w = first + lane < a.chunks ? chunk_weight(first + lane) : 0.0;
       double run = w;
@@ -474,75 +534,61 @@ __global__ void __launch_bounds__(kVerThreads) verify_choose_kernel(const Verify
     if (lane == 0) {
       the_chunk = chosen;
       before_chunk = at - chosen_before;
+      gone_count = n;
     }
   }
   __syncthreads();
-  const int chunk = the_chunk;
+  const int chunk = the_chunk, goners = gone_count;
   if (chunk < 0) {
     if (threadIdx.x == 0) *out = -1;
     return;
   }
-  // inside the chunk: pieces in the order of the row are pieces in turn, then threads, then elements
-  Chunk<T> c;
-  c.load(from_p, chunk, a.vocabulary);
+  // inside the chunk: a piece to a thread, in the order of the row
   const double scale_p = 1.0 / p.sum, scale_q = !named && q.sum > 0.0 ? s.a / q.sum : 0.0, need = before_chunk;
-  double run = 0.0;
+  const int start = chunk * Chunk<T>::kElements + (int)threadIdx.x * E - lead;
+  double w[E], mine = 0.0;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int i = start + e;
+    const bool inside = i >= 0 && i < a.vocabulary;
+    w[e] = inside ? weight(number(logit<T>(from_p, i)), p.top, by) * scale_p : 0.0;
+    if (scale_q != 0.0 && inside) w[e] = __builtin_fmax(w[e] - weight(number(logit<T>(from_q, i)), q.top, by) * scale_q, 0.0);
+  }
+  for (int j = 0; j < goners; ++j)
+#pragma unroll
+    for (int e = 0; e < E; ++e) w[e] = gone[j] == start + e ? 0.0 : w[e];
+#pragma unroll
+  for (int e = 0; e < E; ++e) mine += w[e];
+  double upto = mine;
+#pragma unroll
+  for (int i = 1; i < 64; i *= 2) {
+    const double v = __shfl_up(upto, i);
+    if (lane >= i) upto += v;
+  }
+  if (lane == 63) sums[wave] = upto;
+  __syncthreads();
+  double at = upto - mine;
+  for (int i = 0; i < wave; ++i) at += sums[i];
   int answer = 0x7fffffff, last = -1;
 #pragma unroll
-  for (int piece = 0; piece < kVerPieces; ++piece) {
-    double w[Chunk<T>::E], mine = 0.0;
-#pragma unroll
-    for (int e = 0; e < Chunk<T>::E; ++e) {
-      const int i = Chunk<T>::index(from_p, chunk, piece, e);
-      w[e] = 0.0;
-      if (c.x[piece][e] == -INFINITY) continue;
-      w[e] = weight(c.x[piece][e], p.top, by) * scale_p;
-      if (scale_q != 0.0) {
-        const float y = logit<T>(from_q, i);
-        w[e] = __builtin_fmax(w[e] - weight(y == y ? y : -INFINITY, q.top, by) * scale_q, 0.0);
-      }
-      for (int j = 0; j < goners; ++j)
-        if (gone[j] == i) w[e] = 0.0;
+  for (int e = 0; e < E; ++e) {
+    at += w[e];
+    if (w[e] > 0.0) {
+      if (at > need) answer = min(answer, start + e);
+      last = start + e;
     }
-#pragma unroll
-    for (int e = 0; e < Chunk<T>::E; ++e) mine += w[e];
-    double upto = mine;
-#pragma unroll
-    for (int i = 1; i < 64; i *= 2) {
-      const double v = __shfl_up(upto, i);
-      if (lane >= i) upto += v;
-    }
-    __syncthreads();
-    if (lane == 63) sums[wave] = upto;
-    __syncthreads();
-    double all = 0.0, front = 0.0;
-#pragma unroll
-    for (int i = 0; i < kVerThreads / 64; ++i) {
-      if (i < wave) front += sums[i];
-      all += sums[i];
-    }
-    double at = run + front + upto - mine;
-#pragma unroll
-    for (int e = 0; e < Chunk<T>::E; ++e) {
-      at += w[e];
-      if (w[e] > 0.0) {
-        const int i = Chunk<T>::index(from_p, chunk, piece, e);
-        if (at > need) answer = min(answer, i);
-        last = max(last, i);
-      }
-    }
-    run += all;
   }
   answer = wave_all(answer, [](int x, int y) { return min(x, y); });
   last = wave_all(last, [](int x, int y) { return max(x, y); });
-  __syncthreads();
-  if (lane == 0) found[wave] = answer;
-  if (lane == 0) taken[wave] = last;
+  if (lane == 0) {
+    found[wave] = answer;
+    lasts[wave] = last;
+  }
   __syncthreads();
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kVerThreads / 64; ++i) {
+    for (int i = 0; i < WAVES; ++i) {
       answer = min(answer, found[i]);
-      last = max(last, taken[i]);
+      last = max(last, lasts[i]);
     }
     *out = answer != 0x7fffffff ? answer : last;
   }
