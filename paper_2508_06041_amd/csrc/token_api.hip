@@ -21,10 +21,10 @@ void launch_rope(const RopeArgs& a, bool half, int blocks, size_t lds, hipStream
     hipLaunchKernelGGL((rope_kernel<T, E, false>), dim3(blocks), dim3(kRopeThreads), lds, stream, a);
 }
 
-// The workspace of a verification: the parts of the rows, then the sums of what is left.
+// The workspace of a verification: the parts of the rows, the sums of what is left, what is known of the rows.
 struct VerifySpace {
   int chunks;
-  size_t parts, bytes;
+  size_t parts, rest, bytes;
 };
 
 VerifySpace verify_space(int batch, int nodes, int vocabulary, int dtype, bool draft, int siblings) {
@@ -33,7 +33,8 @@ VerifySpace verify_space(int batch, int nodes, int vocabulary, int dtype, bool d
   s.chunks = (int)(((int64_t)vocabulary + e - 1 + chunk - 1) / chunk);      // a row may start up to e - 1 elements behind a 16-byte boundary
   const size_t all = (size_t)batch * nodes * s.chunks;
   s.parts = all * sizeof(VerifyPart) * (draft ? 2 : 1);
-  s.bytes = s.parts + (draft ? all * siblings * sizeof(double) : 0);
+  s.rest = draft ? (all * siblings * sizeof(double) + 15) / 16 * 16 : 0;
+  s.bytes = s.parts + s.rest + (draft ? (size_t)batch * nodes * sizeof(RowInfo) : 0);
   return s;
 }
 
@@ -52,10 +53,12 @@ template <typename T>
 void launch_verify(const VerifyArgs& a, hipStream_t s) {
   const unsigned rows = (unsigned)a.batch * a.nodes;
   hipLaunchKernelGGL(verify_parts_kernel<T>, dim3(rows * a.chunks, a.draft ? 2 : 1), dim3(kVerThreads), 0, s, a);
-  // a workgroup finds out first whether its row needs a sum at all, so rows share few of them where there are many rows
-  const int groups = std::max(1, std::min(a.chunks, (int)(2048 / rows)));
-  for (int round = 0; a.draft && round < a.siblings; ++round)
+  // few rows want a sum, so those that do are split finely: as many workgroups as fill the chip if one row in four does
+  const int groups = std::max(1, std::min(a.chunks, (int)(4096 / rows)));
+  for (int round = 0; a.draft && round < a.siblings; ++round) {
+    hipLaunchKernelGGL(verify_rows_kernel<T>, dim3((rows + kVerThreads / 64 - 1) / (kVerThreads / 64)), dim3(kVerThreads), 0, s, a, round);
     hipLaunchKernelGGL(verify_rest_kernel<T>, dim3(rows * groups), dim3(kVerThreads), 0, s, a, round, groups);
+  }
   hipLaunchKernelGGL(verify_choose_kernel<T>, dim3(a.batch), dim3(kVerChooseThreads), 0, s, a);
 }
 
@@ -237,6 +240,7 @@ int dpllm_verify(int batch, int nodes, int vocabulary, int dtype, const void* lo
   a.words = words_dev;
   a.parts = (VerifyPart*)ws_dev;
   a.rest = (double*)((char*)ws_dev + space.parts);
+  a.infos = (RowInfo*)((char*)ws_dev + space.parts + space.rest);
   a.batch = batch;
   a.nodes = nodes;
   a.vocabulary = vocabulary;

@@ -21,6 +21,7 @@ struct VerifyPart {      // of a chunk of a row: its largest logit, where that i
   int at;
 };
 
+struct RowInfo;
 struct VerifyArgs {
   const char *logits, *draft;
   int64_t logits_batch, logits_node, draft_batch, draft_node;      // elements
@@ -29,6 +30,7 @@ struct VerifyArgs {
   int32_t *count, *path, *words;
   VerifyPart* parts;       // [2 with draft rows][batch * nodes][chunks]
   double* rest;            // [siblings][batch * nodes][chunks]: sums of max(p - a q, 0)
+  RowInfo* infos;   // [batch * nodes] with draft rows
   int batch, nodes, vocabulary, chunks, siblings;
   Divide by_chunks;
 };
@@ -59,33 +61,38 @@ __device__ __forceinline__ double weight(float x, float top, double by) {
   return x == top ? 1.0 : exp_of(((double)x - (double)top) * by);
 }
 
-// The same for many logits of one row, without a branch: 2^(j / 32) from a table in LDS (32 doubles are all its banks: no two lanes that want
-// different ones meet) and the series of exp to the fifth power for what is left, below ln 2 / 64 (2e-15).  Weights below e^-700 count as 0.  A row
-// whose largest logit is no finite number goes the way above.
+// The same for the sums over many logits of one row, without a branch: 2^(j / 128) from a table in LDS and the series of exp to the fourth power for what is
+// left, below ln 2 / 256 (2e-15).  Logits more than 690 temperatures below the largest, minus infinities and NaN among them, count as the one that is, whose weight of
+// 1e-300 is nothing to a sum.  A row whose largest logit is no finite number, or beside which 695 temperatures are
+// past the floats or lost in their rounding, goes the way above.
+constexpr int kVerTable = 128;
 struct Weigher {
   const double* table;
   double top, by;
-  float limit;      // the largest logit, as it is
-  bool finite;
+  float least;
+  bool plain;
   __device__ __forceinline__ Weigher(const double* table, float top, double by)
-      : table(table), top((double)top), by(by), limit(top), finite(__builtin_isfinite(top)) {}
+      : table(table), top((double)top), by(by), least((float)((double)top - 695.0 / by)) {
+    const double below = ((double)top - (double)least) * by;      // 695, but for the rounding of a float
+    plain = __builtin_isfinite(top) && below > 690.0 && below < 700.0;
+  }
   __device__ __forceinline__ double of(float x) const {
-    const double y = ((double)x - top) * by, magic = 6755399441055744.0;      // 1.5 2^52: the sum's low bits are the rounded value
-    const double t = __builtin_fma(y, 46.166241308446828384, magic), n = t - magic;      // 32 / ln 2
-    const double r = __builtin_fma(n, -0.021660849392498290193, y);
-    double s = __builtin_fma(r, 1.0 / 120.0, 1.0 / 24.0);
-    s = __builtin_fma(s, r, 1.0 / 6.0);
+    const double y = ((double)fmaxf(x, least) - top) * by, magic = 6755399441055744.0;      // 1.5 2^52: the sum's low bits are the rounded value
+    const double t = __builtin_fma(y, 184.66496523378731354, magic), n = t - magic;      // 128 / ln 2
+    const double r = __builtin_fma(n, -0.0054152123481245725483, y);
+    double s = __builtin_fma(r, 1.0 / 24.0, 1.0 / 6.0);
     s = __builtin_fma(s, r, 0.5);
     s = __builtin_fma(s, r, 1.0) * r;
-    const int i = (int)(uint32_t)__builtin_bit_cast(uint64_t, t);
-    const double f = table[i & 31], w = __builtin_fma(f, s, f);
-    const uint64_t bits = __builtin_bit_cast(uint64_t, w) + ((uint64_t)(uint32_t)(i >> 5) << 52);
-    return y > -700.0 ? __builtin_bit_cast(double, bits) : 0.0;
+    const uint32_t i = (uint32_t)__builtin_bit_cast(uint64_t, t);
+    const double f = *reinterpret_cast<const double*>(reinterpret_cast<const char*>(table) + ((i << 3) & (8 * kVerTable - 8)));
+    const uint64_t w = __builtin_bit_cast(uint64_t, __builtin_fma(f, s, f));
+    const uint32_t high = (uint32_t)(w >> 32) + ((i << 13) & 0xfff00000u);      // (i >> 7) << 20
+    return __builtin_bit_cast(double, (uint64_t)high << 32 | (uint32_t)w);
   }
 };
 // Fills the table; a barrier has to follow.
 __device__ __forceinline__ void fill_table(double* table) {
-  if (threadIdx.x < 32) table[threadIdx.x] = exp_of(threadIdx.x * 0.021660849392498290193);
+  if (threadIdx.x < kVerTable) table[threadIdx.x] = exp_of(threadIdx.x * 0.0054152123481245725483);
 }
 
 // The temperature of a sequence: 0 (or less, or NaN) takes the best token.
@@ -155,7 +162,7 @@ template <typename T>
 __global__ void __launch_bounds__(kVerThreads) verify_parts_kernel(const VerifyArgs a) {
   __shared__ float tops[kVerThreads / 64];
   __shared__ int places[kVerThreads / 64];
-  __shared__ double sums[kVerThreads / 64], table[32];
+  __shared__ double sums[kVerThreads / 64], table[kVerTable];
   const int row = a.by_chunks.of(blockIdx.x), chunk = blockIdx.x - row * a.chunks, b = row / a.nodes, node = row - b * a.nodes;
   const char* from = blockIdx.y == 0 ? a.logits + (b * a.logits_batch + node * a.logits_node) * (int64_t)sizeof(T)
                                      : a.draft + (b * a.draft_batch + node * a.draft_node) * (int64_t)sizeof(T);
@@ -191,7 +198,7 @@ __global__ void __launch_bounds__(kVerThreads) verify_parts_kernel(const VerifyA
     const double by = 1.0 / (double)temperature;
     const Weigher w(table, top, by);
     double s = 0.0;
-    if (w.finite) {
+    if (w.plain) {
 #pragma unroll
       for (int p = 0; p < kVerPieces; ++p)
 #pragma unroll
@@ -237,6 +244,11 @@ struct RowState {
   int refused;      // children refused so far
 };
 
+struct RowInfo {
+  RowTop p, q;
+  RowState s;
+};
+
 // A sequence's tree, in LDS; a chain where no parents are given.  A barrier has to follow.
 struct Tree {
   int parents[kVerMaxNodes], tokens[kVerMaxNodes];
@@ -248,20 +260,21 @@ __device__ __forceinline__ void load_tree(const VerifyArgs& g, int b, Tree& t) {
   }
 }
 
-// Tests the children of a node of a sequence with a temperature, by one wavefront; parents and tokens are the sequence's, in LDS.  `ready` sums of max(p - a q, 0) are there.  Several kernels come to
+// Tests the children of a node of a sequence with a temperature, by one wavefront; parents (nullptr: a chain) and tokens are the sequence's.  `ready` sums of max(p - a q, 0) are there.  Several kernels come to
 // the same answers here, so nothing is left to how a compiler pairs products and sums.
 template <typename T>
-__device__ RowState test_children(const VerifyArgs& g, const int* parents, const int* tokens, int b, int node, int ready, const RowTop& p, const RowTop& q) {
+__device__ RowState test_children(const VerifyArgs& g, const int32_t* parents, const int32_t* tokens, int b, int node, int ready, const RowTop& p, const RowTop& q) {
 #pragma clang fp contract(off)
   const int lane = threadIdx.x & 63, row = b * g.nodes + node;
   const char* from_p = g.logits + (b * g.logits_batch + node * g.logits_node) * (int64_t)sizeof(T);
   const char* from_q = g.draft == nullptr ? nullptr : g.draft + (b * g.draft_batch + node * g.draft_node) * (int64_t)sizeof(T);
   const double by = 1.0 / (double)g.temperature[b];
+  auto parent = [&](int i) { return parents == nullptr ? i - 1 : parents[i]; };
   RowState s{-1, -1, 0.0, 1.0, false, 0};
   double gone = 0.0;      // without draft rows: the probability of the refused
   for (int first = node + 1; first < g.nodes; first += 64) {
     const int mine = first + lane;
-    const bool child = mine < g.nodes && parents[mine] == node;
+    const bool child = mine < g.nodes && parent(mine) == node;
     // every lane forms the probabilities of its own node, then the children are gone through in order
     int word = -1;
     double u = 0.0, pw = 0.0, qw = 0.0;
@@ -285,7 +298,7 @@ __device__ RowState test_children(const VerifyArgs& g, const int* parents, const
         const int w = __shfl(word, l);
         bool before = __any(child && lane < l && word == w);
         for (int i = node + 1; !before && i < first; i += 64)
-          before = __any(i + lane < first && parents[i + lane] == node && tokens[i + lane] == w);
+          before = __any(i + lane < first && parent(i + lane) == node && tokens[i + lane] == w);
         const double have = before ? 0.0 : cp;
         if (cu * (1.0 - gone) < have) {
           s.taken = first + l;
@@ -321,41 +334,63 @@ __device__ RowState test_children(const VerifyArgs& g, const int* parents, const
   return s;
 }
 
-// Some chunks of a row whose children were refused up to round `round`: the sums of max(p - a q, 0) with the next a.  Grid: `groups` workgroups to a row.
+// What `round` sums tell about every row; one row to a wavefront.
 template <typename T>
-__global__ void __launch_bounds__(kVerThreads) verify_rest_kernel(const VerifyArgs a, int round, int groups) {
-  __shared__ double sums[kVerThreads / 64], table[32];
-  __shared__ Tree tree;
-  __shared__ RowTop tops[2];
-  __shared__ double next_a;
-  __shared__ int open;
-  const int row = blockIdx.x / groups, b = row / a.nodes, node = row - b * a.nodes;
+__global__ void __launch_bounds__(kVerThreads) verify_rows_kernel(const VerifyArgs a, int round) {
+  const int row = blockIdx.x * (kVerThreads / 64) + (threadIdx.x >> 6);
+  if (row >= a.batch * a.nodes) return;
+  const int b = row / a.nodes, node = row - b * a.nodes;
   const float temperature = a.temperature[b];
   if (greedy(temperature)) return;
   const double by = 1.0 / (double)temperature;
-  load_tree(a, b, tree);
+  RowInfo info;
+  if (round == 0) {
+    info.p = row_top(a.parts + (int64_t)row * a.chunks, a.chunks, by);
+    info.q = row_top(a.parts + ((int64_t)a.batch * a.nodes + row) * a.chunks, a.chunks, by);
+  } else {
+    info = a.infos[row];
+  }
+  info.s = test_children<T>(a, a.parents == nullptr ? nullptr : a.parents + (int64_t)b * a.nodes, a.tokens + (int64_t)b * a.nodes, b, node, round, info.p, info.q);
+  if ((threadIdx.x & 63) == 0) a.infos[row] = info;
+}
+
+// Some chunks of a row whose children were refused up to round `round`: the sums of max(p - a q, 0) with the next a.  Grid: `groups` workgroups to a row.
+// A row that the path does not come to is not worth the sum: some ancestor has taken another child, or none.
+template <typename T>
+__global__ void __launch_bounds__(kVerThreads) verify_rest_kernel(const VerifyArgs a, int round, int groups) {
+  __shared__ double sums[kVerThreads / 64], table[kVerTable];
+  __shared__ int parents[kVerMaxNodes], taken[kVerMaxNodes], wanted;      // taken: -2 where it is still open
+  const int row = blockIdx.x / groups, b = row / a.nodes, node = row - b * a.nodes;
+  const float temperature = a.temperature[b];
+  if (greedy(temperature)) return;
+  const RowInfo info = a.infos[row];
+  if (!info.s.open) return;
+  for (int i = threadIdx.x; i < a.nodes; i += kVerThreads) {
+    const RowState& s = a.infos[(int64_t)b * a.nodes + i].s;
+    parents[i] = a.parents == nullptr ? i - 1 : a.parents[(int64_t)b * a.nodes + i];
+    taken[i] = s.open ? -2 : s.taken;
+  }
   fill_table(table);
-  if (threadIdx.x < 128) {      // the first two wavefronts: the target's row and the draft's
-    const int which = threadIdx.x >> 6;
-    const RowTop r = row_top(a.parts + ((int64_t)which * a.batch * a.nodes + row) * a.chunks, a.chunks, by);
-    if ((threadIdx.x & 63) == 0) tops[which] = r;
-  }
   __syncthreads();
-  const RowTop p = tops[0], q = tops[1];
-  if (threadIdx.x < 64) {
-    const RowState s = test_children<T>(a, tree.parents, tree.tokens, b, node, round, p, q);
-    if (threadIdx.x == 0) {
-      open = s.open;
-      next_a = s.a + s.sum;
+  if (threadIdx.x == 0) {
+    int at = node;
+    bool comes = true;
+    while (comes && at > 0) {
+      const int up = parents[at];
+      comes = (uint32_t)up < (uint32_t)at && (taken[up] == at || taken[up] == -2);
+      at = up;
     }
+    wanted = comes;
   }
   __syncthreads();
-  if (!open) return;
+  if (!wanted) return;
+  const RowTop p = info.p, q = info.q;
+  const double by = 1.0 / (double)temperature, next_a = info.s.a + info.s.sum;
   const char* from_p = a.logits + (b * a.logits_batch + node * a.logits_node) * (int64_t)sizeof(T);
   const char* from_q = a.draft + (b * a.draft_batch + node * a.draft_node) * (int64_t)sizeof(T);
   const double scale_p = p.sum > 0.0 ? 1.0 / p.sum : 0.0, scale_q = q.sum > 0.0 ? next_a / q.sum : 0.0;
   const Weigher wp(table, p.top, by), wq(table, q.top, by);
-  const bool plain = wp.finite && wq.finite, alike = Chunk<T>::lead(from_p) == Chunk<T>::lead(from_q);
+  const bool plain = wp.plain && wq.plain, alike = Chunk<T>::lead(from_p) == Chunk<T>::lead(from_q);
   for (int chunk = blockIdx.x - row * groups; chunk < a.chunks; chunk += groups) {
     Chunk<T> c, d;
     c.load(from_p, chunk, a.vocabulary);
@@ -371,11 +406,11 @@ __global__ void __launch_bounds__(kVerThreads) verify_rest_kernel(const VerifyAr
         }
     }
     double s = 0.0;
-    if (plain) {
+    if (plain) {      // (1e-290 is above what a word without a probability has here and nothing beside one that has any)
 #pragma unroll
       for (int i = 0; i < kVerPieces; ++i)
 #pragma unroll
-        for (int e = 0; e < Chunk<T>::E; ++e) s += __builtin_fmax(wp.of(c.x[i][e]) * scale_p - wq.of(d.x[i][e]) * scale_q, 0.0);
+        for (int e = 0; e < Chunk<T>::E; ++e) s += __builtin_fmax(__builtin_fma(wp.of(c.x[i][e]), scale_p, -__builtin_fma(wq.of(d.x[i][e]), scale_q, 1e-290)), 0.0);
     } else {
 #pragma unroll
       for (int i = 0; i < kVerPieces; ++i)
@@ -417,9 +452,13 @@ __global__ void __launch_bounds__(kVerChooseThreads) verify_choose_kernel(const 
   load_tree(a, b, tree);
   __syncthreads();
   for (int node = wave; node < a.nodes; node += WAVES) {
-    const VerifyPart* parts = a.parts + (b * a.nodes + node) * (int64_t)a.chunks;
-    const RowTop p = row_top(parts, a.chunks, by);
-    RowTop q{};
+    RowTop p, q{};
+    if (best || named) {
+      p = row_top(a.parts + (b * a.nodes + node) * (int64_t)a.chunks, a.chunks, by);
+    } else {
+      p = a.infos[b * a.nodes + node].p;
+      q = a.infos[b * a.nodes + node].q;
+    }
     RowState s{-1, -1, 0.0, 1.0, false, 0};
     if (best) {
       for (int first = node + 1; first < a.nodes && s.taken < 0; first += 64) {
@@ -428,7 +467,6 @@ __global__ void __launch_bounds__(kVerChooseThreads) verify_choose_kernel(const 
         if (same != 0) s.taken = first + __ffsll((unsigned long long)same) - 1;
       }
     } else {
-      if (!named) q = row_top(parts + rows * a.chunks, a.chunks, by);
       s = test_children<T>(a, tree.parents, tree.tokens, b, node, a.siblings, p, q);
     }
     if (lane == 0) {
