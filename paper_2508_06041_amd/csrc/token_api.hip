@@ -54,7 +54,7 @@ void launch_verify(const VerifyArgs& a, hipStream_t s) {
   const unsigned rows = (unsigned)a.batch * a.nodes;
   hipLaunchKernelGGL(verify_parts_kernel<T>, dim3(rows * a.chunks, a.draft ? 2 : 1), dim3(kVerThreads), 0, s, a);
   // few rows want a sum, so those that do are split finely: as many workgroups as fill the chip if one row in four does
-  const int groups = std::max(1, std::min(a.chunks, (int)(4096 / rows)));
+  const int groups = std::max(1, std::min(a.chunks, (int)(16384 / rows)));
   for (int round = 0; a.draft && round < a.siblings; ++round) {
     hipLaunchKernelGGL(verify_rows_kernel<T>, dim3((rows + kVerThreads / 64 - 1) / (kVerThreads / 64)), dim3(kVerThreads), 0, s, a, round);
     hipLaunchKernelGGL(verify_rest_kernel<T>, dim3(rows * groups), dim3(kVerThreads), 0, s, a, round, groups);
