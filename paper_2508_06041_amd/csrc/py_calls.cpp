@@ -183,6 +183,15 @@ bool look(PyObject* o, Tensor* t) {
   return tensor(o, &t->data) && !PyErr_Occurred();
 }
 
+// A new tensor that torch has made like t.
+bool look_new(PyObject* o, const Tensor& like, Tensor* t) {
+  *t = like;
+  const Ref stride(PyObject_CallMethodNoArgs(o, s_stride));
+  if (stride.o == nullptr || !PyTuple_Check(stride.o) || PyTuple_GET_SIZE(stride.o) != t->dim) return false;
+  for (int i = 0; i < t->dim; ++i) t->stride[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(stride.o, i));
+  return tensor(o, &t->data) && !PyErr_Occurred();
+}
+
 // A dense tensor of this type and shape (the first dims of a, b, c).
 bool look_dense(PyObject* o, int dtype, int dims, int64_t a, int64_t b, int64_t c, void** p) {
   Tensor t;
@@ -268,7 +277,7 @@ PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (o == nullptr) return elsewhere();
     PyTuple_SET_ITEM(results.o, i, o);
     Tensor y;
-    if (!look(o, &y) || y.dtype != x[0].dtype || !heads_of(y, &out[i])) return elsewhere();
+    if (!(a[3] == Py_None ? look_new(o, x[i], &y) : look(o, &y)) || y.dtype != x[0].dtype || !heads_of(y, &out[i])) return elsewhere();
     for (int j = 0; j < 4; ++j)
       if (y.size[j] != x[i].size[j]) return elsewhere();
   }
@@ -327,7 +336,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (a[7] == Py_None ? (scale = (float)(1.0 / __builtin_sqrt((double)q.size[3])), false) : !as_float(a[7], &scale)) return elsewhere();
   if (to.attention_bytes((int)b, (int)t, (int)q.size[2], c->heads, (int)q.size[3], max_len, &bytes) != DPLLM_OK) return elsewhere();
   const Ref result(a[8] == Py_None ? PyObject_CallOneArg(empty_like, a[3]) : Py_NewRef(a[8]));
-  if (result.o == nullptr || !look(result.o, &y) || y.dtype != q.dtype || !heads_of(y, &ho)) return elsewhere();
+  if (result.o == nullptr || !(a[8] == Py_None ? look_new(result.o, q, &y) : look(result.o, &y)) || y.dtype != q.dtype || !heads_of(y, &ho)) return elsewhere();
   for (int j = 0; j < 4; ++j)
     if (y.size[j] != q.size[j]) return elsewhere();
   const Ref held(space(a[11], bytes, &ws, &bytes));

@@ -140,7 +140,8 @@ int dpllm_rope(const dpllm_heads* x, const dpllm_heads* out, const int* heads, i
   a.scale = scale;
   a.inverse = inverse;
   const int64_t row = (int64_t)a.heads * a.units;
-  a.at_a_time = 1;
+  // tokens enough for a workgroup's threads to have kRopeAtOnce units each on their way, but not so many that part of the chip has none
+  a.at_a_time = (int)std::max<int64_t>(1, std::min<int64_t>({kRopeThreads * kRopeAtOnce / row, a.all / 512, 16}));
   a.by_tokens = Divide::by(tokens);
   a.by_units = Divide::by(a.units);
   a.by_row = Divide::by((uint32_t)row);
