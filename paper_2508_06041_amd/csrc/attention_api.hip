@@ -15,6 +15,7 @@ namespace {
 struct Plan {
   int rows, mt, waves;   // rows of a kv head; tiles of 16 rows to a wavefront; waves > 0: the kernel for many rows with so many wavefronts
   int tile, row_tiles, slots;
+  bool lone;             // the kernel for few rows with twice the wavefronts, one workgroup to a sequence and kv head
   int64_t groups;        // workgroups
   size_t part, stats, bytes;
 };
@@ -26,9 +27,15 @@ Plan plan_of(int batch, int nodes, int heads, int kv_heads, int head_dim, int64_
   p.mt = head_dim == 256 || p.rows <= 16 || (p.rows > 32 && p.rows <= 64) ? 1 : 2;
   p.tile = 16 * p.mt * std::max(p.waves, 1);
   p.row_tiles = (p.rows + p.tile - 1) / p.tile;
+  // Workgroups: as many as run at once, two to a compute unit (one of eight wavefronts); more parts are more results to write and join (63 nodes over
+  // 130001 tokens 179 us with 256 workgroups, 213 with 512, 242 with 1024; four sequences of 8 nodes 43.6 with 512, 45.9 with 1024).  With many
+  // sequences three parts each, so that long ones do not hold up the rest.
   const int64_t steps = (max_len + kAttTile - 1) / kAttTile + (nodes + kAttTile - 1) / kAttTile, tiles = (int64_t)kv_heads * p.row_tiles;
   const int64_t most = batch * ((steps + kAttWaves - 1) / kAttWaves), fill = ((p.waves == 8 ? 256 : 512) + tiles - 1) / tiles;
-  p.slots = (int)std::max<int64_t>(batch, std::min(most, fill >= 2 * batch ? fill : 3 * (int64_t)batch));
+  // short contexts: eight wavefronts take them in two turns, which is faster than four and a second launch to join the parts (one token of 32 heads
+  // over 8, us in a graph, over 200 tokens 7.3 against 9.1, over 500 9.5 against 8.9)
+  p.lone = p.waves == 0 && p.mt == 1 && (head_dim == 64 || head_dim == 128) && steps <= 14;
+  p.slots = p.lone ? batch : (int)std::max<int64_t>(batch, std::min(most, fill >= 2 * batch ? fill : 3 * (int64_t)batch));
   p.groups = p.slots * tiles;
   const bool whole = p.slots == batch;
   p.part = whole ? 0 : (size_t)p.groups * p.tile * head_dim * sizeof(float);
@@ -40,10 +47,12 @@ Plan plan_of(int batch, int nodes, int heads, int kv_heads, int head_dim, int64_
 template <typename T, int D>
 void launch(const AttentionArgs& a, const Plan& p, hipStream_t s) {
   const dim3 groups((unsigned)p.groups);
-  if (p.waves == 0 && p.mt == 1) hipLaunchKernelGGL((tree_attention_kernel<T, D, 1>), groups, dim3(kAttWaves * 64), 0, s, a);
+  if constexpr (D == 64 || D == 128)
+    if (p.lone) hipLaunchKernelGGL((tree_attention_kernel<T, D, 1, 8>), groups, dim3(8 * 64), 0, s, a);
+  if (p.waves == 0 && p.mt == 1 && !p.lone) hipLaunchKernelGGL((tree_attention_kernel<T, D, 1, kAttWaves>), groups, dim3(kAttWaves * 64), 0, s, a);
   if (p.waves == 4 && p.mt == 1) hipLaunchKernelGGL((tree_attention_wide_kernel<T, D, 1, 4>), groups, dim3(4 * 64), 0, s, a);
   if constexpr (D < 256) {
-    if (p.waves == 0 && p.mt == 2) hipLaunchKernelGGL((tree_attention_kernel<T, D, 2>), groups, dim3(kAttWaves * 64), 0, s, a);
+    if (p.waves == 0 && p.mt == 2) hipLaunchKernelGGL((tree_attention_kernel<T, D, 2, kAttWaves>), groups, dim3(kAttWaves * 64), 0, s, a);
     if (p.waves == 4 && p.mt == 2) hipLaunchKernelGGL((tree_attention_wide_kernel<T, D, 2, 4>), groups, dim3(4 * 64), 0, s, a);
     if (p.waves == 8 && p.mt == 2) hipLaunchKernelGGL((tree_attention_wide_kernel<T, D, 2, 8>), groups, dim3(8 * 64), 0, s, a);
   }

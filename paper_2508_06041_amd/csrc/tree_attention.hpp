@@ -7,7 +7,7 @@
 
 namespace dpllm {
 
-constexpr int kAttWaves = 4;        // wavefronts of a workgroup of the kernel for few rows
+constexpr int kAttWaves = 4;        // wavefronts of a workgroup of the kernel for few rows, where the work is split
 constexpr int kAttTile = 32;        // tokens of a step
 
 struct AttentionArgs {
@@ -394,12 +394,13 @@ __device__ __forceinline__ void add_odd_values(const AttentionArgs& a, Rows<MT, 
 // V is loaded as it lies, D / 16 elements of 8 tokens to a lane, and turned inside the lane, 16 bits at a time.
 // The weights are rounded to the type of V for the value product (their sum is not): half a step of each, so the error is a mean of independent
 // roundings, below the one rounding of the result.
-template <typename T, int D, int MT>
-__global__ void __launch_bounds__(kAttWaves * 64, D <= 128 ? 2 : 1) tree_attention_kernel(const AttentionArgs a) {
+template <typename T, int D, int MT, int WAVES>
+__global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) tree_attention_kernel(const AttentionArgs a) {
   constexpr int KK = D / 32, DV = D / 16, N = DV / 2, R = 16 * MT;
-  __shared__ float sums[kAttWaves][4 * DV * MT][64];
-  __shared__ float2 tops[kAttWaves][MT][16];
-  __shared__ __align__(16) int64_t places[kAttWaves][2][2][kAttTile];      // [..][turn][keys, values][token]
+  constexpr int PER = 4 * DV / WAVES;      // of a lane's 4 DV results, which lie side by side, what a wavefront adds up in the end
+  __shared__ float sums[WAVES][4 * DV * MT][64];
+  __shared__ float2 tops[WAVES][MT][16];
+  __shared__ __align__(16) int64_t places[WAVES][2][2][kAttTile];      // [..][turn][keys, values][token]
   const int lane = threadIdx.x & 63, wave = scalar(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   uint32_t id = blockIdx.x;
   const int h = id % a.kv_heads;
@@ -448,7 +449,7 @@ __global__ void __launch_bounds__(kAttWaves * 64, D <= 128 ? 2 : 1) tree_attenti
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) x.v[i] = load_words<N>(base_v + table[1][8 * g + i]);
-    next = ask(a, share, old_steps, step + kAttWaves);
+    next = ask(a, share, old_steps, step + WAVES);
   };
   bool odd = false;      // among the values of nodes is something that is no finite number
   auto attend = [&](int step, Tokens& x) {
@@ -488,13 +489,13 @@ __global__ void __launch_bounds__(kAttWaves * 64, D <= 128 ? 2 : 1) tree_attenti
     }
   };
   Tokens x;
-  for (int turn = 0; step < last; step += kAttWaves, turn ^= 1) {
+  for (int turn = 0; step < last; step += WAVES, turn ^= 1) {
     load(step, turn, x);
     attend(step, x);
   }
 
-  if (__any(odd)) add_odd_values<T, D, MT, true>(a, rows, share, old_steps, new_v, node, wave, kAttWaves);
-  // the wavefronts' rows meet: each wavefront adds up the quarter 4 g + wave of the elements
+  if (__any(odd)) add_odd_values<T, D, MT, true>(a, rows, share, old_steps, new_v, node, wave, WAVES);
+  // the wavefronts' rows meet: each wavefront adds up its part of the elements
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     float s = rows.sum[mt];
@@ -510,36 +511,36 @@ __global__ void __launch_bounds__(kAttWaves * 64, D <= 128 ? 2 : 1) tree_attenti
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     const int r = row_tile * R + mt * 16 + n;
-    float m = -INFINITY, s = 0.f, f[kAttWaves];
+    float m = -INFINITY, s = 0.f, f[WAVES];
 #pragma unroll
-    for (int w = 0; w < kAttWaves; ++w) m = fmaxf(m, tops[w][mt][n].x);
+    for (int w = 0; w < WAVES; ++w) m = fmaxf(m, tops[w][mt][n].x);
 #pragma unroll
-    for (int w = 0; w < kAttWaves; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
       f[w] = tops[w][mt][n].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((tops[w][mt][n].x - m) * a.scale_log2);
       s += tops[w][mt][n].y * f[w];
     }
-    float e[DV];
+    float e[PER];
 #pragma unroll
-    for (int j = 0; j < DV; ++j) {
+    for (int j = 0; j < PER; ++j) {
       e[j] = 0.f;
 #pragma unroll
-      for (int w = 0; w < kAttWaves; ++w) e[j] += sums[w][(mt * 4 + wave) * DV + j][lane] * f[w];
+      for (int w = 0; w < WAVES; ++w) e[j] += sums[w][mt * 4 * DV + wave * PER + j][lane] * f[w];
     }
     if (r >= a.rows) continue;
-    const int d = DV * (4 * g + wave);
+    const int d = 4 * DV * g + wave * PER;
     if (share.parts == 1) {
       const float by = m == -INFINITY ? 0.f : 1.f / s;
-      uint32_t words[N];
+      uint32_t words[PER / 2];
 #pragma unroll
-      for (int j = 0; j < N; ++j) words[j] = pack2<T>(e[2 * j] * by, e[2 * j + 1] * by);
+      for (int j = 0; j < PER / 2; ++j) words[j] = pack2<T>(e[2 * j] * by, e[2 * j + 1] * by);
       const int head = h * a.group + r - node[mt] * a.group;
       store_words(a.out.data + 2 * (b * a.out.batch_stride + node[mt] * a.out.token_stride + head * a.out.head_stride + d), words);
       if (a.lse != nullptr && g == 0 && wave == 0) a.lse[((int64_t)b * a.nodes + node[mt]) * (a.kv_heads * a.group) + head] = log_sum<T>(m, s, a.scale);
     } else {
       const int64_t row = part_row(a, slot, h, row_tile, R) + mt * 16 + n;
-      uint32_t words[DV];
+      uint32_t words[PER];
 #pragma unroll
-      for (int j = 0; j < DV; ++j) words[j] = __builtin_bit_cast(uint32_t, e[j]);
+      for (int j = 0; j < PER; ++j) words[j] = __builtin_bit_cast(uint32_t, e[j]);
       if (m != -INFINITY) store_words(reinterpret_cast<char*>(a.part + row * D + d), words);
       if (g == 0 && wave == 0) a.stats[row] = make_float2(m, s);
     }
