@@ -86,7 +86,7 @@ struct Weigher {
     const uint32_t i = (uint32_t)__builtin_bit_cast(uint64_t, t);
     const double f = *reinterpret_cast<const double*>(reinterpret_cast<const char*>(table) + ((i << 3) & (8 * kVerTable - 8)));
     const uint64_t w = __builtin_bit_cast(uint64_t, __builtin_fma(f, s, f));
-    const uint32_t high = (uint32_t)(w >> 32) + ((i << 13) & 0xfff00000u);      // (i >> 7) << 20
+    const uint32_t high = ((i & ~127u) << 13) + (uint32_t)(w >> 32);      // (i >> 7) << 20
     return __builtin_bit_cast(double, (uint64_t)high << 32 | (uint32_t)w);
   }
 };
@@ -105,7 +105,7 @@ template <typename T>
 __device__ __forceinline__ float logit(const char* row, int i) { return (float)reinterpret_cast<const T*>(row)[i]; }
 
 // A chunk of a row in registers: piece p of a thread is the 16 bytes (p * threads + thread) of the chunk, counted from the last 16-byte boundary in front
-// of the row.  Pieces that the row covers in part are read element by element; what lies outside, and NaN, is -infinity.
+// of the row.  Pieces that the row covers in part are read element by element; what lies outside is -infinity.
 template <typename T>
 struct Chunk {
   static constexpr int E = Piece<T>::E;
@@ -129,8 +129,6 @@ struct Chunk {
 #pragma unroll
         for (int e = 0; e < E; ++e) x[p][e] = i + e >= 0 && i + e < n ? (float)base[i + e] : -INFINITY;
       }
-#pragma unroll
-      for (int e = 0; e < E; ++e) x[p][e] = number(x[p][e]);
     }
   }
 };
@@ -422,7 +420,7 @@ __global__ void __launch_bounds__(kVerThreads) verify_rest_kernel(const VerifyAr
             x = e == j ? c.x[i][j] : x;
             y = e == j ? d.x[i][j] : y;
           }
-          s += __builtin_fmax(weight(x, p.top, by) * scale_p - weight(y, q.top, by) * scale_q, 0.0);
+          s += __builtin_fmax(weight(number(x), p.top, by) * scale_p - weight(number(y), q.top, by) * scale_q, 0.0);
         }
     }
     __syncthreads();
