@@ -133,11 +133,39 @@ struct Chunk {
   }
 };
 
+// The value of another lane: STEP 0 and 1 exchange inside four lanes, 2 and 3 the fours of eight and the eights of sixteen, 4 and 5 sixteens and halves.  With all six
+// every lane has met every other, without LDS; two lanes that meet form the same sum, so all end with the same bits.
+template <int STEP>
+__device__ __forceinline__ uint32_t other(uint32_t v) {
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  if constexpr (STEP < 4) {
+    constexpr int control = STEP == 0 ? 0xb1 : STEP == 1 ? 0x4e : STEP == 2 ? 0x141 : 0x140;
+    return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, control, 0xf, 0xf, true);
+  } else {
+    const u32x2 p = STEP == 4 ? __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(v, v, false, false))
+                              : __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(v, v, false, false));
+    const uint32_t first = p[0], second = p[1];      // of a pair of rows (halves), in both
+    const bool upper = (threadIdx.x >> STEP) & 1;
+    return upper ? first : second;
+  }
+}
+template <int STEP>
+__device__ __forceinline__ float other(float v) { return __uint_as_float(other<STEP>(__float_as_uint(v))); }
+template <int STEP>
+__device__ __forceinline__ int other(int v) { return (int)other<STEP>((uint32_t)v); }
+template <int STEP>
+__device__ __forceinline__ double other(double v) {
+  const uint64_t w = __builtin_bit_cast(uint64_t, v);
+  return __builtin_bit_cast(double, (uint64_t)other<STEP>((uint32_t)(w >> 32)) << 32 | other<STEP>((uint32_t)w));
+}
 template <typename T, typename F>
 __device__ __forceinline__ T wave_all(T v, F f) {
-#pragma unroll
-  for (int i = 1; i < 64; i *= 2) v = f(v, __shfl_xor(v, i));
-  return v;
+  v = f(v, other<0>(v));
+  v = f(v, other<1>(v));
+  v = f(v, other<2>(v));
+  v = f(v, other<3>(v));
+  v = f(v, other<4>(v));
+  return f(v, other<5>(v));
 }
 __device__ __forceinline__ double wave_sum(double v) {
   return wave_all(v, [](double a, double b) { return a + b; });
@@ -212,24 +240,30 @@ __global__ void __launch_bounds__(kVerThreads) verify_parts_kernel(const VerifyA
   if (threadIdx.x == 0) a.parts[((int64_t)blockIdx.y * a.batch * a.nodes + row) * a.chunks + chunk] = part;
 }
 
-// The softmax of a whole row from its parts, by one wavefront; every lane has the answer.
+// The softmax of a whole row from its parts, by one wavefront; every lane has the answer.  by: 1 / temperature; best: the best token is
+// asked for, not the sum.
 struct RowTop {
   float top;
   int at;          // greedy: the first place of the largest; 0x7fffffff: the row has no number
   double sum;
 };
-__device__ __forceinline__ RowTop row_top(const VerifyPart* parts, int chunks, double by) {
+__device__ __forceinline__ RowTop row_top(const VerifyPart* parts, int chunks, double by, bool best) {
   RowTop r{-INFINITY, 0x7fffffff, 0.0};
   const int lane = threadIdx.x & 63;
-  float top = -INFINITY;
-  for (int i = lane; i < chunks; i += 64) top = fmaxf(top, parts[i].top);
+  const VerifyPart mine = lane < chunks ? parts[lane] : VerifyPart{0.0, -INFINITY, 0x7fffffff};
+  float top = mine.top;
+  for (int i = lane + 64; i < chunks; i += 64) top = fmaxf(top, parts[i].top);
   r.top = wave_all(top, [](float x, float y) { return fmaxf(x, y); });
-  for (int i = lane; i < chunks; i += 64) {
-    if (parts[i].top == r.top) r.at = min(r.at, parts[i].at);
-    r.sum += parts[i].sum * weight(parts[i].top, r.top, by);
+  if (best) {
+    r.at = mine.top == r.top ? mine.at : 0x7fffffff;
+    for (int i = lane + 64; i < chunks; i += 64)
+      if (parts[i].top == r.top) r.at = min(r.at, parts[i].at);
+    r.at = wave_all(r.at, [](int x, int y) { return min(x, y); });
+  } else {
+    r.sum = mine.sum * weight(mine.top, r.top, by);
+    for (int i = lane + 64; i < chunks; i += 64) r.sum += parts[i].sum * weight(parts[i].top, r.top, by);
+    r.sum = wave_sum(r.sum);
   }
-  r.at = wave_all(r.at, [](int x, int y) { return min(x, y); });
-  r.sum = wave_sum(r.sum);
   return r;
 }
 
@@ -258,40 +292,50 @@ __device__ __forceinline__ void load_tree(const VerifyArgs& g, int b, Tree& t) {
   }
 }
 
-// Tests the children of a node of a sequence with a temperature, by one wavefront; parents (nullptr: a chain) and tokens are the sequence's.  `ready` sums of max(p - a q, 0) are there.  Several kernels come to
+// The child that a lane looks at: node `first` + lane, if it is one of `node`'s.
+struct Child {
+  bool is;
+  int word;
+  float u, x, y;      // its uniform and its logits
+};
+template <typename T>
+__device__ __forceinline__ Child child_of(const VerifyArgs& g, const int32_t* parents, const int32_t* tokens, int b, int node, int first) {
+  const int mine = first + (threadIdx.x & 63);
+  Child c{mine < g.nodes && (parents == nullptr ? mine - 1 : parents[mine]) == node, -1, 0.f, -INFINITY, -INFINITY};
+  if (c.is) {
+    c.word = tokens[mine];
+    c.u = g.uniforms[(int64_t)b * g.nodes + mine];
+    if ((uint32_t)c.word < (uint32_t)g.vocabulary) {
+      c.x = number(logit<T>(g.logits + (b * g.logits_batch + node * g.logits_node) * (int64_t)sizeof(T), c.word));
+      if (g.draft != nullptr) c.y = number(logit<T>(g.draft + (b * g.draft_batch + node * g.draft_node) * (int64_t)sizeof(T), c.word));
+    }
+  }
+  return c;
+}
+
+// Tests the children of a node of a sequence with a temperature, by one wavefront; parents (nullptr: a chain) and tokens are the sequence's, c its
+// child_of() from the node behind it on, which is asked for before the sums are known.  `ready` sums of max(p - a q, 0) are there.  Several kernels come to
 // the same answers here, so nothing is left to how a compiler pairs products and sums.
 template <typename T>
-__device__ RowState test_children(const VerifyArgs& g, const int32_t* parents, const int32_t* tokens, int b, int node, int ready, const RowTop& p, const RowTop& q) {
+__device__ RowState test_children(const VerifyArgs& g, const int32_t* parents, const int32_t* tokens, int b, int node, int ready, const RowTop& p, const RowTop& q,
+                                  Child c) {
 #pragma clang fp contract(off)
   const int lane = threadIdx.x & 63, row = b * g.nodes + node;
-  const char* from_p = g.logits + (b * g.logits_batch + node * g.logits_node) * (int64_t)sizeof(T);
-  const char* from_q = g.draft == nullptr ? nullptr : g.draft + (b * g.draft_batch + node * g.draft_node) * (int64_t)sizeof(T);
   const double by = 1.0 / (double)g.temperature[b];
   auto parent = [&](int i) { return parents == nullptr ? i - 1 : parents[i]; };
   RowState s{-1, -1, 0.0, 1.0, false, 0};
   double gone = 0.0;      // without draft rows: the probability of the refused
   for (int first = node + 1; first < g.nodes; first += 64) {
-    const int mine = first + lane;
-    const bool child = mine < g.nodes && parent(mine) == node;
+    if (first > node + 1) c = child_of<T>(g, parents, tokens, b, node, first);
+    const bool child = c.is;
+    const int word = c.word;
+    const double u = (double)c.u;
     // every lane forms the probabilities of its own node, then the children are gone through in order
-    int word = -1;
-    double u = 0.0, pw = 0.0, qw = 0.0;
-    if (child) {
-      word = tokens[mine];
-      u = (double)g.uniforms[(int64_t)b * g.nodes + mine];
-      if ((uint32_t)word < (uint32_t)g.vocabulary) {
-        const float x = logit<T>(from_p, word);
-        pw = p.sum > 0.0 ? weight(number(x), p.top, by) / p.sum : 0.0;
-        if (from_q != nullptr) {
-          const float y = logit<T>(from_q, word);
-          qw = q.sum > 0.0 ? weight(number(y), q.top, by) / q.sum : 0.0;
-        }
-      }
-    }
+    const double pw = child && p.sum > 0.0 ? weight(c.x, p.top, by) / p.sum : 0.0, qw = child && q.sum > 0.0 ? weight(c.y, q.top, by) / q.sum : 0.0;
     for (uint64_t left = __ballot(child); left != 0; left &= left - 1) {
       const int l = __ffsll((unsigned long long)left) - 1;
       const double cu = __shfl(u, l), cp = __shfl(pw, l), cq = __shfl(qw, l);
-      if (from_q == nullptr) {
+      if (g.draft == nullptr) {
         // a word that was refused before has left already
         const int w = __shfl(word, l);
         bool before = __any(child && lane < l && word == w);
@@ -341,14 +385,16 @@ __global__ void __launch_bounds__(kVerThreads) verify_rows_kernel(const VerifyAr
   const float temperature = a.temperature[b];
   if (greedy(temperature)) return;
   const double by = 1.0 / (double)temperature;
+  const int32_t *parents = a.parents == nullptr ? nullptr : a.parents + (int64_t)b * a.nodes, *tokens = a.tokens + (int64_t)b * a.nodes;
+  const Child child = child_of<T>(a, parents, tokens, b, node, node + 1);
   RowInfo info;
   if (round == 0) {
-    info.p = row_top(a.parts + (int64_t)row * a.chunks, a.chunks, by);
-    info.q = row_top(a.parts + ((int64_t)a.batch * a.nodes + row) * a.chunks, a.chunks, by);
+    info.p = row_top(a.parts + (int64_t)row * a.chunks, a.chunks, by, false);
+    info.q = row_top(a.parts + ((int64_t)a.batch * a.nodes + row) * a.chunks, a.chunks, by, false);
   } else {
     info = a.infos[row];
   }
-  info.s = test_children<T>(a, a.parents == nullptr ? nullptr : a.parents + (int64_t)b * a.nodes, a.tokens + (int64_t)b * a.nodes, b, node, round, info.p, info.q);
+  info.s = test_children<T>(a, parents, tokens, b, node, round, info.p, info.q, child);
   if ((threadIdx.x & 63) == 0) a.infos[row] = info;
 }
 
@@ -451,8 +497,10 @@ __global__ void __launch_bounds__(kVerChooseThreads) verify_choose_kernel(const 
   __syncthreads();
   for (int node = wave; node < a.nodes; node += WAVES) {
     RowTop p, q{};
+    Child child{};
+    if (!best) child = child_of<T>(a, tree.parents, tree.tokens, b, node, node + 1);
     if (best || named) {
-      p = row_top(a.parts + (b * a.nodes + node) * (int64_t)a.chunks, a.chunks, by);
+      p = row_top(a.parts + (b * a.nodes + node) * (int64_t)a.chunks, a.chunks, by, best);
     } else {
       p = a.infos[b * a.nodes + node].p;
       q = a.infos[b * a.nodes + node].q;
@@ -465,7 +513,7 @@ __global__ void __launch_bounds__(kVerChooseThreads) verify_choose_kernel(const 
         if (same != 0) s.taken = first + __ffsll((unsigned long long)same) - 1;
       }
     } else {
-      s = test_children<T>(a, tree.parents, tree.tokens, b, node, a.siblings, p, q);
+      s = test_children<T>(a, tree.parents, tree.tokens, b, node, a.siblings, p, q, child);
     }
     if (lane == 0) {
       tops[node] = p;

@@ -18,7 +18,8 @@ def softmax(x, t):
     if x.max() == np.inf:
         w = (x == np.inf).astype(float)
     else:
-        w = np.exp((x - x.max()) / t)
+        w = np.zeros_like(x)
+        w[x > -np.inf] = np.exp((x[x > -np.inf] - x.max()) / t)
     return w / w.sum()
 
 
@@ -163,6 +164,15 @@ def test_masked_infinite_and_missing_logits(dtype, drafted):
     compare(**x)
     x["temperature"][:] = 1e-30
     x["temperature"][::2] = 1e30
+    compare(**x)
+
+
+@pytest.mark.parametrize("drafted", [False, True])
+def test_an_infinite_temperature(drafted):
+    """Every word that is not masked is as likely as any other."""
+    x = inputs("f32", 5, 6, 700, 2, drafted, seed=20)
+    x["logits"][:, :, 100:300] = -math.inf
+    x["temperature"][:] = math.inf
     compare(**x)
 
 
