@@ -616,8 +616,8 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 && MT <= 2 ? 2 : 1) tree_
   constexpr int KK = D / 32, DV = D / 16, R = 16 * MT * WAVES, THREADS = WAVES * 64;
   constexpr int U = (4 * D + THREADS - 1) / THREADS;      // units of 16 bytes of K, and of V, to a thread
   __shared__ __align__(16) char lds_k[2][4 * D * 16], lds_v[2][4 * D * 16];
-  __shared__ __align__(16) int64_t places[4][2][kAttTile];      // [step % 4][keys, values][token]
-  __shared__ uint32_t lds_there[4], lds_odd;
+  __shared__ __align__(16) int64_t places[2 * WAVES][2][kAttTile];      // [step][keys, values][token]
+  __shared__ uint32_t lds_there[2 * WAVES], lds_odd;
   const int lane = threadIdx.x & 63, wave = scalar(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   uint32_t id = blockIdx.x;
   const int h = id % a.kv_heads;
@@ -628,21 +628,18 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 && MT <= 2 ? 2 : 1) tree_
   const int b = share.b, old_steps = steps_of(share.len), first = share.first, last = share.last;
   if (share.part == 0 && h == 0 && row_tile == 0 && threadIdx.x == 0 && a.places != nullptr) a.places[b] = make_int2(slot, share.parts);
 
-  // The first wavefront looks places up, two steps before the products and half a step after it has asked for the page ids.
+  // Places are looked up for as many steps at a time as there are wavefronts, one by each, at least that many steps before they are needed: one wavefront that
+  // does it every step keeps the others waiting at the barrier.
   auto keep_places = [&](int step, const Lookup& l) {
     const Place mine = place_of(a, share, old_steps, step, l);
     if (lane < kAttTile) {
-      places[step & 3][0][lane] = mine.k;
-      places[step & 3][1][lane] = mine.v;
+      places[(step - first) & (2 * WAVES - 1)][0][lane] = mine.k;
+      places[(step - first) & (2 * WAVES - 1)][1][lane] = mine.v;
     }
     const uint32_t there = (uint32_t)__ballot(mine.there);
-    if (lane == 0) lds_there[step & 3] = there;
+    if (lane == 0) lds_there[(step - first) & (2 * WAVES - 1)] = there;
   };
-  if (wave == 0) {
-    const Lookup l = ask(a, share, old_steps, first), m = ask(a, share, old_steps, first + 1);
-    keep_places(first, l);
-    keep_places(first + 1, m);
-  }
+  keep_places(first + wave, ask(a, share, old_steps, first + wave));
   if (threadIdx.x == 0) lds_odd = 0;
   u32x4 q[MT][KK];
   int node[MT];
@@ -665,13 +662,13 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 && MT <= 2 ? 2 : 1) tree_
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       const int u = min((int)threadIdx.x + i * THREADS, 4 * D - 1);
-      x.k[i] = *reinterpret_cast<const u32x4*>(base_k + places[step & 3][0][u / (D / 8)] + 16 * (u % (D / 8)));
+      x.k[i] = *reinterpret_cast<const u32x4*>(base_k + places[(step - first) & (2 * WAVES - 1)][0][u / (D / 8)] + 16 * (u % (D / 8)));
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        x.v[i][j] = *reinterpret_cast<const uint32_t*>(base_v + places[step & 3][1][4 * (u / (D / 2)) + j] + 4 * (u % (D / 2)));
+        x.v[i][j] = *reinterpret_cast<const uint32_t*>(base_v + places[(step - first) & (2 * WAVES - 1)][1][4 * (u / (D / 2)) + j] + 4 * (u % (D / 2)));
     }
   };
-  auto there_in = [&](int step) { return (uint32_t)scalar((int)lds_there[step & 3]); };
+  auto there_in = [&](int step) { return (uint32_t)scalar((int)lds_there[(step - first) & (2 * WAVES - 1)]); };
   auto keep = [&](int step, Units& x) {
     const uint32_t there = there_in(step);
     const bool old = step < old_steps;
@@ -735,11 +732,13 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 && MT <= 2 ? 2 : 1) tree_
   }
   __syncthreads();
   for (int step = first; step < last; ++step) {
-    const Lookup after = ask(a, share, old_steps, step + 2);
+    const bool ahead = ((step - first) & (WAVES - 1)) == 0;
+    Lookup after{};
+    if (ahead) after = ask(a, share, old_steps, step + WAVES + wave);
     load(step + 1, x);
     if (works) attend(step);
     keep(step + 1, x);
-    if (wave == 0) keep_places(step + 2, after);
+    if (ahead) keep_places(step + WAVES + wave, after);
     __syncthreads();
   }
   if (!works) return;
