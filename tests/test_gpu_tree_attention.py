@@ -196,6 +196,30 @@ def test_what_is_not_seen_may_be_anything(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("nodes,length", [(6, 40), (6, 3000), (14, 40), (14, 3000), (70, 3000)])
+def test_odd_values_of_nodes_however_many_rows(dtype, dim, nodes, length):
+    """The same in every kernel, in one part and in several: an infinity and a NaN that some rows see, and what nobody does."""
+    c = Case(dtype, 2, nodes, 4, 2, dim, 16, [length, 5], mask="any", seed=nodes)
+    some, none = 2, nodes - 1
+    c.sees[:, :, some] = c.sees[:, :, none] = False
+    c.mask = words(c.sees)
+    c.k_new[:, none], c.v_new[:, none] = math.nan, -math.inf
+    c.check()
+    c.sees[:, 1::2, some] = True
+    c.mask = words(c.sees)
+    c.v_new[:, some, :, 7], c.v_new[:, some, :, dim - 1] = math.inf, math.nan
+    out = c.run()[0].cpu()
+    hit = c.sees[:, :, some]
+    assert (out[hit][..., 7] == math.inf).all() and out[hit][..., dim - 1].isnan().all()
+    assert out[~hit].isfinite().all()
+    c.v_new[:, some, :, 7] = c.v_new[:, some, :, dim - 1] = 0.0
+    want, _ = c.plain()
+    rest = [i for i in range(dim) if i not in (7, dim - 1)]
+    assert ((out.double() - want).abs()[..., rest] <= c.bound[..., rest]).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_scores_far_apart(dtype):
     """Scores of hundreds; a row whose every score is far below zero; one token that carries all and many that carry little each."""
     Case(dtype, 1, 4, 4, 2, 128, 16, [300], size=30.0).check()
