@@ -133,7 +133,8 @@ def test_attention_over_a_bad_cache(change, code, word):
     ({"cache": cache(page=1 << 30, pages_per_seq=8)}, -2, "tokens"), ({"ws": None}, -4, "workspace"), ({"ws_bytes": 100}, -4, "workspace"), ({"ws": SOME + 8}, -4, "workspace"),
 ])
 def test_attention(change, code, word):
-    refused(lib.dpllm_tree_attention(*dict(ATTEND, cache=change.get("cache", cache(page=64)), max_len=change.get("max_len", 10000),
+    # a cache that is long enough for the work to be split, so that a workspace is needed
+    refused(lib.dpllm_tree_attention(*dict(ATTEND, cache=change.get("cache", cache(page=1024)), max_len=change.get("max_len", 10000),
                                            **{k: v for k, v in change.items() if k not in ("cache", "max_len")}).values()), code, word)
 
 
