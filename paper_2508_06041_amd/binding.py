@@ -108,8 +108,7 @@ _calls.bind(C.cast(lib.dpllm_gemv, C.c_void_p).value, C.cast(lib.dpllm_estimate,
 
 _calls.bind_tokens(tuple(C.cast(f, C.c_void_p).value for f in (lib.dpllm_rope, lib.dpllm_tree_attention_workspace_bytes, lib.dpllm_tree_attention,
                                                                lib.dpllm_verify_workspace_bytes, lib.dpllm_verify, lib.dpllm_cache_append)),
-                   (torch.float16, torch.bfloat16, torch.float32, torch.int32, torch.int64, torch.float64), torch.empty_like,
-                   lambda n: torch.empty(n, dtype=torch.uint8, device="cuda"))
+                   (torch.float16, torch.bfloat16, torch.float32, torch.int32, torch.int64, torch.float64), torch.empty_like)
 
 
 def _stream():

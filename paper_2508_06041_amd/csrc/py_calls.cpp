@@ -126,8 +126,8 @@ struct TokenCalls {
   decltype(&dpllm_verify) verify;
   decltype(&dpllm_cache_append) append;
 } to{};
-// torch.float16, bfloat16, float32, int32, int64, float64, and torch.empty_like; a function of a number that gives so many bytes of device memory
-PyObject *dtypes[6] = {}, *empty_like = nullptr, *some_bytes = nullptr;
+// torch.float16, bfloat16, float32, int32, int64, float64, and torch.empty_like
+PyObject *dtypes[6] = {}, *empty_like = nullptr;
 enum { kInt32 = 3, kInt64 = 4, kFloat64 = 5 };
 PyObject *s_dtype = nullptr, *s_shape = nullptr, *s_stride = nullptr, *s_is_cuda = nullptr, *s_address = nullptr, *s_batch = nullptr, *s_new_empty = nullptr;
 
@@ -224,20 +224,19 @@ bool as_float(PyObject* o, float* f) {
   return !(d == -1.0 && PyErr_Occurred());
 }
 
-// bind_tokens(addresses of the functions of TokenCalls, dtypes, torch.empty_like, some_bytes)
+// bind_tokens(addresses of the functions of TokenCalls, dtypes, torch.empty_like)
 PyObject* bind_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
   void* f[6] = {};
-  bool ok = n == 4 && PyTuple_Check(a[0]) && PyTuple_GET_SIZE(a[0]) == 6 && PyTuple_Check(a[1]) && PyTuple_GET_SIZE(a[1]) == 6;
+  bool ok = n == 3 && PyTuple_Check(a[0]) && PyTuple_GET_SIZE(a[0]) == 6 && PyTuple_Check(a[1]) && PyTuple_GET_SIZE(a[1]) == 6;
   for (int i = 0; ok && i < 6; ++i) ok = address(PyTuple_GET_ITEM(a[0], i), &f[i]);
   if (!ok) {
-    PyErr_SetString(PyExc_TypeError, "bind_tokens(addresses, dtypes, empty_like, some_bytes)");
+    PyErr_SetString(PyExc_TypeError, "bind_tokens(addresses, dtypes, empty_like)");
     return nullptr;
   }
   to = {reinterpret_cast<decltype(to.rope)>(f[0]), reinterpret_cast<decltype(to.attention_bytes)>(f[1]), reinterpret_cast<decltype(to.attention)>(f[2]),
         reinterpret_cast<decltype(to.verify_bytes)>(f[3]), reinterpret_cast<decltype(to.verify)>(f[4]), reinterpret_cast<decltype(to.append)>(f[5])};
   for (int i = 0; i < 6; ++i) Py_XSETREF(dtypes[i], Py_NewRef(PyTuple_GET_ITEM(a[1], i)));
   Py_XSETREF(empty_like, Py_NewRef(a[2]));
-  Py_XSETREF(some_bytes, Py_NewRef(a[3]));
   Py_RETURN_NONE;
 }
 
@@ -296,14 +295,12 @@ bool cache_of(PyObject* o, const dpllm_cache** c, int* batch) {
   return true;
 }
 
-// A workspace of so many bytes (the caller's own is left to the long way); nullptr: something is out of the ordinary.
-PyObject* space(PyObject* given, size_t need, void** p, size_t* bytes) {
+// A workspace of so many bytes, made by a tensor of elements of `es` bytes (the caller's own is left to the long way); nullptr: something is out of the ordinary.
+PyObject* space(PyObject* maker, size_t es, size_t need, void** p) {
   *p = nullptr;
-  *bytes = need;
-  if (given == Py_None && need == 0) return Py_NewRef(Py_None);
-  if (given != Py_None) return nullptr;
-  const Ref n(PyLong_FromSize_t(need));
-  PyObject* o = n.o == nullptr ? nullptr : PyObject_CallOneArg(some_bytes, n.o);
+  if (need == 0) return Py_NewRef(Py_None);
+  const Ref n(PyLong_FromSize_t((need + es - 1) / es));
+  PyObject* o = n.o == nullptr ? nullptr : PyObject_CallMethodOneArg(maker, s_new_empty, n.o);
   if (o != nullptr && tensor(o, p)) return o;
   Py_XDECREF(o);
   return nullptr;
@@ -339,7 +336,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (result.o == nullptr || !(a[8] == Py_None ? look_new(result.o, q, &y) : look(result.o, &y)) || y.dtype != q.dtype || !heads_of(y, &ho)) return elsewhere();
   for (int j = 0; j < 4; ++j)
     if (y.size[j] != q.size[j]) return elsewhere();
-  const Ref held(space(a[11], bytes, &ws, &bytes));
+  const Ref held(a[11] == Py_None ? space(a[3], 2, bytes, &ws) : nullptr);
   if (held.o == nullptr) return elsewhere();
   const int rc = to.attention(c, layer, (int)b, (int)t, (int)q.size[2], static_cast<const int32_t*>(lens), max_len, &hq, a[4] == Py_None ? nullptr : &hk,
                               a[5] == Py_None ? nullptr : &hv, static_cast<const uint64_t*>(m.data), a[6] == Py_None || m.size[0] == 1 ? 0 : m.size[1] * m.size[2],
@@ -372,7 +369,7 @@ PyObject* verify(PyObject*, PyObject* const* a, Py_ssize_t n) {
     PyTuple_SET_ITEM(results.o, i, o);
     if (!tensor(o, &out[i])) return elsewhere();
   }
-  const Ref held(space(Py_None, bytes, &ws, &bytes));
+  const Ref held(space(a[1], 4, bytes, &ws));
   if (held.o == nullptr) return elsewhere();
   const int rc = to.verify((int)x.size[0], (int)x.size[1], (int)x.size[2], x.dtype, x.data, x.stride[0], x.stride[1], d.data, d.stride[0], d.stride[1],
                            static_cast<const int32_t*>(tokens), static_cast<const int32_t*>(parents), static_cast<const float*>(uniforms),
