@@ -52,7 +52,11 @@ int check_verify(const char* who, int batch, int nodes, int vocabulary, int dtyp
 template <typename T>
 void launch_verify(const VerifyArgs& a, hipStream_t s) {
   const unsigned rows = (unsigned)a.batch * a.nodes;
-  hipLaunchKernelGGL(verify_parts_kernel<T>, dim3(rows * a.chunks, a.draft ? 2 : 1), dim3(kVerThreads), 0, s, a);
+  // three rounds of workgroups, whose next chunks come while they work: 768 rows of 128256 words in bf16 take 64 us with one workgroup to a row, 61 with two,
+  // 54 with four, 56 with six, 61 with one to a chunk; few rows one to a chunk
+  const int64_t all = (int64_t)rows * (a.draft ? 2 : 1);
+  const int each = (int)std::min<int64_t>(a.chunks, (3000 + all - 1) / all);
+  hipLaunchKernelGGL(verify_parts_kernel<T>, dim3(rows * each, a.draft ? 2 : 1), dim3(kVerThreads), 0, s, a, each, Divide::by(each));
   // few rows want a sum, so those that do are split finely: as many workgroups as fill the chip if one row in four does
   const int groups = std::max(1, std::min(a.chunks, (int)(16384 / rows)));
   for (int round = 0; a.draft && round < a.siblings; ++round) {
@@ -248,7 +252,6 @@ int dpllm_verify(int batch, int nodes, int vocabulary, int dtype, const void* lo
   a.nodes = nodes;
   a.vocabulary = vocabulary;
   a.chunks = space.chunks;
-  a.by_chunks = Divide::by(space.chunks);
   a.siblings = siblings;
   if (dtype == DPLLM_F16)
     launch_verify<half_t>(a, (hipStream_t)stream);

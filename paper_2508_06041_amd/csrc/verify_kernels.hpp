@@ -32,7 +32,6 @@ struct VerifyArgs {
   double* rest;            // [siblings][batch * nodes][chunks]: sums of max(p - a q, 0)
   RowInfo* infos;   // [batch * nodes] with draft rows
   int batch, nodes, vocabulary, chunks, siblings;
-  Divide by_chunks;
 };
 
 // 2^(t - rint(t)) by the series of exp to its eleventh power (below 1e-14 for arguments up to ln 2 / 2), times 2^rint(t).  y = 0 gives exactly 1;
@@ -61,38 +60,58 @@ __device__ __forceinline__ double weight(float x, float top, double by) {
   return x == top ? 1.0 : exp_of(((double)x - (double)top) * by);
 }
 
-// The same for the sums over many logits of one row, without a branch: 2^(j / 128) from a table in LDS and the series of exp to the fourth power for what is
-// left, below ln 2 / 256 (2e-15).  Logits more than 690 temperatures below the largest, minus infinities and NaN among them, count as the one that is, whose weight of
+// The same for the sums over many logits of one row, without a branch, in few instructions, as these are what the sums are bound by.  (x - top) / temperature is
+// counted in 256ths of a power of two from 2^19 - 256, so that all that come up lie between 2^18 and 2^19: the last two bits of the upper word and the
+// lower word are the fraction r, the eight before them the place in a table of 2^(j / 256) in LDS, and those before the power of two.  1 + c1 r + c2 r^2 + c3 r^3 is
+// 2^(r / 256) to 2e-14, with the largest such error made least and none at 0, so that the largest logit counts exactly 1; the count is rounded to 2^-34, which is
+// 8e-14 of a weight at most.  With a count that is rounded to the nearest whole and the series to the fourth power (1e-15; three instructions in
+// twenty more) verify_parts took 69 us for 768 rows of 128256 words in bf16, with this 60, and 54 since a workgroup takes several chunks of a row.
+// Logits more than 690 temperatures below the largest, minus infinities and NaN among them, count as the one that is, whose weight of
 // 1e-300 is nothing to a sum.  A row whose largest logit is no finite number, or beside which 695 temperatures are
 // past the floats or lost in their rounding, goes the way above.
-constexpr int kVerTable = 128;
+constexpr int kVerTable = 256;      // entries: their lower words, then their upper ones, so that both are one read
 struct Weigher {
-  const double* table;
-  double top, by;
+  const uint32_t* table;
+  double top, steps;
   float least;
   bool plain;
-  __device__ __forceinline__ Weigher(const double* table, float top, double by)
-      : table(table), top((double)top), by(by), least((float)((double)top - 695.0 / by)) {
+  __device__ __forceinline__ Weigher(const uint32_t* table, float top, double by)
+      : table(table), top((double)top), steps(by * 369.32993046757462), least((float)((double)top - 695.0 / by)) {      // 256 / ln 2
     const double below = ((double)top - (double)least) * by;      // 695, but for the rounding of a float
     plain = __builtin_isfinite(top) && below > 690.0 && below < 700.0;
   }
+  // The weight is g * f.  The logit is no signaling NaN (a Chunk's never are), so that one instruction takes the larger.
+  __device__ __forceinline__ void parts(float x, double& g, double& f) const {
+    float z;
+    asm("v_max_f32 %0, %1, %2" : "=v"(z) : "v"(x), "v"(least));
+    const double y = __builtin_fma((double)z - top, steps, 524032.0), r = __builtin_amdgcn_fract(y);      // 2^19 - 256
+    const uint32_t i = (uint32_t)(__builtin_bit_cast(uint64_t, y) >> 32);
+    const uint32_t* at = reinterpret_cast<const uint32_t*>(reinterpret_cast<const char*>(table) + (i & (4 * kVerTable - 4)));
+    uint32_t high;
+    asm("v_lshl_add_u32 %0, %1, 10, %2" : "=v"(high) : "v"(i & ~(4 * kVerTable - 1u)), "v"(at[kVerTable]));
+    g = __builtin_bit_cast(double, (uint64_t)high << 32 | at[0]);
+    f = __builtin_fma(r, 3.312607527945956e-09, 3.6655631008313955e-06);
+    f = __builtin_fma(f, r, 0.0027076061744736664);
+    f = __builtin_fma(f, r, 1.0);
+  }
   __device__ __forceinline__ double of(float x) const {
-    const double y = ((double)fmaxf(x, least) - top) * by, magic = 6755399441055744.0;      // 1.5 2^52: the sum's low bits are the rounded value
-    const double t = __builtin_fma(y, 184.66496523378731354, magic), n = t - magic;      // 128 / ln 2
-    const double r = __builtin_fma(n, -0.0054152123481245725483, y);
-    double s = __builtin_fma(r, 1.0 / 24.0, 1.0 / 6.0);
-    s = __builtin_fma(s, r, 0.5);
-    s = __builtin_fma(s, r, 1.0) * r;
-    const uint32_t i = (uint32_t)__builtin_bit_cast(uint64_t, t);
-    const double f = *reinterpret_cast<const double*>(reinterpret_cast<const char*>(table) + ((i << 3) & (8 * kVerTable - 8)));
-    const uint64_t w = __builtin_bit_cast(uint64_t, __builtin_fma(f, s, f));
-    const uint32_t high = ((i & ~127u) << 13) + (uint32_t)(w >> 32);      // (i >> 7) << 20
-    return __builtin_bit_cast(double, (uint64_t)high << 32 | (uint32_t)w);
+    double g, f;
+    parts(x, g, f);
+    return g * f;
+  }
+  __device__ __forceinline__ double plus(float x, double sum) const {
+    double g, f;
+    parts(x, g, f);
+    return __builtin_fma(g, f, sum);
   }
 };
-// Fills the table; a barrier has to follow.
-__device__ __forceinline__ void fill_table(double* table) {
-  if (threadIdx.x < kVerTable) table[threadIdx.x] = exp_of(threadIdx.x * 0.0054152123481245725483);
+// Fills the table; a barrier has to follow.  The largest logit's count leaves 0x7ff00000 of the power of two's place, which is taken off here.
+__device__ __forceinline__ void fill_table(uint32_t* table) {
+  for (int i = threadIdx.x; i < kVerTable; i += blockDim.x) {
+    const uint64_t w = __builtin_bit_cast(uint64_t, exp_of(i * 0.0027076061740622863));      // ln 2 / 256
+    table[i] = (uint32_t)w;
+    table[kVerTable + i] = (uint32_t)(w >> 32) - 0x7ff00000u;
+  }
 }
 
 // The temperature of a sequence: 0 (or less, or NaN) takes the best token.
@@ -105,7 +124,7 @@ template <typename T>
 __device__ __forceinline__ float logit(const char* row, int i) { return (float)reinterpret_cast<const T*>(row)[i]; }
 
 // A chunk of a row in registers: piece p of a thread is the 16 bytes (p * threads + thread) of the chunk, counted from the last 16-byte boundary in front
-// of the row.  Pieces that the row covers in part are read element by element; what lies outside is -infinity.
+// of the row.  Pieces that the row covers in part are read element by element; what lies outside is -infinity.  NaN are quiet.
 template <typename T>
 struct Chunk {
   static constexpr int E = Piece<T>::E;
@@ -116,20 +135,33 @@ struct Chunk {
   __device__ __forceinline__ static int index(const char* row, int chunk, int p, int e) {
     return chunk * kElements + (p * kVerThreads + (int)threadIdx.x) * E + e - lead(row);
   }
-  __device__ __forceinline__ void load(const char* row, int chunk, int n) {
-    const T* base = reinterpret_cast<const T*>(row);
+  // on its way from memory
+  struct Raw {
+    typename Piece<T>::type v[kVerPieces];
+    __device__ __forceinline__ void load(const char* row, int chunk, int n) {
+      const T* base = reinterpret_cast<const T*>(row);
 #pragma unroll
-    for (int p = 0; p < kVerPieces; ++p) {
-      const int i = index(row, chunk, p, 0);
-      if (i >= 0 && i + E <= n) {
-        const typename Piece<T>::type v = *reinterpret_cast<const typename Piece<T>::type*>(base + i);
+      for (int p = 0; p < kVerPieces; ++p) {
+        const int i = index(row, chunk, p, 0);
+        if (i >= 0 && i + E <= n) {
+          v[p] = *reinterpret_cast<const typename Piece<T>::type*>(base + i);
+        } else {
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[p][e] = (float)v[e];
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) x[p][e] = i + e >= 0 && i + e < n ? (float)base[i + e] : -INFINITY;
+          for (int e = 0; e < E; ++e) v[p][e] = i + e >= 0 && i + e < n ? base[i + e] : (T)-INFINITY;
+        }
       }
     }
+  };
+  __device__ __forceinline__ void take(const Raw& raw) {
+#pragma unroll
+    for (int p = 0; p < kVerPieces; ++p)
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[p][e] = __builtin_canonicalizef((float)raw.v[p][e]);
+  }
+  __device__ __forceinline__ void load(const char* row, int chunk, int n) {
+    Raw raw;
+    raw.load(row, chunk, n);
+    take(raw);
   }
 };
 
@@ -183,61 +215,73 @@ __device__ __forceinline__ double group_sum(double v, double* space) {
   return s;
 }
 
-// One chunk of one row: the parts of its softmax.  Grid: (chunks x rows) x (1, or 2 with draft rows).
+// Some chunks of one row: the parts of its softmax.  Grid: (`groups` workgroups to a row) x (1, or 2 with draft rows).  The next chunk is on its way while
+// this one is summed.
 template <typename T>
-__global__ void __launch_bounds__(kVerThreads) verify_parts_kernel(const VerifyArgs a) {
+__global__ void __launch_bounds__(kVerThreads) verify_parts_kernel(const VerifyArgs a, int groups, const Divide by_groups) {
   __shared__ float tops[kVerThreads / 64];
   __shared__ int places[kVerThreads / 64];
-  __shared__ double sums[kVerThreads / 64], table[kVerTable];
-  const int row = a.by_chunks.of(blockIdx.x), chunk = blockIdx.x - row * a.chunks, b = row / a.nodes, node = row - b * a.nodes;
+  __shared__ double sums[kVerThreads / 64];
+  __shared__ uint32_t table[2 * kVerTable];
+  const int row = by_groups.of(blockIdx.x), b = row / a.nodes, node = row - b * a.nodes;
   const char* from = blockIdx.y == 0 ? a.logits + (b * a.logits_batch + node * a.logits_node) * (int64_t)sizeof(T)
                                      : a.draft + (b * a.draft_batch + node * a.draft_node) * (int64_t)sizeof(T);
   const float temperature = a.temperature[b];
   if (blockIdx.y == 1 && greedy(temperature)) return;
+  int chunk = blockIdx.x - row * groups;
+  typename Chunk<T>::Raw raw;
+  raw.load(from, chunk, a.vocabulary);
   fill_table(table);
-  Chunk<T> c;
-  c.load(from, chunk, a.vocabulary);
-  float top = -INFINITY;
-#pragma unroll
-  for (int p = 0; p < kVerPieces; ++p)
-#pragma unroll
-    for (int e = 0; e < Chunk<T>::E; ++e) top = fmaxf(top, c.x[p][e]);
-  top = wave_all(top, [](float x, float y) { return fmaxf(x, y); });
-  if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kVerThreads / 64; ++w) top = fmaxf(top, tops[w]);
-  VerifyPart part{0.0, top, 0x7fffffff};
-  if (greedy(temperature)) {
-    int at = 0x7fffffff;
+  const double by = 1.0 / (double)temperature;
+  while (true) {
+    Chunk<T> c;
+    c.take(raw);
+    const int next = chunk + groups;
+    if (next < a.chunks) raw.load(from, next, a.vocabulary);
+    float top = -INFINITY;
 #pragma unroll
     for (int p = 0; p < kVerPieces; ++p)
 #pragma unroll
-      for (int e = 0; e < Chunk<T>::E; ++e)
-        if (c.x[p][e] == top && top != -INFINITY) at = min(at, Chunk<T>::index(from, chunk, p, e));
-    at = wave_all(at, [](int x, int y) { return min(x, y); });
-    if ((threadIdx.x & 63) == 0) places[threadIdx.x >> 6] = at;
+      for (int e = 0; e < Chunk<T>::E; ++e) top = fmaxf(top, c.x[p][e]);
+    top = wave_all(top, [](float x, float y) { return fmaxf(x, y); });
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kVerThreads / 64; ++w) part.at = min(part.at, places[w]);
-  } else {
-    const double by = 1.0 / (double)temperature;
-    const Weigher w(table, top, by);
-    double s = 0.0;
-    if (w.plain) {
+    for (int w = 0; w < kVerThreads / 64; ++w) top = fmaxf(top, tops[w]);
+    VerifyPart part{0.0, top, 0x7fffffff};
+    // (either way ends behind a second barrier, so the tops may be written again)
+    if (greedy(temperature)) {
+      int at = 0x7fffffff;
 #pragma unroll
       for (int p = 0; p < kVerPieces; ++p)
 #pragma unroll
-        for (int e = 0; e < Chunk<T>::E; ++e) s += w.of(c.x[p][e]);
+        for (int e = 0; e < Chunk<T>::E; ++e)
+          if (c.x[p][e] == top && top != -INFINITY) at = min(at, Chunk<T>::index(from, chunk, p, e));
+      at = wave_all(at, [](int x, int y) { return min(x, y); });
+      if ((threadIdx.x & 63) == 0) places[threadIdx.x >> 6] = at;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < kVerThreads / 64; ++w) part.at = min(part.at, places[w]);
     } else {
-      for (int i = threadIdx.x; i < Chunk<T>::kElements; i += kVerThreads) {
-        const int at = chunk * Chunk<T>::kElements + i - Chunk<T>::lead(from);
-        if (at >= 0 && at < a.vocabulary) s += weight(number(logit<T>(from, at)), top, by);
+      const Weigher w(table, top, by);
+      double s = 0.0;
+      if (w.plain) {
+#pragma unroll
+        for (int p = 0; p < kVerPieces; ++p)
+#pragma unroll
+          for (int e = 0; e < Chunk<T>::E; ++e) s = w.plus(c.x[p][e], s);
+      } else {
+        for (int i = threadIdx.x; i < Chunk<T>::kElements; i += kVerThreads) {
+          const int at = chunk * Chunk<T>::kElements + i - Chunk<T>::lead(from);
+          if (at >= 0 && at < a.vocabulary) s += weight(number(logit<T>(from, at)), top, by);
+        }
       }
+      part.sum = group_sum(s, sums);
     }
-    part.sum = group_sum(s, sums);
+    if (threadIdx.x == 0) a.parts[((int64_t)blockIdx.y * a.batch * a.nodes + row) * a.chunks + chunk] = part;
+    if (next >= a.chunks) return;
+    chunk = next;
   }
-  if (threadIdx.x == 0) a.parts[((int64_t)blockIdx.y * a.batch * a.nodes + row) * a.chunks + chunk] = part;
 }
 
 // The softmax of a whole row from its parts, by one wavefront; every lane has the answer.  by: 1 / temperature; best: the best token is
@@ -402,7 +446,8 @@ __global__ void __launch_bounds__(kVerThreads) verify_rows_kernel(const VerifyAr
 // A row that the path does not come to is not worth the sum: some ancestor has taken another child, or none.
 template <typename T>
 __global__ void __launch_bounds__(kVerThreads) verify_rest_kernel(const VerifyArgs a, int round, int groups) {
-  __shared__ double sums[kVerThreads / 64], table[kVerTable];
+  __shared__ double sums[kVerThreads / 64];
+  __shared__ uint32_t table[2 * kVerTable];
   __shared__ int parents[kVerMaxNodes], taken[kVerMaxNodes], wanted;      // taken: -2 where it is still open
   const int row = blockIdx.x / groups, b = row / a.nodes, node = row - b * a.nodes;
   const float temperature = a.temperature[b];
@@ -573,8 +618,8 @@ __global__ void __launch_bounds__(kVerChooseThreads) verify_choose_kernel(const 
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       }
     }
-    // The weight of a chunk in what is left.  A sum less its refused parts is off by 1e-16 of the whole; a child is refused by a uniform of at most
-    // 1 - 2^-24, so at least that share of the whole is left, but for one chance in 10^14.
+    // The weight of a chunk in what is left.  A sum less its refused parts is off by 1e-13 of them at most (Weigher; those that are the largest of their chunk are
+    // exact).  Where a share s of the whole is left, and the chance that it comes to that is s, this is 1e-13 / s of it: one draw in 10^13 goes elsewhere.
     auto chunk_weight = [&](int i) {
       if (s.level >= 0) return a.rest[(s.level * rows + row) * a.chunks + i];
       const VerifyPart part = a.parts[row * a.chunks + i];

@@ -167,6 +167,22 @@ def test_masked_infinite_and_missing_logits(dtype, drafted):
     compare(**x)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("drafted", [False, True])
+def test_signaling_nan(dtype, drafted):
+    x = inputs(dtype, 6, 4, 700, 0, drafted, seed=12, greedy=3)
+    for rows in (x["logits"], x["draft"]) if drafted else (x["logits"],):
+        bits, nan = {2: (torch.int16, {"f16": 0x7c01, "bf16": 0x7f81}.get(dtype)), 4: (torch.int32, 0x7f800001)}[rows.element_size()]
+        rows.view(bits)[:, :, 1::3] = nan
+    x["tokens"][:2] = 3
+    compare(**x)
+
+
+@pytest.mark.parametrize("dtype,drafted", [("f32", False), ("f16", True), ("bf16", True)])
+def test_many_long_rows(dtype, drafted):
+    compare(**inputs(dtype, 32, 8, 70001, 0, drafted, seed=13, greedy=5))
+
+
 @pytest.mark.parametrize("drafted", [False, True])
 def test_an_infinite_temperature(drafted):
     """Every word that is not masked is as likely as any other."""
