@@ -203,6 +203,24 @@ __device__ __forceinline__ double wave_sum(double v) {
   return wave_all(v, [](double a, double b) { return a + b; });
 }
 
+// The sum over this lane and those before it: inside sixteen lanes by shifts, then the last of a sixteen is added to the next sixteen and the last of the
+// first half to the second.  A lane that has no source adds 0.
+template <int CONTROL, int ROWS>
+__device__ __forceinline__ double plus_before(double v) {
+  const uint64_t w = __builtin_bit_cast(uint64_t, v);
+  const uint32_t low = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)w, CONTROL, ROWS, 0xf, false);
+  const uint32_t high = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(w >> 32), CONTROL, ROWS, 0xf, false);
+  return v + __builtin_bit_cast(double, (uint64_t)high << 32 | low);
+}
+__device__ __forceinline__ double wave_scan(double v) {
+  v = plus_before<0x111, 0xf>(v);
+  v = plus_before<0x112, 0xf>(v);
+  v = plus_before<0x114, 0xf>(v);
+  v = plus_before<0x118, 0xf>(v);
+  v = plus_before<0x142, 0xa>(v);
+  return plus_before<0x143, 0xc>(v);
+}
+
 // The sum over a workgroup, in every thread; `space` has room for a value per wavefront and may be used again behind the next barrier.
 template <int THREADS = kVerThreads>
 __device__ __forceinline__ double group_sum(double v, double* space) {
@@ -531,7 +549,8 @@ __global__ void __launch_bounds__(kVerChooseThreads) verify_choose_kernel(const 
   __shared__ Tree tree;
   __shared__ RowState states[kVerMaxNodes];
   __shared__ RowTop tops[kVerMaxNodes], draft_tops[kVerMaxNodes];
-  __shared__ double sums[WAVES], before_chunk;
+  __shared__ double sums[WAVES], before_chunk, gone_weights[kVerMaxNodes];
+  __shared__ uint32_t table[2 * kVerTable];
   __shared__ int end, length, the_chunk, gone_count, found[WAVES], lasts[WAVES], gone[kVerMaxNodes];
   const int b = blockIdx.x, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const float temperature = a.temperature[b];
@@ -539,6 +558,7 @@ __global__ void __launch_bounds__(kVerChooseThreads) verify_choose_kernel(const 
   const double by = best ? 0.0 : 1.0 / (double)temperature;
   const int64_t rows = (int64_t)a.batch * a.nodes;
   load_tree(a, b, tree);
+  fill_table(table);
   __syncthreads();
   for (int node = wave; node < a.nodes; node += WAVES) {
     RowTop p, q{};
@@ -613,7 +633,10 @@ __global__ void __launch_bounds__(kVerChooseThreads) verify_choose_kernel(const 
         for (int i = lane; i < n; i += 64) before = before || gone[i] == w;
         if (__any(before) || !(left - pw > 0.0)) continue;
         left -= pw;
-        if (lane == 0) gone[n] = w;
+        if (lane == 0) {
+          gone[n] = w;
+          gone_weights[n] = pw;
+        }
         ++n;
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       }
@@ -625,24 +648,19 @@ __global__ void __launch_bounds__(kVerChooseThreads) verify_choose_kernel(const 
       const VerifyPart part = a.parts[row * a.chunks + i];
       double w = part.sum * weight(part.top, p.top, by) / p.sum;
       for (int j = 0; j < n; ++j)
-        if ((gone[j] + lead) / Chunk<T>::kElements == i) w -= weight(number(logit<T>(from_p, gone[j])), p.top, by) / p.sum;
+        if ((gone[j] + lead) / Chunk<T>::kElements == i) w -= gone_weights[j];
       return __builtin_fmax(w, 0.0);
     };
-    double whole = 0.0;
-    for (int i = lane; i < a.chunks; i += 64) whole += chunk_weight(i);
+    const double first_weight = lane < a.chunks ? chunk_weight(lane) : 0.0;
+    double whole = first_weight;
+    for (int i = lane + 64; i < a.chunks; i += 64) whole += chunk_weight(i);
     whole = wave_sum(whole);
     const double at = (double)a.uniforms[(int64_t)b * a.nodes] * whole;
     double before = 0.0, chosen_before = 0.0, with_before = 0.0;
     int chosen = -1, with = -1;
     for (int first = 0; first < a.chunks && chosen < 0; first += 64) {
-      const double w = first + lane < a.chunks ? chunk_weight(first + lane) : 0.0;
-      double run = w;
-#pragma unroll
-      for (int i = 1; i < 64; i *= 2) {
-        const double v = __shfl_up(run, i);
-        if (lane >= i) run += v;
-      }
-      run += before;
+      const double w = first == 0 ? first_weight : first + lane < a.chunks ? chunk_weight(first + lane) : 0.0;
+      const double run = wave_scan(w) + before;
       const uint64_t over = __ballot(run > at && w > 0.0), some = __ballot(w > 0.0);
       if (over != 0) {
         const int l = __ffsll((unsigned long long)over) - 1;
@@ -675,29 +693,49 @@ __global__ void __launch_bounds__(kVerChooseThreads) verify_choose_kernel(const 
   // inside the chunk: a piece to a thread, in the order of the row
   const double scale_p = 1.0 / p.sum, scale_q = !named && q.sum > 0.0 ? s.a / q.sum : 0.0, need = before_chunk;
   const int start = chunk * Chunk<T>::kElements + (int)threadIdx.x * E - lead;
-  double w[E], mine = 0.0;
+  auto piece = [&](const char* from, bool even) {
+    typename Piece<T>::type v;
+    if (even && start >= 0 && start + E <= a.vocabulary) {
+      v = *reinterpret_cast<const typename Piece<T>::type*>(from + (int64_t)start * sizeof(T));
+    } else {      // all on their way at once: places outside the row read its ends
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] = reinterpret_cast<const T*>(from)[min(max(start + e, 0), a.vocabulary - 1)];
+    }
+    return v;
+  };
+  const typename Piece<T>::type of_p = piece(from_p, true);
+  typename Piece<T>::type of_q{};
+  if (scale_q != 0.0) of_q = piece(from_q, Chunk<T>::lead(from_q) == lead);
+  float x[E], y[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    const int i = start + e;
-    const bool inside = i >= 0 && i < a.vocabulary;
-    w[e] = inside ? weight(number(logit<T>(from_p, i)), p.top, by) * scale_p : 0.0;
-    if (scale_q != 0.0 && inside) w[e] = __builtin_fmax(w[e] - weight(number(logit<T>(from_q, i)), q.top, by) * scale_q, 0.0);
+    x[e] = start + e >= 0 && start + e < a.vocabulary ? number((float)of_p[e]) : -INFINITY;
+    y[e] = number((float)of_q[e]);
+  }
+  const Weigher wp(table, p.top, by), wq(table, q.top, by);
+  double w[E], mine = 0.0;
+  if (wp.plain && (scale_q == 0.0 || wq.plain)) {      // (1e-290 as in the sums of what is left)
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      w[e] = __builtin_fmax(__builtin_fma(wp.of(x[e]), scale_p, scale_q != 0.0 ? -__builtin_fma(wq.of(y[e]), scale_q, 1e-290) : -1e-290), 0.0);
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      w[e] = weight(x[e], p.top, by) * scale_p;
+      if (scale_q != 0.0) w[e] = __builtin_fmax(w[e] - weight(y[e], q.top, by) * scale_q, 0.0);
+    }
   }
   for (int j = 0; j < goners; ++j)
 #pragma unroll
     for (int e = 0; e < E; ++e) w[e] = gone[j] == start + e ? 0.0 : w[e];
 #pragma unroll
   for (int e = 0; e < E; ++e) mine += w[e];
-  double upto = mine;
-#pragma unroll
-  for (int i = 1; i < 64; i *= 2) {
-    const double v = __shfl_up(upto, i);
-    if (lane >= i) upto += v;
-  }
+  const double upto = wave_scan(mine);
   if (lane == 63) sums[wave] = upto;
   __syncthreads();
   double at = upto - mine;
-  for (int i = 0; i < wave; ++i) at += sums[i];
+#pragma unroll
+  for (int i = 0; i < WAVES - 1; ++i) at += i < wave ? sums[i] : 0.0;
   int answer = 0x7fffffff, last = -1;
 #pragma unroll
   for (int e = 0; e < E; ++e) {
@@ -715,6 +753,7 @@ __global__ void __launch_bounds__(kVerChooseThreads) verify_choose_kernel(const 
   }
   __syncthreads();
   if (threadIdx.x == 0) {
+#pragma unroll
     for (int i = 0; i < WAVES; ++i) {
       answer = min(answer, found[i]);
       last = max(last, lasts[i]);
