@@ -203,6 +203,13 @@ __device__ __forceinline__ double wave_sum(double v) {
   return wave_all(v, [](double a, double b) { return a + b; });
 }
 
+// The value of one lane, which is the same for all.
+__device__ __forceinline__ double of_lane(double v, int lane) {
+  const uint64_t w = __builtin_bit_cast(uint64_t, v);
+  const uint32_t low = __builtin_amdgcn_readlane((int)(uint32_t)w, lane), high = __builtin_amdgcn_readlane((int)(uint32_t)(w >> 32), lane);
+  return __builtin_bit_cast(double, (uint64_t)high << 32 | low);
+}
+
 // The sum over this lane and those before it: inside sixteen lanes by shifts, then the last of a sixteen is added to the next sixteen and the last of the
 // first half to the second.  A lane that has no source adds 0.
 template <int CONTROL, int ROWS>
@@ -309,10 +316,14 @@ struct RowTop {
   int at;          // greedy: the first place of the largest; 0x7fffffff: the row has no number
   double sum;
 };
-__device__ __forceinline__ RowTop row_top(const VerifyPart* parts, int chunks, double by, bool best) {
+// mine: my_part(), which may be asked for long before.
+__device__ __forceinline__ VerifyPart my_part(const VerifyPart* parts, int chunks) {
+  const int lane = threadIdx.x & 63;
+  return lane < chunks ? parts[lane] : VerifyPart{0.0, -INFINITY, 0x7fffffff};
+}
+__device__ __forceinline__ RowTop row_top(const VerifyPart* parts, int chunks, double by, bool best, const VerifyPart& mine) {
   RowTop r{-INFINITY, 0x7fffffff, 0.0};
   const int lane = threadIdx.x & 63;
-  const VerifyPart mine = lane < chunks ? parts[lane] : VerifyPart{0.0, -INFINITY, 0x7fffffff};
   float top = mine.top;
   for (int i = lane + 64; i < chunks; i += 64) top = fmaxf(top, parts[i].top);
   r.top = wave_all(top, [](float x, float y) { return fmaxf(x, y); });
@@ -368,8 +379,11 @@ __device__ __forceinline__ Child child_of(const VerifyArgs& g, const int32_t* pa
     c.word = tokens[mine];
     c.u = g.uniforms[(int64_t)b * g.nodes + mine];
     if ((uint32_t)c.word < (uint32_t)g.vocabulary) {
-      c.x = number(logit<T>(g.logits + (b * g.logits_batch + node * g.logits_node) * (int64_t)sizeof(T), c.word));
-      if (g.draft != nullptr) c.y = number(logit<T>(g.draft + (b * g.draft_batch + node * g.draft_node) * (int64_t)sizeof(T), c.word));
+      const char* from_p = g.logits + (b * g.logits_batch + node * g.logits_node) * (int64_t)sizeof(T);      // both on their way before either is looked at
+      const char* from_q = g.draft == nullptr ? from_p : g.draft + (b * g.draft_batch + node * g.draft_node) * (int64_t)sizeof(T);
+      const T x = reinterpret_cast<const T*>(from_p)[c.word], y = reinterpret_cast<const T*>(from_q)[c.word];
+      c.x = number((float)x);
+      c.y = number((float)y);
     }
   }
   return c;
@@ -396,10 +410,10 @@ __device__ RowState test_children(const VerifyArgs& g, const int32_t* parents, c
     const double pw = child && p.sum > 0.0 ? weight(c.x, p.top, by) / p.sum : 0.0, qw = child && q.sum > 0.0 ? weight(c.y, q.top, by) / q.sum : 0.0;
     for (uint64_t left = __ballot(child); left != 0; left &= left - 1) {
       const int l = __ffsll((unsigned long long)left) - 1;
-      const double cu = __shfl(u, l), cp = __shfl(pw, l), cq = __shfl(qw, l);
+      const double cu = of_lane(u, l), cp = of_lane(pw, l), cq = of_lane(qw, l);
       if (g.draft == nullptr) {
         // a word that was refused before has left already
-        const int w = __shfl(word, l);
+        const int w = __builtin_amdgcn_readlane(word, l);
         bool before = __any(child && lane < l && word == w);
         for (int i = node + 1; !before && i < first; i += 64)
           before = __any(i + lane < first && parent(i + lane) == node && tokens[i + lane] == w);
@@ -448,11 +462,17 @@ __global__ void __launch_bounds__(kVerThreads) verify_rows_kernel(const VerifyAr
   if (greedy(temperature)) return;
   const double by = 1.0 / (double)temperature;
   const int32_t *parents = a.parents == nullptr ? nullptr : a.parents + (int64_t)b * a.nodes, *tokens = a.tokens + (int64_t)b * a.nodes;
+  const VerifyPart *parts = a.parts + (int64_t)row * a.chunks, *draft_parts = parts + (int64_t)a.batch * a.nodes * a.chunks;
+  VerifyPart part{}, draft_part{};
+  if (round == 0) {
+    part = my_part(parts, a.chunks);
+    draft_part = my_part(draft_parts, a.chunks);
+  }
   const Child child = child_of<T>(a, parents, tokens, b, node, node + 1);
   RowInfo info;
   if (round == 0) {
-    info.p = row_top(a.parts + (int64_t)row * a.chunks, a.chunks, by, false);
-    info.q = row_top(a.parts + ((int64_t)a.batch * a.nodes + row) * a.chunks, a.chunks, by, false);
+    info.p = row_top(parts, a.chunks, by, false, part);
+    info.q = row_top(draft_parts, a.chunks, by, false, draft_part);
   } else {
     info = a.infos[row];
   }
@@ -563,9 +583,12 @@ __global__ void __launch_bounds__(kVerChooseThreads) verify_choose_kernel(const 
   for (int node = wave; node < a.nodes; node += WAVES) {
     RowTop p, q{};
     Child child{};
+    const VerifyPart* parts = a.parts + (b * a.nodes + node) * (int64_t)a.chunks;
+    VerifyPart part{};
+    if (best || named) part = my_part(parts, a.chunks);
     if (!best) child = child_of<T>(a, tree.parents, tree.tokens, b, node, node + 1);
     if (best || named) {
-      p = row_top(a.parts + (b * a.nodes + node) * (int64_t)a.chunks, a.chunks, by, best);
+      p = row_top(parts, a.chunks, by, best, part);
     } else {
       p = a.infos[b * a.nodes + node].p;
       q = a.infos[b * a.nodes + node].q;
@@ -627,8 +650,8 @@ __global__ void __launch_bounds__(kVerChooseThreads) verify_choose_kernel(const 
       const int word = child ? tree.tokens[mine] : -1;
       const double have = child ? weight(number(logit<T>(from_p, word)), p.top, by) / p.sum : 0.0;
       for (uint64_t rest = __ballot(child); rest != 0; rest &= rest - 1) {
-        const int l = __ffsll((unsigned long long)rest) - 1, w = __shfl(word, l);
-        const double pw = __shfl(have, l);
+        const int l = __ffsll((unsigned long long)rest) - 1, w = __builtin_amdgcn_readlane(word, l);
+        const double pw = of_lane(have, l);
         bool before = false;
         for (int i = lane; i < n; i += 64) before = before || gone[i] == w;
         if (__any(before) || !(left - pw > 0.0)) continue;
