@@ -290,7 +290,8 @@ int dpllm_rope(const dpllm_heads* x, const dpllm_heads* out, const int* heads, i
  * out = softmax_t(scale q . k_t) v over the tokens t < lens[b] of the cache (kv head h / (heads / cache->heads)) and those nodes j whose bit is set in
  * row i of the mask: bit j % 64 of word mask[b * mask_stride + i * ceil(nodes / 64) + j / 64]; mask_stride 0: one mask for all sequences.  A node sees itself only if
  * its own bit says so.  mask_dev NULL: the nodes are a chain, i sees j <= i.  k_new and v_new NULL: the cache only.  Nothing that is not seen is
- * read as a number: infinities and NaN there change nothing.  A row that sees nothing is zero, its lse minus infinity.  lens: negative is 0, and no
+ * read as a number: infinities and NaN there change nothing.  A row that sees nothing (or scores of minus infinity only) is zero, its lse minus infinity;
+ * one that sees a score of NaN or plus infinity is NaN, and so is its lse.  lens: negative is 0, and no
  * more than the sequence's pages hold.  max_len: how long the longest is expected to be; it sets how the work is split, not the result.
  * q, out: [batch][nodes][heads][head_dim]; k_new, v_new: [batch][nodes][cache->heads][head_dim]; all of the cache's type, DPLLM_F16 or DPLLM_BF16,
  * 16-byte aligned, strides multiples of 8 elements.  head_dim 64, 96, 128 or 256; heads a multiple of cache->heads; nodes up to DPLLM_MAX_NODES.

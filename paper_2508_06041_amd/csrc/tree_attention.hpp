@@ -98,10 +98,13 @@ __device__ __forceinline__ void store_words(char* p, const uint32_t (&w)[N]) {
   }
 }
 
-// The logarithm of the sum of exp(scale x) over a row whose weights relative to the score m add up to s.
+// The weights of a row relative to the score m add up to s, which is 0 only where the row has no score: the largest counts 1 or more.  A row whose scores are
+// NaN has a NaN for a sum and maybe no m, so it is the sum that tells, and the NaN that ends up in the result.
+__device__ __forceinline__ float one_over(float s) { return s == 0.f ? 0.f : 1.f / s; }
+// The logarithm of the sum of exp(scale x) over the row.
 template <typename T>
 __device__ __forceinline__ float log_sum(float m, float s, float scale) {
-  return m == -INFINITY ? m : m * scale + (__builtin_amdgcn_logf(s) - Matrix<T>::kLift) * 0.69314718055994530942f;
+  return s == 0.f ? -INFINITY : m * scale + (__builtin_amdgcn_logf(s) - Matrix<T>::kLift) * 0.69314718055994530942f;
 }
 
 // The largest value of the four lanes of a row (16 lanes apart).
@@ -529,7 +532,7 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) tree_attention_k
     if (r >= a.rows) continue;
     const int d = 4 * DV * g + wave * PER;
     if (share.parts == 1) {
-      const float by = m == -INFINITY ? 0.f : 1.f / s;
+      const float by = one_over(s);
       uint32_t words[PER / 2];
 #pragma unroll
       for (int j = 0; j < PER / 2; ++j) words[j] = pack2<T>(e[2 * j] * by, e[2 * j + 1] * by);
@@ -547,7 +550,8 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) tree_attention_k
   }
 }
 
-// The parts of a row meet: one wavefront to a row.  Tops first, then sums of eight parts at a time, so that their loads are on the way together.
+// The parts of a row meet: one wavefront to a row.  Tops first, then sums of eight parts at a time, so that their loads are on the way together.  (A part without a
+// top is not read.  It may have a NaN for a sum: then so has the row, and all of the result is NaN.)
 template <typename T, int D>
 __global__ void __launch_bounds__(256) tree_attention_join_kernel(const AttentionArgs a, int rows_of_tile, Divide by_rows, Divide by_heads, Divide by_tile, uint32_t all_rows) {
   const int lane = threadIdx.x & 63;
@@ -596,7 +600,7 @@ __global__ void __launch_bounds__(256) tree_attention_join_kernel(const Attentio
         }
     }
   }
-  const float by = m == -INFINITY ? 0.f : 1.f / s;
+  const float by = one_over(s);
   const int node = a.by_group.of(r), head = h * a.group + r - node * a.group;
   char* out = a.out.data + 2 * (b * a.out.batch_stride + node * a.out.token_stride + head * a.out.head_stride + at);
   if (D >= 128 || lane < D / 2)
@@ -752,7 +756,7 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 && MT <= 2 ? 2 : 1) tree_
     if (r >= a.rows) continue;
     const float m = rows.top[mt];
     if (share.parts == 1) {
-      const float by = m == -INFINITY ? 0.f : 1.f / s;
+      const float by = one_over(s);
       const int head = h * a.group + r - node[mt] * a.group;
       char* out = a.out.data + 2 * (b * a.out.batch_stride + node[mt] * a.out.token_stride + head * a.out.head_stride + 4 * g);
 #pragma unroll

@@ -1,0 +1,64 @@
+"""Attention of drafted tokens where queries, seen keys or scores are no ordinary numbers, against the formula in 64 bits."""
+import math
+
+import pytest
+import torch
+
+from test_gpu_tree_attention import TYPES, Case, words
+
+pytestmark = pytest.mark.gpu
+
+# nodes, heads, kv heads: one row to a kv head, a tile of 16 rows that is full, one of 32, and the kernels for many rows
+ROWS = [(1, 2, 2), (1, 16, 1), (4, 8, 1), (9, 8, 2), (70, 4, 2)]
+LENGTHS = [40, 3000]      # in one part and in several
+
+
+def check(c, **kw):
+    """As Case.check(), and NaN are where the formula has them, in the rows and in lse."""
+    out, lse = (x.double().cpu() for x in c.run(**kw))
+    want, want_lse = c.plain()
+    assert torch.equal(out.isnan(), want.isnan()) and torch.equal(lse.isnan(), want_lse.isnan())
+    some = ~want.isnan()
+    assert ((out - want).abs() <= c.bound)[some].all()
+    some, none = ~want_lse.isnan() & (want_lse != -math.inf), want_lse == -math.inf
+    assert torch.equal(lse == -math.inf, none) and ((lse - want_lse).abs() <= c.lse_bound)[some].all()
+    return want_lse
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("length", LENGTHS)
+@pytest.mark.parametrize("nodes,heads,kv", ROWS)
+def test_queries_that_are_no_numbers(dtype, nodes, heads, kv, length):
+    """A NaN in a query, or an infinity that meets keys of both signs, makes its row NaN and no other one, however the work is split."""
+    c = Case(dtype, 2, nodes, heads, kv, 128, 16, [length, 5], mask="tree", seed=nodes)
+    c.q[0, nodes - 1, 0, 5] = math.nan
+    if heads > 2:
+        c.q[0, 0, heads - 1, 127], c.q[1, 0, 2, 0] = math.inf, math.nan
+        c.q[0, 0, heads - 1, 126] = math.inf
+    lse = check(c)
+    assert lse.isnan().sum() == (1 if heads == 2 else 3)
+    for max_len in (0, 100000):
+        check(c, max_len=max_len)
+    c.q[:] = math.nan
+    assert check(c).isnan().all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("length", LENGTHS)
+@pytest.mark.parametrize("nodes,heads,kv", ROWS)
+def test_seen_keys_that_are_no_numbers(dtype, nodes, heads, kv, length):
+    """A NaN in a key makes the rows that see it NaN."""
+    c = Case(dtype, 2, nodes, heads, kv, 64, 16, [length, 5], mask="any", seed=nodes)
+    c.sees[:, :, nodes - 1] = False
+    c.sees[0, ::2, nodes - 1] = True
+    c.mask = words(c.sees)
+    c.k_new[0, nodes - 1, 0, 3] = math.nan
+    lse = check(c)
+    assert torch.equal(lse[0, :, 0].isnan(), c.sees[0, :, nodes - 1]) and not lse[1].isnan().any()
+    at = c.table[1, 0].item()
+    c.k[0, at, 4, kv - 1, 0] = math.nan      # the last token of the second sequence
+    lse = check(c)
+    assert lse[1, :, heads - 1].isnan().all()
+    if length > 1000:                        # among a thousand others, in one of the middle parts
+        c.k[0, c.table[0, 100].item(), 7] = math.nan
+        assert check(c)[0].isnan().all()
