@@ -118,8 +118,10 @@ __device__ __forceinline__ float row_max(float x) {
 }
 
 // What a wavefront has of its rows: the weighted values, the weights' sum, and the score `top` they are relative to: a weight is
-// 2^((x - top) scale + lift), formed as 2^(x scale + from); with huge tops, whose product with the scale may be past the floats though the scores are not,
+// 2^((x - top) scale + lift), formed as 2^(x scale + from).  from is rounded to a step of its size, which all weights of the row share: nothing next to the
+// rounding of the scores themselves, but beside products of more than kHuge it would come to more than the weights' range (and the products may be past the floats).  There
 // top is taken from the scores first and from is the lift.
+constexpr float kHuge = 65536.f;      // steps of 2^-7: weights within 0.3 % of what they should be
 constexpr float kNoTop = 1e37f;      // `from` of a row without a score yet: the first one it gets has an infinite weight
 template <int MT, int DV>
 struct Rows {
@@ -207,7 +209,7 @@ __device__ __forceinline__ void weigh(Rows<MT, DV>& r, Scores<MT>& s, float scal
       const float next = fmaxf(r.top[mt], row_max(most));
       const float less = r.top[mt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((r.top[mt] - next) * scale_log2);
       r.top[mt] = next;
-      huge = huge || (next != -INFINITY && __builtin_fabsf(next) > 1e38f);
+      huge = huge || (next != -INFINITY && __builtin_fabsf(next) * scale_log2 > kHuge);
       r.sum[mt] *= less;
 #pragma unroll
       for (int j = 0; j < DV; ++j) r.o[mt][j] *= less;

@@ -62,3 +62,30 @@ def test_seen_keys_that_are_no_numbers(dtype, nodes, heads, kv, length):
     if length > 1000:                        # among a thousand others, in one of the middle parts
         c.k[0, c.table[0, 100].item(), 7] = math.nan
         assert check(c)[0].isnan().all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("length", LENGTHS)
+@pytest.mark.parametrize("nodes,heads,kv", ROWS)
+@pytest.mark.parametrize("value", [1e5, -3e6, 1e9, -1e12, 1e20, -1e36, 1e38])
+def test_scores_far_from_zero(dtype, length, nodes, heads, kv, value):
+    """The same score for all tokens, another one in every row: all weights are equal.  Then one token further from zero: it has all of the weight, or none."""
+    c = Case(dtype, 1, nodes, heads, kv, 64, 16, [length], new=False, scale=value)
+    c.q[:], c.k[:] = 0.0, 0.0
+    size = 1 + torch.arange(nodes * heads).reshape(nodes, heads) % 64 / 64      # good in either type
+    c.q[0, :, :, 0] = size.to(c.t)
+    c.k[..., 0] = 1.0
+    values = c.v[0, c.table[0].long()].flatten(0, 1)[:length].double().repeat_interleave(heads // kv, 1)      # [token][head][d]
+    odd = length // 3
+    for alone in (False, True):
+        if alone:
+            c.k[0, c.table[0, odd // 16], odd % 16, :, 0] = 1.5
+        out, lse = (x.double().cpu() for x in c.run())
+        some = values if not alone else values[odd:odd + 1] if value > 0 else torch.cat([values[:odd], values[odd + 1:]])
+        want = some.mean(0)
+        # equal weights are rounded alike, half a step; sums in 32 bits, one rounding of the result
+        eps = torch.finfo(c.t).eps / 2
+        bound = (eps + (length + 4) * 2.0 ** -24) * some.abs().mean(0) + eps * want.abs() + 2.0 ** -24
+        assert ((out[0] - want).abs() <= bound).all()
+        top = size.double() * value * (1.5 if alone and value > 0 else 1.0)
+        assert ((lse[0] - top).abs() <= 2.0 ** -21 * top.abs() + math.log(length) + 1).all()
