@@ -122,18 +122,18 @@ __device__ __forceinline__ float row_max(float x) {
 // rounding of the scores themselves, but beside products of more than kHuge it would come to more than the weights' range (and the products may be past the floats).  There
 // top is taken from the scores first and from is the lift.
 constexpr float kHuge = 65536.f;      // steps of 2^-7: weights within 0.3 % of what they should be
-constexpr float kNoTop = 1e37f;      // `from` of a row without a score yet: the first one it gets has an infinite weight
 template <int MT, int DV>
 struct Rows {
   f32x4 o[MT][DV];
   float sum[MT], top[MT], from[MT];      // sum: of the lane's own tokens
-  bool huge;
+  bool huge, waiting;      // waiting: some row has no score yet
   __device__ __forceinline__ void clear() {
     huge = false;
+    waiting = true;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       top[mt] = -INFINITY;
-      from[mt] = kNoTop;
+      from[mt] = 0.f;
       sum[mt] = 0.f;
 #pragma unroll
       for (int j = 0; j < DV; ++j) o[mt][j] = f32x4{0, 0, 0, 0};
@@ -169,9 +169,9 @@ __device__ __forceinline__ void mask(Scores<MT>& s, const uint32_t (&seen)[MT]) 
     for (int i = 0; i < 8; ++i) s[mt][i / 4][i % 4] = (seen[mt] >> i) & 1 ? s[mt][i / 4][i % 4] : -INFINITY;
 }
 
-// The weights of a step, rounded for the value product, and their sum.  They are formed with the `top` there is: only where a lane's weights come to more than kLimit
-// does top follow the largest score, with an exchange between lanes and a scaling of o, and the weights are formed again.  That is the first step with a score and few after
-// it; all others look for no maximum at all.
+// The weights of a step, rounded for the value product, and their sum.  They are formed with the `top` there is: only where a lane's weights come to more than kLimit,
+// or a row has none, does top follow the largest score, with an exchange between lanes and a scaling of o, and the weights are formed again.  That is the first step with
+// a score and few after it (but all steps of a wavefront with a row that sees nothing, of which only nodes make some); all others look for no maximum at all.
 template <typename T, int MT, int DV>
 __device__ __forceinline__ void weigh(Rows<MT, DV>& r, Scores<MT>& s, float scale_log2, u32x4 (&w)[MT]) {
   constexpr float kLift = Matrix<T>::kLift;
@@ -199,8 +199,8 @@ __device__ __forceinline__ void weigh(Rows<MT, DV>& r, Scores<MT>& s, float scal
   bool behind = false;
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) behind = behind || add[mt] > Matrix<T>::kLimit;
-  if (__any(behind)) {
-    bool huge = false;
+  if (r.waiting || __any(behind)) {
+    bool huge = false, waiting = false;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       float most = s[mt][0][0];
@@ -217,8 +217,11 @@ __device__ __forceinline__ void weigh(Rows<MT, DV>& r, Scores<MT>& s, float scal
     r.huge = __any(huge);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
-      r.from[mt] = r.top[mt] == -INFINITY ? kNoTop : r.huge ? kLift : __builtin_fmaf(-r.top[mt], scale_log2, kLift);
+      r.from[mt] = r.top[mt] == -INFINITY ? 0.f : r.huge ? kLift : __builtin_fmaf(-r.top[mt], scale_log2, kLift);
     form();
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) waiting = waiting || (r.top[mt] == -INFINITY && add[mt] == add[mt]);      // (a row of NaN waits for nothing)
+    r.waiting = __any(waiting);
   }
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {

@@ -89,3 +89,21 @@ def test_scores_far_from_zero(dtype, length, nodes, heads, kv, value):
         assert ((out[0] - want).abs() <= bound).all()
         top = size.double() * value * (1.5 if alone and value > 0 else 1.0)
         assert ((lse[0] - top).abs() <= 2.0 ** -21 * top.abs() + math.log(length) + 1).all()
+
+
+@pytest.mark.parametrize("length", LENGTHS)
+@pytest.mark.parametrize("nodes,heads", [(1, 1), (1, 16), (2, 16), (4, 16), (9, 16)])
+@pytest.mark.parametrize("value", [torch.finfo(torch.bfloat16).min, -2e37])
+def test_scores_next_to_the_lowest(length, nodes, heads, value):
+    """Scores that are all the same, far below zero: all weights are equal, in tiles that are full and in such that are not."""
+    c = Case("bf16", 1, nodes, heads, 1, 64, 16, [length], new=False, scale=1.0)
+    c.q[:], c.k[:] = 0.0, 0.0
+    c.q[..., 0] = 1.0
+    c.k[..., 0] = value
+    out, lse = c.run()
+    values = c.v[0, c.table[0].long(), :, 0].flatten(0, 1)[:length].double()
+    want = values.mean(0)
+    # the weights are powers of two up to the last bit of a float; sums in 32 bits, one rounding of the result
+    bound = (length + 4) * 2.0 ** -24 * values.abs().mean(0) + 2.0 ** -8 * want.abs() + 2.0 ** -24
+    assert ((out.double().cpu() - want).abs() <= bound).all()
+    assert (lse / c.k[0, 0, 0, 0, 0].item() - 1).abs().max() <= 2.0 ** -20
