@@ -340,6 +340,18 @@ __device__ __forceinline__ RowTop row_top(const VerifyPart* parts, int chunks, d
   return r;
 }
 
+// max(p - a q, 0) of a word from its weights.  Both products are rounded before they meet: one that is subtracted as it is from a rounded one leaves its rounding,
+// and equal rows would leave something everywhere.  `none` is taken off besides.
+__device__ __forceinline__ double left_of(double weight_p, double scale_p, double weight_q, double scale_q, double none) {
+#pragma clang fp contract(off)
+  const double p = weight_p * scale_p, q = __builtin_fma(weight_q, scale_q, none);
+  return __builtin_fmax(p - q, 0.0);
+}
+
+// A sum of what is left that is no more than this is what the rounding of equal probabilities comes to, and nothing is left: weights and the two rows' sums are
+// good to 1e-13 each (the rows may be cut into chunks at different words).
+constexpr double kNothingLeft = 4e-13;
+
 // What the tests of a row's children came to.
 struct RowState {
   int taken;        // the child that stands, or -1
@@ -442,7 +454,7 @@ __device__ RowState test_children(const VerifyArgs& g, const int32_t* parents, c
       double rest = 0.0;
       for (int i = lane; i < g.chunks; i += 64) rest += g.rest[((int64_t)j * g.batch * g.nodes + row) * g.chunks + i];
       rest = wave_sum(rest);
-      if (rest > 0.0) {      // (else nothing of the target is left beside the draft, and the distribution stays)
+      if (rest > kNothingLeft) {      // (else nothing of the target is left beside the draft, and the distribution stays)
         s.a += s.sum;
         s.sum = rest;
         s.level = j;
@@ -537,7 +549,7 @@ __global__ void __launch_bounds__(kVerThreads) verify_rest_kernel(const VerifyAr
 #pragma unroll
       for (int i = 0; i < kVerPieces; ++i)
 #pragma unroll
-        for (int e = 0; e < Chunk<T>::E; ++e) s += __builtin_fmax(__builtin_fma(wp.of(c.x[i][e]), scale_p, -__builtin_fma(wq.of(d.x[i][e]), scale_q, 1e-290)), 0.0);
+        for (int e = 0; e < Chunk<T>::E; ++e) s += left_of(wp.of(c.x[i][e]), scale_p, wq.of(d.x[i][e]), scale_q, 1e-290);
     } else {
 #pragma unroll
       for (int i = 0; i < kVerPieces; ++i)
@@ -549,7 +561,7 @@ __global__ void __launch_bounds__(kVerThreads) verify_rest_kernel(const VerifyAr
             x = e == j ? c.x[i][j] : x;
             y = e == j ? d.x[i][j] : y;
           }
-          s += __builtin_fmax(weight(number(x), p.top, by) * scale_p - weight(number(y), q.top, by) * scale_q, 0.0);
+          s += left_of(weight(number(x), p.top, by), scale_p, weight(number(y), q.top, by), scale_q, 0.0);
         }
     }
     __syncthreads();
@@ -739,14 +751,10 @@ __global__ void __launch_bounds__(kVerChooseThreads) verify_choose_kernel(const 
   double w[E], mine = 0.0;
   if (wp.plain && (scale_q == 0.0 || wq.plain)) {      // (1e-290 as in the sums of what is left)
 #pragma unroll
-    for (int e = 0; e < E; ++e)
-      w[e] = __builtin_fmax(__builtin_fma(wp.of(x[e]), scale_p, scale_q != 0.0 ? -__builtin_fma(wq.of(y[e]), scale_q, 1e-290) : -1e-290), 0.0);
+    for (int e = 0; e < E; ++e) w[e] = left_of(wp.of(x[e]), scale_p, scale_q != 0.0 ? wq.of(y[e]) : 0.0, scale_q, 1e-290);
   } else {
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      w[e] = weight(x[e], p.top, by) * scale_p;
-      if (scale_q != 0.0) w[e] = __builtin_fmax(w[e] - weight(y[e], q.top, by) * scale_q, 0.0);
-    }
+    for (int e = 0; e < E; ++e) w[e] = left_of(weight(x[e], p.top, by), scale_p, scale_q != 0.0 ? weight(y[e], q.top, by) : 0.0, scale_q, 0.0);
   }
   for (int j = 0; j < goners; ++j)
 #pragma unroll
