@@ -352,6 +352,9 @@ __device__ __forceinline__ double left_of(double weight_p, double scale_p, doubl
 // good to 1e-13 each (the rows may be cut into chunks at different words).
 constexpr double kNothingLeft = 4e-13;
 
+// Chunks of less than this are not drawn from.  A word's weight counts from 1e-290 of the whole on where it is drawn, and a chunk of 8192 words that comes to 1e-280 has one.
+constexpr double kLeastChunk = 1e-280;
+
 // What the tests of a row's children came to.
 struct RowState {
   int taken;        // the child that stands, or -1
@@ -434,7 +437,7 @@ __device__ RowState test_children(const VerifyArgs& g, const int32_t* parents, c
           s.taken = first + l;
           return s;
         }
-        if (1.0 - gone - have > 0.0) gone += have;
+        if (1.0 - gone - have > kNothingLeft) gone += have;
         ++s.refused;
         continue;
       }
@@ -666,7 +669,7 @@ __global__ void __launch_bounds__(kVerChooseThreads) verify_choose_kernel(const 
         const double pw = of_lane(have, l);
         bool before = false;
         for (int i = lane; i < n; i += 64) before = before || gone[i] == w;
-        if (__any(before) || !(left - pw > 0.0)) continue;
+        if (__any(before) || !(left - pw > kNothingLeft)) continue;
         left -= pw;
         if (lane == 0) {
           gone[n] = w;
@@ -677,14 +680,19 @@ __global__ void __launch_bounds__(kVerChooseThreads) verify_choose_kernel(const 
       }
     }
     // The weight of a chunk in what is left.  A sum less its refused parts is off by 1e-13 of them at most (Weigher; those that are the largest of their chunk are
-    // exact).  Where a share s of the whole is left, and the chance that it comes to that is s, this is 1e-13 / s of it: one draw in 10^13 goes elsewhere.
+    // exact).  Where a share s of the whole is left, and the chance that it comes to that is s, this is 1e-13 / s of it: one draw in 10^13 goes elsewhere.  A chunk in
+    // which that is all there is has nothing to draw.
     auto chunk_weight = [&](int i) {
-      if (s.level >= 0) return a.rest[(s.level * rows + row) * a.chunks + i];
+      if (s.level >= 0) {
+        const double w = a.rest[(s.level * rows + row) * a.chunks + i];
+        return w > kLeastChunk ? w : 0.0;
+      }
       const VerifyPart part = a.parts[row * a.chunks + i];
-      double w = part.sum * weight(part.top, p.top, by) / p.sum;
+      double w = part.sum * weight(part.top, p.top, by) / p.sum, refused = 0.0;
       for (int j = 0; j < n; ++j)
-        if ((gone[j] + lead) / Chunk<T>::kElements == i) w -= gone_weights[j];
-      return __builtin_fmax(w, 0.0);
+        if ((gone[j] + lead) / Chunk<T>::kElements == i) refused += gone_weights[j];
+      w -= refused;
+      return w > 2e-13 * refused && w > kLeastChunk ? w : 0.0;
     };
     const double first_weight = lane < a.chunks ? chunk_weight(lane) : 0.0;
     double whole = first_weight;
