@@ -166,23 +166,39 @@ def _need(ok, what):
         raise DpllmError(DPLLM_EINVAL, what)
 
 
+def _on(t, what):
+    """Whether t is on the device.  On another one than the current it is refused: the call would run on the current device's stream."""
+    if not t.is_cuda:
+        return False
+    _need(t.get_device() == torch._C._cuda_getDevice(), "%s is on device %d, which is not the current one" % (what, t.get_device()))
+    return True
+
+
 def _dtype(t, what):
-    _need(t.dtype in _DTYPES and t.is_cuda, what + " has to be a device tensor of float16, bfloat16 or float32")
+    _need(t.dtype in _DTYPES and _on(t, what), what + " has to be a device tensor of float16, bfloat16 or float32")
     return _DTYPES[t.dtype]
+
+
+def _space(t):
+    """The pointer and bytes of a caller's workspace (or of none)."""
+    if t is None:
+        return None, 0
+    _need(_on(t, "the workspace") and t.is_contiguous(), "the workspace has to be a contiguous device tensor")
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
 def _index(t, shape, what):
     """The pointer of a contiguous int32 device tensor of this shape (None: not given)."""
     if t is None:
         return None
-    _need(t.dtype == torch.int32 and t.is_cuda and tuple(t.shape) == tuple(shape) and t.is_contiguous(),
+    _need(t.dtype == torch.int32 and _on(t, what) and tuple(t.shape) == tuple(shape) and t.is_contiguous(),
           "%s has to be a contiguous int32 device tensor %s" % (what, list(shape)))
     return t.data_ptr()
 
 
 def _view(t, what):
     """dpllm_heads of a tensor [batch][tokens][heads][head_dim] (or of one layer of such)."""
-    _need(t.dim() == 4 and t.is_cuda, what + " has to be a device tensor [batch][tokens][heads][head_dim]")
+    _need(t.dim() == 4 and _on(t, what), what + " has to be a device tensor [batch][tokens][heads][head_dim]")
     b, n, h, d = t.stride()
     _need(d == 1 or t.shape[3] == 1 or t.numel() == 0, "the last dimension of %s has to be contiguous" % what)
     return _Heads(t.data_ptr(), b, n, h)
@@ -216,7 +232,7 @@ def dpllm_rope(x, positions, freqs, out=None, scale=1.0, layout=DPLLM_ROPE_HALF,
     for t, o in zip(xs, outs):
         _need(t.dtype == o.dtype == first.dtype and t.shape == o.shape and t.shape[:2] == (b, n) and t.shape[3] == d,
               "the tensors of dpllm_rope share type, sequences, tokens and head_dim, and out the shapes of x")
-    _need(freqs.dtype == torch.float64 and freqs.is_cuda and freqs.is_contiguous() and freqs.dim() == 1, "freqs has to be a contiguous float64 device vector")
+    _need(freqs.dtype == torch.float64 and _on(freqs, "freqs") and freqs.is_contiguous() and freqs.dim() == 1, "freqs has to be a contiguous float64 device vector")
     pos = _index(positions, (n,) if positions.dim() == 1 else (b, n), "positions")
     m = len(xs)
     _call(lib.dpllm_rope((_Heads * m)(*views), (_Heads * m)(*into), (C.c_int * m)(*[t.shape[2] for t in xs]), m, b, n, d, dtype, 2 * freqs.shape[0],
@@ -230,20 +246,21 @@ class Cache:
     table sequence b has page b.  The table may change on the device at any time; the object holds the tensors alive."""
 
     def __init__(self, k, v, table=None):
-        _need(k.dim() == 5 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype and k.is_cuda and v.is_cuda,
-              "k and v have to be device tensors [layers][pages][page][heads][head_dim] of one type, shape and strides")
-        dtype = _dtype(k, "k")
+        _need(k.dim() == 5 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype and k.is_cuda and v.is_cuda and
+              k.get_device() == v.get_device(),
+              "k and v have to be device tensors [layers][pages][page][heads][head_dim] of one type, shape, strides and device")
+        _need(k.dtype in _DTYPES, "k and v have to be float16, bfloat16 or float32")
         _need(k.stride(4) == 1 or k.shape[4] == 1, "the last dimension of k and v has to be contiguous")
         if table is not None:
-            _need(table.dtype == torch.int32 and table.is_cuda and table.dim() == 2 and (table.stride(1) == 1 or table.shape[1] == 1),
-                  "table has to be an int32 device tensor [batch][pages per sequence]")
-        self.k, self.v, self.table = k, v, table
+            _need(table.dtype == torch.int32 and table.is_cuda and table.get_device() == k.get_device() and table.dim() == 2 and
+                  (table.stride(1) == 1 or table.shape[1] == 1), "table has to be an int32 tensor [batch][pages per sequence] on the device of k and v")
+        self.k, self.v, self.table, self.device = k, v, table, k.get_device()
         self.layers, self.pages, self.page, self.heads, self.head_dim = k.shape
         self.pages_per_seq = 1 if table is None else table.shape[1]
         self.batch = self.pages if table is None else table.shape[0]
         self.capacity = self.pages_per_seq * self.page
         self.c = _Cache(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), k.stride(3), _ptr(table), 0 if table is None else table.stride(0),
-                        dtype, self.layers, self.pages, self.page, self.pages_per_seq, self.heads, self.head_dim)
+                        _DTYPES[k.dtype], self.layers, self.pages, self.page, self.pages_per_seq, self.heads, self.head_dim)
         self.address = C.addressof(self.c)
 
 
@@ -262,6 +279,7 @@ def dpllm_tree_attention(cache, layer, lens, q, k_new=None, v_new=None, mask=Non
         return made
     if made != _calls.ELSEWHERE:
         _call(made)
+    _on(cache.k, "the cache")
     _need(q.dim() == 4 and q.dtype == cache.k.dtype and q.shape[3] == cache.head_dim, "q has to be [batch][nodes][heads][head_dim] of the cache's type and head_dim")
     b, n, h, d = q.shape
     _need(b <= cache.batch, "q has more sequences than the cache")
@@ -274,9 +292,9 @@ def dpllm_tree_attention(cache, layer, lens, q, k_new=None, v_new=None, mask=Non
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     _need(out.shape == q.shape and out.dtype == q.dtype, "out has to have the shape and type of q")
     if mask is not None:
-        _need(mask.dtype == torch.int64 and mask.is_cuda and mask.is_contiguous() and mask.dim() == 3 and mask.shape[0] in (1, b) and
+        _need(mask.dtype == torch.int64 and _on(mask, "mask") and mask.is_contiguous() and mask.dim() == 3 and mask.shape[0] in (1, b) and
               mask.shape[1:] == (n, (n + 63) // 64), "mask has to be a contiguous int64 device tensor [batch or 1][nodes][ceil(nodes / 64)]")
-    _need(lse is None or (lse.dtype == torch.float32 and lse.is_cuda and lse.shape == (b, n, h) and lse.is_contiguous()),
+    _need(lse is None or (lse.dtype == torch.float32 and _on(lse, "lse") and lse.shape == (b, n, h) and lse.is_contiguous()),
           "lse has to be a contiguous float32 device tensor [batch][nodes][heads]")
     max_len = cache.capacity if max_len is None else min(max_len, cache.capacity)
     if workspace is None:
@@ -285,8 +303,7 @@ def dpllm_tree_attention(cache, layer, lens, q, k_new=None, v_new=None, mask=Non
     _call(lib.dpllm_tree_attention(C.byref(cache.c), layer, b, n, h, _index(lens, (b,), "lens"), max_len, C.byref(_view(q, "q")),
                                    None if k_new is None else C.byref(_view(k_new, "k_new")), None if v_new is None else C.byref(_view(v_new, "v_new")),
                                    _ptr(mask), 0 if mask is None or mask.shape[0] == 1 else mask.stride(0), d ** -0.5 if scale is None else scale,
-                                   C.byref(_view(out, "out")), _ptr(lse), _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
-                                   _stream()))
+                                   C.byref(_view(out, "out")), _ptr(lse), *_space(workspace), _stream()))
     return out
 
 
@@ -311,10 +328,10 @@ def dpllm_verify(logits, tokens, uniforms, temperature, parents=None, draft=None
     _need(logits.dim() == 3 and (logits.stride(2) == 1 or logits.shape[2] == 1 or logits.numel() == 0), "logits has to be [batch][nodes][vocabulary], the words contiguous")
     b, n, v = logits.shape
     if draft is not None:
-        _need(draft.shape == logits.shape and draft.dtype == logits.dtype and draft.is_cuda and (draft.stride(2) == 1 or v == 1 or draft.numel() == 0),
-              "draft has to have the shape and type of logits, the words contiguous")
+        _need(draft.shape == logits.shape and draft.dtype == logits.dtype and _on(draft, "draft") and (draft.stride(2) == 1 or v == 1 or draft.numel() == 0),
+              "draft has to be a device tensor of the shape and type of logits, the words contiguous")
     for t, shape, what in ((uniforms, (b, n), "uniforms"), (temperature, (b,), "temperature")):
-        _need(t.dtype == torch.float32 and t.is_cuda and tuple(t.shape) == shape and t.is_contiguous(), "%s has to be a contiguous float32 device tensor %s" % (what, list(shape)))
+        _need(t.dtype == torch.float32 and _on(t, what) and tuple(t.shape) == shape and t.is_contiguous(), "%s has to be a contiguous float32 device tensor %s" % (what, list(shape)))
     if siblings is None:
         siblings = 1 if parents is None else max(1, n - 1)
     count = torch.empty(b, dtype=torch.int32, device="cuda") if count is None else count
@@ -324,8 +341,7 @@ def dpllm_verify(logits, tokens, uniforms, temperature, parents=None, draft=None
         workspace = torch.empty(dpllm_verify_workspace_bytes(b, n, v, dtype, draft is not None, siblings), dtype=torch.uint8, device="cuda")
     _call(lib.dpllm_verify(b, n, v, dtype, _ptr(logits), logits.stride(0), logits.stride(1), _ptr(draft), 0 if draft is None else draft.stride(0),
                            0 if draft is None else draft.stride(1), _index(tokens, (b, n), "tokens"), _index(parents, (b, n), "parents"), _ptr(uniforms), _ptr(temperature),
-                           siblings, _index(count, (b,), "count"), _index(path, (b, n), "path"), _index(words, (b, n), "words"), _ptr(workspace),
-                           workspace.numel() * workspace.element_size(), _stream()))
+                           siblings, _index(count, (b,), "count"), _index(path, (b, n), "path"), _index(words, (b, n), "words"), *_space(workspace), _stream()))
     return count, path, words
 
 
@@ -335,13 +351,14 @@ def dpllm_cache_append(cache, lens, k_new, v_new, path=None, count=None, layer=0
     made = _calls.append(cache, lens, k_new, v_new, path, count, layer)
     if made != _calls.ELSEWHERE:
         return _call(made)
+    _on(cache.k, "the cache")
     if k_new.dim() == 4:
         k_new, v_new = k_new.unsqueeze(0), v_new.unsqueeze(0)
     _need(k_new.dim() == 5 and k_new.shape == v_new.shape and k_new.dtype == v_new.dtype == cache.k.dtype,
           "k_new and v_new have to be [layers][batch][nodes][heads][head_dim] of the cache's type")
     layers, b, n, h, d = k_new.shape
     _need((h, d) == (cache.heads, cache.head_dim) and b <= cache.batch, "k_new and v_new have to fit the cache's heads, head_dim and sequences")
-    _need(layers == 0 or (k_new[0].is_cuda and v_new[0].is_cuda), "k_new and v_new have to be device tensors")
+    _need(layers == 0 or (_on(k_new, "k_new") and _on(v_new, "v_new")), "k_new and v_new have to be device tensors")
     if layers == 0:
         return
     _call(lib.dpllm_cache_append(C.byref(cache.c), layer, layers, b, n, _index(lens, (b,), "lens"), C.byref(_view(k_new[0], "k_new")), k_new.stride(0),

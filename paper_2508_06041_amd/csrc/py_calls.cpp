@@ -44,11 +44,11 @@ bool address(PyObject* o, void** p) {
 
 bool tensor(PyObject* o, void** p) { return !PyLong_Check(o) && address(o, p); }
 
-// the current stream of the current device
-bool stream(void** p) {
+// the current stream of the current device, and that device
+bool stream(void** p, int* device = nullptr) {
   PyObject* d = PyObject_CallNoArgs(get_device);
   PyObject* s = d != nullptr ? PyObject_CallOneArg(get_stream, d) : nullptr;
-  const bool ok = s != nullptr && PyLong_Check(s);
+  const bool ok = s != nullptr && PyLong_Check(s) && (device == nullptr || as_int(d, device));
   if (ok) *p = PyLong_AsVoidPtr(s);
   Py_XDECREF(d);
   Py_XDECREF(s);
@@ -129,7 +129,7 @@ struct TokenCalls {
 // torch.float16, bfloat16, float32, int32, int64, float64, and torch.empty_like
 PyObject *dtypes[6] = {}, *empty_like = nullptr;
 enum { kInt32 = 3, kInt64 = 4, kFloat64 = 5 };
-PyObject *s_dtype = nullptr, *s_shape = nullptr, *s_stride = nullptr, *s_is_cuda = nullptr, *s_address = nullptr, *s_batch = nullptr, *s_new_empty = nullptr;
+PyObject *s_dtype = nullptr, *s_shape = nullptr, *s_stride = nullptr, *s_get_device = nullptr, *s_address = nullptr, *s_batch = nullptr, *s_device = nullptr, *s_new_empty = nullptr;
 
 // A reference that is given back.
 struct Ref {
@@ -162,15 +162,23 @@ struct Tensor {
   }
 };
 
-// What there is to know of a device tensor that is not empty; false: something is out of the ordinary.
-bool look(PyObject* o, Tensor* t) {
+// What a call is made on: the current device and its stream.
+struct Place {
+  void* stream;
+  int device;
+  bool find() { return ::stream(&stream, &device); }
+};
+
+// What there is to know of a tensor on the current device that is not empty; false: something is out of the ordinary.
+bool look(PyObject* o, const Place& at, Tensor* t) {
   const Ref type(PyObject_GetAttr(o, s_dtype));
   t->dtype = -1;
   for (int i = 0; i < 6; ++i)
     if (type.o != nullptr && type.o == dtypes[i]) t->dtype = i;
   if (t->dtype < 0) return false;
-  const Ref cuda(PyObject_GetAttr(o, s_is_cuda)), shape(PyObject_GetAttr(o, s_shape)), stride(PyObject_CallMethodNoArgs(o, s_stride));
-  if (cuda.o != Py_True || shape.o == nullptr || stride.o == nullptr || !PyTuple_Check(shape.o) || !PyTuple_Check(stride.o)) return false;
+  const Ref device(PyObject_CallMethodNoArgs(o, s_get_device)), shape(PyObject_GetAttr(o, s_shape)), stride(PyObject_CallMethodNoArgs(o, s_stride));
+  int index = -1;
+  if (device.o == nullptr || !as_int(device.o, &index) || index != at.device || shape.o == nullptr || stride.o == nullptr || !PyTuple_Check(shape.o) || !PyTuple_Check(stride.o)) return false;
   t->dim = (int)PyTuple_GET_SIZE(shape.o);
   if (t->dim > kMaxDim || PyTuple_GET_SIZE(stride.o) != t->dim) return false;
   t->count = 1;
@@ -193,17 +201,17 @@ bool look_new(PyObject* o, const Tensor& like, Tensor* t) {
 }
 
 // A dense tensor of this type and shape (the first dims of a, b, c).
-bool look_dense(PyObject* o, int dtype, int dims, int64_t a, int64_t b, int64_t c, void** p) {
+bool look_dense(PyObject* o, const Place& at, int dtype, int dims, int64_t a, int64_t b, int64_t c, void** p) {
   Tensor t;
-  if (!look(o, &t) || !t.is(dtype, dims) || !t.dense(dims)) return false;
+  if (!look(o, at, &t) || !t.is(dtype, dims) || !t.dense(dims)) return false;
   if (t.size[0] != a || (dims > 1 && t.size[1] != b) || (dims > 2 && t.size[2] != c)) return false;
   *p = t.data;
   return true;
 }
 // the same, or None
-bool look_dense_or_none(PyObject* o, int dtype, int dims, int64_t a, int64_t b, int64_t c, void** p) {
+bool look_dense_or_none(PyObject* o, const Place& at, int dtype, int dims, int64_t a, int64_t b, int64_t c, void** p) {
   *p = nullptr;
-  return o == Py_None || look_dense(o, dtype, dims, a, b, c, p);
+  return o == Py_None || look_dense(o, at, dtype, dims, a, b, c, p);
 }
 
 // [batch][tokens][heads][head_dim], the last without gaps
@@ -259,16 +267,16 @@ PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
   dpllm_heads in[DPLLM_MAX_TENSORS], out[DPLLM_MAX_TENSORS];
   int heads[DPLLM_MAX_TENSORS], layout = 0;
   float scale = 0.f;
-  void* s = nullptr;
+  Place place;
   const int inverse = PyObject_IsTrue(a[6]);
-  if (!look(a[1], &pos) || pos.dtype != kInt32 || pos.dim < 1 || pos.dim > 2 || !pos.dense(pos.dim) || !look(a[2], &freqs) || !freqs.is(kFloat64, 1) ||
-      !freqs.dense(1) || freqs.size[0] > DPLLM_MAX_HEAD_DIM || !as_float(a[4], &scale) || !as_int(a[5], &layout) || inverse < 0 || !stream(&s))
+  if (!place.find() || !look(a[1], place, &pos) || pos.dtype != kInt32 || pos.dim < 1 || pos.dim > 2 || !pos.dense(pos.dim) || !look(a[2], place, &freqs) || !freqs.is(kFloat64, 1) ||
+      !freqs.dense(1) || freqs.size[0] > DPLLM_MAX_HEAD_DIM || !as_float(a[4], &scale) || !as_int(a[5], &layout) || inverse < 0)
     return elsewhere();
   const Ref results(PyTuple_New(m));
   if (results.o == nullptr) return elsewhere();
   for (int i = 0; i < m; ++i) {
     const Ref t(item(a[0], i));
-    if (!look(t.o, &x[i]) || x[i].dtype > 2 || !heads_of(x[i], &in[i]) || x[i].dtype != x[0].dtype || x[i].size[0] != x[0].size[0] ||
+    if (!look(t.o, place, &x[i]) || x[i].dtype > 2 || !heads_of(x[i], &in[i]) || x[i].dtype != x[0].dtype || x[i].size[0] != x[0].size[0] ||
         x[i].size[1] != x[0].size[1] || x[i].size[3] != x[0].size[3])
       return elsewhere();
     heads[i] = (int)x[i].size[2];
@@ -276,21 +284,24 @@ PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (o == nullptr) return elsewhere();
     PyTuple_SET_ITEM(results.o, i, o);
     Tensor y;
-    if (!(a[3] == Py_None ? look_new(o, x[i], &y) : look(o, &y)) || y.dtype != x[0].dtype || !heads_of(y, &out[i])) return elsewhere();
+    if (!(a[3] == Py_None ? look_new(o, x[i], &y) : look(o, place, &y)) || y.dtype != x[0].dtype || !heads_of(y, &out[i])) return elsewhere();
     for (int j = 0; j < 4; ++j)
       if (y.size[j] != x[i].size[j]) return elsewhere();
   }
   if (pos.size[pos.dim - 1] != x[0].size[1] || (pos.dim == 2 && pos.size[0] != x[0].size[0])) return elsewhere();
   const int rc = to.rope(in, out, heads, m, (int)x[0].size[0], (int)x[0].size[1], (int)x[0].size[3], x[0].dtype, (int)(2 * freqs.size[0]), layout,
-                         static_cast<const double*>(freqs.data), scale, static_cast<const int32_t*>(pos.data), pos.dim == 1 ? 0 : x[0].size[1], inverse, s);
+                         static_cast<const double*>(freqs.data), scale, static_cast<const int32_t*>(pos.data), pos.dim == 1 ? 0 : x[0].size[1], inverse, place.stream);
   return answer(rc, PyTuple_Check(a[0]) ? Py_NewRef(results.o) : item(results.o, 0));
 }
 
-// The dpllm_cache of a Cache object, and its sequences.
-bool cache_of(PyObject* o, const dpllm_cache** c, int* batch) {
-  const Ref at(PyObject_GetAttr(o, s_address)), b(PyObject_GetAttr(o, s_batch));
+// The dpllm_cache of a Cache object on the current device, and its sequences.
+bool cache_of(PyObject* o, const Place& place, const dpllm_cache** c, int* batch) {
+  const Ref at(PyObject_GetAttr(o, s_address)), b(PyObject_GetAttr(o, s_batch)), device(PyObject_GetAttr(o, s_device));
   void* p = nullptr;
-  if (at.o == nullptr || b.o == nullptr || !PyLong_Check(at.o) || !address(at.o, &p) || p == nullptr || !as_int(b.o, batch)) return false;
+  int index = -1;
+  if (at.o == nullptr || b.o == nullptr || device.o == nullptr || !PyLong_Check(at.o) || !address(at.o, &p) || p == nullptr || !as_int(b.o, batch) ||
+      !as_int(device.o, &index) || index != place.device)
+    return false;
   *c = static_cast<const dpllm_cache*>(p);
   return true;
 }
@@ -313,19 +324,20 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Tensor q, k{}, v{}, m{}, y;
   dpllm_heads hq, hk{}, hv{}, ho;
   float scale = 0.f;
-  void *lens = nullptr, *lse = nullptr, *s = nullptr, *ws = nullptr;
+  void *lens = nullptr, *lse = nullptr, *ws = nullptr;
+  Place place;
   size_t bytes = 0;
-  if (n != 12 || to.attention == nullptr || !cache_of(a[0], &c, &sequences) || !as_int(a[1], &layer) || !look(a[3], &q) || q.dtype != c->dtype || !heads_of(q, &hq) ||
-      q.size[3] != c->head_dim || q.size[0] > sequences || !look_dense(a[2], kInt32, 1, q.size[0], 0, 0, &lens) || (a[4] == Py_None) != (a[5] == Py_None) ||
-      !look_dense_or_none(a[9], 2, 3, q.size[0], q.size[1], q.size[2], &lse) || !stream(&s))
+  if (n != 12 || to.attention == nullptr || !place.find() || !cache_of(a[0], place, &c, &sequences) || !as_int(a[1], &layer) || !look(a[3], place, &q) || q.dtype != c->dtype || !heads_of(q, &hq) ||
+      q.size[3] != c->head_dim || q.size[0] > sequences || !look_dense(a[2], place, kInt32, 1, q.size[0], 0, 0, &lens) || (a[4] == Py_None) != (a[5] == Py_None) ||
+      !look_dense_or_none(a[9], place, 2, 3, q.size[0], q.size[1], q.size[2], &lse))
     return elsewhere();
   const int64_t b = q.size[0], t = q.size[1];
   if (a[4] != Py_None) {
-    if (!look(a[4], &k) || !look(a[5], &v) || !heads_of(k, &hk) || !heads_of(v, &hv)) return elsewhere();
+    if (!look(a[4], place, &k) || !look(a[5], place, &v) || !heads_of(k, &hk) || !heads_of(v, &hv)) return elsewhere();
     for (const Tensor* x : {&k, &v})
       if (x->dtype != q.dtype || x->size[0] != b || x->size[1] != t || x->size[2] != c->heads || x->size[3] != q.size[3]) return elsewhere();
   }
-  if (a[6] != Py_None && (!look(a[6], &m) || !m.is(kInt64, 3) || !m.dense(3) || (m.size[0] != 1 && m.size[0] != b) || m.size[1] != t || m.size[2] != (t + 63) / 64))
+  if (a[6] != Py_None && (!look(a[6], place, &m) || !m.is(kInt64, 3) || !m.dense(3) || (m.size[0] != 1 && m.size[0] != b) || m.size[1] != t || m.size[2] != (t + 63) / 64))
     return elsewhere();
   const int64_t capacity = (int64_t)c->pages_per_seq * c->page;
   if (a[10] == Py_None ? (max_len = capacity > INT32_MAX ? INT32_MAX : (int)capacity, false) : !as_int(a[10], &max_len)) return elsewhere();
@@ -333,30 +345,31 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (a[7] == Py_None ? (scale = (float)(1.0 / __builtin_sqrt((double)q.size[3])), false) : !as_float(a[7], &scale)) return elsewhere();
   if (to.attention_bytes((int)b, (int)t, (int)q.size[2], c->heads, (int)q.size[3], max_len, &bytes) != DPLLM_OK) return elsewhere();
   const Ref result(a[8] == Py_None ? PyObject_CallOneArg(empty_like, a[3]) : Py_NewRef(a[8]));
-  if (result.o == nullptr || !(a[8] == Py_None ? look_new(result.o, q, &y) : look(result.o, &y)) || y.dtype != q.dtype || !heads_of(y, &ho)) return elsewhere();
+  if (result.o == nullptr || !(a[8] == Py_None ? look_new(result.o, q, &y) : look(result.o, place, &y)) || y.dtype != q.dtype || !heads_of(y, &ho)) return elsewhere();
   for (int j = 0; j < 4; ++j)
     if (y.size[j] != q.size[j]) return elsewhere();
   const Ref held(a[11] == Py_None ? space(a[3], 2, bytes, &ws) : nullptr);
   if (held.o == nullptr) return elsewhere();
   const int rc = to.attention(c, layer, (int)b, (int)t, (int)q.size[2], static_cast<const int32_t*>(lens), max_len, &hq, a[4] == Py_None ? nullptr : &hk,
                               a[5] == Py_None ? nullptr : &hv, static_cast<const uint64_t*>(m.data), a[6] == Py_None || m.size[0] == 1 ? 0 : m.size[1] * m.size[2],
-                              scale, &ho, static_cast<float*>(lse), ws, bytes, s);
+                              scale, &ho, static_cast<float*>(lse), ws, bytes, place.stream);
   return answer(rc, Py_NewRef(result.o));
 }
 
 // verify(logits, tokens, uniforms, temperature, parents, draft, siblings), outputs and workspace new
 PyObject* verify(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Tensor x, d{};
-  void *tokens = nullptr, *parents = nullptr, *uniforms = nullptr, *temperature = nullptr, *s = nullptr, *ws = nullptr, *out[3] = {};
+  void *tokens = nullptr, *parents = nullptr, *uniforms = nullptr, *temperature = nullptr, *ws = nullptr, *out[3] = {};
+  Place place;
   int siblings = 0;
   size_t bytes = 0;
-  if (n != 7 || to.verify == nullptr || !look(a[0], &x) || x.dtype > 2 || x.dim != 3 || (x.stride[2] != 1 && x.size[2] != 1) ||
-      !look_dense(a[1], kInt32, 2, x.size[0], x.size[1], 0, &tokens) || !look_dense(a[2], 2, 2, x.size[0], x.size[1], 0, &uniforms) ||
-      !look_dense(a[3], 2, 1, x.size[0], 0, 0, &temperature) || !look_dense_or_none(a[4], kInt32, 2, x.size[0], x.size[1], 0, &parents) ||
-      !as_int(a[6], &siblings) || !stream(&s))
+  if (n != 7 || to.verify == nullptr || !place.find() || !look(a[0], place, &x) || x.dtype > 2 || x.dim != 3 || (x.stride[2] != 1 && x.size[2] != 1) ||
+      !look_dense(a[1], place, kInt32, 2, x.size[0], x.size[1], 0, &tokens) || !look_dense(a[2], place, 2, 2, x.size[0], x.size[1], 0, &uniforms) ||
+      !look_dense(a[3], place, 2, 1, x.size[0], 0, 0, &temperature) || !look_dense_or_none(a[4], place, kInt32, 2, x.size[0], x.size[1], 0, &parents) ||
+      !as_int(a[6], &siblings))
     return elsewhere();
   if (a[5] != Py_None) {
-    if (!look(a[5], &d) || d.dtype != x.dtype || d.dim != 3 || (d.stride[2] != 1 && d.size[2] != 1)) return elsewhere();
+    if (!look(a[5], place, &d) || d.dtype != x.dtype || d.dim != 3 || (d.stride[2] != 1 && d.size[2] != 1)) return elsewhere();
     for (int i = 0; i < 3; ++i)
       if (d.size[i] != x.size[i]) return elsewhere();
   }
@@ -374,7 +387,7 @@ PyObject* verify(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const int rc = to.verify((int)x.size[0], (int)x.size[1], (int)x.size[2], x.dtype, x.data, x.stride[0], x.stride[1], d.data, d.stride[0], d.stride[1],
                            static_cast<const int32_t*>(tokens), static_cast<const int32_t*>(parents), static_cast<const float*>(uniforms),
                            static_cast<const float*>(temperature), siblings, static_cast<int32_t*>(out[0]), static_cast<int32_t*>(out[1]),
-                           static_cast<int32_t*>(out[2]), ws, bytes, s);
+                           static_cast<int32_t*>(out[2]), ws, bytes, place.stream);
   return answer(rc, Py_NewRef(results.o));
 }
 
@@ -383,9 +396,10 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const dpllm_cache* c = nullptr;
   int sequences = 0, layer = 0;
   Tensor k, v;
-  void *lens = nullptr, *path = nullptr, *count = nullptr, *s = nullptr;
-  if (n != 7 || to.append == nullptr || !cache_of(a[0], &c, &sequences) || !look(a[2], &k) || !look(a[3], &v) || k.dtype != c->dtype || v.dtype != c->dtype ||
-      k.dim != v.dim || k.dim < 4 || !as_int(a[6], &layer) || !stream(&s))
+  void *lens = nullptr, *path = nullptr, *count = nullptr;
+  Place place;
+  if (n != 7 || to.append == nullptr || !place.find() || !cache_of(a[0], place, &c, &sequences) || !look(a[2], place, &k) || !look(a[3], place, &v) || k.dtype != c->dtype || v.dtype != c->dtype ||
+      k.dim != v.dim || k.dim < 4 || !as_int(a[6], &layer))
     return elsewhere();
   const int at = k.dim - 4;
   for (int i = 0; i < k.dim; ++i)
@@ -393,12 +407,12 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const int64_t b = k.size[at], t = k.size[at + 1];
   for (const Tensor* x : {&k, &v})
     if (x->stride[at + 3] != 1 && x->size[at + 3] != 1) return elsewhere();
-  if (k.size[at + 2] != c->heads || k.size[at + 3] != c->head_dim || b > sequences || !look_dense(a[1], kInt32, 1, b, 0, 0, &lens) ||
-      !look_dense_or_none(a[4], kInt32, 2, b, t, 0, &path) || !look_dense_or_none(a[5], kInt32, 1, b, 0, 0, &count))
+  if (k.size[at + 2] != c->heads || k.size[at + 3] != c->head_dim || b > sequences || !look_dense(a[1], place, kInt32, 1, b, 0, 0, &lens) ||
+      !look_dense_or_none(a[4], place, kInt32, 2, b, t, 0, &path) || !look_dense_or_none(a[5], place, kInt32, 1, b, 0, 0, &count))
     return elsewhere();
   const dpllm_heads hk{k.data, k.stride[at], k.stride[at + 1], k.stride[at + 2]}, hv{v.data, v.stride[at], v.stride[at + 1], v.stride[at + 2]};
   const int rc = to.append(c, layer, at ? (int)k.size[0] : 1, (int)b, (int)t, static_cast<const int32_t*>(lens), &hk, at ? k.stride[0] : 0, &hv,
-                           at ? v.stride[0] : 0, static_cast<const int32_t*>(path), t, static_cast<const int32_t*>(count), s);
+                           at ? v.stride[0] : 0, static_cast<const int32_t*>(path), t, static_cast<const int32_t*>(count), place.stream);
   return PyLong_FromLong(rc);
 }
 
@@ -425,11 +439,12 @@ PyMODINIT_FUNC PyInit__calls() {
   s_dtype = PyUnicode_InternFromString("dtype");
   s_shape = PyUnicode_InternFromString("shape");
   s_stride = PyUnicode_InternFromString("stride");
-  s_is_cuda = PyUnicode_InternFromString("is_cuda");
+  s_get_device = PyUnicode_InternFromString("get_device");
   s_address = PyUnicode_InternFromString("address");
   s_batch = PyUnicode_InternFromString("batch");
+  s_device = PyUnicode_InternFromString("device");
   s_new_empty = PyUnicode_InternFromString("new_empty");
-  for (PyObject* s : {s_dtype, s_shape, s_stride, s_is_cuda, s_address, s_batch, s_new_empty})
+  for (PyObject* s : {s_dtype, s_shape, s_stride, s_get_device, s_address, s_batch, s_device, s_new_empty})
     if (s == nullptr) return nullptr;
   if (s_data_ptr == nullptr || s_dim == nullptr || s_size == nullptr || zero == nullptr) return nullptr;
   PyObject* m = PyModule_Create(&definition);
