@@ -258,6 +258,16 @@ PyObject* answer(int rc, PyObject* result) {
   return PyLong_FromLong(rc);
 }
 
+// A launch may wait for room in the queue: other threads of Python go on meanwhile, as with dpllm_gemv.
+template <typename F>
+int unlocked(F call) {
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = call();
+  Py_END_ALLOW_THREADS
+  return rc;
+}
+
 // rope(x, positions, freqs, out, scale, layout, inverse)
 PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const int m = n == 7 && PyTuple_Check(a[0]) ? (int)PyTuple_GET_SIZE(a[0]) : 1;
@@ -289,8 +299,10 @@ PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
       if (y.size[j] != x[i].size[j]) return elsewhere();
   }
   if (pos.size[pos.dim - 1] != x[0].size[1] || (pos.dim == 2 && pos.size[0] != x[0].size[0])) return elsewhere();
-  const int rc = to.rope(in, out, heads, m, (int)x[0].size[0], (int)x[0].size[1], (int)x[0].size[3], x[0].dtype, (int)(2 * freqs.size[0]), layout,
-                         static_cast<const double*>(freqs.data), scale, static_cast<const int32_t*>(pos.data), pos.dim == 1 ? 0 : x[0].size[1], inverse, place.stream);
+  const int rc = unlocked([&] {
+    return to.rope(in, out, heads, m, (int)x[0].size[0], (int)x[0].size[1], (int)x[0].size[3], x[0].dtype, (int)(2 * freqs.size[0]), layout,
+                   static_cast<const double*>(freqs.data), scale, static_cast<const int32_t*>(pos.data), pos.dim == 1 ? 0 : x[0].size[1], inverse, place.stream);
+  });
   return answer(rc, PyTuple_Check(a[0]) ? Py_NewRef(results.o) : item(results.o, 0));
 }
 
@@ -350,9 +362,11 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (y.size[j] != q.size[j]) return elsewhere();
   const Ref held(a[11] == Py_None ? space(a[3], 2, bytes, &ws) : nullptr);
   if (held.o == nullptr) return elsewhere();
-  const int rc = to.attention(c, layer, (int)b, (int)t, (int)q.size[2], static_cast<const int32_t*>(lens), max_len, &hq, a[4] == Py_None ? nullptr : &hk,
-                              a[5] == Py_None ? nullptr : &hv, static_cast<const uint64_t*>(m.data), a[6] == Py_None || m.size[0] == 1 ? 0 : m.size[1] * m.size[2],
-                              scale, &ho, static_cast<float*>(lse), ws, bytes, place.stream);
+  const int rc = unlocked([&] {
+    return to.attention(c, layer, (int)b, (int)t, (int)q.size[2], static_cast<const int32_t*>(lens), max_len, &hq, a[4] == Py_None ? nullptr : &hk,
+                        a[5] == Py_None ? nullptr : &hv, static_cast<const uint64_t*>(m.data), a[6] == Py_None || m.size[0] == 1 ? 0 : m.size[1] * m.size[2],
+                        scale, &ho, static_cast<float*>(lse), ws, bytes, place.stream);
+  });
   return answer(rc, Py_NewRef(result.o));
 }
 
@@ -384,10 +398,12 @@ PyObject* verify(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
   const Ref held(space(a[1], 4, bytes, &ws));
   if (held.o == nullptr) return elsewhere();
-  const int rc = to.verify((int)x.size[0], (int)x.size[1], (int)x.size[2], x.dtype, x.data, x.stride[0], x.stride[1], d.data, d.stride[0], d.stride[1],
-                           static_cast<const int32_t*>(tokens), static_cast<const int32_t*>(parents), static_cast<const float*>(uniforms),
-                           static_cast<const float*>(temperature), siblings, static_cast<int32_t*>(out[0]), static_cast<int32_t*>(out[1]),
-                           static_cast<int32_t*>(out[2]), ws, bytes, place.stream);
+  const int rc = unlocked([&] {
+    return to.verify((int)x.size[0], (int)x.size[1], (int)x.size[2], x.dtype, x.data, x.stride[0], x.stride[1], d.data, d.stride[0], d.stride[1],
+                     static_cast<const int32_t*>(tokens), static_cast<const int32_t*>(parents), static_cast<const float*>(uniforms),
+                     static_cast<const float*>(temperature), siblings, static_cast<int32_t*>(out[0]), static_cast<int32_t*>(out[1]),
+                     static_cast<int32_t*>(out[2]), ws, bytes, place.stream);
+  });
   return answer(rc, Py_NewRef(results.o));
 }
 
@@ -411,8 +427,10 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
       !look_dense_or_none(a[4], place, kInt32, 2, b, t, 0, &path) || !look_dense_or_none(a[5], place, kInt32, 1, b, 0, 0, &count))
     return elsewhere();
   const dpllm_heads hk{k.data, k.stride[at], k.stride[at + 1], k.stride[at + 2]}, hv{v.data, v.stride[at], v.stride[at + 1], v.stride[at + 2]};
-  const int rc = to.append(c, layer, at ? (int)k.size[0] : 1, (int)b, (int)t, static_cast<const int32_t*>(lens), &hk, at ? k.stride[0] : 0, &hv,
-                           at ? v.stride[0] : 0, static_cast<const int32_t*>(path), t, static_cast<const int32_t*>(count), place.stream);
+  const int rc = unlocked([&] {
+    return to.append(c, layer, at ? (int)k.size[0] : 1, (int)b, (int)t, static_cast<const int32_t*>(lens), &hk, at ? k.stride[0] : 0, &hv,
+                     at ? v.stride[0] : 0, static_cast<const int32_t*>(path), t, static_cast<const int32_t*>(count), place.stream);
+  });
   return PyLong_FromLong(rc);
 }
 

@@ -144,3 +144,17 @@ def test_a_workspace_with_gaps(made, f):
     with pytest.raises(dp.DpllmError, match="workspace"):
         getattr(dp, f)(**dict(CALLS[f](), workspace=on(torch.zeros(256, dtype=torch.uint8)[::4])))
     assert made == []
+
+
+@pytest.mark.parametrize("f", CALLS)
+def test_the_interpreter_is_free_while_the_library_works(made, f):
+    """The function that is called says whether its thread holds the interpreter's lock: 0 is no, and OK.  (ctypes gives it back on the long way.)"""
+    holds = C.cast(C.pythonapi.PyGILState_Check, C.c_void_p).value
+    nothing = C.CFUNCTYPE(C.c_int, *[C.c_int] * 6, C.POINTER(C.c_size_t))(lambda *a: 0)      # no workspace is needed
+    none = C.cast(nothing, C.c_void_p).value
+    calls.bind_tokens((holds, none, holds, none, holds, holds), (torch.float16, torch.bfloat16, torch.float32, torch.int32, torch.int64, torch.float64),
+                      torch.empty_like)
+    for args in ways(f, CALLS[f]()):
+        getattr(dp, f)(**args)
+    # only what brings a workspace was called the long way: natively the lock was free
+    assert made == ([f] if "workspace" in CALLS[f]() else [])
