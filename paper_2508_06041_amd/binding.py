@@ -213,7 +213,7 @@ def dpllm_rope_frequencies(rotary_dim, base=10000.0, scaling=DPLLM_ROPE_PLAIN, f
 
 def dpllm_rope(x, positions, freqs, out=None, scale=1.0, layout=DPLLM_ROPE_HALF, inverse=False):
     """x: a tensor [batch][tokens][heads][head_dim], or a tuple of such that share everything but their heads (queries, keys).  positions: int32
-    [batch][tokens], or [tokens] for all sequences.  out: where the results go (x itself: in place); new tensors unless given."""
+    [batch][tokens], or [tokens] for all sequences.  out: where the results go (x itself: in place); new tensors unless given, with x's order of dimensions."""
     made = _calls.rope(x, positions, freqs, out, scale, layout, inverse)
     if type(made) is not int:
         return made
@@ -224,7 +224,7 @@ def dpllm_rope(x, positions, freqs, out=None, scale=1.0, layout=DPLLM_ROPE_HALF,
     _need(0 < len(xs) <= 4, "dpllm_rope takes 1 to 4 tensors")
     first = xs[0]
     dtype = _dtype(first, "x")
-    outs = tuple(torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in xs) if out is None else (out,) if isinstance(out, torch.Tensor) else tuple(out)
+    outs = tuple(torch.empty_like(t) for t in xs) if out is None else (out,) if isinstance(out, torch.Tensor) else tuple(out)
     _need(len(outs) == len(xs), "out has to hold a tensor for each of x")
     views = [_view(t, "x") for t in xs]
     into = [_view(t, "out") for t in outs]
@@ -272,8 +272,9 @@ def dpllm_tree_attention_workspace_bytes(batch, nodes, heads, kv_heads, head_dim
 
 def dpllm_tree_attention(cache, layer, lens, q, k_new=None, v_new=None, mask=None, scale=None, out=None, lse=None, max_len=None, workspace=None):
     """q: [batch][nodes][heads][head_dim]; k_new, v_new: [batch][nodes][cache.heads][head_dim].  mask: int64 [batch or 1][nodes][ceil(nodes / 64)], bit j of
-    row i: node i sees node j; None: a chain.  scale: 1 / sqrt(head_dim) unless given.  lse: float32 [batch][nodes][heads] to be filled.  max_len: how long
-    the longest context is expected to be (the cache's capacity unless given).  workspace: uint8, allocated for the call unless given."""
+    row i: node i sees node j; None: a chain.  scale: 1 / sqrt(head_dim) unless given.  out: a new tensor with q's order of dimensions unless given.  lse:
+    float32 [batch][nodes][heads] to be filled.  max_len: how long the longest context is expected to be (the cache's capacity unless given).  workspace:
+    uint8, allocated for the call unless given."""
     made = _calls.attention(cache, layer, lens, q, k_new, v_new, mask, scale, out, lse, max_len, workspace)
     if type(made) is not int:
         return made
@@ -289,7 +290,7 @@ def dpllm_tree_attention(cache, layer, lens, q, k_new=None, v_new=None, mask=Non
         _need(k_new.shape == new and v_new.shape == new and k_new.dtype == v_new.dtype == q.dtype,
               "k_new and v_new have to be [batch][nodes][kv heads][head_dim] of the cache's type")
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = torch.empty_like(q)
     _need(out.shape == q.shape and out.dtype == q.dtype, "out has to have the shape and type of q")
     if mask is not None:
         _need(mask.dtype == torch.int64 and _on(mask, "mask") and mask.is_contiguous() and mask.dim() == 3 and mask.shape[0] in (1, b) and

@@ -158,3 +158,21 @@ def test_the_interpreter_is_free_while_the_library_works(made, f):
         getattr(dp, f)(**args)
     # only what brings a workspace was called the long way: natively the lock was free
     assert made == ([f] if "workspace" in CALLS[f]() else [])
+
+
+def heads_first(x):
+    """The same tensor, laid out head after head."""
+    return x.transpose(1, 2).contiguous().transpose(1, 2)
+
+
+def test_results_are_laid_out_alike_either_way(made):
+    """Results that a call makes follow the order of the inputs' dimensions, natively and the long way."""
+    a = rope_args()
+    x = heads_first(a["x"])
+    got = [dp.dpllm_rope(y, a["positions"], a["freqs"]) for y in ((x,), [x])]      # (a list is out of the ordinary)
+    assert made == ["dpllm_rope"] * 2 and [g[0].stride() for g in got] == [x.stride()] * 2
+    a = attention_args()
+    del a["out"]
+    a["q"] = q = heads_first(a["q"])
+    got = [dp.dpllm_tree_attention(**dict(a, workspace=w)) for w in (None, a["workspace"])]
+    assert [g.stride() for g in got] == [q.stride()] * 2
