@@ -213,7 +213,8 @@ def dpllm_rope_frequencies(rotary_dim, base=10000.0, scaling=DPLLM_ROPE_PLAIN, f
 
 def dpllm_rope(x, positions, freqs, out=None, scale=1.0, layout=DPLLM_ROPE_HALF, inverse=False):
     """x: a tensor [batch][tokens][heads][head_dim], or a tuple of such that share everything but their heads (queries, keys).  positions: int32
-    [batch][tokens], or [tokens] for all sequences.  out: where the results go (x itself: in place); new tensors unless given, with x's order of dimensions."""
+    [batch][tokens], or [tokens] for all sequences.  out: where the results go (x itself: in place); new tensors unless given, with x's order of dimensions.
+    New results of tensors that require a gradient have one."""
     made = _calls.rope(x, positions, freqs, out, scale, layout, inverse)
     if type(made) is not int:
         return made
@@ -223,6 +224,10 @@ def dpllm_rope(x, positions, freqs, out=None, scale=1.0, layout=DPLLM_ROPE_HALF,
     xs = (x,) if isinstance(x, torch.Tensor) else tuple(x)
     _need(0 < len(xs) <= 4, "dpllm_rope takes 1 to 4 tensors")
     first = xs[0]
+    if torch.is_grad_enabled() and any(t.requires_grad for t in (*xs, *(() if out is None else (out,) if isinstance(out, torch.Tensor) else out))):
+        _need(out is None, "results that go into out have no gradient, but one of the tensors requires one")
+        outs = _Rope.apply(positions, freqs, scale, layout, bool(inverse), *xs)
+        return outs[0] if isinstance(x, torch.Tensor) else outs
     dtype = _dtype(first, "x")
     outs = tuple(torch.empty_like(t) for t in xs) if out is None else (out,) if isinstance(out, torch.Tensor) else tuple(out)
     _need(len(outs) == len(xs), "out has to hold a tensor for each of x")
@@ -238,6 +243,26 @@ def dpllm_rope(x, positions, freqs, out=None, scale=1.0, layout=DPLLM_ROPE_HALF,
     _call(lib.dpllm_rope((_Heads * m)(*views), (_Heads * m)(*into), (C.c_int * m)(*[t.shape[2] for t in xs]), m, b, n, d, dtype, 2 * freqs.shape[0],
                          layout, freqs.data_ptr(), scale, pos, 0 if positions.dim() == 1 else n, 1 if inverse else 0, _stream()))
     return outs[0] if isinstance(x, torch.Tensor) else outs
+
+
+class _Rope(torch.autograd.Function):
+    """dpllm_rope of tensors that require a gradient: a rotation's transpose is the inverse one, with the same scale."""
+
+    @staticmethod
+    def forward(ctx, positions, freqs, scale, layout, inverse, *xs):
+        ctx.save_for_backward(positions, freqs)
+        ctx.how = scale, layout, inverse
+        return dpllm_rope(xs, positions, freqs, scale=scale, layout=layout, inverse=inverse)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        positions, freqs = ctx.saved_tensors
+        scale, layout, inverse = ctx.how
+        wanted = ctx.needs_input_grad[5:]
+        # (the gradient of a sum is one number for all elements: the last dimension has no stride)
+        given = tuple(g if g.stride(3) == 1 else g.contiguous() for g, w in zip(grads, wanted) if w)
+        made = iter(dpllm_rope(given, positions, freqs, scale=scale, layout=layout, inverse=not inverse))
+        return (None,) * 5 + tuple(next(made) if w else None for w in wanted)
 
 
 class Cache:
@@ -274,7 +299,7 @@ def dpllm_tree_attention(cache, layer, lens, q, k_new=None, v_new=None, mask=Non
     """q: [batch][nodes][heads][head_dim]; k_new, v_new: [batch][nodes][cache.heads][head_dim].  mask: int64 [batch or 1][nodes][ceil(nodes / 64)], bit j of
     row i: node i sees node j; None: a chain.  scale: 1 / sqrt(head_dim) unless given.  out: a new tensor with q's order of dimensions unless given.  lse:
     float32 [batch][nodes][heads] to be filled.  max_len: how long the longest context is expected to be (the cache's capacity unless given).  workspace:
-    uint8, allocated for the call unless given."""
+    uint8, allocated for the call unless given.  The result has no gradient."""
     made = _calls.attention(cache, layer, lens, q, k_new, v_new, mask, scale, out, lse, max_len, workspace)
     if type(made) is not int:
         return made

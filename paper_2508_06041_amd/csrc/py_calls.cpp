@@ -129,7 +129,7 @@ struct TokenCalls {
 // torch.float16, bfloat16, float32, int32, int64, float64, and torch.empty_like
 PyObject *dtypes[6] = {}, *empty_like = nullptr;
 enum { kInt32 = 3, kInt64 = 4, kFloat64 = 5 };
-PyObject *s_dtype = nullptr, *s_shape = nullptr, *s_stride = nullptr, *s_get_device = nullptr, *s_address = nullptr, *s_batch = nullptr, *s_device = nullptr, *s_new_empty = nullptr;
+PyObject *s_dtype = nullptr, *s_shape = nullptr, *s_stride = nullptr, *s_get_device = nullptr, *s_address = nullptr, *s_batch = nullptr, *s_device = nullptr, *s_new_empty = nullptr, *s_requires_grad = nullptr;
 
 // A reference that is given back.
 struct Ref {
@@ -268,6 +268,12 @@ int unlocked(F call) {
   return rc;
 }
 
+// whether a gradient is asked for, which is binding.py's business
+bool graded(PyObject* o) {
+  const Ref r(PyObject_GetAttr(o, s_requires_grad));
+  return r.o != Py_False;
+}
+
 // rope(x, positions, freqs, out, scale, layout, inverse)
 PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const int m = n == 7 && PyTuple_Check(a[0]) ? (int)PyTuple_GET_SIZE(a[0]) : 1;
@@ -286,7 +292,7 @@ PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (results.o == nullptr) return elsewhere();
   for (int i = 0; i < m; ++i) {
     const Ref t(item(a[0], i));
-    if (!look(t.o, place, &x[i]) || x[i].dtype > 2 || !heads_of(x[i], &in[i]) || x[i].dtype != x[0].dtype || x[i].size[0] != x[0].size[0] ||
+    if (!look(t.o, place, &x[i]) || graded(t.o) || x[i].dtype > 2 || !heads_of(x[i], &in[i]) || x[i].dtype != x[0].dtype || x[i].size[0] != x[0].size[0] ||
         x[i].size[1] != x[0].size[1] || x[i].size[3] != x[0].size[3])
       return elsewhere();
     heads[i] = (int)x[i].size[2];
@@ -294,7 +300,7 @@ PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (o == nullptr) return elsewhere();
     PyTuple_SET_ITEM(results.o, i, o);
     Tensor y;
-    if (!(a[3] == Py_None ? look_new(o, x[i], &y) : look(o, place, &y)) || y.dtype != x[0].dtype || !heads_of(y, &out[i])) return elsewhere();
+    if (!(a[3] == Py_None ? look_new(o, x[i], &y) : look(o, place, &y) && !graded(o)) || y.dtype != x[0].dtype || !heads_of(y, &out[i])) return elsewhere();
     for (int j = 0; j < 4; ++j)
       if (y.size[j] != x[i].size[j]) return elsewhere();
   }
@@ -462,7 +468,8 @@ PyMODINIT_FUNC PyInit__calls() {
   s_batch = PyUnicode_InternFromString("batch");
   s_device = PyUnicode_InternFromString("device");
   s_new_empty = PyUnicode_InternFromString("new_empty");
-  for (PyObject* s : {s_dtype, s_shape, s_stride, s_get_device, s_address, s_batch, s_device, s_new_empty})
+  s_requires_grad = PyUnicode_InternFromString("requires_grad");
+  for (PyObject* s : {s_dtype, s_shape, s_stride, s_get_device, s_address, s_batch, s_device, s_new_empty, s_requires_grad})
     if (s == nullptr) return nullptr;
   if (s_data_ptr == nullptr || s_dim == nullptr || s_size == nullptr || zero == nullptr) return nullptr;
   PyObject* m = PyModule_Create(&definition);

@@ -176,3 +176,14 @@ def test_results_are_laid_out_alike_either_way(made):
     a["q"] = q = heads_first(a["q"])
     got = [dp.dpllm_tree_attention(**dict(a, workspace=w)) for w in (None, a["workspace"])]
     assert [g.stride() for g in got] == [q.stride()] * 2
+
+
+def test_a_gradient_that_results_in_out_would_not_have(made):
+    a = rope_args()
+    for change in ({"x": a["x"].requires_grad_()}, {"out": a["out"].requires_grad_()}):
+        with pytest.raises(dp.DpllmError, match="gradient"):
+            dp.dpllm_rope(**dict(a, **change))
+    assert made == []
+    with torch.no_grad():
+        dp.dpllm_rope(**a)
+    assert made == ["dpllm_rope"]
