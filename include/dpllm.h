@@ -235,7 +235,7 @@ int dpllm_decode_step_parts(dpllm_model* m, const void* const* xs, void* const* 
 #define DPLLM_MAX_HEAD_DIM 1024
 #define DPLLM_MAX_TENSORS 4    /* tensors of one dpllm_rope                              */
 
-/* A device tensor [batch][tokens][heads][head_dim]; strides in elements, of head_dim 1. */
+/* A device tensor [batch][tokens][heads][head_dim]; strides in elements, of head_dim 1.  The stride of a dimension of 1 may be anything (in a cache too). */
 typedef struct dpllm_heads {
   void* data;
   int64_t batch_stride, token_stride, head_stride;

@@ -106,21 +106,22 @@ int dpllm_tree_attention(const dpllm_cache* cache, int layer, int batch, int nod
   if (batch == 0 || nodes == 0) return DPLLM_OK;
   if (!lens_dev || !q || !out || !q->data || !out->data || !k_new != !v_new || (k_new && (!k_new->data || !v_new->data)))
     return refuse(DPLLM_EINVAL, "%s: a pointer is NULL (k_new and v_new may be, together)", who);
-  if (!pieces(*q, 2) || !pieces(*out, 2) || (k_new && (!pieces(*k_new, 2) || !pieces(*v_new, 2))) || ((uintptr_t)cache->k | (uintptr_t)cache->v) % 16 ||
-      (cache->layer_stride | cache->page_stride | cache->token_stride | cache->head_stride) % 8)
+  const dpllm_cache c = reached(*cache);
+  const dpllm_heads queries = reached(*q, batch, nodes, heads), results = reached(*out, batch, nodes, heads);
+  const dpllm_heads keys = k_new ? reached(*k_new, batch, nodes, c.heads) : dpllm_heads{}, values = k_new ? reached(*v_new, batch, nodes, c.heads) : dpllm_heads{};
+  if (!pieces(queries, 2) || !pieces(results, 2) || !pieces(keys, 2) || !pieces(values, 2) || ((uintptr_t)c.k | (uintptr_t)c.v) % 16 ||
+      (c.layer_stride | c.page_stride | c.token_stride | c.head_stride) % 8)
     return refuse(DPLLM_EINVAL, "%s: tensors have to be aligned to 16 bytes, with strides of whole 8 elements", who);
   const Plan p = plan_of(batch, nodes, heads, cache->heads, cache->head_dim, std::min<int64_t>(max_len, (int64_t)cache->pages_per_seq * cache->page));
   if (p.groups > 0x7fffff || (int64_t)batch * heads * nodes > 0x7fffff) return refuse(DPLLM_ESHAPE, "%s: %lld workgroups", who, (long long)p.groups);
   if (p.bytes > 0 && (!ws_dev || ws_bytes < p.bytes || (uintptr_t)ws_dev % 16))
     return refuse(DPLLM_ESTATE, "%s: needs a workspace of %zu bytes, aligned to 16", who, p.bytes);
   AttentionArgs a{};
-  a.cache = view(*cache, layer);
-  a.q = view(*q);
-  a.out = view(*out);
-  if (k_new) {
-    a.k_new = view(*k_new);
-    a.v_new = view(*v_new);
-  }
+  a.cache = view(c, layer);
+  a.q = view(queries);
+  a.out = view(results);
+  a.k_new = view(keys);
+  a.v_new = view(values);
   a.lens = lens_dev;
   a.mask = mask_dev;
   a.mask_stride = mask_stride;

@@ -124,9 +124,10 @@ int dpllm_rope(const dpllm_heads* x, const dpllm_heads* out, const int* heads, i
     all_heads += heads[i];
     if (all_heads * head_dim > (1 << 24)) return refuse(DPLLM_ESHAPE, "dpllm_rope: %lld heads of %d", (long long)all_heads, head_dim);
     a.end[i] = (int)all_heads;
-    a.x[i] = view(x[i]);
-    a.out[i] = view(out[i]);
-    vector = vector && pieces(x[i], es) && pieces(out[i], es);
+    const dpllm_heads from = reached(x[i], batch, tokens, heads[i]), to = reached(out[i], batch, tokens, heads[i]);
+    a.x[i] = view(from);
+    a.out[i] = view(to);
+    vector = vector && pieces(from, es) && pieces(to, es);
     same = same && x[i].data == out[i].data;
   }
   if (batch == 0 || tokens == 0) return DPLLM_OK;
@@ -175,14 +176,16 @@ int dpllm_cache_append(const dpllm_cache* cache, int first_layer, int n_layers, 
   if (((uintptr_t)k_new->data | (uintptr_t)v_new->data) % es) return refuse(DPLLM_EINVAL, "%s: k_new or v_new is not aligned to its elements", who);
   if (n_layers == 0 || batch == 0 || nodes == 0) return DPLLM_OK;
   if (!k_new->data || !v_new->data) return refuse(DPLLM_EINVAL, "%s: k_new or v_new is NULL", who);
-  const bool vector = cache->head_dim % wide == 0 && pieces(*k_new, es) && pieces(*v_new, es) && (k_layer_stride | v_layer_stride) % wide == 0 &&
-                      ((uintptr_t)cache->k | (uintptr_t)cache->v) % 16 == 0 &&
-                      (cache->layer_stride | cache->page_stride | cache->token_stride | cache->head_stride) % wide == 0;
+  const dpllm_cache c = reached(*cache);
+  const dpllm_heads k = reached(*k_new, batch, nodes, c.heads), v = reached(*v_new, batch, nodes, c.heads);
+  if (n_layers == 1) k_layer_stride = v_layer_stride = 0;
+  const bool vector = c.head_dim % wide == 0 && pieces(k, es) && pieces(v, es) && (k_layer_stride | v_layer_stride) % wide == 0 &&
+                      ((uintptr_t)c.k | (uintptr_t)c.v) % 16 == 0 && (c.layer_stride | c.page_stride | c.token_stride | c.head_stride) % wide == 0;
   const int e = vector ? wide : 1;
   AppendArgs a{};
-  a.cache = view(*cache, first_layer);
-  a.k = view(*k_new);
-  a.v = view(*v_new);
+  a.cache = view(c, first_layer);
+  a.k = view(k);
+  a.v = view(v);
   a.k_layer = k_layer_stride;
   a.v_layer = v_layer_stride;
   a.lens = lens_dev;

@@ -14,6 +14,18 @@ int launched(const char* who);
 // Errors of a cache as such, with `batch` sequences in it; 0: none.
 int check_cache(const char* who, const dpllm_cache* cache, int batch);
 
+// The same without the strides that no element is reached by: those of dimensions of 1 may be anything.
+inline dpllm_heads reached(const dpllm_heads& t, int batch, int tokens, int heads) {
+  return {t.data, batch > 1 ? t.batch_stride : 0, tokens > 1 ? t.token_stride : 0, heads > 1 ? t.head_stride : 0};
+}
+inline dpllm_cache reached(dpllm_cache c) {
+  if (c.layers == 1) c.layer_stride = 0;
+  if (c.pages == 1) c.page_stride = 0;
+  if (c.page == 1) c.token_stride = 0;
+  if (c.heads == 1) c.head_stride = 0;
+  return c;
+}
+
 inline Heads view(const dpllm_heads& t) { return {(char*)t.data, t.batch_stride, t.token_stride, t.head_stride}; }
 
 inline CacheView view(const dpllm_cache& c, int layer) {
