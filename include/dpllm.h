@@ -308,8 +308,8 @@ int dpllm_tree_attention(const dpllm_cache* cache, int layer, int batch, int nod
 /* Which drafted tokens stand, and the token behind them.  Row i of `logits` is the target's answer behind node i, p_i = softmax(logits_i / temperature[b]);
  * row i of `draft` the draft's, q_i, from which the tokens of i's children were drawn, each by itself.  From the root (node 0) on, the children of a node are
  * asked in the order of their numbers: child c stands if uniforms[c] q(c) < r(c), where r is p at first and norm(max(r - q, 0)) behind every child that
- * did not stand (r stays where nothing is left: no more than 4e-13 of it, which is what equal rows may come to).  With draft_dev NULL the children were named, not drawn: c stands if uniforms[c] < r(c), and a
- * child that does not leaves r (unless it is all there is, again to 4e-13).  The first child that stands is the next node; where none does, the token behind is drawn from r: the first word whose running sum of r exceeds uniforms[0] times
+ * did not stand (r stays where nothing is left; a word of which no more than 4e-13 is left has nothing, as equal rows may come to that).  With draft_dev NULL the children were named, not drawn: c stands if uniforms[c] < r(c), and a
+ * child that does not leaves r (unless it is all there is, to 4e-13).  The first child that stands is the next node; where none does, the token behind is drawn from r: the first word whose running sum of r exceeds uniforms[0] times
  * the whole, words of less than 1e-280 left out.  Tokens so chosen are distributed as if drawn from the target.  temperature[b] 0 (or less, or NaN): a child stands if it is the word with
  * the largest logit, the lowest such word where several are, and that word is the token behind; the draft rows are not read.
  * logits, draft: dtype [batch][nodes][vocabulary], the words contiguous, strides in elements.  tokens: int32 [batch][nodes] (that of node 0 is not read); a token outside the

@@ -340,17 +340,17 @@ __device__ __forceinline__ RowTop row_top(const VerifyPart* parts, int chunks, d
   return r;
 }
 
-// max(p - a q, 0) of a word from its weights.  Both products are rounded before they meet: one that is subtracted as it is from a rounded one leaves its rounding,
-// and equal rows would leave something everywhere.  `none` is taken off besides.
+// max(p - a q, 0) of a word from its weights; with a > 0 scale_p has kSure in it.  Both products are rounded before they meet: one that is subtracted as it is from a
+// rounded one leaves its rounding.  `none` is taken off besides.
 __device__ __forceinline__ double left_of(double weight_p, double scale_p, double weight_q, double scale_q, double none) {
 #pragma clang fp contract(off)
   const double p = weight_p * scale_p, q = __builtin_fma(weight_q, scale_q, none);
   return __builtin_fmax(p - q, 0.0);
 }
 
-// A sum of what is left that is no more than this is what the rounding of equal probabilities comes to, and nothing is left: weights and the two rows' sums are
-// good to 1e-13 each (the rows may be cut into chunks at different words).
-constexpr double kNothingLeft = 4e-13;
+// Weights and rows' sums are good to 1e-13 each, and two rows may be cut into chunks at different words: of a word of which less than 4e-13 of its probability is left
+// beside the draft nothing may be left in truth, and nothing is taken to be, so that equal rows leave nothing at all.  What is left of others may be as little as it will.
+constexpr double kNothingLeft = 4e-13, kSure = 1.0 - kNothingLeft;
 
 // Chunks of less than this are not drawn from.  A word's weight counts from 1e-290 of the whole on where it is drawn, and a chunk of 8192 words that comes to 1e-280 has one.
 constexpr double kLeastChunk = 1e-280;
@@ -441,8 +441,8 @@ __device__ RowState test_children(const VerifyArgs& g, const int32_t* parents, c
         ++s.refused;
         continue;
       }
-      const double have = __builtin_fmax(cp - s.a * cq, 0.0);
-      if (cu * cq * s.sum < have) {
+      const double have = s.level < 0 ? cp : __builtin_fmax(cp * kSure - s.a * cq, 0.0) / s.sum;
+      if (cu * cq < have) {
         s.taken = first + l;
         return s;
       }
@@ -457,7 +457,7 @@ __device__ RowState test_children(const VerifyArgs& g, const int32_t* parents, c
       double rest = 0.0;
       for (int i = lane; i < g.chunks; i += 64) rest += g.rest[((int64_t)j * g.batch * g.nodes + row) * g.chunks + i];
       rest = wave_sum(rest);
-      if (rest > kNothingLeft) {      // (else nothing of the target is left beside the draft, and the distribution stays)
+      if (rest > 0.0) {      // (else nothing of the target is left beside the draft, and the distribution stays)
         s.a += s.sum;
         s.sum = rest;
         s.level = j;
@@ -530,7 +530,7 @@ __global__ void __launch_bounds__(kVerThreads) verify_rest_kernel(const VerifyAr
   const double by = 1.0 / (double)temperature, next_a = info.s.a + info.s.sum;
   const char* from_p = a.logits + (b * a.logits_batch + node * a.logits_node) * (int64_t)sizeof(T);
   const char* from_q = a.draft + (b * a.draft_batch + node * a.draft_node) * (int64_t)sizeof(T);
-  const double scale_p = p.sum > 0.0 ? 1.0 / p.sum : 0.0, scale_q = q.sum > 0.0 ? next_a / q.sum : 0.0;
+  const double scale_p = p.sum > 0.0 ? kSure / p.sum : 0.0, scale_q = q.sum > 0.0 ? next_a / q.sum : 0.0;
   const Weigher wp(table, p.top, by), wq(table, q.top, by);
   const bool plain = wp.plain && wq.plain, alike = Chunk<T>::lead(from_p) == Chunk<T>::lead(from_q);
   for (int chunk = blockIdx.x - row * groups; chunk < a.chunks; chunk += groups) {
@@ -734,7 +734,7 @@ __global__ void __launch_bounds__(kVerChooseThreads) verify_choose_kernel(const 
     return;
   }
   // inside the chunk: a piece to a thread, in the order of the row
-  const double scale_p = 1.0 / p.sum, scale_q = !named && q.sum > 0.0 ? s.a / q.sum : 0.0, need = before_chunk;
+  const double scale_p = (s.level >= 0 ? kSure : 1.0) / p.sum, scale_q = !named && q.sum > 0.0 ? s.a / q.sum : 0.0, need = before_chunk;
   const int start = chunk * Chunk<T>::kElements + (int)threadIdx.x * E - lead;
   auto piece = [&](const char* from, bool even) {
     typename Piece<T>::type v;

@@ -48,3 +48,24 @@ def test_something_is_left_beside_rows_that_are_nearly_equal(dtype):
     uniforms[:, 0] = torch.rand(b, generator=g)
     lengths = compare(logits.cuda(), tokens.cuda(), None, uniforms.cuda(), torch.full((b,), 1.1, device="cuda"), draft.cuda())
     assert lengths == [1] * b
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_next_to_nothing_is_left(dtype):
+    """Rows that agree on a word of nearly all of the probability: however little the target has more of the others, that is what is left."""
+    b, v = 16, 9001
+    g = torch.Generator().manual_seed(4)
+    logits = torch.rand(b, 3, v, generator=g) * 4.0 - 8.0
+    logits[:, :, 100] = 0.0
+    draft = logits - 1.0
+    draft[:, :, 100] = 0.0
+    draft[:, :, 5000:] = logits[:, :, 5000:] + 0.5            # only words before 5000 have something left
+    tokens = torch.full((b, 3), -1, dtype=torch.int32)
+    tokens[:, 2] = 8000
+    tokens[::2, 2] = 7
+    uniforms = torch.rand(b, 3, generator=g)
+    uniforms[:, 2] = 1.0 - 2.0 ** -24
+    parents = torch.tensor([[-1, 0, 0]] * b, dtype=torch.int32)
+    temperature = torch.tensor([0.05, 0.06, 0.08, 0.1, 0.12, 0.15, 0.2, 0.4] * 2)
+    lengths = compare(logits.to(TYPES[dtype]).cuda(), tokens.cuda(), parents.cuda(), uniforms.cuda(), temperature.cuda(), draft.to(TYPES[dtype]).cuda(), siblings=2)
+    assert set(lengths) <= {1, 2}
