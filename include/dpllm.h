@@ -275,7 +275,7 @@ int dpllm_rope_frequencies(int rotary_dim, double base, int scaling, double fact
  * head, i < rotary_dim / 2, is (i, i + rotary_dim / 2) with DPLLM_ROPE_HALF and (2i, 2i + 1) with DPLLM_ROPE_INTERLEAVED; with
  * t = position * freqs[i] it becomes scale * (a cos t - b sin t, a sin t + b cos t).  inverse != 0: -t instead, which is the
  * transpose: from the gradient of the outputs it makes the gradient of the inputs.  Elements from rotary_dim on are copied.  Angles are formed
- * in 64 bits, products in 32, results rounded once.
+ * in 64 bits, their sines and the products in 32, results rounded once.
  * x, out: host arrays of `tensors` views with heads[i] heads each; out[i] may be x[i] itself and must not overlap it otherwise.
  * positions_dev: int32, positions_dev[b * positions_stride + t]; positions_stride 0: the same for every sequence.  freqs_dev: fp64.
  * dtype: DPLLM_F16, DPLLM_BF16 or DPLLM_F32.  batch or tokens 0: nothing to do.
@@ -315,7 +315,7 @@ int dpllm_tree_attention(const dpllm_cache* cache, int layer, int batch, int nod
  * logits, draft: dtype [batch][nodes][vocabulary], the words contiguous, strides in elements.  tokens: int32 [batch][nodes] (that of node 0 is not read); a token outside the
  * vocabulary never stands.  parents: int32 [batch][nodes]; a node whose parent is not a lower node is nobody's child; NULL: a chain.  uniforms: float
  * [batch][nodes] in [0, 1).  temperature: float [batch].  Logits of minus infinity and NaN have probability 0; where one is plus infinity, only such have any.
- * siblings (with draft rows only): the most children that a node has; a call makes that many passes over the rows whose children are refused.  Where a node has
+ * siblings (with draft rows only): the most children that a node has; a call makes that many passes over the rows whose children are refused, two launches each.  Where a node has
  * more, those beyond that did not stand leave r as it was and the children behind them are not asked.
  * count [batch]: how many nodes stand, the root among them, which is also how many tokens there are in words.  path [batch][nodes]: those nodes.  words [batch][nodes]:
  * the tokens of the drafted ones among them, then the token behind (-1 where the last row has no finite logit).  The rest of both is -1.  path and count are
@@ -332,7 +332,7 @@ int dpllm_verify(int batch, int nodes, int vocabulary, int dtype, const void* lo
  * page and sequences with a negative length are left out; counts above nodes are taken as nodes.  lens is not changed (add the counts
  * behind the call).  k_new, v_new: views of one layer's [batch][nodes][heads][head_dim] with the cache's type, layers k_layer_stride and v_layer_stride
  * elements apart; they must not overlap the cache.  Slots that two sequences share take either's values.
- * Errors: EINVAL, ESHAPE, EHIP. */
+ * Errors: EINVAL, ESHAPE, ERANGE (layers), EHIP. */
 int dpllm_cache_append(const dpllm_cache* cache, int first_layer, int n_layers, int batch, int nodes, const int32_t* lens_dev,
                        const dpllm_heads* k_new, int64_t k_layer_stride, const dpllm_heads* v_new, int64_t v_layer_stride,
                        const int32_t* path_dev, int64_t path_stride, const int32_t* count_dev, void* stream);

@@ -341,7 +341,7 @@ def dpllm_verify_workspace_bytes(batch, nodes, vocabulary, dtype, draft, sibling
 
 def dpllm_verify(logits, tokens, uniforms, temperature, parents=None, draft=None, siblings=None, count=None, path=None, words=None, workspace=None):
     """logits, draft: [batch][nodes][vocabulary] of one type; tokens, parents: int32 [batch][nodes]; uniforms: float32 [batch][nodes]; temperature: float32
-    [batch].  siblings: the most children that a node has (1 for a chain; every node but the root unless given).  Returns (count [batch], path, words
+    [batch].  siblings: the most children that a node has (1 for a chain; every node but the root unless given, and with draft rows each is two launches).  Returns (count [batch], path, words
     [batch][nodes]), int32, new tensors unless given.  workspace: uint8, allocated for the call unless given."""
     if count is None and path is None and words is None and workspace is None:
         made = _calls.verify(logits, tokens, uniforms, temperature, parents, draft,

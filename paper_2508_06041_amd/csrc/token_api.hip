@@ -52,7 +52,7 @@ int check_verify(const char* who, int batch, int nodes, int vocabulary, int dtyp
 template <typename T>
 void launch_verify(const VerifyArgs& a, hipStream_t s) {
   const unsigned rows = (unsigned)a.batch * a.nodes;
-  // three rounds of workgroups, whose next chunks come while they work: 768 rows of 128256 words in bf16 take 64 us with one workgroup to a row, 61 with two,
+  // three rounds of workgroups, whose next chunks come while they work: 640 rows (and 128 that are not read) of 128256 words in bf16 take 64 us with one workgroup to a row, 61 with two,
   // 54 with four, 56 with six, 61 with one to a chunk; few rows one to a chunk
   const int64_t all = (int64_t)rows * (a.draft ? 2 : 1);
   const int each = (int)std::min<int64_t>(a.chunks, (3000 + all - 1) / all);

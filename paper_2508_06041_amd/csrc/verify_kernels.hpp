@@ -65,7 +65,8 @@ __device__ __forceinline__ double weight(float x, float top, double by) {
 // lower word are the fraction r, the eight before them the place in a table of 2^(j / 256) in LDS, and those before the power of two.  1 + c1 r + c2 r^2 + c3 r^3 is
 // 2^(r / 256) to 2e-14, with the largest such error made least and none at 0, so that the largest logit counts exactly 1; the count is rounded to 2^-34, which is
 // 8e-14 of a weight at most.  With a count that is rounded to the nearest whole and the series to the fourth power (1e-15; three instructions in
-// twenty more) verify_parts took 69 us for 768 rows of 128256 words in bf16, with this 60, and 54 since a workgroup takes several chunks of a row.
+// twenty more) verify_parts took 69 us for 48 sequences of 8 nodes with draft rows of 128256 words in bf16 (16 of the sequences take the best token: 66 million
+// weights), with this 60, and 54 since a workgroup takes several chunks of a row.
 // Logits more than 690 temperatures below the largest, minus infinities and NaN among them, count as the one that is, whose weight of
 // 1e-300 is nothing to a sum.  A row whose largest logit is no finite number, or beside which 695 temperatures are
 // past the floats or lost in their rounding, goes the way above.
