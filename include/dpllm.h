@@ -253,8 +253,7 @@ typedef struct dpllm_cache {
   int32_t dtype, layers, pages, page, pages_per_seq, heads, head_dim;
 } dpllm_cache;
 
-/* Text of the last refusal of dpllm_rope_frequencies, dpllm_rope, dpllm_tree_attention, dpllm_verify or dpllm_cache_append in the
- * calling thread (valid until the next one). */
+/* Text of the last refusal of one of the calls from here to dpllm_sample in the calling thread (valid until the next one). */
 const char* dpllm_call_error(void);
 
 /* The angles per position that dpllm_rope takes: freqs[i], i < rotary_dim / 2 (host, radians), and *scale, what the rotated part is
@@ -336,6 +335,92 @@ int dpllm_verify(int batch, int nodes, int vocabulary, int dtype, const void* lo
 int dpllm_cache_append(const dpllm_cache* cache, int first_layer, int n_layers, int batch, int nodes, const int32_t* lens_dev,
                        const dpllm_heads* k_new, int64_t k_layer_stride, const dpllm_heads* v_new, int64_t v_layer_stride,
                        const int32_t* path_dev, int64_t path_stride, const int32_t* count_dev, void* stream);
+
+/*
+ * A cache in 8 or 4 bits, and what else a decode step does between its linears.  On the same terms as the calls above.
+ *
+ *   dpllm_norm_rope            norms of queries and keys for each head and their rotary positions in one pass, and the gradient of that
+ *   dpllm_quantized_append     keys and values are quantised as they go into the cache
+ *   dpllm_quantized_read       and come back
+ *   dpllm_quantized_attention  attention of new tokens over such a cache and over one another
+ *   dpllm_sample               the next token: temperature, top-k, top-p and min-p
+ */
+
+/* Norms of the heads of up to DPLLM_MAX_TENSORS tensors (the queries and the keys, say) of the same tokens, with a learned weight each, and their rotary positions:
+ * n = x / sqrt(mean of x^2 over the head + eps), out = the rotation of dpllm_rope (layout, freqs_dev, scale, positions) of weight * n.  rotary_dim 0: no rotation; freqs_dev and
+ * positions_dev may be NULL.  weights: host array of `tensors` device pointers (or NULL: all are 1; so is one that is NULL), each [head_dim] for all heads where
+ * weight_strides[i] is 0, else of head h from weight_strides[i] * h on, of weight_dtype.  x, out, heads, dtype, positions: as for dpllm_rope; out[i] may be x[i]
+ * itself and must not overlap it otherwise.  Sums and products are in 32 bits, results are rounded once.
+ * backward: from the gradients of the outputs, grads[i], it makes those of the inputs, grad_x[i] (which may be grads[i] or x[i] itself), and of the weights, grad_weights[i] (NULL: none is
+ * wanted; as NULL is for the array), which are laid out as the weights and summed over tokens, and over heads that share one, in 32 bits, in the same order every time.  ws_dev: 16-byte aligned, of
+ * dpllm_norm_rope_backward_workspace_bytes for the same sizes (0: NULL is accepted), used until the call's kernels have run.
+ * batch or tokens 0: nothing to do but to clear the gradients of weights.  Errors: EINVAL, ESHAPE, ESTATE (workspace), EHIP. */
+int dpllm_norm_rope(const dpllm_heads* x, const dpllm_heads* out, const int* heads, const void* const* weights, const int64_t* weight_strides, int weight_dtype,
+                    float eps, int tensors, int batch, int tokens, int head_dim, int dtype, int rotary_dim, int layout, const double* freqs_dev, float scale,
+                    const int32_t* positions_dev, int64_t positions_stride, void* stream);
+int dpllm_norm_rope_backward_workspace_bytes(const int* heads, const int64_t* weight_strides, int tensors, int batch, int tokens, int head_dim, size_t* bytes);
+int dpllm_norm_rope_backward(const dpllm_heads* x, const dpllm_heads* grads, const dpllm_heads* grad_x, const int* heads, const void* const* weights,
+                             void* const* grad_weights, const int64_t* weight_strides, int weight_dtype, float eps, int tensors, int batch, int tokens, int head_dim, int dtype,
+                             int rotary_dim, int layout, const double* freqs_dev, float scale, const int32_t* positions_dev, int64_t positions_stride, void* ws_dev,
+                             size_t ws_bytes, void* stream);
+
+/* A paged cache as dpllm_cache, whose keys and values are codes with one 32-bit word for each token and head (k_scales, v_scales):
+ *   E4M3  a byte each, OCP e4m3; the word is a float, the smallest power of two with which the largest size of the head is at most 448
+ *   INT8  a byte each, -127 ... 127, round(127 x / the largest size); the word is a float, the largest size / 127
+ *   INT4  half a byte each, element 2i in the lower half of byte i: bit 3 the sign, m below, for offset +- scale (m + 1/2).  The word is two bfloat16: the scale in the lower
+ *         half, the offset in the upper.  offset = (lowest + highest) / 2; scale = an eighth of the larger distance of those from it, rounded up, or 0 where they are equal;
+ *         a value is at floor((x - offset) / scale), within -8 ... 7
+ * Sizes (and distances) below 2^-100 that are not 0 count as 2^-100.  A head with a value that is no finite number is held as NaN.
+ * Strides of codes are in bytes, those of scales in words, the same for keys and values; the codes of a head lie side by side. */
+#define DPLLM_CACHE_E4M3 1
+#define DPLLM_CACHE_INT8 2
+#define DPLLM_CACHE_INT4 3
+typedef struct dpllm_quantized_cache {
+  void *k, *v, *k_scales, *v_scales;
+  int64_t layer_stride, page_stride, token_stride, head_stride;
+  int64_t scale_layer_stride, scale_page_stride, scale_token_stride, scale_head_stride;
+  const int32_t* table;
+  int64_t table_stride;
+  int32_t format, layers, pages, page, pages_per_seq, heads, head_dim;
+} dpllm_quantized_cache;
+
+/* dpllm_cache_append into such a cache; k_new and v_new are of `dtype` (DPLLM_F16, DPLLM_BF16 or DPLLM_F32).  A slot that two sequences share may end with one's codes
+ * and the other's scale: sequences may share pages only where none of them is written.  head_dim up to DPLLM_MAX_HEAD_DIM, even for INT4.
+ * Errors: EINVAL, ESHAPE, ERANGE (layers), EHIP. */
+int dpllm_quantized_append(const dpllm_quantized_cache* cache, int first_layer, int n_layers, int batch, int nodes, const int32_t* lens_dev, int dtype,
+                           const dpllm_heads* k_new, int64_t k_layer_stride, const dpllm_heads* v_new, int64_t v_layer_stride, const int32_t* path_dev,
+                           int64_t path_stride, const int32_t* count_dev, void* stream);
+
+/* What the cache holds of tokens first[b] ... + tokens - 1 of every sequence, for n_layers layers from first_layer on, into k_out and v_out: [layers][batch][tokens][heads][head_dim]
+ * of `dtype`, layers k_layer_stride and v_layer_stride elements apart.  first_dev NULL: from token 0 on.  count_dev NULL: all of them, else those from count[b] on are written as zeros, as are
+ * tokens that no page holds (those in front of token 0 among them).  Values are products (and sums) in 32 bits, rounded once more for the shorter types.
+ * Errors: EINVAL, ESHAPE, ERANGE (layers), EHIP. */
+int dpllm_quantized_read(const dpllm_quantized_cache* cache, int first_layer, int n_layers, int batch, int tokens, const int32_t* first_dev, const int32_t* count_dev,
+                         int dtype, const dpllm_heads* k_out, int64_t k_layer_stride, const dpllm_heads* v_out, int64_t v_layer_stride, void* stream);
+
+/* dpllm_tree_attention over such a cache: the same arguments and rules, with `dtype` (DPLLM_F16 or DPLLM_BF16) the type of q, k_new, v_new and out, which are not quantised.  The
+ * cached tokens count as what their codes and scales stand for, unrounded; their weights are rounded to bfloat16 for the value product, for DPLLM_F16 to 16 bits.  Codes and their
+ * strides are aligned to 16 bytes.  A head that holds NaN makes NaN of the rows that see it.
+ * Errors: EINVAL, ESHAPE, ERANGE (layer), ESTATE (workspace), EHIP. */
+int dpllm_quantized_attention_workspace_bytes(int batch, int nodes, int heads, int kv_heads, int head_dim, int max_len, size_t* bytes);
+int dpllm_quantized_attention(const dpllm_quantized_cache* cache, int layer, int batch, int nodes, int heads, int dtype, const int32_t* lens_dev, int max_len,
+                              const dpllm_heads* q, const dpllm_heads* k_new, const dpllm_heads* v_new, const uint64_t* mask_dev, int64_t mask_stride, float scale,
+                              const dpllm_heads* out, float* lse_dev, void* ws_dev, size_t ws_bytes, void* stream);
+
+/* A word for every row of logits [rows][vocabulary] (dtype, the words contiguous, rows `stride` elements apart) by a given uniform number.  Words are ordered by their logits, the largest
+ * first, equal ones by their numbers, with weights e = exp((logit - largest) / temperature[row]); those of less than 2^-64 are left out.  Of the others stay
+ *   the first top_k[row] (0 or less: all);
+ *   of these each in front of which less than top_p[row] of their sum lies (1 or more, or NaN: all; the first always stays);
+ *   of these each with e at least min_p[row] (0 or less, or NaN: all; the first always stays).
+ * words[row] is the first of them, by number, whose running sum (by number) exceeds uniforms[row] times their whole: what dpllm_verify draws behind a lone node
+ * where nothing is filtered.  kept[row], if kept_dev is not NULL: how many stayed.  temperature 0 (or less, or NaN): the largest logit, the lowest such word where several are.  Logits of minus infinity and NaN
+ * never stay; where one is plus infinity only such do, with equal weights.  A row without a word to draw gives -1 (and keeps 0).  top_k, top_p, min_p, temperature, uniforms: [rows] on the
+ * device; the first three may be NULL.  Everything is computed in 64 bits, in an order that does not change.  ws_dev: 16-byte aligned, of
+ * dpllm_sample_workspace_bytes, used until the call's kernels have run.  Errors: EINVAL, ESHAPE, ESTATE (workspace), EHIP. */
+int dpllm_sample_workspace_bytes(int rows, int vocabulary, int dtype, size_t* bytes);
+int dpllm_sample(int rows, int vocabulary, int dtype, const void* logits_dev, int64_t stride, const float* uniforms_dev, const float* temperature_dev,
+                 const int32_t* top_k_dev, const float* top_p_dev, const float* min_p_dev, int32_t* words_dev, int32_t* kept_dev, void* ws_dev, size_t ws_bytes,
+                 void* stream);
 
 /* Parity aid: writes the canonical k-bit codes of linear `id`, uint8 [out][in], read back
  * from the private device layout, to idx_dev (device).  Errors: EINVAL, ERANGE, ESTATE, EHIP. */

@@ -21,6 +21,7 @@ DPLLM_F16, DPLLM_BF16, DPLLM_F32 = 0, 1, 2
 DPLLM_MAX_NODES = 256
 DPLLM_ROPE_PLAIN, DPLLM_ROPE_LINEAR, DPLLM_ROPE_NTK, DPLLM_ROPE_YARN, DPLLM_ROPE_BANDS = 0, 1, 2, 3, 4
 DPLLM_ROPE_HALF, DPLLM_ROPE_INTERLEAVED = 0, 1
+DPLLM_CACHE_E4M3, DPLLM_CACHE_INT8, DPLLM_CACHE_INT4 = 1, 2, 3
 
 SYMBOLS = ["dpllm_model_create", "dpllm_model_destroy", "dpllm_last_error", "dpllm_linear_device_bytes",
            "dpllm_workspace_bytes", "dpllm_set_workspace",
@@ -30,7 +31,9 @@ SYMBOLS = ["dpllm_model_create", "dpllm_model_destroy", "dpllm_last_error", "dpl
            "dpllm_debug_set_polls", "dpllm_debug_set_one_launch", "dpllm_debug_step_launches", "dpllm_debug_copy", "dpllm_debug_read",
            "dpllm_call_error", "dpllm_rope_frequencies", "dpllm_rope",
            "dpllm_tree_attention_workspace_bytes", "dpllm_tree_attention", "dpllm_verify_workspace_bytes",
-           "dpllm_verify", "dpllm_cache_append"]
+           "dpllm_verify", "dpllm_cache_append",
+           "dpllm_norm_rope", "dpllm_norm_rope_backward_workspace_bytes", "dpllm_norm_rope_backward", "dpllm_quantized_append", "dpllm_quantized_read",
+           "dpllm_quantized_attention_workspace_bytes", "dpllm_quantized_attention", "dpllm_sample_workspace_bytes", "dpllm_sample"]
 
 
 class DpllmError(RuntimeError):
@@ -49,6 +52,14 @@ class _Cache(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("layer_stride", C.c_int64), ("page_stride", C.c_int64), ("token_stride", C.c_int64),
                 ("head_stride", C.c_int64), ("table", C.c_void_p), ("table_stride", C.c_int64), ("dtype", C.c_int32), ("layers", C.c_int32),
                 ("pages", C.c_int32), ("page", C.c_int32), ("pages_per_seq", C.c_int32), ("heads", C.c_int32), ("head_dim", C.c_int32)]
+
+
+class _QuantizedCache(C.Structure):
+    """dpllm_quantized_cache."""
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_scales", "v_scales")] + \
+               [(p + n + "_stride", C.c_int64) for p in ("", "scale_") for n in ("layer", "page", "token", "head")] + \
+               [("table", C.c_void_p), ("table_stride", C.c_int64)] + \
+               [(n, C.c_int32) for n in ("format", "layers", "pages", "page", "pages_per_seq", "heads", "head_dim")]
 
 
 def _load():
@@ -93,6 +104,17 @@ def _load():
     L.dpllm_verify_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32, C.POINTER(sz)]
     L.dpllm_verify.argtypes = [i32, i32, i32, i32, vp, i64, i64, vp, i64, i64, vp, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
     L.dpllm_cache_append.argtypes = [cache, i32, i32, i32, i32, vp, heads, i64, heads, i64, vp, i64, vp, vp]
+    quantized = C.POINTER(_QuantizedCache)
+    L.dpllm_norm_rope.argtypes = [heads, heads, C.POINTER(i32), C.POINTER(vp), C.POINTER(i64), i32, f32, i32, i32, i32, i32, i32, i32, i32, vp, f32, vp, i64, vp]
+    L.dpllm_norm_rope_backward_workspace_bytes.argtypes = [C.POINTER(i32), C.POINTER(i64), i32, i32, i32, i32, C.POINTER(sz)]
+    L.dpllm_norm_rope_backward.argtypes = [heads, heads, heads, C.POINTER(i32), C.POINTER(vp), C.POINTER(vp), C.POINTER(i64), i32, f32, i32, i32, i32, i32, i32, i32, i32,
+                                           vp, f32, vp, i64, vp, sz, vp]
+    L.dpllm_quantized_append.argtypes = [quantized, i32, i32, i32, i32, vp, i32, heads, i64, heads, i64, vp, i64, vp, vp]
+    L.dpllm_quantized_read.argtypes = [quantized, i32, i32, i32, i32, vp, vp, i32, heads, i64, heads, i64, vp]
+    L.dpllm_quantized_attention_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32, C.POINTER(sz)]
+    L.dpllm_quantized_attention.argtypes = [quantized, i32, i32, i32, i32, i32, vp, i32, heads, heads, heads, vp, i64, f32, heads, vp, vp, sz, vp]
+    L.dpllm_sample_workspace_bytes.argtypes = [i32, i32, i32, C.POINTER(sz)]
+    L.dpllm_sample.argtypes = [i32, i32, i32, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     return L
 
 
@@ -390,6 +412,265 @@ def dpllm_cache_append(cache, lens, k_new, v_new, path=None, count=None, layer=0
     _call(lib.dpllm_cache_append(C.byref(cache.c), layer, layers, b, n, _index(lens, (b,), "lens"), C.byref(_view(k_new[0], "k_new")), k_new.stride(0),
                                  C.byref(_view(v_new[0], "v_new")), v_new.stride(0), _index(path, (b, n), "path"), n,
                                  _index(count, (b,), "count"), _stream()))
+
+
+def _norm_weights(xs, weights, contiguous=False):
+    """The weights of the tensors xs as tensors (or None) of one type, and what the library takes of them: pointers, strides, that type."""
+    ws = (None,) * len(xs) if weights is None else (weights,) if isinstance(weights, torch.Tensor) else tuple(weights)
+    _need(len(ws) == len(xs), "there has to be a weight (or None) for each tensor")
+    made, dtype = [], None
+    for t, w in zip(xs, ws):
+        if w is not None:
+            h, d = t.shape[2], t.shape[3]
+            _need(w.dtype in _DTYPES and _on(w, "a weight") and w.shape in ((d,), (h, d)), "a weight has to be a device tensor [head_dim] or [heads][head_dim]")
+            _need(dtype in (None, w.dtype), "the weights have to be of one type")
+            dtype = w.dtype
+            if (w.dim() == 2 and w.stride(0) == 0 and h > 1) or (d > 1 and w.stride(-1) != 1) or (contiguous and not w.is_contiguous()):
+                w = w.contiguous()
+        made.append(w)
+    n = len(xs)
+    return made, (C.c_void_p * n)(*[_ptr(w) for w in made]), (C.c_int64 * n)(*[w.stride(0) if w is not None and w.dim() == 2 and w.shape[0] > 1 else 0 for w in made]), \
+        DPLLM_F32 if dtype is None else _DTYPES[dtype]
+
+
+def _norm_plan(first, positions, freqs):
+    """Pointers and sizes of a rotation: rotary_dim, freqs, positions, their stride."""
+    if freqs is None:
+        return 0, None, None, 0
+    b, n = first.shape[:2]
+    _need(freqs.dtype == torch.float64 and _on(freqs, "freqs") and freqs.is_contiguous() and freqs.dim() == 1, "freqs has to be a contiguous float64 device vector")
+    _need(positions is not None, "a rotation needs positions")
+    return 2 * freqs.shape[0], freqs.data_ptr(), _index(positions, (n,) if positions.dim() == 1 else (b, n), "positions"), 0 if positions.dim() == 1 else n
+
+
+def _same_tokens(xs, others, what):
+    first = xs[0]
+    _need(first.dim() == 4 and len(xs) == len(others), what + " has to hold a tensor [batch][tokens][heads][head_dim] for each of x")
+    for t, o in zip(xs, others):
+        _need(t.dtype == o.dtype == first.dtype and t.dim() == 4 and t.shape == o.shape and t.shape[:2] == first.shape[:2] and t.shape[3] == first.shape[3],
+              "the tensors share type, sequences, tokens and head_dim, and %s the shapes of x" % what)
+
+
+def dpllm_norm_rope(x, weights, positions=None, freqs=None, eps=1e-6, out=None, scale=1.0, layout=DPLLM_ROPE_HALF):
+    """x: a tensor [batch][tokens][heads][head_dim], or a tuple of such that share everything but their heads (queries, keys).  weights: a tensor [head_dim] or [heads][head_dim]
+    for each (None: 1), all of one type.  positions, freqs, scale, layout: as for dpllm_rope; freqs None: the norm alone.  out: where the results go (x itself: in place); new tensors
+    unless given.  New results have a gradient with respect to x and the weights."""
+    xs = (x,) if isinstance(x, torch.Tensor) else tuple(x)
+    _need(0 < len(xs) <= 4, "dpllm_norm_rope takes 1 to 4 tensors")
+    outs = None if out is None else (out,) if isinstance(out, torch.Tensor) else tuple(out)
+    given = () if weights is None else (weights,) if isinstance(weights, torch.Tensor) else tuple(w for w in weights if w is not None)
+    if torch.is_grad_enabled() and any(t.requires_grad for t in (*xs, *given, *(outs or ()))):
+        _need(outs is None, "results that go into out have no gradient, but one of the tensors requires one")
+        ws = (None,) * len(xs) if weights is None else (weights,) if isinstance(weights, torch.Tensor) else tuple(weights)
+        made = _NormRope.apply(positions, freqs, eps, scale, layout, len(xs), *xs, *ws)
+        return made[0] if isinstance(x, torch.Tensor) else made
+    dtype = _dtype(xs[0], "x")
+    outs = tuple(torch.empty_like(t) for t in xs) if outs is None else outs
+    _same_tokens(xs, outs, "out")
+    views, into = [_view(t, "x") for t in xs], [_view(t, "out") for t in outs]
+    held, ws, strides, w_dtype = _norm_weights(xs, weights)
+    rotary, f, pos, pos_stride = _norm_plan(xs[0], positions, freqs)
+    b, n, _, d = xs[0].shape
+    m = len(xs)
+    _call(lib.dpllm_norm_rope((_Heads * m)(*views), (_Heads * m)(*into), (C.c_int * m)(*[t.shape[2] for t in xs]), ws, strides, w_dtype, eps, m, b, n, d, dtype, rotary, layout,
+                              f, scale, pos, pos_stride, _stream()))
+    return outs[0] if isinstance(x, torch.Tensor) else outs
+
+
+def dpllm_norm_rope_backward_workspace_bytes(heads, weight_strides, batch, tokens, head_dim):
+    m, n = len(heads), C.c_size_t(0)
+    _call(lib.dpllm_norm_rope_backward_workspace_bytes((C.c_int * m)(*heads), (C.c_int64 * m)(*weight_strides), m, batch, tokens, head_dim, C.byref(n)))
+    return n.value
+
+
+def dpllm_norm_rope_backward(x, grads, weights, positions=None, freqs=None, eps=1e-6, out=None, scale=1.0, layout=DPLLM_ROPE_HALF, wanted=None, workspace=None):
+    """The gradients of the inputs and of the weights of dpllm_norm_rope from those of its results, grads, as (like x, like weights).  out: where those of the inputs go (grads or x
+    themselves, say).  wanted: a truth value for each weight whether its gradient is (all are unless given; the others give None).  workspace: uint8, allocated for the call unless given."""
+    lone = isinstance(x, torch.Tensor)
+    xs, gs = (x,) if lone else tuple(x), (grads,) if isinstance(grads, torch.Tensor) else tuple(grads)
+    _need(0 < len(xs) <= 4, "dpllm_norm_rope_backward takes 1 to 4 tensors")
+    dtype = _dtype(xs[0], "x")
+    outs = tuple(torch.empty_like(t) for t in xs) if out is None else (out,) if isinstance(out, torch.Tensor) else tuple(out)
+    _same_tokens(xs, gs, "grads")
+    _same_tokens(xs, outs, "out")
+    views, grad_views, into = [_view(t, "x") for t in xs], [_view(t, "grads") for t in gs], [_view(t, "out") for t in outs]
+    held, ws, strides, w_dtype = _norm_weights(xs, weights, contiguous=True)
+    wanted = [w is not None and (wanted is None or bool(wanted[i])) for i, w in enumerate(held)]
+    made = tuple(torch.empty_like(w) if g else None for w, g in zip(held, wanted))
+    rotary, f, pos, pos_stride = _norm_plan(xs[0], positions, freqs)
+    b, n, _, d = xs[0].shape
+    m = len(xs)
+    heads = [t.shape[2] for t in xs]
+    if workspace is None and any(wanted):
+        need = dpllm_norm_rope_backward_workspace_bytes(heads, list(strides), b, n, d)
+        workspace = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
+    _call(lib.dpllm_norm_rope_backward((_Heads * m)(*views), (_Heads * m)(*grad_views), (_Heads * m)(*into), (C.c_int * m)(*heads), ws,
+                                       (C.c_void_p * m)(*[_ptr(g) for g in made]), strides, w_dtype, eps, m, b, n, d, dtype, rotary, layout, f, scale, pos, pos_stride,
+                                       *_space(workspace), _stream()))
+    return (outs[0], made[0]) if lone else (outs, made)
+
+
+class _NormRope(torch.autograd.Function):
+    """dpllm_norm_rope of tensors (or weights) that require a gradient."""
+
+    @staticmethod
+    def forward(ctx, positions, freqs, eps, scale, layout, n, *tensors):
+        xs, ws = tensors[:n], tensors[n:]
+        ctx.save_for_backward(positions, freqs, *tensors)
+        ctx.how = eps, scale, layout, n
+        return dpllm_norm_rope(xs, ws, positions, freqs, eps=eps, scale=scale, layout=layout)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, *grads):
+        positions, freqs, *tensors = ctx.saved_tensors
+        eps, scale, layout, n = ctx.how
+        needs = ctx.needs_input_grad[6:]
+        # (the gradient of a sum is one number for all elements: the last dimension has no stride)
+        grads = tuple(g if g.stride(3) == 1 or g.shape[3] == 1 else g.contiguous() for g in grads)
+        some = [i for i in range(n) if needs[i] or needs[n + i]]
+        made = [None] * (2 * n)
+        outs, weights = dpllm_norm_rope_backward(tuple(tensors[i] for i in some), tuple(grads[i] for i in some), tuple(tensors[n + i] for i in some), positions, freqs, eps=eps,
+                                                 scale=scale, layout=layout, wanted=[needs[n + i] for i in some])
+        for i, o, w in zip(some, outs, weights):
+            made[i], made[n + i] = o if needs[i] else None, w
+        return (None,) * 6 + tuple(made)
+
+
+class QuantizedCache:
+    """A paged cache of keys and values in 8 or 4 bits: views of the caller's tensors.  k, v: codes, uint8 [layers][pages][page][heads][bytes of a head] with the same strides; k_scales, v_scales:
+    float32 [layers][pages][page][heads], of DPLLM_CACHE_INT4 bfloat16 [layers][pages][page][heads][2] (scale, offset).  table: as of Cache.  The object holds the tensors alive."""
+
+    def __init__(self, k, v, k_scales, v_scales, format, table=None):
+        _need(format in (DPLLM_CACHE_E4M3, DPLLM_CACHE_INT8, DPLLM_CACHE_INT4), "unknown format %s" % (format,))
+        pair = format == DPLLM_CACHE_INT4
+        _need(k.dim() == 5 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype == torch.uint8,
+              "k and v have to be uint8 tensors [layers][pages][page][heads][bytes] of one shape and strides")
+        _need(k.stride(4) == 1 or k.shape[4] == 1, "the last dimension of k and v has to be contiguous")
+        of = (*k.shape[:4], 2) if pair else tuple(k.shape[:4])
+        _need(k_scales.shape == of and v_scales.shape == of and k_scales.stride() == v_scales.stride() and
+              k_scales.dtype == v_scales.dtype == (torch.bfloat16 if pair else torch.float32),
+              "k_scales and v_scales have to be %s tensors %s with the same strides" % ("bfloat16" if pair else "float32", list(of)))
+        _need(all(t.is_cuda and t.get_device() == k.get_device() for t in (k, v, k_scales, v_scales)), "codes and scales have to be on one device")
+        by = 2 if pair else 1
+        strides = [s if n > 1 else 0 for s, n in zip(k_scales.stride()[:4], of)]
+        _need(not pair or (k_scales.stride(4) == 1 and all(s % 2 == 0 for s in strides)), "scale and offset of a head have to lie side by side, and whole such pairs apart")
+        if table is not None:
+            _need(table.dtype == torch.int32 and table.is_cuda and table.get_device() == k.get_device() and table.dim() == 2 and
+                  (table.stride(1) == 1 or table.shape[1] == 1), "table has to be an int32 tensor [batch][pages per sequence] on the device of k and v")
+        self.k, self.v, self.k_scales, self.v_scales, self.format, self.table, self.device = k, v, k_scales, v_scales, format, table, k.get_device()
+        self.layers, self.pages, self.page, self.heads, size = k.shape
+        self.head_dim = 2 * size if pair else size
+        self.pages_per_seq = 1 if table is None else table.shape[1]
+        self.batch = self.pages if table is None else table.shape[0]
+        self.capacity = self.pages_per_seq * self.page
+        self.c = _QuantizedCache(_ptr(k), _ptr(v), _ptr(k_scales), _ptr(v_scales), *k.stride()[:4], *[s // by for s in strides], _ptr(table),
+                                 0 if table is None else table.stride(0), format, self.layers, self.pages, self.page, self.pages_per_seq, self.heads, self.head_dim)
+        self.address = C.addressof(self.c)
+
+    @classmethod
+    def zeros(cls, format, layers, pages, page, heads, head_dim, table=None):
+        """A new one on the current device."""
+        pair = format == DPLLM_CACHE_INT4
+        _need(not pair or head_dim % 2 == 0, "head_dim has to be even for DPLLM_CACHE_INT4")
+        codes = [torch.zeros(layers, pages, page, heads, head_dim // 2 if pair else head_dim, dtype=torch.uint8, device="cuda") for _ in range(2)]
+        scales = [torch.zeros(layers, pages, page, heads, *((2,) if pair else ()), dtype=torch.bfloat16 if pair else torch.float32, device="cuda") for _ in range(2)]
+        return cls(*codes, *scales, format, table)
+
+
+def dpllm_quantized_append(cache, lens, k_new, v_new, path=None, count=None, layer=0):
+    """dpllm_cache_append into a QuantizedCache; k_new and v_new are float16, bfloat16 or float32."""
+    _on(cache.k, "the cache")
+    if k_new.dim() == 4:
+        k_new, v_new = k_new.unsqueeze(0), v_new.unsqueeze(0)
+    _need(k_new.dim() == 5 and k_new.shape == v_new.shape and k_new.dtype == v_new.dtype and k_new.dtype in _DTYPES,
+          "k_new and v_new have to be [layers][batch][nodes][heads][head_dim] of one type")
+    layers, b, n, h, d = k_new.shape
+    _need((h, d) == (cache.heads, cache.head_dim) and b <= cache.batch, "k_new and v_new have to fit the cache's heads, head_dim and sequences")
+    _need(layers == 0 or (_on(k_new, "k_new") and _on(v_new, "v_new")), "k_new and v_new have to be device tensors")
+    if layers == 0:
+        return
+    _call(lib.dpllm_quantized_append(C.byref(cache.c), layer, layers, b, n, _index(lens, (b,), "lens"), _DTYPES[k_new.dtype], C.byref(_view(k_new[0], "k_new")),
+                                     k_new.stride(0), C.byref(_view(v_new[0], "v_new")), v_new.stride(0), _index(path, (b, n), "path"), n, _index(count, (b,), "count"), _stream()))
+
+
+def dpllm_quantized_read(cache, first, tokens, dtype=torch.bfloat16, count=None, layer=0, layers=None, out=None):
+    """What a QuantizedCache holds of `tokens` tokens from first[b] on (int32 [batch]; None: 0), as (keys, values) [batch][tokens][heads][head_dim], of `layers` layers from `layer` on
+    with a dimension more if that is given.  count: int32 [batch]; from there on, and where the cache holds nothing, are zeros.  out: a pair of tensors to be filled."""
+    _on(cache.k, "the cache")
+    b = cache.batch if first is None and count is None else (count if first is None else first).shape[0]
+    shape = (1 if layers is None else layers, b, tokens, cache.heads, cache.head_dim)
+    _need(dtype in _DTYPES, "dtype has to be float16, bfloat16 or float32")
+    if out is None:
+        k, v = (torch.empty(shape, dtype=dtype, device="cuda") for _ in range(2))
+    else:
+        k, v = (t.unsqueeze(0) if layers is None else t for t in out)
+        _need(k.shape == shape and v.shape == shape and k.dtype == v.dtype == dtype and _on(k, "out") and _on(v, "out"), "out has to be two device tensors %s of dtype" % (list(shape),))
+    _need(b <= cache.batch, "there are more sequences than the cache has")
+    if shape[0] > 0:
+        _call(lib.dpllm_quantized_read(C.byref(cache.c), layer, shape[0], b, tokens, _index(first, (b,), "first"), _index(count, (b,), "count"), _DTYPES[dtype],
+                                       C.byref(_view(k[0], "out")), k.stride(0), C.byref(_view(v[0], "out")), v.stride(0), _stream()))
+    return tuple(out) if out is not None else (k, v) if layers is not None else (k[0], v[0])
+
+
+def dpllm_quantized_attention_workspace_bytes(batch, nodes, heads, kv_heads, head_dim, max_len):
+    n = C.c_size_t(0)
+    _call(lib.dpllm_quantized_attention_workspace_bytes(batch, nodes, heads, kv_heads, head_dim, max_len, C.byref(n)))
+    return n.value
+
+
+def dpllm_quantized_attention(cache, layer, lens, q, k_new=None, v_new=None, mask=None, scale=None, out=None, lse=None, max_len=None, workspace=None):
+    """dpllm_tree_attention over a QuantizedCache; q, k_new, v_new and out are float16 or bfloat16.  The result has no gradient."""
+    _on(cache.k, "the cache")
+    dtype = _dtype(q, "q")
+    _need(q.dim() == 4 and q.shape[3] == cache.head_dim, "q has to be [batch][nodes][heads][head_dim] of the cache's head_dim")
+    b, n, h, d = q.shape
+    _need(b <= cache.batch, "q has more sequences than the cache")
+    new = (b, n, cache.heads, d)
+    _need((k_new is None) == (v_new is None), "k_new and v_new are given together or not at all")
+    if k_new is not None:
+        _need(k_new.shape == new and v_new.shape == new and k_new.dtype == v_new.dtype == q.dtype,
+              "k_new and v_new have to be [batch][nodes][kv heads][head_dim] of q's type")
+    if out is None:
+        out = torch.empty_like(q)
+    _need(out.shape == q.shape and out.dtype == q.dtype, "out has to have the shape and type of q")
+    if mask is not None:
+        _need(mask.dtype == torch.int64 and _on(mask, "mask") and mask.is_contiguous() and mask.dim() == 3 and mask.shape[0] in (1, b) and
+              mask.shape[1:] == (n, (n + 63) // 64), "mask has to be a contiguous int64 device tensor [batch or 1][nodes][ceil(nodes / 64)]")
+    _need(lse is None or (lse.dtype == torch.float32 and _on(lse, "lse") and lse.shape == (b, n, h) and lse.is_contiguous()),
+          "lse has to be a contiguous float32 device tensor [batch][nodes][heads]")
+    max_len = cache.capacity if max_len is None else min(max_len, cache.capacity)
+    if workspace is None:
+        need = dpllm_quantized_attention_workspace_bytes(b, n, h, cache.heads, d, max_len)
+        workspace = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
+    _call(lib.dpllm_quantized_attention(C.byref(cache.c), layer, b, n, h, dtype, _index(lens, (b,), "lens"), max_len, C.byref(_view(q, "q")),
+                                        None if k_new is None else C.byref(_view(k_new, "k_new")), None if v_new is None else C.byref(_view(v_new, "v_new")),
+                                        _ptr(mask), 0 if mask is None or mask.shape[0] == 1 else mask.stride(0), d ** -0.5 if scale is None else scale,
+                                        C.byref(_view(out, "out")), _ptr(lse), *_space(workspace), _stream()))
+    return out
+
+
+def dpllm_sample_workspace_bytes(rows, vocabulary, dtype):
+    n = C.c_size_t(0)
+    _call(lib.dpllm_sample_workspace_bytes(rows, vocabulary, dtype, C.byref(n)))
+    return n.value
+
+
+def dpllm_sample(logits, uniforms, temperature, top_k=None, top_p=None, min_p=None, words=None, kept=None, workspace=None):
+    """A word for every row of logits [rows][vocabulary], int32 [rows].  uniforms, temperature, top_p, min_p: float32 [rows]; top_k: int32 [rows]; the last three None: no such
+    filter.  words: a new tensor unless given.  kept: int32 [rows], to be filled with how many words could have been drawn.  workspace: uint8, allocated for the call unless given."""
+    dtype = _dtype(logits, "logits")
+    _need(logits.dim() == 2 and (logits.stride(1) == 1 or logits.shape[1] == 1 or logits.numel() == 0), "logits has to be [rows][vocabulary], the words contiguous")
+    n, v = logits.shape
+    for t, what in ((uniforms, "uniforms"), (temperature, "temperature"), (top_p, "top_p"), (min_p, "min_p")):
+        _need((t is None and what in ("top_p", "min_p")) or (t is not None and t.dtype == torch.float32 and _on(t, what) and tuple(t.shape) == (n,) and t.is_contiguous()),
+              "%s has to be a contiguous float32 device tensor [%d]" % (what, n))
+    words = torch.empty(n, dtype=torch.int32, device="cuda") if words is None else words
+    if workspace is None:
+        workspace = torch.empty(dpllm_sample_workspace_bytes(n, v, dtype), dtype=torch.uint8, device="cuda")
+    _call(lib.dpllm_sample(n, v, dtype, _ptr(logits), logits.stride(0), _ptr(uniforms), _ptr(temperature), _index(top_k, (n,), "top_k"), _ptr(top_p), _ptr(min_p),
+                           _index(words, (n,), "words"), _index(kept, (n,), "kept"), *_space(workspace), _stream()))
+    return words
 
 
 class Model:

@@ -1,0 +1,11 @@
+// The attention over a cache of int8 codes; see quantized_attention.hpp.
+#include <hip/hip_runtime.h>
+
+#include "quantized_launch.hpp"
+
+namespace dpllm {
+template <>
+void launch_quantized<kInt8>(int dtype, int head_dim, const QuantizedArgs& a, const AttentionPlan& p, hipStream_t s) {
+  launch_dtype<kInt8>(dtype, head_dim, a, p, s);
+}
+}  // namespace dpllm

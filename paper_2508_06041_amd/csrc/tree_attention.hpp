@@ -169,11 +169,15 @@ __device__ __forceinline__ void mask(Scores<MT>& s, const uint32_t (&seen)[MT]) 
     for (int i = 0; i < 8; ++i) s[mt][i / 4][i % 4] = (seen[mt] >> i) & 1 ? s[mt][i / 4][i % 4] : -INFINITY;
 }
 
-// The weights of a step, rounded for the value product, and their sum.  They are formed with the `top` there is: only where a lane's weights come to more than kLimit,
+// The weights of a step, rounded for the value product (or as they are), and their sum.  They are formed with the `top` there is: only where a lane's weights come to more than kLimit,
 // or a row has none, does top follow the largest score, with an exchange between lanes and a scaling of o, and the weights are formed again.  That is the first step with
 // a score and few after it (but all steps of a wavefront with a row that sees nothing, of which only nodes make some); all others look for no maximum at all.
-template <typename T, int MT, int DV>
-__device__ __forceinline__ void weigh(Rows<MT, DV>& r, Scores<MT>& s, float scale_log2, u32x4 (&w)[MT]) {
+// W: u32x4, or the weights as they are.
+struct Weights {
+  float w[8];
+};
+template <typename T, int MT, int DV, typename W>
+__device__ __forceinline__ void weigh(Rows<MT, DV>& r, Scores<MT>& s, float scale_log2, W (&w)[MT]) {
   constexpr float kLift = Matrix<T>::kLift;
   float x[MT][8], add[MT];
   auto form = [&]() {
@@ -226,8 +230,13 @@ __device__ __forceinline__ void weigh(Rows<MT, DV>& r, Scores<MT>& s, float scal
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     r.sum[mt] += add[mt];
+    if constexpr (sizeof(W) == sizeof(u32x4)) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[mt][i] = pack2<T>(x[mt][2 * i], x[mt][2 * i + 1]);
+      for (int i = 0; i < 4; ++i) w[mt][i] = pack2<T>(x[mt][2 * i], x[mt][2 * i + 1]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[mt].w[i] = x[mt][i];
+    }
   }
 }
 

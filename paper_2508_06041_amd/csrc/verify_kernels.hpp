@@ -7,6 +7,7 @@
 // Answers are whole numbers, so nothing may hang on the order of additions: logits are widened, and differences, exponentials and sums are kept, in
 // 64 bits; two orders of a sum of 10^5 terms differ by about 1e-14, and so do the numbers that a probability of 2^-24 steps is compared with.
 #pragma once
+#include "lanes.hpp"
 #include "token_common.hpp"
 
 namespace dpllm {
@@ -165,44 +166,6 @@ struct Chunk {
     take(raw);
   }
 };
-
-// The value of another lane: STEP 0 and 1 exchange inside four lanes, 2 and 3 the fours of eight and the eights of sixteen, 4 and 5 sixteens and halves.  With all six
-// every lane has met every other, without LDS; two lanes that meet form the same sum, so all end with the same bits.
-template <int STEP>
-__device__ __forceinline__ uint32_t other(uint32_t v) {
-  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-  if constexpr (STEP < 4) {
-    constexpr int control = STEP == 0 ? 0xb1 : STEP == 1 ? 0x4e : STEP == 2 ? 0x141 : 0x140;
-    return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, control, 0xf, 0xf, true);
-  } else {
-    const u32x2 p = STEP == 4 ? __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(v, v, false, false))
-                              : __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(v, v, false, false));
-    const uint32_t first = p[0], second = p[1];      // of a pair of rows (halves), in both
-    const bool upper = (threadIdx.x >> STEP) & 1;
-    return upper ? first : second;
-  }
-}
-template <int STEP>
-__device__ __forceinline__ float other(float v) { return __uint_as_float(other<STEP>(__float_as_uint(v))); }
-template <int STEP>
-__device__ __forceinline__ int other(int v) { return (int)other<STEP>((uint32_t)v); }
-template <int STEP>
-__device__ __forceinline__ double other(double v) {
-  const uint64_t w = __builtin_bit_cast(uint64_t, v);
-  return __builtin_bit_cast(double, (uint64_t)other<STEP>((uint32_t)(w >> 32)) << 32 | other<STEP>((uint32_t)w));
-}
-template <typename T, typename F>
-__device__ __forceinline__ T wave_all(T v, F f) {
-  v = f(v, other<0>(v));
-  v = f(v, other<1>(v));
-  v = f(v, other<2>(v));
-  v = f(v, other<3>(v));
-  v = f(v, other<4>(v));
-  return f(v, other<5>(v));
-}
-__device__ __forceinline__ double wave_sum(double v) {
-  return wave_all(v, [](double a, double b) { return a + b; });
-}
 
 // The value of one lane, which is the same for all.
 __device__ __forceinline__ double of_lane(double v, int lane) {

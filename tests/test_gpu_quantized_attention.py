@@ -1,0 +1,267 @@
+"""Attention over a cache in 8 or 4 bits against the formula in 64 bits, with what codes and scales stand for."""
+import math
+
+import pytest
+import torch
+
+import paper_2508_06041_amd as dp
+from test_gpu_quantized_cache import FORMS, decoded, ints, new_cache
+from test_gpu_tree_attention import TYPES, words
+
+pytestmark = pytest.mark.gpu
+
+
+def normal(*shape, seed, size=1.0):
+    return torch.randn(*shape, generator=torch.Generator().manual_seed(seed)) * size
+
+
+class Case:
+    """Inputs, and the answer in 64 bits with how far off it may be."""
+
+    def __init__(self, form, dtype, batch, nodes, heads, kv, dim, page, lens, mask="chain", seed=1, size=1.0, spare=3, new=True, scale=None, offset=0.0):
+        g = torch.Generator().manual_seed(seed)
+        self.form, self.t, self.lens = form, TYPES[dtype], lens
+        self.scale = dim ** -0.5 if scale is None else scale
+        each = max(1, -(-max(lens) // page))
+        pages = batch * each + spare
+        self.table = torch.randperm(pages, generator=g)[:batch * each].reshape(batch, each).to(torch.int32)
+        self.cache = new_cache(form, 2, pages, page, kv, dim, self.table.cuda(), fill=0x7e)      # (0x7f is NaN in e4m3)
+        self.cache.k_scales.fill_(math.nan)
+        self.cache.v_scales.fill_(math.nan)
+        most = max(max(lens), 1)
+        k, v = (normal(1, batch, most, kv, dim, seed=seed + i) + offset for i in (1, 2))
+        dp.dpllm_quantized_append(self.cache, torch.zeros(batch, dtype=torch.int32, device="cuda"), k.cuda(), v.cuda(), count=ints([max(n, 0) for n in lens]), layer=1)
+        self.q = normal(batch, nodes, heads, dim, seed=seed + 3, size=size).to(self.t)
+        self.k_new, self.v_new = (normal(batch, nodes, kv, dim, seed=seed + i).to(self.t) if new else None for i in (4, 5))
+        if mask == "chain":
+            self.sees = torch.ones(nodes, nodes, dtype=torch.bool).tril()[None].expand(batch, -1, -1)
+        elif mask == "tree":
+            self.sees = torch.zeros(batch, nodes, nodes, dtype=torch.bool)
+            for b in range(batch):
+                for i in range(nodes):
+                    if i:
+                        self.sees[b, i] = self.sees[b, int(torch.randint(0, i, (1,), generator=g))]
+                    self.sees[b, i, i] = True
+        else:                                    # anything, rows that see no node among it
+            self.sees = torch.rand(batch, nodes, nodes, generator=g) < 0.3
+            self.sees[:, ::3] = False
+        self.mask = None if mask == "chain" else words(self.sees)
+
+    def call(self, max_len=None, **kw):
+        lse = torch.full(self.q.shape[:3], 7.0, device="cuda")
+        new = [None if x is None else x.cuda() for x in (self.k_new, self.v_new)]
+        out = dp.dpllm_quantized_attention(self.cache, 1, ints(self.lens), self.q.cuda(), *new, mask=self.mask, scale=self.scale, lse=lse, max_len=max_len, **kw)
+        return out, lse
+
+    def plain(self):
+        b, n, h, d = self.q.shape
+        kv = self.cache.heads
+        out, lse = torch.zeros(b, n, h, d, dtype=torch.float64), torch.zeros(b, n, h, dtype=torch.float64)
+        self.bound, self.lse_bound = torch.zeros_like(out), torch.zeros_like(lse)
+        eps = torch.finfo(self.t).eps / 2
+        pools = [decoded(p[1], s[1], self.form).cuda() for p, s in ((self.cache.k, self.cache.k_scales), (self.cache.v, self.cache.v_scales))]
+        # how large codes times scales get, and the offset beside them, which may cancel
+        scales = self.cache.k_scales[1].double(), self.cache.v_scales[1].double()
+        if self.form == "int4":
+            parts = [(s[..., 1:].abs() + s[..., :1] * 7.5).expand(*s.shape[:-1], d) for s in scales]
+        else:
+            parts = [p.abs() for p in pools]
+        for s in range(b):
+            ids = self.table[s].tolist()
+            ok = torch.tensor([0 <= i < self.cache.pages for i in ids]).repeat_interleave(self.cache.page)
+            ids = [i if 0 <= i < self.cache.pages else 0 for i in ids]
+            length = max(0, min(self.lens[s], ok.numel()))
+            ok = ok[:length]
+            keys, values, key_parts, value_parts = (p[ids].flatten(0, 1)[:length] for p in (*pools, *parts))
+            sees, own = ok[None].expand(n, length), 0
+            if self.k_new is not None:
+                k, v = self.k_new[s].double().cuda(), self.v_new[s].double().cuda()
+                keys, values, key_parts, value_parts = torch.cat([keys, k]), torch.cat([values, v]), torch.cat([key_parts, k.abs()]), torch.cat([value_parts, v.abs()])
+                sees, own = torch.cat([sees, self.sees[s]], dim=1), n
+            sees = sees.cuda()
+            for i in range(h):
+                j = i * kv // h
+                q, k, v = self.q[s, :, i].double().cuda(), keys[:, j], values[:, j]
+                x = (q @ k.t().contiguous() * self.scale).masked_fill(~sees, -math.inf)
+                size = (q.abs() @ key_parts[:, j].t().contiguous() * abs(self.scale)).masked_fill(~sees, 0.0)
+                for r in range(n):               # only what the row sees, so that anything may stand elsewhere
+                    at = sees[r]
+                    if not at.any():
+                        lse[s, r, i] = -math.inf
+                        continue
+                    y, w = x[r, at], v[at]
+                    p = torch.softmax(y, 0)
+                    o = p @ w
+                    out[s, r, i], lse[s, r, i] = o.cpu(), torch.logsumexp(y, 0).cpu()
+                    # a score is a sum of d products in 32 bits (times a scale, plus an offset), and an exponent's error is a weight's relative one, in numerator and denominator; the
+                    # weight is rounded to the type (half a step; for the cached tokens of float16 to two bfloat16, 2^-16), the sums over the tokens are in 32 bits, and so is the
+                    # sum of the offsets; then the result is rounded
+                    score = 2.0 ** -23 * (d + 8) * size[r, at].max().item() + 2.0 ** -20
+                    some = (eps if own or self.t == torch.bfloat16 else 2.0 ** -15) + 2 * score + 2 * (at.sum().item() + 8) * 2.0 ** -24
+                    self.bound[s, r, i] = (some * (p @ value_parts[at][:, j]) + eps * o.abs()).cpu() + torch.finfo(self.t).smallest_normal * eps
+                    self.lse_bound[s, r, i] = score + at.sum().item() * 2.0 ** -24 + 2.0 ** -22 * (1 + abs(lse[s, r, i].item()))
+        return out, lse
+
+    def check(self, max_len=None):
+        got, lse = self.call(max_len)
+        want, want_lse = self.plain()
+        err = (got.double().cpu() - want).abs()
+        assert (err <= self.bound).all(), (err - self.bound).max()
+        assert torch.equal(torch.isinf(lse.cpu()), torch.isinf(want_lse))
+        fine = torch.isfinite(want_lse)
+        assert ((lse.double().cpu() - want_lse).abs()[fine] <= self.lse_bound[fine]).all()
+        return got
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("batch,nodes,heads,kv,dim,page,lens,mask", [
+    (1, 1, 1, 1, 64, 16, [1], "chain"), (1, 1, 32, 8, 128, 16, [900], "chain"), (1, 1, 8, 2, 64, 32, [333], "chain"), (2, 1, 8, 8, 96, 7, [77, 31], "chain"),
+    (3, 1, 4, 4, 256, 5, [33, 0, 64], "chain"), (2, 5, 8, 2, 64, 16, [40, 129], "tree"), (3, 13, 8, 1, 128, 64, [300, 1, 0], "tree"),
+    (2, 17, 6, 3, 96, 32, [65, 200], "any"), (2, 33, 4, 2, 256, 16, [100, 31], "any"), (1, 65, 2, 1, 64, 16, [50], "tree"), (1, 7, 7, 7, 128, 1, [95], "any"),
+    (5, 2, 16, 2, 128, 16, [0, 1, 31, 32, 33], "chain"), (1, 130, 3, 1, 128, 16, [70], "tree"), (2, 256, 2, 2, 64, 64, [10, 90], "tree")])
+def test_against_the_formula(form, dtype, batch, nodes, heads, kv, dim, page, lens, mask):
+    Case(form, dtype, batch, nodes, heads, kv, dim, page, lens, mask).check()
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("batch,nodes,heads,kv,dim,lens", [
+    (1, 1, 16, 2, 128, [9001]), (2, 4, 8, 2, 64, [5000, 12345]), (12, 1, 4, 1, 96, [1, 7000, 20, 300, 0, 64, 4097, 33, 2, 1000, 31, 512]), (1, 3, 8, 1, 256, [4100]),
+    (70, 1, 2, 1, 64, [i * 13 % 700 for i in range(70)]), (1, 40, 8, 2, 128, [6000])])
+def test_split_work(form, dtype, batch, nodes, heads, kv, dim, lens):
+    """Long contexts and many sequences, with the work split for what max_len says; how it is split changes no more than the order of sums."""
+    c = Case(form, dtype, batch, nodes, heads, kv, dim, 64, lens, "chain", seed=3)
+    c.check()
+    c.check(max_len=1)
+    a, b = c.call()[0], c.call()[0]
+    assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_keys_and_values_far_from_zero(form, dtype):
+    Case(form, dtype, 2, 3, 8, 2, 128, 16, [400, 77], "tree", offset=3.0).check()
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_scales_of_scores(form):
+    """A negative scale, none at all, scores so large that one token takes all."""
+    for scale in (-0.3, 0.0, 8.0):
+        Case(form, "bf16", 1, 4, 4, 2, 64, 16, [100], "tree", scale=scale).check()
+    Case(form, "f16", 1, 2, 4, 2, 64, 16, [100], size=100.0).check()
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_the_cache_alone_and_rows_that_see_nothing(form, dtype):
+    Case(form, dtype, 3, 5, 8, 2, 128, 16, [0, 40, 700], new=False).check()
+    c = Case(form, dtype, 3, 7, 8, 2, 64, 16, [0, 3, 0], "any")
+    got = c.check()
+    assert (got[0, ::3] == 0).all()
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_pages_that_do_not_exist(form):
+    c = Case(form, "f16", 3, 2, 4, 2, 64, 16, [112, 112, 112])
+    c.table[0, 2] = -1
+    c.table[1] = c.cache.pages
+    c.table[2, 0], c.table[2, 6] = 1 << 30, -7
+    c.cache.table.copy_(c.table)
+    c.check()
+    c.lens = [5000, -3, 112]      # past the pages, and negative
+    c.check()
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("nodes", [1, 20])
+def test_numbers_that_are_none(form, dtype, nodes):
+    """Whatever lies where nothing is seen changes nothing (the cache is full of it); a token whose head holds NaN makes NaN of those that see it."""
+    c = Case(form, dtype, 2, nodes, 8, 2, 128, 16, [50, 300])
+    bad = torch.full((2, 1, 2, 128), math.nan).cuda()
+    bad[:, :, 1] = 1.0             # the second head is a number
+    dp.dpllm_quantized_append(c.cache, ints([7, 123]), bad, bad, count=ints([1, 0]), layer=0)      # another layer
+    first, _ = c.call()
+    assert torch.isfinite(first).all()
+    good = torch.zeros(2, 1, 2, 128).cuda()
+    for k, v in ((bad, good), (good, bad)):
+        d = Case(form, dtype, 2, nodes, 8, 2, 128, 16, [50, 300])
+        dp.dpllm_quantized_append(d.cache, ints([7, 123]), k, v, count=ints([1, 0]), layer=1)
+        got, lse = d.call()
+        assert torch.isnan(got[0, :, :4]).all() and torch.isfinite(got[0, :, 4:]).all() and torch.equal(got[1], first[1])
+        assert torch.isnan(lse[0, :, :4]).all() == (k is not good)
+    # nodes: infinities and NaN that are not seen
+    if nodes > 1:
+        c.k_new[:, 5], c.v_new[:, 5] = math.nan, math.inf
+        c.v_new[:, 6] = math.nan
+        sees = torch.ones(nodes, nodes, dtype=torch.bool).tril()[None].expand(2, -1, -1).clone()
+        sees[:, :, 5:7] = False
+        sees[0, 19, 6] = True
+        c.mask = words(sees)
+        got, _ = c.call()
+        assert torch.isnan(got[0, 19]).all() and torch.isfinite(got[0, :19]).all() and torch.isfinite(got[1]).all()
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_layouts(form):
+    """Queries as slices of a projection, results in place of them, pages that hold head after head, one stretch per sequence."""
+    c = Case(form, "bf16", 2, 3, 8, 2, 128, 16, [20, 47])
+    want, _ = c.call()
+    qkv = torch.cat([c.q, c.k_new, c.v_new], 2).cuda()
+    got = dp.dpllm_quantized_attention(c.cache, 1, ints(c.lens), qkv[:, :, :8], qkv[:, :, 8:10], qkv[:, :, 10:], scale=c.scale)
+    assert torch.equal(got, want)
+    turned = [x.transpose(2, 3).contiguous().transpose(2, 3) for x in (c.cache.k, c.cache.v, c.cache.k_scales, c.cache.v_scales)]
+    other = dp.QuantizedCache(*turned, c.cache.format, c.cache.table)
+    assert torch.equal(dp.dpllm_quantized_attention(other, 1, ints(c.lens), qkv[:, :, :8], qkv[:, :, 8:10], qkv[:, :, 10:], scale=c.scale), want)
+    flat = [x[:, c.table.cuda().long()].flatten(2, 3) for x in (c.cache.k, c.cache.v, c.cache.k_scales, c.cache.v_scales)]
+    lone = dp.QuantizedCache(*flat, c.cache.format)
+    assert torch.equal(dp.dpllm_quantized_attention(lone, 1, ints(c.lens), qkv[:, :, :8], qkv[:, :, 8:10], qkv[:, :, 10:], scale=c.scale, max_len=48), want)
+
+
+def test_a_long_cache():
+    """Codes past 2^32 bytes."""
+    cache = dp.QuantizedCache(*(torch.zeros(1, 300, 16384, 8, 128, dtype=torch.uint8, device="cuda") for _ in range(2)),      # 5.0e9 bytes each
+                              *(torch.zeros(1, 300, 16384, 8, device="cuda") for _ in range(2)), dp.DPLLM_CACHE_INT8, ints([[299, 298, 0]]))
+    k, v = normal(1, 600, 8, 128, seed=1).cuda(), normal(1, 600, 8, 128, seed=2).cuda()
+    dp.dpllm_quantized_append(cache, ints([16000]), k, v)
+    q = (normal(1, 1, 8, 128, seed=3) * 20).half().cuda()
+    got = dp.dpllm_quantized_attention(cache, 0, ints([16600]), q)
+    held_k, held_v = (x[0].double() for x in dp.dpllm_quantized_read(cache, ints([16000]), 600, dtype=torch.float32))
+    x = torch.cat([torch.zeros(16000, 8, dtype=torch.float64, device="cuda"), (held_k * q[0, 0].double()).sum(-1) * 128 ** -0.5])
+    p = torch.softmax(x, 0)[16000:]
+    want = (p[:, :, None] * held_v).sum(0)
+    assert ((got[0, 0].double() - want).abs() <= 2.0 ** -10 * (p[:, :, None] * held_v.abs()).sum(0) + 2.0 ** -11 * want.abs() + 2.0 ** -24).all()
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_graphs_that_share_a_workspace_and_streams(form):
+    """Two captured graphs with one workspace, replayed in turns; lengths and tables are read when the kernels run."""
+    c = Case(form, "f16", 2, 2, 8, 2, 64, 16, [3000, 100])
+    need = dp.dpllm_quantized_attention_workspace_bytes(2, 2, 8, 2, 64, 3000)
+    space = torch.empty(need, dtype=torch.uint8, device="cuda")
+    lens, q = ints([3000, 100]), c.q.cuda()
+    outs = [torch.zeros_like(q) for _ in range(2)]
+    new = c.k_new.cuda(), c.v_new.cuda()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graphs = []
+    for i in range(2):
+        def step():
+            dp.dpllm_quantized_attention(c.cache, 1, lens, q, *new, scale=c.scale * (i + 1), out=outs[i], max_len=3000, workspace=space)
+        with torch.cuda.stream(side):
+            step()
+        torch.cuda.current_stream().wait_stream(side)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            step()
+        graphs.append(g)
+    for turn in range(4):
+        lens.copy_(torch.tensor([3000 - 700 * turn, 100 - 5 * turn]))
+        q.mul_(0.9)
+        want = [dp.dpllm_quantized_attention(c.cache, 1, lens, q, *new, scale=c.scale * (i + 1), max_len=3000) for i in range(2)]
+        torch.cuda.synchronize()
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, w) for o, w in zip(outs, want))
