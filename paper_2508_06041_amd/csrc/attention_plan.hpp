@@ -17,11 +17,11 @@ struct AttentionPlan {
   size_t part, stats, bytes;
 };
 
-inline AttentionPlan plan_attention(int batch, int nodes, int heads, int kv_heads, int head_dim, int64_t max_len, bool few = false) {
+inline AttentionPlan plan_attention(int batch, int nodes, int heads, int kv_heads, int head_dim, int64_t max_len) {
   AttentionPlan p;
   p.rows = nodes * (heads / kv_heads);
-  p.waves = p.rows <= 32 || few ? 0 : p.rows <= 128 || head_dim == 256 ? 4 : 8;
-  p.mt = head_dim == 256 || p.rows <= 16 || (p.waves > 0 && p.rows <= 64) ? 1 : 2;
+  p.waves = p.rows <= 32 ? 0 : p.rows <= 128 || head_dim == 256 ? 4 : 8;
+  p.mt = head_dim == 256 || p.rows <= 16 || (p.rows > 32 && p.rows <= 64) ? 1 : 2;
   p.tile = 16 * p.mt * std::max(p.waves, 1);
   p.row_tiles = (p.rows + p.tile - 1) / p.tile;
   // Workgroups: as many as run at once, two to a compute unit (one of eight wavefronts); more parts are more results to write and join (63 nodes over

@@ -11,11 +11,11 @@ using namespace dpllm;
 
 namespace dpllm {
 template <>
-void launch_quantized<kE4m3>(int, int, const QuantizedArgs&, const AttentionPlan&, hipStream_t);
+void launch_quantized<kE4m3>(int, int, const QuantizedArgs&, const QuantizedPlan&, hipStream_t);
 template <>
-void launch_quantized<kInt8>(int, int, const QuantizedArgs&, const AttentionPlan&, hipStream_t);
+void launch_quantized<kInt8>(int, int, const QuantizedArgs&, const QuantizedPlan&, hipStream_t);
 template <>
-void launch_quantized<kInt4>(int, int, const QuantizedArgs&, const AttentionPlan&, hipStream_t);
+void launch_quantized<kInt4>(int, int, const QuantizedArgs&, const QuantizedPlan&, hipStream_t);
 }  // namespace dpllm
 
 namespace {
@@ -172,7 +172,7 @@ int dpllm_quantized_attention_workspace_bytes(int batch, int nodes, int heads, i
   if (!bytes) return refuse(DPLLM_EINVAL, "%s: bytes is NULL", who);
   if (int rc = check_attention(who, batch, nodes, heads, kv_heads, head_dim)) return rc;
   if (max_len < 0) return refuse(DPLLM_ESHAPE, "%s: max_len %d", who, max_len);
-  *bytes = batch == 0 || nodes == 0 ? 0 : plan_attention(batch, nodes, heads, kv_heads, head_dim, max_len, true).bytes;
+  *bytes = batch == 0 || nodes == 0 ? 0 : plan_quantized(batch, nodes, heads, kv_heads, head_dim, max_len).bytes;
   return DPLLM_OK;
 }
 
@@ -196,7 +196,7 @@ int dpllm_quantized_attention(const dpllm_quantized_cache* cache, int layer, int
   if (!pieces(queries, 2) || !pieces(results, 2) || !pieces(keys, 2) || !pieces(values, 2) || ((uintptr_t)c.k | (uintptr_t)c.v) % 16 ||
       (c.layer_stride | c.page_stride | c.token_stride | c.head_stride) % 16)
     return refuse(DPLLM_EINVAL, "%s: tensors and codes have to be aligned to 16 bytes, with strides of whole 16 bytes", who);
-  const AttentionPlan p = plan_attention(batch, nodes, heads, c.heads, c.head_dim, std::min<int64_t>(max_len, (int64_t)c.pages_per_seq * c.page), true);
+  const QuantizedPlan p = plan_quantized(batch, nodes, heads, c.heads, c.head_dim, std::min<int64_t>(max_len, (int64_t)c.pages_per_seq * c.page));
   if (p.groups > 0x7fffff || (int64_t)batch * heads * nodes > 0x7fffff) return refuse(DPLLM_ESHAPE, "%s: %lld workgroups", who, (long long)p.groups);
   if (p.bytes > 0 && (!ws_dev || ws_bytes < p.bytes || (uintptr_t)ws_dev % 16))
     return refuse(DPLLM_ESTATE, "%s: needs a workspace of %zu bytes, aligned to 16", who, p.bytes);
@@ -209,6 +209,9 @@ int dpllm_quantized_attention(const dpllm_quantized_cache* cache, int layer, int
   a.scale_token = w.scale_token;
   a.scale_head = w.scale_head;
   fill_attention(a, p, batch, nodes, heads, c.heads, k_new != nullptr, scale);
+  a.least = p.least;
+  a.heads_at_once = p.heads;
+  a.turns = p.turns;
   a.q = view(queries);
   a.out = view(results);
   a.k_new = view(keys);

@@ -15,6 +15,7 @@ namespace dpllm {
 struct QuantizedArgs : AttentionArgs {      // cache: codes, strides in bytes
   const uint32_t *k_scales, *v_scales;      // of the layer; strides in words
   int64_t scale_page, scale_token, scale_head;
+  int heads_at_once, turns;                 // wavefronts of a workgroup: heads x turns
 };
 
 template <int FORMAT, int D>
@@ -23,6 +24,10 @@ struct Held {
   static constexpr int BITS = FORMAT == kInt4 ? 4 : 8;
   static constexpr int KW = D * BITS / 128;              // words of a key to a lane: a quarter of it
   static constexpr int VW = (DV * BITS + 31) / 32;       // words of a value to a lane
+  static constexpr int BYTES = D * BITS / 8;             // of a key or value
+  static constexpr int PIECES = BYTES / 16;
+  static constexpr int ROW = PIECES % 2 ? BYTES : BYTES + 16;      // in LDS: an odd number of pieces, so that sixteen rows are in as many banks
+  static constexpr int LOADS = (32 * PIECES + 63) / 64;  // pieces of 32 keys to a lane
 };
 
 // Dimension j of the values that lane n of sixteen holds.  Six to a lane are four and two, so that both are read at their alignment.
@@ -44,6 +49,15 @@ __device__ __forceinline__ Codes<N> load_codes(const char* p) {
 #pragma unroll
   for (int i = 0; i < N; ++i) c.w[i] = r.w[i];
   return c;
+}
+
+// 16 bytes of a token.  Heads that fill whole lines of 128 bytes are read once and need not stay in the caches (400000 tokens of 8 heads of 128 e4m3 codes, 845 MB: 187 us with them,
+// 168 past them); others share their lines with a neighbour, which is to find them there (in 4 bits 143 against 157).
+template <bool ONCE>
+__device__ __forceinline__ u32x4 load_piece(const char* p) {
+  const u32x4* at = reinterpret_cast<const u32x4*>(p);
+  if constexpr (ONCE) return __builtin_nontemporal_load(at);
+  return *at;
 }
 
 // Lane n's codes of a value that starts at p.
@@ -74,7 +88,7 @@ __device__ __forceinline__ u32x4 in_code_order(u32x4 x) {
 template <int FORMAT, typename T, int N>
 __device__ __forceinline__ u32x4 key_operand(const Codes<N>& c, int kk) {
   if constexpr (FORMAT == kInt4) {
-    const uint32_t even = level_bytes(c.w[kk]), odd = level_bytes(c.w[kk] >> 4);
+    const uint32_t even = level_bytes<false>(c.w[kk]), odd = level_bytes<true>(c.w[kk]);
     return u32x4{two_codes<FORMAT, T>(even, false), two_codes<FORMAT, T>(even, true), two_codes<FORMAT, T>(odd, false), two_codes<FORMAT, T>(odd, true)};
   } else {
     return u32x4{two_codes<FORMAT, T>(c.w[2 * kk], false), two_codes<FORMAT, T>(c.w[2 * kk], true), two_codes<FORMAT, T>(c.w[2 * kk + 1], false),
@@ -85,17 +99,18 @@ __device__ __forceinline__ u32x4 key_operand(const Codes<N>& c, int kk) {
 template <int FORMAT, int DV, int N>
 __device__ __forceinline__ void value_pairs(const Codes<N>& a, const Codes<N>& b, uint32_t (&pair)[DV]) {
   if constexpr (FORMAT == kInt4) {
+    auto half = [&](int first, uint32_t x, uint32_t y) {      // dimensions first, first + 2, ...
+      const uint32_t low = __builtin_amdgcn_perm(y, x, 0x05010400u), high = __builtin_amdgcn_perm(y, x, 0x07030602u);
+      if (first < DV) pair[first] = two_codes<FORMAT, bfloat_t>(low, false);
+      if (first + 2 < DV) pair[first + 2] = two_codes<FORMAT, bfloat_t>(low, true);
+      if (first + 4 < DV) pair[first + 4] = two_codes<FORMAT, bfloat_t>(high, false);
+      if (first + 6 < DV) pair[first + 6] = two_codes<FORMAT, bfloat_t>(high, true);
+    };
 #pragma unroll
-    for (int w = 0; w < N; ++w)
-#pragma unroll
-      for (int odd = 0; odd < 2; ++odd) {
-        const uint32_t x = level_bytes(a.w[w] >> (4 * odd)), y = level_bytes(b.w[w] >> (4 * odd));
-        const uint32_t low = __builtin_amdgcn_perm(y, x, 0x05010400u), high = __builtin_amdgcn_perm(y, x, 0x07030602u);
-        if (8 * w + odd < DV) pair[8 * w + odd] = two_codes<FORMAT, bfloat_t>(low, false);
-        if (8 * w + odd + 2 < DV) pair[8 * w + odd + 2] = two_codes<FORMAT, bfloat_t>(low, true);
-        if (8 * w + odd + 4 < DV) pair[8 * w + odd + 4] = two_codes<FORMAT, bfloat_t>(high, false);
-        if (8 * w + odd + 6 < DV) pair[8 * w + odd + 6] = two_codes<FORMAT, bfloat_t>(high, true);
-      }
+    for (int w = 0; w < N; ++w) {
+      half(8 * w, level_bytes<false>(a.w[w]), level_bytes<false>(b.w[w]));
+      half(8 * w + 1, level_bytes<true>(a.w[w]), level_bytes<true>(b.w[w]));
+    }
   } else {
 #pragma unroll
     for (int w = 0; w < N; ++w) {
@@ -139,6 +154,25 @@ __device__ __forceinline__ HeldPlace held_place(const QuantizedArgs& a, const Sh
   return p;
 }
 
+// Workgroups go to the eight parts of the chip in turns, and each part has a cache of its own with lines of 128 bytes, which hold one head of a token, or two.  So the heads
+// (and tiles of rows) of a slot are on the same part, next to one another: a token's heads are read together, and no line twice.
+// Of the heads, `heads` are taken by a workgroup.
+__device__ __forceinline__ void place_group(const QuantizedArgs& a, int heads, int& slot, int& h, int& row_tile) {
+  const uint32_t sets = (uint32_t)(a.kv_heads / heads), tiles = sets * a.row_tiles, even = (uint32_t)a.slots / 8 * 8;
+  uint32_t t;
+  if (blockIdx.x < even * tiles) {
+    const uint32_t j = blockIdx.x >> 3;
+    slot = (int)(j / tiles * 8 + (blockIdx.x & 7));
+    t = j % tiles;
+  } else {
+    const uint32_t j = blockIdx.x - even * tiles;
+    slot = (int)(even + j / tiles);
+    t = j % tiles;
+  }
+  h = (int)(t % sets) * heads;
+  row_tile = (int)(t / sets);
+}
+
 // Queries in the order of a lane's quarter of a key: element 8 kk + e of lane group g is g D / 4 + 8 kk + e of the head.
 template <int FORMAT, int D, int MT>
 __device__ __forceinline__ void load_quarters(const QuantizedArgs& a, int b, int h, int first, u32x4 (&q)[MT][D / 32], int (&node)[MT]) {
@@ -176,18 +210,74 @@ __device__ __forceinline__ void sum_queries(const u32x4 (&q)[MT][D / 32], float 
   }
 }
 
-// Scores of codes become scores of keys.  k: the words of the lane's eight tokens.
+// Scores of codes become scores of keys, with the scales (and offsets) of the lane's eight tokens.
 template <int FORMAT, int MT>
-__device__ __forceinline__ void scale_scores(Scores<MT>& s, const uint32_t (&k)[8], const float (&q_sum)[MT]) {
+__device__ __forceinline__ void scale_scores(Scores<MT>& s, const float (&scale)[8], const float (&offset)[8], const float (&q_sum)[MT]) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float by = scale_of<FORMAT>(k[i]);
+  for (int i = 0; i < 8; ++i)
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       const float x = s[mt][i / 4][i % 4];
-      s[mt][i / 4][i % 4] = FORMAT == kInt4 ? __builtin_fmaf(x, by, offset_of(k[i]) * q_sum[mt]) : x * by;
+      s[mt][i / 4][i % 4] = FORMAT == kInt4 ? __builtin_fmaf(x, scale[i], offset[i] * q_sum[mt]) : x * scale[i];
     }
+}
+
+// The parts of a row meet: a workgroup to a row, since a lone long sequence has hundreds of parts.  Groups of D / 4 threads take parts in turns, four elements to a thread, and meet
+// in LDS.  (A part that its rows saw nothing of has no top and has not been written; it may have a NaN for a sum, which is what the row is then.)
+template <typename T, int D, int THREADS>
+__global__ void __launch_bounds__(THREADS) quantized_join_kernel(const QuantizedArgs a, int rows_of_tile, Divide by_rows, Divide by_heads, Divide by_tile) {
+  constexpr int W = D / 4, G = THREADS / W, WAVES = THREADS / 64;
+  __shared__ float factors[THREADS], wave_tops[WAVES], wave_sums[WAVES];
+  __shared__ f32x4 meet[G][W];
+  const uint32_t bh = by_rows.of(blockIdx.x), r = blockIdx.x - bh * a.rows, b = by_heads.of(bh), h = bh - b * a.kv_heads, row_tile = by_tile.of(r);
+  const int2 place = a.places[b];
+  const int parts = place.y;
+  if (parts == 1) return;      // its workgroup has written the result
+  const int64_t first = part_row(a, place.x, h, row_tile, rows_of_tile) + (r - row_tile * rows_of_tile), step = (int64_t)a.kv_heads * a.row_tiles * rows_of_tile;
+  const int wave = threadIdx.x >> 6, group = threadIdx.x / W, at = 4 * (threadIdx.x % W);
+  float m = -INFINITY, s = 0.f;
+  f32x4 e{0, 0, 0, 0};
+  for (int p0 = 0; p0 < parts; p0 += THREADS) {
+    const int p = p0 + (int)threadIdx.x, here = min(THREADS, parts - p0);
+    const float2 mine = p < parts ? a.stats[first + p * step] : make_float2(-INFINITY, 0.f);
+    const float top = wave_all(mine.x, [](float x, float y) { return fmaxf(x, y); });
+    if ((threadIdx.x & 63) == 0) wave_tops[wave] = top;
+    __syncthreads();
+    float next = m;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) next = fmaxf(next, wave_tops[w]);
+    const float less = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - next) * a.scale_log2);
+    const float f = mine.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mine.x - next) * a.scale_log2);
+    const float add = wave_all(f * mine.y, [](float x, float y) { return x + y; });
+    factors[threadIdx.x] = f;
+    if ((threadIdx.x & 63) == 0) wave_sums[wave] = add;
+    __syncthreads();
+    s *= less;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) s += wave_sums[w];
+    e *= less;
+    m = next;
+    if (group < G)
+#pragma unroll 4
+      for (int i = group; i < here; i += G) {
+        const float by = factors[i];
+        const f32x4 v = *reinterpret_cast<const f32x4*>(a.part + (first + (p0 + i) * step) * D + at);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) e[j] += by == 0.f ? 0.f : by * v[j];
+      }
+    __syncthreads();
   }
+  if (group < G) meet[group][threadIdx.x % W] = e;
+  __syncthreads();
+  const int node = a.by_group.of(r), head = h * a.group + r - node * a.group;
+  if (group == 0) {
+#pragma unroll
+    for (int i = 1; i < G; ++i) e += meet[i][threadIdx.x];
+    const float by = one_over(s);
+    *reinterpret_cast<uint2*>(a.out.data + 2 * (b * a.out.batch_stride + node * a.out.token_stride + head * a.out.head_stride + at)) =
+        make_uint2(pack2<T>(e[0] * by, e[1] * by), pack2<T>(e[2] * by, e[3] * by));
+  }
+  if (a.lse != nullptr && threadIdx.x == 0) a.lse[((int64_t)b * a.nodes + node) * (a.kv_heads * a.group) + head] = log_sum<T>(m, s, a.scale);
 }
 
 // The kernel for few rows: as tree_attention_kernel, with steps of codes in front of those of the nodes.  A lane reads a quarter of each of two keys (16 to 64
@@ -197,27 +287,28 @@ template <int FORMAT, typename T, int D, int MT, int WAVES>
 __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) quantized_attention_kernel(const QuantizedArgs a) {
   typedef Held<FORMAT, D> H;
   constexpr int KK = D / 32, DV = D / 16, R = 16 * MT;
-  constexpr int PER = 4 * DV / WAVES;      // of a lane's 4 DV results, what a wavefront adds up in the end
+  constexpr int RUN = D == 96 ? DV : DV / 2;      // a wavefront adds up so many of a lane's 4 DV results at a time in the end
   constexpr bool TWO = __is_same(T, half_t);
-  __shared__ float sums[WAVES][4 * DV * MT][64];
+  // the tokens of a step of each wavefront, and in the end the wavefronts' results
+  constexpr int kTokens = 2 * kAttTile * H::ROW, kSums = 4 * DV * MT * 64 * (int)sizeof(float);
+  __shared__ __align__(16) char tokens[WAVES][kTokens > kSums ? kTokens : kSums];
   __shared__ float offsets[WAVES][MT][16];
   __shared__ float2 tops[WAVES][MT][16];
-  __shared__ __align__(16) int64_t places[WAVES][2][kAttTile];
-  __shared__ __align__(16) uint32_t words[WAVES][2][kAttTile];      // of keys, of values
+  __shared__ __align__(16) int64_t places[WAVES][kAttTile];
+  __shared__ __align__(16) float scales_of[WAVES][FORMAT == kInt4 ? 4 : 2][kAttTile];      // of keys, of values, offsets of keys, of values
   const int lane = threadIdx.x & 63, wave = scalar(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
-  uint32_t id = blockIdx.x;
-  const int h = id % a.kv_heads;
-  id /= a.kv_heads;
-  const int row_tile = id % a.row_tiles, slot = id / a.row_tiles;
+  int slot, first_head, row_tile;
+  place_group(a, a.heads_at_once, slot, first_head, row_tile);
+  const int turns = a.turns, turn = wave / a.heads_at_once, mate = wave - turn * a.heads_at_once, h = first_head + mate;
   const Share share = share_of(a, slot);
   if (share.b < 0) return;
   const int b = share.b, old_steps = steps_of(share.len), last = share.last, last_old = min(last, old_steps);
-  if (share.part == 0 && h == 0 && row_tile == 0 && threadIdx.x == 0 && a.places != nullptr) a.places[b] = make_int2(slot, share.parts);
+  if (share.part == 0 && first_head == 0 && row_tile == 0 && threadIdx.x == 0 && a.places != nullptr) a.places[b] = make_int2(slot, share.parts);
 
   u32x4 q[MT][KK];
   float q_sum[MT] = {}, offset[MT] = {};
   int node[MT];
-  int step = share.first + wave;
+  int step = share.first + turn;
   Lookup next = ask_held(a, share, last_old, step);
   load_quarters<FORMAT, D, MT>(a, b, h, row_tile * R, q, node);
   if (FORMAT == kInt4) sum_queries<T, D, MT>(q, q_sum);
@@ -226,24 +317,31 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) quantized_attent
   const int k_token = 8 * (n >> 2) + (n & 3);      // of the first 16; the second are 4 further
   const char *cache_k = a.cache.k + h * a.cache.head_stride, *cache_v = a.cache.v + h * a.cache.head_stride;
   const uint32_t* scales = (lane < kAttTile ? a.k_scales : a.v_scales) + h * a.scale_head;
+  // A wavefront loads the keys and values of a step as they lie, 16 bytes to a lane and neighbours to neighbours, and turns them round in LDS: a lane's own quarter of a key is
+  // next to no other lane's, and the cache would be asked for every lane by itself (four times the accesses, 500 a step, which is what bound it).
   struct Tokens {
-    Codes<H::KW> k[2];
-    Codes<H::VW> v[8];
+    u32x4 k[H::LOADS], v[H::LOADS];
     uint32_t word, there;
   };
-  auto load = [&](int step, int turn, Tokens& x) {
+  char* const turn_k = tokens[wave];
+  char* const turn_v = tokens[wave] + kAttTile * H::ROW;
+  auto load = [&](int step, Tokens& x) {
     const HeldPlace mine = held_place(a, share, last_old, step, next);
+    // loads come back in their order: the places of the step behind this one are asked for in front of its tokens, so that nobody waits for those to look a place up
+    next = ask_held(a, share, last_old, step + turns);
     x.word = scales[mine.scale_at];
     if (!mine.there) x.word = 0u;
-    if (lane < kAttTile) places[wave][turn][lane] = mine.at;
+    if (lane < kAttTile) places[wave][lane] = mine.at;
     x.there = (uint32_t)__ballot(mine.there);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int half = 0; half < 2; ++half) x.k[half] = load_codes<H::KW>(cache_k + places[wave][turn][k_token + 4 * half] + g * (D * H::BITS / 32));
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x.v[i] = load_value<FORMAT, D>(cache_v + places[wave][turn][8 * g + i], n);
-    next = ask_held(a, share, last_old, step + WAVES);
+    for (int i = 0; i < H::LOADS; ++i) {
+      const int piece = 64 * i + lane, row = min(piece / H::PIECES, kAttTile - 1);
+      const int key = 8 * ((row & 15) >> 2) + (row & 3) + 4 * (row >> 4);      // as score() numbers the tokens
+      x.k[i] = load_piece<H::BYTES % 128 == 0>(cache_k + places[wave][key] + 16 * (piece % H::PIECES));
+      x.v[i] = load_piece<H::BYTES % 128 == 0>(cache_v + places[wave][row] + 16 * (piece % H::PIECES));
+    }
   };
   // The sums of offsets are relative to the rows' tops too.
   auto follow = [&](const float (&before)[MT]) {
@@ -253,27 +351,45 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) quantized_attent
   };
   auto attend = [&](Tokens& x) {
     const bool all = x.there == 0xffffffffu;
-    words[wave][lane >> 5][lane & 31] = x.word;
+    scales_of[wave][lane >> 5][lane & 31] = scale_of<FORMAT>(x.word);
+    if (FORMAT == kInt4) scales_of[wave][2 + (lane >> 5)][lane & 31] = offset_of(x.word);
+#pragma unroll
+    for (int i = 0; i < H::LOADS; ++i) {
+      const int piece = 64 * i + lane, at = piece / H::PIECES * H::ROW + 16 * (piece % H::PIECES);
+      if (32 * H::PIECES % 64 != 0 && piece >= 32 * H::PIECES) continue;
+      *reinterpret_cast<u32x4*>(turn_k + at) = x.k[i];
+      *reinterpret_cast<u32x4*>(turn_v + at) = x.v[i];
+    }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    uint32_t k_word[8], v_word[8];
+    auto eight = [&](int which, float (&to)[8]) {      // of the lane's tokens
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const u32x4 p = *reinterpret_cast<const u32x4*>(&words[wave][0][8 * g + 4 * i]), r = *reinterpret_cast<const u32x4*>(&words[wave][1][8 * g + 4 * i]);
+      for (int i = 0; i < 2; ++i) {
+        const f32x4 p = *reinterpret_cast<const f32x4*>(&scales_of[wave][which][8 * g + 4 * i]);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        k_word[4 * i + j] = p[j];
-        v_word[4 * i + j] = r[j];
+        for (int j = 0; j < 4; ++j) to[4 * i + j] = p[j];
       }
+    };
+    float k_scale[8], v_scale[8], k_offset[8], v_offset[8];
+    eight(0, k_scale);
+    eight(1, v_scale);
+    if (FORMAT == kInt4) {
+      eight(2, k_offset);
+      eight(3, v_offset);
     }
     u32x4 k[2][KK];
 #pragma unroll
-    for (int half = 0; half < 2; ++half)
+    for (int half = 0; half < 2; ++half) {
+      const Codes<H::KW> codes = load_codes<H::KW>(turn_k + (16 * half + n) * H::ROW + g * (H::BYTES / 4));
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) k[half][kk] = key_operand<FORMAT, T>(x.k[half], kk);
+      for (int kk = 0; kk < KK; ++kk) k[half][kk] = key_operand<FORMAT, T>(codes, kk);
+    }
+    Codes<H::VW> v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = load_value<FORMAT, D>(turn_v + (8 * g + i) * H::ROW, n);
     Scores<MT> s;
     score<T, D, MT>(q, k, s);
-    scale_scores<FORMAT, MT>(s, k_word, q_sum);
+    scale_scores<FORMAT, MT>(s, k_scale, k_offset, q_sum);
     if (!all) {
       uint32_t seen[MT];
 #pragma unroll
@@ -283,7 +399,7 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) quantized_attent
 #pragma unroll
       for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int j = 0; j < H::VW; ++j) x.v[i].w[j] = (x.there >> (8 * g + i)) & 1 ? x.v[i].w[j] : 0u;
+        for (int j = 0; j < H::VW; ++j) v[i].w[j] = (x.there >> (8 * g + i)) & 1 ? v[i].w[j] : 0u;
     }
     Weights w[MT];
     float before[MT];
@@ -296,36 +412,36 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) quantized_attent
     for (int mt = 0; mt < MT; ++mt) {
       if (FORMAT == kInt4)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) offset[mt] = __builtin_fmaf(w[mt].w[i], offset_of(v_word[i]), offset[mt]);
+        for (int i = 0; i < 8; ++i) offset[mt] = __builtin_fmaf(w[mt].w[i], v_offset[i], offset[mt]);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) w[mt].w[i] *= scale_of<FORMAT>(v_word[i]);
+      for (int i = 0; i < 8; ++i) w[mt].w[i] *= v_scale[i];
       p[mt] = rounded(w[mt].w);
       if (TWO) rest[mt] = rest_of(w[mt].w, p[mt]);
     }
     uint32_t pairs[4][DV];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) value_pairs<FORMAT, DV>(x.v[2 * i], x.v[2 * i + 1], pairs[i]);
+    for (int i = 0; i < 4; ++i) value_pairs<FORMAT, DV>(v[2 * i], v[2 * i + 1], pairs[i]);
 #pragma unroll
-    for (int j = 0; j < DV; ++j) {
-      const u32x4 t{pairs[0][j], pairs[1][j], pairs[2][j], pairs[3][j]};
+    for (int j = 0; j < DV; ++j)
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        rows.o[mt][j] = Matrix<bfloat_t>::mad(t, p[mt], rows.o[mt][j]);
-        if (TWO) rows.o[mt][j] = Matrix<bfloat_t>::mad(t, rest[mt], rows.o[mt][j]);
-      }
-    }
+      for (int mt = 0; mt < MT; ++mt) rows.o[mt][j] = Matrix<bfloat_t>::mad(u32x4{pairs[0][j], pairs[1][j], pairs[2][j], pairs[3][j]}, p[mt], rows.o[mt][j]);
+    if (TWO)
+#pragma unroll
+      for (int j = 0; j < DV; ++j)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) rows.o[mt][j] = Matrix<bfloat_t>::mad(u32x4{pairs[0][j], pairs[1][j], pairs[2][j], pairs[3][j]}, rest[mt], rows.o[mt][j]);
   };
   if (step < last_old) {
     Tokens x, y;
-    load(step, 0, x);
-    for (; step < last_old; step += 2 * WAVES) {
-      load(step + WAVES, 1, y);
+    load(step, x);
+    for (; step < last_old; step += 2 * turns) {
+      load(step + turns, y);
       attend(x);
-      if (step + WAVES >= last_old) {
-        step += WAVES;
+      if (step + turns >= last_old) {
+        step += turns;
         break;
       }
-      load(step + 2 * WAVES, 0, x);
+      load(step + 2 * turns, x);
       attend(y);
     }
   }
@@ -334,7 +450,7 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) quantized_attent
   const char *new_k = a.k_new.data + 2 * (b * a.k_new.batch_stride + h * a.k_new.head_stride),
              *new_v = a.v_new.data + 2 * (b * a.v_new.batch_stride + h * a.v_new.head_stride);
   bool odd = false;      // among the values is something that is no finite number
-  for (; step < last; step += WAVES) {
+  for (; step < last; step += turns) {
     const int t0 = (step - old_steps) * kAttTile, here = a.seen_nodes - t0;
     u32x4 k[2][KK], w[MT];
     Scores<MT> s;
@@ -379,7 +495,7 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) quantized_attent
   if (__any(odd)) {      // a value above a weight of zero is left out; a weight above zero changes no infinity and no NaN
 #pragma unroll 1
     for (int t = max(share.first - old_steps, 0) * kAttTile; t < min((last - old_steps) * kAttTile, a.seen_nodes); ++t) {
-      if ((old_steps + t / kAttTile - share.first) % WAVES != wave) continue;
+      if ((old_steps + t / kAttTile - share.first) % turns != turn) continue;
       const T* values = reinterpret_cast<const T*>(new_v) + t * a.v_new.token_stride;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -393,80 +509,106 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) quantized_attent
     }
   }
 
-  // the wavefronts' rows meet: each wavefront adds up its part of the elements
+  // Elements [from, from + L) of the four times DV of row r: where they go.
+  auto put = [&](auto length, int mt, int r, int from, const float* e, float m, float s) {
+    constexpr int L = decltype(length)::value;
+    const int d = value_dim<D>(4 * g + from / DV, from % DV);
+    if (share.parts == 1) {
+      const float by = one_over(s);
+      uint32_t w[L / 2];
+#pragma unroll
+      for (int j = 0; j < L / 2; ++j) w[j] = pack2<T>(e[2 * j] * by, e[2 * j + 1] * by);
+      store_words(a.out.data + 2 * (b * a.out.batch_stride + node[mt] * a.out.token_stride + (h * a.group + r - node[mt] * a.group) * a.out.head_stride + d), w);
+    } else if (m != -INFINITY) {
+      uint32_t w[L];
+#pragma unroll
+      for (int j = 0; j < L; ++j) w[j] = __builtin_bit_cast(uint32_t, e[j]);
+      store_words(reinterpret_cast<char*>(a.part + (part_row(a, slot, h, row_tile, R) + mt * 16 + n) * D + d), w);
+    }
+  };
+  auto put_run = [&](int mt, int r, int from, const float* e, float m, float s) {
+    if constexpr (D == 96) {
+      put(std::integral_constant<int, 4>(), mt, r, from, e, m, s);
+      put(std::integral_constant<int, 2>(), mt, r, from + 4, e + 4, m, s);
+    } else {
+      put(std::integral_constant<int, RUN>(), mt, r, from, e, m, s);
+    }
+  };
+  auto put_stats = [&](int mt, int r, float m, float s) {
+    if (share.parts != 1)
+      a.stats[part_row(a, slot, h, row_tile, R) + mt * 16 + n] = make_float2(m, s);
+    else if (a.lse != nullptr)
+      a.lse[((int64_t)b * a.nodes + node[mt]) * (a.kv_heads * a.group) + h * a.group + r - node[mt] * a.group] = log_sum<T>(m, s, a.scale);
+  };
+  float sum[MT];
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
-    float s = rows.sum[mt];
-    s += __shfl_xor(s, 16);
-    s += __shfl_xor(s, 32);
-    float f = offset[mt];
+    sum[mt] = rows.sum[mt] + __shfl_xor(rows.sum[mt], 16);
+    sum[mt] += __shfl_xor(sum[mt], 32);
     if (FORMAT == kInt4) {
-      f += __shfl_xor(f, 16);
-      f += __shfl_xor(f, 32);
+      offset[mt] += __shfl_xor(offset[mt], 16);
+      offset[mt] += __shfl_xor(offset[mt], 32);
     }
+  }
+  if (turns == 1) {      // every wavefront has a head to itself
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      const int r = row_tile * R + mt * 16 + n;
+      if (r >= a.rows) continue;
+#pragma unroll
+      for (int from = 0; from < 4 * DV; from += RUN) {
+        float e[RUN];
+#pragma unroll
+        for (int j = 0; j < RUN; ++j) e[j] = rows.o[mt][(from + j) % DV][(from + j) / DV] + offset[mt];
+        put_run(mt, r, from, e, rows.top[mt], sum[mt]);
+      }
+      if (g == 0) put_stats(mt, r, rows.top[mt], sum[mt]);
+    }
+    return;
+  }
+  // the rows of the wavefronts of a head meet: each adds up its part of the elements
+  auto sums_of = [&](int w) { return reinterpret_cast<float*>(tokens[w]); };
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
     if (g == 0) {
-      tops[wave][mt][n] = make_float2(rows.top[mt], s);
-      offsets[wave][mt][n] = f;
+      tops[wave][mt][n] = make_float2(rows.top[mt], sum[mt]);
+      offsets[wave][mt][n] = offset[mt];
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int j = 0; j < DV; ++j) sums[wave][(mt * 4 + i) * DV + j][lane] = rows.o[mt][j][i];
+      for (int j = 0; j < DV; ++j) sums_of(wave)[((mt * 4 + i) * DV + j) * 64 + lane] = rows.o[mt][j][i];
   }
   __syncthreads();
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     const int r = row_tile * R + mt * 16 + n;
-    float m = -INFINITY, s = 0.f, f[WAVES], plus = 0.f;
+    float m = -INFINITY, s = 0.f, plus = 0.f, f[WAVES];
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) m = fmaxf(m, tops[w][mt][n].x);
+    for (int t = 0; t < WAVES; ++t)
+      if (t < turns) m = fmaxf(m, tops[mate + t * a.heads_at_once][mt][n].x);
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-      f[w] = tops[w][mt][n].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((tops[w][mt][n].x - m) * a.scale_log2);
-      s += tops[w][mt][n].y * f[w];
-      if (FORMAT == kInt4) plus += offsets[w][mt][n] * f[w];
-    }
-    float e[PER];
-#pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      e[j] = plus;
-#pragma unroll
-      for (int w = 0; w < WAVES; ++w) e[j] += sums[w][mt * 4 * DV + wave * PER + j][lane] * f[w];
+    for (int t = 0; t < WAVES; ++t) {
+      f[t] = 0.f;
+      if (t >= turns) continue;
+      const float2 x = tops[mate + t * a.heads_at_once][mt][n];
+      f[t] = x.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((x.x - m) * a.scale_log2);
+      s += x.y * f[t];
+      if (FORMAT == kInt4) plus += offsets[mate + t * a.heads_at_once][mt][n] * f[t];
     }
     if (r >= a.rows) continue;
-    const bool whole = share.parts == 1;
-    const int head = h * a.group + r - node[mt] * a.group;
-    const float by = one_over(s);
-    char* out = a.out.data + 2 * (b * a.out.batch_stride + node[mt] * a.out.token_stride + head * a.out.head_stride);
-    const int64_t row = part_row(a, slot, h, row_tile, R) + mt * 16 + n;
-    // the elements wave * PER ... of [4][DV], in runs that lie side by side
-    auto put = [&](auto length, int from) {
-      constexpr int L = decltype(length)::value;
-      const int d = value_dim<D>(4 * g + (wave * PER + from) / DV, (wave * PER + from) % DV);
-      if (whole) {
-        uint32_t w[L / 2];
+    for (int from = turn * RUN; from < 4 * DV; from += turns * RUN) {
+      float e[RUN];
 #pragma unroll
-        for (int j = 0; j < L / 2; ++j) w[j] = pack2<T>(e[from + 2 * j] * by, e[from + 2 * j + 1] * by);
-        store_words(out + 2 * d, w);
-      } else if (m != -INFINITY) {
-        uint32_t w[L];
+      for (int j = 0; j < RUN; ++j) {
+        e[j] = plus;
 #pragma unroll
-        for (int j = 0; j < L; ++j) w[j] = __builtin_bit_cast(uint32_t, e[from + j]);
-        store_words(reinterpret_cast<char*>(a.part + row * D + d), w);
+        for (int t = 0; t < WAVES; ++t)
+          if (t < turns) e[j] += sums_of(mate + t * a.heads_at_once)[(mt * 4 * DV + from + j) * 64 + lane] * f[t];
       }
-    };
-    if constexpr (D == 96) {
-      put(std::integral_constant<int, 4>(), 0);
-      put(std::integral_constant<int, 2>(), 4);
-    } else {
-      put(std::integral_constant<int, PER>(), 0);
+      put_run(mt, r, from, e, m, s);
     }
-    if (g == 0 && wave == 0) {
-      if (!whole)
-        a.stats[row] = make_float2(m, s);
-      else if (a.lse != nullptr)
-        a.lse[((int64_t)b * a.nodes + node[mt]) * (a.kv_heads * a.group) + head] = log_sum<T>(m, s, a.scale);
-    }
+    if (g == 0 && turn == 0) put_stats(mt, r, m, s);
   }
 }
 

@@ -5,7 +5,7 @@
 
 namespace dpllm {
 template <>
-void launch_quantized<kE4m3>(int dtype, int head_dim, const QuantizedArgs& a, const AttentionPlan& p, hipStream_t s) {
+void launch_quantized<kE4m3>(int dtype, int head_dim, const QuantizedArgs& a, const QuantizedPlan& p, hipStream_t s) {
   launch_dtype<kE4m3>(dtype, head_dim, a, p, s);
 }
 }  // namespace dpllm

@@ -41,8 +41,13 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
-// Four levels, a byte each with the sign in bit 3 and the magnitude m below, as e4m3 numbers of size (2m + 1) / 512.
-__device__ __forceinline__ uint32_t level_bytes(uint32_t x) { return (((x & 0x07070707u) << 1) | 0x01010101u) | ((x & 0x08080808u) << 4); }
+// The four levels in the lower (ODD: upper) halves of four bytes, a sign and a magnitude m each, as e4m3 numbers of size (2m + 1) / 512: that type's numbers below 1/32 are whole 512ths, so the
+// size's byte is 2m + 1, which comes out of a table of eight.
+template <bool ODD>
+__device__ __forceinline__ uint32_t level_bytes(uint32_t x) {
+  const uint32_t size = __builtin_amdgcn_perm(0x0f0d0b09u, 0x07050301u, (ODD ? x >> 4 : x) & 0x07070707u);
+  return ((ODD ? x : x << 4) & 0x80808080u) | (size & ~0x80808080u);
+}
 
 // Two of four codes (the lower two or the upper two bytes; of int4 level_bytes) as T.
 template <int FORMAT, typename T>
@@ -325,8 +330,8 @@ __global__ void __launch_bounds__(kQuantThreads) quantized_read_kernel(const Deq
       }
     }
     if (FORMAT == kInt4) {
-      if (W > 1) w[W - 1] = level_bytes(apart(w[0] >> 16));
-      w[0] = level_bytes(apart(w[0] & 0xffffu));
+      if (W > 1) w[W - 1] = level_bytes<false>(apart(w[0] >> 16));
+      w[0] = level_bytes<false>(apart(w[0] & 0xffffu));
     }
     float x[E];
 #pragma unroll

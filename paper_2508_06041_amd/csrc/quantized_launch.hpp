@@ -5,13 +5,41 @@
 
 namespace dpllm {
 
+// The split over a quantised cache.
+struct QuantizedPlan : AttentionPlan {
+  int heads, turns;      // of the kernel for few rows: kv heads that share a workgroup, and wavefronts to each
+  int least;             // steps of the smallest part worth a workgroup
+};
+
+inline QuantizedPlan plan_quantized(int batch, int nodes, int heads, int kv_heads, int head_dim, int64_t max_len) {
+  QuantizedPlan p{};
+  p.rows = nodes * (heads / kv_heads);
+  p.mt = head_dim == 256 || p.rows <= 16 ? 1 : 2;
+  p.tile = 16 * p.mt;
+  p.row_tiles = (p.rows + p.tile - 1) / p.tile;
+  const int64_t steps = (max_len + kAttTile - 1) / kAttTile + (nodes + kAttTile - 1) / kAttTile;
+  p.lone = p.mt == 1 && (head_dim == 64 || head_dim == 128) && steps <= 14;
+  p.heads = p.lone ? 1 : kv_heads % 4 == 0 ? 4 : kv_heads % 2 == 0 ? 2 : 1;
+  p.turns = (p.lone ? 8 : kAttWaves) / p.heads;
+  p.least = p.turns;
+  const int64_t tiles = (int64_t)kv_heads / p.heads * p.row_tiles;
+  const int64_t most = batch * ((steps + p.least - 1) / p.least), fill = (512 + tiles - 1) / tiles;
+  p.slots = p.lone ? batch : (int)std::max<int64_t>(batch, std::min(most, fill >= 2 * batch ? fill : 3 * (int64_t)batch));
+  p.groups = p.slots * tiles;
+  const size_t part_rows = p.slots == batch ? 0 : (size_t)p.slots * kv_heads * p.row_tiles * p.tile;
+  p.part = part_rows * head_dim * sizeof(float);
+  p.stats = part_rows * sizeof(float2);
+  p.bytes = part_rows == 0 ? 0 : p.part + p.stats + (size_t)batch * sizeof(int2);
+  return p;
+}
+
 template <int FORMAT>
-void launch_quantized(int dtype, int head_dim, const QuantizedArgs& a, const AttentionPlan& p, hipStream_t s);
+void launch_quantized(int dtype, int head_dim, const QuantizedArgs& a, const QuantizedPlan& p, hipStream_t s);
 
 namespace {
 
 template <int FORMAT, typename T, int D>
-void launch_kernel(const QuantizedArgs& a, const AttentionPlan& p, hipStream_t s) {
+void launch_kernel(const QuantizedArgs& a, const QuantizedPlan& p, hipStream_t s) {
   const dim3 groups((unsigned)p.groups);
   if constexpr (D == 64 || D == 128)
     if (p.lone) hipLaunchKernelGGL((quantized_attention_kernel<FORMAT, T, D, 1, 8>), groups, dim3(8 * 64), 0, s, a);
@@ -19,14 +47,17 @@ void launch_kernel(const QuantizedArgs& a, const AttentionPlan& p, hipStream_t s
   if constexpr (D < 256)
     if (p.waves == 0 && p.mt == 2) hipLaunchKernelGGL((quantized_attention_kernel<FORMAT, T, D, 2, kAttWaves>), groups, dim3(kAttWaves * 64), 0, s, a);
   if (p.bytes > 0) {
-    const uint32_t all_rows = (uint32_t)a.batch * a.kv_heads * a.rows;
-    hipLaunchKernelGGL((tree_attention_join_kernel<T, D>), dim3((all_rows + 3) / 4), dim3(256), 0, s, a, p.tile, Divide::by(a.rows), Divide::by(a.kv_heads),
-                       Divide::by(p.tile), all_rows);
+    const dim3 rows((uint32_t)a.batch * a.kv_heads * a.rows);
+    const Divide by_rows = Divide::by(a.rows), by_heads = Divide::by(a.kv_heads), by_tile = Divide::by(p.tile);
+    if (p.slots >= 32 * a.batch)
+      hipLaunchKernelGGL((quantized_join_kernel<T, D, 512>), rows, dim3(512), 0, s, a, p.tile, by_rows, by_heads, by_tile);
+    else
+      hipLaunchKernelGGL((quantized_join_kernel<T, D, 128>), rows, dim3(128), 0, s, a, p.tile, by_rows, by_heads, by_tile);
   }
 }
 
 template <int FORMAT, typename T>
-void launch_head_dim(int head_dim, const QuantizedArgs& a, const AttentionPlan& p, hipStream_t s) {
+void launch_head_dim(int head_dim, const QuantizedArgs& a, const QuantizedPlan& p, hipStream_t s) {
   if (head_dim == 64) launch_kernel<FORMAT, T, 64>(a, p, s);
   if (head_dim == 96) launch_kernel<FORMAT, T, 96>(a, p, s);
   if (head_dim == 128) launch_kernel<FORMAT, T, 128>(a, p, s);
@@ -34,7 +65,7 @@ void launch_head_dim(int head_dim, const QuantizedArgs& a, const AttentionPlan& 
 }
 
 template <int FORMAT>
-void launch_dtype(int dtype, int head_dim, const QuantizedArgs& a, const AttentionPlan& p, hipStream_t s) {
+void launch_dtype(int dtype, int head_dim, const QuantizedArgs& a, const QuantizedPlan& p, hipStream_t s) {
   if (dtype == DPLLM_F16)
     launch_head_dim<FORMAT, half_t>(head_dim, a, p, s);
   else
