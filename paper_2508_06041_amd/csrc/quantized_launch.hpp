@@ -14,16 +14,19 @@ struct QuantizedPlan : AttentionPlan {
 inline QuantizedPlan plan_quantized(int batch, int nodes, int heads, int kv_heads, int head_dim, int64_t max_len) {
   QuantizedPlan p{};
   p.rows = nodes * (heads / kv_heads);
+  // up to 64 rows go to wavefronts that take every step of codes apart by themselves, two tiles of rows at most to each (52 rows over 65001 tokens, 4 sequences, int4: 96 us; the kernel that shares
+  // that 116), more to the kernel that shares it (100 rows, int8: 99 against 123; 240 rows, e4m3: 138 against 166)
+  p.waves = p.rows <= 64 || head_dim == 256 ? 0 : p.rows <= 128 ? 4 : 8;
   p.mt = head_dim == 256 || p.rows <= 16 ? 1 : 2;
-  p.tile = 16 * p.mt;
+  p.tile = 16 * p.mt * std::max(p.waves, 1);
   p.row_tiles = (p.rows + p.tile - 1) / p.tile;
   const int64_t steps = (max_len + kAttTile - 1) / kAttTile + (nodes + kAttTile - 1) / kAttTile;
-  p.lone = p.mt == 1 && (head_dim == 64 || head_dim == 128) && steps <= 14;
-  p.heads = p.lone ? 1 : kv_heads % 4 == 0 ? 4 : kv_heads % 2 == 0 ? 2 : 1;
+  p.lone = p.waves == 0 && p.mt == 1 && (head_dim == 64 || head_dim == 128) && steps <= 14;
+  p.heads = p.lone || p.waves > 0 ? 1 : kv_heads % 4 == 0 ? 4 : kv_heads % 2 == 0 ? 2 : 1;
   p.turns = (p.lone ? 8 : kAttWaves) / p.heads;
-  p.least = p.turns;
+  p.least = p.waves > 0 ? kAttWaves : p.turns;
   const int64_t tiles = (int64_t)kv_heads / p.heads * p.row_tiles;
-  const int64_t most = batch * ((steps + p.least - 1) / p.least), fill = (512 + tiles - 1) / tiles;
+  const int64_t most = batch * ((steps + p.least - 1) / p.least), fill = ((p.waves == 8 ? 256 : 512) + tiles - 1) / tiles;
   p.slots = p.lone ? batch : (int)std::max<int64_t>(batch, std::min(most, fill >= 2 * batch ? fill : 3 * (int64_t)batch));
   p.groups = p.slots * tiles;
   const size_t part_rows = p.slots == batch ? 0 : (size_t)p.slots * kv_heads * p.row_tiles * p.tile;
@@ -43,6 +46,10 @@ void launch_kernel(const QuantizedArgs& a, const QuantizedPlan& p, hipStream_t s
   const dim3 groups((unsigned)p.groups);
   if constexpr (D == 64 || D == 128)
     if (p.lone) hipLaunchKernelGGL((quantized_attention_kernel<FORMAT, T, D, 1, 8>), groups, dim3(8 * 64), 0, s, a);
+  if constexpr (D < 256) {
+    if (p.waves == 4) hipLaunchKernelGGL((quantized_attention_wide_kernel<FORMAT, T, D, 2, 4>), groups, dim3(4 * 64), 0, s, a);
+    if (p.waves == 8) hipLaunchKernelGGL((quantized_attention_wide_kernel<FORMAT, T, D, 2, 8>), groups, dim3(8 * 64), 0, s, a);
+  }
   if (p.waves == 0 && p.mt == 1 && !p.lone) hipLaunchKernelGGL((quantized_attention_kernel<FORMAT, T, D, 1, kAttWaves>), groups, dim3(kAttWaves * 64), 0, s, a);
   if constexpr (D < 256)
     if (p.waves == 0 && p.mt == 2) hipLaunchKernelGGL((quantized_attention_kernel<FORMAT, T, D, 2, kAttWaves>), groups, dim3(kAttWaves * 64), 0, s, a);
