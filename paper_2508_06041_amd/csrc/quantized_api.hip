@@ -56,14 +56,13 @@ bool whole_codes(const dpllm_quantized_cache& c, int elements) {
   return ((uintptr_t)c.k | (uintptr_t)c.v) % bytes == 0 && (c.layer_stride | c.page_stride | c.token_stride | c.head_stride) % bytes == 0;
 }
 
-// f(format, type, wide, one) with the constants that belong to the arguments
+// f(format, type) with the constants that belong to the arguments
 template <typename F>
-void choose(int format, int dtype, bool wide, F f) {
-  auto by_wide = [&](auto form, auto type) { wide ? f(form, type, std::true_type()) : f(form, type, std::false_type()); };
+void choose(int format, int dtype, F f) {
   auto by_type = [&](auto form) {
-    if (dtype == DPLLM_F16) by_wide(form, half_t());
-    if (dtype == DPLLM_BF16) by_wide(form, bfloat_t());
-    if (dtype == DPLLM_F32) by_wide(form, float());
+    if (dtype == DPLLM_F16) f(form, half_t());
+    if (dtype == DPLLM_BF16) f(form, bfloat_t());
+    if (dtype == DPLLM_F32) f(form, float());
   };
   if (format == kE4m3) by_type(std::integral_constant<int, kE4m3>());
   if (format == kInt8) by_type(std::integral_constant<int, kInt8>());
@@ -78,7 +77,7 @@ int check_layers(const char* who, const dpllm_quantized_cache* cache, int first_
   if (dtype < DPLLM_F16 || dtype > DPLLM_F32) return refuse(DPLLM_EINVAL, "%s: unknown dtype %d", who, dtype);
   if (first_layer < 0 || n_layers < 0 || n_layers > cache->layers - first_layer || n_layers > 32767)
     return refuse(DPLLM_ERANGE, "%s: layers %d to %lld of %d", who, first_layer, (long long)first_layer + n_layers, cache->layers);
-  if (batch < 0 || tokens < 0 || tokens > (1 << 24)) return refuse(DPLLM_ESHAPE, "%s: %d sequences of %d tokens", who, batch, tokens);
+  if (batch < 0 || batch > 65535 || tokens < 0 || tokens > (1 << 24)) return refuse(DPLLM_ESHAPE, "%s: %d sequences of %d tokens (at most 65535 of 2^24)", who, batch, tokens);
   if (((uintptr_t)k->data | (uintptr_t)v->data) % (dtype == DPLLM_F32 ? 4 : 2)) return refuse(DPLLM_EINVAL, "%s: keys or values are not aligned to their elements", who);
   return DPLLM_OK;
 }
@@ -114,19 +113,26 @@ int dpllm_quantized_append(const dpllm_quantized_cache* cache, int first_layer, 
   a.tokens = nodes;
   a.heads = c.heads;
   a.head_dim = c.head_dim;
-  const int e = vector ? wide : 4;
+  const int pieces_each = !vector ? 0 : c.head_dim % (2 * wide) == 0 && whole_codes(c, 2 * wide) ? 2 : 1;
+  const int e = vector ? pieces_each * wide : 4;
   a.units = (c.head_dim + e - 1) / e;
   while ((1 << a.log_lanes) < std::min(a.units, 64)) ++a.log_lanes;
   a.lanes = 1 << a.log_lanes;
+  // as many tokens to a workgroup as leave eight workgroups to a compute unit, eight heads to a group of lanes at most
   const int teams = kQuantThreads >> a.log_lanes;
-  a.at_a_time = std::max(1, std::min(16, 2 * teams / c.heads));
-  const dim3 grid(batch, 2 * n_layers, (nodes + a.at_a_time - 1) / a.at_a_time);
-  if (grid.z > 65535) return refuse(DPLLM_ESHAPE, "%s: %d nodes", who, nodes);
-  choose(c.format, dtype, vector, [&](auto form, auto type, auto is_wide) {
-    if (a.units <= a.lanes)
-      hipLaunchKernelGGL((quantized_append_kernel<decltype(form)::value, decltype(type), decltype(is_wide)::value, true>), grid, dim3(kQuantThreads), 0, (hipStream_t)stream, a);
-    else
-      hipLaunchKernelGGL((quantized_append_kernel<decltype(form)::value, decltype(type), decltype(is_wide)::value, false>), grid, dim3(kQuantThreads), 0, (hipStream_t)stream, a);
+  const int64_t all = (int64_t)nodes * c.heads * batch * 2 * n_layers;
+  const int per = std::max(1, (int)std::min<int64_t>(8, all / ((int64_t)teams * 2048)));
+  a.at_a_time = std::max(1, std::min(kQuantTokens, per * teams / c.heads));
+  const dim3 grid((nodes + a.at_a_time - 1) / a.at_a_time, 2 * n_layers, batch);
+  choose(c.format, dtype, [&](auto form, auto type) {
+    auto launch = [&](auto n, auto one) {
+      hipLaunchKernelGGL((quantized_append_kernel<decltype(form)::value, decltype(type), decltype(n)::value, decltype(one)::value>), grid, dim3(kQuantThreads), 0,
+                         (hipStream_t)stream, a);
+    };
+    auto by_one = [&](auto n) { a.units <= a.lanes ? launch(n, std::true_type()) : launch(n, std::false_type()); };
+    if (pieces_each == 0) by_one(std::integral_constant<int, 0>());
+    if (pieces_each == 1) by_one(std::integral_constant<int, 1>());
+    if (pieces_each == 2) by_one(std::integral_constant<int, 2>());
   });
   return launched(who);
 }
@@ -155,14 +161,20 @@ int dpllm_quantized_read(const dpllm_quantized_cache* cache, int first_layer, in
   const int e = vector ? wide : 4;
   a.head_units = (c.head_dim + e - 1) / e;
   a.units = a.head_units * c.heads;
-  a.by_units = Divide::by(a.units);
   a.by_head = Divide::by(a.head_units);
-  a.at_a_time = std::max(1, std::min(16, 2 * kQuantThreads / a.units));
-  const int64_t chunks = (tokens + a.at_a_time - 1) / a.at_a_time;
-  if (chunks > 65535) return refuse(DPLLM_ESHAPE, "%s: %d tokens", who, tokens);
-  const dim3 grid(batch, 2 * n_layers, (unsigned)chunks);
-  choose(c.format, dtype, vector, [&](auto form, auto type, auto is_wide) {
-    hipLaunchKernelGGL((quantized_read_kernel<decltype(form)::value, decltype(type), decltype(is_wide)::value>), grid, dim3(kQuantThreads), 0, (hipStream_t)stream, a);
+  a.span = std::min(a.units, kQuantThreads);
+  a.by_span = Divide::by(a.span);
+  a.tokens_at_once = kQuantThreads / a.span;
+  // as many tokens to a workgroup as leave eight workgroups to a compute unit, 16 units to a thread at most
+  const int64_t all = (int64_t)tokens * a.units * batch * 2 * n_layers;
+  const int per = std::max(1, (int)std::min<int64_t>(16, all / (kQuantThreads * 2048)));
+  a.at_a_time = std::max(1, std::min(kQuantTokens, per * kQuantThreads / a.units));
+  const dim3 grid((tokens + a.at_a_time - 1) / a.at_a_time, 2 * n_layers, batch);
+  choose(c.format, dtype, [&](auto form, auto type) {
+    if (vector)
+      hipLaunchKernelGGL((quantized_read_kernel<decltype(form)::value, decltype(type), true>), grid, dim3(kQuantThreads), 0, (hipStream_t)stream, a);
+    else
+      hipLaunchKernelGGL((quantized_read_kernel<decltype(form)::value, decltype(type), false>), grid, dim3(kQuantThreads), 0, (hipStream_t)stream, a);
   });
   return launched(who);
 }

@@ -92,42 +92,68 @@ __device__ __forceinline__ void four_values(uint32_t w, uint32_t scales, float (
 }
 
 // ---- numbers to codes ----
-// What a head's word takes: the largest size, as bits, so that NaN and infinity are larger than all else; of int4 the lowest and highest value too.
+// What a head's word takes: the largest size, of int4 the lowest and highest value; infinite where a value is no finite number.
 struct Extent {
-  uint32_t most;
-  float lo, hi;
+  float most, lo, hi;
 };
-__device__ __forceinline__ void extend(Extent& e, float x) {
-  e.most = max(e.most, __float_as_uint(x) & 0x7fffffffu);
-  e.lo = fminf(e.lo, x);
-  e.hi = fmaxf(e.hi, x);
+// (of values that may be signaling NaN, which the compiler would see to first)
+__device__ __forceinline__ float least_of(float a, float b, float c) {
+  float r;
+  asm("v_min3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+__device__ __forceinline__ float most_of(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+__device__ __forceinline__ float most_size(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, |%2|, |%3|" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+template <int FORMAT, int E>
+__device__ __forceinline__ void extend(Extent& e, const float (&x)[E]) {
+  bool nan = false;
+#pragma unroll
+  for (int i = 0; i < E; i += 2) {
+    nan = nan || __builtin_isunordered(x[i], x[i + 1]);
+    if (FORMAT == kInt4) {
+      e.lo = least_of(e.lo, x[i], x[i + 1]);
+      e.hi = most_of(e.hi, x[i], x[i + 1]);
+    } else {
+      e.most = most_size(e.most, x[i], x[i + 1]);
+    }
+  }
+  if (nan) e.most = e.hi = INFINITY;
 }
 struct Coder {
   uint32_t word;
-  float scale, offset, by, top;      // by: 1 / scale, or 127 / top
-  bool flat, bad;                    // flat: all values are the offset
+  float scale, offset, by, top;      // by: 1 / scale, or 127 / top, to 2^-22
+  bool bad;
 };
 template <int FORMAT>
 __device__ __forceinline__ Coder coder_of(const Extent& e) {
 #pragma clang fp contract(off)
   Coder c{};
-  c.bad = e.most >= 0x7f800000u;
   if (FORMAT == kInt4) {
     const float middle = e.lo * 0.5f + e.hi * 0.5f;
-    const bfloat_t offset = (bfloat_t)middle;
-    c.offset = (float)offset;
+    c.offset = (float)(bfloat_t)middle;
     const float reach = fmaxf(e.hi - c.offset, c.offset - e.lo);
-    c.flat = !(reach > 0.f);
     const uint32_t up = (__float_as_uint(fmaxf(reach, kLeast) * 0.125f) + 0xffffu) & 0xffff0000u;
     c.scale = __uint_as_float(up);
-    c.by = 1.0f / c.scale;
-    c.bad = c.bad || up >= 0x7f800000u || (__float_as_uint(c.offset) & 0x7fffffffu) >= 0x7f800000u;
-    c.word = c.bad ? kNan32 >> 16 : (c.flat ? 0u : up >> 16) | __float_as_uint(c.offset);
+    c.by = __builtin_amdgcn_rcpf(c.scale);
+    c.bad = up >= 0x7f800000u || !__builtin_isfinite(c.offset);
+    c.word = c.bad ? kNan32 >> 16 : (reach > 0.f ? up >> 16 : 0u) | __float_as_uint(c.offset);      // (0: all values are the offset)
   } else {
-    c.top = fmaxf(__uint_as_float(e.most), kLeast);
+    c.bad = e.most == INFINITY;
+    c.top = fmaxf(e.most, kLeast);
     if (FORMAT == kInt8) {
-      c.scale = c.top / 127.0f;
-      c.by = 127.0f / c.top;
+      // the quotient to the last bit: its remainder is known exactly
+      constexpr float k127th = 1.f / 127.f;
+      const float near = c.top * k127th;
+      c.scale = __builtin_fmaf(__builtin_fmaf(-127.f, near, c.top), k127th, near);
+      c.by = __builtin_amdgcn_rcpf(c.scale);      // (that of the largest float is none that it gives)
     } else {
       // top = m 2^e, 448 = 1.75 2^8: the exponent is e - 8, one more if m is above 1.75
       const uint32_t bits = __float_as_uint(c.top), exponent = (bits >> 23) - 8u + ((bits & 0x7fffffu) > 0x600000u ? 1u : 0u);
@@ -139,63 +165,71 @@ __device__ __forceinline__ Coder coder_of(const Extent& e) {
   return c;
 }
 
-// Four values as codes (of int4 nibbles in the lower bits of bytes).  The quotients of int8 and int4 are products with the reciprocal, and where one lands within 2^-14 of a border
-// they are formed again as quotients: a product is off by 2^-23 of itself, of 127 at most, so the codes are those of quotients rounded once.
-template <int FORMAT>
-__device__ __forceinline__ uint32_t four_codes(const Coder& c, const float (&x)[4]) {
+// Values as codes, side by side.  The quotients of int8 and int4 are products with the reciprocal; where it matters remainders decide, which are exact for values of 16 bits (x 127 and n top have 18 bits,
+// n scale has 12).
+template <int FORMAT, int E>
+__device__ __forceinline__ void codes_of(const Coder& c, const float (&x)[E], uint32_t (&w)[FORMAT == kInt4 ? (E + 7) / 8 : E / 4]) {
 #pragma clang fp contract(off)
-  uint32_t w = 0;
-  if (c.bad) return 0u;
   if constexpr (FORMAT == kE4m3) {
-    w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[0] * c.by, x[1] * c.by, 0, false);
-    w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2] * c.by, x[3] * c.by, (int)w, true);
+#pragma unroll
+    for (int i = 0; i < E / 4; ++i) {
+      w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i] * c.by, x[4 * i + 1] * c.by, 0, false);
+      w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i + 2] * c.by, x[4 * i + 3] * c.by, (int)w[i], true);
+    }
   } else if constexpr (FORMAT == kInt8) {
-    float n[4], off = 0.f;
+    float n[E], off = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float t = x[i] * c.by;
+    for (int i = 0; i < E; i += 2) {
+      const float t = x[i] * c.by, u = x[i + 1] * c.by;
       n[i] = __builtin_rintf(t);
-      off = fmaxf(off, __builtin_fabsf(t - n[i]));
+      n[i + 1] = __builtin_rintf(u);
+      off = most_size(off, t - n[i], u - n[i + 1]);
     }
-    if (off > 0.5f - 0x1p-14f) {
-      const float down = c.top > 0x1p100f ? 0x1p-20f : 1.f;      // 127 x stays a float
+    if (__any(off > 0.5f - 0x1p-14f)) {
+      asm volatile("");      // (a branch: few wavefronts have such a value, and all would take the remainders)
+      const float down = c.top > 0x1p100f ? 0x1p-20f : 1.f, top = c.top * down;      // 127 x stays a float
 #pragma unroll
-      for (int i = 0; i < 4; ++i) n[i] = __builtin_rintf(x[i] * down * 127.0f / (c.top * down));
+      for (int i = 0; i < E; ++i) {
+        const float rest = __builtin_fmaf(-n[i], top, x[i] * down * 127.f), twice = 2.f * __builtin_fabsf(rest);
+        const bool odd = ((int)n[i] & 1) != 0;
+        if (twice > top || (twice == top && odd)) n[i] += __builtin_copysignf(1.f, rest);
+      }
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w |= ((uint32_t)(int)n[i] & 0xffu) << (8 * i);
+    for (int i = 0; i < E / 4; ++i) {
+      w[i] = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[i] |= ((uint32_t)(int)n[4 * i + j] & 0xffu) << (8 * j);
+    }
   } else {
-    float n[4], low = 1.f, high = 0.f;
+    // The magnitude, n or -1 - n, is the whole part of |x - offset| / scale, which a product that is a little large gives or exceeds by 1: so the remainder's sign decides.  Values on a border, where the remainder
+    // is 0, belong to the level above, which for negative ones is the smaller magnitude; they are as many as five in a thousand of bfloat16 values, so all go this way.
+    const float by = c.by * (1.f + 0x1p-20f);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float t = (x[i] - c.offset) * c.by;
-      n[i] = __builtin_floorf(t);
-      low = fminf(low, t - n[i]);
-      high = fmaxf(high, t - n[i]);
-    }
-    if (low < 0x1p-14f || high > 1.f - 0x1p-14f)
+    for (int i = 0; i < (E + 7) / 8; ++i) {
+      w[i] = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) n[i] = __builtin_floorf((x[i] - c.offset) / c.scale);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int level = (int)fminf(fmaxf(n[i], -8.f), 7.f);
-      w |= (uint32_t)(level < 0 ? 7 - level : level) << (8 * i);      // 8 + (-1 - level)
+      for (int j = 0; j < (E < 8 ? E : 8); ++j) {
+        const float d = x[8 * i + j] - c.offset, whole = __builtin_truncf(fminf(__builtin_fabsf(d) * by, 7.5f)), rest = __builtin_fmaf(-whole, c.scale, __builtin_fabsf(d));
+        const uint32_t negative = __float_as_uint(d) >> 31;
+        const uint32_t m = (uint32_t)((int)whole + ((__builtin_bit_cast(int, rest) - (int)negative) >> 31));
+        w[i] |= (m | negative << 3) << (4 * j);
+      }
     }
   }
-  return w;
+  if (c.bad)
+#pragma unroll
+    for (uint32_t& v : w) v = 0;
 }
-// Four nibbles of four bytes, side by side.
-__device__ __forceinline__ uint32_t side_by_side(uint32_t w) {
-  w |= w >> 4;      // bytes 0 and 2 hold two codes each
-  return (w & 0xffu) | ((w >> 8) & 0xff00u);
-}
-__device__ __forceinline__ uint32_t apart(uint32_t w) {      // back: 16 bits to four bytes
+// Four nibbles side by side to the lower halves of four bytes.
+__device__ __forceinline__ uint32_t apart(uint32_t w) {
   w = (w & 0xffu) | ((w & 0xff00u) << 8);
   return (w & 0x000f000fu) | ((w & 0x00f000f0u) << 4);
 }
 
 // ---- append ----
 constexpr int kQuantThreads = 256;
+constexpr int kQuantTokens = 64;      // most tokens to a workgroup
 
 struct QuantizeArgs {
   QuantizedView cache;           // the first layer written
@@ -207,77 +241,105 @@ struct QuantizeArgs {
   int tokens, heads, head_dim, units, lanes, log_lanes, at_a_time;      // units of E elements to a head, lanes that share one
 };
 
-// A group of `lanes` lanes (a power of two) quantises a head of a token: its values are read once into registers where there are no more units than lanes (ONE), else twice.
-// Grid: (sequence, 2 layers + (keys, values), at_a_time tokens).  A unit is E elements; without WIDE it is read and written element by element, and the last may be short.
-// Bound by the latency of a launch for single tokens, by memory for prompts.
-template <int FORMAT, typename T, bool WIDE, bool ONE>
+// A group of `lanes` lanes (a power of two) quantises a head of a token: its values are read once into registers where there are no more units than lanes (ONE), the next head's while this one is
+// quantised, else twice.
+// Grid: (at_a_time tokens, 2 layers + (keys, values), sequence), whose places are looked up first.  A unit is N pieces of 16 bytes, two where a head divides into those (what is done once for a head and lane
+// is as much as for 16 elements); N = 0: four elements that are read and written by themselves, of which the last unit may have fewer.
+// Bound by the latency of a launch for single tokens, by memory and the vector unit for prompts.
+template <int FORMAT, typename T, int N, bool ONE>
 __global__ void __launch_bounds__(kQuantThreads) quantized_append_kernel(const QuantizeArgs a) {
-  constexpr int E = WIDE ? Piece<T>::E : 4, W = E / 4;
+  constexpr bool WIDE = N > 0;
+  constexpr int P = Piece<T>::E, E = WIDE ? N * P : 4, W = FORMAT == kInt4 ? (E + 7) / 8 : E / 4;
   typedef typename Piece<T>::type piece;
-  const int b = blockIdx.x, layer = blockIdx.y >> 1, first = blockIdx.z * a.at_a_time;
+  __shared__ int64_t places[kQuantTokens][2];
+  __shared__ int nodes[kQuantTokens];      // -1: none goes there
+  const int b = blockIdx.z, layer = blockIdx.y >> 1, first = blockIdx.x * a.at_a_time;
   const bool values = blockIdx.y & 1;
   int n = a.count == nullptr ? a.tokens : min(a.count[b], a.tokens);
   n = min(n - first, a.at_a_time);
   if (n <= 0) return;
   const int base = a.lens[b];
   if (base < 0) return;
+  if ((int)threadIdx.x < n) {
+    const uint32_t place = first + threadIdx.x;
+    int node = a.path == nullptr ? (int)place : a.path[b * a.path_stride + place];
+    int64_t at = 0, scale_at = 0;
+    if ((uint32_t)node >= (uint32_t)a.tokens || (uint32_t)base + place > 0x7fffffffu || !a.cache.find(b, (uint32_t)base + place, &at, &scale_at)) node = -1;
+    nodes[threadIdx.x] = node;
+    places[threadIdx.x][0] = at;
+    places[threadIdx.x][1] = scale_at;
+  }
+  __syncthreads();
   const Heads& from = values ? a.v : a.k;
   const T* src = reinterpret_cast<const T*>(from.data) + layer * (values ? a.v_layer : a.k_layer) + b * from.batch_stride;
   char* codes = (values ? a.cache.v : a.cache.k) + layer * a.cache.layer;
   uint32_t* scales = (values ? a.cache.v_scales : a.cache.k_scales) + layer * a.cache.scale_layer;
-  const int lane = threadIdx.x & (a.lanes - 1), teams = kQuantThreads >> a.log_lanes;
-  for (int i = threadIdx.x >> a.log_lanes; i < n * a.heads; i += teams) {
-    const uint32_t t = a.by_heads.of(i), h = i - t * a.heads, place = first + t;
-    const int node = a.path == nullptr ? (int)place : a.path[b * a.path_stride + place];
-    int64_t at, scale_at;
-    if ((uint32_t)node >= (uint32_t)a.tokens || (uint32_t)base + place > 0x7fffffffu || !a.cache.find(b, (uint32_t)base + place, &at, &scale_at)) continue;
-    const T* head = src + node * from.token_stride + h * from.head_stride;
+  const int lane = threadIdx.x & (a.lanes - 1), teams = kQuantThreads >> a.log_lanes, rows = n * a.heads;
+  struct Row {
+    int t, h, node;
+    piece p[WIDE ? N : 1];
+  };
+  auto head_of = [&](const Row& r) { return src + r.node * from.token_stride + r.h * from.head_stride; };
+  auto load = [&](Row& r, int u) {
+    if constexpr (WIDE)
+#pragma unroll
+      for (int j = 0; j < N; ++j) r.p[j] = *reinterpret_cast<const piece*>(head_of(r) + u * E + j * P);
+  };
+  auto find = [&](int i) {
+    Row r;
+    r.node = -1;
+    if (i >= rows) return r;
+    r.t = a.by_heads.of(i);
+    r.h = i - r.t * a.heads;
+    r.node = nodes[r.t];
+    if (ONE && r.node >= 0 && lane < a.units) load(r, lane);
+    return r;
+  };
+  Row next = find(threadIdx.x >> a.log_lanes);
+  for (int i = threadIdx.x >> a.log_lanes; i < rows; i += teams) {
+    Row row = next;
+    next = find(i + teams);      // on its way meanwhile
+    if (row.node < 0) continue;
     float x[E];
-    auto load = [&](int u) {
-      if constexpr (WIDE) {
-        const piece p = *reinterpret_cast<const piece*>(head + u * E);
+    auto take = [&](int u) {
+      if (!ONE) load(row, u);
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = (float)p[e];
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = (float)head[min(u * E + e, a.head_dim - 1)];      // (the last element again changes no extent)
+      for (int e = 0; e < E; ++e) {
+        if constexpr (WIDE)
+          x[e] = (float)row.p[e / P][e % P];
+        else
+          x[e] = (float)head_of(row)[min(u * E + e, a.head_dim - 1)];      // (the last element again changes no extent)
       }
     };
-    Extent extent{0u, INFINITY, -INFINITY};
+    Extent extent{0.f, INFINITY, -INFINITY};
     for (int u = lane; u < a.units; u += a.lanes) {
-      load(u);
-#pragma unroll
-      for (int e = 0; e < E; ++e) extend(extent, x[e]);
+      take(u);
+      extend<FORMAT, E>(extent, x);
     }
-    extent.most = team_all(extent.most, a.lanes, [](uint32_t p, uint32_t q) { return max(p, q); });
     if (FORMAT == kInt4) {
-      extent.lo = team_all(extent.lo, a.lanes, [](float p, float q) { return fminf(p, q); });
-      extent.hi = team_all(extent.hi, a.lanes, [](float p, float q) { return fmaxf(p, q); });
+      extent.lo = team_all(extent.lo, a.lanes, [](float p, float q) { return least_of(p, p, q); });
+      extent.hi = team_all(extent.hi, a.lanes, [](float p, float q) { return most_of(p, p, q); });
+    } else {
+      extent.most = team_all(extent.most, a.lanes, [](float p, float q) { return most_of(p, p, q); });
     }
     const Coder c = coder_of<FORMAT>(extent);
-    if (lane == 0) scales[scale_at + h * a.cache.scale_head] = c.word;
-    char* to = codes + at + h * a.cache.head;
+    if (lane == 0) scales[places[row.t][1] + row.h * a.cache.scale_head] = c.word;
+    char* to = codes + places[row.t][0] + row.h * a.cache.head;
     for (int u = lane; u < a.units; u += a.lanes) {
-      if (!ONE) load(u);
+      if (!ONE) take(u);
       uint32_t w[W];
-#pragma unroll
-      for (int i = 0; i < W; ++i) {
-        const float four[4] = {x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
-        w[i] = four_codes<FORMAT>(c, four);
-        if (FORMAT == kInt4) w[i] = side_by_side(w[i]);
-      }
+      codes_of<FORMAT, E>(c, x, w);
       if constexpr (!WIDE) {
         const int bytes = FORMAT == kInt4 ? min(2, a.head_dim / 2 - 2 * u) : min(4, a.head_dim - 4 * u);
         for (int i = 0; i < bytes; ++i) to[u * (FORMAT == kInt4 ? 2 : 4) + i] = (char)(w[0] >> (8 * i));
-      } else if constexpr (FORMAT == kInt4) {
-        if constexpr (W == 1)
-          *reinterpret_cast<uint16_t*>(to + 2 * u) = (uint16_t)w[0];
-        else
-          *reinterpret_cast<uint32_t*>(to + 4 * u) = w[0] | w[1] << 16;
+      } else if constexpr (FORMAT == kInt4 && E == 4) {
+        *reinterpret_cast<uint16_t*>(to + 2 * u) = (uint16_t)w[0];
       } else if constexpr (W == 1) {
         *reinterpret_cast<uint32_t*>(to + 4 * u) = w[0];
-      } else {
+      } else if constexpr (W == 2) {
         *reinterpret_cast<uint2*>(to + 8 * u) = make_uint2(w[0], w[1]);
+      } else {
+        *reinterpret_cast<u32x4*>(to + 16 * u) = u32x4{w[0], w[1], w[2], w[3]};
       }
     }
   }
@@ -289,69 +351,100 @@ struct DequantizeArgs {
   Heads k, v;                    // [layers][batch][tokens][heads][head_dim]
   int64_t k_layer, v_layer;
   const int32_t *first, *count;
-  Divide by_units, by_head;      // units of a token, of a head
-  int tokens, head_dim, units, head_units, at_a_time;
+  Divide by_span, by_head;       // units of a head
+  int tokens, head_dim, units, head_units, at_a_time, span, tokens_at_once;      // units of a token, of a head; units of a token and tokens that a workgroup takes at once
 };
+constexpr int kReadAtOnce = 4;      // tokens that a thread has on their way
 
-// A thread makes a unit of E elements; grid as above.  What the cache does not hold is written as zeros.
+// A workgroup makes at_a_time tokens of a layer of a sequence, keys or values; it looks their places up first.  A thread makes units of E elements, kReadAtOnce of them side by side.  What the cache
+// does not hold is written as zeros.
 template <int FORMAT, typename T, bool WIDE>
 __global__ void __launch_bounds__(kQuantThreads) quantized_read_kernel(const DequantizeArgs a) {
   constexpr int E = WIDE ? Piece<T>::E : 4, W = E / 4;
   typedef typename Piece<T>::type piece;
-  const int b = blockIdx.x, layer = blockIdx.y >> 1, first = blockIdx.z * a.at_a_time;
+  __shared__ int64_t places[kQuantTokens][2];      // -1: nothing is held
+  const int b = blockIdx.z, layer = blockIdx.y >> 1, first = blockIdx.x * a.at_a_time;
   const bool values = blockIdx.y & 1;
   const Heads& into = values ? a.v : a.k;
   T* dst = reinterpret_cast<T*>(into.data) + layer * (values ? a.v_layer : a.k_layer) + b * into.batch_stride;
   const char* codes = (values ? a.cache.v : a.cache.k) + layer * a.cache.layer;
   const uint32_t* scales = (values ? a.cache.v_scales : a.cache.k_scales) + layer * a.cache.scale_layer;
-  const int64_t from = a.first == nullptr ? 0 : a.first[b];
-  const int held = a.count == nullptr ? a.tokens : a.count[b];
-  const uint32_t end = (uint32_t)min(a.tokens - first, a.at_a_time) * a.units;
-  for (uint32_t i = threadIdx.x; i < end; i += kQuantThreads) {
-    const uint32_t t = a.by_units.of(i), u = i - t * a.units, h = a.by_head.of(u), e0 = (u - h * a.head_units) * E;
-    const int64_t place = from + first + t;
-    int64_t at, scale_at;
-    uint32_t w[W] = {}, word = 0;
-    const bool there = (int)(first + t) < held && place >= 0 && place <= 0x7fffffff && a.cache.find(b, (uint32_t)place, &at, &scale_at);
-    if (there) {
-      word = scales[scale_at + h * a.cache.scale_head];
-      const char* p = codes + at + h * a.cache.head + (FORMAT == kInt4 ? e0 / 2 : e0);
+  const int tokens = min(a.tokens - first, a.at_a_time);
+  if ((int)threadIdx.x < tokens) {
+    const int held = a.count == nullptr ? a.tokens : a.count[b];
+    const int64_t place = (a.first == nullptr ? 0 : (int64_t)a.first[b]) + first + threadIdx.x;
+    int64_t at = -1, scale_at = 0;
+    if (first + (int)threadIdx.x >= held || place < 0 || place > 0x7fffffff || !a.cache.find(b, (uint32_t)place, &at, &scale_at)) at = -1;
+    places[threadIdx.x][0] = at;
+    places[threadIdx.x][1] = scale_at;
+  }
+  __syncthreads();
+  // a thread has the same unit of every so many tokens (and every 256th, if a token has more), so that nothing is divided on the way
+  const int t0 = a.by_span.of(threadIdx.x), each = a.tokens_at_once;
+  if (t0 >= each) return;
+  for (int u = (int)threadIdx.x - t0 * a.span; u < a.units; u += a.span) {
+    const uint32_t h = a.by_head.of(u), e0 = (u - h * a.head_units) * E;
+    const int64_t in_token = h * a.cache.head + (FORMAT == kInt4 ? e0 / 2 : e0), scale_in = h * a.cache.scale_head;
+    T* out = dst + first * into.token_stride + h * into.head_stride + e0;
+  for (int t = t0; t < tokens; t += kReadAtOnce * each) {
+    struct Unit {
+      uint32_t w[W], word;
+      bool there;
+    } x[kReadAtOnce];
+#pragma unroll
+    for (int k = 0; k < kReadAtOnce; ++k) {
+      x[k] = Unit{};
+      const int at_token = t + k * each;
+      const int64_t at = at_token < tokens ? places[at_token][0] : -1;
+      x[k].there = at >= 0;
+      if (at < 0) continue;
+      x[k].word = scales[places[at_token][1] + scale_in];
+      const char* p = codes + at + in_token;
       if constexpr (!WIDE) {
         const int bytes = FORMAT == kInt4 ? min(2, (a.head_dim - (int)e0) / 2) : min(4, a.head_dim - (int)e0);
-        for (int j = 0; j < bytes; ++j) w[0] |= (uint32_t)(uint8_t)p[j] << (8 * j);
+        for (int j = 0; j < bytes; ++j) x[k].w[0] |= (uint32_t)(uint8_t)p[j] << (8 * j);
       } else if constexpr (FORMAT == kInt4) {
         if constexpr (W == 1)
-          w[0] = *reinterpret_cast<const uint16_t*>(p);
+          x[k].w[0] = *reinterpret_cast<const uint16_t*>(p);
         else
-          w[0] = *reinterpret_cast<const uint32_t*>(p);
+          x[k].w[0] = *reinterpret_cast<const uint32_t*>(p);
+      } else if constexpr (W == 1) {
+        x[k].w[0] = *reinterpret_cast<const uint32_t*>(p);
       } else {
-#pragma unroll
-        for (int j = 0; j < W; ++j) w[j] = reinterpret_cast<const uint32_t*>(p)[j];
+        const uint2 two = *reinterpret_cast<const uint2*>(p);
+        x[k].w[0] = two.x;
+        x[k].w[1] = two.y;
       }
     }
-    if (FORMAT == kInt4) {
-      if (W > 1) w[W - 1] = level_bytes<false>(apart(w[0] >> 16));
-      w[0] = level_bytes<false>(apart(w[0] & 0xffffu));
+#pragma unroll
+    for (int k = 0; k < kReadAtOnce; ++k) {
+      if (t + k * each >= tokens) continue;
+      uint32_t* w = x[k].w;
+      if (FORMAT == kInt4) {
+        if (W > 1) w[W - 1] = level_bytes<false>(apart(w[0] >> 16));
+        w[0] = level_bytes<false>(apart(w[0] & 0xffffu));
+      }
+      float y[E];
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        float four[4];
+        four_values<FORMAT>(w[j], x[k].word, four);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[4 * j + e] = x[k].there ? four[e] : 0.f;
+      }
+      T* to = out + (t + k * each) * into.token_stride;
+      if constexpr (WIDE) {
+        piece p;
+#pragma unroll
+        for (int e = 0; e < E; ++e) p[e] = (T)y[e];
+        __builtin_nontemporal_store(p, reinterpret_cast<piece*>(to));
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if ((int)e0 + e < a.head_dim) to[e] = (T)y[e];
+      }
     }
-    float x[E];
-#pragma unroll
-    for (int j = 0; j < W; ++j) {
-      float four[4];
-      four_values<FORMAT>(w[j], word, four);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[4 * j + e] = there ? four[e] : 0.f;
-    }
-    T* to = dst + (first + t) * into.token_stride + h * into.head_stride + e0;
-    if constexpr (WIDE) {
-      piece p;
-#pragma unroll
-      for (int e = 0; e < E; ++e) p[e] = (T)x[e];
-      *reinterpret_cast<piece*>(to) = p;
-    } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e)
-        if ((int)e0 + e < a.head_dim) to[e] = (T)x[e];
-    }
+  }
   }
 }
 
