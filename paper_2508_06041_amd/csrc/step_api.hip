@@ -15,7 +15,8 @@ namespace {
 // What both directions of the norms check and fill alike.  others: one or two more views of each tensor.
 struct NormSetup {
   NormArgs a;
-  bool half, vector;
+  bool half;
+  int elements;      // of a unit: pieces of 16 bytes, of 8 or single
 };
 
 int setup_norm(const char* who, NormSetup* made, const dpllm_heads* x, const dpllm_heads* g, const dpllm_heads* out, const int* heads, const void* const* weights,
@@ -35,7 +36,8 @@ int setup_norm(const char* who, NormSetup* made, const dpllm_heads* x, const dpl
   if (rotary_dim > 0 && some && (!freqs || !positions)) return refuse(DPLLM_EINVAL, "%s: freqs or positions is NULL", who);
   const int es = dtype == DPLLM_F32 ? 4 : 2, ws = weight_dtype == DPLLM_F32 ? 4 : 2, wide = 16 / es;
   made->half = layout == DPLLM_ROPE_HALF && rotary_dim > 0;
-  bool vector = rotary_dim % (made->half ? 2 * wide : wide) == 0 && (head_dim - rotary_dim) % wide == 0;
+  auto whole = [&](int e) { return rotary_dim % (made->half ? 2 * e : e) == 0 && (head_dim - rotary_dim) % e == 0; };
+  bool vector = true;
   NormArgs& a = made->a;
   a = {};
   int64_t all_heads = 0;
@@ -56,8 +58,9 @@ int setup_norm(const char* who, NormSetup* made, const dpllm_heads* x, const dpl
     if ((uintptr_t)a.weights[i] % ws) return refuse(DPLLM_EINVAL, "%s: weight %d is not aligned to its elements", who, i);
     vector = vector && (uintptr_t)a.weights[i] % 16 == 0 && a.weight_strides[i] * ws % 16 == 0;
   }
-  made->vector = vector;
-  const int e = vector ? wide : 1;
+  // Eight elements to a lane at most: with sixteen (two pieces of 16 bytes where pairs lie apart) the gradient has registers for three wavefronts to a SIMD and took 86.6 us, with eight 73.3.
+  const int most = made->half ? 4 : wide, e = !vector ? 1 : whole(most) ? most : whole(wide / 2) ? wide / 2 : 1;
+  made->elements = e;
   a.freqs = freqs;
   a.positions = positions;
   a.positions_stride = positions_stride;
@@ -75,8 +78,6 @@ int setup_norm(const char* who, NormSetup* made, const dpllm_heads* x, const dpl
   a.eps = eps;
   a.scale = scale;
   a.by_tokens = Divide::by(std::max(tokens, 1));
-  a.by_heads = Divide::by(a.heads);
-  a.by_pairs = Divide::by(std::max(a.pairs, 1));
   return DPLLM_OK;
 }
 
@@ -88,35 +89,42 @@ void choose_norm(const NormSetup& s, int dtype, F f) {
   };
   auto by_half = [&](auto type, auto e) { s.half ? by_one(type, e, std::true_type()) : by_one(type, e, std::false_type()); };
   auto by_e = [&](auto type) {
-    if (s.vector)
-      by_half(type, std::integral_constant<int, 16 / sizeof(type)>());
-    else
-      by_half(type, std::integral_constant<int, 1>());
+    constexpr int kWide = 16 / sizeof(type);
+    if constexpr (kWide == 8)
+      if (s.elements == kWide) by_one(type, std::integral_constant<int, kWide>(), std::false_type());
+    if constexpr (kWide == 4)
+      if (s.elements == kWide) by_half(type, std::integral_constant<int, kWide>());
+    if (s.elements == kWide / 2) by_half(type, std::integral_constant<int, kWide / 2>());
+    if (s.elements == 1) by_half(type, std::integral_constant<int, 1>());
   };
   if (dtype == DPLLM_F16) by_e(half_t());
   if (dtype == DPLLM_BF16) by_e(bfloat_t());
   if (dtype == DPLLM_F32) by_e(float());
 }
 
-// How the gradient's work is dealt out: workgroups to each weight.
+// How the gradient's work is dealt out: workgroups to each set of heads, teams groups of lanes to a wavefront.
 struct NormSplit {
-  int splits[kNormTensors], first[kNormTensors + 1], group_heads[kNormTensors], groups_end[kNormTensors];
-  int64_t tokens_each[kNormTensors];
+  int splits[kNormTensors], first[kNormTensors + 1], set_heads[kNormTensors], own[kNormTensors], weights_end[kNormTensors];
+  int64_t tokens_each[kNormTensors], parts_at[kNormTensors], parts;
 };
-NormSplit split_norm(const int* heads, const int64_t* weight_strides, int tensors, int64_t all) {
+constexpr int kNormGroups = 1280;      // five to a compute unit, as many as registers allow: 57 us for the gradient of 4 sequences of 2049 tokens, 32 + 8 heads of 128; 1024: 58, 1536: 64, 2048: 61
+NormSplit split_norm(const int* heads, const int64_t* weight_strides, int tensors, int64_t all, int teams) {
   NormSplit s{};
   int64_t all_heads = 0;
   for (int i = 0; i < tensors; ++i) all_heads += heads[i];
   for (int i = 0; i < tensors; ++i) {
-    const bool own = weight_strides && weight_strides[i] != 0;
-    const int groups = own ? heads[i] : 1;
-    s.group_heads[i] = own ? 1 : heads[i];
-    // about 1500 workgroups in all, which is as many as run at once, each of at least 16 heads
-    const int64_t wish = std::max<int64_t>(1, 1536 * s.group_heads[i] / all_heads), most = std::max<int64_t>(1, all * s.group_heads[i] / 16);
-    s.splits[i] = (int)std::min(wish, most);
-    s.tokens_each[i] = std::max<int64_t>(1, (all + s.splits[i] - 1) / s.splits[i]);
-    s.first[i + 1] = s.first[i] + groups * s.splits[i];
-    s.groups_end[i] = groups + (i > 0 ? s.groups_end[i - 1] : 0);
+    const bool each = weight_strides && weight_strides[i] != 0;
+    s.own[i] = each ? teams : 1;
+    s.set_heads[i] = each ? teams : heads[i];
+    const int sets = (heads[i] + s.set_heads[i] - 1) / s.set_heads[i];
+    // about kNormGroups workgroups in all, each of at least 16 heads
+    const int64_t wish = std::max<int64_t>(1, (int64_t)kNormGroups * std::min(s.set_heads[i], heads[i]) / all_heads), most = std::max<int64_t>(1, all * s.set_heads[i] / 16);
+    s.tokens_each[i] = std::max<int64_t>(1, (all + std::min(wish, most) - 1) / std::min(wish, most));
+    s.splits[i] = (int)std::max<int64_t>(1, (all + s.tokens_each[i] - 1) / s.tokens_each[i]);
+    s.first[i + 1] = s.first[i] + sets * s.splits[i];
+    s.parts_at[i] = s.parts;
+    s.parts += (int64_t)sets * s.splits[i] * s.own[i];
+    s.weights_end[i] = (each ? heads[i] : 1) + (i > 0 ? s.weights_end[i - 1] : 0);
   }
   for (int i = tensors; i < kNormTensors; ++i) s.first[i + 1] = s.first[i];
   return s;
@@ -167,13 +175,13 @@ int dpllm_norm_rope(const dpllm_heads* x, const dpllm_heads* out, const int* hea
     return rc;
   NormArgs& a = s.a;
   if (a.all == 0) return DPLLM_OK;
-  // tokens enough for every group of lanes to have two heads on their way, but not so many that part of the chip has none
-  const int teams = kNormThreads >> a.log_lanes;
-  a.at_a_time = (int)std::max<int64_t>(1, std::min<int64_t>({2 * teams / a.heads, a.all / 512, 16}));
-  const int64_t blocks = std::min<int64_t>((a.all + a.at_a_time - 1) / a.at_a_time, 1 << 20);
+  // a token's heads in one wavefront if tokens alone give the chip wavefronts enough, else in several
+  const int teams = 64 >> a.log_lanes, waves = kNormThreads / 64, rounds = (a.heads + teams - 1) / teams, chunks = (int)std::min<int64_t>(rounds, std::max<int64_t>(1, 4096 / a.all));
+  a.heads_each = (rounds + chunks - 1) / chunks * teams;
+  const dim3 grid((unsigned)std::min<int64_t>((a.all + waves - 1) / waves, 1 << 20), (unsigned)((a.heads + a.heads_each - 1) / a.heads_each));
   choose_norm(s, dtype, [&](auto type, auto e, auto half, auto one) {
-    hipLaunchKernelGGL((norm_rope_kernel<decltype(type), decltype(e)::value, decltype(half)::value, decltype(one)::value>), dim3((unsigned)blocks), dim3(kNormThreads),
-                       sizeof(float2) * a.at_a_time * a.pairs, (hipStream_t)stream, a);
+    hipLaunchKernelGGL((norm_rope_kernel<decltype(type), decltype(e)::value, decltype(half)::value, decltype(one)::value>), grid, dim3(kNormThreads),
+                       sizeof(float2) * waves * a.pairs, (hipStream_t)stream, a);
   });
   return launched(who);
 }
@@ -190,7 +198,10 @@ int dpllm_norm_rope_backward_workspace_bytes(const int* heads, const int64_t* we
   }
   if (head_dim < 1 || head_dim > DPLLM_MAX_HEAD_DIM || all_heads * head_dim > (1 << 24)) return refuse(DPLLM_ESHAPE, "%s: %lld heads of %d", who, (long long)all_heads, head_dim);
   const int64_t all = (int64_t)batch * tokens;
-  *bytes = all == 0 ? 0 : (size_t)split_norm(heads, weight_strides, tensors, all).first[tensors] * head_dim * sizeof(float);
+  // the groups of lanes of a wavefront depend on types and strides as well, and are at most those of 16 elements to a lane
+  int64_t parts = 0;
+  for (int teams = 1; teams <= std::min(64, std::max(1, 1024 / head_dim)); teams *= 2) parts = std::max(parts, split_norm(heads, weight_strides, tensors, all, teams).parts);
+  *bytes = all == 0 ? 0 : (size_t)parts * head_dim * sizeof(float);
   return DPLLM_OK;
 }
 
@@ -212,8 +223,8 @@ int dpllm_norm_rope_backward(const dpllm_heads* x, const dpllm_heads* grads, con
   }
   const NormArgs& a = s.a;
   if (a.all == 0 && !wanted) return DPLLM_OK;
-  const NormSplit split = split_norm(heads, weights ? weight_strides : nullptr, tensors, a.all);
-  const size_t need = a.all == 0 || !wanted ? 0 : (size_t)split.first[tensors] * head_dim * sizeof(float);
+  const NormSplit split = split_norm(heads, weights ? weight_strides : nullptr, tensors, a.all, 64 >> a.log_lanes);
+  const size_t need = a.all == 0 || !wanted ? 0 : (size_t)split.parts * head_dim * sizeof(float);
   if (need > 0 && (!ws_dev || ws_bytes < need || (uintptr_t)ws_dev % 16)) return refuse(DPLLM_ESTATE, "%s: needs a workspace of %zu bytes, aligned to 16", who, need);
   NormBackArgs k{};
   k.n = a;
@@ -221,25 +232,25 @@ int dpllm_norm_rope_backward(const dpllm_heads* x, const dpllm_heads* grads, con
   for (int i = 0; i < kNormTensors; ++i) {
     k.first[i + 1] = split.first[i + 1];
     k.splits[i] = a.all == 0 ? 0 : split.splits[i];
-    k.group_heads[i] = std::max(split.group_heads[i], 1);
-    k.by_group[i] = Divide::by(k.group_heads[i]);
+    k.set_heads[i] = std::max(split.set_heads[i], 1);
+    k.own[i] = std::max(split.own[i], 1);
+    k.parts_at[i] = split.parts_at[i];
+    k.by_own[i] = Divide::by(k.own[i]);
     k.by_splits[i] = Divide::by(std::max(split.splits[i], 1));
     k.tokens_each[i] = split.tokens_each[i];
     k.grad_weights[i] = i < tensors && grad_weights ? grad_weights[i] : nullptr;
-    k.groups_end[i] = i < tensors ? split.groups_end[i] : split.groups_end[tensors - 1];
+    k.weights_end[i] = i < tensors ? split.weights_end[i] : split.weights_end[tensors - 1];
   }
-  const int teams = kNormThreads >> a.log_lanes;
   if (a.all > 0) {
-    k.n.at_a_time = (int)std::max<int64_t>(1, std::min<int64_t>(16, 4 * teams / k.group_heads[0]));
-    const size_t lds = sizeof(float2) * k.n.at_a_time * a.pairs + sizeof(float) * teams * head_dim;
+    const size_t lds = (kNormThreads / 64) * (sizeof(float2) * a.pairs + sizeof(float) * (64 >> a.log_lanes) * head_dim);
     choose_norm(s, dtype, [&](auto type, auto e, auto half, auto one) {
       hipLaunchKernelGGL((norm_rope_backward_kernel<decltype(type), decltype(e)::value, decltype(half)::value, decltype(one)::value>), dim3(split.first[tensors]),
                          dim3(kNormThreads), lds, (hipStream_t)stream, k);
     });
   }
   if (wanted) {
-    const int each = (head_dim + 63) / 64;
-    const dim3 grid(split.groups_end[tensors - 1] * each), threads(kNormJoin);
+    const int each = (head_dim + kNormColumns - 1) / kNormColumns;
+    const dim3 grid(split.weights_end[tensors - 1] * each), threads(kNormJoin);
     if (weight_dtype == DPLLM_F16) hipLaunchKernelGGL(norm_rope_join_kernel<half_t>, grid, threads, 0, (hipStream_t)stream, k, each);
     if (weight_dtype == DPLLM_BF16) hipLaunchKernelGGL(norm_rope_join_kernel<bfloat_t>, grid, threads, 0, (hipStream_t)stream, k, each);
     if (weight_dtype == DPLLM_F32) hipLaunchKernelGGL(norm_rope_join_kernel<float>, grid, threads, 0, (hipStream_t)stream, k, each);
