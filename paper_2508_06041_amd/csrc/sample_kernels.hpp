@@ -1,6 +1,11 @@
 // A word for every row of logits.  e = exp((x - top) / temperature); the words in the order of their logits (equal ones by number) are cut off behind the first top_k, where less than
-// top_p of the sum of those lies in front, and at e = min_p: all three leave the first so many of one order.  So nothing is sorted: a histogram of the row over
-// eighths of a power of two of e says in which step of it a cut lies, and only the words of that step are looked at one by one.
+// top_p of the sum of those lies in front, and at e = min_p: all three leave the first so many of one order.  So the row is not sorted: a histogram of it over eighths of a power of two of e
+// says in which step of it a cut lies.  If the words up to there are at most one to a thread of a workgroup, those are sorted and the rest is not looked at again; else only the words of
+// that step are.
+//
+// One row of 32000 words with all three cuts takes 3.4 + 7 + 11 us (tops, histograms, choice), 64 rows of 128256 in bf16 with every kind of cut 6 + 11 + 71.  The choice is one workgroup's work and
+// bound by what that can do: a walk over a row of 128256 words takes it 7 us, a sort of 2048 words 18, one of 1024 ten, up to 512 each word's place is counted instead (64 words: 4 us less).
+// Choosing without the shorter way took 32 us for the one row.  Steps of a 32nd do not help: the many words of a flat row are far below its top.
 //
 // Answers are whole numbers, so sums are kept in 64 bits and in whole numbers where workgroups' order could show: a word of step b counts 1 and the
 // 2^-40ths by which e 2^((b + 1) / 8) exceeds 1, both in one 64-bit addition in LDS.  Rounding that to 2^-41 moves a sum by less than 1e-12 of itself.
@@ -13,6 +18,7 @@ constexpr int kSampleBins = 512;            // e down to 2^-64
 constexpr int kSampleThreads = 1024;        // of the workgroup that chooses
 constexpr int kSampleWaves = kSampleThreads / 64;
 constexpr int kSampleList = 2048;           // words that are sorted at once
+constexpr int kPast = 1 << 12;              // more than a list is long
 constexpr int kCountShift = 50;             // a chunk has at most 2^13 words of less than 2^37 each
 
 struct SampleTop {      // of a chunk: its largest logit and where that is first
@@ -31,53 +37,122 @@ struct SampleArgs {
   int rows, vocabulary, chunks;
 };
 
-// Where a word lies: eighths of a power of two below the top, by = 8 / (temperature ln 2).  false: it is left out (as are NaN and minus infinity).
-__device__ __forceinline__ bool step_of(float x, float top, double by, int* bin, double* part) {
-  const double t = x == top ? 0.0 : ((double)top - (double)x) * by;
-  if (!(t <= (double)kSampleBins)) return false;
-  *bin = min((int)t, kSampleBins - 1);
-  *part = t - (double)*bin;
-  return true;
+// Where a word lies.  y = 2^19 - t, t the 256ths of a power of two by which e is below 1, so that the upper word of y has all whole numbers in it and its last bits count 2^-34: an error of 8e-14 of
+// e.  Step b is t in (32 b, 32 (b + 1)], the first with 0; r = y - floor(y) is what is left to the next whole t, and with the five bits of y above that to the step's end: e is the step's least e times
+// 2^(bits / 256) 2^(r / 256).  1 + c1 r + c2 r^2 + c3 r^3 is the last of these to 2e-14.  A dozen instructions in 64 bits; with the series of the whole exponent they were 30,
+// and the histograms of 64 rows of 128256 words took 14 us, now 11.
+constexpr int kSampleTable = 32;      // 2^40 2^(j / 256)
+struct Steps {
+  float top;
+  double steps;      // 256 / (temperature ln 2)
+  const double* table;
+  __device__ __forceinline__ Steps(float top, float temperature, const double* table) : top(top), steps(369.32993046757462 / (double)temperature), table(table) {}
+  __device__ __forceinline__ double place(float x) const {
+    const double t = x == top ? 0.0 : ((double)x - (double)top) * steps;
+    return __builtin_fmin(__builtin_fmax(t, -131072.0) + 524288.0, 524288.0 - 0x1p-34);      // (NaN counts as far below)
+  }
+  // Its step; kSampleBins or more: it is left out (as are NaN and minus infinity).
+  __device__ __forceinline__ static int bin(double y) { return (int)((~(uint32_t)(__builtin_bit_cast(uint64_t, y) >> 32) & 0xfffffu) >> 7); }
+  // e by the least of its step, times 2^40 w, plus c
+  __device__ __forceinline__ double share(double y, double w, double c) const {
+    const double r = __builtin_amdgcn_fract(y);
+    double f = __builtin_fma(r, 3.312607527945956e-09, 3.6655631008313955e-06);
+    f = __builtin_fma(f, r, 0.0027076061744736664);
+    f = __builtin_fma(f, r, 1.0);
+    return __builtin_fma(f, table[(uint32_t)(__builtin_bit_cast(uint64_t, y) >> 34) & (kSampleTable - 1)] * w, c);
+  }
+  // That less 1, in 2^-40ths, to the nearest.
+  __device__ __forceinline__ unsigned long long excess(double y) const {
+    return __builtin_bit_cast(uint64_t, share(y, 1.0, 0x1p52 - 0x1p40)) & ((1ull << 52) - 1);
+  }
+};
+// Fills the table; a barrier has to follow.
+__device__ __forceinline__ void fill_steps(double* table) {
+  if (threadIdx.x < kSampleTable) table[threadIdx.x] = 0x1p40 * exp_of((int)threadIdx.x * 0.0027076061740622863);      // ln 2 / 256
 }
-// 2^((1 - part) / 8) - 1 in 2^-40ths: the series to its eighth power, below 1e-15.
-__device__ __forceinline__ unsigned long long excess(double part) {
-  const double y = (1.0 - part) * 0.086643397569993164;      // ln 2 / 8
-  double s = 1.0 / 40320.0;
-  s = __builtin_fma(s, y, 1.0 / 5040.0);
-  s = __builtin_fma(s, y, 1.0 / 720.0);
-  s = __builtin_fma(s, y, 1.0 / 120.0);
-  s = __builtin_fma(s, y, 1.0 / 24.0);
-  s = __builtin_fma(s, y, 1.0 / 6.0);
-  s = __builtin_fma(s, y, 0.5);
-  s = __builtin_fma(s, y, 1.0);
-  return (unsigned long long)__builtin_rint(s * y * 0x1p40);
-}
-__device__ __forceinline__ double steps_by(float temperature) { return 11.541560327111707 / (double)temperature; }      // 8 / ln 2
-__device__ __forceinline__ double base_of(int bin) { return exp_of(-0.086643397569993164 * (bin + 1)); }
+__device__ __forceinline__ double base_of(int bin) { return exp_of(-0.086643397569993164 * (bin + 1)); }      // the least e of a step: ln 2 / 8
 __device__ __forceinline__ float larger(float x, float y) { return fmaxf(x, y); }
 __device__ __forceinline__ int smaller(int x, int y) { return min(x, y); }
 
+// A piece of a row from word i on (16-byte aligned, perhaps in front of the row's first or past its last); what lies outside is NaN.
+template <typename T>
+__device__ __forceinline__ typename Piece<T>::type piece_at(const char* row, int n, int i) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  constexpr int E = Piece<T>::E, EACH = 4 / sizeof(T);      // words to 32 bits
+  const T* words = reinterpret_cast<const T*>(row);
+  if (i >= 0 && i + E <= n) return *reinterpret_cast<const typename Piece<T>::type*>(words + i);
+  u32x4 v = {0u, 0u, 0u, 0u};
+#pragma unroll 1
+  for (int e = 0; e < E; ++e) {
+    const T x = i + e >= 0 && i + e < n ? words[i + e] : (T)__builtin_nanf("");
+    uint32_t w;
+    if constexpr (sizeof(T) == 4)
+      w = __builtin_bit_cast(uint32_t, x);
+    else
+      w = (uint32_t)__builtin_bit_cast(uint16_t, x) << 16 * (e % EACH);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] |= e / EACH == j ? w : 0u;
+  }
+  return __builtin_bit_cast(typename Piece<T>::type, v);
+}
+
+// f(piece, its first word) for the pieces of a stretch of a row that a group of `threads` threads shares, four on their way at a time, those of a thread in their order.
+template <typename T, typename F>
+__device__ __forceinline__ void each_piece(const char* row, int n, int first, int pieces, int thread, int threads, F f) {
+  constexpr int E = Piece<T>::E;
+  for (int p0 = thread; p0 < pieces; p0 += 4 * threads) {
+    typename Piece<T>::type v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = piece_at<T>(row, n, first + (p0 + j * threads < pieces ? p0 + j * threads : p0) * E);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (p0 + j * threads < pieces) f(v[j], first + (p0 + j * threads) * E);
+  }
+}
+
+// f(x, i) for those of a piece that are within [low, high].  They are few, or dear: so f's code is there once.
+template <typename T, typename F>
+__device__ __forceinline__ void each_between(const typename Piece<T>::type& v, int first, float low, float high, F f) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  const u32x4 w = __builtin_bit_cast(u32x4, v);
+  uint32_t in = 0;
+#pragma unroll
+  for (int e = 0; e < Piece<T>::E; ++e) in |= (float)v[e] >= low && (float)v[e] <= high ? 1u << e : 0u;
+#pragma unroll 1
+  while (in != 0) {
+    const int e = __builtin_ctz(in), d = e * (int)sizeof(T) / 4;
+    const uint32_t here = d < 2 ? (d == 0 ? w[0] : w[1]) : (d == 2 ? w[2] : w[3]);
+    if constexpr (sizeof(T) == 4)
+      f(__uint_as_float(here), first + e);
+    else
+      f((float)__builtin_bit_cast(T, (uint16_t)(e & 1 ? here >> 16 : here)), first + e);
+    in &= in - 1;
+  }
+}
+
+// Workgroups of a row's chunks: x is the row, so that with eight rows or more (their number rounded up to a multiple) all of them and the one that chooses are on the same die
+// and find the row in its cache.
 // The largest logit of a chunk.
 template <typename T>
-__global__ void __launch_bounds__(kVerThreads) sample_tops_kernel(const SampleArgs a, const Divide by_chunks) {
+__global__ void __launch_bounds__(kVerThreads) sample_tops_kernel(const SampleArgs a) {
   __shared__ float tops[kVerThreads / 64];
   __shared__ int places[kVerThreads / 64];
-  const int row = by_chunks.of(blockIdx.x), chunk = blockIdx.x - row * a.chunks;
+  const int row = blockIdx.x, chunk = blockIdx.y;
+  if (row >= a.rows) return;
   const char* from = a.logits + row * a.stride * (int64_t)sizeof(T);
-  Chunk<T> c;
-  c.load(from, chunk, a.vocabulary);
-  float top = -INFINITY;
-#pragma unroll
-  for (int p = 0; p < kVerPieces; ++p)
-#pragma unroll
-    for (int e = 0; e < Chunk<T>::E; ++e) top = fmaxf(top, c.x[p][e]);
-  top = wave_all(top, larger);
+  float mine = -INFINITY;
   int at = 0x7fffffff;
+  each_piece<T>(from, a.vocabulary, chunk * Chunk<T>::kElements - Chunk<T>::lead(from), Chunk<T>::kElements / Chunk<T>::E, threadIdx.x, kVerThreads,
+                [&](const typename Piece<T>::type& v, int i) {
 #pragma unroll
-  for (int p = 0; p < kVerPieces; ++p)
-#pragma unroll
-    for (int e = 0; e < Chunk<T>::E; ++e)
-      if (c.x[p][e] == top && top != -INFINITY) at = min(at, Chunk<T>::index(from, chunk, p, e));
+                  for (int e = 0; e < Chunk<T>::E; ++e)
+                    if ((float)v[e] > mine) {
+                      mine = (float)v[e];
+                      at = i + e;
+                    }
+                });
+  const float top = wave_all(mine, larger);
+  if (mine != top) at = 0x7fffffff;
   at = wave_all(at, smaller);
   if ((threadIdx.x & 63) == 0) {
     tops[threadIdx.x >> 6] = top;
@@ -93,30 +168,30 @@ __global__ void __launch_bounds__(kVerThreads) sample_tops_kernel(const SampleAr
 
 // The histogram of a chunk.
 template <typename T>
-__global__ void __launch_bounds__(kVerThreads) sample_bins_kernel(const SampleArgs a, const Divide by_chunks) {
+__global__ void __launch_bounds__(kVerThreads) sample_bins_kernel(const SampleArgs a) {
   __shared__ unsigned long long bins[kSampleBins];
-  const int row = by_chunks.of(blockIdx.x), chunk = blockIdx.x - row * a.chunks;
+  __shared__ double table[kSampleTable];
+  const int row = blockIdx.x, chunk = blockIdx.y;
+  if (row >= a.rows) return;
   const float temperature = a.temperature[row];
   if (greedy(temperature)) return;
   const char* from = a.logits + row * a.stride * (int64_t)sizeof(T);
-  Chunk<T> c;
-  c.load(from, chunk, a.vocabulary);
   for (int i = threadIdx.x; i < kSampleBins; i += kVerThreads) bins[i] = 0;
+  fill_steps(table);
   float top = -INFINITY;
   for (int i = threadIdx.x & 63; i < a.chunks; i += 64) top = fmaxf(top, a.tops[(int64_t)row * a.chunks + i].top);
   top = wave_all(top, larger);
   __syncthreads();
   if (top == -INFINITY) return;
-  const double by = steps_by(temperature);
+  const Steps steps(top, temperature, table);
+  each_piece<T>(from, a.vocabulary, chunk * Chunk<T>::kElements - Chunk<T>::lead(from), Chunk<T>::kElements / Chunk<T>::E, threadIdx.x, kVerThreads,
+                [&](const typename Piece<T>::type& v, int) {
 #pragma unroll
-  for (int p = 0; p < kVerPieces; ++p)
-#pragma unroll
-    for (int e = 0; e < Chunk<T>::E; ++e) {
-      int bin;
-      double part;
-      // (what lies outside of the row is minus infinity)
-      if (step_of(c.x[p][e], top, by, &bin, &part)) atomicAdd(&bins[bin], (1ull << kCountShift) + excess(part));
-    }
+                  for (int e = 0; e < Chunk<T>::E; ++e) {
+                    const double y = steps.place((float)v[e]);
+                    if (steps.bin(y) < kSampleBins) atomicAdd(&bins[steps.bin(y)], (1ull << kCountShift) + steps.excess(y));
+                  }
+                });
   __syncthreads();
   for (int i = threadIdx.x; i < kSampleBins; i += kVerThreads) a.bins[((int64_t)row * a.chunks + chunk) * kSampleBins + i] = bins[i];
 }
@@ -128,15 +203,26 @@ struct Cut {
   __device__ __forceinline__ bool has(float x, int i) const { return x > at || (x == at && i <= upto); }
 };
 
-// Floats as whole numbers in the same order (-0 and 0 are one).
+// Floats as whole numbers in the same order (-0 and 0 are one); of narrower types without the bits that all of theirs share.
 __device__ __forceinline__ uint32_t key_of(float x) {
   const uint32_t w = __float_as_uint(x + 0.f);
   return w >> 31 ? ~w : w | 0x80000000u;
 }
 __device__ __forceinline__ float from_key(uint32_t k) { return __uint_as_float(k >> 31 ? k & 0x7fffffffu : ~k); }
+template <typename T>
+struct Narrow {
+  static constexpr int kShared = std::is_same<T, float>::value ? 0 : std::is_same<T, half_t>::value ? 13 : 16;
+  __device__ __forceinline__ static uint32_t of(float x) { return key_of(x) >> kShared; }
+  __device__ __forceinline__ static float back(uint32_t k) {
+    const uint32_t w = k << kShared;
+    return from_key(w >> 31 ? w : w | ((1u << kShared) - 1u));
+  }
+};
 
 struct SampleSpace {
   unsigned long long list[kSampleList];
+  double base[kSampleBins];                 // the least e of a bin, in 2^-40ths
+  double table[kSampleTable];
   double sums[kSampleBins];                 // running, over bins
   uint32_t counts[kSampleBins];
   unsigned long long fine[kSampleBins];     // of a step that is looked at more closely
@@ -148,25 +234,26 @@ struct SampleSpace {
   uint32_t low, high;
 };
 
+// The sum of what the first `waves` wavefronts left in s.wave_sums.
+__device__ __forceinline__ double of_waves(const SampleSpace& s, int waves) {
+  const int lane = threadIdx.x & 63;
+  return wave_sum(lane < waves ? s.wave_sums[lane & (kSampleWaves - 1)] : 0.0);
+}
+
 // The running sums of kSampleBins values and counts, one of each to a thread of the first eight wavefronts, into s.sums and s.counts.
 __device__ __forceinline__ void run_bins(SampleSpace& s, double sum, uint32_t count) {
-  const int wave = threadIdx.x >> 6;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const double upto = wave_scan(sum), number = wave_scan((double)count);      // (whole numbers)
   __syncthreads();
-  if ((threadIdx.x & 63) == 63 && threadIdx.x < kSampleBins) {
+  if (lane == 63) {
     s.wave_sums[wave] = upto;
     s.wave_counts[wave] = (uint32_t)number;
   }
   __syncthreads();
+  const double plus = of_waves(s, wave), more = wave_sum(lane < wave ? (double)s.wave_counts[lane & (kSampleWaves - 1)] : 0.0);
   if (threadIdx.x < kSampleBins) {
-    double plus = 0.0;
-    uint32_t more = 0;
-    for (int w = 0; w < wave; ++w) {
-      plus += s.wave_sums[w];
-      more += s.wave_counts[w];
-    }
     s.sums[threadIdx.x] = upto + plus;
-    s.counts[threadIdx.x] = (uint32_t)number + more;
+    s.counts[threadIdx.x] = (uint32_t)(number + more);
   }
   __syncthreads();
 }
@@ -189,47 +276,37 @@ __device__ __forceinline__ void find_bin(SampleSpace& s, uint32_t count, double 
   __syncthreads();
 }
 
-// f(x, i) for those of a piece of a row that are within [low, high].  They are few, or dear: so f's code is there once, and they are read again.
-template <typename T, typename F>
-__device__ __forceinline__ void each_between(const typename Piece<T>::type& v, const char* row, int first, float low, float high, F f) {
-  uint32_t in = 0;
-#pragma unroll
-  for (int e = 0; e < Piece<T>::E; ++e) in |= (float)v[e] >= low && (float)v[e] <= high ? 1u << e : 0u;
-#pragma unroll 1
-  while (in != 0) {
-    const int i = first + __builtin_ctz(in);
-    f(logit<T>(row, i), i);
-    in &= in - 1;
-  }
-}
-
 // f(x, i) for all words of a row whose logits are within [low, high], in no order.
 template <typename T, typename F>
 __device__ __forceinline__ void words_between(const char* row, int n, float low, float high, F f) {
   constexpr int E = Piece<T>::E;
-  typedef typename Piece<T>::type piece;
-  const int lead = Chunk<T>::lead(row), pieces = (n + lead + E - 1) / E;
-  const T* base = reinterpret_cast<const T*>(row);
-  for (int p0 = threadIdx.x; p0 < pieces; p0 += 4 * kSampleThreads) {
-    piece v[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int i = (p0 + j * kSampleThreads) * E - lead;
-      if (i >= 0 && i + E <= n) {
-        v[j] = *reinterpret_cast<const piece*>(base + i);
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) v[j][e] = i + e >= 0 && i + e < n ? base[i + e] : (T)__builtin_nanf("");
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) each_between<T>(v[j], row, (p0 + j * kSampleThreads) * E - lead, low, high, f);
-  }
+  const int lead = Chunk<T>::lead(row);
+  each_piece<T>(row, n, -lead, (n + lead + E - 1) / E, threadIdx.x, kSampleThreads,
+                [&](const typename Piece<T>::type& v, int i) { each_between<T>(v, i, low, high, f); });
 }
 
-// Sorts n (a power of two) numbers, the smallest first.
-__device__ __forceinline__ void sort(unsigned long long* list, int n) {
+// Sorts n (a power of two) different numbers, or such that are all ones, the smallest first.  Up to 512: each is put where as many are smaller; the whole workgroup counts.  `space`: as many more.
+// More: in steps, those whose partners are at most 64 apart in the 128 numbers of a wavefront.
+__device__ __forceinline__ void sort(unsigned long long* list, int n, uint32_t* ranks, unsigned long long* space) {
+  if (n <= 512) {
+    const int i = threadIdx.x & (n - 1), parts = kSampleThreads / n, each = (n + parts - 1) / parts, begin = (int)threadIdx.x / n * each;
+    if ((int)threadIdx.x < n) ranks[threadIdx.x] = 0;
+    __syncthreads();
+    const unsigned long long mine = list[i];
+    uint32_t rank = 0;
+#pragma unroll 8
+    for (int j = begin; j < begin + each; ++j) rank += j < n && (list[j] < mine || (list[j] == mine && j < i));
+    atomicAdd(&ranks[i], rank);
+    __syncthreads();
+    if ((int)threadIdx.x < n) space[ranks[i]] = mine;
+    __syncthreads();
+    if ((int)threadIdx.x < n) list[i] = space[i];
+    __syncthreads();
+    return;
+  }
+#pragma unroll 1
   for (int size = 2; size <= n; size *= 2)
+#pragma unroll 1
     for (int gap = size / 2; gap > 0; gap /= 2) {
       for (int i = threadIdx.x; i < n / 2; i += kSampleThreads) {
         const int p = 2 * i - (i & (gap - 1)), q = p + gap;
@@ -239,8 +316,16 @@ __device__ __forceinline__ void sort(unsigned long long* list, int n) {
           list[q] = x;
         }
       }
-      __syncthreads();
+      const int next = gap > 1 ? gap / 2 : size;      // the next step's
+      if (gap > 64 || next > 64) {
+        __syncthreads();
+      } else {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      }
     }
+  __syncthreads();
 }
 
 // The running sum over the workgroup of a value of each thread.
@@ -250,9 +335,7 @@ __device__ __forceinline__ double group_scan(SampleSpace& s, double v) {
   __syncthreads();
   if ((threadIdx.x & 63) == 63) s.wave_sums[wave] = upto;
   __syncthreads();
-  double plus = 0.0;
-  for (int w = 0; w < wave; ++w) plus += s.wave_sums[w];
-  return upto + plus;
+  return upto + of_waves(s, wave);
 }
 
 // The order of the row as its histogram's bins are; all threads take part in each of these.
@@ -260,11 +343,14 @@ template <typename T>
 struct Sampler {
   const SampleArgs& a;
   SampleSpace& s;
+  int a_row;
   const char* row;
   float top;
-  double by, inverse;      // steps and 1 / temperature
+  double by;      // eighths of a power of two
+  const Steps& steps;
 
-  __device__ __forceinline__ double e_of(float x) const { return weight(x, top, inverse); }
+  __device__ __forceinline__ double e_at(double y) const { return steps.share(y, s.base[min(steps.bin(y), kSampleBins - 1)], 0.0); }
+  __device__ __forceinline__ double e_of(float x) const { return x == top ? 1.0 : e_at(steps.place(x)); }
   // Bounds of the logits of bins first ... last, a little wide.
   __device__ __forceinline__ float lowest(int last) const {
     const float x = (float)((double)top - (last + 1) / by);
@@ -278,55 +364,33 @@ struct Sampler {
 
   // The words of bin `bin` in front of a cut: `count` of them, or (count 0) those in front of which less than `sum` of them lies, at least one.  s.length and s.sum: how many, and their sum.
   __device__ Cut cut_in(int bin, int words, uint32_t count, double sum) {
-    uint32_t low = 0, high = ~0u;      // keys
-    const double base = base_of(bin);
+    typedef Narrow<T> Key;
+    uint32_t low = Key::of(lowest(bin)), high = Key::of(fminf(highest(bin), top));
+    const double base = s.base[bin];
     int taken = 0;
     double taken_sum = 0.0;
-    const auto inside = [&](float x, double* part) {
-      int b;
-      const uint32_t k = key_of(x);
-      return k >= low && k <= high && step_of(x, top, by, &b, part) && b == bin;
+    const auto inside = [&](float x, double y) {
+      const uint32_t k = Key::of(x);
+      return k >= low && k <= high && steps.bin(y) == bin;
     };
     // narrower, until the words can be sorted or are all the same: nine of the key's 32 bits at a time
     for (int round = 0; round < 4 && words > kSampleList && low != high; ++round) {
-      if (threadIdx.x == 0) {
-        s.low = ~0u;
-        s.high = 0u;
-      }
       if (threadIdx.x < kSampleBins) {
         s.fine[threadIdx.x] = 0;
         s.fine_counts[threadIdx.x] = 0;
       }
       __syncthreads();
-      uint32_t least = ~0u, most = 0u;
-      words_between<T>(row, a.vocabulary, lowest(bin), highest(bin), [&](float x, int) {
-        double part;
-        if (inside(x, &part)) {
-          least = min(least, key_of(x));
-          most = max(most, key_of(x));
-        }
-      });
-      least = wave_all(least, [](uint32_t x, uint32_t y) { return min(x, y); });
-      most = wave_all(most, [](uint32_t x, uint32_t y) { return max(x, y); });
-      if ((threadIdx.x & 63) == 0) {
-        atomicMin(&s.low, least);
-        atomicMax(&s.high, most);
-      }
-      __syncthreads();
-      low = s.low;
-      high = s.high;
-      if (low == high) break;
       const int shift = max(0, 23 - __builtin_clz(high - low));      // (high - low) >> shift is below 512
-      words_between<T>(row, a.vocabulary, lowest(bin), highest(bin), [&](float x, int) {
-        double part;
-        if (inside(x, &part)) {
-          atomicAdd(&s.fine_counts[(high - key_of(x)) >> shift], 1u);
-          atomicAdd(&s.fine[(high - key_of(x)) >> shift], excess(part));
+      words_between<T>(row, a.vocabulary, Key::back(low), Key::back(high), [&](float x, int) {
+        const double y = steps.place(x);
+        if (inside(x, y)) {
+          atomicAdd(&s.fine_counts[(high - Key::of(x)) >> shift], 1u);
+          atomicAdd(&s.fine[(high - Key::of(x)) >> shift], steps.excess(y));
         }
       });
       __syncthreads();
       const int i = min((int)threadIdx.x, kSampleBins - 1);
-      run_bins(s, base * ((double)s.fine_counts[i] + (double)s.fine[i] * 0x1p-40), s.fine_counts[i]);
+      run_bins(s, base * ((double)s.fine_counts[i] * 0x1p40 + (double)s.fine[i]), s.fine_counts[i]);
       find_bin(s, count > 0 ? count - taken : 0u, sum - taken_sum);
       taken += s.before;
       taken_sum += s.sum_before;
@@ -342,15 +406,14 @@ struct Sampler {
       while (size < words) size *= 2;
       for (int i = threadIdx.x; i < size; i += kSampleThreads) s.list[i] = ~0ull;
       __syncthreads();
-      words_between<T>(row, a.vocabulary, lowest(bin), highest(bin), [&](float x, int i) {
-        double part;
-        if (inside(x, &part)) {
+      words_between<T>(row, a.vocabulary, Key::back(low), Key::back(high), [&](float x, int i) {
+        if (inside(x, steps.place(x))) {
           const int at = atomicAdd(&s.length, 1);
           if (at < kSampleList) s.list[at] = (unsigned long long)~key_of(x) << 32 | (uint32_t)i;
         }
       });
       __syncthreads();
-      sort(s.list, size);
+      sort(s.list, size, s.fine_counts, s.fine);
       // two words to a thread
       const int i = 2 * threadIdx.x;
       double e[2];
@@ -384,7 +447,7 @@ struct Sampler {
       return {from_key(~(uint32_t)(w >> 32)), (int)(uint32_t)w};
     }
     // all the same: so many of them by their numbers
-    const float x = from_key(high);
+    const float x = Key::back(high);
     const double e = e_of(x);
     int n = count > 0 ? (int)count - taken : (int)fmin((sum - taken_sum) / e, (double)words);
     if (count == 0) {
@@ -394,33 +457,46 @@ struct Sampler {
     n = min(max(n, 1), words);
     int upto = 0x7fffffff;
     if (n < words) {
-      // the n-th by number: a stretch of the row at a time
-      int seen = 0;
-      for (int first = 0; first < a.vocabulary; first += 8 * kSampleThreads) {
+      // the n-th by number: first in which chunk, then there
+      typedef Chunk<T> C;
+      uint32_t* in_chunk = reinterpret_cast<uint32_t*>(s.list);      // [up to kSampleList chunks]
+      for (int c = threadIdx.x >> 6; c < a.chunks; c += kSampleWaves) {
         int mine = 0;
+        each_piece<T>(row, a.vocabulary, c * C::kElements - C::lead(row), C::kElements / C::E, threadIdx.x & 63, 64, [&](const typename Piece<T>::type& v, int) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int i = first + 8 * threadIdx.x + j;
-          mine += i < a.vocabulary && logit<T>(row, i) == x;
-        }
-        const int before = (int)group_scan(s, (double)mine) - mine;
-        if (seen + before < n && n <= seen + before + mine) {
-          int k = seen + before;
-#pragma unroll 1
-          for (int j = 0; j < 8; ++j) {
-            const int i = first + 8 * threadIdx.x + j;
-            if (i < a.vocabulary && logit<T>(row, i) == x && ++k == n) s.found = i;
-          }
-        }
-        int all = 0;
-        for (int w = 0; w < kSampleWaves; ++w) all += (int)s.wave_sums[w];
-        seen += all;
-        __syncthreads();
-        if (seen >= n) {
-          upto = s.found;
-          break;
-        }
+          for (int j = 0; j < C::E; ++j) mine += (float)v[j] == x;
+        });
+        mine = (int)wave_sum((double)mine);
+        if ((threadIdx.x & 63) == 0) in_chunk[c] = (uint32_t)mine;
       }
+      __syncthreads();
+      int two[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) two[j] = 2 * (int)threadIdx.x + j < a.chunks ? (int)in_chunk[2 * threadIdx.x + j] : 0;
+      int before = (int)group_scan(s, (double)(two[0] + two[1])) - two[0] - two[1];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        if (before < n && n <= before + two[j]) {
+          s.found = 2 * (int)threadIdx.x + j;
+          s.before = before;
+        }
+        before += two[j];
+      }
+      __syncthreads();
+      constexpr int EACH = C::kElements / kSampleThreads;
+      const int first = s.found * C::kElements + EACH * (int)threadIdx.x - C::lead(row), wanted = n - s.before;
+      static_assert(EACH == C::E, "a piece to a thread");
+      const typename Piece<T>::type v = piece_at<T>(row, a.vocabulary, first);
+      int mine = 0;
+#pragma unroll
+      for (int j = 0; j < EACH; ++j) mine += (float)v[j] == x;
+      int k = (int)group_scan(s, (double)mine) - mine;
+      if (k < wanted && wanted <= k + mine)
+#pragma unroll
+        for (int j = 0; j < EACH; ++j)
+          if ((float)v[j] == x && ++k == wanted) s.found = first + j;
+      __syncthreads();
+      upto = s.found;
     }
     if (threadIdx.x == 0) {
       s.length = taken + n;
@@ -428,6 +504,63 @@ struct Sampler {
     }
     __syncthreads();
     return {x, upto};
+  }
+
+  // The draw among the `words` words (at most one to a thread) of bins up to `bound`: the first k of them, of those the first up to p of `whole` (below 0: of their sum), of those with e of `least` or more.
+  __device__ void draw(int bound, int words, int k, double whole, double p, double least) {
+    if (threadIdx.x == 0) {
+      s.length = 0;
+      s.found = 0;
+      s.before = 0x7fffffff;
+    }
+    int size = 2;
+    while (size < words) size *= 2;
+    if ((int)threadIdx.x < size) s.list[threadIdx.x] = ~0ull;
+    __syncthreads();
+    words_between<T>(row, a.vocabulary, lowest(bound), INFINITY, [&](float x, int i) {
+      if (steps.bin(steps.place(x)) <= bound) s.list[atomicAdd(&s.length, 1) & (kSampleThreads - 1)] = (unsigned long long)~key_of(x) << 32 | (uint32_t)i;
+    });
+    __syncthreads();
+    sort(s.list, size, s.fine_counts, s.fine);
+    const int i = threadIdx.x, word = (int)(uint32_t)s.list[i];
+    const double e = i < words ? e_of(from_key(~(uint32_t)(s.list[i] >> 32))) : 0.0;
+    double upto = group_scan(s, e);
+    if (i == min(k, words) - 1) s.sum = upto;
+    __syncthreads();
+    const double part = whole < 0.0 ? s.sum : whole;
+    const bool stays = i < words && i < k && (i == 0 || ((p >= 1.0 || upto - e < p * part) && (least == 0.0 || e >= least)));
+    const uint64_t these = __ballot(stays);
+    if (these != 0 && (threadIdx.x & 63) == 0) atomicMax(&s.found, (int)threadIdx.x + 64 - __builtin_clzll(these));
+    __syncthreads();
+    const int kept = s.found;
+    if (i == kept - 1) s.sum_before = upto;
+    double* weights = reinterpret_cast<double*>(s.list + kSampleThreads);
+    weights[i] = e;
+    __syncthreads();
+    const double want = (double)a.uniforms[a_row] * s.sum_before;
+    // in the order of the words' numbers: of a few each adds up all in front of it, more are sorted again
+    int number = word;
+    double run = 0.0;
+    if (kept <= 128) {
+      if (i < kept) {
+#pragma unroll 8
+        for (int j = 0; j < kept; ++j) run += (int)(uint32_t)s.list[j] <= word ? weights[j] : 0.0;
+        atomicMax(&s.length, word + kPast);
+      }
+    } else {
+      s.list[i] = i < kept ? (unsigned long long)(uint32_t)word << 32 | (uint32_t)i : ~0ull;
+      __syncthreads();
+      sort(s.list, size, s.fine_counts, s.fine);
+      number = (int)(uint32_t)(s.list[i] >> 32);
+      run = group_scan(s, i < kept ? weights[(uint32_t)s.list[i]] : 0.0);
+      if (i == kept - 1) atomicMax(&s.length, number + kPast);
+    }
+    if (i < kept && run > want) atomicMin(&s.before, number);
+    __syncthreads();
+    if (i == 0) {
+      a.words[a_row] = min(s.before, s.length - kPast);      // (rounding may leave the sum short of its whole: then it is the last that stays)
+      if (a.kept != nullptr) a.kept[a_row] = kept;
+    }
   }
 };
 
@@ -457,9 +590,11 @@ __global__ void __launch_bounds__(kSampleThreads) sample_choose_kernel(const Sam
 
   // the bins of the row: two threads to each
   {
+    fill_steps(s.table);
     const int b = threadIdx.x & (kSampleBins - 1), half = threadIdx.x / kSampleBins;
     uint32_t count = 0;
     unsigned long long more = 0;
+#pragma unroll 4
     for (int c = half; c < a.chunks; c += 2) {
       const unsigned long long w = bins[(int64_t)c * kSampleBins + b];
       count += (uint32_t)(w >> kCountShift);
@@ -474,27 +609,50 @@ __global__ void __launch_bounds__(kSampleThreads) sample_choose_kernel(const Sam
       more += s.fine[b];
       count += s.fine_counts[b];
     }
-    run_bins(s, base_of(b) * ((double)count + (double)more * 0x1p-40), half == 0 ? count : 0u);
+    const double base = 0x1p-40 * base_of(b);
+    if (half == 0) s.base[b] = base;
+    run_bins(s, base * ((double)count * 0x1p40 + (double)more), half == 0 ? count : 0u);
   }
   const int total = (int)s.counts[kSampleBins - 1];
   const double whole = s.sums[kSampleBins - 1];
-  Sampler<T> sampler{a, s, from, top, steps_by(temperature), 1.0 / (double)temperature};
+  const Steps steps(top, temperature, s.table);
+  Sampler<T> sampler{a, s, row, from, top, 11.541560327111707 / (double)temperature, steps};      // 8 / ln 2
 
   const int k = a.top_k == nullptr || a.top_k[row] <= 0 ? total : min(a.top_k[row], total);
   double p = a.top_p == nullptr ? 1.0 : (double)a.top_p[row], least = a.min_p == nullptr ? 0.0 : (double)a.min_p[row];
   if (!(least > 0.0)) least = 0.0;
+  if (!(p < 1.0)) p = 1.0;
   const bool first_only = p <= 0.0 || least > 1.0;
+  // Where the cut lies at most; where p is of the sum of the first k, all of those are wanted.  If a thread each is enough for the words up to there, they are sorted and the rest of the row is not looked at again.
+  const int mine = min((int)threadIdx.x, kSampleBins - 1);
+  const double my_sum = s.sums[mine];
+  const uint32_t my_count = s.counts[mine];
+  int bound = kSampleBins - 1;
+  if (first_only || k < total) {
+    find_bin(s, first_only ? 1u : (uint32_t)k, 0.0);
+    bound = s.found;
+    __syncthreads();
+  }
+  const bool all_of_k = k < total && p < 1.0;
+  if (p < 1.0 && !first_only && !all_of_k) {
+    find_bin(s, 0u, p * whole * (1.0 + 0x1p-30));
+    bound = min(bound, s.found);
+    __syncthreads();
+  }
+  if (least > 0.0 && !first_only && !all_of_k) bound = min(bound, max((int)(-log2f((float)least) * 8.f) + 1, 0));
+  if (s.counts[bound] <= (uint32_t)kSampleThreads) {
+    sampler.draw(bound, (int)s.counts[bound], first_only ? 1 : k, k < total ? -1.0 : whole, first_only ? 1.0 : p, first_only ? 0.0 : least);
+    return;
+  }
+
   Cut cut{-INFINITY, 0x7fffffff};
   int last = kSampleBins - 1;      // the bin of the last word that stays, or a later one
   double part = whole;             // of the words in front of the first cut
   // first the cut behind so many words, then that behind so much of their sum.  (A bin's words share the space of the bins' running sums.)
-  const int mine = min((int)threadIdx.x, kSampleBins - 1);
-  const double my_sum = s.sums[mine];
-  const uint32_t my_count = s.counts[mine];
 #pragma unroll 1
   for (int stage = 0; stage < 2; ++stage) {
     const uint32_t count = stage > 0 ? 0u : first_only ? 1u : (uint32_t)k;
-    if (stage == 0 ? !first_only && k >= total : first_only || !(p < 1.0)) continue;
+    if (stage == 0 ? !first_only && k >= total : first_only || p == 1.0) continue;
     __syncthreads();
     if (threadIdx.x < kSampleBins) {
       s.sums[threadIdx.x] = my_sum;
@@ -511,68 +669,63 @@ __global__ void __launch_bounds__(kSampleThreads) sample_choose_kernel(const Sam
     last = min(last, bin);
     __syncthreads();
   }
-  if (least > 0.0) {
-    const float t = -log2f((float)least) * 8.f;
-    if (t < (float)last) last = max((int)t, 0);
+  // Bins in front of `near` stay as a whole and are known by chunks, those behind `far` go; the words between are looked at one by one, a chunk to a wavefront.
+  int near = last, far = last;
+  if (least > 0.0 && !first_only) {
+    const int t = (int)fminf(-log2f((float)least) * 8.f, (float)kSampleBins);      // (or one beside it)
+    near = max(min(near, t - 1), 0);
+    far = min(far, t + 1);
   }
-
-  // Bins that stay as a whole are known by chunks; those around the cut are looked at word by word, a chunk to a wavefront.
-  const int near = max(last - 1, 0), far = min(last + 1, kSampleBins - 1);
-  const float low = sampler.lowest(far), high = sampler.highest(near);
-  auto stays = [&](float x, int i, int* bin) {
-    double rest;
-    return step_of(x, top, sampler.by, bin, &rest) && cut.has(x, i) && (least == 0.0 || first_only || sampler.e_of(x) >= least);
+  const float low = fmaxf(sampler.lowest(far), cut.at), high = sampler.highest(near);
+  // e of a word that stays, else 0
+  auto e_if_kept = [&](float x, int i, int from) {
+    const double y = steps.place(x);
+    const int bin = steps.bin(y);
+    if (bin < from || bin >= kSampleBins || !cut.has(x, i)) return 0.0;
+    const double e = x == top ? 1.0 : sampler.e_at(y);
+    return least == 0.0 || first_only || e >= least ? e : 0.0;
   };
   double* chunk_sums = reinterpret_cast<double*>(s.list);      // [up to kSampleList chunks]
   int kept = 0;
   __syncthreads();
   for (int c = wave; c < a.chunks; c += kSampleWaves) {
     double sum = 0.0;
-    for (int b = lane; b < near; b += 64) {
-      const unsigned long long w = bins[(int64_t)c * kSampleBins + b];
-      kept += (int)(w >> kCountShift);
-      sum += base_of(b) * ((double)(w >> kCountShift) + (double)(w & kMask) * 0x1p-40);
-    }
-    constexpr int E = Piece<T>::E;
-    typedef typename Piece<T>::type piece;
-    const T* words = reinterpret_cast<const T*>(from);
-    for (int q = lane; q < Chunk<T>::kElements / E; q += 64) {
-      const int i = c * Chunk<T>::kElements + q * E - Chunk<T>::lead(from);
-      piece v;
-      if (i >= 0 && i + E <= a.vocabulary) {
-        v = *reinterpret_cast<const piece*>(words + i);
-      } else {
+    bool any = false;
+    unsigned long long w[kSampleBins / 64];
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = i + e >= 0 && i + e < a.vocabulary ? words[i + e] : (T)__builtin_nanf("");
-      }
-      each_between<T>(v, from, i, low, high, [&](float x, int at) {
-        int bin;
-        if (stays(x, at, &bin) && bin >= near) {
-          sum += sampler.e_of(x);
-          ++kept;
-        }
-      });
+    for (int j = 0; j < kSampleBins / 64; ++j) w[j] = bins[(int64_t)c * kSampleBins + 64 * j + lane];
+#pragma unroll
+    for (int j = 0; j < kSampleBins / 64; ++j) {
+      any = any || (64 * j + lane >= near && 64 * j + lane <= far && w[j] != 0);
+      if (64 * j + lane >= near) continue;
+      kept += (int)(w[j] >> kCountShift);
+      sum += s.base[64 * j + lane] * ((double)(w[j] >> kCountShift) * 0x1p40 + (double)(w[j] & kMask));
     }
+    if (__any(any))
+      each_piece<T>(from, a.vocabulary, c * Chunk<T>::kElements - Chunk<T>::lead(from), Chunk<T>::kElements / Chunk<T>::E, lane, 64, [&](const typename Piece<T>::type& v, int i) {
+        each_between<T>(v, i, low, high, [&](float x, int at) {
+          const double e = e_if_kept(x, at, near);
+          sum += e;
+          kept += e > 0.0;
+        });
+      });
     sum = wave_sum(sum);
     if (lane == 0) chunk_sums[c] = sum;
   }
   __syncthreads();
+  if (threadIdx.x == 0) s.before = 0;
+  __syncthreads();
   kept = (int)wave_sum((double)kept);
-  if (lane == 0) s.wave_counts[wave] = (uint32_t)kept;
+  if (lane == 0) atomicAdd(&s.before, kept);
   // the chunk of the word: two chunks to a thread
   double pair[2];
 #pragma unroll
   for (int j = 0; j < 2; ++j) pair[j] = 2 * (int)threadIdx.x + j < a.chunks ? chunk_sums[2 * threadIdx.x + j] : 0.0;
   double upto = group_scan(s, pair[0] + pair[1]);
-  double all = 0.0;
-  for (int w = 0; w < kSampleWaves; ++w) all += s.wave_sums[w];
-  const double want = (double)a.uniforms[row] * all;
+  const double all = of_waves(s, kSampleWaves), want = (double)a.uniforms[row] * all;
   if (threadIdx.x == 0) {
     s.found = 0x7fffffff;
     s.length = -1;      // the last chunk with a word
-    uint32_t n = 0;
-    for (int w = 0; w < kSampleWaves; ++w) n += s.wave_counts[w];
-    if (a.kept != nullptr) a.kept[row] = (int)n;
   }
   __syncthreads();
 #pragma unroll
@@ -595,15 +748,14 @@ __global__ void __launch_bounds__(kSampleThreads) sample_choose_kernel(const Sam
   __syncthreads();
   constexpr int EACH = Chunk<T>::kElements / kSampleThreads;
   const int first = chunk * Chunk<T>::kElements + EACH * (int)threadIdx.x - Chunk<T>::lead(from);
-  auto e_at = [&](int i) {
-    if (i < 0 || i >= a.vocabulary) return 0.0;
-    const float x = logit<T>(from, i);
-    int bin;
-    return stays(x, i, &bin) ? sampler.e_of(x) : 0.0;
-  };
-  double sum = 0.0;
-#pragma unroll 1
-  for (int j = 0; j < EACH; ++j) sum += e_at(first + j);
+  static_assert(EACH == Chunk<T>::E, "a piece to a thread");
+  const typename Piece<T>::type x = piece_at<T>(from, a.vocabulary, first);
+  double e[EACH], sum = 0.0;
+#pragma unroll
+  for (int j = 0; j < EACH; ++j) {
+    e[j] = e_if_kept((float)x[j], first + j, 0);
+    sum += e[j];
+  }
   upto = s.sum_before + group_scan(s, sum);
   if (sum > 0.0) {
     atomicMax(&s.length, (int)threadIdx.x);
@@ -613,14 +765,13 @@ __global__ void __launch_bounds__(kSampleThreads) sample_choose_kernel(const Sam
   if ((int)threadIdx.x != min(s.found, s.length)) return;      // (rounding may leave the sum short of its whole: then it is the last that stays)
   double run = upto - sum;
   int word = -1;
-#pragma unroll 1
+#pragma unroll
   for (int j = 0; j < EACH; ++j) {
-    const double e = e_at(first + j);
-    run += e;
-    if (e > 0.0) word = first + j;
-    if (e > 0.0 && run > want) break;
+    if (e[j] > 0.0 && !(word >= 0 && run > want)) word = first + j;
+    run += e[j];
   }
   a.words[row] = word;
+  if (a.kept != nullptr) a.kept[row] = s.before;
 }
 
 }  // namespace dpllm

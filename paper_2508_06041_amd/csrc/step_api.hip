@@ -155,9 +155,9 @@ int check_sample(const char* who, int rows, int vocabulary, int dtype) {
 
 template <typename T>
 void launch_sample(const SampleArgs& a, hipStream_t s) {
-  const unsigned groups = (unsigned)a.rows * a.chunks;
-  hipLaunchKernelGGL(sample_tops_kernel<T>, dim3(groups), dim3(kVerThreads), 0, s, a, Divide::by(a.chunks));
-  hipLaunchKernelGGL(sample_bins_kernel<T>, dim3(groups), dim3(kVerThreads), 0, s, a, Divide::by(a.chunks));
+  const dim3 groups(a.rows < 8 ? a.rows : (a.rows + 7) / 8 * 8, a.chunks);
+  hipLaunchKernelGGL(sample_tops_kernel<T>, groups, dim3(kVerThreads), 0, s, a);
+  hipLaunchKernelGGL(sample_bins_kernel<T>, groups, dim3(kVerThreads), 0, s, a);
   hipLaunchKernelGGL(sample_choose_kernel<T>, dim3(a.rows), dim3(kSampleThreads), 0, s, a);
 }
 
