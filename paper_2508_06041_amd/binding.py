@@ -131,6 +131,9 @@ _calls.bind(C.cast(lib.dpllm_gemv, C.c_void_p).value, C.cast(lib.dpllm_estimate,
 _calls.bind_tokens(tuple(C.cast(f, C.c_void_p).value for f in (lib.dpllm_rope, lib.dpllm_tree_attention_workspace_bytes, lib.dpllm_tree_attention,
                                                                lib.dpllm_verify_workspace_bytes, lib.dpllm_verify, lib.dpllm_cache_append)),
                    (torch.float16, torch.bfloat16, torch.float32, torch.int32, torch.int64, torch.float64), torch.empty_like)
+_calls.bind_step(tuple(C.cast(f, C.c_void_p).value for f in (lib.dpllm_norm_rope, lib.dpllm_quantized_append, lib.dpllm_quantized_read,
+                                                             lib.dpllm_quantized_attention_workspace_bytes, lib.dpllm_quantized_attention, lib.dpllm_sample_workspace_bytes,
+                                                             lib.dpllm_sample)))
 
 
 def _stream():
@@ -455,6 +458,11 @@ def dpllm_norm_rope(x, weights, positions=None, freqs=None, eps=1e-6, out=None, 
     """x: a tensor [batch][tokens][heads][head_dim], or a tuple of such that share everything but their heads (queries, keys).  weights: a tensor [head_dim] or [heads][head_dim]
     for each (None: 1), all of one type.  positions, freqs, scale, layout: as for dpllm_rope; freqs None: the norm alone.  out: where the results go (x itself: in place); new tensors
     unless given.  New results have a gradient with respect to x and the weights."""
+    made = _calls.norm_rope(x, weights, positions, freqs, eps, out, scale, layout)
+    if type(made) is not int:
+        return made
+    if made != _calls.ELSEWHERE:
+        _call(made)
     xs = (x,) if isinstance(x, torch.Tensor) else tuple(x)
     _need(0 < len(xs) <= 4, "dpllm_norm_rope takes 1 to 4 tensors")
     outs = None if out is None else (out,) if isinstance(out, torch.Tensor) else tuple(out)
@@ -580,6 +588,9 @@ class QuantizedCache:
 
 def dpllm_quantized_append(cache, lens, k_new, v_new, path=None, count=None, layer=0):
     """dpllm_cache_append into a QuantizedCache; k_new and v_new are float16, bfloat16 or float32."""
+    made = _calls.quantized_append(cache, lens, k_new, v_new, path, count, layer)
+    if made != _calls.ELSEWHERE:
+        return _call(made)
     _on(cache.k, "the cache")
     if k_new.dim() == 4:
         k_new, v_new = k_new.unsqueeze(0), v_new.unsqueeze(0)
@@ -597,6 +608,12 @@ def dpllm_quantized_append(cache, lens, k_new, v_new, path=None, count=None, lay
 def dpllm_quantized_read(cache, first, tokens, dtype=torch.bfloat16, count=None, layer=0, layers=None, out=None):
     """What a QuantizedCache holds of `tokens` tokens from first[b] on (int32 [batch]; None: 0), as (keys, values) [batch][tokens][heads][head_dim], of `layers` layers from `layer` on
     with a dimension more if that is given.  count: int32 [batch]; from there on, and where the cache holds nothing, are zeros.  out: a pair of tensors to be filled."""
+    if out is None:
+        made = _calls.quantized_read(cache, cache.k, first, tokens, dtype, count, layer, layers)
+        if type(made) is not int:
+            return made
+        if made != _calls.ELSEWHERE:
+            _call(made)
     _on(cache.k, "the cache")
     b = cache.batch if first is None and count is None else (count if first is None else first).shape[0]
     shape = (1 if layers is None else layers, b, tokens, cache.heads, cache.head_dim)
@@ -621,6 +638,11 @@ def dpllm_quantized_attention_workspace_bytes(batch, nodes, heads, kv_heads, hea
 
 def dpllm_quantized_attention(cache, layer, lens, q, k_new=None, v_new=None, mask=None, scale=None, out=None, lse=None, max_len=None, workspace=None):
     """dpllm_tree_attention over a QuantizedCache; q, k_new, v_new and out are float16 or bfloat16.  The result has no gradient."""
+    made = _calls.quantized_attention(cache, layer, lens, q, k_new, v_new, mask, scale, out, lse, max_len, workspace)
+    if type(made) is not int:
+        return made
+    if made != _calls.ELSEWHERE:
+        _call(made)
     _on(cache.k, "the cache")
     dtype = _dtype(q, "q")
     _need(q.dim() == 4 and q.shape[3] == cache.head_dim, "q has to be [batch][nodes][heads][head_dim] of the cache's head_dim")
@@ -659,6 +681,12 @@ def dpllm_sample_workspace_bytes(rows, vocabulary, dtype):
 def dpllm_sample(logits, uniforms, temperature, top_k=None, top_p=None, min_p=None, words=None, kept=None, workspace=None):
     """A word for every row of logits [rows][vocabulary], int32 [rows].  uniforms, temperature, top_p, min_p: float32 [rows]; top_k: int32 [rows]; the last three None: no such
     filter.  words: a new tensor unless given.  kept: int32 [rows], to be filled with how many words could have been drawn.  workspace: uint8, allocated for the call unless given."""
+    if workspace is None:
+        made = _calls.sample(logits, uniforms, temperature, top_k, top_p, min_p, words, kept)
+        if type(made) is not int:
+            return made
+        if made != _calls.ELSEWHERE:
+            _call(made)
     dtype = _dtype(logits, "logits")
     _need(logits.dim() == 2 and (logits.stride(1) == 1 or logits.shape[1] == 1 or logits.numel() == 0), "logits has to be [rows][vocabulary], the words contiguous")
     n, v = logits.shape

@@ -126,6 +126,16 @@ struct TokenCalls {
   decltype(&dpllm_verify) verify;
   decltype(&dpllm_cache_append) append;
 } to{};
+// and those of a step over a quantised cache
+struct StepCalls {
+  decltype(&dpllm_norm_rope) norm_rope;
+  decltype(&dpllm_quantized_append) append;
+  decltype(&dpllm_quantized_read) read;
+  decltype(&dpllm_quantized_attention_workspace_bytes) attention_bytes;
+  decltype(&dpllm_quantized_attention) attention;
+  decltype(&dpllm_sample_workspace_bytes) sample_bytes;
+  decltype(&dpllm_sample) sample;
+} step{};
 // torch.float16, bfloat16, float32, int32, int64, float64, and torch.empty_like
 PyObject *dtypes[6] = {}, *empty_like = nullptr;
 enum { kInt32 = 3, kInt64 = 4, kFloat64 = 5 };
@@ -248,6 +258,21 @@ PyObject* bind_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
+// bind_step(addresses of the functions of StepCalls), behind bind_tokens
+PyObject* bind_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  void* f[7] = {};
+  bool ok = n == 1 && PyTuple_Check(a[0]) && PyTuple_GET_SIZE(a[0]) == 7;
+  for (int i = 0; ok && i < 7; ++i) ok = address(PyTuple_GET_ITEM(a[0], i), &f[i]);
+  if (!ok) {
+    PyErr_SetString(PyExc_TypeError, "bind_step(addresses)");
+    return nullptr;
+  }
+  step = {reinterpret_cast<decltype(step.norm_rope)>(f[0]), reinterpret_cast<decltype(step.append)>(f[1]), reinterpret_cast<decltype(step.read)>(f[2]),
+          reinterpret_cast<decltype(step.attention_bytes)>(f[3]), reinterpret_cast<decltype(step.attention)>(f[4]), reinterpret_cast<decltype(step.sample_bytes)>(f[5]),
+          reinterpret_cast<decltype(step.sample)>(f[6])};
+  Py_RETURN_NONE;
+}
+
 // a new reference to the i-th of a tuple of tensors, or to a lone tensor
 PyObject* item(PyObject* o, int i) { return Py_NewRef(PyTuple_Check(o) ? PyTuple_GET_ITEM(o, i) : o); }
 
@@ -312,15 +337,16 @@ PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return answer(rc, PyTuple_Check(a[0]) ? Py_NewRef(results.o) : item(results.o, 0));
 }
 
-// The dpllm_cache of a Cache object on the current device, and its sequences.
-bool cache_of(PyObject* o, const Place& place, const dpllm_cache** c, int* batch) {
+// The dpllm_cache of a Cache object (or what a QuantizedCache has) on the current device, and its sequences.
+template <typename C>
+bool cache_of(PyObject* o, const Place& place, const C** c, int* batch) {
   const Ref at(PyObject_GetAttr(o, s_address)), b(PyObject_GetAttr(o, s_batch)), device(PyObject_GetAttr(o, s_device));
   void* p = nullptr;
   int index = -1;
   if (at.o == nullptr || b.o == nullptr || device.o == nullptr || !PyLong_Check(at.o) || !address(at.o, &p) || p == nullptr || !as_int(b.o, batch) ||
       !as_int(device.o, &index) || index != place.device)
     return false;
-  *c = static_cast<const dpllm_cache*>(p);
+  *c = static_cast<const C*>(p);
   return true;
 }
 
@@ -335,9 +361,10 @@ PyObject* space(PyObject* maker, size_t es, size_t need, void** p) {
   return nullptr;
 }
 
-// attention(cache, layer, lens, q, k_new, v_new, mask, scale, out, lse, max_len, workspace)
-PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  const dpllm_cache* c = nullptr;
+// attention(cache, layer, lens, q, k_new, v_new, mask, scale, out, lse, max_len, workspace), the same over both kinds of cache.  takes(cache, type): whether q may be of it.
+template <typename C, typename Takes, typename Bytes, typename Call>
+PyObject* attention_over(PyObject* const* a, Py_ssize_t n, Takes takes, Bytes need, Call call) {
+  const C* c = nullptr;
   int sequences = 0, layer = 0, max_len = 0;
   Tensor q, k{}, v{}, m{}, y;
   dpllm_heads hq, hk{}, hv{}, ho;
@@ -345,7 +372,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   void *lens = nullptr, *lse = nullptr, *ws = nullptr;
   Place place;
   size_t bytes = 0;
-  if (n != 12 || to.attention == nullptr || !place.find() || !cache_of(a[0], place, &c, &sequences) || !as_int(a[1], &layer) || !look(a[3], place, &q) || q.dtype != c->dtype || !heads_of(q, &hq) ||
+  if (n != 12 || need == nullptr || !place.find() || !cache_of(a[0], place, &c, &sequences) || !as_int(a[1], &layer) || !look(a[3], place, &q) || !takes(*c, q.dtype) || !heads_of(q, &hq) ||
       q.size[3] != c->head_dim || q.size[0] > sequences || !look_dense(a[2], place, kInt32, 1, q.size[0], 0, 0, &lens) || (a[4] == Py_None) != (a[5] == Py_None) ||
       !look_dense_or_none(a[9], place, 2, 3, q.size[0], q.size[1], q.size[2], &lse))
     return elsewhere();
@@ -361,7 +388,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (a[10] == Py_None ? (max_len = capacity > INT32_MAX ? INT32_MAX : (int)capacity, false) : !as_int(a[10], &max_len)) return elsewhere();
   if (max_len > capacity) max_len = (int)capacity;
   if (a[7] == Py_None ? (scale = (float)(1.0 / __builtin_sqrt((double)q.size[3])), false) : !as_float(a[7], &scale)) return elsewhere();
-  if (to.attention_bytes((int)b, (int)t, (int)q.size[2], c->heads, (int)q.size[3], max_len, &bytes) != DPLLM_OK) return elsewhere();
+  if (need((int)b, (int)t, (int)q.size[2], c->heads, (int)q.size[3], max_len, &bytes) != DPLLM_OK) return elsewhere();
   const Ref result(a[8] == Py_None ? PyObject_CallOneArg(empty_like, a[3]) : Py_NewRef(a[8]));
   if (result.o == nullptr || !(a[8] == Py_None ? look_new(result.o, q, &y) : look(result.o, place, &y)) || y.dtype != q.dtype || !heads_of(y, &ho)) return elsewhere();
   for (int j = 0; j < 4; ++j)
@@ -369,11 +396,19 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const Ref held(a[11] == Py_None ? space(a[3], 2, bytes, &ws) : nullptr);
   if (held.o == nullptr) return elsewhere();
   const int rc = unlocked([&] {
-    return to.attention(c, layer, (int)b, (int)t, (int)q.size[2], static_cast<const int32_t*>(lens), max_len, &hq, a[4] == Py_None ? nullptr : &hk,
-                        a[5] == Py_None ? nullptr : &hv, static_cast<const uint64_t*>(m.data), a[6] == Py_None || m.size[0] == 1 ? 0 : m.size[1] * m.size[2],
-                        scale, &ho, static_cast<float*>(lse), ws, bytes, place.stream);
+    return call(c, layer, (int)b, (int)t, (int)q.size[2], q.dtype, static_cast<const int32_t*>(lens), max_len, &hq, a[4] == Py_None ? nullptr : &hk,
+                a[5] == Py_None ? nullptr : &hv, static_cast<const uint64_t*>(m.data), a[6] == Py_None || m.size[0] == 1 ? 0 : m.size[1] * m.size[2],
+                scale, &ho, static_cast<float*>(lse), ws, bytes, place.stream);
   });
   return answer(rc, Py_NewRef(result.o));
+}
+PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return attention_over<dpllm_cache>(a, n, [](const dpllm_cache& c, int type) { return type == c.dtype; }, to.attention_bytes,
+                                     [](const dpllm_cache* c, int layer, int b, int t, int heads, int, auto... rest) { return to.attention(c, layer, b, t, heads, rest...); });
+}
+PyObject* quantized_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return attention_over<dpllm_quantized_cache>(a, n, [](const dpllm_quantized_cache&, int type) { return type == DPLLM_F16 || type == DPLLM_BF16; }, step.attention_bytes,
+                                               [](auto... all) { return step.attention(all...); });
 }
 
 // verify(logits, tokens, uniforms, temperature, parents, draft, siblings), outputs and workspace new
@@ -413,14 +448,15 @@ PyObject* verify(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return answer(rc, Py_NewRef(results.o));
 }
 
-// append(cache, lens, k_new, v_new, path, count, layer)
-PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  const dpllm_cache* c = nullptr;
+// append(cache, lens, k_new, v_new, path, count, layer), the same into both kinds of cache
+template <typename C, typename Takes, typename Call>
+PyObject* append_to(PyObject* const* a, Py_ssize_t n, Takes takes, Call call) {
+  const C* c = nullptr;
   int sequences = 0, layer = 0;
   Tensor k, v;
   void *lens = nullptr, *path = nullptr, *count = nullptr;
   Place place;
-  if (n != 7 || to.append == nullptr || !place.find() || !cache_of(a[0], place, &c, &sequences) || !look(a[2], place, &k) || !look(a[3], place, &v) || k.dtype != c->dtype || v.dtype != c->dtype ||
+  if (n != 7 || !place.find() || !cache_of(a[0], place, &c, &sequences) || !look(a[2], place, &k) || !look(a[3], place, &v) || !takes(*c, k.dtype) || v.dtype != k.dtype ||
       k.dim != v.dim || k.dim < 4 || !as_int(a[6], &layer))
     return elsewhere();
   const int at = k.dim - 4;
@@ -434,10 +470,137 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return elsewhere();
   const dpllm_heads hk{k.data, k.stride[at], k.stride[at + 1], k.stride[at + 2]}, hv{v.data, v.stride[at], v.stride[at + 1], v.stride[at + 2]};
   const int rc = unlocked([&] {
-    return to.append(c, layer, at ? (int)k.size[0] : 1, (int)b, (int)t, static_cast<const int32_t*>(lens), &hk, at ? k.stride[0] : 0, &hv,
-                     at ? v.stride[0] : 0, static_cast<const int32_t*>(path), t, static_cast<const int32_t*>(count), place.stream);
+    return call(c, layer, at ? (int)k.size[0] : 1, (int)b, (int)t, static_cast<const int32_t*>(lens), k.dtype, &hk, at ? k.stride[0] : 0, &hv,
+                at ? v.stride[0] : 0, static_cast<const int32_t*>(path), t, static_cast<const int32_t*>(count), place.stream);
   });
   return PyLong_FromLong(rc);
+}
+PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return append_to<dpllm_cache>(a, n, [](const dpllm_cache& c, int type) { return to.append != nullptr && type == c.dtype; },
+                                [](const dpllm_cache* c, int layer, int layers, int b, int t, const int32_t* lens, int, auto... rest) {
+                                  return to.append(c, layer, layers, b, t, lens, rest...);
+                                });
+}
+PyObject* quantized_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return append_to<dpllm_quantized_cache>(a, n, [](const dpllm_quantized_cache&, int type) { return step.append != nullptr && type <= DPLLM_F32; },
+                                          [](auto... all) { return step.append(all...); });
+}
+
+// norm_rope(x, weights, positions, freqs, eps, out, scale, layout)
+PyObject* norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  const bool several = n == 8 && PyTuple_Check(a[0]);
+  const int m = several ? (int)PyTuple_GET_SIZE(a[0]) : 1;
+  if (n != 8 || step.norm_rope == nullptr || m < 1 || m > DPLLM_MAX_TENSORS) return elsewhere();
+  for (PyObject* o : {a[1], a[5]})
+    if (o != Py_None && (PyTuple_Check(o) ? (int)PyTuple_GET_SIZE(o) != m : several)) return elsewhere();
+  Tensor x[DPLLM_MAX_TENSORS], pos{}, freqs{};
+  dpllm_heads in[DPLLM_MAX_TENSORS], out[DPLLM_MAX_TENSORS];
+  int heads[DPLLM_MAX_TENSORS], layout = 0, weight_type = -1;
+  const void* weights[DPLLM_MAX_TENSORS] = {};
+  int64_t strides[DPLLM_MAX_TENSORS] = {};
+  float scale = 0.f, eps = 0.f;
+  Place place;
+  if (!place.find() || (a[2] == Py_None) != (a[3] == Py_None) || !as_float(a[4], &eps) || !as_float(a[6], &scale) || !as_int(a[7], &layout)) return elsewhere();
+  if (a[3] != Py_None && (!look(a[2], place, &pos) || pos.dtype != kInt32 || pos.dim < 1 || pos.dim > 2 || !pos.dense(pos.dim) || !look(a[3], place, &freqs) ||
+                          !freqs.is(kFloat64, 1) || !freqs.dense(1) || freqs.size[0] > DPLLM_MAX_HEAD_DIM))
+    return elsewhere();
+  const Ref results(PyTuple_New(m));
+  if (results.o == nullptr) return elsewhere();
+  for (int i = 0; i < m; ++i) {
+    const Ref t(item(a[0], i));
+    if (!look(t.o, place, &x[i]) || graded(t.o) || x[i].dtype > 2 || !heads_of(x[i], &in[i]) || x[i].dtype != x[0].dtype || x[i].size[0] != x[0].size[0] ||
+        x[i].size[1] != x[0].size[1] || x[i].size[3] != x[0].size[3])
+      return elsewhere();
+    heads[i] = (int)x[i].size[2];
+    const Ref given(a[1] == Py_None ? Py_NewRef(Py_None) : item(a[1], i));
+    if (given.o != Py_None) {
+      Tensor w;
+      if (!look(given.o, place, &w) || graded(given.o) || w.dtype > 2 || (weight_type >= 0 && w.dtype != weight_type) || w.dim < 1 || w.dim > 2 || w.size[w.dim - 1] != x[i].size[3] ||
+          !w.dense(1) || (w.dim == 2 && (w.size[0] != heads[i] || (heads[i] > 1 && w.stride[0] == 0))))
+        return elsewhere();
+      weight_type = w.dtype;
+      weights[i] = w.data;
+      strides[i] = w.dim == 2 && heads[i] > 1 ? w.stride[0] : 0;
+    }
+    PyObject* o = a[5] == Py_None ? PyObject_CallOneArg(empty_like, t.o) : item(a[5], i);
+    if (o == nullptr) return elsewhere();
+    PyTuple_SET_ITEM(results.o, i, o);
+    Tensor y;
+    if (!(a[5] == Py_None ? look_new(o, x[i], &y) : look(o, place, &y) && !graded(o)) || y.dtype != x[0].dtype || !heads_of(y, &out[i])) return elsewhere();
+    for (int j = 0; j < 4; ++j)
+      if (y.size[j] != x[i].size[j]) return elsewhere();
+  }
+  if (a[3] != Py_None && (pos.size[pos.dim - 1] != x[0].size[1] || (pos.dim == 2 && pos.size[0] != x[0].size[0]))) return elsewhere();
+  const int rc = unlocked([&] {
+    return step.norm_rope(in, out, heads, weights, strides, weight_type < 0 ? DPLLM_F32 : weight_type, eps, m, (int)x[0].size[0], (int)x[0].size[1], (int)x[0].size[3], x[0].dtype,
+                          a[3] == Py_None ? 0 : (int)(2 * freqs.size[0]), layout, static_cast<const double*>(freqs.data), scale, static_cast<const int32_t*>(pos.data),
+                          a[3] == Py_None || pos.dim == 1 ? 0 : x[0].size[1], place.stream);
+  });
+  return answer(rc, several ? Py_NewRef(results.o) : item(results.o, 0));
+}
+
+// quantized_read(cache, codes, first, tokens, dtype, count, layer, layers) into new tensors; codes: the cache's k
+PyObject* quantized_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  const dpllm_quantized_cache* c = nullptr;
+  int sequences = 0, tokens = 0, layer = 0, layers = 1, type = -1;
+  void *first = nullptr, *count = nullptr;
+  Place place;
+  if (n != 8 || step.read == nullptr || !place.find() || !cache_of(a[0], place, &c, &sequences) || !as_int(a[3], &tokens) || !as_int(a[6], &layer) ||
+      (a[7] != Py_None && !as_int(a[7], &layers)) || tokens < 1 || layers < 1)
+    return elsewhere();
+  for (int i = 0; i < 3; ++i)
+    if (a[4] == dtypes[i]) type = i;
+  int64_t b = sequences;
+  PyObject* by = a[2] != Py_None ? a[2] : a[5];
+  if (by != Py_None) {
+    Tensor t;
+    if (!look(by, place, &t) || !t.is(kInt32, 1)) return elsewhere();
+    b = t.size[0];
+  }
+  if (type < 0 || b < 1 || b > sequences || !look_dense_or_none(a[2], place, kInt32, 1, b, 0, 0, &first) || !look_dense_or_none(a[5], place, kInt32, 1, b, 0, 0, &count)) return elsewhere();
+  const bool several = a[7] != Py_None;
+  const Ref shape(several ? Py_BuildValue("(iLiii)", layers, (long long)b, tokens, c->heads, c->head_dim) : Py_BuildValue("(Liii)", (long long)b, tokens, c->heads, c->head_dim)), results(PyTuple_New(2)), names(Py_BuildValue("(O)", s_dtype));
+  if (shape.o == nullptr || results.o == nullptr || names.o == nullptr) return elsewhere();
+  void* p[2] = {};
+  for (int i = 0; i < 2; ++i) {
+    PyObject* args[3] = {a[1], shape.o, a[4]};
+    PyObject* o = PyObject_VectorcallMethod(s_new_empty, args, 2, names.o);
+    if (o == nullptr) return elsewhere();
+    PyTuple_SET_ITEM(results.o, i, o);
+    if (!tensor(o, &p[i])) return elsewhere();
+  }
+  const int64_t head = c->head_dim, token = head * c->heads, sequence = token * tokens;
+  const dpllm_heads k{p[0], sequence, token, head}, v{p[1], sequence, token, head};
+  const int rc = unlocked([&] {
+    return step.read(c, layer, layers, (int)b, tokens, static_cast<const int32_t*>(first), static_cast<const int32_t*>(count), type, &k, sequence * b, &v, sequence * b, place.stream);
+  });
+  return answer(rc, Py_NewRef(results.o));
+}
+
+// sample(logits, uniforms, temperature, top_k, top_p, min_p, words, kept), the workspace new
+PyObject* sample(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Tensor x;
+  void *uniforms = nullptr, *temperature = nullptr, *top_k = nullptr, *top_p = nullptr, *min_p = nullptr, *words = nullptr, *kept = nullptr, *ws = nullptr;
+  Place place;
+  size_t bytes = 0;
+  if (n != 8 || step.sample == nullptr || !place.find() || !look(a[0], place, &x) || x.dtype > 2 || x.dim != 2 || (x.stride[1] != 1 && x.size[1] != 1)) return elsewhere();
+  const int64_t b = x.size[0];
+  if (!look_dense(a[1], place, 2, 1, b, 0, 0, &uniforms) || !look_dense(a[2], place, 2, 1, b, 0, 0, &temperature) || !look_dense_or_none(a[3], place, kInt32, 1, b, 0, 0, &top_k) ||
+      !look_dense_or_none(a[4], place, 2, 1, b, 0, 0, &top_p) || !look_dense_or_none(a[5], place, 2, 1, b, 0, 0, &min_p) || !look_dense_or_none(a[7], place, kInt32, 1, b, 0, 0, &kept) ||
+      step.sample_bytes((int)b, (int)x.size[1], x.dtype, &bytes) != DPLLM_OK)
+    return elsewhere();
+  const Ref names(Py_BuildValue("(O)", s_dtype)), number(PyLong_FromLongLong(b));
+  PyObject* args[3] = {a[1], number.o, dtypes[kInt32]};
+  const Ref result(names.o == nullptr || number.o == nullptr ? nullptr : a[6] == Py_None ? PyObject_VectorcallMethod(s_new_empty, args, 2, names.o) : Py_NewRef(a[6]));
+  if (result.o == nullptr || !(a[6] == Py_None ? tensor(result.o, &words) : look_dense(result.o, place, kInt32, 1, b, 0, 0, &words))) return elsewhere();
+  const Ref held(space(a[1], 4, bytes, &ws));
+  if (held.o == nullptr) return elsewhere();
+  const int rc = unlocked([&] {
+    return step.sample((int)b, (int)x.size[1], x.dtype, x.data, x.stride[0], static_cast<const float*>(uniforms), static_cast<const float*>(temperature),
+                       static_cast<const int32_t*>(top_k), static_cast<const float*>(top_p), static_cast<const float*>(min_p), static_cast<int32_t*>(words),
+                       static_cast<int32_t*>(kept), ws, bytes, place.stream);
+  });
+  return answer(rc, Py_NewRef(result.o));
 }
 
 using Fast = PyObject* (*)(PyObject*, PyObject* const*, Py_ssize_t);
@@ -450,6 +613,12 @@ PyMethodDef methods[] = {{"bind", as_method(bind), METH_FASTCALL, nullptr},
                          {"attention", as_method(attention), METH_FASTCALL, nullptr},
                          {"verify", as_method(verify), METH_FASTCALL, nullptr},
                          {"append", as_method(append), METH_FASTCALL, nullptr},
+                         {"bind_step", as_method(bind_step), METH_FASTCALL, nullptr},
+                         {"norm_rope", as_method(norm_rope), METH_FASTCALL, nullptr},
+                         {"quantized_append", as_method(quantized_append), METH_FASTCALL, nullptr},
+                         {"quantized_read", as_method(quantized_read), METH_FASTCALL, nullptr},
+                         {"quantized_attention", as_method(quantized_attention), METH_FASTCALL, nullptr},
+                         {"sample", as_method(sample), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef definition = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
