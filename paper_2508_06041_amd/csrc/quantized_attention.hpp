@@ -3,7 +3,8 @@
 // With key codes c, their scale s (and offset f) the score of a cached token is x = s (q . c) + f (sum of q), and with value codes d, scale u (and offset g) its part of the
 // result is w u d + w g.  So the codes go into the matrix pipe as they are, whole or half numbers that 16 bits hold exactly, and scales and offsets
 // meet scores and weights in 32 bits: no value is rounded that was not rounded when it was quantised.  The weights w u are rounded to float16 whatever the results are (three bits more than
-// bfloat16 has, as the codes are exact in either); u relative to a power of two that is above all the wavefront has met, so that w u is in the range that w is kept in (tree_attention.hpp).
+// bfloat16 has, as the codes are exact in either), and what that leaves is a second product where the results are float16 too, which would be half as far off again without it (at 3 % of a call's
+// time for few rows, 11 % for 52 over the longest contexts, 97 -> 108 us); u relative to a power of two that is above all the wavefront has met, so that w u is in the range that w is kept in (tree_attention.hpp).
 #pragma once
 #include <type_traits>
 
@@ -266,7 +267,7 @@ struct QuantizedRows : Rows<MT, DV> {
 
 // A step's share of the results: products of codes s, scales (and offsets) of keys, times scale_log2, and of values, these by the unit, of the lane's tokens; values(v): theirs, in the
 // order of value_pairs.
-template <int FORMAT, int D, int MT, typename F>
+template <int FORMAT, typename T, int D, int MT, typename F>
 __device__ __forceinline__ void add_values(const QuantizedArgs& a, QuantizedRows<MT, D / 16>& rows, Scores<MT>& s, const float (&q_sum)[MT], const float (&k_scale)[8],
                                            const float (&k_offset)[8], const float (&v_scale)[8], const float (&v_offset)[8], F values) {
   Weights w[MT];
@@ -275,7 +276,8 @@ __device__ __forceinline__ void add_values(const QuantizedArgs& a, QuantizedRows
   for (int mt = 0; mt < MT; ++mt) before[mt] = rows.top[mt];
   weigh_codes<FORMAT, MT, D / 16>(rows, s, k_scale, k_offset, q_sum, a.scale_log2, w);
   if (FORMAT == kInt4) rows.follow(before, a.scale_log2);
-  u32x4 p[MT];
+  constexpr bool FINE = std::is_same<T, half_t>::value;
+  u32x4 p[MT], rest[MT];
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     if (FORMAT == kInt4)
@@ -283,13 +285,24 @@ __device__ __forceinline__ void add_values(const QuantizedArgs& a, QuantizedRows
       for (int i = 0; i < 8; ++i) rows.offset[mt] = __builtin_fmaf(w[mt].w[i], v_offset[i], rows.offset[mt]);
 #pragma unroll
     for (int i = 0; i < 4; ++i) p[mt][i] = pack2<half_t>(w[mt].w[2 * i] * v_scale[2 * i], w[mt].w[2 * i + 1] * v_scale[2 * i + 1]);
+    if (FINE)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        typedef half_t halves __attribute__((ext_vector_type(2)));
+        const uint32_t both = p[mt][i];      // (__builtin_bit_cast of an element takes the vector's first)
+        const halves h = __builtin_bit_cast(halves, both);
+        rest[mt][i] = pack2<half_t>(__builtin_fmaf(w[mt].w[2 * i], v_scale[2 * i], -(float)h[0]), __builtin_fmaf(w[mt].w[2 * i + 1], v_scale[2 * i + 1], -(float)h[1]));
+      }
   }
   u32x4 v[D / 16];
   values(v);
 #pragma unroll
   for (int j = 0; j < D / 16; ++j)
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) rows.o[mt][j] = Matrix<half_t>::mad(v[j], p[mt], rows.o[mt][j]);
+    for (int mt = 0; mt < MT; ++mt) {
+      rows.o[mt][j] = Matrix<half_t>::mad(v[j], p[mt], rows.o[mt][j]);
+      if (FINE) rows.o[mt][j] = Matrix<half_t>::mad(v[j], rest[mt], rows.o[mt][j]);
+    }
 }
 
 // Behind the steps of codes: the results become whole (relative to the tops alone), and the nodes' steps from `step` on, every turns-th, are added as they are.  For bfloat16, whose values may be of any
@@ -624,7 +637,7 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) quantized_attent
 #pragma unroll
         for (int j = 0; j < H::VW; ++j) v[i].w[j] = (x.there >> (8 * g + i)) & 1 ? v[i].w[j] : 0u;
     }
-    add_values<FORMAT, D, MT>(a, rows, s, q_sum, k_scale, k_offset, v_scale, v_offset, [&](u32x4(&to)[DV]) {
+    add_values<FORMAT, T, D, MT>(a, rows, s, q_sum, k_scale, k_offset, v_scale, v_offset, [&](u32x4(&to)[DV]) {
       uint32_t pairs[4][DV];
 #pragma unroll
       for (int i = 0; i < 4; ++i) value_pairs<FORMAT, DV>(v[2 * i], v[2 * i + 1], pairs[i]);
@@ -848,7 +861,7 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) quantized_attent
       for (int mt = 0; mt < MT; ++mt) seen[mt] = (there >> (8 * g)) & 0xffu;
       mask<MT>(s, seen);
     }
-    add_values<FORMAT, D, MT>(a, rows, s, q_sum, k_scale, k_offset, v_scale, v_offset, [&](u32x4(&v)[DV]) {
+    add_values<FORMAT, T, D, MT>(a, rows, s, q_sum, k_scale, k_offset, v_scale, v_offset, [&](u32x4(&v)[DV]) {
 #pragma unroll
       for (int j = 0; j < DV; ++j) {
         const int d = value_dim<D>(n, j);
