@@ -131,7 +131,8 @@ _calls.bind(C.cast(lib.dpllm_gemv, C.c_void_p).value, C.cast(lib.dpllm_estimate,
 _calls.bind_tokens(tuple(C.cast(f, C.c_void_p).value for f in (lib.dpllm_rope, lib.dpllm_tree_attention_workspace_bytes, lib.dpllm_tree_attention,
                                                                lib.dpllm_verify_workspace_bytes, lib.dpllm_verify, lib.dpllm_cache_append)),
                    (torch.float16, torch.bfloat16, torch.float32, torch.int32, torch.int64, torch.float64), torch.empty_like)
-_calls.bind_step(tuple(C.cast(f, C.c_void_p).value for f in (lib.dpllm_norm_rope, lib.dpllm_quantized_append, lib.dpllm_quantized_read,
+_calls.bind_step(tuple(C.cast(f, C.c_void_p).value for f in (lib.dpllm_norm_rope, lib.dpllm_norm_rope_backward_workspace_bytes, lib.dpllm_norm_rope_backward,
+                                                             lib.dpllm_quantized_append, lib.dpllm_quantized_read,
                                                              lib.dpllm_quantized_attention_workspace_bytes, lib.dpllm_quantized_attention, lib.dpllm_sample_workspace_bytes,
                                                              lib.dpllm_sample)))
 
@@ -494,6 +495,12 @@ def dpllm_norm_rope_backward_workspace_bytes(heads, weight_strides, batch, token
 def dpllm_norm_rope_backward(x, grads, weights, positions=None, freqs=None, eps=1e-6, out=None, scale=1.0, layout=DPLLM_ROPE_HALF, wanted=None, workspace=None):
     """The gradients of the inputs and of the weights of dpllm_norm_rope from those of its results, grads, as (like x, like weights).  out: where those of the inputs go (grads or x
     themselves, say).  wanted: a truth value for each weight whether its gradient is (all are unless given; the others give None).  workspace: uint8, allocated for the call unless given."""
+    if workspace is None:
+        made = _calls.norm_rope_backward(x, grads, weights, positions, freqs, eps, out, scale, layout, wanted)
+        if type(made) is not int:
+            return made
+        if made != _calls.ELSEWHERE:
+            _call(made)
     lone = isinstance(x, torch.Tensor)
     xs, gs = (x,) if lone else tuple(x), (grads,) if isinstance(grads, torch.Tensor) else tuple(grads)
     _need(0 < len(xs) <= 4, "dpllm_norm_rope_backward takes 1 to 4 tensors")

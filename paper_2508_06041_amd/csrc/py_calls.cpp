@@ -129,6 +129,8 @@ struct TokenCalls {
 // and those of a step over a quantised cache
 struct StepCalls {
   decltype(&dpllm_norm_rope) norm_rope;
+  decltype(&dpllm_norm_rope_backward_workspace_bytes) norm_bytes;
+  decltype(&dpllm_norm_rope_backward) norm_backward;
   decltype(&dpllm_quantized_append) append;
   decltype(&dpllm_quantized_read) read;
   decltype(&dpllm_quantized_attention_workspace_bytes) attention_bytes;
@@ -260,16 +262,16 @@ PyObject* bind_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 // bind_step(addresses of the functions of StepCalls), behind bind_tokens
 PyObject* bind_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  void* f[7] = {};
-  bool ok = n == 1 && PyTuple_Check(a[0]) && PyTuple_GET_SIZE(a[0]) == 7;
-  for (int i = 0; ok && i < 7; ++i) ok = address(PyTuple_GET_ITEM(a[0], i), &f[i]);
+  void* f[9] = {};
+  bool ok = n == 1 && PyTuple_Check(a[0]) && PyTuple_GET_SIZE(a[0]) == 9;
+  for (int i = 0; ok && i < 9; ++i) ok = address(PyTuple_GET_ITEM(a[0], i), &f[i]);
   if (!ok) {
     PyErr_SetString(PyExc_TypeError, "bind_step(addresses)");
     return nullptr;
   }
-  step = {reinterpret_cast<decltype(step.norm_rope)>(f[0]), reinterpret_cast<decltype(step.append)>(f[1]), reinterpret_cast<decltype(step.read)>(f[2]),
-          reinterpret_cast<decltype(step.attention_bytes)>(f[3]), reinterpret_cast<decltype(step.attention)>(f[4]), reinterpret_cast<decltype(step.sample_bytes)>(f[5]),
-          reinterpret_cast<decltype(step.sample)>(f[6])};
+  step = {reinterpret_cast<decltype(step.norm_rope)>(f[0]), reinterpret_cast<decltype(step.norm_bytes)>(f[1]), reinterpret_cast<decltype(step.norm_backward)>(f[2]),
+          reinterpret_cast<decltype(step.append)>(f[3]), reinterpret_cast<decltype(step.read)>(f[4]), reinterpret_cast<decltype(step.attention_bytes)>(f[5]),
+          reinterpret_cast<decltype(step.attention)>(f[6]), reinterpret_cast<decltype(step.sample_bytes)>(f[7]), reinterpret_cast<decltype(step.sample)>(f[8])};
   Py_RETURN_NONE;
 }
 
@@ -486,57 +488,125 @@ PyObject* quantized_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
                                           [](auto... all) { return step.append(all...); });
 }
 
-// norm_rope(x, weights, positions, freqs, eps, out, scale, layout)
-PyObject* norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  const bool several = n == 8 && PyTuple_Check(a[0]);
-  const int m = several ? (int)PyTuple_GET_SIZE(a[0]) : 1;
-  if (n != 8 || step.norm_rope == nullptr || m < 1 || m > DPLLM_MAX_TENSORS) return elsewhere();
-  for (PyObject* o : {a[1], a[5]})
-    if (o != Py_None && (PyTuple_Check(o) ? (int)PyTuple_GET_SIZE(o) != m : several)) return elsewhere();
+// What both directions of the norms take: x, weights, positions, freqs, eps, out, scale, layout, and grads where those are not nullptr.
+struct Norms {
+  int m, heads[DPLLM_MAX_TENSORS], layout = 0, weight_type = -1;
   Tensor x[DPLLM_MAX_TENSORS], pos{}, freqs{};
-  dpllm_heads in[DPLLM_MAX_TENSORS], out[DPLLM_MAX_TENSORS];
-  int heads[DPLLM_MAX_TENSORS], layout = 0, weight_type = -1;
+  dpllm_heads in[DPLLM_MAX_TENSORS], grads[DPLLM_MAX_TENSORS], out[DPLLM_MAX_TENSORS];
   const void* weights[DPLLM_MAX_TENSORS] = {};
   int64_t strides[DPLLM_MAX_TENSORS] = {};
   float scale = 0.f, eps = 0.f;
   Place place;
-  if (!place.find() || (a[2] == Py_None) != (a[3] == Py_None) || !as_float(a[4], &eps) || !as_float(a[6], &scale) || !as_int(a[7], &layout)) return elsewhere();
-  if (a[3] != Py_None && (!look(a[2], place, &pos) || pos.dtype != kInt32 || pos.dim < 1 || pos.dim > 2 || !pos.dense(pos.dim) || !look(a[3], place, &freqs) ||
-                          !freqs.is(kFloat64, 1) || !freqs.dense(1) || freqs.size[0] > DPLLM_MAX_HEAD_DIM))
-    return elsewhere();
-  const Ref results(PyTuple_New(m));
-  if (results.o == nullptr) return elsewhere();
-  for (int i = 0; i < m; ++i) {
-    const Ref t(item(a[0], i));
-    if (!look(t.o, place, &x[i]) || graded(t.o) || x[i].dtype > 2 || !heads_of(x[i], &in[i]) || x[i].dtype != x[0].dtype || x[i].size[0] != x[0].size[0] ||
+  bool turned;
+  int rotary() const { return turned ? (int)(2 * freqs.size[0]) : 0; }
+  int64_t positions_stride() const { return turned && pos.dim == 2 ? x[0].size[1] : 0; }
+  int type() const { return weight_type < 0 ? DPLLM_F32 : weight_type; }
+};
+bool look_norms(Norms& k, PyObject* xs, PyObject* ws, PyObject* positions, PyObject* freqs, PyObject* eps, PyObject* outs, PyObject* scale, PyObject* layout, PyObject* grads, PyObject* results) {
+  k.turned = freqs != Py_None;
+  if (!k.place.find() || (positions == Py_None) != (freqs == Py_None) || !as_float(eps, &k.eps) || !as_float(scale, &k.scale) || !as_int(layout, &k.layout)) return false;
+  if (k.turned && (!look(positions, k.place, &k.pos) || k.pos.dtype != kInt32 || k.pos.dim < 1 || k.pos.dim > 2 || !k.pos.dense(k.pos.dim) || !look(freqs, k.place, &k.freqs) ||
+                   !k.freqs.is(kFloat64, 1) || !k.freqs.dense(1) || k.freqs.size[0] > DPLLM_MAX_HEAD_DIM))
+    return false;
+  const Tensor* x = k.x;
+  auto alike = [&](const Tensor& t, int i) {
+    for (int j = 0; j < 4; ++j)
+      if (t.size[j] != x[i].size[j]) return false;
+    return t.dtype == x[0].dtype;
+  };
+  for (int i = 0; i < k.m; ++i) {
+    const Ref t(item(xs, i));
+    if (!look(t.o, k.place, &k.x[i]) || graded(t.o) || x[i].dtype > 2 || !heads_of(x[i], &k.in[i]) || x[i].dtype != x[0].dtype || x[i].size[0] != x[0].size[0] ||
         x[i].size[1] != x[0].size[1] || x[i].size[3] != x[0].size[3])
-      return elsewhere();
-    heads[i] = (int)x[i].size[2];
-    const Ref given(a[1] == Py_None ? Py_NewRef(Py_None) : item(a[1], i));
+      return false;
+    k.heads[i] = (int)x[i].size[2];
+    const Ref given(ws == Py_None ? Py_NewRef(Py_None) : item(ws, i));
     if (given.o != Py_None) {
       Tensor w;
-      if (!look(given.o, place, &w) || graded(given.o) || w.dtype > 2 || (weight_type >= 0 && w.dtype != weight_type) || w.dim < 1 || w.dim > 2 || w.size[w.dim - 1] != x[i].size[3] ||
-          !w.dense(1) || (w.dim == 2 && (w.size[0] != heads[i] || (heads[i] > 1 && w.stride[0] == 0))))
-        return elsewhere();
-      weight_type = w.dtype;
-      weights[i] = w.data;
-      strides[i] = w.dim == 2 && heads[i] > 1 ? w.stride[0] : 0;
+      // (gradients are laid out as their weights, which have no gaps then)
+      if (!look(given.o, k.place, &w) || graded(given.o) || w.dtype > 2 || (k.weight_type >= 0 && w.dtype != k.weight_type) || w.dim < 1 || w.dim > 2 || w.size[w.dim - 1] != x[i].size[3] ||
+          !w.dense(grads ? w.dim : 1) || (w.dim == 2 && (w.size[0] != k.heads[i] || (k.heads[i] > 1 && w.stride[0] == 0))))
+        return false;
+      k.weight_type = w.dtype;
+      k.weights[i] = w.data;
+      k.strides[i] = w.dim == 2 && k.heads[i] > 1 ? w.stride[0] : 0;
     }
-    PyObject* o = a[5] == Py_None ? PyObject_CallOneArg(empty_like, t.o) : item(a[5], i);
-    if (o == nullptr) return elsewhere();
-    PyTuple_SET_ITEM(results.o, i, o);
+    if (grads) {
+      const Ref g(item(grads, i));
+      Tensor y;
+      if (!look(g.o, k.place, &y) || graded(g.o) || !heads_of(y, &k.grads[i]) || !alike(y, i)) return false;
+    }
+    PyObject* o = outs == Py_None ? PyObject_CallOneArg(empty_like, t.o) : item(outs, i);
+    if (o == nullptr) return false;
+    PyTuple_SET_ITEM(results, i, o);
     Tensor y;
-    if (!(a[5] == Py_None ? look_new(o, x[i], &y) : look(o, place, &y) && !graded(o)) || y.dtype != x[0].dtype || !heads_of(y, &out[i])) return elsewhere();
-    for (int j = 0; j < 4; ++j)
-      if (y.size[j] != x[i].size[j]) return elsewhere();
+    if (!(outs == Py_None ? look_new(o, x[i], &y) : look(o, k.place, &y) && !graded(o)) || !heads_of(y, &k.out[i]) || !alike(y, i)) return false;
   }
-  if (a[3] != Py_None && (pos.size[pos.dim - 1] != x[0].size[1] || (pos.dim == 2 && pos.size[0] != x[0].size[0]))) return elsewhere();
+  return !k.turned || (k.pos.size[k.pos.dim - 1] == x[0].size[1] && (k.pos.dim == 1 || k.pos.size[0] == x[0].size[0]));
+}
+// whether each of the others (or None) goes with xs: how many those are, else 0
+int count_norms(PyObject* xs, std::initializer_list<PyObject*> others) {
+  const bool several = PyTuple_Check(xs);
+  const int m = several ? (int)PyTuple_GET_SIZE(xs) : 1;
+  if (m < 1 || m > DPLLM_MAX_TENSORS) return 0;
+  for (PyObject* o : others)
+    if (o != Py_None && (PyTuple_Check(o) ? (int)PyTuple_GET_SIZE(o) != m : several)) return 0;
+  return m;
+}
+
+// norm_rope(x, weights, positions, freqs, eps, out, scale, layout)
+PyObject* norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Norms k;
+  k.m = n == 8 && step.norm_rope != nullptr ? count_norms(a[0], {a[1], a[5]}) : 0;
+  if (k.m == 0) return elsewhere();
+  const Ref results(PyTuple_New(k.m));
+  if (results.o == nullptr || !look_norms(k, a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], nullptr, results.o)) return elsewhere();
   const int rc = unlocked([&] {
-    return step.norm_rope(in, out, heads, weights, strides, weight_type < 0 ? DPLLM_F32 : weight_type, eps, m, (int)x[0].size[0], (int)x[0].size[1], (int)x[0].size[3], x[0].dtype,
-                          a[3] == Py_None ? 0 : (int)(2 * freqs.size[0]), layout, static_cast<const double*>(freqs.data), scale, static_cast<const int32_t*>(pos.data),
-                          a[3] == Py_None || pos.dim == 1 ? 0 : x[0].size[1], place.stream);
+    return step.norm_rope(k.in, k.out, k.heads, k.weights, k.strides, k.type(), k.eps, k.m, (int)k.x[0].size[0], (int)k.x[0].size[1], (int)k.x[0].size[3], k.x[0].dtype, k.rotary(), k.layout,
+                          static_cast<const double*>(k.freqs.data), k.scale, static_cast<const int32_t*>(k.pos.data), k.positions_stride(), k.place.stream);
   });
-  return answer(rc, several ? Py_NewRef(results.o) : item(results.o, 0));
+  return answer(rc, PyTuple_Check(a[0]) ? Py_NewRef(results.o) : item(results.o, 0));
+}
+
+// norm_rope_backward(x, grads, weights, positions, freqs, eps, out, scale, layout, wanted), the workspace new
+PyObject* norm_rope_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Norms k;
+  k.m = n == 10 && step.norm_backward != nullptr ? count_norms(a[0], {a[1], a[2], a[6]}) : 0;
+  if (k.m == 0 || a[1] == Py_None) return elsewhere();
+  const Ref results(PyTuple_New(k.m)), made(PyTuple_New(k.m));
+  if (results.o == nullptr || made.o == nullptr || !look_norms(k, a[0], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[1], results.o)) return elsewhere();
+  void *grads[DPLLM_MAX_TENSORS] = {}, *ws = nullptr;
+  size_t bytes = 0;
+  bool some = false;
+  for (int i = 0; i < k.m; ++i) {
+    int want = k.weights[i] != nullptr;
+    if (want && a[9] != Py_None) {
+      const Ref w(PySequence_GetItem(a[9], i));
+      want = w.o == nullptr ? -1 : PyObject_IsTrue(w.o);
+    }
+    if (want < 0) return elsewhere();
+    PyObject* o = Py_None;
+    if (want) {
+      const Ref w(item(a[2], i));
+      o = PyObject_CallOneArg(empty_like, w.o);
+      if (o == nullptr) return elsewhere();
+    } else {
+      Py_INCREF(o);
+    }
+    PyTuple_SET_ITEM(made.o, i, o);
+    if (want && !tensor(o, &grads[i])) return elsewhere();
+    some = some || want;
+  }
+  if (some && step.norm_bytes(k.heads, k.strides, k.m, (int)k.x[0].size[0], (int)k.x[0].size[1], (int)k.x[0].size[3], &bytes) != DPLLM_OK) return elsewhere();
+  const Ref first(item(a[0], 0)), held(space(first.o, k.x[0].dtype == DPLLM_F32 ? 4 : 2, bytes, &ws));
+  if (held.o == nullptr) return elsewhere();
+  const int rc = unlocked([&] {
+    return step.norm_backward(k.in, k.grads, k.out, k.heads, k.weights, grads, k.strides, k.type(), k.eps, k.m, (int)k.x[0].size[0], (int)k.x[0].size[1], (int)k.x[0].size[3], k.x[0].dtype,
+                              k.rotary(), k.layout, static_cast<const double*>(k.freqs.data), k.scale, static_cast<const int32_t*>(k.pos.data), k.positions_stride(), ws, bytes,
+                              k.place.stream);
+  });
+  if (PyTuple_Check(a[0])) return answer(rc, PyTuple_Pack(2, results.o, made.o));
+  return answer(rc, PyTuple_Pack(2, PyTuple_GET_ITEM(results.o, 0), PyTuple_GET_ITEM(made.o, 0)));
 }
 
 // quantized_read(cache, codes, first, tokens, dtype, count, layer, layers) into new tensors; codes: the cache's k
@@ -615,6 +685,7 @@ PyMethodDef methods[] = {{"bind", as_method(bind), METH_FASTCALL, nullptr},
                          {"append", as_method(append), METH_FASTCALL, nullptr},
                          {"bind_step", as_method(bind_step), METH_FASTCALL, nullptr},
                          {"norm_rope", as_method(norm_rope), METH_FASTCALL, nullptr},
+                         {"norm_rope_backward", as_method(norm_rope_backward), METH_FASTCALL, nullptr},
                          {"quantized_append", as_method(quantized_append), METH_FASTCALL, nullptr},
                          {"quantized_read", as_method(quantized_read), METH_FASTCALL, nullptr},
                          {"quantized_attention", as_method(quantized_attention), METH_FASTCALL, nullptr},

@@ -9,7 +9,7 @@ import paper_2508_06041_amd as dp
 from paper_2508_06041_amd import binding
 from test_token_devices import OnAnother, OnDevice, calls, heads_first, on
 
-NATIVE = ("dpllm_norm_rope", "dpllm_quantized_append", "dpllm_quantized_read", "dpllm_quantized_attention_workspace_bytes", "dpllm_quantized_attention", "dpllm_sample_workspace_bytes", "dpllm_sample")
+NATIVE = ("dpllm_norm_rope", "dpllm_norm_rope_backward_workspace_bytes", "dpllm_norm_rope_backward", "dpllm_quantized_append", "dpllm_quantized_read", "dpllm_quantized_attention_workspace_bytes", "dpllm_quantized_attention", "dpllm_sample_workspace_bytes", "dpllm_sample")
 DTYPES = (torch.float16, torch.bfloat16, torch.float32, torch.int32, torch.int64, torch.float64)
 KINDS = {"e4m3": dp.DPLLM_CACHE_E4M3, "int8": dp.DPLLM_CACHE_INT8, "int4": dp.DPLLM_CACHE_INT4}
 
@@ -48,7 +48,7 @@ def made(monkeypatch):
                 got.append((name, [plain(v) for v in a]))
             return 0
         return f
-    for name in (*NATIVE, "dpllm_norm_rope_backward", "dpllm_norm_rope_backward_workspace_bytes"):
+    for name in NATIVE:
         stubs[name] = C.CFUNCTYPE(C.c_int, *getattr(binding.lib, name).argtypes)(need(name))
         monkeypatch.setattr(binding.lib, name, stubs[name])
     calls.bind(1, 1, lambda: 0, lambda device: 0)
@@ -181,8 +181,9 @@ def test_the_interpreter_is_free_while_the_library_works(made, f):
     holds = C.cast(C.pythonapi.PyGILState_Check, C.c_void_p).value
     nothing = C.CFUNCTYPE(C.c_int, *[C.c_int] * 6, C.POINTER(C.c_size_t))(lambda *a: 0)      # no workspace is needed
     small = C.CFUNCTYPE(C.c_int, *[C.c_int] * 3, C.POINTER(C.c_size_t))(lambda *a: 0)
-    none = [C.cast(p, C.c_void_p).value for p in (nothing, small)]
-    calls.bind_step((holds, holds, holds, none[0], holds, none[1], holds))
+    norms = C.CFUNCTYPE(C.c_int, C.c_void_p, C.c_void_p, *[C.c_int] * 4, C.POINTER(C.c_size_t))(lambda *a: 0)
+    none = [C.cast(p, C.c_void_p).value for p in (nothing, small, norms)]
+    calls.bind_step((holds, none[2], holds, holds, holds, none[0], holds, none[1], holds))
     args = list(ways(f, CALLS[f]()))[1]      # (without results of the caller's, which goes the native way)
     if f == "dpllm_sample":
         args["logits"] = zeros(2, 10)
@@ -203,6 +204,15 @@ def test_both_ways_pass_on_the_same(made):
         for positions in (a["positions"], zeros(3, dtype=torch.int32)):
             same("dpllm_norm_rope", dict(x=xs, weights=weights, positions=positions, freqs=a["freqs"], out=outs, eps=1e-5, scale=0.5, layout=1), {"x": list(xs)})
     same("dpllm_norm_rope", dict(x=xs[0], weights=a["weights"], out=outs[0]), {"out": [outs[0]]})
+    a = back_args()
+    del a["workspace"], a["out"]
+    xs, outs = (a["x"], zeros(2, 3, 2, 64)), (zeros(2, 3, 4, 64), zeros(2, 3, 2, 64))
+    for weights, wanted in (((a["weights"], zeros(64, dtype=torch.float32)), None), ((a["weights"], None), [False, True]), (None, None)):
+        args = dict(a, x=xs, grads=(a["grads"], zeros(2, 3, 2, 64)), weights=weights, wanted=wanted, out=outs, layout=1, scale=2.0)
+        got = [dp.dpllm_norm_rope_backward(**dict(args, **change)) for change in ({}, {"workspace": zeros(64, dtype=torch.uint8)})]
+        for o, w in got:
+            assert o[0] is outs[0] and o[1] is outs[1]
+            assert [None if t is None else t.shape for t in w] == [None if t is None or (wanted and not wanted[i]) else t.shape for i, t in enumerate(weights or (None, None))]
     a = append_args()
     calls_made = len(made)
     same("dpllm_quantized_append", dict(a, layer=0), {"count": on(torch.zeros(2, 2, dtype=torch.int32)[:, 0].contiguous())})
@@ -218,12 +228,13 @@ def test_both_ways_pass_on_the_same(made):
         del args["workspace"]
         same("dpllm_sample", args, {"workspace": a["workspace"]})
     native, long = made[::2], made[1::2]
-    kept = {"dpllm_quantized_attention": -3, "dpllm_sample": -3}      # (the workspace is another)
+    kept = {"dpllm_quantized_attention": (-3,), "dpllm_sample": (-3,), "dpllm_norm_rope_backward": (-3, -2, 5)}      # (the workspace, its bytes and new gradients are others)
     assert len(native) == len(long) > 10
     for (f, x), (g, y) in zip(native, long):
         assert f == g
         if f in kept:
-            del x[kept[f]], y[kept[f]]
+            for i in kept[f]:
+                del x[i], y[i]
         if f == "dpllm_quantized_append":
             del x[-2], y[-2]      # count, which is a copy
         assert x == y, f
