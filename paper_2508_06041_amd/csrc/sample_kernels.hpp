@@ -3,9 +3,10 @@
 // says in which step of it a cut lies.  If the words up to there are at most one to a thread of a workgroup, those are sorted and the rest is not looked at again; else only the words of
 // that step are.
 //
-// One row of 32000 words with all three cuts takes 3.4 + 7 + 11 us (tops, histograms, choice), 64 rows of 128256 in bf16 with every kind of cut 6 + 11 + 71.  The choice is one workgroup's work and
-// bound by what that can do: a walk over a row of 128256 words takes it 7 us, a sort of 2048 words 18, one of 1024 ten, up to 512 each word's place is counted instead (64 words: 4 us less).
-// Choosing without the shorter way took 32 us for the one row.  Steps of a 32nd do not help: the many words of a flat row are far below its top.
+// One row of 32000 words with all three cuts takes 3.2 + 6.9 + 10.6 us (tops, histograms, choice), 64 rows of 128256 in bf16 with every kind of cut 5.8 + 11.7 + 50.  The choice is one workgroup's
+// work and bound by what that can do: a walk over a row of 128256 words takes it 7 us and more with much to do on the way, so the shorter way (32 us for the one row without it) and what is kept in
+// LDS count (the 64 rows: 71 where the words of a step were sorted 2048 at a time and looked for in the row again).  Up to 512 words are sorted by counting each one's place (64: 4 us less than in
+// steps).  Steps of a 32nd do not help: the many words of a flat row are far below its top.
 //
 // Answers are whole numbers, so sums are kept in 64 bits and in whole numbers where workgroups' order could show: a word of step b counts 1 and the
 // 2^-40ths by which e 2^((b + 1) / 8) exceeds 1, both in one 64-bit addition in LDS.  Rounding that to 2^-41 moves a sum by less than 1e-12 of itself.
@@ -17,7 +18,9 @@ namespace dpllm {
 constexpr int kSampleBins = 512;            // e down to 2^-64
 constexpr int kSampleThreads = 1024;        // of the workgroup that chooses
 constexpr int kSampleWaves = kSampleThreads / 64;
-constexpr int kSampleList = 2048;           // words that are sorted at once
+constexpr int kSampleList = 2048;           // words that LDS holds
+constexpr int kSampleSort = 512;            // and that are sorted, but for those of the shorter way
+constexpr int kSampleChunks = 1088;         // at most, of a row of 2^22 words
 constexpr int kPast = 1 << 12;              // more than a list is long
 constexpr int kCountShift = 50;             // a chunk has at most 2^13 words of less than 2^37 each
 
@@ -220,7 +223,8 @@ struct Narrow {
 };
 
 struct SampleSpace {
-  unsigned long long list[kSampleList];
+  unsigned long long list[kSampleList];     // ~key << 32 | number
+  unsigned long long chunks[kSampleChunks];
   double base[kSampleBins];                 // the least e of a bin, in 2^-40ths
   double table[kSampleTable];
   double sums[kSampleBins];                 // running, over bins
@@ -231,7 +235,7 @@ struct SampleSpace {
   uint32_t wave_counts[kSampleWaves];
   double sum, sum_before;
   int found, before, length;
-  uint32_t low, high;
+  int listed, listed_bin;                   // the list has all words of a bin: how many (else 0), and which
 };
 
 // The sum of what the first `waves` wavefronts left in s.wave_sums.
@@ -362,6 +366,7 @@ struct Sampler {
     return first == 0 || x != x ? INFINITY : x + __builtin_fabsf(x) * 0x1p-20f + 0x1p-120f;
   }
 
+  __device__ __forceinline__ float listed_logit(int i) const { return from_key(~(uint32_t)(s.list[i] >> 32)); }
   // The words of bin `bin` in front of a cut: `count` of them, or (count 0) those in front of which less than `sum` of them lies, at least one.  s.length and s.sum: how many, and their sum.
   __device__ Cut cut_in(int bin, int words, uint32_t count, double sum) {
     typedef Narrow<T> Key;
@@ -373,21 +378,43 @@ struct Sampler {
       const uint32_t k = Key::of(x);
       return k >= low && k <= high && steps.bin(y) == bin;
     };
-    // narrower, until the words can be sorted or are all the same: nine of the key's 32 bits at a time
-    for (int round = 0; round < 4 && words > kSampleList && low != high; ++round) {
+    int listed = 0;
+    // narrower, until the words can be sorted or are all the same: nine of the key's 32 bits at a time, over the row until LDS holds the words, then over those
+    for (int round = 0;; ++round) {
+      if (listed == 0 && words <= kSampleList) {
+        listed = words;
+        if (threadIdx.x == 0) {
+          s.length = 0;
+          s.listed = round == 0 ? words : 0;
+          s.listed_bin = bin;
+        }
+        __syncthreads();
+        words_between<T>(row, a.vocabulary, Key::back(low), Key::back(high), [&](float x, int i) {
+          if (inside(x, steps.place(x))) {
+            const int at = atomicAdd(&s.length, 1);
+            if (at < kSampleList) s.list[at] = (unsigned long long)~key_of(x) << 32 | (uint32_t)i;
+          }
+        });
+        __syncthreads();
+      }
+      if (words <= kSampleSort || low == high || round == 4) break;
       if (threadIdx.x < kSampleBins) {
         s.fine[threadIdx.x] = 0;
         s.fine_counts[threadIdx.x] = 0;
       }
       __syncthreads();
       const int shift = max(0, 23 - __builtin_clz(high - low));      // (high - low) >> shift is below 512
-      words_between<T>(row, a.vocabulary, Key::back(low), Key::back(high), [&](float x, int) {
+      const auto add = [&](float x) {
         const double y = steps.place(x);
         if (inside(x, y)) {
           atomicAdd(&s.fine_counts[(high - Key::of(x)) >> shift], 1u);
           atomicAdd(&s.fine[(high - Key::of(x)) >> shift], steps.excess(y));
         }
-      });
+      };
+      if (listed > 0)
+        for (int i = threadIdx.x; i < listed; i += kSampleThreads) add(listed_logit(i));
+      else
+        words_between<T>(row, a.vocabulary, Key::back(low), Key::back(high), [&](float x, int) { add(x); });
       __syncthreads();
       const int i = min((int)threadIdx.x, kSampleBins - 1);
       run_bins(s, base * ((double)s.fine_counts[i] * 0x1p40 + (double)s.fine[i]), s.fine_counts[i]);
@@ -400,47 +427,33 @@ struct Sampler {
       high = upper;
       __syncthreads();
     }
-    if (words <= kSampleList) {
-      if (threadIdx.x == 0) s.length = 0;
+    if (words <= kSampleSort) {
+      unsigned long long* few = s.fine;
       int size = 2;
       while (size < words) size *= 2;
-      for (int i = threadIdx.x; i < size; i += kSampleThreads) s.list[i] = ~0ull;
+      if (threadIdx.x == 0) s.length = 0;
+      if ((int)threadIdx.x < size) few[threadIdx.x] = ~0ull;
       __syncthreads();
-      words_between<T>(row, a.vocabulary, Key::back(low), Key::back(high), [&](float x, int i) {
-        if (inside(x, steps.place(x))) {
-          const int at = atomicAdd(&s.length, 1);
-          if (at < kSampleList) s.list[at] = (unsigned long long)~key_of(x) << 32 | (uint32_t)i;
-        }
-      });
-      __syncthreads();
-      sort(s.list, size, s.fine_counts, s.fine);
-      // two words to a thread
-      const int i = 2 * threadIdx.x;
-      double e[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) e[j] = i + j < words ? e_of(from_key(~(uint32_t)(s.list[i + j] >> 32))) : 0.0;
-      const double upto = group_scan(s, e[0] + e[1]);
-      if (threadIdx.x == 0) s.found = -1;
-      __syncthreads();
-      int last = -1;      // the last of this thread's that stays
-      double last_sum = 0.0;
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const double front = upto - (j == 0 ? e[0] + e[1] : e[1]);
-        if (i + j < words && (count > 0 ? (uint32_t)(taken + i + j) < count : i + j + taken == 0 || taken_sum + front < sum)) {
-          last = i + j;
-          last_sum = front + e[j];
-        }
+      for (int i = threadIdx.x; i < listed; i += kSampleThreads) {
+        const float x = listed_logit(i);
+        if (inside(x, steps.place(x))) few[atomicAdd(&s.length, 1) & (kSampleSort - 1)] = s.list[i];
       }
-      atomicMax(&s.found, last);
       __syncthreads();
-      if (last >= 0 && last == s.found) s.sum = taken_sum + last_sum;
+      sort(few, size, s.fine_counts, reinterpret_cast<unsigned long long*>(s.sums));
+      const int i = threadIdx.x;
+      const double e = i < words ? e_of(from_key(~(uint32_t)(few[i] >> 32))) : 0.0, upto = group_scan(s, e), front = upto - e;
+      if (i == 0) s.found = -1;
+      __syncthreads();
+      const bool stays = i < words && (count > 0 ? (uint32_t)(taken + i) < count : i + taken == 0 || taken_sum + front < sum);
+      if (stays) atomicMax(&s.found, i);
+      __syncthreads();
+      if (stays && i == s.found) s.sum = taken_sum + upto;
       const int found = max(s.found, 0);
-      if (threadIdx.x == 0) {
+      if (i == 0) {
         s.length = taken + s.found + 1;
         if (s.found < 0) s.sum = taken_sum;
       }
-      const unsigned long long w = s.list[found];
+      const unsigned long long w = few[found];
       __syncthreads();
       // (rounding between two ways to the same sum may leave none of these: then the cut is in front of the first)
       if (s.length == taken) return {from_key(~(uint32_t)(w >> 32)), -1};
@@ -459,7 +472,7 @@ struct Sampler {
     if (n < words) {
       // the n-th by number: first in which chunk, then there
       typedef Chunk<T> C;
-      uint32_t* in_chunk = reinterpret_cast<uint32_t*>(s.list);      // [up to kSampleList chunks]
+      uint32_t* in_chunk = reinterpret_cast<uint32_t*>(s.chunks);
       for (int c = threadIdx.x >> 6; c < a.chunks; c += kSampleWaves) {
         int mine = 0;
         each_piece<T>(row, a.vocabulary, c * C::kElements - C::lead(row), C::kElements / C::E, threadIdx.x & 63, 64, [&](const typename Piece<T>::type& v, int) {
@@ -538,24 +551,26 @@ struct Sampler {
     weights[i] = e;
     __syncthreads();
     const double want = (double)a.uniforms[a_row] * s.sum_before;
-    // in the order of the words' numbers: of a few each adds up all in front of it, more are sorted again
-    int number = word;
-    double run = 0.0;
-    if (kept <= 128) {
-      if (i < kept) {
-#pragma unroll 8
-        for (int j = 0; j < kept; ++j) run += (int)(uint32_t)s.list[j] <= word ? weights[j] : 0.0;
-        atomicMax(&s.length, word + kPast);
+    // in the order of the words' numbers: of a few, eight lanes add up all in front of each; more are sorted again
+    if (kept <= kSampleThreads / 8) {
+      const int t = i / 8, number = (int)(uint32_t)s.list[t];
+      double run = 0.0;
+#pragma unroll 4
+      for (int j = i & 7; j < kept; j += 8) run += (int)(uint32_t)s.list[j] <= number ? weights[j] : 0.0;
+      run = team_all(run, 8, [](double x, double y) { return x + y; });
+      if (t < kept && (i & 7) == 0) {
+        atomicMax(&s.length, number + kPast);
+        if (run > want) atomicMin(&s.before, number);
       }
     } else {
       s.list[i] = i < kept ? (unsigned long long)(uint32_t)word << 32 | (uint32_t)i : ~0ull;
       __syncthreads();
       sort(s.list, size, s.fine_counts, s.fine);
-      number = (int)(uint32_t)(s.list[i] >> 32);
-      run = group_scan(s, i < kept ? weights[(uint32_t)s.list[i]] : 0.0);
+      const int number = (int)(uint32_t)(s.list[i] >> 32);
+      const double run = group_scan(s, i < kept ? weights[(uint32_t)s.list[i]] : 0.0);
       if (i == kept - 1) atomicMax(&s.length, number + kPast);
+      if (i < kept && run > want) atomicMin(&s.before, number);
     }
-    if (i < kept && run > want) atomicMin(&s.before, number);
     __syncthreads();
     if (i == 0) {
       a.words[a_row] = min(s.before, s.length - kPast);      // (rounding may leave the sum short of its whole: then it is the last that stays)
@@ -645,6 +660,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_choose_kernel(const Sam
     return;
   }
 
+  if (threadIdx.x == 0) s.listed = 0;
   Cut cut{-INFINITY, 0x7fffffff};
   int last = kSampleBins - 1;      // the bin of the last word that stays, or a later one
   double part = whole;             // of the words in front of the first cut
@@ -685,11 +701,21 @@ __global__ void __launch_bounds__(kSampleThreads) sample_choose_kernel(const Sam
     const double e = x == top ? 1.0 : sampler.e_at(y);
     return least == 0.0 || first_only || e >= least ? e : 0.0;
   };
-  double* chunk_sums = reinterpret_cast<double*>(s.list);      // [up to kSampleList chunks]
   int kept = 0;
+  // Words of the cut's step that LDS still has are added up from there, in 2^-51ths, so that their order does not matter.
+  for (int c = threadIdx.x; c < a.chunks; c += kSampleThreads) s.chunks[c] = 0;
+  __syncthreads();
+  const bool held = s.listed > 0 && s.listed_bin == last && near == last && far == last;
+  if (held)
+    for (int j = threadIdx.x; j < s.listed; j += kSampleThreads) {
+      const int i = (int)(uint32_t)s.list[j];
+      const double e = e_if_kept(sampler.listed_logit(j), i, near);
+      if (e > 0.0) atomicAdd(&s.chunks[(i + Chunk<T>::lead(from)) / Chunk<T>::kElements], (unsigned long long)__builtin_rint(e * 0x1p51));
+      kept += e > 0.0;
+    }
   __syncthreads();
   for (int c = wave; c < a.chunks; c += kSampleWaves) {
-    double sum = 0.0;
+    double sum = lane == 0 ? (double)s.chunks[c] * 0x1p-51 : 0.0;
     bool any = false;
     unsigned long long w[kSampleBins / 64];
 #pragma unroll
@@ -701,7 +727,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_choose_kernel(const Sam
       kept += (int)(w[j] >> kCountShift);
       sum += s.base[64 * j + lane] * ((double)(w[j] >> kCountShift) * 0x1p40 + (double)(w[j] & kMask));
     }
-    if (__any(any))
+    if (!held && __any(any))
       each_piece<T>(from, a.vocabulary, c * Chunk<T>::kElements - Chunk<T>::lead(from), Chunk<T>::kElements / Chunk<T>::E, lane, 64, [&](const typename Piece<T>::type& v, int i) {
         each_between<T>(v, i, low, high, [&](float x, int at) {
           const double e = e_if_kept(x, at, near);
@@ -710,7 +736,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_choose_kernel(const Sam
         });
       });
     sum = wave_sum(sum);
-    if (lane == 0) chunk_sums[c] = sum;
+    if (lane == 0) s.chunks[c] = __builtin_bit_cast(unsigned long long, sum);
   }
   __syncthreads();
   if (threadIdx.x == 0) s.before = 0;
@@ -720,7 +746,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_choose_kernel(const Sam
   // the chunk of the word: two chunks to a thread
   double pair[2];
 #pragma unroll
-  for (int j = 0; j < 2; ++j) pair[j] = 2 * (int)threadIdx.x + j < a.chunks ? chunk_sums[2 * threadIdx.x + j] : 0.0;
+  for (int j = 0; j < 2; ++j) pair[j] = 2 * (int)threadIdx.x + j < a.chunks ? __builtin_bit_cast(double, (uint64_t)s.chunks[2 * threadIdx.x + j]) : 0.0;
   double upto = group_scan(s, pair[0] + pair[1]);
   const double all = of_waves(s, kSampleWaves), want = (double)a.uniforms[row] * all;
   if (threadIdx.x == 0) {
