@@ -355,17 +355,17 @@ struct Sampler {
 
   __device__ __forceinline__ double e_at(double y) const { return steps.share(y, s.base[min(steps.bin(y), kSampleBins - 1)], 0.0); }
   __device__ __forceinline__ double e_of(float x) const { return x == top ? 1.0 : e_at(steps.place(x)); }
-  // Bounds of the logits of bins first ... last, a little wide.
+  // Bounds of the logits of bins first ... last, a little wide: by the rounding to a float, and by much more than places are rounded by.
+  __device__ __forceinline__ float wide(float x) const { return __builtin_fabsf(x) * 0x1p-20f + (float)(0x1p-25 / by) + 0x1p-120f; }
   __device__ __forceinline__ float lowest(int last) const {
-    const float x = (float)((double)top - (last + 1) / by);
     if (top == INFINITY) return top;
-    return x != x || last >= kSampleBins - 1 ? -INFINITY : x - __builtin_fabsf(x) * 0x1p-20f - 0x1p-120f;
+    const float x = (float)((double)top - (last + 1) / by), low = x - wide(x);
+    return low != low || last >= kSampleBins - 1 ? -INFINITY : low;
   }
   __device__ __forceinline__ float highest(int first) const {
-    const float x = (float)((double)top - first / by);
-    return first == 0 || x != x ? INFINITY : x + __builtin_fabsf(x) * 0x1p-20f + 0x1p-120f;
+    const float x = (float)((double)top - first / by), high = x + wide(x);
+    return first == 0 || high != high ? INFINITY : high;
   }
-
   __device__ __forceinline__ float listed_logit(int i) const { return from_key(~(uint32_t)(s.list[i] >> 32)); }
   // The words of bin `bin` in front of a cut: `count` of them, or (count 0) those in front of which less than `sum` of them lies, at least one.  s.length and s.sum: how many, and their sum.
   __device__ Cut cut_in(int bin, int words, uint32_t count, double sum) {
