@@ -743,7 +743,8 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) quantized_attent
   const int b = share.b, old_steps = steps_of(share.len), first = share.first, last_old = min(share.last, old_steps);
   if (share.part == 0 && h == 0 && row_tile == 0 && threadIdx.x == 0 && a.places != nullptr) a.places[b] = make_int2(slot, share.parts);
 
-  // Places and scales are looked up for as many steps at a time as there are wavefronts, one by each, that many steps before they are needed.
+  // Places and scales are looked up for as many steps at a time as there are wavefronts, one by each, that many steps before they are needed.  Loads are up to three steps ahead.
+  static_assert(WAVES >= 4, "places of the steps that loads are ahead by");
   const uint32_t* scales = (lane < kAttTile ? a.k_scales : a.v_scales) + h * a.scale_head;
   struct Found {
     HeldPlace place;
