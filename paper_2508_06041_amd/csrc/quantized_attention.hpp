@@ -4,7 +4,7 @@
 // result is w u d + w g.  So the codes go into the matrix pipe as they are, whole or half numbers that 16 bits hold exactly, and scales and offsets
 // meet scores and weights in 32 bits: no value is rounded that was not rounded when it was quantised.  The weights w u are rounded to float16 whatever the results are (three bits more than
 // bfloat16 has, as the codes are exact in either), and what that leaves is a second product where the results are float16 too, which would be half as far off again without it (at 3 % of a call's
-// time for few rows, 11 % for 52 over the longest contexts, 97 -> 108 us); u relative to a power of two that is above all the wavefront has met, so that w u is in the range that w is kept in (tree_attention.hpp).
+// time for few rows, 4 to 9 % for 52 over the longest contexts, 96 -> 105 us in INT4); u relative to a power of two that is above all the wavefront has met, so that w u is in the range that w is kept in (tree_attention.hpp).
 #pragma once
 #include <type_traits>
 
@@ -284,15 +284,16 @@ __device__ __forceinline__ void add_values(const QuantizedArgs& a, QuantizedRows
 #pragma unroll
       for (int i = 0; i < 8; ++i) rows.offset[mt] = __builtin_fmaf(w[mt].w[i], v_offset[i], rows.offset[mt]);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) p[mt][i] = pack2<half_t>(w[mt].w[2 * i] * v_scale[2 * i], w[mt].w[2 * i + 1] * v_scale[2 * i + 1]);
-    if (FINE)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 4; ++i) {
+      uint32_t both = pack2<half_t>(w[mt].w[2 * i] * v_scale[2 * i], w[mt].w[2 * i + 1] * v_scale[2 * i + 1]);      // (__builtin_bit_cast of a vector's element takes its first)
+      p[mt][i] = both;
+      if (FINE) {
+        asm("" : "+v"(both));      // (else each half is made once more)
         typedef half_t halves __attribute__((ext_vector_type(2)));
-        const uint32_t both = p[mt][i];      // (__builtin_bit_cast of an element takes the vector's first)
         const halves h = __builtin_bit_cast(halves, both);
         rest[mt][i] = pack2<half_t>(__builtin_fmaf(w[mt].w[2 * i], v_scale[2 * i], -(float)h[0]), __builtin_fmaf(w[mt].w[2 * i + 1], v_scale[2 * i + 1], -(float)h[1]));
       }
+    }
   }
   u32x4 v[D / 16];
   values(v);
