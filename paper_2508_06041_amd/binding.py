@@ -459,7 +459,7 @@ def dpllm_norm_rope(x, weights, positions=None, freqs=None, eps=1e-6, out=None, 
     """x: a tensor [batch][tokens][heads][head_dim], or a tuple of such that share everything but their heads (queries, keys).  weights: a tensor [head_dim] or [heads][head_dim]
     for each (None: 1), all of one type.  positions, freqs, scale, layout: as for dpllm_rope; freqs None: the norm alone.  out: where the results go (x itself: in place); new tensors
     unless given.  New results have a gradient with respect to x and the weights."""
-    made = _calls.norm_rope(x, weights, positions, freqs, eps, out, scale, layout)
+    made = _calls.norm_rope(x, weights, positions, freqs, eps, out, scale, layout, torch.is_grad_enabled())
     if type(made) is not int:
         return made
     if made != _calls.ELSEWHERE:

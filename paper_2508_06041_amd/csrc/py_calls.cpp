@@ -488,7 +488,7 @@ PyObject* quantized_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
                                           [](auto... all) { return step.append(all...); });
 }
 
-// What both directions of the norms take: x, weights, positions, freqs, eps, out, scale, layout, and grads where those are not nullptr.
+// What both directions of the norms take: x, weights, positions, freqs, eps, out, scale, layout, and grads where those are not nullptr.  recorded: tensors that require a gradient are binding.py's business.
 struct Norms {
   int m, heads[DPLLM_MAX_TENSORS], layout = 0, weight_type = -1;
   Tensor x[DPLLM_MAX_TENSORS], pos{}, freqs{};
@@ -502,7 +502,7 @@ struct Norms {
   int64_t positions_stride() const { return turned && pos.dim == 2 ? x[0].size[1] : 0; }
   int type() const { return weight_type < 0 ? DPLLM_F32 : weight_type; }
 };
-bool look_norms(Norms& k, PyObject* xs, PyObject* ws, PyObject* positions, PyObject* freqs, PyObject* eps, PyObject* outs, PyObject* scale, PyObject* layout, PyObject* grads, PyObject* results) {
+bool look_norms(Norms& k, PyObject* xs, PyObject* ws, PyObject* positions, PyObject* freqs, PyObject* eps, PyObject* outs, PyObject* scale, PyObject* layout, PyObject* grads, PyObject* results, bool recorded) {
   k.turned = freqs != Py_None;
   if (!k.place.find() || (positions == Py_None) != (freqs == Py_None) || !as_float(eps, &k.eps) || !as_float(scale, &k.scale) || !as_int(layout, &k.layout)) return false;
   if (k.turned && (!look(positions, k.place, &k.pos) || k.pos.dtype != kInt32 || k.pos.dim < 1 || k.pos.dim > 2 || !k.pos.dense(k.pos.dim) || !look(freqs, k.place, &k.freqs) ||
@@ -516,7 +516,7 @@ bool look_norms(Norms& k, PyObject* xs, PyObject* ws, PyObject* positions, PyObj
   };
   for (int i = 0; i < k.m; ++i) {
     const Ref t(item(xs, i));
-    if (!look(t.o, k.place, &k.x[i]) || graded(t.o) || x[i].dtype > 2 || !heads_of(x[i], &k.in[i]) || x[i].dtype != x[0].dtype || x[i].size[0] != x[0].size[0] ||
+    if (!look(t.o, k.place, &k.x[i]) || (recorded && graded(t.o)) || x[i].dtype > 2 || !heads_of(x[i], &k.in[i]) || x[i].dtype != x[0].dtype || x[i].size[0] != x[0].size[0] ||
         x[i].size[1] != x[0].size[1] || x[i].size[3] != x[0].size[3])
       return false;
     k.heads[i] = (int)x[i].size[2];
@@ -524,7 +524,7 @@ bool look_norms(Norms& k, PyObject* xs, PyObject* ws, PyObject* positions, PyObj
     if (given.o != Py_None) {
       Tensor w;
       // (gradients are laid out as their weights, which have no gaps then)
-      if (!look(given.o, k.place, &w) || graded(given.o) || w.dtype > 2 || (k.weight_type >= 0 && w.dtype != k.weight_type) || w.dim < 1 || w.dim > 2 || w.size[w.dim - 1] != x[i].size[3] ||
+      if (!look(given.o, k.place, &w) || (recorded && graded(given.o)) || w.dtype > 2 || (k.weight_type >= 0 && w.dtype != k.weight_type) || w.dim < 1 || w.dim > 2 || w.size[w.dim - 1] != x[i].size[3] ||
           !w.dense(grads ? w.dim : 1) || (w.dim == 2 && (w.size[0] != k.heads[i] || (k.heads[i] > 1 && w.stride[0] == 0))))
         return false;
       k.weight_type = w.dtype;
@@ -534,13 +534,13 @@ bool look_norms(Norms& k, PyObject* xs, PyObject* ws, PyObject* positions, PyObj
     if (grads) {
       const Ref g(item(grads, i));
       Tensor y;
-      if (!look(g.o, k.place, &y) || graded(g.o) || !heads_of(y, &k.grads[i]) || !alike(y, i)) return false;
+      if (!look(g.o, k.place, &y) || !heads_of(y, &k.grads[i]) || !alike(y, i)) return false;
     }
     PyObject* o = outs == Py_None ? PyObject_CallOneArg(empty_like, t.o) : item(outs, i);
     if (o == nullptr) return false;
     PyTuple_SET_ITEM(results, i, o);
     Tensor y;
-    if (!(outs == Py_None ? look_new(o, x[i], &y) : look(o, k.place, &y) && !graded(o)) || !heads_of(y, &k.out[i]) || !alike(y, i)) return false;
+    if (!(outs == Py_None ? look_new(o, x[i], &y) : look(o, k.place, &y) && !(recorded && graded(o))) || !heads_of(y, &k.out[i]) || !alike(y, i)) return false;
   }
   return !k.turned || (k.pos.size[k.pos.dim - 1] == x[0].size[1] && (k.pos.dim == 1 || k.pos.size[0] == x[0].size[0]));
 }
@@ -554,13 +554,13 @@ int count_norms(PyObject* xs, std::initializer_list<PyObject*> others) {
   return m;
 }
 
-// norm_rope(x, weights, positions, freqs, eps, out, scale, layout)
+// norm_rope(x, weights, positions, freqs, eps, out, scale, layout, recorded)
 PyObject* norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Norms k;
-  k.m = n == 8 && step.norm_rope != nullptr ? count_norms(a[0], {a[1], a[5]}) : 0;
+  k.m = n == 9 && step.norm_rope != nullptr ? count_norms(a[0], {a[1], a[5]}) : 0;
   if (k.m == 0) return elsewhere();
   const Ref results(PyTuple_New(k.m));
-  if (results.o == nullptr || !look_norms(k, a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], nullptr, results.o)) return elsewhere();
+  if (results.o == nullptr || !look_norms(k, a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], nullptr, results.o, a[8] != Py_False)) return elsewhere();
   const int rc = unlocked([&] {
     return step.norm_rope(k.in, k.out, k.heads, k.weights, k.strides, k.type(), k.eps, k.m, (int)k.x[0].size[0], (int)k.x[0].size[1], (int)k.x[0].size[3], k.x[0].dtype, k.rotary(), k.layout,
                           static_cast<const double*>(k.freqs.data), k.scale, static_cast<const int32_t*>(k.pos.data), k.positions_stride(), k.place.stream);
@@ -574,7 +574,7 @@ PyObject* norm_rope_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   k.m = n == 10 && step.norm_backward != nullptr ? count_norms(a[0], {a[1], a[2], a[6]}) : 0;
   if (k.m == 0 || a[1] == Py_None) return elsewhere();
   const Ref results(PyTuple_New(k.m)), made(PyTuple_New(k.m));
-  if (results.o == nullptr || made.o == nullptr || !look_norms(k, a[0], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[1], results.o)) return elsewhere();
+  if (results.o == nullptr || made.o == nullptr || !look_norms(k, a[0], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[1], results.o, false)) return elsewhere();
   void *grads[DPLLM_MAX_TENSORS] = {}, *ws = nullptr;
   size_t bytes = 0;
   bool some = false;

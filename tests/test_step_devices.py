@@ -276,6 +276,22 @@ def test_a_gradient_that_results_in_out_would_not_have(made):
     assert names(made) == ["dpllm_norm_rope"]
 
 
+def test_what_records_nothing_goes_the_native_way(made, monkeypatch):
+    """Weights and inputs that require a gradient, where none is recorded; and the gradient itself, whose inputs do."""
+    def never(*a, **k):
+        raise AssertionError("the long way")
+    monkeypatch.setattr(binding, "_norm_weights", never)
+    a = norm_args()
+    graded = zeros(64, dtype=torch.float32).requires_grad_()
+    with torch.no_grad():
+        dp.dpllm_norm_rope(a["x"], graded, a["positions"], a["freqs"])
+    b = back_args()
+    del b["workspace"]
+    dp.dpllm_norm_rope_backward(**dict(b, x=b["x"].requires_grad_(), weights=b["weights"].requires_grad_()))
+    assert names(made) == ["dpllm_norm_rope", "dpllm_norm_rope_backward"]
+    assert dp.dpllm_norm_rope(a["x"], graded, a["positions"], a["freqs"]).requires_grad
+
+
 BAD = [
     ("dpllm_norm_rope", {"weights": (zeros(64), zeros(64))}, "weight"), ("dpllm_norm_rope", {"weights": zeros(63, dtype=torch.float32)}, "weight"), ("dpllm_norm_rope", {"weights": zeros(3, 64)}, "weight"),
     ("dpllm_norm_rope", {"positions": None}, "positions"), ("dpllm_norm_rope", {"positions": zeros(2, 4, dtype=torch.int32)}, "positions"), ("dpllm_norm_rope", {"x": zeros(3, 4, 64)}, "out"),
