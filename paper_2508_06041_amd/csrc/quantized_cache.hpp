@@ -203,14 +203,15 @@ __device__ __forceinline__ void codes_of(const Coder& c, const float (&x)[E], ui
     }
   } else {
     // The magnitude, n or -1 - n, is the whole part of |x - offset| / scale, which a product that is a little large gives or exceeds by 1: so the remainder's sign decides.  Values on a border, where the remainder
-    // is 0, belong to the level above, which for negative ones is the smaller magnitude; they are as many as five in a thousand of bfloat16 values, so all go this way.
+    // is 0, belong to the level above, which for negative ones is the smaller magnitude; they are as many as five in a thousand of bfloat16 values, so all go this way.  -0.0 less an offset of 0 is -0.0,
+    // which has no smaller magnitude and is not below the offset: 0 is added, which makes it 0 and leaves all other differences as they are.
     const float by = c.by * (1.f + 0x1p-20f);
 #pragma unroll
     for (int i = 0; i < (E + 7) / 8; ++i) {
       w[i] = 0;
 #pragma unroll
       for (int j = 0; j < (E < 8 ? E : 8); ++j) {
-        const float d = x[8 * i + j] - c.offset, whole = __builtin_truncf(fminf(__builtin_fabsf(d) * by, 7.5f)), rest = __builtin_fmaf(-whole, c.scale, __builtin_fabsf(d));
+        const float d = (x[8 * i + j] - c.offset) + 0.f, whole = __builtin_truncf(fminf(__builtin_fabsf(d) * by, 7.5f)), rest = __builtin_fmaf(-whole, c.scale, __builtin_fabsf(d));
         const uint32_t negative = __float_as_uint(d) >> 31;
         const uint32_t m = (uint32_t)((int)whole + ((__builtin_bit_cast(int, rest) - (int)negative) >> 31));
         w[i] |= (m | negative << 3) << (4 * j);
