@@ -2,12 +2,11 @@
 //
 // With key codes c, their scale s (and offset f) the score of a cached token is x = s (q . c) + f (sum of q), and with value codes d, scale u (and offset g) its part of the
 // result is w u d + w g.  So the codes go into the matrix pipe as they are, whole or half numbers that 16 bits hold exactly, and scales and offsets
-// meet scores and weights in 32 bits: no value is rounded that was not rounded when it was quantised.  The weights w u are rounded to float16 whatever the results are (three bits more than
-// bfloat16 has, as the codes are exact in either), and what that leaves is a second product where the results are float16 too, which would be half as far off again without it (at 3 % of a call's
-// time for few rows, 4 to 9 % for 52 over the longest contexts, 96 -> 105 us in INT4); u relative to a power of two that is above all the wavefront has met, so that w u is in the range that w is kept in (tree_attention.hpp).
+// meet scores and weights in 32 bits: no value is rounded that was not rounded when it was quantised.  Codes are exact in bfloat16, which has the range of a float, so the weights w u go there as they
+// are however far the scales of tokens lie apart, in two parts (the second is what rounding the first leaves): 16 bits of them, an error of 2^-18, which is nothing beside the rounding of either type's results.
+// (In float16 they would have to be relative to a common unit, beside which the weights of tokens of small values vanish.)  Results of bfloat16 took as long with one part in float16 for up to 16 rows, 6 % (INT4)
+// and 8 % less for 52, 10 to 24 % less in the kernel for many rows (100 rows over 9000 to 65001 tokens 126 us instead of 149 in e4m3, 142 instead of 156 in INT4), but were off by up to a step more.
 #pragma once
-#include <type_traits>
-
 #include "quantized_cache.hpp"
 #include "tree_attention.hpp"
 
@@ -96,16 +95,16 @@ __device__ __forceinline__ u32x4 key_operand(const Codes<N>& c, int kk) {
                  two_codes<FORMAT, T>(c.w[2 * kk + 1], true)};
   }
 }
-// Dimensions 0 ... DV - 1 of two tokens' values, a pair of float16 for each.
+// Dimensions 0 ... DV - 1 of two tokens' values, a pair of bfloat16 for each.
 template <int FORMAT, int DV, int N>
 __device__ __forceinline__ void value_pairs(const Codes<N>& a, const Codes<N>& b, uint32_t (&pair)[DV]) {
   if constexpr (FORMAT == kInt4) {
     auto half = [&](int first, uint32_t x, uint32_t y) {      // dimensions first, first + 2, ...
       const uint32_t low = __builtin_amdgcn_perm(y, x, 0x05010400u), high = __builtin_amdgcn_perm(y, x, 0x07030602u);
-      if (first < DV) pair[first] = two_codes<FORMAT, half_t>(low, false);
-      if (first + 2 < DV) pair[first + 2] = two_codes<FORMAT, half_t>(low, true);
-      if (first + 4 < DV) pair[first + 4] = two_codes<FORMAT, half_t>(high, false);
-      if (first + 6 < DV) pair[first + 6] = two_codes<FORMAT, half_t>(high, true);
+      if (first < DV) pair[first] = two_codes<FORMAT, bfloat_t>(low, false);
+      if (first + 2 < DV) pair[first + 2] = two_codes<FORMAT, bfloat_t>(low, true);
+      if (first + 4 < DV) pair[first + 4] = two_codes<FORMAT, bfloat_t>(high, false);
+      if (first + 6 < DV) pair[first + 6] = two_codes<FORMAT, bfloat_t>(high, true);
     };
 #pragma unroll
     for (int w = 0; w < N; ++w) {
@@ -116,10 +115,10 @@ __device__ __forceinline__ void value_pairs(const Codes<N>& a, const Codes<N>& b
 #pragma unroll
     for (int w = 0; w < N; ++w) {
       const uint32_t low = __builtin_amdgcn_perm(b.w[w], a.w[w], 0x05010400u), high = __builtin_amdgcn_perm(b.w[w], a.w[w], 0x07030602u);
-      pair[4 * w] = two_codes<FORMAT, half_t>(low, false);
-      pair[4 * w + 1] = two_codes<FORMAT, half_t>(low, true);
-      if (4 * w + 2 < DV) pair[4 * w + 2] = two_codes<FORMAT, half_t>(high, false);
-      if (4 * w + 3 < DV) pair[4 * w + 3] = two_codes<FORMAT, half_t>(high, true);
+      pair[4 * w] = two_codes<FORMAT, bfloat_t>(low, false);
+      pair[4 * w + 1] = two_codes<FORMAT, bfloat_t>(low, true);
+      if (4 * w + 2 < DV) pair[4 * w + 2] = two_codes<FORMAT, bfloat_t>(high, false);
+      if (4 * w + 3 < DV) pair[4 * w + 3] = two_codes<FORMAT, bfloat_t>(high, true);
     }
   }
 }
@@ -200,6 +199,17 @@ __device__ __forceinline__ void sum_queries(const u32x4 (&q)[MT][D / 32], float 
   }
 }
 
+// Two numbers as T, into word i of p, and what that leaves of them into that of rest.
+template <typename T>
+__device__ __forceinline__ void two_parts(float a, float b, u32x4& p, u32x4& rest, int i) {
+  typedef T two __attribute__((ext_vector_type(2)));
+  uint32_t both = pack2<T>(a, b);      // (__builtin_bit_cast of a vector's element takes its first)
+  p[i] = both;
+  asm("" : "+v"(both));      // (else each half is made once more)
+  const two h = __builtin_bit_cast(two, both);
+  rest[i] = pack2<T>(a - (float)h[0], b - (float)h[1]);
+}
+
 // The weights of a step from the products of codes, with the scales (and offsets) of the lane's eight tokens, which come multiplied by scale_log2.  Mostly scales, the scale of scores and
 // the tops meet in one operation; where a top has to follow (see weigh()), or scores are huge, the products become scores first.
 template <int FORMAT, int MT, int DV>
@@ -235,27 +245,17 @@ __device__ __forceinline__ void weigh_codes(Rows<MT, DV>& r, Scores<MT>& s, cons
   weigh<half_t, MT, DV>(r, s, scale_log2, w);
 }
 
-// What a wavefront has of its rows: the sums of tree_attention.hpp, those of the offsets of values, which are relative to the same tops, and the unit of the value product: a power of two that
-// no scale of values met so far is above (0: there was none but 0), which the results are relative to.
+// The weights come 2^12 times as large as they are (kLift of Matrix<half_t>); scales and offsets of values are multiplied by this, so that the results are not lifted.
+constexpr float kUnlift = 0x1p-12f;
+
+// What a wavefront has of its rows: the sums of tree_attention.hpp and those of the offsets of values, which are relative to the same tops.
 template <int MT, int DV>
 struct QuantizedRows : Rows<MT, DV> {
-  float offset[MT], unit, by_unit;
+  float offset[MT];
   __device__ __forceinline__ void clear_all() {
     this->clear();
-    unit = 0.f;
-    by_unit = 1.f;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) offset[mt] = 0.f;
-  }
-  __device__ __forceinline__ void raise_unit(float most) {      // the same in all lanes
-    const uint32_t exponent = min(max((__float_as_uint(most) >> 23) + 1u, 4u), 250u);
-    const float less = unit * __uint_as_float((254u - exponent) << 23);
-    unit = __uint_as_float(exponent << 23);
-    by_unit = __uint_as_float((254u - exponent) << 23);
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int j = 0; j < DV; ++j) this->o[mt][j] *= less;
   }
   // before: the tops when the offsets' sums were right
   __device__ __forceinline__ void follow(const float (&before)[MT], float scale_log2) {
@@ -265,7 +265,7 @@ struct QuantizedRows : Rows<MT, DV> {
   }
 };
 
-// A step's share of the results: products of codes s, scales (and offsets) of keys, times scale_log2, and of values, these by the unit, of the lane's tokens; values(v): theirs, in the
+// A step's share of the results: products of codes s, scales (and offsets) of keys, times scale_log2, and of values, times kUnlift, of the lane's tokens; values(v): theirs, in the
 // order of value_pairs.
 template <int FORMAT, typename T, int D, int MT, typename F>
 __device__ __forceinline__ void add_values(const QuantizedArgs& a, QuantizedRows<MT, D / 16>& rows, Scores<MT>& s, const float (&q_sum)[MT], const float (&k_scale)[8],
@@ -276,7 +276,6 @@ __device__ __forceinline__ void add_values(const QuantizedArgs& a, QuantizedRows
   for (int mt = 0; mt < MT; ++mt) before[mt] = rows.top[mt];
   weigh_codes<FORMAT, MT, D / 16>(rows, s, k_scale, k_offset, q_sum, a.scale_log2, w);
   if (FORMAT == kInt4) rows.follow(before, a.scale_log2);
-  constexpr bool FINE = std::is_same<T, half_t>::value;
   u32x4 p[MT], rest[MT];
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
@@ -284,16 +283,7 @@ __device__ __forceinline__ void add_values(const QuantizedArgs& a, QuantizedRows
 #pragma unroll
       for (int i = 0; i < 8; ++i) rows.offset[mt] = __builtin_fmaf(w[mt].w[i], v_offset[i], rows.offset[mt]);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      uint32_t both = pack2<half_t>(w[mt].w[2 * i] * v_scale[2 * i], w[mt].w[2 * i + 1] * v_scale[2 * i + 1]);      // (__builtin_bit_cast of a vector's element takes its first)
-      p[mt][i] = both;
-      if (FINE) {
-        asm("" : "+v"(both));      // (else each half is made once more)
-        typedef half_t halves __attribute__((ext_vector_type(2)));
-        const halves h = __builtin_bit_cast(halves, both);
-        rest[mt][i] = pack2<half_t>(__builtin_fmaf(w[mt].w[2 * i], v_scale[2 * i], -(float)h[0]), __builtin_fmaf(w[mt].w[2 * i + 1], v_scale[2 * i + 1], -(float)h[1]));
-      }
-    }
+    for (int i = 0; i < 4; ++i) two_parts<bfloat_t>(w[mt].w[2 * i] * v_scale[2 * i], w[mt].w[2 * i + 1] * v_scale[2 * i + 1], p[mt], rest[mt], i);
   }
   u32x4 v[D / 16];
   values(v);
@@ -301,24 +291,28 @@ __device__ __forceinline__ void add_values(const QuantizedArgs& a, QuantizedRows
   for (int j = 0; j < D / 16; ++j)
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-      rows.o[mt][j] = Matrix<half_t>::mad(v[j], p[mt], rows.o[mt][j]);
-      if (FINE) rows.o[mt][j] = Matrix<half_t>::mad(v[j], rest[mt], rows.o[mt][j]);
+      rows.o[mt][j] = Matrix<bfloat_t>::mad(v[j], p[mt], rows.o[mt][j]);
+      rows.o[mt][j] = Matrix<bfloat_t>::mad(v[j], rest[mt], rows.o[mt][j]);
     }
 }
 
-// Behind the steps of codes: the results become whole (relative to the tops alone), and the nodes' steps from `step` on, every turns-th, are added as they are.  For bfloat16, whose values may be of any
-// size, the lift of the weights is taken off first.
+// Behind the steps of codes: the nodes' steps from `step` on, every turns-th, are added as they are.  For float16 the results are lifted meanwhile as the weights are; of bfloat16, whose values may be of any
+// size, the weights' lift is taken off.
 template <int FORMAT, typename T, int D, int MT>
 __device__ __forceinline__ void attend_nodes(const QuantizedArgs& a, QuantizedRows<MT, D / 16>& rows, const Share& share, int old_steps, int h, int step, int turn, int turns,
                                              const u32x4 (&q)[MT][D / 32], const int (&node)[MT]) {
   constexpr int KK = D / 32, DV = D / 16;
-  constexpr float kDown = __is_same(T, bfloat_t) ? 0x1p-12f : 1.f;
+  constexpr bool LIFT = __is_same(T, half_t);
+  constexpr float kDown = LIFT ? 1.f : kUnlift;
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, b = share.b, last = share.last, k_token = 8 * (n >> 2) + (n & 3);
-  const float back = (rows.unit == 0.f ? 1.f : rows.unit) * kDown;
+  if (step >= last) return;
+  auto times = [&](float by) {
 #pragma unroll
-  for (int mt = 0; mt < MT; ++mt)
+    for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-    for (int j = 0; j < DV; ++j) rows.o[mt][j] *= back;
+      for (int j = 0; j < DV; ++j) rows.o[mt][j] *= by;
+  };
+  if (LIFT) times(1.f / kUnlift);
   const char *new_k = a.k_new.data + 2 * (b * a.k_new.batch_stride + h * a.k_new.head_stride),
              *new_v = a.v_new.data + 2 * (b * a.v_new.batch_stride + h * a.v_new.head_stride);
   bool odd = false;      // among the values is something that is no finite number
@@ -369,6 +363,7 @@ __device__ __forceinline__ void attend_nodes(const QuantizedArgs& a, QuantizedRo
       for (int mt = 0; mt < MT; ++mt) rows.o[mt][j] = Matrix<T>::mad(t, w[mt], rows.o[mt][j]);
     }
   }
+  if (LIFT) times(kUnlift);
   if (__any(odd)) {      // a value above a weight of zero is left out; a weight above zero changes no infinity and no NaN
 #pragma unroll 1
     for (int t = max(share.first - old_steps, 0) * kAttTile; t < min((last - old_steps) * kAttTile, a.seen_nodes); ++t) {
@@ -428,20 +423,17 @@ struct RowWriter {
 };
 
 // The sums over a row's lanes, and nothing is lifted any more.
-template <int FORMAT, typename T, int MT, int DV>
+template <int FORMAT, int MT, int DV>
 __device__ __forceinline__ void settle(QuantizedRows<MT, DV>& rows) {
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     float s = rows.sum[mt], f = rows.offset[mt];
     s += __shfl_xor(s, 16);
-    rows.sum[mt] = (s + __shfl_xor(s, 32)) * 0x1p-12f;
+    rows.sum[mt] = (s + __shfl_xor(s, 32)) * kUnlift;
     if (FORMAT == kInt4) {
       f += __shfl_xor(f, 16);
-      rows.offset[mt] = (f + __shfl_xor(f, 32)) * 0x1p-12f;
+      rows.offset[mt] = f + __shfl_xor(f, 32);
     }
-    if (__is_same(T, half_t))
-#pragma unroll
-      for (int j = 0; j < DV; ++j) rows.o[mt][j] *= 0x1p-12f;
   }
 }
 
@@ -586,11 +578,9 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) quantized_attent
   };
   auto attend = [&](Tokens& x) {
     const bool all = x.there == 0xffffffffu;
-    const float scale = scale_of<FORMAT>(x.word);
-    if (__any(lane >= kAttTile && __builtin_fabsf(scale) > rows.unit))
-      rows.raise_unit(wave_all(lane >= kAttTile ? __builtin_fabsf(scale) : 0.f, [](float p, float r) { return fmaxf(p, r); }));
-    scales_of[wave][lane >> 5][lane & 31] = scale * (lane >= kAttTile ? rows.by_unit : a.scale_log2);
-    if (FORMAT == kInt4) scales_of[wave][2 + (lane >> 5)][lane & 31] = offset_of(x.word) * (lane >= kAttTile ? 1.f : a.scale_log2);
+    const float by = lane >= kAttTile ? kUnlift : a.scale_log2;
+    scales_of[wave][lane >> 5][lane & 31] = scale_of<FORMAT>(x.word) * by;
+    if (FORMAT == kInt4) scales_of[wave][2 + (lane >> 5)][lane & 31] = offset_of(x.word) * by;
 #pragma unroll
     for (int i = 0; i < H::LOADS; ++i) {
       const int piece = 64 * i + lane, at = piece / H::PIECES * H::ROW + 16 * (piece % H::PIECES);
@@ -666,7 +656,7 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) quantized_attent
   }
 
   attend_nodes<FORMAT, T, D, MT>(a, rows, share, old_steps, h, step, turn, turns, q, node);
-  settle<FORMAT, T, MT, DV>(rows);
+  settle<FORMAT, MT, DV>(rows);
   const RowWriter<T, D> to{a, b, h, slot, row_tile, R, share.parts};
   if (turns == 1) {      // every wavefront has a head to itself
     write_rows<T, D, MT>(to, rows, row_tile * R, 0, node);
@@ -723,7 +713,7 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) quantized_attent
 //   K: pieces of 8 elements [D / 8][32 tokens] as in tree_attention_wide_kernel, the elements in the order of key_operand;
 //   V: turned, [4 groups of 8 tokens][D] of 16 bytes, element d of sixteen in place (d + d / 16) % 16 of them, so that neither four neighbours of a piece nor the lanes that read D / 16
 //      elements apart meet in a bank;
-//   scales (and offsets): of the keys times scale_log2, of the values by the unit, which is the same in all wavefronts.
+//   scales (and offsets): of the keys times scale_log2, of the values times kUnlift.
 // A unit of work is 16 bytes of a token's key, or 4 bytes of each of four tokens' values.
 template <int FORMAT, typename T, int D, int MT, int WAVES>
 __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) quantized_attention_wide_kernel(const QuantizedArgs a) {
@@ -735,7 +725,6 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) quantized_attent
   __shared__ __align__(16) float lds_scales[2][SETS][kAttTile];
   __shared__ __align__(16) int64_t places[2 * WAVES][kAttTile];      // [step][token]
   __shared__ uint32_t lds_words[2 * WAVES][2][kAttTile], lds_there[2 * WAVES];
-  __shared__ float lds_most[2 * WAVES];      // the largest scale of values of a step
   const int lane = threadIdx.x & 63, wave = scalar(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   int slot, h, row_tile;
   place_group(a, 1, slot, h, row_tile);
@@ -762,11 +751,7 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) quantized_attent
     if (lane < kAttTile) places[at][lane] = f.place.at;
     lds_words[at][lane >> 5][lane & 31] = f.word;
     const uint32_t there = (uint32_t)__ballot(f.place.there);
-    const float most = wave_all(lane >= kAttTile ? __builtin_fabsf(scale_of<FORMAT>(f.word)) : 0.f, [](float x, float y) { return fmaxf(x, y); });
-    if (lane == 0) {
-      lds_there[at] = there;
-      lds_most[at] = most;
-    }
+    if (lane == 0) lds_there[at] = there;
   };
   keep_places(first + wave, find(first + wave, ask_held(a, share, last_old, first + wave)));
   u32x4 q[MT][KK];
@@ -795,12 +780,11 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) quantized_attent
   auto keep = [&](int step, const u32x4 (&x)[U]) {
     const int at = (step - first) & (2 * WAVES - 1);
     const uint32_t there = (uint32_t)scalar((int)lds_there[at]);
-    const float most = lds_most[at];
-    if (__any(most > rows.unit)) rows.raise_unit(most);
     if (threadIdx.x < 64) {
       const uint32_t word = lds_words[at][lane >> 5][lane & 31];
-      lds_scales[step & 1][lane >> 5][lane & 31] = scale_of<FORMAT>(word) * (lane >= kAttTile ? rows.by_unit : a.scale_log2);
-      if (FORMAT == kInt4) lds_scales[step & 1][2 + (lane >> 5)][lane & 31] = offset_of(word) * (lane >= kAttTile ? 1.f : a.scale_log2);
+      const float by = lane >= kAttTile ? kUnlift : a.scale_log2;
+      lds_scales[step & 1][lane >> 5][lane & 31] = scale_of<FORMAT>(word) * by;
+      if (FORMAT == kInt4) lds_scales[step & 1][2 + (lane >> 5)][lane & 31] = offset_of(word) * by;
     }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
@@ -903,7 +887,7 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) quantized_attent
   }
   if (!works) return;
   attend_nodes<FORMAT, T, D, MT>(a, rows, share, old_steps, h, max(first, old_steps), 0, 1, q, node);
-  settle<FORMAT, T, MT, DV>(rows);
+  settle<FORMAT, MT, DV>(rows);
   write_rows<T, D, MT>(RowWriter<T, D>{a, b, h, slot, row_tile, R, share.parts}, rows, row_tile * R + wave * 16 * MT, wave * 16 * MT, node);
 }
 
