@@ -399,8 +399,8 @@ int dpllm_quantized_read(const dpllm_quantized_cache* cache, int first_layer, in
                          int dtype, const dpllm_heads* k_out, int64_t k_layer_stride, const dpllm_heads* v_out, int64_t v_layer_stride, void* stream);
 
 /* dpllm_tree_attention over such a cache: the same arguments and rules, with `dtype` (DPLLM_F16 or DPLLM_BF16) the type of q, k_new, v_new and out, which are not quantised.  The
- * cached tokens count as what their codes and scales stand for, unrounded; the products of their weights and the scales of their values are rounded to 16 bits for the value product, whatever their size.  Codes and their
- * strides are aligned to 16 bytes.  A head that holds NaN makes NaN of the rows that see it.
+ * cached tokens count as what their codes and scales stand for, unrounded; the products of their weights and the scales of their values are rounded to 16 bits for the value product, whatever their size, and
+ * the weights of the new tokens likewise (to 22 bits where the type is float16).  Codes and their strides are aligned to 16 bytes.  A head that holds NaN makes NaN of the rows that see it.
  * Errors: EINVAL, ESHAPE, ERANGE (layer), ESTATE (workspace), EHIP. */
 int dpllm_quantized_attention_workspace_bytes(int batch, int nodes, int heads, int kv_heads, int head_dim, int max_len, size_t* bytes);
 int dpllm_quantized_attention(const dpllm_quantized_cache* cache, int layer, int batch, int nodes, int heads, int dtype, const int32_t* lens_dev, int max_len,

@@ -3,9 +3,10 @@
 // With key codes c, their scale s (and offset f) the score of a cached token is x = s (q . c) + f (sum of q), and with value codes d, scale u (and offset g) its part of the
 // result is w u d + w g.  So the codes go into the matrix pipe as they are, whole or half numbers that 16 bits hold exactly, and scales and offsets
 // meet scores and weights in 32 bits: no value is rounded that was not rounded when it was quantised.  Codes are exact in bfloat16, which has the range of a float, so the weights w u go there as they
-// are however far the scales of tokens lie apart, in two parts (the second is what rounding the first leaves): 16 bits of them, an error of 2^-18, which is nothing beside the rounding of either type's results.
-// (In float16 they would have to be relative to a common unit, beside which the weights of tokens of small values vanish.)  Results of bfloat16 took as long with one part in float16 for up to 16 rows, 6 % (INT4)
-// and 8 % less for 52, 10 to 24 % less in the kernel for many rows (100 rows over 9000 to 65001 tokens 126 us instead of 149 in e4m3, 142 instead of 156 in INT4), but were off by up to a step more.
+// are however far the scales of tokens lie apart, in two parts (the second is what rounding the first leaves): 16 bits of them, an error of 2^-16, which is little beside the rounding of either type's results.
+// (In float16 they would have to be relative to a common unit, beside which the weights of tokens of small values vanish.)  Results of bfloat16 took less with one part in float16: for up to 16 rows nothing in
+// 8 bits and 5 % in INT4, for 52 rows 5 to 7 %, in the kernel for many rows 10 to 20 % (100 rows over 9000 to 65001 tokens 126 us instead of 143 in e4m3, 142 instead of 157 in INT4); but they were off by up to a
+// step more.
 #pragma once
 #include "quantized_cache.hpp"
 #include "tree_attention.hpp"
@@ -296,7 +297,7 @@ __device__ __forceinline__ void add_values(const QuantizedArgs& a, QuantizedRows
     }
 }
 
-// Behind the steps of codes: the nodes' steps from `step` on, every turns-th, are added as they are.  For float16 the results are lifted meanwhile as the weights are; of bfloat16, whose values may be of any
+// Behind the steps of codes: the nodes' steps from `step` on, every turns-th, are added as they are, their weights in two parts too.  For float16 the results are lifted meanwhile as the weights are; of bfloat16, whose values may be of any
 // size, the weights' lift is taken off.
 template <int FORMAT, typename T, int D, int MT>
 __device__ __forceinline__ void attend_nodes(const QuantizedArgs& a, QuantizedRows<MT, D / 16>& rows, const Share& share, int old_steps, int h, int step, int turn, int turns,
@@ -318,7 +319,7 @@ __device__ __forceinline__ void attend_nodes(const QuantizedArgs& a, QuantizedRo
   bool odd = false;      // among the values is something that is no finite number
   for (; step < last; step += turns) {
     const int t0 = (step - old_steps) * kAttTile, here = a.seen_nodes - t0;
-    u32x4 k[2][KK], w[MT];
+    u32x4 k[2][KK], w[MT], rest[MT];
     Scores<MT> s;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
@@ -353,14 +354,17 @@ __device__ __forceinline__ void attend_nodes(const QuantizedArgs& a, QuantizedRo
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[mt][i] = pack2<T>(weights[mt].w[2 * i] * kDown, weights[mt].w[2 * i + 1] * kDown);
+      for (int i = 0; i < 4; ++i) two_parts<T>(weights[mt].w[2 * i] * kDown, weights[mt].w[2 * i + 1] * kDown, w[mt], rest[mt], i);
 #pragma unroll
     for (int j = 0; j < DV; ++j) {
       u32x4 t;
 #pragma unroll
       for (int i = 0; i < 4; ++i) t[i] = __builtin_amdgcn_perm(v[2 * i + 1][j / 2], v[2 * i][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt) rows.o[mt][j] = Matrix<T>::mad(t, w[mt], rows.o[mt][j]);
+      for (int mt = 0; mt < MT; ++mt) {
+        rows.o[mt][j] = Matrix<T>::mad(t, w[mt], rows.o[mt][j]);
+        rows.o[mt][j] = Matrix<T>::mad(t, rest[mt], rows.o[mt][j]);
+      }
     }
   }
   if (LIFT) times(kUnlift);
