@@ -312,7 +312,7 @@ class Cache:
         self.capacity = self.pages_per_seq * self.page
         self.c = _Cache(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), k.stride(3), _ptr(table), 0 if table is None else table.stride(0),
                         _DTYPES[k.dtype], self.layers, self.pages, self.page, self.pages_per_seq, self.heads, self.head_dim)
-        self.address = C.addressof(self.c)
+        self.address, self.size = C.addressof(self.c), C.sizeof(self.c)      # (its size tells the native part which kind it is)
 
 
 def dpllm_tree_attention_workspace_bytes(batch, nodes, heads, kv_heads, head_dim, max_len):
@@ -331,6 +331,7 @@ def dpllm_tree_attention(cache, layer, lens, q, k_new=None, v_new=None, mask=Non
         return made
     if made != _calls.ELSEWHERE:
         _call(made)
+    _need(isinstance(cache, Cache), "cache has to be a Cache")
     _on(cache.k, "the cache")
     _need(q.dim() == 4 and q.dtype == cache.k.dtype and q.shape[3] == cache.head_dim, "q has to be [batch][nodes][heads][head_dim] of the cache's type and head_dim")
     b, n, h, d = q.shape
@@ -403,6 +404,7 @@ def dpllm_cache_append(cache, lens, k_new, v_new, path=None, count=None, layer=0
     made = _calls.append(cache, lens, k_new, v_new, path, count, layer)
     if made != _calls.ELSEWHERE:
         return _call(made)
+    _need(isinstance(cache, Cache), "cache has to be a Cache")
     _on(cache.k, "the cache")
     if k_new.dim() == 4:
         k_new, v_new = k_new.unsqueeze(0), v_new.unsqueeze(0)
@@ -581,7 +583,7 @@ class QuantizedCache:
         self.capacity = self.pages_per_seq * self.page
         self.c = _QuantizedCache(_ptr(k), _ptr(v), _ptr(k_scales), _ptr(v_scales), *k.stride()[:4], *[s // by for s in strides], _ptr(table),
                                  0 if table is None else table.stride(0), format, self.layers, self.pages, self.page, self.pages_per_seq, self.heads, self.head_dim)
-        self.address = C.addressof(self.c)
+        self.address, self.size = C.addressof(self.c), C.sizeof(self.c)      # (its size tells the native part which kind it is)
 
     @classmethod
     def zeros(cls, format, layers, pages, page, heads, head_dim, table=None):
@@ -598,6 +600,7 @@ def dpllm_quantized_append(cache, lens, k_new, v_new, path=None, count=None, lay
     made = _calls.quantized_append(cache, lens, k_new, v_new, path, count, layer)
     if made != _calls.ELSEWHERE:
         return _call(made)
+    _need(isinstance(cache, QuantizedCache), "cache has to be a QuantizedCache")
     _on(cache.k, "the cache")
     if k_new.dim() == 4:
         k_new, v_new = k_new.unsqueeze(0), v_new.unsqueeze(0)
@@ -616,11 +619,12 @@ def dpllm_quantized_read(cache, first, tokens, dtype=torch.bfloat16, count=None,
     """What a QuantizedCache holds of `tokens` tokens from first[b] on (int32 [batch]; None: 0), as (keys, values) [batch][tokens][heads][head_dim], of `layers` layers from `layer` on
     with a dimension more if that is given.  count: int32 [batch]; from there on, and where the cache holds nothing, are zeros.  out: a pair of tensors to be filled."""
     if out is None:
-        made = _calls.quantized_read(cache, cache.k, first, tokens, dtype, count, layer, layers)
+        made = _calls.quantized_read(cache, getattr(cache, "k", None), first, tokens, dtype, count, layer, layers)
         if type(made) is not int:
             return made
         if made != _calls.ELSEWHERE:
             _call(made)
+    _need(isinstance(cache, QuantizedCache), "cache has to be a QuantizedCache")
     _on(cache.k, "the cache")
     b = cache.batch if first is None and count is None else (count if first is None else first).shape[0]
     shape = (1 if layers is None else layers, b, tokens, cache.heads, cache.head_dim)
@@ -650,6 +654,7 @@ def dpllm_quantized_attention(cache, layer, lens, q, k_new=None, v_new=None, mas
         return made
     if made != _calls.ELSEWHERE:
         _call(made)
+    _need(isinstance(cache, QuantizedCache), "cache has to be a QuantizedCache")
     _on(cache.k, "the cache")
     dtype = _dtype(q, "q")
     _need(q.dim() == 4 and q.shape[3] == cache.head_dim, "q has to be [batch][nodes][heads][head_dim] of the cache's head_dim")

@@ -339,14 +339,15 @@ PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return answer(rc, PyTuple_Check(a[0]) ? Py_NewRef(results.o) : item(results.o, 0));
 }
 
-// The dpllm_cache of a Cache object (or what a QuantizedCache has) on the current device, and its sequences.
+// The dpllm_cache of a Cache object (or what a QuantizedCache has, which is of another size) on the current device, and its sequences.
 template <typename C>
 bool cache_of(PyObject* o, const Place& place, const C** c, int* batch) {
-  const Ref at(PyObject_GetAttr(o, s_address)), b(PyObject_GetAttr(o, s_batch)), device(PyObject_GetAttr(o, s_device));
+  static_assert(sizeof(dpllm_cache) != sizeof(dpllm_quantized_cache), "their sizes tell them apart");
+  const Ref at(PyObject_GetAttr(o, s_address)), size(PyObject_GetAttr(o, s_size)), b(PyObject_GetAttr(o, s_batch)), device(PyObject_GetAttr(o, s_device));
   void* p = nullptr;
-  int index = -1;
-  if (at.o == nullptr || b.o == nullptr || device.o == nullptr || !PyLong_Check(at.o) || !address(at.o, &p) || p == nullptr || !as_int(b.o, batch) ||
-      !as_int(device.o, &index) || index != place.device)
+  int index = -1, bytes = 0;
+  if (at.o == nullptr || size.o == nullptr || b.o == nullptr || device.o == nullptr || !PyLong_Check(at.o) || !address(at.o, &p) || p == nullptr || !as_int(size.o, &bytes) ||
+      bytes != (int)sizeof(C) || !as_int(b.o, batch) || !as_int(device.o, &index) || index != place.device)
     return false;
   *c = static_cast<const C*>(p);
   return true;
