@@ -7,6 +7,7 @@ import ctypes as C
 import os
 
 import torch
+from torch.autograd import forward_ad
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libdpllm.so")
@@ -230,6 +231,13 @@ def _view(t, what):
     return _Heads(t.data_ptr(), b, n, h)
 
 
+def _no_tangents(*given):
+    """Tensors (or tuples of them, or None) of a call that has a gradient; in forward mode it has none, and would lose what they carry."""
+    for g in given:
+        for t in (g,) if isinstance(g, torch.Tensor) else g or ():
+            _need(t is None or forward_ad.unpack_dual(t).tangent is None, "this call has no derivative in forward mode, but one of the tensors has a tangent")
+
+
 def dpllm_rope_frequencies(rotary_dim, base=10000.0, scaling=DPLLM_ROPE_PLAIN, factor=1.0, trained=0, low=1.0, high=32.0):
     """(angles per position: device, float64 [rotary_dim / 2]; what the rotated part is multiplied by): made once, for dpllm_rope."""
     f, scale = (C.c_double * max(1, rotary_dim // 2))(), C.c_float(0.0)
@@ -240,7 +248,9 @@ def dpllm_rope_frequencies(rotary_dim, base=10000.0, scaling=DPLLM_ROPE_PLAIN, f
 def dpllm_rope(x, positions, freqs, out=None, scale=1.0, layout=DPLLM_ROPE_HALF, inverse=False):
     """x: a tensor [batch][tokens][heads][head_dim], or a tuple of such that share everything but their heads (queries, keys).  positions: int32
     [batch][tokens], or [tokens] for all sequences.  out: where the results go (x itself: in place); new tensors unless given, with x's order of dimensions.
-    New results of tensors that require a gradient have one."""
+    New results of tensors that require a gradient have one (in reverse mode; a tensor with a tangent is refused)."""
+    if forward_ad._current_level >= 0:
+        _no_tangents(x)
     made = _calls.rope(x, positions, freqs, out, scale, layout, inverse)
     if type(made) is not int:
         return made
@@ -460,7 +470,9 @@ def _same_tokens(xs, others, what):
 def dpllm_norm_rope(x, weights, positions=None, freqs=None, eps=1e-6, out=None, scale=1.0, layout=DPLLM_ROPE_HALF):
     """x: a tensor [batch][tokens][heads][head_dim], or a tuple of such that share everything but their heads (queries, keys).  weights: a tensor [head_dim] or [heads][head_dim]
     for each (None: 1), all of one type.  positions, freqs, scale, layout: as for dpllm_rope; freqs None: the norm alone.  out: where the results go (x itself: in place); new tensors
-    unless given.  New results have a gradient with respect to x and the weights."""
+    unless given.  New results have a gradient with respect to x and the weights (in reverse mode; a tensor with a tangent is refused)."""
+    if forward_ad._current_level >= 0:
+        _no_tangents(x, weights)
     made = _calls.norm_rope(x, weights, positions, freqs, eps, out, scale, layout, torch.is_grad_enabled())
     if type(made) is not int:
         return made
@@ -497,6 +509,8 @@ def dpllm_norm_rope_backward_workspace_bytes(heads, weight_strides, batch, token
 def dpllm_norm_rope_backward(x, grads, weights, positions=None, freqs=None, eps=1e-6, out=None, scale=1.0, layout=DPLLM_ROPE_HALF, wanted=None, workspace=None):
     """The gradients of the inputs and of the weights of dpllm_norm_rope from those of its results, grads, as (like x, like weights).  out: where those of the inputs go (grads or x
     themselves, say).  wanted: a truth value for each weight whether its gradient is (all are unless given; the others give None).  workspace: uint8, allocated for the call unless given."""
+    if forward_ad._current_level >= 0:
+        _no_tangents(x, grads, weights)
     if workspace is None:
         made = _calls.norm_rope_backward(x, grads, weights, positions, freqs, eps, out, scale, layout, wanted)
         if type(made) is not int:
