@@ -262,20 +262,26 @@ __device__ __forceinline__ void run_bins(SampleSpace& s, double sum, uint32_t co
   __syncthreads();
 }
 
-// The first bin up to which there are `count` words, or (count 0) a sum of `sum`; the last one with a word if there is none.  s.found, s.before and s.sum_before: what lies in front.
+// The first bin with words up to which there are `count` words, or (count 0) a sum of `sum`; the last one with words if there is none.  s.found, s.before and s.sum_before: what lies in front.
+// A running sum is added up in another order for each bin, so next to one it may be less, or exceed it without a word in between, by their rounding: bins without words are passed over, and the lowest that fits
+// is the one.
 __device__ __forceinline__ void find_bin(SampleSpace& s, uint32_t count, double sum) {
   const int b = threadIdx.x;
+  uint32_t front = 0;
   if (b < kSampleBins) {
-    const uint32_t upto = s.counts[b], front = b == 0 ? 0u : s.counts[b - 1], all = s.counts[kSampleBins - 1];
-    const double s_upto = s.sums[b], s_front = b == 0 ? 0.0 : s.sums[b - 1];
-    const bool here = count > 0 ? upto >= count : s_upto >= sum, there = b > 0 && (count > 0 ? front >= count : s_front >= sum);
-    const bool last = upto == all && front < all;      // (rounding may leave a sum short of its whole)
-    const bool none = count > 0 ? all < count : s.sums[kSampleBins - 1] < sum;
-    if (none ? last : here && !there) {
-      s.found = b;
-      s.before = (int)front;
-      s.sum_before = s_front;
-    }
+    const uint32_t upto = s.counts[b], all = s.counts[kSampleBins - 1];
+    front = b == 0 ? 0u : s.counts[b - 1];
+    const uint64_t fits = __ballot(upto > front && (upto == all || (count > 0 ? upto >= count : s.sums[b] >= sum)));
+    if ((b & 63) == 0) s.wave_counts[b >> 6] = fits == 0 ? kSampleBins - 1 : b + __builtin_ctzll(fits);
+  }
+  __syncthreads();
+  uint32_t first = kSampleBins - 1;
+#pragma unroll
+  for (int w = 0; w < kSampleBins / 64; ++w) first = min(first, s.wave_counts[w]);
+  if (b == (int)first) {
+    s.found = b;
+    s.before = (int)front;
+    s.sum_before = b == 0 ? 0.0 : s.sums[b - 1];
   }
   __syncthreads();
 }
@@ -455,7 +461,7 @@ struct Sampler {
       }
       const unsigned long long w = few[found];
       __syncthreads();
-      // (rounding between two ways to the same sum may leave none of these: then the cut is in front of the first)
+      // (rounding between two ways to the same sum may leave none of these, as what is left of it may come to nothing or less: then the cut is in front of the first)
       if (s.length == taken) return {from_key(~(uint32_t)(w >> 32)), -1};
       return {from_key(~(uint32_t)(w >> 32)), (int)(uint32_t)w};
     }
