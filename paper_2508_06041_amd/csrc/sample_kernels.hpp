@@ -9,7 +9,8 @@
 // steps).  Steps of a 32nd do not help: the many words of a flat row are far below its top.
 //
 // Answers are whole numbers, so sums are kept in 64 bits and in whole numbers where workgroups' order could show: a word of step b counts 1 and the
-// 2^-40ths by which e 2^((b + 1) / 8) exceeds 1, both in one 64-bit addition in LDS.  Rounding that to 2^-41 moves a sum by less than 1e-12 of itself.
+// 2^-40ths by which e 2^(b / 8) is below 1, both in one 64-bit addition in LDS.  Rounding that to 2^-41 moves a sum by less than 1e-12 of itself, and the sum of words as large as the largest, of which there
+// may be nothing else, not at all: each counts 1.
 #pragma once
 #include "verify_kernels.hpp"
 
@@ -41,10 +42,10 @@ struct SampleArgs {
 };
 
 // Where a word lies.  y = 2^19 - t, t the 256ths of a power of two by which e is below 1, so that the upper word of y has all whole numbers in it and its last bits count 2^-34: an error of 8e-14 of
-// e.  Step b is t in (32 b, 32 (b + 1)], the first with 0; r = y - floor(y) is what is left to the next whole t, and with the five bits of y above that to the step's end: e is the step's least e times
-// 2^(bits / 256) 2^(r / 256).  1 + c1 r + c2 r^2 + c3 r^3 is the last of these to 2e-14.  A dozen instructions in 64 bits; with the series of the whole exponent they were 30,
+// e.  Step b is t in (32 b, 32 (b + 1)], the first with 0; r = y - floor(y) is what is left to the next whole t, and with the five bits of y above that to the step's end: e is the step's first e, 2^(-b / 8), times
+// 2^((bits - 32) / 256) 2^(r / 256).  1 + c1 r + c2 r^2 + c3 r^3 is the last of these to 2e-14.  A dozen instructions in 64 bits; with the series of the whole exponent they were 30,
 // and the histograms of 64 rows of 128256 words took 14 us, now 11.
-constexpr int kSampleTable = 32;      // 2^40 2^(j / 256)
+constexpr int kSampleTable = 32;      // 2^40 2^((j - 32) / 256)
 struct Steps {
   float top;
   double steps;      // 256 / (temperature ln 2)
@@ -56,7 +57,7 @@ struct Steps {
   }
   // Its step; kSampleBins or more: it is left out (as are NaN and minus infinity).
   __device__ __forceinline__ static int bin(double y) { return (int)((~(uint32_t)(__builtin_bit_cast(uint64_t, y) >> 32) & 0xfffffu) >> 7); }
-  // e by the least of its step, times 2^40 w, plus c
+  // e by the first of its step, times 2^40 w, plus c
   __device__ __forceinline__ double share(double y, double w, double c) const {
     const double r = __builtin_amdgcn_fract(y);
     double f = __builtin_fma(r, 3.312607527945956e-09, 3.6655631008313955e-06);
@@ -64,16 +65,16 @@ struct Steps {
     f = __builtin_fma(f, r, 1.0);
     return __builtin_fma(f, table[(uint32_t)(__builtin_bit_cast(uint64_t, y) >> 34) & (kSampleTable - 1)] * w, c);
   }
-  // That less 1, in 2^-40ths, to the nearest.
-  __device__ __forceinline__ unsigned long long excess(double y) const {
-    return __builtin_bit_cast(uint64_t, share(y, 1.0, 0x1p52 - 0x1p40)) & ((1ull << 52) - 1);
+  // What that is below 1, in 2^-40ths, to the nearest; that of the largest logit, whose y is 2^-34 short of 2^19, is 0.
+  __device__ __forceinline__ unsigned long long lack(double y) const {
+    return __builtin_bit_cast(uint64_t, share(y, -1.0, 0x1p52 + 0x1p40)) & ((1ull << 52) - 1);
   }
 };
 // Fills the table; a barrier has to follow.
 __device__ __forceinline__ void fill_steps(double* table) {
-  if (threadIdx.x < kSampleTable) table[threadIdx.x] = 0x1p40 * exp_of((int)threadIdx.x * 0.0027076061740622863);      // ln 2 / 256
+  if (threadIdx.x < kSampleTable) table[threadIdx.x] = 0x1p40 * exp_of(((int)threadIdx.x - kSampleTable) * 0.0027076061740622863);      // ln 2 / 256
 }
-__device__ __forceinline__ double base_of(int bin) { return exp_of(-0.086643397569993164 * (bin + 1)); }      // the least e of a step: ln 2 / 8
+__device__ __forceinline__ double base_of(int bin) { return exp_of(-0.086643397569993164 * bin); }      // the first e of a step, which none of its is above: ln 2 / 8
 __device__ __forceinline__ float larger(float x, float y) { return fmaxf(x, y); }
 __device__ __forceinline__ int smaller(int x, int y) { return min(x, y); }
 
@@ -192,7 +193,7 @@ __global__ void __launch_bounds__(kVerThreads) sample_bins_kernel(const SampleAr
 #pragma unroll
                   for (int e = 0; e < Chunk<T>::E; ++e) {
                     const double y = steps.place((float)v[e]);
-                    if (steps.bin(y) < kSampleBins) atomicAdd(&bins[steps.bin(y)], (1ull << kCountShift) + steps.excess(y));
+                    if (steps.bin(y) < kSampleBins) atomicAdd(&bins[steps.bin(y)], (1ull << kCountShift) + steps.lack(y));
                   }
                 });
   __syncthreads();
@@ -225,7 +226,7 @@ struct Narrow {
 struct SampleSpace {
   unsigned long long list[kSampleList];     // ~key << 32 | number
   unsigned long long chunks[kSampleChunks];
-  double base[kSampleBins];                 // the least e of a bin, in 2^-40ths
+  double base[kSampleBins];                 // the first e of a bin, in 2^-40ths
   double table[kSampleTable];
   double sums[kSampleBins];                 // running, over bins
   uint32_t counts[kSampleBins];
@@ -414,7 +415,7 @@ struct Sampler {
         const double y = steps.place(x);
         if (inside(x, y)) {
           atomicAdd(&s.fine_counts[(high - Key::of(x)) >> shift], 1u);
-          atomicAdd(&s.fine[(high - Key::of(x)) >> shift], steps.excess(y));
+          atomicAdd(&s.fine[(high - Key::of(x)) >> shift], steps.lack(y));
         }
       };
       if (listed > 0)
@@ -423,7 +424,7 @@ struct Sampler {
         words_between<T>(row, a.vocabulary, Key::back(low), Key::back(high), [&](float x, int) { add(x); });
       __syncthreads();
       const int i = min((int)threadIdx.x, kSampleBins - 1);
-      run_bins(s, base * ((double)s.fine_counts[i] * 0x1p40 + (double)s.fine[i]), s.fine_counts[i]);
+      run_bins(s, base * ((double)s.fine_counts[i] * 0x1p40 - (double)s.fine[i]), s.fine_counts[i]);
       find_bin(s, count > 0 ? count - taken : 0u, sum - taken_sum);
       taken += s.before;
       taken_sum += s.sum_before;
@@ -614,25 +615,25 @@ __global__ void __launch_bounds__(kSampleThreads) sample_choose_kernel(const Sam
     fill_steps(s.table);
     const int b = threadIdx.x & (kSampleBins - 1), half = threadIdx.x / kSampleBins;
     uint32_t count = 0;
-    unsigned long long more = 0;
+    unsigned long long less = 0;
 #pragma unroll 4
     for (int c = half; c < a.chunks; c += 2) {
       const unsigned long long w = bins[(int64_t)c * kSampleBins + b];
       count += (uint32_t)(w >> kCountShift);
-      more += w & kMask;
+      less += w & kMask;
     }
     if (half == 1) {
-      s.fine[b] = more;
+      s.fine[b] = less;
       s.fine_counts[b] = count;
     }
     __syncthreads();
     if (half == 0) {
-      more += s.fine[b];
+      less += s.fine[b];
       count += s.fine_counts[b];
     }
     const double base = 0x1p-40 * base_of(b);
     if (half == 0) s.base[b] = base;
-    run_bins(s, base * ((double)count * 0x1p40 + (double)more), half == 0 ? count : 0u);
+    run_bins(s, base * ((double)count * 0x1p40 - (double)less), half == 0 ? count : 0u);
   }
   const int total = (int)s.counts[kSampleBins - 1];
   const double whole = s.sums[kSampleBins - 1];
@@ -731,7 +732,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_choose_kernel(const Sam
       any = any || (64 * j + lane >= near && 64 * j + lane <= far && w[j] != 0);
       if (64 * j + lane >= near) continue;
       kept += (int)(w[j] >> kCountShift);
-      sum += s.base[64 * j + lane] * ((double)(w[j] >> kCountShift) * 0x1p40 + (double)(w[j] & kMask));
+      sum += s.base[64 * j + lane] * ((double)(w[j] >> kCountShift) * 0x1p40 - (double)(w[j] & kMask));
     }
     if (!held && __any(any))
       each_piece<T>(from, a.vocabulary, c * Chunk<T>::kElements - Chunk<T>::lead(from), Chunk<T>::kElements / Chunk<T>::E, lane, 64, [&](const typename Piece<T>::type& v, int i) {
