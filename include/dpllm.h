@@ -369,7 +369,7 @@ int dpllm_norm_rope_backward(const dpllm_heads* x, const dpllm_heads* grads, con
  *   INT8  a byte each, -127 ... 127, round(127 x / the largest size); the word is a float, the largest size / 127
  *   INT4  half a byte each, element 2i in the lower half of byte i: bit 3 the sign, m below, for offset +- scale (m + 1/2).  The word is two bfloat16: the scale in the lower
  *         half, the offset in the upper.  offset = (lowest + highest) / 2; scale = an eighth of the larger distance of those from it, rounded up, or 0 where they are equal;
- *         a value is at floor((x - offset) / scale), within -8 ... 7
+ *         a value is at floor((x - offset) / scale), within -8 ... 7.  (Where offset or scale are past the largest bfloat16, which only floats next to the largest come to, the head is held as NaN.)
  * Sizes (and distances) below 2^-100 that are not 0 count as 2^-100.  A head with a value that is no finite number is held as NaN.
  * Strides of codes are in bytes, those of scales in words, the same for keys and values; the codes of a head lie side by side. */
 #define DPLLM_CACHE_E4M3 1
@@ -393,7 +393,7 @@ int dpllm_quantized_append(const dpllm_quantized_cache* cache, int first_layer, 
 
 /* What the cache holds of tokens first[b] ... + tokens - 1 of every sequence, for n_layers layers from first_layer on, into k_out and v_out: [layers][batch][tokens][heads][head_dim]
  * of `dtype`, layers k_layer_stride and v_layer_stride elements apart.  first_dev NULL: from token 0 on.  count_dev NULL: all of them, else those from count[b] on are written as zeros, as are
- * tokens that no page holds (those in front of token 0 among them).  Values are products (and sums) in 32 bits, rounded once more for the shorter types.
+ * tokens that no page holds (those in front of token 0 among them).  Values are products (and sums), formed in 32 bits or exactly and rounded to dtype.
  * Errors: EINVAL, ESHAPE, ERANGE (layers), EHIP. */
 int dpllm_quantized_read(const dpllm_quantized_cache* cache, int first_layer, int n_layers, int batch, int tokens, const int32_t* first_dev, const int32_t* count_dev,
                          int dtype, const dpllm_heads* k_out, int64_t k_layer_stride, const dpllm_heads* v_out, int64_t v_layer_stride, void* stream);

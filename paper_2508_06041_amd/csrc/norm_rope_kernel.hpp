@@ -182,8 +182,8 @@ __device__ __forceinline__ void met() {      // LDS that a wavefront's lanes hav
 
 // A wavefront takes a token and heads_each of its heads, a group of `lanes` lanes a head; so token, position and tensor are the same for a wavefront and what depends on them is done once, by scalar
 // instructions.  ONE: a head has no more units than lanes, is read once, and kNormAtOnce heads of a group are on their way; else it is read again behind its sum.
-// Bound by memory: 156 MB of three prompts of 2111 tokens, 40 + 8 heads of 128, in 34.4 us, 4.5 TB/s (a copy has 5.1).  With workgroups that took a few tokens' heads in turn, addresses and sines made
-// lane by lane, it was 48 us.  One token takes 4 us of latency (position, sines, one head).
+// Bound by memory: 156 MB of three prompts of 2111 tokens, 40 + 8 heads of 128, in 29 us, 5.4 TB/s (a copy has 5.1; a call in a loop over other inputs each time 36.6).  With workgroups that took a few tokens' heads in turn,
+// addresses and sines made lane by lane, it took 48 where this took 34.  One token takes 4 us of latency (position, sines, one head).
 constexpr int kNormAtOnce = 2;
 template <typename T, int E, bool HALF, bool ONE>
 __global__ void __launch_bounds__(kNormThreads) norm_rope_kernel(const NormArgs a) {
@@ -285,7 +285,7 @@ struct NormBackArgs {
 };
 
 // A workgroup takes a stretch of tokens of a set of heads, its wavefronts every fourth token: a lane has the same elements of the same weight throughout and adds its gradient up in registers (in LDS
-// where a lane has several units).  252 MB of 4 sequences of 2049 tokens, 32 + 8 heads of 128, in 57 us, 4.4 TB/s, the join's 4.5 us among them; memory and instructions (300 to a head's step) both near
+// where a lane has several units).  252 MB of 4 sequences of 2049 tokens, 32 + 8 heads of 128, in 52 us and 5 to join, 4.4 TB/s in all (a call in a loop 64); memory and instructions (300 to a head's step) both near
 // their bounds: 73 us before roots, sums and loads were freed of branches.  Wavefronts and groups of lanes meet in LDS at the end, in their order, so the sum does not change from run to run.
 template <typename T, int E, bool HALF, bool ONE>
 __global__ void __launch_bounds__(kNormThreads) norm_rope_backward_kernel(const NormBackArgs k) {

@@ -52,8 +52,8 @@ __device__ __forceinline__ Codes<N> load_codes(const char* p) {
   return c;
 }
 
-// 16 bytes of a token.  Heads that fill whole lines of 128 bytes are read once and need not stay in the caches (400000 tokens of 8 heads of 128 e4m3 codes, 845 MB: 187 us with them,
-// 168 past them); others share their lines with a neighbour, which is to find them there (in 4 bits 143 against 157).
+// 16 bytes of a token.  Heads that fill whole lines of 128 bytes are read once and need not stay in the caches (400000 tokens of 8 heads of 128 e4m3 codes, 845 MB: 159 us with them,
+// 139 past them); others share their lines with a neighbour, which is to find them there (heads of 64: 95 us against 102 past them, in 4 bits 82 against 94).
 template <bool ONCE>
 __device__ __forceinline__ u32x4 load_piece(const char* p) {
   const u32x4* at = reinterpret_cast<const u32x4*>(p);
@@ -864,7 +864,7 @@ __global__ void __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) quantized_attent
     __syncthreads();
     u32x4 x[U], y[U];
     load(first, x);
-    constexpr bool TWO = FORMAT != kInt4 || D < 128;      // two steps of loads are on their way, if there are registers for them (52 rows: 116 us, 127 with one)
+    constexpr bool TWO = FORMAT != kInt4 || D < 128;      // two steps of loads are on their way, if there are registers for them (100 rows in 8 bits 154 us, with one 162)
     if (TWO) load(first + 1, y);
     keep(first, x);
     __syncthreads();

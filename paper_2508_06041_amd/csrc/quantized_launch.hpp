@@ -14,8 +14,9 @@ struct QuantizedPlan : AttentionPlan {
 inline QuantizedPlan plan_quantized(int batch, int nodes, int heads, int kv_heads, int head_dim, int64_t max_len) {
   QuantizedPlan p{};
   p.rows = nodes * (heads / kv_heads);
-  // up to 64 rows go to wavefronts that take every step of codes apart by themselves, two tiles of rows at most to each (52 rows over 65001 tokens, 4 sequences, int4: 96 us; the kernel that shares
-  // that 116), more to the kernel that shares it (100 rows, int8: 99 against 123; 240 rows, e4m3: 138 against 166)
+  // Up to 64 rows go to wavefronts that take every step of codes apart by themselves, two tiles of rows at most to each, more to the kernel that shares that.  us with the former / with the latter, 4 sequences of
+  // 9000 to 65001 tokens, heads of 128 (of 64): 36 to 64 rows, for which half the wavefronts of the latter have no rows, e4m3 106 / 134 (64 / 96), int8 112 / 139 (69 / 98), int4 93 / 144 (76 / 118); 100 rows e4m3
+  // 175 / 148 (97 / 104), int8 187 / 149 (110 / 107), int4 156 / 156 (126 / 122).  (68 rows of int4 are past where they should be, 129 / 149; 240 rows over two sequences 134 to 154 / 126 to 133.)
   p.waves = p.rows <= 64 || head_dim == 256 ? 0 : p.rows <= 128 ? 4 : 8;
   p.mt = head_dim == 256 || p.rows <= 16 ? 1 : 2;
   p.tile = 16 * p.mt * std::max(p.waves, 1);

@@ -3,7 +3,7 @@
 // says in which step of it a cut lies.  If the words up to there are at most one to a thread of a workgroup, those are sorted and the rest is not looked at again; else only the words of
 // that step are.
 //
-// One row of 32000 words with all three cuts takes 3.2 + 6.9 + 10.6 us (tops, histograms, choice), 64 rows of 128256 in bf16 with every kind of cut 5.8 + 11.7 + 50.  The choice is one workgroup's
+// One row of 32000 words with all three cuts takes 3.2 + 6.8 + 10.8 us (tops, histograms, choice), 64 rows of 128256 in bf16 with every kind of cut 5.7 + 11.3 + 53.5.  The choice is one workgroup's
 // work and bound by what that can do: a walk over a row of 128256 words takes it 7 us and more with much to do on the way, so the shorter way (32 us for the one row without it) and what is kept in
 // LDS count (the 64 rows: 71 where the words of a step were sorted 2048 at a time and looked for in the row again).  Up to 512 words are sorted by counting each one's place (64: 4 us less than in
 // steps).  Steps of a 32nd do not help: the many words of a flat row are far below its top.

@@ -107,7 +107,7 @@ struct NormSplit {
   int splits[kNormTensors], first[kNormTensors + 1], set_heads[kNormTensors], own[kNormTensors], weights_end[kNormTensors];
   int64_t tokens_each[kNormTensors], parts_at[kNormTensors], parts;
 };
-constexpr int kNormGroups = 1280;      // five to a compute unit, as many as registers allow: 57 us for the gradient of 4 sequences of 2049 tokens, 32 + 8 heads of 128; 1024: 58, 1536: 64, 2048: 61
+constexpr int kNormGroups = 1280;      // five to a compute unit, as many as registers allow: 57 us (with the join) for the gradient of 4 sequences of 2049 tokens, 32 + 8 heads of 128; 1024: 58, 1536: 64, 2048: 61
 NormSplit split_norm(const int* heads, const int64_t* weight_strides, int tensors, int64_t all, int teams) {
   NormSplit s{};
   int64_t all_heads = 0;
